@@ -168,7 +168,7 @@ def prepare(case, seed):
         import paper_2608_23144_gb300 as aw
         s["cache"] = aw.awsrc_kv_cache(k, v, k_exp, v_exp)
         s["batch"] = aw.awsrc_kv_batch(s["q_start"], s["kv_len"], table, n, s["max_new"], s["max_kv"])
-        s["ws"] = aw.awsrc_attention_workspace(s["cache"], s["batch"], H)
+        s["ws"] = aw.awsrc_attention_workspace(s["cache"], H)
     return s
 
 
@@ -176,11 +176,11 @@ def run(s):
     if own:
         import paper_2608_23144_gb300 as aw
         if s["case"]["op"] == "append":
-            aw.awsrc_kv_append(s["cache"], s["batch"], s["q"], s["k"], s["v"], s["cos"], s["sin"],
-                               interleaved=s["case"]["interleaved"], q_out=s["out"], workspace=s["ws"])
+            aw.awsrc_kv_append(s["cache"], s["batch"], s["q"], s["k"], s["v"], s["cos"], s["sin"], s["ws"],
+                               interleaved=s["case"]["interleaved"], q_out=s["out"])
             return {"q": s["out"], "k": s["k_cache"], "v": s["v_cache"], "k_exp": s["k_exp"], "v_exp": s["v_exp"]}
-        aw.awsrc_paged_attention(s["cache"], s["batch"], s["q"], sm_scale=s["sm_scale"], out=s["out"], lse=s["lse"],
-                                 workspace=s["ws"])
+        aw.awsrc_paged_attention(s["cache"], s["batch"], s["q"], s["ws"], sm_scale=s["sm_scale"], out=s["out"],
+                                 lse=s["lse"])
         return {"out": s["out"], "lse": s["lse"]}
     return plain_append(s) if s["case"]["op"] == "append" else plain_attention(s)
 
