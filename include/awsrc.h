@@ -482,6 +482,123 @@ awsrc_status awsrc_packed_gemv_batch(const awsrc_params* prm, int32_t n_mod, con
                                      int32_t n_task, const awsrc_gemv_task* tasks, const void* sidecar,
                                      size_t sidecar_bytes, int32_t M, void* stream);
 
+/* ------------------------------------------------- paged 8-bit KV cache -- */
+
+/*
+ * Between the packed products of a layer: the keys and values of past tokens in
+ * a paged cache held in 8 bits, and attention over it. The paper has neither;
+ * both are this library's serving extension.
+ *
+ * Cache. n_pages pages of `page` tokens; a block is (page, kv head). Codes are
+ * e4m3 (1 sign, 4 exponent, 3 fraction bits, bias 7, largest 448); a block has
+ * one power-of-two scale 2^e for its keys and one for its values, in the
+ * convention of the records' POW2 scales: e = smallest integer with
+ * amax <= 448 * 2^e, at least -32; a code stands for code * 2^e. An exponent of
+ * -128 marks a block that received a non-finite value or one above 448 * 2^31:
+ * it stands for NaN. Byte layout (operand order of the tensor cores: the
+ * reduced axis in runs of 16 bytes):
+ *   k      [n_pages][n_kv_heads][head_dim / 16][page][16]  (16 dims of a token)
+ *   v      [n_pages][n_kv_heads][page / 16][head_dim][16]  (16 tokens of a dim)
+ *   k_exp, v_exp  [n_pages][n_kv_heads] int8
+ *   page       16, 32, 64 or 128;  head_dim  64 or 128.
+ *   k, v       device, 16-byte aligned.
+ */
+typedef struct awsrc_kv_cache {
+  int32_t n_pages, page, n_kv_heads, head_dim;
+  uint8_t* k;
+  uint8_t* v;
+  int8_t* k_exp;
+  int8_t* v_exp;
+} awsrc_kv_cache;
+
+/*
+ * The sequences of one step. Sequence b has the q_start[b + 1] - q_start[b]
+ * newest of its kv_len[b] tokens in this call (rows q_start[b] .. of q, k, v;
+ * none is allowed); token p of it lies in page page_table[b * table_stride +
+ * p / page], row p % page. The arrays are read on the device, so that a
+ * captured graph follows their contents.
+ *   n_tok    rows of q, k and v (q_start[n_seq]); 0 makes every call a no-op.
+ *   max_new, max_kv  the largest number of new tokens and kv_len the arrays may
+ *            hold: they choose launch shapes. Results stay right for larger
+ *            contents, only slower.
+ * Entries that cannot be right (q_start outside [0, n_tok] or falling,
+ * kv_len < new tokens or beyond the table's row, a page outside the cache) are
+ * skipped and reported as bit 3 (8) of awsrc_workspace_status.
+ */
+typedef struct awsrc_kv_batch {
+  int32_t n_seq, n_tok, max_new, max_kv, table_stride, pad_;
+  const int32_t* q_start;     /* n_seq + 1 */
+  const int32_t* kv_len;      /* n_seq, the new tokens included */
+  const int32_t* page_table;  /* n_seq x table_stride */
+} awsrc_kv_batch;
+
+/* Rows [n_tok][heads][head_dim] of dtype F32 or BF16: element (t, h, d) at
+ * t * tok_stride + h * head_stride + d (elements). Any strides; 16-byte aligned
+ * rows and strides are read in vectors. */
+typedef struct awsrc_rows {
+  void* p;
+  int64_t tok_stride, head_stride;
+  int32_t dtype, pad_;
+} awsrc_rows;
+
+/*
+ * awsrc_attention_workspace_bytes — device bytes of the workspace that
+ * awsrc_kv_append (its fault word) and awsrc_paged_attention (partial results
+ * of sequences shared among blocks) use; one workspace serves any batch of this
+ * cache on one stream. Host-only.
+ * awsrc_attention_workspace_init — makes a new workspace usable (clears the
+ * fault word and the arrival counters, which every call leaves cleared). Once
+ * per workspace. The fault word of these calls accumulates until
+ * awsrc_workspace_status reads and clears it.
+ * Errors: INVALID_ARG, SHAPE, WORKSPACE, CUDA.
+ */
+awsrc_status awsrc_attention_workspace_bytes(const awsrc_kv_cache* cache, int32_t n_heads, size_t* bytes);
+awsrc_status awsrc_attention_workspace_init(const awsrc_kv_cache* cache, int32_t n_heads, void* workspace,
+                                            size_t workspace_bytes, void* stream);
+
+/*
+ * awsrc_kv_append — writes the batch's new keys and values into the cache and
+ * rotates q and k by position on the way. Token at position p, pairs
+ * i < rotary_dim / 2: (x1, x2) = dims (i, i + rotary_dim / 2), or (2i, 2i + 1)
+ * when interleaved; x1' = x1 cos[p][i] - x2 sin[p][i], x2' = x2 cos[p][i] +
+ * x1 sin[p][i] in binary32, every operation rounded; the other dims pass
+ * unchanged. q_out = the rotated q rounded to its dtype (q_out may be q).
+ * A block's exponent becomes e = max(e_old, e(amax of its new tokens)); e_old
+ * counts only when the page already held tokens of the sequence (its first new
+ * row is not 0). Codes are x * 2^-e rounded to nearest even; when e grows, the
+ * block's older codes become code * 2^(e_old - e), rounded the same way (exact
+ * but for codes that leave e4m3's normal range). A block whose exponent is -128
+ * stays so until its page is written from row 0 again; its new codes are 0.
+ *   n_heads    query heads, a multiple of n_kv_heads; q, q_out [n_tok][n_heads].
+ *   k, v       [n_tok][n_kv_heads]; q, k, v and q_out share a dtype.
+ *   cos, sin   device, rope_rows x rotary_dim / 2 floats (NULL when rotary_dim
+ *              is 0); a token at p >= rope_rows is skipped and reported.
+ * A page that takes new tokens must belong to one sequence of the batch.
+ * Bit-reproducible. Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA.
+ */
+awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const awsrc_kv_batch* batch, int32_t n_heads,
+                             const awsrc_rows* q, const awsrc_rows* k, const awsrc_rows* v,
+                             const awsrc_rows* q_out, const float* cos, const float* sin, int32_t rope_rows,
+                             int32_t rotary_dim, int32_t interleaved, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/*
+ * awsrc_paged_attention — for query i of a sequence (position p = kv_len - new
+ * + i) and query head h, over the cached tokens j of kv head
+ * h / (n_heads / n_kv_heads): s_j = sm_scale * q . k_j for j < kv_len and, when
+ * causal, j <= p; out = sum_j softmax(s)_j v_j, lse = log sum_j exp(s_j). A query
+ * that sees no token gets out = 0, lse = -inf.
+ *   q, out   [n_tok][n_heads], the same dtype (out must not overlap q).
+ *   lse      device, n_tok x n_heads floats, or NULL.
+ * F32 keeps q and the softmax weights in two binary16 terms (22 bits) each and
+ * sums in binary32. BF16 keeps q exact and the weights in 8 bits or more; out is
+ * rounded once. Sums run in a fixed order: results repeat bit for bit.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA.
+ */
+awsrc_status awsrc_paged_attention(const awsrc_kv_cache* cache, const awsrc_kv_batch* batch, int32_t n_heads,
+                                   const awsrc_rows* q, const awsrc_rows* out, float* lse, float sm_scale,
+                                   int32_t causal, void* workspace, size_t workspace_bytes, void* stream);
+
 /*
  * awsrc_workspace_status — synchronises `stream`, then reads and clears the
  * device fault word kept in the first bytes of an encode/select/decode
@@ -493,6 +610,8 @@ awsrc_status awsrc_packed_gemv_batch(const awsrc_params* prm, int32_t n_mod, con
  *            (for its codes) gave a different gain than the search found
  *            (never expected).
  * Bit 2 (4): a bounded wait inside a kernel gave up (never expected).
+ * Bit 3 (8): a paged-cache batch held an entry that cannot be right (skipped).
+ *            The paged-cache calls do not clear the word when they start.
  */
 awsrc_status awsrc_workspace_status(void* workspace, void* stream, uint32_t* flags);
 

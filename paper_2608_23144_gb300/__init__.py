@@ -55,3 +55,13 @@ from ._binding import (  # noqa: F401
     module_array,
     params,
 )
+from ._paged import (  # noqa: F401
+    KvBatch,
+    KvCache,
+    awsrc_attention_workspace,
+    awsrc_kv_append,
+    awsrc_kv_batch,
+    awsrc_kv_cache,
+    awsrc_kv_cache_alloc,
+    awsrc_paged_attention,
+)

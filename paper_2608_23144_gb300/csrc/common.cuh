@@ -25,6 +25,7 @@ constexpr int kMaxModsPerLaunch = 16;
 constexpr uint32_t kFaultRecord = 1u;     // decoder: record names a tile/seed out of range
 constexpr uint32_t kFaultSelfCheck = 2u;  // encoder: the winner's recomputation disagrees with the search
 constexpr uint32_t kFaultTimeout = 4u;    // a bounded wait gave up
+constexpr uint32_t kFaultBatch = 8u;      // paged cache: a batch entry that cannot be right (skipped)
 constexpr size_t kStatusBytes = 256;
 
 // Host-validated parameters plus derived constants, passed by value.

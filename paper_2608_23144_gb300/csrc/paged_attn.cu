@@ -1,0 +1,567 @@
+// paged_attn.cu — attention of a few query rows per kv head over the paged 8-bit
+// cache: decode steps, drafts, and every case the tensor-memory kernel does not
+// take.
+//
+// Mathematics, per kv head with scores in base 2: x_j = (q . k_j) 2^(ek_j)
+// sm_scale log2(e) + ev_j, where 2^ek, 2^ev are the block scales of the codes.
+// With m = max x, p_j = 2^(x_j - m + 15): O = sum p_j c_j over the value codes
+// c_j and l = sum p_j 2^-ev_j give out = O / l and lse = (m - 15 + log2 l) ln 2.
+// Putting 2^ev into the exponent leaves the codes to the tensor cores as they
+// are (exact in binary16) and keeps p at most 2^15.
+//
+// Rows are query tokens x the query heads that share a kv head. Both products
+// run transposed, tokens (or dims) as the 16 MMA rows and 8 query rows as the
+// columns, so that a decode step of up to 8 heads per kv head wastes nothing.
+// F32 splits q (scaled by a power of two per row) and p into two binary16 terms;
+// the second term costs one more MMA on the same codes.
+//
+// Bound by the cache's bytes when rows are few. A warp takes 64 tokens at a
+// time: its lanes read 16-byte runs straight into MMA fragments (the cache's
+// byte order is chosen for that), the order of tokens and dims inside the
+// fragments being free as long as both operands agree.
+//
+// Work: the (sequence, row tile, kv head, 64-token block) units of the batch in
+// this order are dealt out in equal contiguous shares to the thread blocks,
+// whatever the lengths. A tile that several blocks share is joined by the last
+// one to arrive, in block order, from partial results in the workspace; nothing
+// waits.
+#include "internal.h"
+#include "kv_paged.cuh"
+
+namespace awsrc {
+
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kWarps = kThreads / 32;
+constexpr int kUnit = 64;         // tokens per unit
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kPBits = 15.0f;   // p is at most 2^15
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Transposes an 8 x 8 tile of binary16 held two columns per lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 half2_floats(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+
+__device__ __forceinline__ uint4 ldg16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+
+// 16 codes -> A-fragment words: f[2i] the first pair of word i, f[2i + 1] the second.
+__device__ __forceinline__ void widen(const uint4& v, uint32_t* f) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = e4m3x2_half2(w[i] & 0xFFFFu);
+    f[2 * i + 1] = e4m3x2_half2(w[i] >> 16);
+  }
+}
+
+// A word whose first n bytes are ones.
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (n <= 0 ? 0u : (1u << (8 * n)) - 1u); }
+
+template <typename T>
+__device__ __forceinline__ float elem(const T* p);
+template <>
+__device__ __forceinline__ float elem(const float* p) { return __ldg(p); }
+template <>
+__device__ __forceinline__ float elem(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+
+// A row tile of one sequence and its unit count per kv head.
+struct Tile {
+  int b, t;        // sequence, row tile
+  KvSeq s;
+  int blocks;      // 64-token blocks that some row of the tile sees, at least 1
+};
+
+// Tokens the last row of tile t sees.
+__device__ __forceinline__ int tile_tokens(const AttnArgs& a, const KvSeq& s, int t, int tile_rows) {
+  if (!a.causal) return s.kv;
+  const int last = min((t + 1) * tile_rows, s.n * a.c.group) - 1;
+  return s.kv - s.n + last / a.c.group + 1;
+}
+__device__ __forceinline__ int tile_blocks(const AttnArgs& a, const KvSeq& s, int t, int tile_rows) {
+  return max(1, (tile_tokens(a, s, t, tile_rows) + kUnit - 1) / kUnit);
+}
+__device__ __forceinline__ int seq_tiles(const AttnArgs& a, const KvSeq& s, int tile_rows) {
+  return s.n > 0 ? (s.n * a.c.group + tile_rows - 1) / tile_rows : 0;
+}
+__device__ int64_t seq_units(const AttnArgs& a, const KvSeq& s, int tile_rows) {
+  const int nt = seq_tiles(a, s, tile_rows);
+  int64_t u = 0;
+  for (int t = 0; t < nt; ++t) u += tile_blocks(a, s, t, tile_rows);
+  return u * a.c.kv_heads;
+}
+
+// Inclusive sum over the block of one value per thread; *all its total.
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* all) {
+  __shared__ int64_t wsum[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();  // an earlier call's readers are done
+  if (lane == 31) wsum[warp] = x;
+  __syncthreads();
+  int64_t t = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) x += wsum[w];
+    t += wsum[w];
+  }
+  *all = t;
+  return x;
+}
+
+// Thread-block-wide state of the walk over units.
+struct Walk {
+  int64_t chunk;         // units per block
+  int64_t tile_first;    // first unit of (tile, head 0)
+  Tile tl;
+};
+
+template <int NT, int WR>
+struct Shape {
+  static constexpr int kRowsPerWarp = 8 * NT;
+  static constexpr int kRows = kRowsPerWarp * WR;  // query rows of a tile
+  static constexpr int kTokWarps = kWarps / WR;    // warps that share the tokens of a row group
+};
+
+template <int D>
+struct RowStride { static constexpr int value = D + 4; };  // floats of a row in shared memory
+
+// Element d of row r of a finished tile, and its lse.
+template <typename T, int D>
+__device__ __forceinline__ void write_final(const AttnArgs& a, const Tile& tl, int h, int tile_rows, int r, int d,
+                                            float o, float m, float l) {
+  const int row = tl.t * tile_rows + r;
+  const int tok = tl.s.first + row / a.c.group, head = h * a.c.group + row % a.c.group;
+  const float v = l == 0.0f ? 0.0f : __fdiv_rn(o, l);
+  T* p = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.ts + (int64_t)head * a.out.hs + d;
+  if constexpr (sizeof(T) == 2)
+    *p = __float2bfloat16_rn(v);
+  else
+    *p = v;
+  if (d == 0 && a.lse)
+    a.lse[(int64_t)tok * a.c.n_heads + head] = l == 0.0f ? -INFINITY : (m - kPBits + log2f(l)) * kLn2;
+}
+
+template <typename T, int D, int NT, int WR>
+__global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+  using S = Shape<NT, WR>;
+  constexpr bool kSplit = sizeof(T) == 4;
+  constexpr int kTerms = kSplit ? 2 : 1;
+  constexpr int kC = D / 64;           // 16-byte runs of a token's dims per lane
+  constexpr int kStride = RowStride<D>::value;
+  __shared__ float so[S::kTokWarps][S::kRows][kStride];
+  __shared__ float sm[S::kTokWarps][S::kRows], sl[S::kTokWarps][S::kRows];
+  __shared__ int last_flag;
+  __shared__ int64_t s_seq[2];
+  const KvArgs& c = a.c;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int g = lane >> 2, t4 = lane & 3;
+  const int wr = warp % WR, wt = warp / WR;
+
+  // ---- this block's share of the units
+  int64_t total = 0;
+  for (int base = 0; base < c.n_seq; base += kThreads) {
+    const int b = base + (int)threadIdx.x;
+    int64_t u = 0, all;
+    if (b < c.n_seq) {
+      const KvSeq s = kv_seq(c, b);
+      if (s.n < 0 && blockIdx.x == 0) atomicOr(c.status, kFaultBatch);
+      u = seq_units(a, s, S::kRows);
+    }
+    block_scan(u, &all);
+    total += all;
+  }
+  Walk w;
+  w.chunk = max((int64_t)a.min_units, (total + gridDim.x - 1) / gridDim.x);
+  int64_t u = w.chunk * blockIdx.x;
+  const int64_t u_end = min(total, u + w.chunk);
+  if (u >= u_end) return;
+  {
+    int64_t before = 0;
+    for (int base = 0; base < c.n_seq; base += kThreads) {
+      const int b = base + (int)threadIdx.x;
+      int64_t n = 0, all;
+      if (b < c.n_seq) n = seq_units(a, kv_seq(c, b), S::kRows);
+      const int64_t hi = before + block_scan(n, &all);
+      if (u < hi && u >= hi - n) {
+        s_seq[0] = b;
+        s_seq[1] = hi - n;
+      }
+      before += all;
+      if (u < before) break;
+    }
+    __syncthreads();
+    w.tl.b = (int)s_seq[0];
+    w.tile_first = s_seq[1];
+    w.tl.s = kv_seq(c, w.tl.b);
+    w.tl.t = 0;
+    for (;;) {
+      w.tl.blocks = tile_blocks(a, w.tl.s, w.tl.t, S::kRows);
+      const int64_t n = (int64_t)w.tl.blocks * c.kv_heads;
+      if (u < w.tile_first + n) break;
+      w.tile_first += n;
+      ++w.tl.t;
+    }
+  }
+
+  while (u < u_end) {
+    // ---- one segment: blocks [blk0, blk1) of (tile, head)
+    const Tile& tl = w.tl;
+    const int h = (int)((u - w.tile_first) / tl.blocks);
+    const int64_t seg_first = w.tile_first + (int64_t)h * tl.blocks;  // unit of block 0
+    const int blk0 = (int)(u - seg_first);
+    const int blk1 = (int)min((int64_t)tl.blocks, u_end - seg_first);
+    const int rows = min(S::kRows, tl.s.n * c.group - tl.t * S::kRows);
+    const int32_t* table = c.table + (int64_t)tl.b * c.table_stride;
+
+    // ---- query fragments: row r0 + 8 nt + g, dims 16 t4 .. + 15 (+ 64)
+    uint32_t qf[NT][kTerms][kC * 8];
+    float rm[NT][2];     // score multiplier of rows 2 t4, 2 t4 + 1
+    int lim[NT][2];      // last token these rows see
+    int lim_min = INT32_MAX;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = wr * S::kRowsPerWarp + 8 * nt + g;
+      const int row = tl.t * S::kRows + r;
+      const bool have = r < rows;
+      const int tok = row / c.group;
+      float x[kC * 16];
+      if (have) {
+        const T* p = static_cast<const T*>(a.q.p) + (int64_t)(tl.s.first + tok) * a.q.ts +
+                     (int64_t)(h * c.group + row % c.group) * a.q.hs + 16 * t4;
+#pragma unroll
+        for (int i = 0; i < kC; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[16 * i + j] = elem<T>(p + 64 * i + j);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kC * 16; ++i) x[i] = 0.0f;
+      }
+      float amax = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kC * 16; ++i) amax = fmaxf(amax, fabsf(x[i]));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      // the row times 2^up has its largest element in [2^14, 2^15)
+      const int ex = (int)(__float_as_uint(amax) >> 23) - 127;
+      const int up = min(max(14 - ex, -120), 100);
+      const float f = pow2f(up), mul = a.score_mul * pow2f(-up);
+#pragma unroll
+      for (int i = 0; i < kC * 8; ++i) {
+        const float y0 = __fmul_rn(x[2 * i], f), y1 = __fmul_rn(x[2 * i + 1], f);
+        qf[nt][0][i] = half2_bits(y0, y1);
+        if constexpr (kSplit) {
+          const float2 hi = half2_floats(qf[nt][0][i]);
+          qf[nt][1][i] = half2_bits(__fsub_rn(y0, hi.x), __fsub_rn(y1, hi.y));
+        }
+      }
+      const int see = a.causal ? tl.s.kv - tl.s.n + tok : tl.s.kv - 1;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        rm[nt][i] = __shfl_sync(0xffffffffu, mul, 4 * (2 * t4 + i));
+        lim[nt][i] = __shfl_sync(0xffffffffu, have ? see : -1, 4 * (2 * t4 + i));
+      }
+      int lo = have ? see : INT32_MAX;
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      lim_min = min(lim_min, lo);
+    }
+
+    float o[NT][D / 16][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) m[nt][i] = -INFINITY, l[nt][i] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[nt][dt][i] = 0.0f;
+    }
+
+    for (int blk = blk0 + wt; blk < blk1; blk += S::kTokWarps) {
+      // pages of this lane's key tokens (16-token group g / 2) and value tokens (group t4)
+      const int jk = blk * kUnit + 16 * (g >> 1), jv = blk * kUnit + 16 * t4;
+      int pk = jk < tl.s.kv ? __ldg(table + (jk >> c.log_page)) : 0;
+      int pv = __shfl_sync(0xffffffffu, pk, 8 * t4);
+      const bool bad = pk < 0 || pk >= c.n_pages;
+      if (bad) {
+        atomicOr(c.status, kFaultBatch);
+        pk = 0;
+      }
+      const bool vbad = pv < 0 || pv >= c.n_pages;
+      if (vbad) pv = 0;
+      const int rk = jk & (c.page - 1), rv = jv & (c.page - 1);
+      const uint8_t* kb = c.k + block_off<D>(c, pk, h);
+      const uint8_t* vb = c.v + block_off<D>(c, pv, h) + (((int64_t)(rv >> 4) * D) << 4);
+      const int ek = __ldg(c.k_exp + (int64_t)pk * c.kv_heads + h), ev = __ldg(c.v_exp + (int64_t)pk * c.kv_heads + h);
+
+      // ---- scores: 4 MMA row tiles of 16 tokens; tile s, rows 0-7: tokens
+      // 16 (g / 2) + 4 s + g % 2, rows 8-15: two further
+      float x[NT][4][4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[nt][s][i] = 0.0f;
+        const int row = rk + 4 * s + (g & 1);
+#pragma unroll
+        for (int cc = 0; cc < kC; ++cc) {
+          const uint8_t* kp = kb + ((((t4 + 4 * cc) << c.log_page) + row) << 4);
+          uint32_t f0[8], f1[8];
+          widen(ldg16(kp), f0);
+          widen(ldg16(kp + 32), f1);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t fr[4] = {f0[2 * i], f1[2 * i], f0[2 * i + 1], f1[2 * i + 1]};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int q = kTerms - 1; q >= 0; --q)
+                mma(x[nt][s], fr, qf[nt][q][8 * cc + 2 * i], qf[nt][q][8 * cc + 2 * i + 1]);
+          }
+        }
+      }
+
+      // ---- softmax weights; this lane's tokens lie in one block
+      const float nan = __int_as_float(0x7FC00000);
+      const float sk = ek == kExpNan ? nan : pow2f(ek), evf = ev == kExpNan ? nan : (float)ev;
+      const float un = ev == kExpNan ? nan : pow2f(-ev);
+      const bool masked = blk * kUnit + kUnit - 1 > lim_min || __any_sync(0xffffffffu, bad);
+      uint32_t pf[NT][kTerms][8];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float k = __fmul_rn(rm[nt][i], sk);
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              float y = __fmaf_rn(x[nt][s][2 * hf + i], k, evf);
+              if (masked && (bad || jk + 4 * s + (g & 1) + 2 * hf > lim[nt][i])) y = -INFINITY;
+              x[nt][s][2 * hf + i] = y;
+              mx[i] = fmaxf(mx[i], y);
+            }
+#pragma unroll
+          for (int of = 4; of < 32; of <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], of));
+          const float mn = fmaxf(m[nt][i], mx[i]);
+          const float base = mn == -INFINITY ? 0.0f : mn;
+          const float al = ex2(__fsub_rn(m[nt][i], base));
+          m[nt][i] = mn;
+          float sum = 0.0f;
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const float p = ex2(__fsub_rn(x[nt][s][2 * hf + i], __fsub_rn(base, kPBits)));
+              x[nt][s][2 * hf + i] = p;
+              sum = __fadd_rn(sum, p);
+            }
+          l[nt][i] = __fmaf_rn(l[nt][i], al, sum == 0.0f ? 0.0f : __fmul_rn(sum, un));
+#pragma unroll
+          for (int dt = 0; dt < D / 16; ++dt) {
+            o[nt][dt][i] = __fmul_rn(o[nt][dt][i], al);
+            o[nt][dt][2 + i] = __fmul_rn(o[nt][dt][2 + i], al);
+          }
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const float p0 = x[nt][s][2 * hf], p1 = x[nt][s][2 * hf + 1];
+            const uint32_t hi = half2_bits(p0, p1);
+            pf[nt][0][2 * s + hf] = transpose8(hi);
+            if constexpr (kSplit) {
+              const float2 b = half2_floats(hi);
+              pf[nt][1][2 * s + hf] = transpose8(half2_bits(__fsub_rn(p0, b.x), __fsub_rn(p1, b.y)));
+            }
+          }
+      }
+
+      // ---- O^T += V^T P^T: MMA row tiles of 16 dims, 4 steps of 16 tokens.
+      // Rows that hold no token yet may hold any bytes, e4m3's NaN among them.
+      const bool tail = masked && (blk * kUnit + kUnit > tl.s.kv || __any_sync(0xffffffffu, vbad));
+      uint4 keep = make_uint4(~0u, ~0u, ~0u, ~0u);
+      if (tail) {
+        const int have = vbad ? 0 : tl.s.kv - jv;
+        keep.x = first_bytes(have);
+        keep.y = first_bytes(have - 4);
+        keep.z = first_bytes(have - 8);
+        keep.w = first_bytes(have - 12);
+      }
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        const uint8_t* vp = vb + ((16 * dt + g) << 4);
+        uint4 v0 = ldg16(vp), v1 = ldg16(vp + 128);
+        if (tail) {
+          v0 = make_uint4(v0.x & keep.x, v0.y & keep.y, v0.z & keep.z, v0.w & keep.w);
+          v1 = make_uint4(v1.x & keep.x, v1.y & keep.y, v1.z & keep.z, v1.w & keep.w);
+        }
+        uint32_t f0[8], f1[8];
+        widen(v0, f0);
+        widen(v1, f1);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const uint32_t fr[4] = {f0[2 * s], f1[2 * s], f0[2 * s + 1], f1[2 * s + 1]};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int q = kTerms - 1; q >= 0; --q) mma(o[nt][dt], fr, pf[nt][q][2 * s], pf[nt][q][2 * s + 1]);
+        }
+      }
+    }
+
+    // ---- the warps' results to shared memory
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float t = l[nt][i];
+#pragma unroll
+        for (int of = 4; of < 32; of <<= 1) t = __fadd_rn(t, __shfl_xor_sync(0xffffffffu, t, of));
+        const int r = wr * S::kRowsPerWarp + 8 * nt + 2 * t4 + i;
+        if (g == 0) {
+          sm[wt][r] = m[nt][i];
+          sl[wt][r] = t;
+        }
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+          so[wt][r][16 * dt + g] = o[nt][dt][i];
+          so[wt][r][16 * dt + 8 + g] = o[nt][dt][2 + i];
+        }
+      }
+    __syncthreads();
+
+    const bool whole = blk0 == 0 && blk1 == tl.blocks;
+    const int bid = blockIdx.x;
+    const int c0 = (int)(seg_first / w.chunk), c1 = (int)((seg_first + tl.blocks - 1) / w.chunk);
+    float* slot = a.partial + (int64_t)(2 * bid + (bid == c0 ? 1 : 0)) * a.slot_floats;
+    for (int i = threadIdx.x; i < rows * D; i += kThreads) {
+      const int r = i / D, d = i % D;
+      float mx = sm[0][r];
+#pragma unroll
+      for (int k = 1; k < S::kTokWarps; ++k) mx = fmaxf(mx, sm[k][r]);
+      const float base = mx == -INFINITY ? 0.0f : mx;
+      float os = 0.0f, ls = 0.0f;
+#pragma unroll
+      for (int k = 0; k < S::kTokWarps; ++k) {
+        const float f = ex2(__fsub_rn(sm[k][r], base));
+        os = __fmaf_rn(so[k][r][d], f, os);
+        ls = __fmaf_rn(sl[k][r], f, ls);
+      }
+      if (whole) {
+        write_final<T, D>(a, tl, h, S::kRows, r, d, os, mx, ls);
+      } else {
+        slot[r * D + d] = os;
+        if (d == 0) {
+          slot[S::kRows * D + r] = mx;
+          slot[S::kRows * D + S::kRows + r] = ls;
+        }
+      }
+    }
+    if (!whole) {
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const int n = c1 - c0 + 1;
+        const int seen = atomicAdd(a.arrived + c0, 1);
+        last_flag = seen == n - 1;
+        if (last_flag) a.arrived[c0] = 0;  // as every call leaves it
+      }
+      __syncthreads();
+      if (last_flag) {
+        __threadfence();
+        for (int i = threadIdx.x; i < rows * D; i += kThreads) {
+          const int r = i / D, d = i % D;
+          float mx = -INFINITY;
+          for (int k = c0; k <= c1; ++k) {
+            const float* sp = a.partial + (int64_t)(2 * k + (k == c0 ? 1 : 0)) * a.slot_floats;
+            mx = fmaxf(mx, __ldcg(sp + S::kRows * D + r));
+          }
+          const float base = mx == -INFINITY ? 0.0f : mx;
+          float os = 0.0f, ls = 0.0f;
+          for (int k = c0; k <= c1; ++k) {
+            const float* sp = a.partial + (int64_t)(2 * k + (k == c0 ? 1 : 0)) * a.slot_floats;
+            const float f = ex2(__fsub_rn(__ldcg(sp + S::kRows * D + r), base));
+            os = __fmaf_rn(__ldcg(sp + r * D + d), f, os);
+            ls = __fmaf_rn(__ldcg(sp + S::kRows * D + S::kRows + r), f, ls);
+          }
+          write_final<T, D>(a, tl, h, S::kRows, r, d, os, mx, ls);
+        }
+      }
+    }
+    __syncthreads();  // shared memory is free for the next segment
+
+    // ---- the next (tile, head)
+    u = seg_first + blk1;
+    if (u < u_end && h + 1 == c.kv_heads) {
+      w.tile_first += (int64_t)tl.blocks * c.kv_heads;
+      if (++w.tl.t >= seq_tiles(a, w.tl.s, S::kRows)) {
+        w.tl.t = 0;
+        do {
+          w.tl.s = kv_seq(c, ++w.tl.b);
+        } while (w.tl.s.n <= 0);  // units remain, so a sequence with rows follows
+      }
+      w.tl.blocks = tile_blocks(a, w.tl.s, w.tl.t, S::kRows);
+    }
+  }
+}
+
+template <typename T, int D, int NT, int WR>
+cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
+  const int64_t tiles = tiles_upper(a.c, Shape<NT, WR>::kRows);
+  AttnArgs b = a;
+  b.min_units = Shape<NT, WR>::kTokWarps;
+  int64_t grid = kMaxAttnBlocks;
+  const int64_t most = tiles * a.c.kv_heads * max_blocks;
+  if (grid > most) grid = most;
+  paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, kThreads, 0, st>>>(b);
+  note_launches(1);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t pick(const AttnArgs& a, int max_new, int64_t max_blocks, cudaStream_t st) {
+  const int64_t rows = (int64_t)max_new * a.c.group;
+  if (rows <= 8) return launch<T, D, 1, 1>(a, max_blocks, st);
+  if (rows <= 16) return launch<T, D, 2, 1>(a, max_blocks, st);
+  return launch<T, D, 2, 4>(a, max_blocks, st);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_rows(const AttnArgs& a, int head_dim, int dtype, int max_new, int max_kv, cudaStream_t st) {
+  const int64_t mb = max_kv > kUnit ? ((int64_t)max_kv + kUnit - 1) / kUnit : 1;
+  if (dtype == AWSRC_DTYPE_BF16)
+    return head_dim == 128 ? pick<__nv_bfloat16, 128>(a, max_new, mb, st) : pick<__nv_bfloat16, 64>(a, max_new, mb, st);
+  return head_dim == 128 ? pick<float, 128>(a, max_new, mb, st) : pick<float, 64>(a, max_new, mb, st);
+}
+
+}  // namespace awsrc
