@@ -653,14 +653,17 @@ void awsrc_set_search_pruning(int32_t enabled);
  * then records bit 2 of the workspace's fault word, waits (with the same
  * limit) for its own copies and tensor-core work still in flight, frees its
  * tensor memory and exits, so the GPU context stays usable.
- *   wait_ns      the limit of every such wait in later awsrc_encode_tiles
- *                calls (0: the default 2 s).
+ *   wait_ns      the limit of every such wait in later awsrc_encode_tiles and
+ *                awsrc_paged_attention calls (0: the default 2 s).
  *   stall_chunk  >= 0: the C = 64, P = 4, AWSRC-U search issues no copies of
  *                its seed chunks from this one (counted within each block's
  *                range of 32-seed chunks) on, so its waits for that chunk run
- *                out; -1: normal operation.
- * The call's candidates are then undefined and awsrc_workspace_status reports
- * bit 2. awsrc_set_wait_test(0, -1) restores normal operation.
+ *                out; the tensor-memory kernel of awsrc_paged_attention stops
+ *                its copies the same way, counted in blocks of 128 tokens; -1:
+ *                normal operation.
+ * The call's results are then undefined and awsrc_workspace_status reports
+ * bit 2. awsrc_set_wait_test(0, -1) restores normal operation; an attention
+ * workspace has to go through awsrc_attention_workspace_init again.
  */
 void awsrc_set_wait_test(uint64_t wait_ns, int32_t stall_chunk);
 

@@ -116,6 +116,9 @@ EncodeLayout encode_layout(const Prm& pr, int32_t n_mod, const awsrc_module* mod
 
 }  // namespace
 
+uint64_t wait_limit_ns() { return g_wait_ns ? g_wait_ns : kWaitLimitNs; }
+int wait_test_stall() { return g_stall_chunk; }
+
 void note_launches(int n) { g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
 
 awsrc_status cuda_fail(cudaError_t e, const char* where) {

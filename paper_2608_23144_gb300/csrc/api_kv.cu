@@ -24,15 +24,17 @@ awsrc_status check_cache(const awsrc_kv_cache* c, int32_t n_heads, bool pointers
 
 struct AttnLayout {
   size_t arrived, partial, total;
-  int64_t slot_floats;
+  int64_t row_slot, tile_slot;  // floats of a partial result of either kernel
 };
 
 AttnLayout attn_layout(const awsrc_kv_cache& c) {
   AttnLayout L{};
   L.arrived = kStatusBytes;
   L.partial = L.arrived + align_up((size_t)kMaxAttnBlocks * sizeof(int), 256);
-  L.slot_floats = (int64_t)kSlotRows * (c.head_dim + 2);
-  L.total = L.partial + align_up((size_t)2 * kMaxAttnBlocks * L.slot_floats * sizeof(float), 256);
+  L.row_slot = (int64_t)kSlotRows * (c.head_dim + 2);
+  L.tile_slot = (int64_t)kTileSlotRows * (c.head_dim + 2);
+  const size_t rows = (size_t)2 * kMaxAttnBlocks * L.row_slot, tiles = (size_t)2 * kMaxTileBlocks * L.tile_slot;
+  L.total = L.partial + align_up((rows > tiles ? rows : tiles) * sizeof(float), 256);
   return L;
 }
 
@@ -149,9 +151,15 @@ awsrc_status awsrc_paged_attention(const awsrc_kv_cache* cache, const awsrc_kv_b
   a.causal = causal;
   a.arrived = reinterpret_cast<int*>(ws + L.arrived);
   a.partial = reinterpret_cast<float*>(ws + L.partial);
-  a.slot_floats = L.slot_floats;
-  const cudaError_t e = launch_paged_rows(a, cache->head_dim, q->dtype, batch->max_new, batch->max_kv,
-                                          (cudaStream_t)stream);
+  a.wait_ns = wait_limit_ns();
+  a.stall = wait_test_stall();
+  // BF16 with more rows per kv head than the row kernel takes in one warp tile
+  // goes to the tensor-memory kernel
+  const bool tiles = q->dtype == AWSRC_DTYPE_BF16 && (int64_t)batch->max_new * a.c.group > 16;
+  a.slot_floats = tiles ? L.tile_slot : L.row_slot;
+  const cudaError_t e = tiles ? launch_paged_tiles(a, cache->head_dim, batch->max_kv, (cudaStream_t)stream)
+                              : launch_paged_rows(a, cache->head_dim, q->dtype, batch->max_new, batch->max_kv,
+                                                  (cudaStream_t)stream);
   return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "paged_attention");
 }
 

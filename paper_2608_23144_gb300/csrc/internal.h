@@ -20,6 +20,11 @@ void set_error_message(const char* fmt, ...);
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// Limit of the kernels' bounded waits and the stall of the calling host thread's
+// wait test (awsrc_set_wait_test; -1: none).
+uint64_t wait_limit_ns();
+int wait_test_stall();
+
 // Launch counter behind awsrc_kernel_launches(): every launch site adds its kernels.
 void note_launches(int n);
 

@@ -73,6 +73,9 @@ __device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t codes) {
 // for partial results of the first and last tile it shares with others.
 constexpr int kMaxAttnBlocks = 304;
 constexpr int kSlotRows = 64;
+// The tensor-memory kernel: one per SM, 256 rows.
+constexpr int kMaxTileBlocks = 152;
+constexpr int kTileSlotRows = 256;
 
 struct AttnArgs {
   KvArgs c;
@@ -81,10 +84,166 @@ struct AttnArgs {
   float score_mul;  // sm_scale log2(e)
   int causal;
   int min_units;    // least share of a block
-  int* arrived;     // per block: arrivals at the shared tile that begins in its share
+  int* arrived;     // per block (two for each, one per 128 rows): arrivals at the shared tile that begins in its share
   float* partial;
   int64_t slot_floats;
+  uint64_t wait_ns;  // limit of the tensor-memory kernel's waits
+  int stall;         // test of that limit: no copies from this block of tokens on (-1: never)
 };
+
+// ------------------------------------------------------------ work sharing --
+// A batch is cut into units: (sequence, tile of ROWS query rows, kv head, block
+// of UNIT tokens), in this order; rows are query tokens x the heads of a kv
+// head. A tile has as many blocks as its last row sees tokens, at least one.
+// The thread blocks of a launch take equal contiguous shares, a segment being
+// the part of one (tile, head) in a share.
+struct Segment {
+  int h, blk0, blk1;  // kv head, blocks [blk0, blk1)
+  int rows;           // query rows of the tile
+  int64_t first;      // unit of block 0
+  int c0, c1;         // thread blocks that share (tile, head)
+  bool whole;         // this one has it alone
+};
+
+template <int ROWS, int UNIT, int WARPS>
+struct UnitWalk {
+  int64_t chunk, u, u_end, tile_first;
+  int b, t, blocks;  // sequence, tile and the tile's blocks
+  KvSeq s;
+
+  __device__ __forceinline__ static int blocks_of(const AttnArgs& a, const KvSeq& s, int t) {
+    int see = s.kv;
+    if (a.causal) {
+      const int last = min((t + 1) * ROWS, s.n * a.c.group) - 1;
+      see = s.kv - s.n + last / a.c.group + 1;
+    }
+    return max(1, (see + UNIT - 1) / UNIT);
+  }
+  __device__ __forceinline__ static int tiles_of(const AttnArgs& a, const KvSeq& s) {
+    return s.n > 0 ? (s.n * a.c.group + ROWS - 1) / ROWS : 0;
+  }
+  __device__ static int64_t units_of(const AttnArgs& a, const KvSeq& s) {
+    const int nt = tiles_of(a, s);
+    int64_t n = 0;
+    for (int i = 0; i < nt; ++i) n += blocks_of(a, s, i);
+    return n * a.c.kv_heads;
+  }
+  // Inclusive sum over the first WARPS warps of one value per thread; *all its total.
+  __device__ __forceinline__ static int64_t scan(int64_t x, int64_t* all) {
+    __shared__ int64_t wsum[WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    __syncthreads();  // an earlier call's readers are done
+    if (lane == 31 && warp < WARPS) wsum[warp] = x;
+    __syncthreads();
+    int64_t t = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) x += wsum[w];
+      t += wsum[w];
+    }
+    *all = t;
+    return x;
+  }
+  // Finds the share of this thread block (every thread calls it); false when it is empty.
+  __device__ bool start(const AttnArgs& a) {
+    __shared__ int64_t found[2];
+    const KvArgs& c = a.c;
+    constexpr int kN = 32 * WARPS;
+    int64_t total = 0, all;
+    for (int base = 0; base < c.n_seq; base += kN) {
+      const int i = base + (int)threadIdx.x;
+      int64_t n = 0;
+      if (threadIdx.x < kN && i < c.n_seq) {
+        const KvSeq q = kv_seq(c, i);
+        if (q.n < 0 && blockIdx.x == 0) atomicOr(c.status, kFaultBatch);
+        n = units_of(a, q);
+      }
+      scan(n, &all);
+      total += all;
+    }
+    chunk = max((int64_t)a.min_units, (total + gridDim.x - 1) / gridDim.x);
+    u = chunk * blockIdx.x;
+    u_end = min(total, u + chunk);
+    if (u >= u_end) return false;
+    int64_t before = 0;
+    for (int base = 0; base < c.n_seq; base += kN) {
+      const int i = base + (int)threadIdx.x;
+      int64_t n = 0;
+      if (threadIdx.x < kN && i < c.n_seq) n = units_of(a, kv_seq(c, i));
+      const int64_t hi = before + scan(n, &all);
+      if (u < hi && u >= hi - n) {
+        found[0] = i;
+        found[1] = hi - n;
+      }
+      before += all;
+      if (u < before) break;
+    }
+    __syncthreads();
+    b = (int)found[0];
+    tile_first = found[1];
+    s = kv_seq(c, b);
+    for (t = 0;; ++t) {
+      blocks = blocks_of(a, s, t);
+      const int64_t n = (int64_t)blocks * c.kv_heads;
+      if (u < tile_first + n) return true;
+      tile_first += n;
+    }
+  }
+  __device__ __forceinline__ bool more() const { return u < u_end; }
+  __device__ __forceinline__ Segment segment(const AttnArgs& a) const {
+    Segment g;
+    g.h = (int)((u - tile_first) / blocks);
+    g.first = tile_first + (int64_t)g.h * blocks;
+    g.blk0 = (int)(u - g.first);
+    g.blk1 = (int)min((int64_t)blocks, u_end - g.first);
+    g.rows = min(ROWS, s.n * a.c.group - t * ROWS);
+    g.c0 = (int)(g.first / chunk);
+    g.c1 = (int)((g.first + blocks - 1) / chunk);
+    g.whole = g.blk0 == 0 && g.blk1 == blocks;
+    return g;
+  }
+  __device__ __forceinline__ void advance(const AttnArgs& a, const Segment& g) {
+    u = g.first + g.blk1;
+    if (u >= u_end || g.h + 1 < a.c.kv_heads) return;
+    tile_first += (int64_t)blocks * a.c.kv_heads;
+    if (++t >= tiles_of(a, s)) {
+      t = 0;
+      do {
+        s = kv_seq(a.c, ++b);
+      } while (s.n <= 0);  // units remain, so a sequence with rows follows
+    }
+    blocks = blocks_of(a, s, t);
+  }
+};
+
+// The slot of thread block k's partial result of a tile that begins in c0's share.
+__device__ __forceinline__ float* partial_slot(const AttnArgs& a, int k, int c0) {
+  return a.partial + (int64_t)(2 * k + (k == c0 ? 1 : 0)) * a.slot_floats;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// A word whose first n bytes are ones.
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (n <= 0 ? 0u : (1u << (8 * n)) - 1u); }
+
+// 16 codes -> binary16 pairs in order.
+__device__ __forceinline__ void widen(const uint4& v, uint32_t* f) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = e4m3x2_half2(w[i] & 0xFFFFu);
+    f[2 * i + 1] = e4m3x2_half2(w[i] >> 16);
+  }
+}
 
 // Row tiles a batch can have at most.
 inline int64_t tiles_upper(const KvArgs& c, int tile_rows) {
@@ -95,5 +254,6 @@ cudaError_t launch_kv_append(const KvArgs& c, int head_dim, int dtype, const KvR
                              const KvRows& v, const KvRows& qo, const float* cos, const float* sin, int rope_rows,
                              int rotary_dim, int interleaved, cudaStream_t st);
 cudaError_t launch_paged_rows(const AttnArgs& a, int head_dim, int dtype, int max_new, int max_kv, cudaStream_t st);
+cudaError_t launch_paged_tiles(const AttnArgs& a, int head_dim, int max_kv, cudaStream_t st);  // BF16
 
 }  // namespace awsrc

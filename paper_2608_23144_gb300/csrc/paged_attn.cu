@@ -38,12 +38,6 @@ constexpr int kUnit = 64;         // tokens per unit
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPBits = 15.0f;   // p is at most 2^15
 
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
 __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -66,80 +60,12 @@ __device__ __forceinline__ float2 half2_floats(uint32_t v) { return __half22floa
 
 __device__ __forceinline__ uint4 ldg16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
 
-// 16 codes -> A-fragment words: f[2i] the first pair of word i, f[2i + 1] the second.
-__device__ __forceinline__ void widen(const uint4& v, uint32_t* f) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = e4m3x2_half2(w[i] & 0xFFFFu);
-    f[2 * i + 1] = e4m3x2_half2(w[i] >> 16);
-  }
-}
-
-// A word whose first n bytes are ones.
-__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (n <= 0 ? 0u : (1u << (8 * n)) - 1u); }
-
 template <typename T>
 __device__ __forceinline__ float elem(const T* p);
 template <>
 __device__ __forceinline__ float elem(const float* p) { return __ldg(p); }
 template <>
 __device__ __forceinline__ float elem(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-
-// A row tile of one sequence and its unit count per kv head.
-struct Tile {
-  int b, t;        // sequence, row tile
-  KvSeq s;
-  int blocks;      // 64-token blocks that some row of the tile sees, at least 1
-};
-
-// Tokens the last row of tile t sees.
-__device__ __forceinline__ int tile_tokens(const AttnArgs& a, const KvSeq& s, int t, int tile_rows) {
-  if (!a.causal) return s.kv;
-  const int last = min((t + 1) * tile_rows, s.n * a.c.group) - 1;
-  return s.kv - s.n + last / a.c.group + 1;
-}
-__device__ __forceinline__ int tile_blocks(const AttnArgs& a, const KvSeq& s, int t, int tile_rows) {
-  return max(1, (tile_tokens(a, s, t, tile_rows) + kUnit - 1) / kUnit);
-}
-__device__ __forceinline__ int seq_tiles(const AttnArgs& a, const KvSeq& s, int tile_rows) {
-  return s.n > 0 ? (s.n * a.c.group + tile_rows - 1) / tile_rows : 0;
-}
-__device__ int64_t seq_units(const AttnArgs& a, const KvSeq& s, int tile_rows) {
-  const int nt = seq_tiles(a, s, tile_rows);
-  int64_t u = 0;
-  for (int t = 0; t < nt; ++t) u += tile_blocks(a, s, t, tile_rows);
-  return u * a.c.kv_heads;
-}
-
-// Inclusive sum over the block of one value per thread; *all its total.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* all) {
-  __shared__ int64_t wsum[kWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();  // an earlier call's readers are done
-  if (lane == 31) wsum[warp] = x;
-  __syncthreads();
-  int64_t t = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) x += wsum[w];
-    t += wsum[w];
-  }
-  *all = t;
-  return x;
-}
-
-// Thread-block-wide state of the walk over units.
-struct Walk {
-  int64_t chunk;         // units per block
-  int64_t tile_first;    // first unit of (tile, head 0)
-  Tile tl;
-};
 
 template <int NT, int WR>
 struct Shape {
@@ -153,10 +79,9 @@ struct RowStride { static constexpr int value = D + 4; };  // floats of a row in
 
 // Element d of row r of a finished tile, and its lse.
 template <typename T, int D>
-__device__ __forceinline__ void write_final(const AttnArgs& a, const Tile& tl, int h, int tile_rows, int r, int d,
-                                            float o, float m, float l) {
-  const int row = tl.t * tile_rows + r;
-  const int tok = tl.s.first + row / a.c.group, head = h * a.c.group + row % a.c.group;
+__device__ __forceinline__ void write_final(const AttnArgs& a, const KvSeq& s, int row, int h, int d, float o, float m,
+                                            float l) {
+  const int tok = s.first + row / a.c.group, head = h * a.c.group + row % a.c.group;
   const float v = l == 0.0f ? 0.0f : __fdiv_rn(o, l);
   T* p = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.ts + (int64_t)head * a.out.hs + d;
   if constexpr (sizeof(T) == 2)
@@ -177,67 +102,18 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
   __shared__ float so[S::kTokWarps][S::kRows][kStride];
   __shared__ float sm[S::kTokWarps][S::kRows], sl[S::kTokWarps][S::kRows];
   __shared__ int last_flag;
-  __shared__ int64_t s_seq[2];
   const KvArgs& c = a.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t4 = lane & 3;
   const int wr = warp % WR, wt = warp / WR;
 
-  // ---- this block's share of the units
-  int64_t total = 0;
-  for (int base = 0; base < c.n_seq; base += kThreads) {
-    const int b = base + (int)threadIdx.x;
-    int64_t u = 0, all;
-    if (b < c.n_seq) {
-      const KvSeq s = kv_seq(c, b);
-      if (s.n < 0 && blockIdx.x == 0) atomicOr(c.status, kFaultBatch);
-      u = seq_units(a, s, S::kRows);
-    }
-    block_scan(u, &all);
-    total += all;
-  }
-  Walk w;
-  w.chunk = max((int64_t)a.min_units, (total + gridDim.x - 1) / gridDim.x);
-  int64_t u = w.chunk * blockIdx.x;
-  const int64_t u_end = min(total, u + w.chunk);
-  if (u >= u_end) return;
-  {
-    int64_t before = 0;
-    for (int base = 0; base < c.n_seq; base += kThreads) {
-      const int b = base + (int)threadIdx.x;
-      int64_t n = 0, all;
-      if (b < c.n_seq) n = seq_units(a, kv_seq(c, b), S::kRows);
-      const int64_t hi = before + block_scan(n, &all);
-      if (u < hi && u >= hi - n) {
-        s_seq[0] = b;
-        s_seq[1] = hi - n;
-      }
-      before += all;
-      if (u < before) break;
-    }
-    __syncthreads();
-    w.tl.b = (int)s_seq[0];
-    w.tile_first = s_seq[1];
-    w.tl.s = kv_seq(c, w.tl.b);
-    w.tl.t = 0;
-    for (;;) {
-      w.tl.blocks = tile_blocks(a, w.tl.s, w.tl.t, S::kRows);
-      const int64_t n = (int64_t)w.tl.blocks * c.kv_heads;
-      if (u < w.tile_first + n) break;
-      w.tile_first += n;
-      ++w.tl.t;
-    }
-  }
-
-  while (u < u_end) {
-    // ---- one segment: blocks [blk0, blk1) of (tile, head)
-    const Tile& tl = w.tl;
-    const int h = (int)((u - w.tile_first) / tl.blocks);
-    const int64_t seg_first = w.tile_first + (int64_t)h * tl.blocks;  // unit of block 0
-    const int blk0 = (int)(u - seg_first);
-    const int blk1 = (int)min((int64_t)tl.blocks, u_end - seg_first);
-    const int rows = min(S::kRows, tl.s.n * c.group - tl.t * S::kRows);
-    const int32_t* table = c.table + (int64_t)tl.b * c.table_stride;
+  UnitWalk<S::kRows, kUnit, kWarps> w;
+  if (!w.start(a)) return;
+  while (w.more()) {
+    const Segment sg = w.segment(a);
+    const KvSeq s = w.s;
+    const int h = sg.h, rows = sg.rows, row0 = w.t * S::kRows;
+    const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
 
     // ---- query fragments: row r0 + 8 nt + g, dims 16 t4 .. + 15 (+ 64)
     uint32_t qf[NT][kTerms][kC * 8];
@@ -247,12 +123,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = wr * S::kRowsPerWarp + 8 * nt + g;
-      const int row = tl.t * S::kRows + r;
+      const int row = row0 + r;
       const bool have = r < rows;
       const int tok = row / c.group;
       float x[kC * 16];
       if (have) {
-        const T* p = static_cast<const T*>(a.q.p) + (int64_t)(tl.s.first + tok) * a.q.ts +
+        const T* p = static_cast<const T*>(a.q.p) + (int64_t)(s.first + tok) * a.q.ts +
                      (int64_t)(h * c.group + row % c.group) * a.q.hs + 16 * t4;
 #pragma unroll
         for (int i = 0; i < kC; ++i)
@@ -280,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
           qf[nt][1][i] = half2_bits(__fsub_rn(y0, hi.x), __fsub_rn(y1, hi.y));
         }
       }
-      const int see = a.causal ? tl.s.kv - tl.s.n + tok : tl.s.kv - 1;
+      const int see = a.causal ? s.kv - s.n + tok : s.kv - 1;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         rm[nt][i] = __shfl_sync(0xffffffffu, mul, 4 * (2 * t4 + i));
@@ -303,10 +179,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         for (int i = 0; i < 4; ++i) o[nt][dt][i] = 0.0f;
     }
 
-    for (int blk = blk0 + wt; blk < blk1; blk += S::kTokWarps) {
+    for (int blk = sg.blk0 + wt; blk < sg.blk1; blk += S::kTokWarps) {
       // pages of this lane's key tokens (16-token group g / 2) and value tokens (group t4)
       const int jk = blk * kUnit + 16 * (g >> 1), jv = blk * kUnit + 16 * t4;
-      int pk = jk < tl.s.kv ? __ldg(table + (jk >> c.log_page)) : 0;
+      int pk = jk < s.kv ? __ldg(table + (jk >> c.log_page)) : 0;
       int pv = __shfl_sync(0xffffffffu, pk, 8 * t4);
       const bool bad = pk < 0 || pk >= c.n_pages;
       if (bad) {
@@ -407,10 +283,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
 
       // ---- O^T += V^T P^T: MMA row tiles of 16 dims, 4 steps of 16 tokens.
       // Rows that hold no token yet may hold any bytes, e4m3's NaN among them.
-      const bool tail = masked && (blk * kUnit + kUnit > tl.s.kv || __any_sync(0xffffffffu, vbad));
+      const bool tail = masked && (blk * kUnit + kUnit > s.kv || __any_sync(0xffffffffu, vbad));
       uint4 keep = make_uint4(~0u, ~0u, ~0u, ~0u);
       if (tail) {
-        const int have = vbad ? 0 : tl.s.kv - jv;
+        const int have = vbad ? 0 : s.kv - jv;
         keep.x = first_bytes(have);
         keep.y = first_bytes(have - 4);
         keep.z = first_bytes(have - 8);
@@ -459,10 +335,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
       }
     __syncthreads();
 
-    const bool whole = blk0 == 0 && blk1 == tl.blocks;
-    const int bid = blockIdx.x;
-    const int c0 = (int)(seg_first / w.chunk), c1 = (int)((seg_first + tl.blocks - 1) / w.chunk);
-    float* slot = a.partial + (int64_t)(2 * bid + (bid == c0 ? 1 : 0)) * a.slot_floats;
+    float* slot = partial_slot(a, blockIdx.x, sg.c0);
     for (int i = threadIdx.x; i < rows * D; i += kThreads) {
       const int r = i / D, d = i % D;
       float mx = sm[0][r];
@@ -476,8 +349,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         os = __fmaf_rn(so[k][r][d], f, os);
         ls = __fmaf_rn(sl[k][r], f, ls);
       }
-      if (whole) {
-        write_final<T, D>(a, tl, h, S::kRows, r, d, os, mx, ls);
+      if (sg.whole) {
+        write_final<T, D>(a, s, row0 + r, h, d, os, mx, ls);
       } else {
         slot[r * D + d] = os;
         if (d == 0) {
@@ -486,14 +359,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         }
       }
     }
-    if (!whole) {
+    if (!sg.whole) {
       __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
-        const int n = c1 - c0 + 1;
-        const int seen = atomicAdd(a.arrived + c0, 1);
-        last_flag = seen == n - 1;
-        if (last_flag) a.arrived[c0] = 0;  // as every call leaves it
+        last_flag = atomicAdd(a.arrived + sg.c0, 1) == sg.c1 - sg.c0;
+        if (last_flag) a.arrived[sg.c0] = 0;  // as every call leaves it
       }
       __syncthreads();
       if (last_flag) {
@@ -501,36 +372,25 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         for (int i = threadIdx.x; i < rows * D; i += kThreads) {
           const int r = i / D, d = i % D;
           float mx = -INFINITY;
-          for (int k = c0; k <= c1; ++k) {
-            const float* sp = a.partial + (int64_t)(2 * k + (k == c0 ? 1 : 0)) * a.slot_floats;
+          for (int k = sg.c0; k <= sg.c1; ++k) {
+            const float* sp = partial_slot(a, k, sg.c0);
             mx = fmaxf(mx, __ldcg(sp + S::kRows * D + r));
           }
           const float base = mx == -INFINITY ? 0.0f : mx;
           float os = 0.0f, ls = 0.0f;
-          for (int k = c0; k <= c1; ++k) {
-            const float* sp = a.partial + (int64_t)(2 * k + (k == c0 ? 1 : 0)) * a.slot_floats;
+          for (int k = sg.c0; k <= sg.c1; ++k) {
+            const float* sp = partial_slot(a, k, sg.c0);
             const float f = ex2(__fsub_rn(__ldcg(sp + S::kRows * D + r), base));
             os = __fmaf_rn(__ldcg(sp + r * D + d), f, os);
             ls = __fmaf_rn(__ldcg(sp + S::kRows * D + S::kRows + r), f, ls);
           }
-          write_final<T, D>(a, tl, h, S::kRows, r, d, os, mx, ls);
+          write_final<T, D>(a, s, row0 + r, h, d, os, mx, ls);
         }
       }
     }
     __syncthreads();  // shared memory is free for the next segment
 
-    // ---- the next (tile, head)
-    u = seg_first + blk1;
-    if (u < u_end && h + 1 == c.kv_heads) {
-      w.tile_first += (int64_t)tl.blocks * c.kv_heads;
-      if (++w.tl.t >= seq_tiles(a, w.tl.s, S::kRows)) {
-        w.tl.t = 0;
-        do {
-          w.tl.s = kv_seq(c, ++w.tl.b);
-        } while (w.tl.s.n <= 0);  // units remain, so a sequence with rows follows
-      }
-      w.tl.blocks = tile_blocks(a, w.tl.s, w.tl.t, S::kRows);
-    }
+    w.advance(a, sg);
   }
 }
 

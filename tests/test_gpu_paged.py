@@ -406,3 +406,22 @@ def test_empty_batches_do_nothing(aw):
     assert aw.awsrc_kv_append(cache, b, q, k, k, None, None, ws).shape == (0, 2, 64)
     assert aw.awsrc_paged_attention(cache, b, q, ws).shape == (0, 2, 64)
     assert aw.awsrc_kernel_launches() == n0 and aw.awsrc_workspace_status(ws) == 0
+
+
+def test_waits_that_run_out_are_reported(aw):
+    """The tensor-memory kernel's bounded waits: its copies stop after some blocks (100 ms limit), the call returns, the
+    fault word says so and the next call works on a workspace made ready again."""
+    gen = torch.Generator().manual_seed(12)
+    new, kv = [300, 40], [9000, 400]  # shares of 4 blocks and more
+    _, table, pages = make_batch(aw, gen, new, kv, 32)
+    cache = random_cache(aw, gen, pages, 2, 128, 32)
+    q = torch.randn(sum(new), 6, 128, generator=gen).to(BF16)
+    for stall in (0, 1, 3):
+        ws = aw.awsrc_attention_workspace(cache, 6)
+        aw.awsrc_set_wait_test(100_000_000, stall)
+        try:
+            aw.awsrc_paged_attention(cache, step_batch(aw, new, kv, table), q.cuda(), ws)
+            assert aw.awsrc_workspace_status(ws) == 4
+        finally:
+            aw.awsrc_set_wait_test()
+    check_attention(aw, cache, q, new, kv, table, True)
