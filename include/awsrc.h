@@ -550,7 +550,7 @@ typedef struct awsrc_rows {
  * fault word and the arrival counters, which every call leaves cleared). Once
  * per workspace. The fault word of these calls accumulates until
  * awsrc_workspace_status reads and clears it.
- * Errors: INVALID_ARG, SHAPE, WORKSPACE, CUDA.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA.
  */
 awsrc_status awsrc_attention_workspace_bytes(const awsrc_kv_cache* cache, int32_t n_heads, size_t* bytes);
 awsrc_status awsrc_attention_workspace_init(const awsrc_kv_cache* cache, int32_t n_heads, void* workspace,
@@ -569,7 +569,9 @@ awsrc_status awsrc_attention_workspace_init(const awsrc_kv_cache* cache, int32_t
  * block's older codes become code * 2^(e_old - e), rounded the same way (exact
  * but for codes that leave e4m3's normal range). A block whose exponent is -128
  * stays so until its page is written from row 0 again; its new codes are 0.
- *   n_heads    query heads, a multiple of n_kv_heads; q, q_out [n_tok][n_heads].
+ *   n_heads    query heads, a multiple of n_kv_heads (at most 1024 times as
+ *              many, else UNSUPPORTED); q, q_out
+ *              [n_tok][n_heads].
  *   k, v       [n_tok][n_kv_heads]; q, k, v and q_out share a dtype.
  *   cos, sin   device, rope_rows x rotary_dim / 2 floats (NULL when rotary_dim
  *              is 0); a token at p >= rope_rows is skipped and reported.

@@ -17,6 +17,7 @@ awsrc_status check_cache(const awsrc_kv_cache* c, int32_t n_heads, bool pointers
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return AWSRC_ERR_SHAPE;
   if (c->head_dim != 64 && c->head_dim != 128) return AWSRC_ERR_SHAPE;
   if (n_heads % c->n_kv_heads != 0) return AWSRC_ERR_SHAPE;
+  if (n_heads / c->n_kv_heads > 1024) return AWSRC_ERR_UNSUPPORTED;
   if (pointers && (!c->k || !c->v || !c->k_exp || !c->v_exp || !aligned(c->k, 16) || !aligned(c->v, 16)))
     return AWSRC_ERR_INVALID_ARG;
   return AWSRC_OK;

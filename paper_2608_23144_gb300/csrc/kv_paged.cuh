@@ -94,18 +94,20 @@ struct AttnArgs {
 // ------------------------------------------------------------ work sharing --
 // A batch is cut into units: (sequence, tile of ROWS query rows, kv head, block
 // of UNIT tokens), in this order; rows are query tokens x the heads of a kv
-// head. A tile has as many blocks as its last row sees tokens, at least one.
-// The thread blocks of a launch take equal contiguous shares, a segment being
-// the part of one (tile, head) in a share.
+// head. A tile has as many blocks as its last row sees tokens, at least one;
+// OVER further units in front of them stand for what starting and finishing a
+// tile costs. The thread blocks of a launch take equal contiguous shares, a
+// segment being the part of one (tile, head) in a share.
 struct Segment {
   int h, blk0, blk1;  // kv head, blocks [blk0, blk1)
   int rows;           // query rows of the tile
   int64_t first;      // unit of block 0
+  bool empty;         // no block of it lies in this share
   int c0, c1;         // thread blocks that share (tile, head)
   bool whole;         // this one has it alone
 };
 
-template <int ROWS, int UNIT, int WARPS>
+template <int ROWS, int UNIT, int WARPS, int OVER>
 struct UnitWalk {
   int64_t chunk, u, u_end, tile_first;
   int b, t, blocks;  // sequence, tile and the tile's blocks
@@ -125,7 +127,7 @@ struct UnitWalk {
   __device__ static int64_t units_of(const AttnArgs& a, const KvSeq& s) {
     const int nt = tiles_of(a, s);
     int64_t n = 0;
-    for (int i = 0; i < nt; ++i) n += blocks_of(a, s, i);
+    for (int i = 0; i < nt; ++i) n += blocks_of(a, s, i) + OVER;
     return n * a.c.kv_heads;
   }
   // Inclusive sum over the first WARPS warps of one value per thread; *all its total.
@@ -189,7 +191,7 @@ struct UnitWalk {
     s = kv_seq(c, b);
     for (t = 0;; ++t) {
       blocks = blocks_of(a, s, t);
-      const int64_t n = (int64_t)blocks * c.kv_heads;
+      const int64_t n = (int64_t)(blocks + OVER) * c.kv_heads;
       if (u < tile_first + n) return true;
       tile_first += n;
     }
@@ -197,20 +199,29 @@ struct UnitWalk {
   __device__ __forceinline__ bool more() const { return u < u_end; }
   __device__ __forceinline__ Segment segment(const AttnArgs& a) const {
     Segment g;
-    g.h = (int)((u - tile_first) / blocks);
-    g.first = tile_first + (int64_t)g.h * blocks;
-    g.blk0 = (int)(u - g.first);
+    g.h = (int)(u - tile_first) / (blocks + OVER);
+    g.first = tile_first + (int64_t)g.h * (blocks + OVER) + OVER;
+    g.blk0 = max(0, (int)(u - g.first));
     g.blk1 = (int)min((int64_t)blocks, u_end - g.first);
     g.rows = min(ROWS, s.n * a.c.group - t * ROWS);
-    g.c0 = (int)(g.first / chunk);
-    g.c1 = (int)((g.first + blocks - 1) / chunk);
+    g.empty = g.blk1 <= g.blk0;
     g.whole = g.blk0 == 0 && g.blk1 == blocks;
+    // blocks before this share and from its end on, in shares (32-bit divisions)
+    if (g.empty) {
+      g.c0 = g.c1 = blockIdx.x;
+      return g;
+    }
+    const int share = (int)min(chunk, (int64_t)INT32_MAX);
+    const int64_t u0 = chunk * blockIdx.x;
+    g.c0 = g.first >= u0 ? (int)blockIdx.x : (int)blockIdx.x - ((int)(u0 - g.first) + share - 1) / share;
+    const int64_t over = g.first + blocks - (u0 + chunk);
+    g.c1 = over <= 0 ? (int)blockIdx.x : (int)blockIdx.x + ((int)over + share - 1) / share;
     return g;
   }
   __device__ __forceinline__ void advance(const AttnArgs& a, const Segment& g) {
     u = g.first + g.blk1;
     if (u >= u_end || g.h + 1 < a.c.kv_heads) return;
-    tile_first += (int64_t)blocks * a.c.kv_heads;
+    tile_first += (int64_t)(blocks + OVER) * a.c.kv_heads;
     if (++t >= tiles_of(a, s)) {
       t = 0;
       do {
@@ -218,6 +229,25 @@ struct UnitWalk {
       } while (s.n <= 0);  // units remain, so a sequence with rows follows
     }
     blocks = blocks_of(a, s, t);
+  }
+};
+
+// Query rows row0 .. of a tile -> token and head within the group, without a
+// division per row: x / group for x < group + 256 by multiplication, exact while
+// x group < 2^22 (groups up to 1024; the entry point refuses larger ones).
+struct RowMap {
+  int tok0, rem0, group;
+  uint32_t inv;
+  __device__ __forceinline__ RowMap(const KvArgs& c, int row0) {
+    group = c.group;
+    tok0 = row0 / group;
+    rem0 = row0 - tok0 * group;
+    inv = (1u << 22) / (uint32_t)group + 1;
+  }
+  __device__ __forceinline__ void at(int i, int* tok, int* head) const {
+    const int x = rem0 + i, q = (int)(((uint32_t)x * inv) >> 22);
+    *tok = tok0 + q;
+    *head = x - q * group;
   }
 };
 

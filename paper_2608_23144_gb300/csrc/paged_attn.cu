@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
   const int g = lane >> 2, t4 = lane & 3;
   const int wr = warp % WR, wt = warp / WR;
 
-  UnitWalk<S::kRows, kUnit, kWarps> w;
+  UnitWalk<S::kRows, kUnit, kWarps, 0> w;
   if (!w.start(a)) return;
   while (w.more()) {
     const Segment sg = w.segment(a);

@@ -20,7 +20,7 @@
 // One thread block per SM and 256 rows (query tokens x the heads of a kv head)
 // in two tiles of 128, so that one tile's softmax runs under the other's
 // products. Warps 0-3 and 4-7: softmax, one row per thread; 8-11: widening; 12:
-// MMA issue; 13: bulk copies. Tensor memory: S 2 x 128 columns, over whose
+// MMA issue; 13: bulk copies (14, 15 idle). Tensor memory: S 2 x 128 columns, over whose
 // first 64 P is written; O 2 x D columns. Per tile and block of 128 tokens:
 //   MMA:     P ready -> O += P V; S = Q K of the next block -> commit
 //   softmax: S ready -> m, P, l; O rescaled by its own threads, only when a row
@@ -47,14 +47,18 @@ using namespace tc05;
 
 constexpr int BM = 128, BN = 128;
 constexpr int kRows = 2 * BM;
-constexpr int kThreads = 448;
+constexpr int kThreads = 512;
 constexpr int kMmaWarp = 12, kLoadWarp = 13;
 constexpr int NK = 3, NV = 2, NW = 2;  // stages: keys, value codes, widened values
 constexpr uint32_t kTmemCols = 512;
+// Registers per thread by role: 512 x 128 at launch = 256 x 184 + 256 x 72.
+constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPBits = 6.0f;         // p is at most 2^6 when m is the maximum,
+constexpr float kTiny = 1e-37f;        // least score multiplier: hidden scores of -inf stay -inf
 constexpr float kGrow = 8.0f;          // and at most 2^(6 + 8) < 65504 when m lags
-using Walk = UnitWalk<kRows, BN, 4>;
+constexpr int kOver = 4;               // a tile's start and end, in blocks
+using Walk = UnitWalk<kRows, BN, 4, kOver>;
 
 template <int N>
 struct Idesc { static constexpr uint32_t value = idesc_f16(BM, N); };  // formats 0: e4m3, binary16
@@ -67,6 +71,7 @@ struct Smem {
   uint8_t w[NW][BN / 8][D][16];     // binary16, 8 tokens
   unsigned long long k_full[NK], k_empty[NK], v_full[NV], v_empty[NV], w_full[NW], w_empty[NW];
   unsigned long long q_full[2], s_full[2], p_full[2], o_full[2], group[2], drain;
+  float4 group_of[8][2][8];  // softmax warp, block parity: scale of the keys, exponent and unscaling of the values, tokens
   uint32_t tmem;
   int dead, last[2];
 };
@@ -79,7 +84,7 @@ struct Ctx {
 
 // Bounded wait of a whole warp; false, for all lanes, once any wait of the
 // block has given up.
-__device__ __noinline__ bool wait_slow(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+__device__ __forceinline__ bool wait_slow(const Ctx& x, unsigned long long* mb, uint32_t parity) {
   const uint64_t t0 = globaltimer();
   bool ok;
   for (;;) {
@@ -140,6 +145,17 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float max16(const float* v) {
+  const float a = max3(v[0], v[1], v[2]), b = max3(v[3], v[4], v[5]), c = max3(v[6], v[7], v[8]);
+  const float d = max3(v[9], v[10], v[11]), e = max3(v[12], v[13], v[14]);
+  return max3(max3(a, b, c), max3(d, e, v[15]), v[15]);
+}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // What the lanes of a warp know about the eight 16-token groups of a block,
@@ -162,6 +178,14 @@ __device__ __forceinline__ Groups load_groups(const KvArgs& c, const int32_t* ta
     }
   }
   return g;
+}
+
+// The tokens of group lane % 8 alone.
+__device__ __forceinline__ int group_tokens(const KvArgs& c, const int32_t* table, int kv, int blk) {
+  const int j = blk * BN + 16 * (threadIdx.x & 7);
+  if (j >= kv) return 0;
+  const int pg = __ldg(table + (j >> c.log_page));
+  return pg >= 0 && pg < c.n_pages ? min(16, kv - j) : 0;
 }
 
 // ------------------------------------------------------------------- copies --
@@ -226,40 +250,42 @@ template <int D>
 __device__ void mma_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
   constexpr uint32_t kIdescS = Idesc<BN>::value, kIdescO = Idesc<D>::value;
   const uint32_t tmem = sm.tmem;
-  uint32_t n = 0, np[2] = {0, 0}, nq[2] = {0, 0};
+  uint32_t n = 0, nq0 = 0, nq1 = 0, np0 = 0, np1 = 0;
   auto qk = [&](int t, uint32_t blk) {
-    const uint32_t kb = smem_addr(&sm.k[blk % NK][0][0][0]);
+    const uint64_t kd = desc(smem_addr(&sm.k[blk % NK][0][0][0]), BN * 16);
+    const uint64_t qd = desc(smem_addr(&sm.q[t][0][0][0][0]), BM * 16);
 #pragma unroll
-    for (int term = 0; term < 2; ++term) {
-      const uint32_t qb = smem_addr(&sm.q[t][term][0][0][0]);
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s)
-        umma_f8(tmem + t * BN, desc(qb + s * 2 * BM * 16, BM * 16), desc(kb + s * 2 * BN * 16, BN * 16), kIdescS,
-                term + s > 0);
-    }
+    for (int s = 0; s < D / 16; ++s)  // both terms: 32 dims a step, 2 runs of 16 further each
+      umma_f8(tmem + t * BN, qd + s * (2 * BM * 16 >> 4), kd + (s & (D / 32 - 1)) * (2 * BN * 16 >> 4), kIdescS, s > 0);
     umma_commit(&sm.s_full[t]);
   };
   bool ok = true;
   while (ok && w.more()) {
     const Segment sg = w.segment(a);
+    if (sg.empty) {
+      w.advance(a, sg);
+      continue;
+    }
     const int nt = sg.rows > BM ? 2 : 1, nb = sg.blk1 - sg.blk0;
-    for (int t = 0; ok && t < nt; ++t) ok = wait_lane(x, &sm.q_full[t], nq[t]++ & 1);
+    ok = wait_lane(x, &sm.q_full[0], nq0++ & 1) && (nt == 1 || wait_lane(x, &sm.q_full[1], nq1++ & 1));
     if (!ok || !(ok = wait_lane(x, &sm.k_full[n % NK], (n / NK) & 1))) break;
     tc_fence_after();
-    for (int t = 0; t < nt; ++t) qk(t, n);
+    qk(0, n);
+    if (nt == 2) qk(1, n);
     umma_commit(&sm.k_empty[n % NK]);
     for (int i = 0; ok && i < nb; ++i, ++n) {
       const uint32_t n1 = n + 1;
       if (i + 1 < nb && !(ok = wait_lane(x, &sm.k_full[n1 % NK], (n1 / NK) & 1))) break;
       if (!(ok = wait_lane(x, &sm.w_full[n % NW], (n / NW) & 1))) break;
-      const uint32_t vb = smem_addr(&sm.w[n % NW][0][0][0]);
-      for (int t = 0; t < nt; ++t) {
-        if (!(ok = wait_lane(x, &sm.p_full[t], np[t]++ & 1))) break;
+      const uint64_t vd = desc(smem_addr(&sm.w[n % NW][0][0][0]), D * 16);
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t) {
+        if (t == nt) break;
+        if (!(ok = wait_lane(x, &sm.p_full[t], (t ? np1++ : np0++) & 1))) break;
         tc_fence_after();
 #pragma unroll
         for (int s = 0; s < BN / 16; ++s)
-          umma_f16_ts(tmem + 2 * BN + t * D, tmem + t * BN + s * 8, desc(vb + s * 2 * D * 16, D * 16), kIdescO,
-                      i + s > 0);
+          umma_f16_ts(tmem + 2 * BN + t * D, tmem + t * BN + s * 8, vd + s * (2 * D * 16 >> 4), kIdescO, i + s > 0);
         if (i + 1 < nb)
           qk(t, n1);
         else
@@ -287,21 +313,23 @@ __device__ void widen_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x)
   while (ok && w.more()) {
     const Segment sg = w.segment(a);
     const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
+    int next = sg.empty ? 0 : group_tokens(c, table, w.s.kv, sg.blk0);
     for (int blk = sg.blk0; blk < sg.blk1; ++blk, ++n) {
-      const Groups g = load_groups(c, table, w.s.kv, sg.h, blk);
+      const int cur = next;
+      if (blk + 1 < sg.blk1) next = group_tokens(c, table, w.s.kv, blk + 1);
       // rows that hold no token may hold any bytes, e4m3's NaN among them: zeros
-      const bool tail = __any_sync(0xffffffffu, (threadIdx.x & 31) < 8 && g.have < 16);
+      const bool tail = __any_sync(0xffffffffu, cur < 16);
       if (!(ok = wait_warp(x, &sm.v_full[n % NV], (n / NV) & 1)) ||
           !(ok = wait_warp(x, &sm.w_empty[n % NW], ((n / NW) & 1) ^ 1)))
         break;
       const uint8_t* src = &sm.v[n % NV][0][0][0];
       uint8_t* dst = &sm.w[n % NW][0][0][0];
-#pragma unroll
+#pragma unroll 2
       for (int i = 0; i < BN / 16 * D / 128; ++i) {
         const int e = tid + 128 * i, run = e / D, d = e % D;
         uint4 v = *reinterpret_cast<const uint4*>(src + (size_t)e * 16);
         if (tail) {
-          const int have = __shfl_sync(0xffffffffu, g.have, run);
+          const int have = __shfl_sync(0xffffffffu, cur, run);
           v.x &= first_bytes(have);
           v.y &= first_bytes(have - 4);
           v.z &= first_bytes(have - 8);
@@ -321,69 +349,101 @@ __device__ void widen_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x)
 }
 
 // ------------------------------------------------------------------ softmax --
-__device__ __forceinline__ void load_q8(const __nv_bfloat16* p, bool vec, float* y) {
-  if (vec) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      y[2 * j] = __uint_as_float(u[j] << 16);
-      y[2 * j + 1] = __uint_as_float(u[j] & 0xFFFF0000u);
+// The warp's 32 query rows of tile t -> two e4m3 terms in shared memory; returns
+// the multiplier of the scores of row 32 (warp % 4) + lane. Consecutive lanes
+// read consecutive dims of a row (8 each), loads of the next
+// rows in flight.
+template <int D>
+__device__ float stage_q(const AttnArgs& a, Smem<D>& sm, int t, const KvSeq& s, int h, const RowMap& map, int rows) {
+  constexpr int kLanes = D / 8, kPer = 32 / kLanes, kIt = 32 / kPer;  // lanes of a row, rows at a time
+  constexpr int kB = 4;                                               // such steps worked on together
+  const int lane = threadIdx.x & 31, r0 = threadIdx.x & 96;
+  const int sub = lane % kLanes, first = t * BM + r0 + lane / kLanes;
+  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(a.q.p) + (int64_t)s.first * a.q.ts +
+                            (int64_t)(h * a.c.group) * a.q.hs + 8 * sub;
+  uint4 v[kB];
+  auto load = [&](int i) {
+    uint4 q = make_uint4(0u, 0u, 0u, 0u);
+    const int r = first + kPer * i;
+    if (r < rows) {
+      int tok, head;
+      map.at(r, &tok, &head);
+      const __nv_bfloat16* p = qp + (int64_t)tok * a.q.ts + (int64_t)head * a.q.hs;
+      if (reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+        q = __ldg(reinterpret_cast<const uint4*>(p));
+      } else {
+        const uint16_t* u = reinterpret_cast<const uint16_t*>(p);
+        q = make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16,
+                       u[6] | (uint32_t)u[7] << 16);
+      }
     }
-  } else {
+    return q;
+  };
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = __bfloat162float(p[j]);
+  for (int j = 0; j < kB; ++j) v[j] = load(j);
+  float rm = 0.0f;
+#pragma unroll 1
+  for (int i0 = 0; i0 < kIt; i0 += kB) {
+    float y[kB][8], amax[kB];
+#pragma unroll
+    for (int b = 0; b < kB; ++b) {
+      const uint32_t w[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+      amax[b] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        y[b][2 * j] = __uint_as_float(w[j] << 16);
+        y[b][2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        amax[b] = fmax_nan(amax[b], fmax_nan(fabsf(y[b][2 * j]), fabsf(y[b][2 * j + 1])));
+      }
+    }
+    if (i0 + kB < kIt) {
+#pragma unroll
+      for (int b = 0; b < kB; ++b) v[b] = load(i0 + kB + b);
+    }
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1)
+#pragma unroll
+      for (int b = 0; b < kB; ++b) amax[b] = fmax_nan(amax[b], __shfl_xor_sync(0xffffffffu, amax[b], o));
+#pragma unroll
+    for (int b = 0; b < kB; ++b) {
+      // the row times 2^up has its largest element in [2^7, 2^8)
+      const int ex = (int)(__float_as_uint(amax[b]) >> 23) - 127;
+      const int up = min(max(7 - ex, -120), 100);
+      const float f = a.score_mul < 0.0f ? -pow2f(up) : pow2f(up);
+      const float mul = amax[b] < INFINITY ? fabsf(a.score_mul) * pow2f(-up) : __int_as_float(0x7FC00000);
+      const float got = __shfl_sync(0xffffffffu, mul, (lane % kPer) * kLanes);
+      if (lane / kPer == i0 + b) rm = got;
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = __fmul_rn(y[b][4 * j + e], f);
+        const uint32_t h0 = e4m3x2(z[0], z[1]), h1 = e4m3x2(z[2], z[3]);
+        const uint32_t w0 = e4m3x2_half2(h0), w1 = e4m3x2_half2(h1);
+        const float2 b0 = __half22float2(*reinterpret_cast<const __half2*>(&w0));
+        const float2 b1 = __half22float2(*reinterpret_cast<const __half2*>(&w1));
+        hi[j] = h0 | (h1 << 16);
+        lo[j] = e4m3x2(__fsub_rn(z[0], b0.x), __fsub_rn(z[1], b0.y)) |
+                (e4m3x2(__fsub_rn(z[2], b1.x), __fsub_rn(z[3], b1.y)) << 16);
+      }
+      const int r = r0 + kPer * (i0 + b) + lane / kLanes;
+      *reinterpret_cast<uint2*>(&sm.q[t][0][sub >> 1][r][8 * (sub & 1)]) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(&sm.q[t][1][sub >> 1][r][8 * (sub & 1)]) = make_uint2(lo[0], lo[1]);
+    }
   }
+  return rm;
 }
 
-// Row r of tile t -> its query row as two e4m3 terms in shared memory; returns
-// the multiplier of its scores.
+// Finished rows go to the output through the tile's query staging, free once its
+// products are done, so that consecutive lanes write consecutive dims.
 template <int D>
-__device__ float stage_q(const AttnArgs& a, Smem<D>& sm, int t, int r, const __nv_bfloat16* p) {
-  const bool vec = reinterpret_cast<uintptr_t>(p) % 16 == 0;
-  float amax = 0.0f;
-  if (p != nullptr) {
-#pragma unroll 4
-    for (int i = 0; i < D / 8; ++i) {
-      float y[8];
-      load_q8(p + 8 * i, vec, y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) amax = fmax_nan(amax, fabsf(y[j]));
-    }
+struct RowStage {
+  // 16-byte units of a row, rotated by the row against bank conflicts
+  __device__ __forceinline__ static uint4* at(Smem<D>& sm, int t, int r, int unit) {
+    return reinterpret_cast<uint4*>(&sm.q[t][0][0][0][0]) + r * (D / 8) + ((unit + r) & (D / 8 - 1));
   }
-  // the row times 2^up has its largest element in [2^7, 2^8)
-  const int ex = (int)(__float_as_uint(amax) >> 23) - 127;
-  const int up = min(max(7 - ex, -120), 100);
-  const float f = a.score_mul < 0.0f ? -pow2f(up) : pow2f(up);
-#pragma unroll 2
-  for (int i = 0; i < D / 16; ++i) {
-    uint32_t hi[4], lo[4];
-    float xs[16];
-    if (p != nullptr) {
-      load_q8(p + 16 * i, vec, xs);
-      load_q8(p + 16 * i + 8, vec, xs + 8);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) xs[j] = 0.0f;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = __fmul_rn(xs[4 * j + e], f);
-      const uint32_t h0 = e4m3x2(y[0], y[1]), h1 = e4m3x2(y[2], y[3]);
-      const uint32_t w0 = e4m3x2_half2(h0), w1 = e4m3x2_half2(h1);
-      const float2 b0 = __half22float2(*reinterpret_cast<const __half2*>(&w0));
-      const float2 b1 = __half22float2(*reinterpret_cast<const __half2*>(&w1));
-      hi[j] = h0 | (h1 << 16);
-      lo[j] = e4m3x2(__fsub_rn(y[0], b0.x), __fsub_rn(y[1], b0.y)) |
-              (e4m3x2(__fsub_rn(y[2], b1.x), __fsub_rn(y[3], b1.y)) << 16);
-    }
-    *reinterpret_cast<uint4*>(&sm.q[t][0][i][r][0]) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4*>(&sm.q[t][1][i][r][0]) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-  }
-  return amax < INFINITY ? fabsf(a.score_mul) * pow2f(-up) : __int_as_float(0x7FC00000);
-}
+};
 
 template <int D>
 __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
@@ -397,16 +457,16 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
   for (; w.more();) {
     const Segment sg = w.segment(a);
     const KvSeq s = w.s;
-    if (sg.rows <= t * BM) {  // this tile has no row
+    if (sg.empty || sg.rows <= t * BM) {  // nothing here, or no row in this tile
       w.advance(a, sg);
       continue;
     }
     const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
-    const int row = w.t * kRows + t * BM + r;
+    const RowMap map(c, w.t * kRows);
     const bool have = t * BM + r < sg.rows;
-    const int tok = row / c.group, head = sg.h * c.group + row % c.group;
-    const float rm = stage_q<D>(a, sm, t, r, have ? static_cast<const __nv_bfloat16*>(a.q.p) + (int64_t)(s.first + tok) * a.q.ts +
-                                                        (int64_t)head * a.q.hs : nullptr);
+    int tok, head;
+    map.at(t * BM + r, &tok, &head);
+    const float rm = stage_q<D>(a, sm, t, s, sg.h, map, sg.rows);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     mbar_arrive(&sm.q_full[t]);
     const int lim = !have ? INT32_MAX : (a.causal ? s.kv - s.n + tok : s.kv - 1);
@@ -421,37 +481,34 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
       if (blk + 1 < sg.blk1) g = load_groups(c, table, s.kv, sg.h, blk + 1);
       const bool masked = blk * BN + BN - 1 > lim_min || __any_sync(0xffffffffu, lane < 8 && cur.have < 16);
       const int col = lim == INT32_MAX ? BN : lim - blk * BN;  // last column this row sees
-      // lane i < 8: the scale of group i's keys, the exponent and unscaling of its values
-      const float gk = cur.ek == kExpNan ? nan : pow2f(cur.ek);
-      const float ge = cur.ev == kExpNan ? nan : (float)cur.ev;
-      const float gu = cur.ev == kExpNan ? nan : pow2f(-cur.ev);
+      float4* gc = sm.group_of[warp][blk & 1];
+      if (lane < 8)
+        gc[lane] = make_float4(pow2f(cur.ek), cur.ek == kExpNan || cur.ev == kExpNan ? nan : (float)cur.ev,
+                               pow2f(-cur.ev), __int_as_float(cur.have));
+      __syncwarp();
       if (!wait_warp(x, &sm.s_full[t], ns++ & 1)) return;
       tc_fence_after();
 
-      // ---- maximum
+      // ---- the row of S, and its maximum
+      float v[BN];
+#pragma unroll
+      for (int i = 0; i < BN / 16; ++i) tmem_ld16(ts + 16 * i, v + 16 * i);
+      tmem_wait_ld(v);
+#pragma unroll
+      for (int i = 1; i < BN / 16; ++i) tmem_tie(v + 16 * i);
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int lc = min(col - 16 * i, __float_as_int(gc[i].w) - 1);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[16 * i + j] = j <= lc ? v[16 * i + j] : -INFINITY;
+        }
+      }
       float mx = -INFINITY;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[32];
-        tmem_ld16(ts + 32 * q, v);
-        tmem_ld16(ts + 32 * q + 16, v + 16);
-        tmem_wait_ld(v);
-        tmem_tie(v + 16);
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const int gi = 2 * q + hf;
-          const float k = __fmul_rn(rm, __shfl_sync(0xffffffffu, gk, gi)), e = __shfl_sync(0xffffffffu, ge, gi);
-          float raw = -INFINITY;
-          if (masked) {
-            const int lc = min(col, 16 * gi + __shfl_sync(0xffffffffu, cur.have, gi) - 1);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) raw = 16 * gi + j <= lc ? fmaxf(raw, v[16 * hf + j]) : raw;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) raw = fmaxf(raw, v[16 * hf + j]);
-          }
-          mx = fmaxf(mx, __fmaf_rn(raw, k, e));
-        }
+      for (int i = 0; i < 8; ++i) {
+        const float4 k = gc[i];
+        mx = fmaxf(mx, __fmaf_rn(max16(v + 16 * i), fmaxf(__fmul_rn(rm, k.x), kTiny), k.y));
       }
 
       // ---- running maximum; O and l follow when it grew by more than 2^kGrow
@@ -462,56 +519,46 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
         l = __fmul_rn(l, f);
         m = mn;
         if (blk > sg.blk0) {
+#pragma unroll 1
+          for (int q = 0; q < D / 16; ++q) {
+            float o[16];
+            tmem_ld16(to + 16 * q, o);
+            tmem_wait_ld(o);
+            uint32_t b[16];
 #pragma unroll
-          for (int q = 0; q < D / 32; ++q) {
-            float v[32];
-            tmem_ld16(to + 32 * q, v);
-            tmem_ld16(to + 32 * q + 16, v + 16);
-            tmem_wait_ld(v);
-            tmem_tie(v + 16);
-            uint32_t b[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) b[j] = __float_as_uint(__fmul_rn(v[j], f));
-            tmem_st16(to + 32 * q, b);
-            tmem_st16(to + 32 * q + 16, b + 16);
+            for (int j = 0; j < 16; ++j) b[j] = __float_as_uint(__fmul_rn(o[j], f));
+            tmem_st16(to + 16 * q, b);
           }
         }
       }
-      const float off = kPBits - (m == -INFINITY ? 0.0f : m);
+      const float off = rm < INFINITY ? kPBits - (m == -INFINITY ? 0.0f : m) : nan;
 
-      // ---- weights
+      // ---- weights (a marked block or a query that is not finite: NaN through e)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[32];
-        tmem_ld16(ts + 32 * q, v);
-        tmem_ld16(ts + 32 * q + 16, v + 16);
-        tmem_wait_ld(v);
-        tmem_tie(v + 16);
-        uint32_t b[16];
+      for (int i = 0; i < 8; ++i) {
+        const float4 k = gc[i];
+        const float kx = fmaxf(__fmul_rn(rm, k.x), kTiny);
+        float e = __fadd_rn(k.y, off);
+        if (masked && min(col - 16 * i, __float_as_int(k.w) - 1) < 0) e = 0.0f;  // hidden: -inf whatever the block
+        float2 p[8];
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const int gi = 2 * q + hf;
-          const float k = __fmul_rn(rm, __shfl_sync(0xffffffffu, gk, gi));
-          const float e = __fadd_rn(__shfl_sync(0xffffffffu, ge, gi), off);
-          const float un = __shfl_sync(0xffffffffu, gu, gi);
-          const int lc = min(col, 16 * gi + __shfl_sync(0xffffffffu, cur.have, gi) - 1);
-          float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll
-          for (int j = 0; j < 16; j += 2) {
-            const float2 y = __ffma2_rn(make_float2(v[16 * hf + j], v[16 * hf + j + 1]), make_float2(k, k), make_float2(e, e));
-            float2 p = make_float2(ex2(y.x), ex2(y.y));
-            if (masked) {
-              p.x = 16 * gi + j <= lc ? p.x : 0.0f;
-              p.y = 16 * gi + j + 1 <= lc ? p.y : 0.0f;
-            }
-            sum = __fadd2_rn(sum, p);
-            const __half2 hp = __floats2half2_rn(p.x, p.y);
-            b[8 * hf + j / 2] = *reinterpret_cast<const uint32_t*>(&hp);
-          }
-          const float sg1 = __fadd_rn(sum.x, sum.y);
-          l = sg1 == 0.0f ? l : __fmaf_rn(sg1, un, l);
+        for (int j = 0; j < 8; ++j) {
+          const float2 y = __ffma2_rn(make_float2(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]), make_float2(kx, kx),
+                                      make_float2(e, e));
+          p[j] = make_float2(ex2(y.x), ex2(y.y));
         }
-        tmem_st16(ts + 16 * q, b);  // P over columns of S already read
+        uint32_t h[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const __half2 hp = __floats2half2_rn(p[j].x, p[j].y);
+          h[j] = *reinterpret_cast<const uint32_t*>(&hp);
+        }
+        tmem_st8(ts + 8 * i, h);  // P over S, which is in registers
+        const float2 s0 = __fadd2_rn(__fadd2_rn(p[0], p[1]), __fadd2_rn(p[2], p[3]));
+        const float2 s1 = __fadd2_rn(__fadd2_rn(p[4], p[5]), __fadd2_rn(p[6], p[7]));
+        const float2 s2 = __fadd2_rn(s0, s1);
+        const float sum = __fadd_rn(s2.x, s2.y);
+        l = sum == 0.0f ? l : __fmaf_rn(sum, k.z, l);
       }
       st_wait();
       tc_fence_before();
@@ -522,34 +569,50 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
     if (!wait_warp(x, &sm.o_full[t], no++ & 1)) return;
     tc_fence_after();
     float* slot = partial_slot(a, blockIdx.x, sg.c0) + (int64_t)t * BM * (D + 2) + r;
-    __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(s.first + tok) * a.out.ts + (int64_t)head * a.out.hs;
-    auto put = [&](int d, const float* o, float inv) {  // 8 dims of a finished row
+    auto put = [&](int d, const float* o, float inv) {  // 8 dims of a finished row to the staging
       uint32_t b[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const __nv_bfloat162 hb = __floats2bfloat162_rn(__fmul_rn(o[2 * j], inv), __fmul_rn(o[2 * j + 1], inv));
         b[j] = *reinterpret_cast<const uint32_t*>(&hb);
       }
-      if (reinterpret_cast<uintptr_t>(op) % 16 == 0) {
-        *reinterpret_cast<uint4*>(op + d) = make_uint4(b[0], b[1], b[2], b[3]);
-      } else {
-        uint16_t* o16 = reinterpret_cast<uint16_t*>(op + d);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o16[j] = (uint16_t)(b[j >> 1] >> (16 * (j & 1)));
-      }
+      *RowStage<D>::at(sm, t, r, d / 8) = make_uint4(b[0], b[1], b[2], b[3]);
     };
-    auto put_lse = [&](float mm, float ll) {
-      if (a.lse) a.lse[(int64_t)(s.first + tok) * c.n_heads + head] = ll == 0.0f ? -INFINITY : (mm - kPBits + log2f(ll)) * kLn2;
+    auto flush = [&](float mm, float ll) {  // the warp's staged rows to the output
+      if (have && a.lse)
+        a.lse[(int64_t)(s.first + tok) * c.n_heads + sg.h * c.group + head] = ll == 0.0f ? -INFINITY : (mm - kPBits + log2f(ll)) * kLn2;
+      __syncwarp();
+      constexpr int kLanes = D / 8, kPer = 32 / kLanes;
+#pragma unroll 4
+      for (int i = 0; i < 32 / kPer; ++i) {
+        const int rr = (r & 96) + kPer * i + lane / kLanes, sub = lane % kLanes;
+        if (t * BM + rr < sg.rows) {
+          int tok2, head2;
+          map.at(t * BM + rr, &tok2, &head2);
+          __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(s.first + tok2) * a.out.ts +
+                              (int64_t)(sg.h * c.group + head2) * a.out.hs + 8 * sub;
+          const uint4 v = *RowStage<D>::at(sm, t, rr, sub);
+          if (reinterpret_cast<uintptr_t>(op) % 16 == 0) {
+            *reinterpret_cast<uint4*>(op) = v;
+          } else {
+            const uint32_t b[4] = {v.x, v.y, v.z, v.w};
+            uint16_t* o16 = reinterpret_cast<uint16_t*>(op);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o16[j] = (uint16_t)(b[j >> 1] >> (16 * (j & 1)));
+          }
+        }
+      }
+      __syncwarp();
     };
     const float inv = l == 0.0f ? 0.0f : __frcp_rn(l);
-#pragma unroll
+#pragma unroll 1
     for (int q = 0; q < D / 32; ++q) {
       float v[32];
       tmem_ld16(to + 32 * q, v);
       tmem_ld16(to + 32 * q + 16, v + 16);
       tmem_wait_ld(v);
       tmem_tie(v + 16);
-      if (have && sg.whole) {
+      if (sg.whole) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) put(32 * q + 8 * j, v + 8 * j, inv);
       } else if (have) {
@@ -559,7 +622,7 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
     }
     tc_fence_before();
     if (sg.whole) {
-      if (have) put_lse(m, l);
+      flush(m, l);
     } else {
       if (have) {
         slot[D * BM] = m;
@@ -577,7 +640,7 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
       }
       mbar_arrive(&sm.group[t]);
       if (!wait_warp(x, &sm.group[t], ng++ & 1)) return;
-      if (*(volatile int*)&sm.last[t] && have) {
+      if (*(volatile int*)&sm.last[t]) {
         __threadfence();
         const int64_t at = (int64_t)t * BM * (D + 2) + r;
         float mm = -INFINITY;
@@ -589,21 +652,30 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
           ll = __fmaf_rn(__ldcg(sp + (D + 1) * BM), ex2(__fsub_rn(__ldcg(sp + D * BM), base)), ll);
         }
         const float iv = ll == 0.0f ? 0.0f : __frcp_rn(ll);
-        for (int d = 0; d < D; d += 8) {
-          float o[8];
+        constexpr int kD = 16;  // dims at a time, their loads in flight together
+        for (int d = 0; d < D; d += kD) {
+          float o[kD];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] = 0.0f;
+          for (int j = 0; j < kD; ++j) o[j] = 0.0f;
+#pragma unroll 2
           for (int k = sg.c0; k <= sg.c1; ++k) {
             const float* sp = partial_slot(a, k, sg.c0) + at;
             const float f = ex2(__fsub_rn(__ldcg(sp + D * BM), base));
+            float y[kD];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = __fmaf_rn(__ldcg(sp + (d + j) * BM), f, o[j]);
+            for (int j = 0; j < kD; ++j) y[j] = __ldcg(sp + (d + j) * BM);
+#pragma unroll
+            for (int j = 0; j < kD; ++j) o[j] = __fmaf_rn(y[j], f, o[j]);
           }
-          put(d, o, iv);
+#pragma unroll
+          for (int j = 0; j < kD; j += 8) put(d + j, o + j, iv);
         }
-        put_lse(mm, ll);
+        flush(mm, ll);
       }
     }
+    // the staging is the next tile's query operand, which the warps fill together
+    mbar_arrive(&sm.group[t]);
+    if (!wait_warp(x, &sm.group[t], ng++ & 1)) return;
     w.advance(a, sg);
   }
 }
@@ -642,14 +714,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
   tc_fence_after();
   const Ctx x{a.wait_ns, a.c.status, &sm.dead};
   if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     softmax_role<D>(a, w, sm, x);
-  } else if (warp < kMmaWarp) {
-    widen_role<D>(a, w, sm, x);
-  } else if (warp == kMmaWarp) {
-    if ((threadIdx.x & 31) == 0) mma_role<D>(a, w, sm, x);
-    __syncwarp();
   } else {
-    load_role<D>(a, w, sm, x);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp < kMmaWarp) {
+      widen_role<D>(a, w, sm, x);
+    } else if (warp == kMmaWarp) {
+      if ((threadIdx.x & 31) == 0) mma_role<D>(a, w, sm, x);
+      __syncwarp();
+    } else if (warp == kLoadWarp) {
+      load_role<D>(a, w, sm, x);
+    }
   }
   tc_fence_before();
   __syncthreads();
