@@ -155,8 +155,9 @@ awsrc_status awsrc_paged_attention(const awsrc_kv_cache* cache, const awsrc_kv_b
   a.wait_ns = wait_limit_ns();
   a.stall = wait_test_stall();
   // BF16 with more rows per kv head than the row kernel takes in one warp tile
-  // goes to the tensor-memory kernel
-  const bool tiles = q->dtype == AWSRC_DTYPE_BF16 && (int64_t)batch->max_new * a.c.group > 16;
+  // goes to the tensor-memory kernel, which reads and writes rows in vectors
+  const bool tiles = q->dtype == AWSRC_DTYPE_BF16 && (int64_t)batch->max_new * a.c.group > 16 &&
+                     rows_aligned(a.q, 2) && rows_aligned(a.out, 2);
   a.slot_floats = tiles ? L.tile_slot : L.row_slot;
   const cudaError_t e = tiles ? launch_paged_tiles(a, cache->head_dim, batch->max_kv, (cudaStream_t)stream)
                               : launch_paged_rows(a, cache->head_dim, q->dtype, batch->max_new, batch->max_kv,

@@ -417,10 +417,6 @@ cudaError_t launch(const AppendArgs& a, bool vec, int64_t blocks, cudaStream_t s
   return cudaGetLastError();
 }
 
-bool rows_aligned(const KvRows& r, size_t elt) {
-  return (reinterpret_cast<uintptr_t>(r.p) | (uintptr_t)(r.ts * (int64_t)elt) | (uintptr_t)(r.hs * (int64_t)elt)) % 16 == 0;
-}
-
 }  // namespace
 
 cudaError_t launch_kv_append(const KvArgs& c, int head_dim, int dtype, const KvRows& q, const KvRows& k,

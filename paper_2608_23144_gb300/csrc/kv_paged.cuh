@@ -17,6 +17,11 @@ struct KvRows {  // [token][head][dim], strides in elements
   int64_t ts, hs;
 };
 
+// Every row of r (elements of elt bytes) starts on a 16-byte boundary.
+inline bool rows_aligned(const KvRows& r, size_t elt) {
+  return (reinterpret_cast<uintptr_t>(r.p) | (uintptr_t)(r.ts * (int64_t)elt) | (uintptr_t)(r.hs * (int64_t)elt)) % 16 == 0;
+}
+
 struct KvArgs {
   uint8_t *k, *v;
   int8_t *k_exp, *v_exp;

@@ -19,8 +19,8 @@
 //
 // One thread block per SM and 256 rows (query tokens x the heads of a kv head)
 // in two tiles of 128, so that one tile's softmax runs under the other's
-// products. Warps 0-3 and 4-7: softmax, one row per thread; 8-11: widening; 12:
-// MMA issue; 13: bulk copies (14, 15 idle). Tensor memory: S 2 x 128 columns, over whose
+// products. Warps 0-3 and 4-7: softmax, one row per thread; 8-11: widening; 12
+// and 13: MMA issue; 14: bulk copies (15 idle). Tensor memory: S 2 x 128 columns, over whose
 // first 64 P is written; O 2 x D columns. Per tile and block of 128 tokens:
 //   MMA:     P ready -> O += P V; S = Q K of the next block -> commit
 //   softmax: S ready -> m, P, l; O rescaled by its own threads, only when a row
@@ -48,11 +48,10 @@ using namespace tc05;
 constexpr int BM = 128, BN = 128;
 constexpr int kRows = 2 * BM;
 constexpr int kThreads = 512;
-constexpr int kMmaWarp = 12, kLoadWarp = 13;
+constexpr int kMmaWarp = 12, kLoadWarp = 14, kWalkWarp = 15;
+constexpr int kRing = 4, kReaders = 15;  // segments handed out ahead; warps that read them
 constexpr int NK = 3, NV = 2, NW = 2;  // stages: keys, value codes, widened values
 constexpr uint32_t kTmemCols = 512;
-// Registers per thread by role: 512 x 128 at launch = 256 x 184 + 256 x 72.
-constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPBits = 6.0f;         // p is at most 2^6 when m is the maximum,
 constexpr float kTiny = 1e-37f;        // least score multiplier: hidden scores of -inf stay -inf
@@ -63,14 +62,22 @@ using Walk = UnitWalk<kRows, BN, 4, kOver>;
 template <int N>
 struct Idesc { static constexpr uint32_t value = idesc_f16(BM, N); };  // formats 0: e4m3, binary16
 
+// A segment as the roles read it: blocks [blk0, blk1) of kv head h for the query
+// rows [row0, row0 + rows) of sequence b; b < 0 ends the walk.
+struct SegRec {
+  int b, h, blk0, blk1, row0, rows, first, n, kv, c0, c1, whole;
+};
+
 template <int D>
 struct Smem {
-  uint8_t q[2][2][D / 16][BM][16];  // tile, term, 16 dims
+  uint8_t q[2][2][D / 16][BM + 1][16];  // tile, term, 16 dims; runs one row apart in the banks
   uint8_t k[NK][D / 16][BN][16];
   uint8_t v[NV][BN / 16][D][16];
   uint8_t w[NW][BN / 8][D][16];     // binary16, 8 tokens
   unsigned long long k_full[NK], k_empty[NK], v_full[NV], v_empty[NV], w_full[NW], w_empty[NW];
-  unsigned long long q_full[2], s_full[2], p_full[2], o_full[2], group[2], drain;
+  unsigned long long q_full[2], s_full[2], p_full[2], o_full[2], group[2], turn[2], drain[2];
+  unsigned long long seg_full[kRing], seg_empty[kRing];
+  SegRec seg[kRing];
   float4 group_of[8][2][8];  // softmax warp, block parity: scale of the keys, exponent and unscaling of the values, tokens
   uint32_t tmem;
   int dead, last[2];
@@ -84,7 +91,7 @@ struct Ctx {
 
 // Bounded wait of a whole warp; false, for all lanes, once any wait of the
 // block has given up.
-__device__ __forceinline__ bool wait_slow(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+__device__ __noinline__ bool wait_slow(const Ctx& x, unsigned long long* mb, uint32_t parity) {
   const uint64_t t0 = globaltimer();
   bool ok;
   for (;;) {
@@ -188,17 +195,40 @@ __device__ __forceinline__ int group_tokens(const KvArgs& c, const int32_t* tabl
   return pg >= 0 && pg < c.n_pages ? min(16, kv - j) : 0;
 }
 
+// --------------------------------------------------------------------- walk --
+// One lane walks the share and hands the segments to the roles through a ring,
+// so that the walk's divisions are in one place and in nobody's way.
+template <int D>
+__device__ __noinline__ void walk_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
+  uint32_t i = 0;
+  for (; w.more();) {
+    const Segment g = w.segment(a);
+    if (!g.empty) {
+      if (!wait_lane(x, &sm.seg_empty[i % kRing], ((i / kRing) & 1) ^ 1)) return;
+      sm.seg[i % kRing] = SegRec{w.b, g.h, g.blk0, g.blk1, w.t * kRows, g.rows, w.s.first, w.s.n, w.s.kv, g.c0, g.c1, g.whole};
+      mbar_arrive(&sm.seg_full[i % kRing]);
+      ++i;
+    }
+    w.advance(a, g);
+  }
+  if (!wait_lane(x, &sm.seg_empty[i % kRing], ((i / kRing) & 1) ^ 1)) return;
+  sm.seg[i % kRing].b = -1;
+  mbar_arrive(&sm.seg_full[i % kRing]);
+}
+
 // ------------------------------------------------------------------- copies --
 template <int D>
-__device__ void load_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
+__device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
   const KvArgs& c = a.c;
   const int lane = threadIdx.x & 31;
   const int per = BN >> c.log_page;  // pages of a block
-  uint32_t n = 0;
+  uint32_t n = 0, is = 0;
   bool ok = true;
-  while (ok && w.more()) {
-    const Segment sg = w.segment(a);
-    const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
+  for (; ok; ++is) {
+    if (!(ok = wait_warp(x, &sm.seg_full[is % kRing], (is / kRing) & 1))) break;
+    const SegRec& sg = sm.seg[is % kRing];
+    if (sg.b < 0) break;
+    const int32_t* table = c.table + (int64_t)sg.b * c.table_stride;
     for (int blk = sg.blk0; ok && blk < sg.blk1; ++blk, ++n) {
       if ((int)n == a.stall) {  // the limit's test
         ok = false;
@@ -207,7 +237,7 @@ __device__ void load_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) 
       // lane i < per: page i of the block
       int pg = -1;
       const int j = blk * BN + (lane << c.log_page);
-      if (lane < per && j < w.s.kv) {
+      if (lane < per && j < sg.kv) {
         pg = __ldg(table + (j >> c.log_page));
         if (pg < 0 || pg >= c.n_pages) {
           atomicOr(c.status, kFaultBatch);
@@ -237,7 +267,8 @@ __device__ void load_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) 
                  &sm.v_full[vs]);
       __syncwarp();
     }
-    if (ok) w.advance(a, sg);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.seg_empty[is % kRing]);
   }
   if (!ok && lane == 0) {  // copies in flight land before the block ends
     for (uint32_t j = n > NK ? n - NK : 0; j < n; ++j) (void)mbar_wait(&sm.k_full[j % NK], (j / NK) & 1, x.wait_ns);
@@ -246,77 +277,95 @@ __device__ void load_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) 
 }
 
 // ----------------------------------------------------------------- products --
+// One warp issues the products of tile t, so that its waits pass under the other
+// tile's products. The two take turns, a block's products at a time: left to
+// interleave, both tiles' products ended together and so did their softmax.
 template <int D>
-__device__ void mma_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
+__device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
   constexpr uint32_t kIdescS = Idesc<BN>::value, kIdescO = Idesc<D>::value;
-  const uint32_t tmem = sm.tmem;
-  uint32_t n = 0, nq0 = 0, nq1 = 0, np0 = 0, np1 = 0;
-  auto qk = [&](int t, uint32_t blk) {
-    const uint64_t kd = desc(smem_addr(&sm.k[blk % NK][0][0][0]), BN * 16);
-    const uint64_t qd = desc(smem_addr(&sm.q[t][0][0][0][0]), BM * 16);
+  const uint32_t ts = sm.tmem + t * BN, to = sm.tmem + 2 * BN + t * D;
+  const uint64_t q0 = desc(smem_addr(&sm.q[t][0][0][0][0]), (BM + 1) * 16);
+  const uint64_t k0 = desc(smem_addr(&sm.k[0][0][0][0]), BN * 16);
+  const uint64_t v0 = desc(smem_addr(&sm.w[0][0][0][0]), D * 16);
+  uint32_t n = 0, nq = 0, np = 0, turns = 0, is = 0;
+  // tile 0 has the first turn
+  auto my_turn = [&]() {
+    const uint32_t k = turns++;
+    return t == 0 ? k == 0 || wait_lane(x, &sm.turn[0], (k - 1) & 1) : wait_lane(x, &sm.turn[1], k & 1);
+  };
+  auto qk = [&](uint32_t blk) {
+    const uint64_t kd = k0 + (uint64_t)(blk % NK) * (sizeof(sm.k[0]) >> 4);
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)  // both terms: 32 dims a step, 2 runs of 16 further each
-      umma_f8(tmem + t * BN, qd + s * (2 * BM * 16 >> 4), kd + (s & (D / 32 - 1)) * (2 * BN * 16 >> 4), kIdescS, s > 0);
+      umma_f8(ts, q0 + s * (2 * (BM + 1) * 16 >> 4), kd + (s & (D / 32 - 1)) * (2 * BN * 16 >> 4), kIdescS, s > 0);
     umma_commit(&sm.s_full[t]);
+    umma_commit(&sm.k_empty[blk % NK]);
   };
   bool ok = true;
-  while (ok && w.more()) {
-    const Segment sg = w.segment(a);
-    if (sg.empty) {
-      w.advance(a, sg);
-      continue;
-    }
-    const int nt = sg.rows > BM ? 2 : 1, nb = sg.blk1 - sg.blk0;
-    ok = wait_lane(x, &sm.q_full[0], nq0++ & 1) && (nt == 1 || wait_lane(x, &sm.q_full[1], nq1++ & 1));
-    if (!ok || !(ok = wait_lane(x, &sm.k_full[n % NK], (n / NK) & 1))) break;
-    tc_fence_after();
-    qk(0, n);
-    if (nt == 2) qk(1, n);
-    umma_commit(&sm.k_empty[n % NK]);
-    for (int i = 0; ok && i < nb; ++i, ++n) {
-      const uint32_t n1 = n + 1;
-      if (i + 1 < nb && !(ok = wait_lane(x, &sm.k_full[n1 % NK], (n1 / NK) & 1))) break;
-      if (!(ok = wait_lane(x, &sm.w_full[n % NW], (n / NW) & 1))) break;
-      const uint64_t vd = desc(smem_addr(&sm.w[n % NW][0][0][0]), D * 16);
-#pragma unroll 1
-      for (int t = 0; t < 2; ++t) {
-        if (t == nt) break;
-        if (!(ok = wait_lane(x, &sm.p_full[t], (t ? np1++ : np0++) & 1))) break;
+  for (; ok; ++is) {
+    if (!(ok = wait_lane(x, &sm.seg_full[is % kRing], (is / kRing) & 1))) break;
+    const SegRec& sg = sm.seg[is % kRing];
+    if (sg.b < 0) break;
+    const int nb = sg.blk1 - sg.blk0;
+    if (sg.rows <= t * BM) {  // no row in this tile: its blocks pass
+      if (!(ok = my_turn())) break;
+      mbar_arrive(&sm.turn[t ^ 1]);
+      for (int i = 0; ok && i < nb; ++i, ++n) {
+        if (!(ok = wait_lane(x, &sm.k_full[n % NK], (n / NK) & 1))) break;
+        mbar_arrive(&sm.k_empty[n % NK]);
+        if (!(ok = wait_lane(x, &sm.w_full[n % NW], (n / NW) & 1))) break;
+        mbar_arrive(&sm.w_empty[n % NW]);
+        if (!(ok = my_turn())) break;
+        mbar_arrive(&sm.turn[t ^ 1]);
+      }
+    } else {
+      if (!(ok = wait_lane(x, &sm.q_full[t], nq++ & 1)) || !(ok = wait_lane(x, &sm.k_full[n % NK], (n / NK) & 1)) || !(ok = my_turn()))
+        break;
+      tc_fence_after();
+      qk(n);
+      mbar_arrive(&sm.turn[t ^ 1]);
+      for (int i = 0; i < nb; ++i, ++n) {
+        const uint32_t n1 = n + 1;
+        if (i + 1 < nb && !(ok = wait_lane(x, &sm.k_full[n1 % NK], (n1 / NK) & 1))) break;
+        if (!(ok = wait_lane(x, &sm.w_full[n % NW], (n / NW) & 1))) break;
+        const uint64_t vd = v0 + (uint64_t)(n % NW) * (sizeof(sm.w[0]) >> 4);
+        if (!(ok = wait_lane(x, &sm.p_full[t], np++ & 1)) || !(ok = my_turn())) break;
         tc_fence_after();
 #pragma unroll
         for (int s = 0; s < BN / 16; ++s)
-          umma_f16_ts(tmem + 2 * BN + t * D, tmem + t * BN + s * 8, vd + s * (2 * D * 16 >> 4), kIdescO, i + s > 0);
+          umma_f16_ts(to, ts + s * 8, vd + s * (2 * D * 16 >> 4), kIdescO, i + s > 0);
+        umma_commit(&sm.w_empty[n % NW]);
         if (i + 1 < nb)
-          qk(t, n1);
+          qk(n1);
         else
           umma_commit(&sm.o_full[t]);
+        mbar_arrive(&sm.turn[t ^ 1]);
       }
-      if (!ok) break;
-      umma_commit(&sm.w_empty[n % NW]);
-      if (i + 1 < nb) umma_commit(&sm.k_empty[n1 % NK]);
     }
-    if (ok) w.advance(a, sg);
+    mbar_arrive(&sm.seg_empty[is % kRing]);
   }
   if (!ok) {  // products in flight end before the block does
-    umma_commit(&sm.drain);
-    (void)mbar_wait(&sm.drain, 0, x.wait_ns);
+    umma_commit(&sm.drain[t]);
+    (void)mbar_wait(&sm.drain[t], 0, x.wait_ns);
   }
 }
 
 // ----------------------------------------------------------------- widening --
 template <int D>
-__device__ void widen_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
+__device__ void widen_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
   const KvArgs& c = a.c;
   const int tid = threadIdx.x & 127;
-  uint32_t n = 0;
+  uint32_t n = 0, is = 0;
   bool ok = true;
-  while (ok && w.more()) {
-    const Segment sg = w.segment(a);
-    const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
-    int next = sg.empty ? 0 : group_tokens(c, table, w.s.kv, sg.blk0);
+  for (; ok; ++is) {
+    if (!(ok = wait_warp(x, &sm.seg_full[is % kRing], (is / kRing) & 1))) break;
+    const SegRec& sg = sm.seg[is % kRing];
+    if (sg.b < 0) break;
+    const int32_t* table = c.table + (int64_t)sg.b * c.table_stride;
+    int next = group_tokens(c, table, sg.kv, sg.blk0);
     for (int blk = sg.blk0; blk < sg.blk1; ++blk, ++n) {
       const int cur = next;
-      if (blk + 1 < sg.blk1) next = group_tokens(c, table, w.s.kv, blk + 1);
+      if (blk + 1 < sg.blk1) next = group_tokens(c, table, sg.kv, blk + 1);
       // rows that hold no token may hold any bytes, e4m3's NaN among them: zeros
       const bool tail = __any_sync(0xffffffffu, cur < 16);
       if (!(ok = wait_warp(x, &sm.v_full[n % NV], (n / NV) & 1)) ||
@@ -344,109 +393,193 @@ __device__ void widen_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x)
       mbar_arrive(&sm.w_full[n % NW]);
       mbar_arrive(&sm.v_empty[n % NV]);
     }
-    if (ok) w.advance(a, sg);
+    __syncwarp();
+    if ((tid & 31) == 0) mbar_arrive(&sm.seg_empty[is % kRing]);
   }
 }
 
 // ------------------------------------------------------------------ softmax --
+__device__ __forceinline__ uint32_t e4m3x2_h(__half2 v) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t*>(&v)));
+  return r;
+}
+
 // The warp's 32 query rows of tile t -> two e4m3 terms in shared memory; returns
 // the multiplier of the scores of row 32 (warp % 4) + lane. Consecutive lanes
 // read consecutive dims of a row (8 each), loads of the next
 // rows in flight.
 template <int D>
-__device__ float stage_q(const AttnArgs& a, Smem<D>& sm, int t, const KvSeq& s, int h, const RowMap& map, int rows) {
+__device__ __noinline__ float stage_q(const AttnArgs& a, Smem<D>& sm, int t, const SegRec& sg) {
+  const RowMap map(a.c, sg.row0);
+  const int h = sg.h, rows = sg.rows;
   constexpr int kLanes = D / 8, kPer = 32 / kLanes, kIt = 32 / kPer;  // lanes of a row, rows at a time
-  constexpr int kB = 4;                                               // such steps worked on together
+  constexpr int kB = 8;                                               // such steps worked on together
   const int lane = threadIdx.x & 31, r0 = threadIdx.x & 96;
   const int sub = lane % kLanes, first = t * BM + r0 + lane / kLanes;
-  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(a.q.p) + (int64_t)s.first * a.q.ts +
-                            (int64_t)(h * a.c.group) * a.q.hs + 8 * sub;
-  uint4 v[kB];
-  auto load = [&](int i) {
-    uint4 q = make_uint4(0u, 0u, 0u, 0u);
-    const int r = first + kPer * i;
-    if (r < rows) {
-      int tok, head;
-      map.at(r, &tok, &head);
-      const __nv_bfloat16* p = qp + (int64_t)tok * a.q.ts + (int64_t)head * a.q.hs;
-      if (reinterpret_cast<uintptr_t>(p) % 16 == 0) {
-        q = __ldg(reinterpret_cast<const uint4*>(p));
-      } else {
-        const uint16_t* u = reinterpret_cast<const uint16_t*>(p);
-        q = make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16,
-                       u[6] | (uint32_t)u[7] << 16);
-      }
-    }
-    return q;
-  };
-#pragma unroll
-  for (int j = 0; j < kB; ++j) v[j] = load(j);
+  const int64_t ts = a.q.ts, hs = a.q.hs;
+  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(a.q.p) + sg.first * ts + (int64_t)h * a.c.group * hs + 8 * sub;
   float rm = 0.0f;
 #pragma unroll 1
   for (int i0 = 0; i0 < kIt; i0 += kB) {
-    float y[kB][8], amax[kB];
+    uint4 v[kB];
 #pragma unroll
     for (int b = 0; b < kB; ++b) {
-      const uint32_t w[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
-      amax[b] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        y[b][2 * j] = __uint_as_float(w[j] << 16);
-        y[b][2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-        amax[b] = fmax_nan(amax[b], fmax_nan(fabsf(y[b][2 * j]), fabsf(y[b][2 * j + 1])));
-      }
+      int tok, head;  // rows past the last repeat it: no branch holds a load back
+      map.at(min(first + kPer * (i0 + b), rows - 1), &tok, &head);
+      v[b] = __ldg(reinterpret_cast<const uint4*>(qp + tok * ts + head * hs));
     }
-    if (i0 + kB < kIt) {
+    uint32_t am[kB];  // largest magnitude, as bits: bf16 patterns order like their values, NaN above infinity
 #pragma unroll
-      for (int b = 0; b < kB; ++b) v[b] = load(i0 + kB + b);
+    for (int b = 0; b < kB; ++b) {
+      const uint32_t x = __vmaxu2(__vmaxu2(v[b].x & 0x7FFF7FFFu, v[b].y & 0x7FFF7FFFu),
+                                  __vmaxu2(v[b].z & 0x7FFF7FFFu, v[b].w & 0x7FFF7FFFu));
+      am[b] = max(x & 0xFFFFu, x >> 16);
     }
 #pragma unroll
     for (int o = 1; o < kLanes; o <<= 1)
 #pragma unroll
-      for (int b = 0; b < kB; ++b) amax[b] = fmax_nan(amax[b], __shfl_xor_sync(0xffffffffu, amax[b], o));
+      for (int b = 0; b < kB; ++b) am[b] = max(am[b], __shfl_xor_sync(0xffffffffu, am[b], o));
 #pragma unroll
     for (int b = 0; b < kB; ++b) {
       // the row times 2^up has its largest element in [2^7, 2^8)
-      const int ex = (int)(__float_as_uint(amax[b]) >> 23) - 127;
-      const int up = min(max(7 - ex, -120), 100);
+      const int up = min(max(7 - ((int)(am[b] >> 7) - 127), -120), 100);
       const float f = a.score_mul < 0.0f ? -pow2f(up) : pow2f(up);
-      const float mul = amax[b] < INFINITY ? fabsf(a.score_mul) * pow2f(-up) : __int_as_float(0x7FC00000);
+      const float mul = am[b] < 0x7F80u ? fabsf(a.score_mul) * pow2f(-up) : __int_as_float(0x7FC00000);
       const float got = __shfl_sync(0xffffffffu, mul, (lane % kPer) * kLanes);
       if (lane / kPer == i0 + b) rm = got;
-      uint32_t hi[2], lo[2];
+      const uint32_t w[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+      uint32_t hi[4], lo[4];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float z[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = __fmul_rn(y[b][4 * j + e], f);
-        const uint32_t h0 = e4m3x2(z[0], z[1]), h1 = e4m3x2(z[2], z[3]);
-        const uint32_t w0 = e4m3x2_half2(h0), w1 = e4m3x2_half2(h1);
-        const float2 b0 = __half22float2(*reinterpret_cast<const __half2*>(&w0));
-        const float2 b1 = __half22float2(*reinterpret_cast<const __half2*>(&w1));
-        hi[j] = h0 | (h1 << 16);
-        lo[j] = e4m3x2(__fsub_rn(z[0], b0.x), __fsub_rn(z[1], b0.y)) |
-                (e4m3x2(__fsub_rn(z[2], b1.x), __fsub_rn(z[3], b1.y)) << 16);
+      for (int j = 0; j < 4; ++j) {
+        // binary16 holds the scaled values down to 2^-32 of the row's largest
+        const __half2 y = __floats2half2_rn(__fmul_rn(__uint_as_float(w[j] << 16), f),
+                                            __fmul_rn(__uint_as_float(w[j] & 0xFFFF0000u), f));
+        hi[j] = e4m3x2_h(y);
+        const uint32_t back = e4m3x2_half2(hi[j]);
+        lo[j] = e4m3x2_h(__hsub2(y, *reinterpret_cast<const __half2*>(&back)));
       }
       const int r = r0 + kPer * (i0 + b) + lane / kLanes;
-      *reinterpret_cast<uint2*>(&sm.q[t][0][sub >> 1][r][8 * (sub & 1)]) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2*>(&sm.q[t][1][sub >> 1][r][8 * (sub & 1)]) = make_uint2(lo[0], lo[1]);
+      *reinterpret_cast<uint2*>(&sm.q[t][0][sub >> 1][r][8 * (sub & 1)]) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+      *reinterpret_cast<uint2*>(&sm.q[t][1][sub >> 1][r][8 * (sub & 1)]) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
     }
   }
   return rm;
 }
 
-// Finished rows go to the output through the tile's query staging, free once its
-// products are done, so that consecutive lanes write consecutive dims.
-template <int D>
-struct RowStage {
-  // 16-byte units of a row, rotated by the row against bank conflicts
-  __device__ __forceinline__ static uint4* at(Smem<D>& sm, int t, int r, int unit) {
-    return reinterpret_cast<uint4*>(&sm.q[t][0][0][0][0]) + r * (D / 8) + ((unit + r) & (D / 8 - 1));
+// 16 dims of a finished row.
+__device__ __forceinline__ void put16(__nv_bfloat16* p, const float* o, float inv) {
+  uint32_t b[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const __nv_bfloat162 hb = __floats2bfloat162_rn(__fmul_rn(o[2 * j], inv), __fmul_rn(o[2 * j + 1], inv));
+    b[j] = *reinterpret_cast<const uint32_t*>(&hb);
   }
-};
+  if (reinterpret_cast<uintptr_t>(p) % 32 == 0) {  // a whole sector
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]),
+                 "r"(b[4]), "r"(b[5]), "r"(b[6]), "r"(b[7])
+                 : "memory");
+  } else {
+    *reinterpret_cast<uint4*>(p) = make_uint4(b[0], b[1], b[2], b[3]);
+    *reinterpret_cast<uint4*>(p + 8) = make_uint4(b[4], b[5], b[6], b[7]);
+  }
+}
+
+// The result of a tile: its rows out, or a partial result, joined with the
+// others' by the thread block that comes last. False when a wait gave up.
+template <int D>
+__device__ __noinline__ bool finish_tile(const AttnArgs& a, Smem<D>& sm, const Ctx& x, int t, const SegRec& cs, float m,
+                                         float l, uint32_t no, uint32_t* ng) {
+  const KvArgs& c = a.c;
+  const int r = threadIdx.x & 127;
+  const uint32_t to = sm.tmem + 2 * BN + t * D + ((uint32_t)(32 * ((threadIdx.x >> 5) & 3)) << 16);
+  const bool have = t * BM + r < cs.rows;
+  int tok, head;
+  RowMap(c, cs.row0).at(t * BM + r, &tok, &head);
+  head += cs.h * c.group;
+  // ---- the tile's result
+  if (!wait_warp(x, &sm.o_full[t], no & 1)) return false;
+  tc_fence_after();
+  float* slot = partial_slot(a, blockIdx.x, cs.c0) + (int64_t)t * BM * (D + 2) + r;
+  __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(cs.first + tok) * a.out.ts + (int64_t)head * a.out.hs;
+  auto put_lse = [&](float mm, float ll) {
+    if (a.lse) a.lse[(int64_t)(cs.first + tok) * c.n_heads + head] = ll == 0.0f ? -INFINITY : (mm - kPBits + log2f(ll)) * kLn2;
+  };
+  const float inv = l == 0.0f ? 0.0f : __frcp_rn(l);
+#pragma unroll 1
+  for (int q = 0; q < D / 16; ++q) {
+    float v[16];
+    tmem_ld16(to + 16 * q, v);
+    tmem_wait_ld(v);
+    if (have && cs.whole) {
+      put16(op + 16 * q, v, inv);
+    } else if (have) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) slot[(16 * q + j) * BM] = v[j];
+    }
+  }
+  tc_fence_before();
+  if (cs.whole) {
+    if (have) put_lse(m, l);
+  } else {
+    if (have) {
+      slot[D * BM] = m;
+      slot[(D + 1) * BM] = l;
+    }
+    __threadfence();
+    mbar_arrive(&sm.group[t]);
+    if (!wait_warp(x, &sm.group[t], (*ng)++ & 1)) return false;
+    if (r == 0) {
+      int* arr = a.arrived + 2 * cs.c0 + t;
+      const int last = atomicAdd(arr, 1) == cs.c1 - cs.c0;
+      if (last) *arr = 0;  // as every call leaves it
+      *(volatile int*)&sm.last[t] = last;
+      __threadfence();
+    }
+    mbar_arrive(&sm.group[t]);
+    if (!wait_warp(x, &sm.group[t], (*ng)++ & 1)) return false;
+    if (*(volatile int*)&sm.last[t] && have) {
+      __threadfence();
+      // parts in order, the loads of half a row in flight together
+      const int64_t at = (int64_t)t * BM * (D + 2) + r;
+      float mm = -INFINITY, ll = 0.0f;
+#pragma unroll 4
+      for (int k = cs.c0; k <= cs.c1; ++k) mm = fmaxf(mm, __ldcg(partial_slot(a, k, cs.c0) + at + D * BM));
+      const float base = mm == -INFINITY ? 0.0f : mm;
+      constexpr int kD = 64;
+#pragma unroll 1
+      for (int d = 0; d < D; d += kD) {
+        float o[kD];
+#pragma unroll
+        for (int j = 0; j < kD; ++j) o[j] = 0.0f;
+        ll = 0.0f;
+#pragma unroll 1
+        for (int k = cs.c0; k <= cs.c1; ++k) {
+          const float* sp = partial_slot(a, k, cs.c0) + at;
+          const float km = __ldcg(sp + D * BM), kl = __ldcg(sp + (D + 1) * BM);
+          float y[kD / 2];
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+            for (int j = 0; j < kD / 2; ++j) y[j] = __ldcg(sp + (d + kD / 2 * hf + j) * BM);
+            const float f = ex2(__fsub_rn(km, base));
+            if (hf == 0) ll = __fmaf_rn(kl, f, ll);
+#pragma unroll
+            for (int j = 0; j < kD / 2; ++j) o[kD / 2 * hf + j] = __fmaf_rn(y[j], f, o[kD / 2 * hf + j]);
+          }
+        }
+        const float iv = ll == 0.0f ? 0.0f : __frcp_rn(ll);
+#pragma unroll
+        for (int j = 0; j < kD; j += 16) put16(op + d + j, o + j, iv);
+      }
+      put_lse(mm, ll);
+    }
+  }
+  return true;
+}
 
 template <int D>
-__device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
+__device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
   const KvArgs& c = a.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = warp >> 2, r = threadIdx.x & 127;
@@ -454,61 +587,90 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
   const uint32_t ts = sm.tmem + t * BN + lane_base, to = sm.tmem + 2 * BN + t * D + lane_base;
   const float nan = __int_as_float(0x7FC00000);
   uint32_t ns = 0, no = 0, ng = 0;
-  for (; w.more();) {
-    const Segment sg = w.segment(a);
-    const KvSeq s = w.s;
-    if (sg.empty || sg.rows <= t * BM) {  // nothing here, or no row in this tile
-      w.advance(a, sg);
-      continue;
+  // The ring slot of the next segment with rows of this tile, its query rows sent
+  // to the MMAs; kEnd, kGone when a wait gave up, or kLater: while a slot is held
+  // no segment is passed over, or the ring could run full of what is held.
+  constexpr int kEnd = -1, kGone = -2, kLater = -3;
+  uint32_t is = 0;
+  float rm = 0.0f;
+  auto next = [&](bool held) -> int {
+    for (;; ++is) {
+      const uint32_t slot = is % kRing;
+      if (!wait_warp(x, &sm.seg_full[slot], (is / kRing) & 1)) return kGone;
+      if (sm.seg[slot].b < 0) return kEnd;
+      if (sm.seg[slot].rows > t * BM) {
+        rm = stage_q<D>(a, sm, t, sm.seg[slot]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(&sm.q_full[t]);
+        ++is;
+        return (int)slot;
+      }
+      if (held) return kLater;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.seg_empty[slot]);
     }
-    const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
-    const RowMap map(c, w.t * kRows);
-    const bool have = t * BM + r < sg.rows;
-    int tok, head;
-    map.at(t * BM + r, &tok, &head);
-    const float rm = stage_q<D>(a, sm, t, s, sg.h, map, sg.rows);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    mbar_arrive(&sm.q_full[t]);
-    const int lim = !have ? INT32_MAX : (a.causal ? s.kv - s.n + tok : s.kv - 1);
+  };
+  for (int slot = next(false); slot >= 0;) {
+    const SegRec& cs = sm.seg[slot];
+    const int32_t* table = c.table + (int64_t)cs.b * c.table_stride;
+    const int kv = cs.kv, blk1 = cs.blk1, h = cs.h;
+    int lim = INT32_MAX;  // last token this row sees
+    if (t * BM + r < cs.rows) {
+      int tok, head;
+      RowMap(c, cs.row0).at(t * BM + r, &tok, &head);
+      lim = a.causal ? kv - cs.n + tok : kv - 1;
+    }
     int lim_min = lim;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) lim_min = min(lim_min, __shfl_xor_sync(0xffffffffu, lim_min, o));
-
     float m = -INFINITY, l = 0.0f;
-    Groups g = load_groups(c, table, s.kv, sg.h, sg.blk0);
-    for (int blk = sg.blk0; blk < sg.blk1; ++blk) {
+    Groups g = load_groups(c, table, kv, h, cs.blk0);
+    for (int blk = cs.blk0; blk < blk1; ++blk) {
       const Groups cur = g;
-      if (blk + 1 < sg.blk1) g = load_groups(c, table, s.kv, sg.h, blk + 1);
-      const bool masked = blk * BN + BN - 1 > lim_min || __any_sync(0xffffffffu, lane < 8 && cur.have < 16);
-      const int col = lim == INT32_MAX ? BN : lim - blk * BN;  // last column this row sees
+      if (blk + 1 < blk1) g = load_groups(c, table, kv, h, blk + 1);
+      // lane i < 8: the scale of group i's keys, the exponent and unscaling of its values, its tokens
+      const bool mark = cur.ek == kExpNan || cur.ev == kExpNan;
+      const bool masked = blk * BN + BN - 1 > lim_min || __any_sync(0xffffffffu, lane < 8 && (cur.have < 16 || mark));
       float4* gc = sm.group_of[warp][blk & 1];
       if (lane < 8)
-        gc[lane] = make_float4(pow2f(cur.ek), cur.ek == kExpNan || cur.ev == kExpNan ? nan : (float)cur.ev,
-                               pow2f(-cur.ev), __int_as_float(cur.have));
+        gc[lane] = make_float4(mark ? 1.0f : pow2f(cur.ek), mark ? 0.0f : (float)cur.ev, mark ? 1.0f : pow2f(-cur.ev), 0.0f);
       __syncwarp();
       if (!wait_warp(x, &sm.s_full[t], ns++ & 1)) return;
       tc_fence_after();
-
-      // ---- the row of S, and its maximum
-      float v[BN];
-#pragma unroll
-      for (int i = 0; i < BN / 16; ++i) tmem_ld16(ts + 16 * i, v + 16 * i);
-      tmem_wait_ld(v);
-#pragma unroll
-      for (int i = 1; i < BN / 16; ++i) tmem_tie(v + 16 * i);
-      if (masked) {
-#pragma unroll
+      if (masked) {  // hidden tokens to -inf, visible ones of a marked block to NaN, in place
+        const int col = lim == INT32_MAX ? BN : lim - blk * BN;  // last column this row sees
+#pragma unroll 1
         for (int i = 0; i < 8; ++i) {
-          const int lc = min(col - 16 * i, __float_as_int(gc[i].w) - 1);
+          float v[16];
+          tmem_ld16(ts + 16 * i, v);
+          tmem_wait_ld(v);
+          const int lc = min(col - 16 * i, __shfl_sync(0xffffffffu, cur.have, i) - 1);
+          const bool bad = __shfl_sync(0xffffffffu, mark, i);
+          uint32_t u[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) v[16 * i + j] = j <= lc ? v[16 * i + j] : -INFINITY;
+          for (int j = 0; j < 16; ++j) u[j] = __float_as_uint(j > lc ? -INFINITY : (bad ? nan : v[j]));
+          tmem_st16(ts + 16 * i, u);
         }
+        st_wait();
       }
+
+      // ---- the block's maximum. This loop and the next stay rolled, 64 columns a
+      // step, and what a segment does once lives in functions of its own: with
+      // everything unrolled in line the roles outgrew the instruction cache
       float mx = -INFINITY;
+#pragma unroll 1
+      for (int q = 0; q < 8; q += 4) {
+        float v[64];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 k = gc[i];
-        mx = fmaxf(mx, __fmaf_rn(max16(v + 16 * i), fmaxf(__fmul_rn(rm, k.x), kTiny), k.y));
+        for (int i = 0; i < 4; ++i) tmem_ld16(ts + 16 * (q + i), v + 16 * i);
+        tmem_wait_ld(v);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) tmem_tie(v + 16 * i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 k = gc[q + i];
+          mx = fmaxf(mx, __fmaf_rn(max16(v + 16 * i), fmaxf(__fmul_rn(rm, k.x), kTiny), k.y));
+        }
       }
 
       // ---- running maximum; O and l follow when it grew by more than 2^kGrow
@@ -518,7 +680,7 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
         const float f = mn == -INFINITY ? 1.0f : ex2(__fsub_rn(m, mn));
         l = __fmul_rn(l, f);
         m = mn;
-        if (blk > sg.blk0) {
+        if (blk > cs.blk0) {
 #pragma unroll 1
           for (int q = 0; q < D / 16; ++q) {
             float o[16];
@@ -533,150 +695,49 @@ __device__ void softmax_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& 
       }
       const float off = rm < INFINITY ? kPBits - (m == -INFINITY ? 0.0f : m) : nan;
 
-      // ---- weights (a marked block or a query that is not finite: NaN through e)
+      // ---- weights, P over columns of S already read
+#pragma unroll 1
+      for (int q = 0; q < 8; q += 4) {
+        float v[64];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 k = gc[i];
-        const float kx = fmaxf(__fmul_rn(rm, k.x), kTiny);
-        float e = __fadd_rn(k.y, off);
-        if (masked && min(col - 16 * i, __float_as_int(k.w) - 1) < 0) e = 0.0f;  // hidden: -inf whatever the block
-        float2 p[8];
+        for (int i = 0; i < 4; ++i) tmem_ld16(ts + 16 * (q + i), v + 16 * i);
+        tmem_wait_ld(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float2 y = __ffma2_rn(make_float2(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]), make_float2(kx, kx),
-                                      make_float2(e, e));
-          p[j] = make_float2(ex2(y.x), ex2(y.y));
+        for (int i = 1; i < 4; ++i) tmem_tie(v + 16 * i);
+        uint32_t u[32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 k = gc[q + i];
+          const float kx = fmaxf(__fmul_rn(rm, k.x), kTiny), e = __fadd_rn(k.y, off);
+          float2 p[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float2 y = __ffma2_rn(make_float2(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]), make_float2(kx, kx),
+                                        make_float2(e, e));
+            p[j] = make_float2(ex2(y.x), ex2(y.y));
+            const __half2 hp = __floats2half2_rn(p[j].x, p[j].y);
+            u[8 * i + j] = *reinterpret_cast<const uint32_t*>(&hp);
+          }
+          const float2 s0 = __fadd2_rn(__fadd2_rn(p[0], p[1]), __fadd2_rn(p[2], p[3]));
+          const float2 s1 = __fadd2_rn(__fadd2_rn(p[4], p[5]), __fadd2_rn(p[6], p[7]));
+          const float2 s2 = __fadd2_rn(s0, s1);
+          l = __fmaf_rn(__fadd_rn(s2.x, s2.y), k.z, l);
         }
-        uint32_t h[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const __half2 hp = __floats2half2_rn(p[j].x, p[j].y);
-          h[j] = *reinterpret_cast<const uint32_t*>(&hp);
-        }
-        tmem_st8(ts + 8 * i, h);  // P over S, which is in registers
-        const float2 s0 = __fadd2_rn(__fadd2_rn(p[0], p[1]), __fadd2_rn(p[2], p[3]));
-        const float2 s1 = __fadd2_rn(__fadd2_rn(p[4], p[5]), __fadd2_rn(p[6], p[7]));
-        const float2 s2 = __fadd2_rn(s0, s1);
-        const float sum = __fadd_rn(s2.x, s2.y);
-        l = sum == 0.0f ? l : __fmaf_rn(sum, k.z, l);
+        tmem_st16(ts + 8 * q, u);
+        tmem_st16(ts + 8 * q + 16, u + 16);
       }
       st_wait();
       tc_fence_before();
       mbar_arrive(&sm.p_full[t]);
     }
-
-    // ---- the tile's result
-    if (!wait_warp(x, &sm.o_full[t], no++ & 1)) return;
-    tc_fence_after();
-    float* slot = partial_slot(a, blockIdx.x, sg.c0) + (int64_t)t * BM * (D + 2) + r;
-    auto put = [&](int d, const float* o, float inv) {  // 8 dims of a finished row to the staging
-      uint32_t b[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const __nv_bfloat162 hb = __floats2bfloat162_rn(__fmul_rn(o[2 * j], inv), __fmul_rn(o[2 * j + 1], inv));
-        b[j] = *reinterpret_cast<const uint32_t*>(&hb);
-      }
-      *RowStage<D>::at(sm, t, r, d / 8) = make_uint4(b[0], b[1], b[2], b[3]);
-    };
-    auto flush = [&](float mm, float ll) {  // the warp's staged rows to the output
-      if (have && a.lse)
-        a.lse[(int64_t)(s.first + tok) * c.n_heads + sg.h * c.group + head] = ll == 0.0f ? -INFINITY : (mm - kPBits + log2f(ll)) * kLn2;
-      __syncwarp();
-      constexpr int kLanes = D / 8, kPer = 32 / kLanes;
-#pragma unroll 4
-      for (int i = 0; i < 32 / kPer; ++i) {
-        const int rr = (r & 96) + kPer * i + lane / kLanes, sub = lane % kLanes;
-        if (t * BM + rr < sg.rows) {
-          int tok2, head2;
-          map.at(t * BM + rr, &tok2, &head2);
-          __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(s.first + tok2) * a.out.ts +
-                              (int64_t)(sg.h * c.group + head2) * a.out.hs + 8 * sub;
-          const uint4 v = *RowStage<D>::at(sm, t, rr, sub);
-          if (reinterpret_cast<uintptr_t>(op) % 16 == 0) {
-            *reinterpret_cast<uint4*>(op) = v;
-          } else {
-            const uint32_t b[4] = {v.x, v.y, v.z, v.w};
-            uint16_t* o16 = reinterpret_cast<uint16_t*>(op);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o16[j] = (uint16_t)(b[j >> 1] >> (16 * (j & 1)));
-          }
-        }
-      }
-      __syncwarp();
-    };
-    const float inv = l == 0.0f ? 0.0f : __frcp_rn(l);
-#pragma unroll 1
-    for (int q = 0; q < D / 32; ++q) {
-      float v[32];
-      tmem_ld16(to + 32 * q, v);
-      tmem_ld16(to + 32 * q + 16, v + 16);
-      tmem_wait_ld(v);
-      tmem_tie(v + 16);
-      if (sg.whole) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) put(32 * q + 8 * j, v + 8 * j, inv);
-      } else if (have) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) slot[(32 * q + j) * BM] = v[j];
-      }
-    }
-    tc_fence_before();
-    if (sg.whole) {
-      flush(m, l);
-    } else {
-      if (have) {
-        slot[D * BM] = m;
-        slot[(D + 1) * BM] = l;
-      }
-      __threadfence();
-      mbar_arrive(&sm.group[t]);
-      if (!wait_warp(x, &sm.group[t], ng++ & 1)) return;
-      if (r == 0) {
-        int* arr = a.arrived + 2 * sg.c0 + t;
-        const int last = atomicAdd(arr, 1) == sg.c1 - sg.c0;
-        if (last) *arr = 0;  // as every call leaves it
-        *(volatile int*)&sm.last[t] = last;
-        __threadfence();
-      }
-      mbar_arrive(&sm.group[t]);
-      if (!wait_warp(x, &sm.group[t], ng++ & 1)) return;
-      if (*(volatile int*)&sm.last[t]) {
-        __threadfence();
-        const int64_t at = (int64_t)t * BM * (D + 2) + r;
-        float mm = -INFINITY;
-        for (int k = sg.c0; k <= sg.c1; ++k) mm = fmaxf(mm, __ldcg(partial_slot(a, k, sg.c0) + at + D * BM));
-        const float base = mm == -INFINITY ? 0.0f : mm;
-        float ll = 0.0f;
-        for (int k = sg.c0; k <= sg.c1; ++k) {
-          const float* sp = partial_slot(a, k, sg.c0) + at;
-          ll = __fmaf_rn(__ldcg(sp + (D + 1) * BM), ex2(__fsub_rn(__ldcg(sp + D * BM), base)), ll);
-        }
-        const float iv = ll == 0.0f ? 0.0f : __frcp_rn(ll);
-        constexpr int kD = 16;  // dims at a time, their loads in flight together
-        for (int d = 0; d < D; d += kD) {
-          float o[kD];
-#pragma unroll
-          for (int j = 0; j < kD; ++j) o[j] = 0.0f;
-#pragma unroll 2
-          for (int k = sg.c0; k <= sg.c1; ++k) {
-            const float* sp = partial_slot(a, k, sg.c0) + at;
-            const float f = ex2(__fsub_rn(__ldcg(sp + D * BM), base));
-            float y[kD];
-#pragma unroll
-            for (int j = 0; j < kD; ++j) y[j] = __ldcg(sp + (d + j) * BM);
-#pragma unroll
-            for (int j = 0; j < kD; ++j) o[j] = __fmaf_rn(y[j], f, o[j]);
-          }
-#pragma unroll
-          for (int j = 0; j < kD; j += 8) put(d + j, o + j, iv);
-        }
-        flush(mm, ll);
-      }
-    }
-    // the staging is the next tile's query operand, which the warps fill together
-    mbar_arrive(&sm.group[t]);
-    if (!wait_warp(x, &sm.group[t], ng++ & 1)) return;
-    w.advance(a, sg);
+    // the last block's scores are done with the query staging: the next tile's
+    // rows go there while this one's last products run
+    int after = next(true);
+    if (after == kGone || !finish_tile<D>(a, sm, x, t, cs, m, l, no++, &ng)) return;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.seg_empty[slot]);
+    if (after == kLater) after = next(false);
+    slot = after;
   }
 }
 
@@ -689,17 +750,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
   const int warp = threadIdx.x >> 5;
   if (warp == kLoadWarp) {
     if ((threadIdx.x & 31) == 0) {
-      for (int i = 0; i < NK; ++i) mbar_init(&sm.k_full[i], 1), mbar_init(&sm.k_empty[i], 1);
+      for (int i = 0; i < NK; ++i) mbar_init(&sm.k_full[i], 1), mbar_init(&sm.k_empty[i], 2);
       for (int i = 0; i < NV; ++i) mbar_init(&sm.v_full[i], 1), mbar_init(&sm.v_empty[i], 128);
-      for (int i = 0; i < NW; ++i) mbar_init(&sm.w_full[i], 128), mbar_init(&sm.w_empty[i], 1);
+      for (int i = 0; i < NW; ++i) mbar_init(&sm.w_full[i], 128), mbar_init(&sm.w_empty[i], 2);
       for (int i = 0; i < 2; ++i) {
         mbar_init(&sm.q_full[i], 128);
         mbar_init(&sm.s_full[i], 1);
         mbar_init(&sm.p_full[i], 128);
         mbar_init(&sm.o_full[i], 1);
         mbar_init(&sm.group[i], 128);
+        mbar_init(&sm.turn[i], 1);
+          mbar_init(&sm.drain[i], 1);
       }
-      mbar_init(&sm.drain, 1);
+      for (int i = 0; i < kRing; ++i) mbar_init(&sm.seg_full[i], 1), mbar_init(&sm.seg_empty[i], kReaders);
       sm.dead = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -714,18 +777,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
   tc_fence_after();
   const Ctx x{a.wait_ns, a.c.status, &sm.dead};
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    softmax_role<D>(a, w, sm, x);
+    softmax_role<D>(a, sm, x);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp < kMmaWarp) {
-      widen_role<D>(a, w, sm, x);
-    } else if (warp == kMmaWarp) {
-      if ((threadIdx.x & 31) == 0) mma_role<D>(a, w, sm, x);
-      __syncwarp();
+      widen_role<D>(a, sm, x);
+    } else if (warp < kLoadWarp) {
+      if ((threadIdx.x & 31) == 0) mma_role<D>(sm, x, warp - kMmaWarp);
     } else if (warp == kLoadWarp) {
-      load_role<D>(a, w, sm, x);
+      load_role<D>(a, sm, x);
+    } else if ((threadIdx.x & 31) == 0) {
+      walk_role<D>(a, w, sm, x);
     }
+    __syncwarp();
   }
   tc_fence_before();
   __syncthreads();
