@@ -24,14 +24,15 @@ awsrc_status check_cache(const awsrc_kv_cache* c, int32_t n_heads, bool pointers
 }
 
 struct AttnLayout {
-  size_t arrived, partial, total;
+  size_t arrived, shared, partial, total;
   int64_t row_slot, tile_slot;  // floats of a partial result of either kernel
 };
 
 AttnLayout attn_layout(const awsrc_kv_cache& c) {
   AttnLayout L{};
   L.arrived = kStatusBytes;
-  L.partial = L.arrived + align_up((size_t)kMaxAttnBlocks * sizeof(int), 256);
+  L.shared = L.arrived + align_up((size_t)kMaxAttnBlocks * sizeof(int), 256);
+  L.partial = L.shared + align_up((size_t)kMaxTileBlocks * sizeof(SharedTile), 256);
   L.row_slot = (int64_t)kSlotRows * (c.head_dim + 2);
   L.tile_slot = (int64_t)kTileSlotRows * (c.head_dim + 2);
   const size_t rows = (size_t)2 * kMaxAttnBlocks * L.row_slot, tiles = (size_t)2 * kMaxTileBlocks * L.tile_slot;
@@ -151,6 +152,7 @@ awsrc_status awsrc_paged_attention(const awsrc_kv_cache* cache, const awsrc_kv_b
   a.score_mul = sm_scale * 1.4426950408889634f;
   a.causal = causal;
   a.arrived = reinterpret_cast<int*>(ws + L.arrived);
+  a.shared = reinterpret_cast<SharedTile*>(ws + L.shared);
   a.partial = reinterpret_cast<float*>(ws + L.partial);
   a.wait_ns = wait_limit_ns();
   a.stall = wait_test_stall();

@@ -89,7 +89,8 @@ struct AttnArgs {
   float score_mul;  // sm_scale log2(e)
   int causal;
   int min_units;    // least share of a block
-  int* arrived;     // per block (two for each, one per 128 rows): arrivals at the shared tile that begins in its share
+  int* arrived;     // per block: arrivals at the shared tile that begins in its share (row kernel)
+  struct SharedTile* shared;  // per block: the shared tile that begins in its share (tensor-memory kernel)
   float* partial;
   int64_t slot_floats;
   uint64_t wait_ns;  // limit of the tensor-memory kernel's waits
@@ -129,11 +130,27 @@ struct UnitWalk {
   __device__ __forceinline__ static int tiles_of(const AttnArgs& a, const KvSeq& s) {
     return s.n > 0 ? (s.n * a.c.group + ROWS - 1) / ROWS : 0;
   }
-  __device__ static int64_t units_of(const AttnArgs& a, const KvSeq& s) {
-    const int nt = tiles_of(a, s);
+  // Units of the tiles of s, or with `want` >= 0 the tile that holds unit `want`
+  // of them (*tile, and the units before it as the result). No division per tile:
+  // the token of a tile's last row advances by ROWS / group.
+  __device__ static int64_t units_of(const AttnArgs& a, const KvSeq& s, int64_t want = -1, int* tile = nullptr) {
+    const int nt = tiles_of(a, s), g = a.c.group, heads = a.c.kv_heads;
+    const int dq = ROWS / g, dr = ROWS - dq * g;
+    int q = (ROWS - 1) / g, r = ROWS - 1 - q * g;
     int64_t n = 0;
-    for (int i = 0; i < nt; ++i) n += blocks_of(a, s, i) + OVER;
-    return n * a.c.kv_heads;
+    for (int i = 0; i < nt; ++i) {
+      const int see = a.causal && i + 1 < nt ? s.kv - s.n + q + 1 : s.kv;
+      const int64_t u = (int64_t)(max(1, (see + UNIT - 1) / UNIT) + OVER) * heads;
+      if (want >= 0 && want < n + u) {
+        *tile = i;
+        return n;
+      }
+      n += u;
+      q += dq;
+      r += dr;
+      if (r >= g) r -= g, ++q;
+    }
+    return n;
   }
   // Inclusive sum over the first WARPS warps of one value per thread; *all its total.
   __device__ __forceinline__ static int64_t scan(int64_t x, int64_t* all) {
@@ -161,16 +178,16 @@ struct UnitWalk {
     __shared__ int64_t found[2];
     const KvArgs& c = a.c;
     constexpr int kN = 32 * WARPS;
-    int64_t total = 0, all;
+    int64_t total = 0, all, mine = 0, upto = 0;  // of this thread's sequence in the last chunk
     for (int base = 0; base < c.n_seq; base += kN) {
       const int i = base + (int)threadIdx.x;
-      int64_t n = 0;
+      mine = 0;
       if (threadIdx.x < kN && i < c.n_seq) {
         const KvSeq q = kv_seq(c, i);
         if (q.n < 0 && blockIdx.x == 0) atomicOr(c.status, kFaultBatch);
-        n = units_of(a, q);
+        mine = units_of(a, q);
       }
-      scan(n, &all);
+      upto = total + scan(mine, &all);
       total += all;
     }
     chunk = max((int64_t)a.min_units, (total + gridDim.x - 1) / gridDim.x);
@@ -180,26 +197,23 @@ struct UnitWalk {
     int64_t before = 0;
     for (int base = 0; base < c.n_seq; base += kN) {
       const int i = base + (int)threadIdx.x;
-      int64_t n = 0;
-      if (threadIdx.x < kN && i < c.n_seq) n = units_of(a, kv_seq(c, i));
-      const int64_t hi = before + scan(n, &all);
-      if (u < hi && u >= hi - n) {
-        found[0] = i;
-        found[1] = hi - n;
+      if (c.n_seq > kN) {
+        mine = threadIdx.x < kN && i < c.n_seq ? units_of(a, kv_seq(c, i)) : 0;
+        upto = before + scan(mine, &all);
+        before += all;
       }
-      before += all;
-      if (u < before) break;
+      if (u < upto && u >= upto - mine) {
+        found[0] = i;
+        found[1] = upto - mine;
+      }
+      if (c.n_seq > kN && u < before) break;
     }
     __syncthreads();
     b = (int)found[0];
-    tile_first = found[1];
     s = kv_seq(c, b);
-    for (t = 0;; ++t) {
-      blocks = blocks_of(a, s, t);
-      const int64_t n = (int64_t)(blocks + OVER) * c.kv_heads;
-      if (u < tile_first + n) return true;
-      tile_first += n;
-    }
+    tile_first = found[1] + units_of(a, s, u - found[1], &t);
+    blocks = blocks_of(a, s, t);
+    return true;
   }
   __device__ __forceinline__ bool more() const { return u < u_end; }
   __device__ __forceinline__ Segment segment(const AttnArgs& a) const {
@@ -289,6 +303,11 @@ cudaError_t launch_kv_append(const KvArgs& c, int head_dim, int dtype, const KvR
                              const KvRows& v, const KvRows& qo, const float* cos, const float* sin, int rope_rows,
                              int rotary_dim, int interleaved, cudaStream_t st);
 cudaError_t launch_paged_rows(const AttnArgs& a, int head_dim, int dtype, int max_new, int max_kv, cudaStream_t st);
+// A tile shared by several thread blocks, as the one it begins in leaves it for
+// the joining kernel; rows = 0: none.
+struct SharedTile {
+  int row0, rows, first, h, c1, pad_[3];
+};
 cudaError_t launch_paged_tiles(const AttnArgs& a, int head_dim, int max_kv, cudaStream_t st);  // BF16
 
 }  // namespace awsrc

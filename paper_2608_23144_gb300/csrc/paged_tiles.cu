@@ -29,8 +29,9 @@
 // The byte order of keys and values in the cache is the operand order the
 // tensor cores read, so copies need no rearrangement.
 //
-// Work is shared out as in paged_attn.cu (UnitWalk); tiles that thread blocks
-// share are joined by the last to arrive.
+// Work is shared out as in paged_attn.cu (UnitWalk). Tiles that thread blocks
+// share leave partial results, which a second launch joins on the whole GPU:
+// joined by the last block to arrive, the five parts of a tile took 60 us.
 //
 // Every wait is bounded (wait_ns): one that runs out sets bit 2 of the fault
 // word, stops the block's roles, waits (bounded) for its copies and products in
@@ -54,7 +55,7 @@ constexpr int NK = 3, NV = 2, NW = 2;  // stages: keys, value codes, widened val
 constexpr uint32_t kTmemCols = 512;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPBits = 6.0f;         // p is at most 2^6 when m is the maximum,
-constexpr float kTiny = 1e-37f;        // least score multiplier: hidden scores of -inf stay -inf
+constexpr float kTiny = 0x1p-80f;      // least score multiplier: times a block's scale, hidden scores of -inf stay -inf
 constexpr float kGrow = 8.0f;          // and at most 2^(6 + 8) < 65504 when m lags
 constexpr int kOver = 4;               // a tile's start and end, in blocks
 using Walk = UnitWalk<kRows, BN, 4, kOver>;
@@ -75,12 +76,12 @@ struct Smem {
   uint8_t v[NV][BN / 16][D][16];
   uint8_t w[NW][BN / 8][D][16];     // binary16, 8 tokens
   unsigned long long k_full[NK], k_empty[NK], v_full[NV], v_empty[NV], w_full[NW], w_empty[NW];
-  unsigned long long q_full[2], s_full[2], p_full[2], o_full[2], group[2], turn[2], drain[2];
+  unsigned long long q_full[2], s_full[2], p_full[2], o_full[2], turn[2], drain[2];
   unsigned long long seg_full[kRing], seg_empty[kRing];
   SegRec seg[kRing];
   float4 group_of[8][2][8];  // softmax warp, block parity: scale of the keys, exponent and unscaling of the values, tokens
   uint32_t tmem;
-  int dead, last[2];
+  int dead;
 };
 
 struct Ctx {
@@ -157,11 +158,15 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
                : "memory");
 }
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float max3(float a, float b, float c) {  // one instruction of the half-rate pipe for two
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ float max16(const float* v) {
   const float a = max3(v[0], v[1], v[2]), b = max3(v[3], v[4], v[5]), c = max3(v[6], v[7], v[8]);
   const float d = max3(v[9], v[10], v[11]), e = max3(v[12], v[13], v[14]);
-  return max3(max3(a, b, c), max3(d, e, v[15]), v[15]);
+  return max3(max3(a, b, c), d, fmaxf(e, v[15]));
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -201,8 +206,12 @@ __device__ __forceinline__ int group_tokens(const KvArgs& c, const int32_t* tabl
 template <int D>
 __device__ __noinline__ void walk_role(const AttnArgs& a, Walk w, Smem<D>& sm, const Ctx& x) {
   uint32_t i = 0;
+  SharedTile mine{};
+  a.shared[blockIdx.x] = mine;  // what stands there if a wait gives up
   for (; w.more();) {
     const Segment g = w.segment(a);
+    if (!g.empty && !g.whole && g.c0 == (int)blockIdx.x)
+      mine = SharedTile{w.t * kRows, g.rows, w.s.first, g.h, g.c1, {0, 0, 0}};
     if (!g.empty) {
       if (!wait_lane(x, &sm.seg_empty[i % kRing], ((i / kRing) & 1) ^ 1)) return;
       sm.seg[i % kRing] = SegRec{w.b, g.h, g.blk0, g.blk1, w.t * kRows, g.rows, w.s.first, w.s.n, w.s.kv, g.c0, g.c1, g.whole};
@@ -211,6 +220,7 @@ __device__ __noinline__ void walk_role(const AttnArgs& a, Walk w, Smem<D>& sm, c
     }
     w.advance(a, g);
   }
+  a.shared[blockIdx.x] = mine;
   if (!wait_lane(x, &sm.seg_empty[i % kRing], ((i / kRing) & 1) ^ 1)) return;
   sm.seg[i % kRing].b = -1;
   mbar_arrive(&sm.seg_full[i % kRing]);
@@ -485,11 +495,15 @@ __device__ __forceinline__ void put16(__nv_bfloat16* p, const float* o, float in
   }
 }
 
-// The result of a tile: its rows out, or a partial result, joined with the
-// others' by the thread block that comes last. False when a wait gave up.
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.0f ? -INFINITY : (m - kPBits + log2f(l)) * kLn2;
+}
+
+// The result of a tile: its rows out, or a partial result. False when a wait
+// gave up.
 template <int D>
 __device__ __noinline__ bool finish_tile(const AttnArgs& a, Smem<D>& sm, const Ctx& x, int t, const SegRec& cs, float m,
-                                         float l, uint32_t no, uint32_t* ng) {
+                                         float l, uint32_t no) {
   const KvArgs& c = a.c;
   const int r = threadIdx.x & 127;
   const uint32_t to = sm.tmem + 2 * BN + t * D + ((uint32_t)(32 * ((threadIdx.x >> 5) & 3)) << 16);
@@ -502,9 +516,6 @@ __device__ __noinline__ bool finish_tile(const AttnArgs& a, Smem<D>& sm, const C
   tc_fence_after();
   float* slot = partial_slot(a, blockIdx.x, cs.c0) + (int64_t)t * BM * (D + 2) + r;
   __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(cs.first + tok) * a.out.ts + (int64_t)head * a.out.hs;
-  auto put_lse = [&](float mm, float ll) {
-    if (a.lse) a.lse[(int64_t)(cs.first + tok) * c.n_heads + head] = ll == 0.0f ? -INFINITY : (mm - kPBits + log2f(ll)) * kLn2;
-  };
   const float inv = l == 0.0f ? 0.0f : __frcp_rn(l);
 #pragma unroll 1
   for (int q = 0; q < D / 16; ++q) {
@@ -519,61 +530,12 @@ __device__ __noinline__ bool finish_tile(const AttnArgs& a, Smem<D>& sm, const C
     }
   }
   tc_fence_before();
+  if (!have) return true;
   if (cs.whole) {
-    if (have) put_lse(m, l);
+    if (a.lse) a.lse[(int64_t)(cs.first + tok) * c.n_heads + head] = lse_of(m, l);
   } else {
-    if (have) {
-      slot[D * BM] = m;
-      slot[(D + 1) * BM] = l;
-    }
-    __threadfence();
-    mbar_arrive(&sm.group[t]);
-    if (!wait_warp(x, &sm.group[t], (*ng)++ & 1)) return false;
-    if (r == 0) {
-      int* arr = a.arrived + 2 * cs.c0 + t;
-      const int last = atomicAdd(arr, 1) == cs.c1 - cs.c0;
-      if (last) *arr = 0;  // as every call leaves it
-      *(volatile int*)&sm.last[t] = last;
-      __threadfence();
-    }
-    mbar_arrive(&sm.group[t]);
-    if (!wait_warp(x, &sm.group[t], (*ng)++ & 1)) return false;
-    if (*(volatile int*)&sm.last[t] && have) {
-      __threadfence();
-      // parts in order, the loads of half a row in flight together
-      const int64_t at = (int64_t)t * BM * (D + 2) + r;
-      float mm = -INFINITY, ll = 0.0f;
-#pragma unroll 4
-      for (int k = cs.c0; k <= cs.c1; ++k) mm = fmaxf(mm, __ldcg(partial_slot(a, k, cs.c0) + at + D * BM));
-      const float base = mm == -INFINITY ? 0.0f : mm;
-      constexpr int kD = 64;
-#pragma unroll 1
-      for (int d = 0; d < D; d += kD) {
-        float o[kD];
-#pragma unroll
-        for (int j = 0; j < kD; ++j) o[j] = 0.0f;
-        ll = 0.0f;
-#pragma unroll 1
-        for (int k = cs.c0; k <= cs.c1; ++k) {
-          const float* sp = partial_slot(a, k, cs.c0) + at;
-          const float km = __ldcg(sp + D * BM), kl = __ldcg(sp + (D + 1) * BM);
-          float y[kD / 2];
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-#pragma unroll
-            for (int j = 0; j < kD / 2; ++j) y[j] = __ldcg(sp + (d + kD / 2 * hf + j) * BM);
-            const float f = ex2(__fsub_rn(km, base));
-            if (hf == 0) ll = __fmaf_rn(kl, f, ll);
-#pragma unroll
-            for (int j = 0; j < kD / 2; ++j) o[kD / 2 * hf + j] = __fmaf_rn(y[j], f, o[kD / 2 * hf + j]);
-          }
-        }
-        const float iv = ll == 0.0f ? 0.0f : __frcp_rn(ll);
-#pragma unroll
-        for (int j = 0; j < kD; j += 16) put16(op + d + j, o + j, iv);
-      }
-      put_lse(mm, ll);
-    }
+    slot[D * BM] = m;
+    slot[(D + 1) * BM] = l;
   }
   return true;
 }
@@ -586,7 +548,7 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
   const uint32_t lane_base = (uint32_t)(32 * (warp & 3)) << 16;
   const uint32_t ts = sm.tmem + t * BN + lane_base, to = sm.tmem + 2 * BN + t * D + lane_base;
   const float nan = __int_as_float(0x7FC00000);
-  uint32_t ns = 0, no = 0, ng = 0;
+  uint32_t ns = 0, no = 0;
   // The ring slot of the next segment with rows of this tile, its query rows sent
   // to the MMAs; kEnd, kGone when a wait gave up, or kLater: while a slot is held
   // no segment is passed over, or the ring could run full of what is held.
@@ -600,6 +562,7 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
       if (sm.seg[slot].b < 0) return kEnd;
       if (sm.seg[slot].rows > t * BM) {
         rm = stage_q<D>(a, sm, t, sm.seg[slot]);
+        rm = rm < kTiny ? kTiny : rm;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(&sm.q_full[t]);
         ++is;
@@ -654,13 +617,12 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
         st_wait();
       }
 
-      // ---- the block's maximum. This loop and the next stay rolled, 64 columns a
-      // step, and what a segment does once lives in functions of its own: with
-      // everything unrolled in line the roles outgrew the instruction cache
-      float mx = -INFINITY;
-#pragma unroll 1
-      for (int q = 0; q < 8; q += 4) {
-        float v[64];
+      // ---- the block's maximum, columns 64 .. 127 first; 0 .. 63 stay in registers
+      // for their weights. What a segment does once lives in functions of its own:
+      // in line, the roles' code outgrew the instruction cache
+      float mx = -INFINITY, v[64];
+#pragma unroll
+      for (int q = 4; q >= 0; q -= 4) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) tmem_ld16(ts + 16 * (q + i), v + 16 * i);
         tmem_wait_ld(v);
@@ -669,7 +631,7 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float4 k = gc[q + i];
-          mx = fmaxf(mx, __fmaf_rn(max16(v + 16 * i), fmaxf(__fmul_rn(rm, k.x), kTiny), k.y));
+          mx = fmaxf(mx, __fmaf_rn(max16(v + 16 * i), __fmul_rn(rm, k.x), k.y));
         }
       }
 
@@ -696,19 +658,13 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
       const float off = rm < INFINITY ? kPBits - (m == -INFINITY ? 0.0f : m) : nan;
 
       // ---- weights, P over columns of S already read
-#pragma unroll 1
+#pragma unroll
       for (int q = 0; q < 8; q += 4) {
-        float v[64];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld16(ts + 16 * (q + i), v + 16 * i);
-        tmem_wait_ld(v);
-#pragma unroll
-        for (int i = 1; i < 4; ++i) tmem_tie(v + 16 * i);
         uint32_t u[32];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float4 k = gc[q + i];
-          const float kx = fmaxf(__fmul_rn(rm, k.x), kTiny), e = __fadd_rn(k.y, off);
+          const float kx = __fmul_rn(rm, k.x), e = __fadd_rn(k.y, off);
           float2 p[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -723,8 +679,17 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
           const float2 s2 = __fadd2_rn(s0, s1);
           l = __fmaf_rn(__fadd_rn(s2.x, s2.y), k.z, l);
         }
+        if (q == 0) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmem_ld16(ts + 64 + 16 * i, v + 16 * i);
+        }
         tmem_st16(ts + 8 * q, u);
         tmem_st16(ts + 8 * q + 16, u + 16);
+        if (q == 0) {
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int i = 1; i < 4; ++i) tmem_tie(v + 16 * i);
+        }
       }
       st_wait();
       tc_fence_before();
@@ -733,7 +698,7 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
     // the last block's scores are done with the query staging: the next tile's
     // rows go there while this one's last products run
     int after = next(true);
-    if (after == kGone || !finish_tile<D>(a, sm, x, t, cs, m, l, no++, &ng)) return;
+    if (after == kGone || !finish_tile<D>(a, sm, x, t, cs, m, l, no++)) return;
     __syncwarp();
     if (lane == 0) mbar_arrive(&sm.seg_empty[slot]);
     if (after == kLater) after = next(false);
@@ -746,7 +711,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
   extern __shared__ unsigned char smem_raw[];
   Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
   Walk w;
-  if (!w.start(a)) return;
+  if (!w.start(a)) {
+    if (threadIdx.x == 0) a.shared[blockIdx.x] = SharedTile{};
+    return;
+  }
   const int warp = threadIdx.x >> 5;
   if (warp == kLoadWarp) {
     if ((threadIdx.x & 31) == 0) {
@@ -758,7 +726,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
         mbar_init(&sm.s_full[i], 1);
         mbar_init(&sm.p_full[i], 128);
         mbar_init(&sm.o_full[i], 1);
-        mbar_init(&sm.group[i], 128);
         mbar_init(&sm.turn[i], 1);
           mbar_init(&sm.drain[i], 1);
       }
@@ -798,6 +765,61 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
   }
 }
 
+// Joins the parts of the shared tile that begins in block blockIdx.x's share: 32
+// rows a block, a row per lane, D / 8 dims per warp; parts in order, four of them
+// in flight. The rows leave through shared memory.
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttnArgs a) {
+  constexpr int kD = D / 8;
+  __shared__ float rows[32][D + 1];
+  const SharedTile tile = a.shared[blockIdx.x];
+  const int r0 = 32 * blockIdx.y;
+  if (r0 >= tile.rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
+  const int r = r0 + lane;
+  const bool have = r < tile.rows;
+  const int64_t at = (int64_t)(r / BM) * BM * (D + 2) + r % BM;
+  float m = -INFINITY;
+#pragma unroll 4
+  for (int k = c0; k <= tile.c1; ++k) m = fmaxf(m, partial_slot(a, k, c0)[at + D * BM]);
+  const float base = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f, o[kD];
+#pragma unroll
+  for (int j = 0; j < kD; ++j) o[j] = 0.0f;
+#pragma unroll 4
+  for (int k = c0; k <= tile.c1; ++k) {
+    const float* sp = partial_slot(a, k, c0) + at;
+    const float f = ex2(__fsub_rn(sp[D * BM], base));
+    l = __fmaf_rn(sp[(D + 1) * BM], f, l);
+#pragma unroll
+    for (int j = 0; j < kD; ++j) o[j] = __fmaf_rn(sp[(kD * warp + j) * BM], f, o[j]);
+  }
+  const float inv = l == 0.0f ? 0.0f : __frcp_rn(l);
+#pragma unroll
+  for (int j = 0; j < kD; ++j) rows[lane][kD * warp + j] = __fmul_rn(o[j], inv);
+  const RowMap map(a.c, tile.row0);
+  if (warp == 0 && have && a.lse) {
+    int tok, head;
+    map.at(r, &tok, &head);
+    a.lse[(int64_t)(tile.first + tok) * a.c.n_heads + tile.h * a.c.group + head] = lse_of(m, l);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * D / 8; i += 256) {
+    const int rr = i / (D / 8), d = i % (D / 8) * 8;
+    if (r0 + rr >= tile.rows) break;
+    int tok, head;
+    map.at(r0 + rr, &tok, &head);
+    uint32_t b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __nv_bfloat162 hb = __floats2bfloat162_rn(rows[rr][d + 2 * j], rows[rr][d + 2 * j + 1]);
+      b[j] = *reinterpret_cast<const uint32_t*>(&hb);
+    }
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(tile.first + tok) * a.out.ts +
+                              (int64_t)(tile.h * a.c.group + head) * a.out.hs + d) = make_uint4(b[0], b[1], b[2], b[3]);
+  }
+}
+
 template <int D>
 cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   constexpr int kSmem = (int)sizeof(Smem<D>) + 1024;
@@ -811,6 +833,10 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   if (grid > most) grid = most;
   paged_tiles_kernel<D><<<(unsigned)grid, kThreads, kSmem, st>>>(b);
   note_launches(1);
+  if (grid > 1) {  // one block shares no tile
+    paged_join_kernel<D><<<dim3((unsigned)grid, kRows / 32), 256, 0, st>>>(b);
+    note_launches(1);
+  }
   return cudaGetLastError();
 }
 
