@@ -32,7 +32,7 @@ AttnLayout attn_layout(const awsrc_kv_cache& c) {
   AttnLayout L{};
   L.arrived = kStatusBytes;
   L.shared = L.arrived + align_up((size_t)kMaxAttnBlocks * sizeof(int), 256);
-  L.partial = L.shared + align_up((size_t)kMaxTileBlocks * sizeof(SharedTile), 256);
+  L.partial = L.shared + align_up((size_t)kMaxAttnBlocks * sizeof(SharedTile), 256);
   L.row_slot = (int64_t)kSlotRows * (c.head_dim + 2);
   L.tile_slot = (int64_t)kTileSlotRows * (c.head_dim + 2);
   const size_t rows = (size_t)2 * kMaxAttnBlocks * L.row_slot, tiles = (size_t)2 * kMaxTileBlocks * L.tile_slot;

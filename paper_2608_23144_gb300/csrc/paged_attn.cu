@@ -22,9 +22,9 @@
 //
 // Work: the (sequence, row tile, kv head, 64-token block) units of the batch in
 // this order are dealt out in equal contiguous shares to the thread blocks,
-// whatever the lengths. A tile that several blocks share is joined by the last
-// one to arrive, in block order, from partial results in the workspace; nothing
-// waits.
+// whatever the lengths. A tile that several blocks share is joined in block order
+// from partial results in the workspace, by its last block to arrive or by a
+// second launch; nothing waits.
 #include "internal.h"
 #include "kv_paged.cuh"
 
@@ -37,6 +37,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kUnit = 64;         // tokens per unit
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPBits = 15.0f;   // p is at most 2^15
+constexpr int kMaxParts = 8;      // parts of a tile that its last block joins
 
 __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -92,6 +93,11 @@ __device__ __forceinline__ void write_final(const AttnArgs& a, const KvSeq& s, i
     a.lse[(int64_t)tok * a.c.n_heads + head] = l == 0.0f ? -INFINITY : (m - kPBits + log2f(l)) * kLn2;
 }
 
+struct Place {
+  int jk, pk, ek, ev;
+  bool kbad, pad_;
+};
+
 template <typename T, int D, int NT, int WR>
 __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<NT, WR>;
@@ -99,6 +105,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
   constexpr int kTerms = kSplit ? 2 : 1;
   constexpr int kC = D / 64;           // 16-byte runs of a token's dims per lane
   constexpr int kStride = RowStride<D>::value;
+  constexpr bool kAhead = NT == 1;     // registers for a block's keys and values ahead of their use
   __shared__ float so[S::kTokWarps][S::kRows][kStride];
   __shared__ float sm[S::kTokWarps][S::kRows], sl[S::kTokWarps][S::kRows];
   __shared__ int last_flag;
@@ -108,7 +115,11 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
   const int wr = warp % WR, wt = warp / WR;
 
   UnitWalk<S::kRows, kUnit, kWarps, 0> w;
-  if (!w.start(a)) return;
+  SharedTile mine{};
+  if (!w.start(a)) {
+    if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = mine;
+    return;
+  }
   while (w.more()) {
     const Segment sg = w.segment(a);
     const KvSeq s = w.s;
@@ -179,49 +190,87 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         for (int i = 0; i < 4; ++i) o[nt][dt][i] = 0.0f;
     }
 
-    for (int blk = sg.blk0 + wt; blk < sg.blk1; blk += S::kTokWarps) {
-      // pages of this lane's key tokens (16-token group g / 2) and value tokens (group t4)
-      const int jk = blk * kUnit + 16 * (g >> 1), jv = blk * kUnit + 16 * t4;
-      int pk = jk < s.kv ? __ldg(table + (jk >> c.log_page)) : 0;
-      int pv = __shfl_sync(0xffffffffu, pk, 8 * t4);
-      const bool bad = pk < 0 || pk >= c.n_pages;
-      if (bad) {
+    // Page and block exponents of this lane's key tokens (16-token group g / 2 of
+    // a block; its value tokens' page, group t4, comes by shuffle).
+    auto find = [&](int blk) {
+      Place p{0, 0, 0, 0, false, false};
+      p.jk = blk * kUnit + 16 * (g >> 1);
+      if (blk < sg.blk1 && p.jk < s.kv) p.pk = __ldg(table + (p.jk >> c.log_page));
+      p.kbad = p.pk < 0 || p.pk >= c.n_pages;
+      if (p.kbad) {
         atomicOr(c.status, kFaultBatch);
-        pk = 0;
+        p.pk = 0;
       }
-      const bool vbad = pv < 0 || pv >= c.n_pages;
-      if (vbad) pv = 0;
-      const int rk = jk & (c.page - 1), rv = jv & (c.page - 1);
-      const uint8_t* kb = c.k + block_off<D>(c, pk, h);
-      const uint8_t* vb = c.v + block_off<D>(c, pv, h) + (((int64_t)(rv >> 4) * D) << 4);
-      const int ek = __ldg(c.k_exp + (int64_t)pk * c.kv_heads + h), ev = __ldg(c.v_exp + (int64_t)pk * c.kv_heads + h);
+      p.ek = __ldg(c.k_exp + (int64_t)p.pk * c.kv_heads + h);
+      p.ev = __ldg(c.v_exp + (int64_t)p.pk * c.kv_heads + h);
+      return p;
+    };
+    // Key bytes of MMA row tile i (16 tokens; rows 0-7: tokens 16 (g / 2) + 4 i +
+    // g % 2, rows 8-15: two further), 16 dims at 16 t4 (+ 64).
+    uint4 kreg[4][kC][2];
+    auto load_keys = [&](const Place& p, int i) {
+      const uint8_t* kb = c.k + block_off<D>(c, p.pk, h);
+      const int row = (p.jk & (c.page - 1)) + 4 * i + (g & 1);
+#pragma unroll
+      for (int cc = 0; cc < kC; ++cc) {
+        const uint8_t* kp = kb + ((((t4 + 4 * cc) << c.log_page) + row) << 4);
+        kreg[i][cc][0] = ldg16(kp);
+        kreg[i][cc][1] = ldg16(kp + 32);
+      }
+    };
+    Place next = find(sg.blk0 + wt);
+    if (kAhead) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_keys(next, i);
+    }
+    for (int blk = sg.blk0 + wt; blk < sg.blk1; blk += S::kTokWarps) {
+      const Place cur = next;
+      const bool bad = cur.kbad;
+      const int jk = cur.jk, jv = blk * kUnit + 16 * t4, ek = cur.ek, ev = cur.ev;
+      next = find(blk + S::kTokWarps);
+      const bool vbad = __shfl_sync(0xffffffffu, bad, 8 * t4);
+      const int pv = __shfl_sync(0xffffffffu, cur.pk, 8 * t4);
+      const uint8_t* vb = c.v + block_off<D>(c, pv, h) + (((int64_t)((jv & (c.page - 1)) >> 4) * D) << 4);
+      // value bytes of 8 + 8 dims per MMA row tile, 16 tokens of group t4
+      uint4 vreg[D / 16][2];
+      auto load_values = [&](int dt) {
+        const uint8_t* vp = vb + ((16 * dt + g) << 4);
+        vreg[dt][0] = ldg16(vp);
+        vreg[dt][1] = ldg16(vp + 128);
+      };
+      if (kAhead) {
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) load_values(dt);
+      }
 
-      // ---- scores: 4 MMA row tiles of 16 tokens; tile s, rows 0-7: tokens
-      // 16 (g / 2) + 4 s + g % 2, rows 8-15: two further
+      // ---- scores
       float x[NT][4][4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
+      for (int i = 0; i < 4; ++i) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[nt][s][i] = 0.0f;
-        const int row = rk + 4 * s + (g & 1);
+          for (int j = 0; j < 4; ++j) x[nt][i][j] = 0.0f;
+        if (!kAhead) load_keys(cur, i);
 #pragma unroll
         for (int cc = 0; cc < kC; ++cc) {
-          const uint8_t* kp = kb + ((((t4 + 4 * cc) << c.log_page) + row) << 4);
           uint32_t f0[8], f1[8];
-          widen(ldg16(kp), f0);
-          widen(ldg16(kp + 32), f1);
+          widen(kreg[i][cc][0], f0);
+          widen(kreg[i][cc][1], f1);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t fr[4] = {f0[2 * i], f1[2 * i], f0[2 * i + 1], f1[2 * i + 1]};
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t fr[4] = {f0[2 * j], f1[2 * j], f0[2 * j + 1], f1[2 * j + 1]};
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int q = kTerms - 1; q >= 0; --q)
-                mma(x[nt][s], fr, qf[nt][q][8 * cc + 2 * i], qf[nt][q][8 * cc + 2 * i + 1]);
+                mma(x[nt][i], fr, qf[nt][q][8 * cc + 2 * j], qf[nt][q][8 * cc + 2 * j + 1]);
           }
         }
+      }
+      if (kAhead && blk + S::kTokWarps < sg.blk1) {  // the next block's keys load under the rest of this one
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_keys(next, i);
       }
 
       // ---- softmax weights; this lane's tokens lie in one block
@@ -294,8 +343,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
       }
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt) {
-        const uint8_t* vp = vb + ((16 * dt + g) << 4);
-        uint4 v0 = ldg16(vp), v1 = ldg16(vp + 128);
+        if (!kAhead) load_values(dt);
+        uint4 v0 = vreg[dt][0], v1 = vreg[dt][1];
         if (tail) {
           v0 = make_uint4(v0.x & keep.x, v0.y & keep.y, v0.z & keep.z, v0.w & keep.w);
           v1 = make_uint4(v1.x & keep.x, v1.y & keep.y, v1.z & keep.z, v1.w & keep.w);
@@ -359,7 +408,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         }
       }
     }
-    if (!sg.whole) {
+    if (a.shared) {
+      if (!sg.whole && sg.c0 == (int)blockIdx.x) mine = SharedTile{row0, rows, s.first, h, sg.c1, {0, 0, 0}};
+    } else if (!sg.whole) {
       __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
@@ -372,12 +423,11 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         for (int i = threadIdx.x; i < rows * D; i += kThreads) {
           const int r = i / D, d = i % D;
           float mx = -INFINITY;
-          for (int k = sg.c0; k <= sg.c1; ++k) {
-            const float* sp = partial_slot(a, k, sg.c0);
-            mx = fmaxf(mx, __ldcg(sp + S::kRows * D + r));
-          }
+#pragma unroll 4
+          for (int k = sg.c0; k <= sg.c1; ++k) mx = fmaxf(mx, __ldcg(partial_slot(a, k, sg.c0) + S::kRows * D + r));
           const float base = mx == -INFINITY ? 0.0f : mx;
           float os = 0.0f, ls = 0.0f;
+#pragma unroll 4
           for (int k = sg.c0; k <= sg.c1; ++k) {
             const float* sp = partial_slot(a, k, sg.c0);
             const float f = ex2(__fsub_rn(__ldcg(sp + S::kRows * D + r), base));
@@ -392,6 +442,52 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
 
     w.advance(a, sg);
   }
+  if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = mine;
+}
+
+// Joins the parts of the shared tile that begins in block blockIdx.x's share. A
+// block takes `RB` rows; 8 / RB warps share a row's parts, four in flight each,
+// and are added in order.
+template <typename T, int D, int ROWS, int RB>
+__global__ void __launch_bounds__(256) paged_join_rows_kernel(const __grid_constant__ AttnArgs a) {
+  constexpr int kG = 8 / RB, kV = D / 32;  // warps of a row, dims of a lane
+  __shared__ float so[8][D], sml[8][2];
+  const SharedTile tile = a.shared[blockIdx.x];
+  if ((int)blockIdx.y * RB >= tile.rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
+  const int r = min((int)blockIdx.y * RB + warp / kG, tile.rows - 1), part = warp % kG;
+  float m = -INFINITY, l = 0.0f, o[kV];
+  for (int k = c0 + lane; k <= tile.c1; k += 32) m = fmaxf(m, partial_slot(a, k, c0)[ROWS * D + r]);
+#pragma unroll
+  for (int i = 16; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+  const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int j = 0; j < kV; ++j) o[j] = 0.0f;
+#pragma unroll 4
+  for (int k = c0 + part; k <= tile.c1; k += kG) {
+    const float* sp = partial_slot(a, k, c0);
+    const float f = ex2(__fsub_rn(sp[ROWS * D + r], base));
+    l = __fmaf_rn(sp[ROWS * D + ROWS + r], f, l);
+#pragma unroll
+    for (int j = 0; j < kV; ++j) o[j] = __fmaf_rn(sp[r * D + 32 * j + lane], f, o[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < kV; ++j) so[warp][32 * j + lane] = o[j];
+  if (lane == 0) sml[warp][0] = l;
+  __syncthreads();
+  if (part != 0 || (int)blockIdx.y * RB + warp / kG >= tile.rows) return;
+  // l of the row first, then its dims
+  l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kG; ++k) l = __fadd_rn(l, sml[warp + k][0]);
+  KvSeq s{tile.first, 0, 0};
+#pragma unroll
+  for (int j = 0; j < kV; ++j) {
+    float v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kG; ++k) v = __fadd_rn(v, so[warp + k][32 * j + lane]);
+    write_final<T, D>(a, s, tile.row0 + r, tile.h, 32 * j + lane, v, m, l);
+  }
 }
 
 template <typename T, int D, int NT, int WR>
@@ -402,8 +498,18 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   int64_t grid = kMaxAttnBlocks;
   const int64_t most = tiles * a.c.kv_heads * max_blocks;
   if (grid > most) grid = most;
+  // A tile of few parts is joined by its last block to arrive; where there can be
+  // more, its serial reading took 40 us of a 131k-token decode step, and a second
+  // launch joins all tiles on the whole GPU.
+  const bool join = max_blocks / b.min_units > kMaxParts;
+  if (!join) b.shared = nullptr;
   paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, kThreads, 0, st>>>(b);
   note_launches(1);
+  if (join) {
+    constexpr int kRows = Shape<NT, WR>::kRows, kRB = kRows <= 16 ? 1 : 8;
+    paged_join_rows_kernel<T, D, kRows, kRB><<<dim3((unsigned)grid, kRows / kRB), 256, 0, st>>>(b);
+    note_launches(1);
+  }
   return cudaGetLastError();
 }
 
