@@ -74,11 +74,11 @@ __device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t codes) {
   return r;
 }
 
-// Attention: thread blocks a launch may have (two per SM), each with two slots
+// Attention: thread blocks a launch may have (one per SM), each with two slots
 // for partial results of the first and last tile it shares with others.
-constexpr int kMaxAttnBlocks = 304;
-constexpr int kSlotRows = 64;
-// The tensor-memory kernel: one per SM, 256 rows.
+constexpr int kMaxAttnBlocks = 152;
+constexpr int kSlotRows = 128;
+// The tensor-memory kernel: 256 rows.
 constexpr int kMaxTileBlocks = 152;
 constexpr int kTileSlotRows = 256;
 
@@ -87,13 +87,13 @@ struct AttnArgs {
   KvRows q, out;
   float* lse;
   float score_mul;  // sm_scale log2(e)
-  int causal;
+  int causal, vec;  // vec: rows of q are 16-byte aligned
   int min_units;    // least share of a block
   int* arrived;     // per block: arrivals at the shared tile that begins in its share (row kernel)
   struct SharedTile* shared;  // per block: the shared tile that begins in its share (tensor-memory kernel)
   float* partial;
   int64_t slot_floats;
-  uint64_t wait_ns;  // limit of the tensor-memory kernel's waits
+  uint64_t wait_ns;  // limit of the kernels' waits
   int stall;         // test of that limit: no copies from this block of tokens on (-1: never)
 };
 

@@ -15,10 +15,18 @@
 // F32 splits q (scaled by a power of two per row) and p into two binary16 terms;
 // the second term costs one more MMA on the same codes.
 //
-// Bound by the cache's bytes when rows are few. A warp takes 64 tokens at a
-// time: its lanes read 16-byte runs straight into MMA fragments (the cache's
-// byte order is chosen for that), the order of tokens and dims inside the
-// fragments being free as long as both operands agree.
+// Bound by the cache's bytes when rows are few. A block is 64 tokens; its keys
+// and values come to shared memory by bulk copies (8 to 16 KB pieces, the cache's
+// byte order being what the fragments want), one or two ahead of the products, so
+// that what is in flight does not cost registers: loaded straight into registers,
+// two blocks ahead made 57 KB of unrolled code whose cold fetch alone was 20 us of
+// a single token's step. Lanes read 4-byte words without bank conflicts (keys:
+// two-way). Fragment slots of lane (g, t): dims 16 i + 4 t + {0..3} in step i of
+// q . k, tokens 16 s + 4 t + {0..3} in step s of p . V; score row tile s has token
+// 16 s + 4 (g / 2) + g % 2 in row g and two further in row 8 + g.
+//
+// Decode (one row tile): every warp has its own ring and takes every eighth block
+// of a segment. Many rows: the warps hold 16 rows each and share one ring.
 //
 // Work: the (sequence, row tile, kv head, 64-token block) units of the batch in
 // this order are dealt out in equal contiguous shares to the thread blocks,
@@ -27,12 +35,15 @@
 // second launch; nothing waits.
 #include "internal.h"
 #include "kv_paged.cuh"
+#include "tc05.cuh"
 
 namespace awsrc {
 
 namespace {
 
-constexpr int kThreads = 128;
+using namespace tc05;
+
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kUnit = 64;         // tokens per unit
 constexpr float kLn2 = 0.6931471805599453f;
@@ -59,14 +70,29 @@ __device__ __forceinline__ uint32_t half2_bits(float a, float b) {
 }
 __device__ __forceinline__ float2 half2_floats(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
-__device__ __forceinline__ uint4 ldg16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
-
 template <typename T>
-__device__ __forceinline__ float elem(const T* p);
+__device__ __forceinline__ void load4(const T* p, bool vec, float* x);
 template <>
-__device__ __forceinline__ float elem(const float* p) { return __ldg(p); }
+__device__ __forceinline__ void load4(const float* p, bool vec, float* x) {
+  if (vec) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = p[i];
+  }
+}
 template <>
-__device__ __forceinline__ float elem(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, bool vec, float* x) {
+  if (vec) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+    x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __bfloat162float(p[i]);
+  }
+}
 
 template <int NT, int WR>
 struct Shape {
@@ -93,26 +119,45 @@ __device__ __forceinline__ void write_final(const AttnArgs& a, const KvSeq& s, i
     a.lse[(int64_t)tok * a.c.n_heads + head] = l == 0.0f ? -INFINITY : (m - kPBits + log2f(l)) * kLn2;
 }
 
+// Shared memory: a ring of key and value blocks per token group; the warps'
+// results lie over it at a segment's end.
+template <int D, int NT, int WR>
+struct RowsSmem {
+  using S = Shape<NT, WR>;
+  static constexpr int kG = S::kTokWarps;                            // token groups
+  static constexpr int NK = WR == 1 ? 2 : 3, NV = WR == 1 ? (D == 64 ? 2 : 1) : 3;
+  union {
+    struct {
+      uint8_t k[kG][NK][kUnit * D], v[kG][NV][kUnit * D];
+    } ring;
+    struct {
+      float o[kG][S::kRows][RowStride<D>::value], m[kG][S::kRows], l[kG][S::kRows];
+    } out;
+  };
+  unsigned long long k_full[kG][NK], k_empty[kG][NK], v_full[kG][NV], v_empty[kG][NV];
+  int dead, last;
+};
+
+// What lanes 0 .. 3 know about the 16-token groups of a block: tokens in it (0
+// for a page that cannot be right), its page and exponents.
 struct Place {
-  int jk, pk, ek, ev;
-  bool kbad, pad_;
+  int pg, have, ek, ev;
 };
 
 template <typename T, int D, int NT, int WR>
-__global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<NT, WR>;
+  using Mem = RowsSmem<D, NT, WR>;
   constexpr bool kSplit = sizeof(T) == 4;
   constexpr int kTerms = kSplit ? 2 : 1;
-  constexpr int kC = D / 64;           // 16-byte runs of a token's dims per lane
-  constexpr int kStride = RowStride<D>::value;
-  constexpr bool kAhead = NT == 1;     // registers for a block's keys and values ahead of their use
-  __shared__ float so[S::kTokWarps][S::kRows][kStride];
-  __shared__ float sm[S::kTokWarps][S::kRows], sl[S::kTokWarps][S::kRows];
-  __shared__ int last_flag;
+  constexpr int kI = D / 16;           // steps of q . k, and row tiles of p . V
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  Mem& sm = *reinterpret_cast<Mem*>(smem_raw);
   const KvArgs& c = a.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t4 = lane & 3;
   const int wr = warp % WR, wt = warp / WR;
+  const int log_pe = min(c.log_page, 6);  // tokens of a page within a block
 
   UnitWalk<S::kRows, kUnit, kWarps, 0> w;
   SharedTile mine{};
@@ -120,38 +165,117 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
     if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = mine;
     return;
   }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < Mem::kG; ++i) {
+      for (int j = 0; j < Mem::NK; ++j) mbar_init(&sm.k_full[i][j], 1), mbar_init(&sm.k_empty[i][j], WR);
+      for (int j = 0; j < Mem::NV; ++j) mbar_init(&sm.v_full[i][j], 1), mbar_init(&sm.v_empty[i][j], WR);
+    }
+    sm.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  // Bounded; once one has given up, all return at once and the results are void.
+  auto wait = [&](unsigned long long* mb, uint32_t parity) {
+    if (mbar_try_wait(mb, parity)) return;
+    const uint64_t t0 = globaltimer();
+    while (!mbar_try_wait(mb, parity)) {
+      if (*(volatile int*)&sm.dead) return;
+      if (globaltimer() - t0 > a.wait_ns) {
+        *(volatile int*)&sm.dead = 1;
+        atomicOr(c.status, kFaultTimeout);
+        return;
+      }
+    }
+  };
+
+  uint32_t nk = 0, nv = 0;  // blocks of this group so far: issued by its first warp, waited for by all
+  uint32_t ik = 0, iv = 0;
   while (w.more()) {
     const Segment sg = w.segment(a);
     const KvSeq s = w.s;
     const int h = sg.h, rows = sg.rows, row0 = w.t * S::kRows;
     const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
 
-    // ---- query fragments: row r0 + 8 nt + g, dims 16 t4 .. + 15 (+ 64)
-    uint32_t qf[NT][kTerms][kC * 8];
+    auto find = [&](int blk) {  // lanes 0 .. 3
+      Place p{0, 0, 0, 0};
+      const int j = blk * kUnit + 16 * (lane & 3);
+      if (lane < 4 && blk < sg.blk1 && j < s.kv) {
+        const int pg = __ldg(table + (j >> c.log_page));
+        if (pg >= 0 && pg < c.n_pages) {
+          p.pg = pg;
+          p.have = min(16, s.kv - j);
+          p.ek = __ldg(c.k_exp + (int64_t)pg * c.kv_heads + h);
+          p.ev = __ldg(c.v_exp + (int64_t)pg * c.kv_heads + h);
+        } else {
+          atomicOr(c.status, kFaultBatch);
+        }
+      }
+      return p;
+    };
+    // The copies of a block's keys or values by the group's first warp: whole
+    // pages, or half a page of 128 tokens (keys then in one piece per 16 dims).
+    auto copy = [&](const Place& p, int blk, bool keys) {
+      const uint32_t n = keys ? ik++ : iv++;
+      const int st = keys ? n % Mem::NK : n % Mem::NV;
+      unsigned long long* full = keys ? &sm.k_full[wt][st] : &sm.v_full[wt][st];
+      wait(keys ? &sm.k_empty[wt][st] : &sm.v_empty[wt][st], ((n / (keys ? Mem::NK : Mem::NV)) & 1) ^ 1);
+      uint8_t* dst = keys ? sm.ring.k[wt][st] : sm.ring.v[wt][st];
+      const uint8_t* src = keys ? c.k : c.v;
+      // lane i < 4: group i; the first group of a page copies it
+      const bool first = lane < 4 && ((16 * lane) & ((1 << log_pe) - 1)) == 0 && p.have > 0;
+      const uint32_t bytes = (uint32_t)D << log_pe;
+      const uint32_t all = __popc(__ballot_sync(0xffffffffu, first)) * bytes;
+      const bool go = a.stall < 0 || (int)n < a.stall;
+      if (lane == 0 && go) mbar_expect_tx(full, all);
+      __syncwarp();
+      if (!go) return;
+      if (c.log_page <= 6) {
+        if (first) bulk_g2s(dst + lane * 16 * D, src + block_off<D>(c, p.pg, h), bytes, full);
+      } else {
+        const int pg = __shfl_sync(0xffffffffu, p.pg, 0), half = blk & 1;
+        const bool have = __shfl_sync(0xffffffffu, p.have, 0) > 0;
+        if (have && keys && lane < kI)
+          bulk_g2s(dst + lane * kUnit * 16, src + block_off<D>(c, pg, h) + ((lane * 128 + half * kUnit) << 4), kUnit * 16, full);
+        if (have && !keys && lane == 0) bulk_g2s(dst, src + block_off<D>(c, pg, h) + half * kUnit * D, kUnit * D, full);
+      }
+    };
+
+    // ---- the first blocks on their way
+    const int b0 = sg.blk0 + wt;
+    Place cur = find(b0);
+    Place nx[Mem::NK - 1];  // blocks whose keys are on their way behind it
+#pragma unroll
+    for (int i = 0; i < Mem::NK - 1; ++i) nx[i] = find(b0 + (i + 1) * S::kTokWarps);
+    if (wr == 0) {
+      if (b0 < sg.blk1) copy(cur, b0, true), copy(cur, b0, false);
+#pragma unroll
+      for (int i = 0; i < Mem::NK - 1; ++i) {
+        const int b = b0 + (i + 1) * S::kTokWarps;
+        if (b < sg.blk1) {
+          copy(nx[i], b, true);
+          if (i + 1 < Mem::NV) copy(nx[i], b, false);
+        }
+      }
+    }
+
+    // ---- query fragments: row wr kRowsPerWarp + 8 nt + g; a row past the last repeats it
+    uint32_t qf[NT][kTerms][2 * kI];
     float rm[NT][2];     // score multiplier of rows 2 t4, 2 t4 + 1
     int lim[NT][2];      // last token these rows see
     int lim_min = INT32_MAX;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = wr * S::kRowsPerWarp + 8 * nt + g;
-      const int row = row0 + r;
       const bool have = r < rows;
-      const int tok = row / c.group;
-      float x[kC * 16];
-      if (have) {
-        const T* p = static_cast<const T*>(a.q.p) + (int64_t)(s.first + tok) * a.q.ts +
-                     (int64_t)(h * c.group + row % c.group) * a.q.hs + 16 * t4;
+      const int row = row0 + min(r, rows - 1), tok = row / c.group;
+      float x[4 * kI];
+      const T* p = static_cast<const T*>(a.q.p) + (int64_t)(s.first + tok) * a.q.ts +
+                   (int64_t)(h * c.group + row - tok * c.group) * a.q.hs + 4 * t4;
 #pragma unroll
-        for (int i = 0; i < kC; ++i)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) x[16 * i + j] = elem<T>(p + 64 * i + j);
-      } else {
-#pragma unroll
-        for (int i = 0; i < kC * 16; ++i) x[i] = 0.0f;
-      }
+      for (int i = 0; i < kI; ++i) load4(p + 16 * i, a.vec, x + 4 * i);
       float amax = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kC * 16; ++i) amax = fmaxf(amax, fabsf(x[i]));
+      for (int i = 0; i < 4 * kI; ++i) amax = fmaxf(amax, fabsf(x[i]));
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
       // the row times 2^up has its largest element in [2^14, 2^15)
@@ -159,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
       const int up = min(max(14 - ex, -120), 100);
       const float f = pow2f(up), mul = a.score_mul * pow2f(-up);
 #pragma unroll
-      for (int i = 0; i < kC * 8; ++i) {
+      for (int i = 0; i < 2 * kI; ++i) {
         const float y0 = __fmul_rn(x[2 * i], f), y1 = __fmul_rn(x[2 * i + 1], f);
         qf[nt][0][i] = half2_bits(y0, y1);
         if constexpr (kSplit) {
@@ -179,191 +303,150 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
       lim_min = min(lim_min, lo);
     }
 
-    float o[NT][D / 16][4], m[NT][2], l[NT][2];
+    float o[NT][kI][4], m[NT][2], l[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) m[nt][i] = -INFINITY, l[nt][i] = 0.0f;
 #pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt)
+      for (int dt = 0; dt < kI; ++dt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[nt][dt][i] = 0.0f;
     }
 
-    // Page and block exponents of this lane's key tokens (16-token group g / 2 of
-    // a block; its value tokens' page, group t4, comes by shuffle).
-    auto find = [&](int blk) {
-      Place p{0, 0, 0, 0, false, false};
-      p.jk = blk * kUnit + 16 * (g >> 1);
-      if (blk < sg.blk1 && p.jk < s.kv) p.pk = __ldg(table + (p.jk >> c.log_page));
-      p.kbad = p.pk < 0 || p.pk >= c.n_pages;
-      if (p.kbad) {
-        atomicOr(c.status, kFaultBatch);
-        p.pk = 0;
-      }
-      p.ek = __ldg(c.k_exp + (int64_t)p.pk * c.kv_heads + h);
-      p.ev = __ldg(c.v_exp + (int64_t)p.pk * c.kv_heads + h);
-      return p;
-    };
-    // Key bytes of MMA row tile i (16 tokens; rows 0-7: tokens 16 (g / 2) + 4 i +
-    // g % 2, rows 8-15: two further), 16 dims at 16 t4 (+ 64).
-    uint4 kreg[4][kC][2];
-    auto load_keys = [&](const Place& p, int i) {
-      const uint8_t* kb = c.k + block_off<D>(c, p.pk, h);
-      const int row = (p.jk & (c.page - 1)) + 4 * i + (g & 1);
-#pragma unroll
-      for (int cc = 0; cc < kC; ++cc) {
-        const uint8_t* kp = kb + ((((t4 + 4 * cc) << c.log_page) + row) << 4);
-        kreg[i][cc][0] = ldg16(kp);
-        kreg[i][cc][1] = ldg16(kp + 32);
-      }
-    };
-    Place next = find(sg.blk0 + wt);
-    if (kAhead) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) load_keys(next, i);
-    }
-    for (int blk = sg.blk0 + wt; blk < sg.blk1; blk += S::kTokWarps) {
-      const Place cur = next;
-      const bool bad = cur.kbad;
-      const int jk = cur.jk, jv = blk * kUnit + 16 * t4, ek = cur.ek, ev = cur.ev;
-      next = find(blk + S::kTokWarps);
-      const bool vbad = __shfl_sync(0xffffffffu, bad, 8 * t4);
-      const int pv = __shfl_sync(0xffffffffu, cur.pk, 8 * t4);
-      const uint8_t* vb = c.v + block_off<D>(c, pv, h) + (((int64_t)((jv & (c.page - 1)) >> 4) * D) << 4);
-      // value bytes of 8 + 8 dims per MMA row tile, 16 tokens of group t4
-      uint4 vreg[D / 16][2];
-      auto load_values = [&](int dt) {
-        const uint8_t* vp = vb + ((16 * dt + g) << 4);
-        vreg[dt][0] = ldg16(vp);
-        vreg[dt][1] = ldg16(vp + 128);
-      };
-      if (kAhead) {
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) load_values(dt);
-      }
+    for (int blk = b0; blk < sg.blk1; blk += S::kTokWarps) {
+      const float nan = __int_as_float(0x7FC00000);
+      const Place far = find(blk + Mem::NK * S::kTokWarps);
+      // some row is hidden from some token, or a group is short or marked
+      const bool odd = cur.have < 16 || cur.ek == kExpNan || cur.ev == kExpNan;
+      const bool masked = blk * kUnit + kUnit - 1 > lim_min || __any_sync(0xffffffffu, lane < 4 && odd);
 
       // ---- scores
+      const int ks = nk % Mem::NK;
+      wait(&sm.k_full[wt][ks], (nk / Mem::NK) & 1);
+      ++nk;
       float x[NT][4][4];
+      const uint8_t* kb = sm.ring.k[wt][ks] + (4 * (g >> 1) + (g & 1)) * 16 + 4 * t4;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[nt][i][j] = 0.0f;
-        if (!kAhead) load_keys(cur, i);
+        const uint8_t* kp = kb + ((16 * i) >> log_pe) * (D << log_pe) + ((16 * i) & ((1 << log_pe) - 1)) * 16;
 #pragma unroll
-        for (int cc = 0; cc < kC; ++cc) {
-          uint32_t f0[8], f1[8];
-          widen(kreg[i][cc][0], f0);
-          widen(kreg[i][cc][1], f1);
+        for (int j = 0; j < kI; ++j) {
+          const uint32_t w0 = *reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4)));
+          const uint32_t w1 = *reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4)) + 32);
+          const uint32_t fr[4] = {e4m3x2_half2(w0 & 0xFFFFu), e4m3x2_half2(w1 & 0xFFFFu), e4m3x2_half2(w0 >> 16),
+                                  e4m3x2_half2(w1 >> 16)};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t fr[4] = {f0[2 * j], f1[2 * j], f0[2 * j + 1], f1[2 * j + 1]};
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int q = kTerms - 1; q >= 0; --q)
-                mma(x[nt][i], fr, qf[nt][q][8 * cc + 2 * j], qf[nt][q][8 * cc + 2 * j + 1]);
-          }
+            for (int q = kTerms - 1; q >= 0; --q) mma(x[nt][i], fr, qf[nt][q][2 * j], qf[nt][q][2 * j + 1]);
         }
       }
-      if (kAhead && blk + S::kTokWarps < sg.blk1) {  // the next block's keys load under the rest of this one
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_keys(next, i);
-      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.k_empty[wt][ks]);
+      if (wr == 0 && blk + Mem::NK * S::kTokWarps < sg.blk1) copy(far, blk + Mem::NK * S::kTokWarps, true);
 
-      // ---- softmax weights; this lane's tokens lie in one block
-      const float nan = __int_as_float(0x7FC00000);
-      const float sk = ek == kExpNan ? nan : pow2f(ek), evf = ev == kExpNan ? nan : (float)ev;
-      const float un = ev == kExpNan ? nan : pow2f(-ev);
-      const bool masked = blk * kUnit + kUnit - 1 > lim_min || __any_sync(0xffffffffu, bad);
+      // ---- softmax weights
       uint32_t pf[NT][kTerms][8];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float k = __fmul_rn(rm[nt][i], sk);
+        for (int i = 0; i < 4; ++i) {
+          const int ek = __shfl_sync(0xffffffffu, cur.ek, i), ev = __shfl_sync(0xffffffffu, cur.ev, i);
+          const int have = __shfl_sync(0xffffffffu, cur.have, i);
+          const float sk = pow2f(ek), ef = ek == kExpNan || ev == kExpNan ? nan : (float)ev;
+          const int j0 = blk * kUnit + 16 * i + 4 * (g >> 1) + (g & 1);
+          const int end = blk * kUnit + 16 * i + have;
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              float y = __fmaf_rn(x[nt][s][2 * hf + i], k, evf);
-              if (masked && (bad || jk + 4 * s + (g & 1) + 2 * hf > lim[nt][i])) y = -INFINITY;
-              x[nt][s][2 * hf + i] = y;
-              mx[i] = fmaxf(mx[i], y);
-            }
-#pragma unroll
-          for (int of = 4; of < 32; of <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], of));
-          const float mn = fmaxf(m[nt][i], mx[i]);
-          const float base = mn == -INFINITY ? 0.0f : mn;
-          const float al = ex2(__fsub_rn(m[nt][i], base));
-          m[nt][i] = mn;
-          float sum = 0.0f;
-#pragma unroll
-          for (int s = 0; s < 4; ++s)
+          for (int q = 0; q < 2; ++q) {
+            const float k = __fmul_rn(rm[nt][q], sk);
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              const float p = ex2(__fsub_rn(x[nt][s][2 * hf + i], __fsub_rn(base, kPBits)));
-              x[nt][s][2 * hf + i] = p;
-              sum = __fadd_rn(sum, p);
+              float y = __fmaf_rn(x[nt][i][2 * hf + q], k, ef);
+              if (masked && (j0 + 2 * hf >= end || j0 + 2 * hf > lim[nt][q])) y = -INFINITY;
+              x[nt][i][2 * hf + q] = y;
+              mx[q] = fmaxf(mx[q], y);
             }
-          l[nt][i] = __fmaf_rn(l[nt][i], al, sum == 0.0f ? 0.0f : __fmul_rn(sum, un));
+          }
+        }
+        float base[2];
 #pragma unroll
-          for (int dt = 0; dt < D / 16; ++dt) {
-            o[nt][dt][i] = __fmul_rn(o[nt][dt][i], al);
-            o[nt][dt][2 + i] = __fmul_rn(o[nt][dt][2 + i], al);
+        for (int q = 0; q < 2; ++q) {
+#pragma unroll
+          for (int of = 4; of < 32; of <<= 1) mx[q] = fmaxf(mx[q], __shfl_xor_sync(0xffffffffu, mx[q], of));
+          const float mn = fmaxf(m[nt][q], mx[q]);
+          const float bs = mn == -INFINITY ? 0.0f : mn;
+          const float al = ex2(__fsub_rn(m[nt][q], bs));
+          m[nt][q] = mn;
+          base[q] = __fsub_rn(bs, kPBits);
+          l[nt][q] = __fmul_rn(l[nt][q], al);
+#pragma unroll
+          for (int dt = 0; dt < kI; ++dt) {
+            o[nt][dt][q] = __fmul_rn(o[nt][dt][q], al);
+            o[nt][dt][2 + q] = __fmul_rn(o[nt][dt][2 + q], al);
           }
         }
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int i = 0; i < 4; ++i) {
+          const int ev = __shfl_sync(0xffffffffu, cur.ev, i);
+          const float un = pow2f(ev == kExpNan ? 0 : -ev);
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
-            const float p0 = x[nt][s][2 * hf], p1 = x[nt][s][2 * hf + 1];
+            const float p0 = ex2(__fsub_rn(x[nt][i][2 * hf], base[0])), p1 = ex2(__fsub_rn(x[nt][i][2 * hf + 1], base[1]));
+            l[nt][0] = __fmaf_rn(p0, un, l[nt][0]);
+            l[nt][1] = __fmaf_rn(p1, un, l[nt][1]);
             const uint32_t hi = half2_bits(p0, p1);
-            pf[nt][0][2 * s + hf] = transpose8(hi);
+            pf[nt][0][2 * i + hf] = transpose8(hi);
             if constexpr (kSplit) {
               const float2 b = half2_floats(hi);
-              pf[nt][1][2 * s + hf] = transpose8(half2_bits(__fsub_rn(p0, b.x), __fsub_rn(p1, b.y)));
+              pf[nt][1][2 * i + hf] = transpose8(half2_bits(__fsub_rn(p0, b.x), __fsub_rn(p1, b.y)));
             }
           }
+        }
       }
 
-      // ---- O^T += V^T P^T: MMA row tiles of 16 dims, 4 steps of 16 tokens.
-      // Rows that hold no token yet may hold any bytes, e4m3's NaN among them.
-      const bool tail = masked && (blk * kUnit + kUnit > s.kv || __any_sync(0xffffffffu, vbad));
-      uint4 keep = make_uint4(~0u, ~0u, ~0u, ~0u);
-      if (tail) {
-        const int have = vbad ? 0 : s.kv - jv;
-        keep.x = first_bytes(have);
-        keep.y = first_bytes(have - 4);
-        keep.z = first_bytes(have - 8);
-        keep.w = first_bytes(have - 12);
+      // ---- O^T += V^T P^T: row tiles of 16 dims, 4 steps of 16 tokens. Rows that
+      // hold no token may hold any bytes, e4m3's NaN among them.
+      const int vs = nv % Mem::NV;
+      wait(&sm.v_full[wt][vs], (nv / Mem::NV) & 1);
+      ++nv;
+      uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keep[i] = first_bytes(__shfl_sync(0xffffffffu, cur.have, i) - 4 * t4);
       }
+      const uint8_t* vb = sm.ring.v[wt][vs] + g * 16 + 4 * t4;
 #pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) {
-        if (!kAhead) load_values(dt);
-        uint4 v0 = vreg[dt][0], v1 = vreg[dt][1];
-        if (tail) {
-          v0 = make_uint4(v0.x & keep.x, v0.y & keep.y, v0.z & keep.z, v0.w & keep.w);
-          v1 = make_uint4(v1.x & keep.x, v1.y & keep.y, v1.z & keep.z, v1.w & keep.w);
-        }
-        uint32_t f0[8], f1[8];
-        widen(v0, f0);
-        widen(v1, f1);
+      for (int dt = 0; dt < kI; ++dt) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const uint32_t fr[4] = {f0[2 * s], f1[2 * s], f0[2 * s + 1], f1[2 * s + 1]};
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vb + (i * D + 16 * dt) * 16) & keep[i];
+          const uint32_t w1 = *reinterpret_cast<const uint32_t*>(vb + (i * D + 16 * dt + 8) * 16) & keep[i];
+          const uint32_t fr[4] = {e4m3x2_half2(w0 & 0xFFFFu), e4m3x2_half2(w1 & 0xFFFFu), e4m3x2_half2(w0 >> 16),
+                                  e4m3x2_half2(w1 >> 16)};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int q = kTerms - 1; q >= 0; --q) mma(o[nt][dt], fr, pf[nt][q][2 * s], pf[nt][q][2 * s + 1]);
+            for (int q = kTerms - 1; q >= 0; --q) mma(o[nt][dt], fr, pf[nt][q][2 * i], pf[nt][q][2 * i + 1]);
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.v_empty[wt][vs]);
+      if (wr == 0 && blk + Mem::NV * S::kTokWarps < sg.blk1)
+        copy(Mem::NV == Mem::NK ? far : nx[Mem::NV - 1], blk + Mem::NV * S::kTokWarps, false);
+      cur = nx[0];
+#pragma unroll
+      for (int i = 0; i + 1 < Mem::NK - 1; ++i) nx[i] = nx[i + 1];
+      nx[Mem::NK - 2] = far;
     }
 
-    // ---- the warps' results to shared memory
+    // ---- the warps' results to shared memory, over the ring
+    __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -373,30 +456,29 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         for (int of = 4; of < 32; of <<= 1) t = __fadd_rn(t, __shfl_xor_sync(0xffffffffu, t, of));
         const int r = wr * S::kRowsPerWarp + 8 * nt + 2 * t4 + i;
         if (g == 0) {
-          sm[wt][r] = m[nt][i];
-          sl[wt][r] = t;
+          sm.out.m[wt][r] = m[nt][i];
+          sm.out.l[wt][r] = t;
         }
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) {
-          so[wt][r][16 * dt + g] = o[nt][dt][i];
-          so[wt][r][16 * dt + 8 + g] = o[nt][dt][2 + i];
+        for (int dt = 0; dt < kI; ++dt) {
+          sm.out.o[wt][r][16 * dt + g] = o[nt][dt][i];
+          sm.out.o[wt][r][16 * dt + 8 + g] = o[nt][dt][2 + i];
         }
       }
     __syncthreads();
-
     float* slot = partial_slot(a, blockIdx.x, sg.c0);
     for (int i = threadIdx.x; i < rows * D; i += kThreads) {
       const int r = i / D, d = i % D;
-      float mx = sm[0][r];
+      float mx = sm.out.m[0][r];
 #pragma unroll
-      for (int k = 1; k < S::kTokWarps; ++k) mx = fmaxf(mx, sm[k][r]);
+      for (int k = 1; k < S::kTokWarps; ++k) mx = fmaxf(mx, sm.out.m[k][r]);
       const float base = mx == -INFINITY ? 0.0f : mx;
       float os = 0.0f, ls = 0.0f;
 #pragma unroll
       for (int k = 0; k < S::kTokWarps; ++k) {
-        const float f = ex2(__fsub_rn(sm[k][r], base));
-        os = __fmaf_rn(so[k][r][d], f, os);
-        ls = __fmaf_rn(sl[k][r], f, ls);
+        const float f = ex2(__fsub_rn(sm.out.m[k][r], base));
+        os = __fmaf_rn(sm.out.o[k][r][d], f, os);
+        ls = __fmaf_rn(sm.out.l[k][r], f, ls);
       }
       if (sg.whole) {
         write_final<T, D>(a, s, row0 + r, h, d, os, mx, ls);
@@ -414,11 +496,11 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
       __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
-        last_flag = atomicAdd(a.arrived + sg.c0, 1) == sg.c1 - sg.c0;
-        if (last_flag) a.arrived[sg.c0] = 0;  // as every call leaves it
+        sm.last = atomicAdd(a.arrived + sg.c0, 1) == sg.c1 - sg.c0;
+        if (sm.last) a.arrived[sg.c0] = 0;  // as every call leaves it
       }
       __syncthreads();
-      if (last_flag) {
+      if (sm.last) {
         __threadfence();
         for (int i = threadIdx.x; i < rows * D; i += kThreads) {
           const int r = i / D, d = i % D;
@@ -438,9 +520,16 @@ __global__ void __launch_bounds__(kThreads, 2) paged_rows_kernel(const __grid_co
         }
       }
     }
-    __syncthreads();  // shared memory is free for the next segment
-
+    // the next segment's copies land where this one's results were
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
     w.advance(a, sg);
+  }
+  if (sm.dead && wr == 0 && lane == 0) {  // copies in flight land before the block ends
+    for (uint32_t i = ik > Mem::NK ? ik - Mem::NK : 0; i < ik; ++i)
+      (void)mbar_wait(&sm.k_full[wt][i % Mem::NK], (i / Mem::NK) & 1, a.wait_ns);
+    for (uint32_t i = iv > Mem::NV ? iv - Mem::NV : 0; i < iv; ++i)
+      (void)mbar_wait(&sm.v_full[wt][i % Mem::NV], (i / Mem::NV) & 1, a.wait_ns);
   }
   if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = mine;
 }
@@ -493,8 +582,14 @@ __global__ void __launch_bounds__(256) paged_join_rows_kernel(const __grid_const
 template <typename T, int D, int NT, int WR>
 cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   const int64_t tiles = tiles_upper(a.c, Shape<NT, WR>::kRows);
+  using Mem = RowsSmem<D, NT, WR>;
+  static_assert(sizeof(Mem) <= 227 * 1024, "shared memory of a block");
+  const cudaError_t e =
+      cudaFuncSetAttribute(paged_rows_kernel<T, D, NT, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Mem));
+  if (e != cudaSuccess) return e;
   AttnArgs b = a;
-  b.min_units = Shape<NT, WR>::kTokWarps;
+  b.min_units = 2 * Shape<NT, WR>::kTokWarps;
+  b.vec = rows_aligned(a.q, sizeof(T));
   int64_t grid = kMaxAttnBlocks;
   const int64_t most = tiles * a.c.kv_heads * max_blocks;
   if (grid > most) grid = most;
@@ -503,7 +598,7 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   // launch joins all tiles on the whole GPU.
   const bool join = max_blocks / b.min_units > kMaxParts;
   if (!join) b.shared = nullptr;
-  paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, kThreads, 0, st>>>(b);
+  paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, kThreads, sizeof(Mem), st>>>(b);
   note_launches(1);
   if (join) {
     constexpr int kRows = Shape<NT, WR>::kRows, kRB = kRows <= 16 ? 1 : 8;
@@ -518,7 +613,7 @@ cudaError_t pick(const AttnArgs& a, int max_new, int64_t max_blocks, cudaStream_
   const int64_t rows = (int64_t)max_new * a.c.group;
   if (rows <= 8) return launch<T, D, 1, 1>(a, max_blocks, st);
   if (rows <= 16) return launch<T, D, 2, 1>(a, max_blocks, st);
-  return launch<T, D, 2, 4>(a, max_blocks, st);
+  return launch<T, D, 2, 8>(a, max_blocks, st);
 }
 
 }  // namespace
