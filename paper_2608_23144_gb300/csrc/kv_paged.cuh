@@ -284,14 +284,18 @@ __device__ __forceinline__ float ex2(float x) {
 // A word whose first n bytes are ones.
 __device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (n <= 0 ? 0u : (1u << (8 * n)) - 1u); }
 
+// 4 codes -> binary16 pairs.
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+}
+
 // 16 codes -> binary16 pairs in order.
 __device__ __forceinline__ void widen(const uint4& v, uint32_t* f) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = e4m3x2_half2(w[i] & 0xFFFFu);
-    f[2 * i + 1] = e4m3x2_half2(w[i] >> 16);
-  }
+  for (int i = 0; i < 4; ++i) widen4(w[i], f[2 * i], f[2 * i + 1]);
 }
 
 // Row tiles a batch can have at most.

@@ -25,8 +25,9 @@
 // q . k, tokens 16 s + 4 t + {0..3} in step s of p . V; score row tile s has token
 // 16 s + 4 (g / 2) + g % 2 in row g and two further in row 8 + g.
 //
-// Decode (one row tile): every warp has its own ring and takes every eighth block
-// of a segment. Many rows: the warps hold 16 rows each and share one ring.
+// Decode (one row tile): eight rings, each with every eighth block of a segment
+// and two warps to halve it. Many rows: the warps hold 16 rows each and share one
+// ring.
 //
 // Work: the (sequence, row tile, kv head, 64-token block) units of the batch in
 // this order are dealt out in equal contiguous shares to the thread blocks,
@@ -43,8 +44,6 @@ namespace {
 
 using namespace tc05;
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kUnit = 64;         // tokens per unit
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPBits = 15.0f;   // p is at most 2^15
@@ -98,7 +97,12 @@ template <int NT, int WR>
 struct Shape {
   static constexpr int kRowsPerWarp = 8 * NT;
   static constexpr int kRows = kRowsPerWarp * WR;  // query rows of a tile
-  static constexpr int kTokWarps = kWarps / WR;    // warps that share the tokens of a row group
+  static constexpr int kTokWarps = 8 / WR;         // token groups: rings of blocks
+  // warps that share a group's blocks, 64 / kH tokens each: two for decode steps,
+  // whose few registers leave room for 16 warps
+  static constexpr int kH = NT == 1 && WR == 1 ? 2 : 1;
+  static constexpr int kWarps = 8 * kH, kThreads = 32 * kWarps;
+  static constexpr int kParts = kTokWarps * kH;    // partial results of a row in the block
 };
 
 template <int D>
@@ -131,7 +135,7 @@ struct RowsSmem {
       uint8_t k[kG][NK][kUnit * D], v[kG][NV][kUnit * D];
     } ring;
     struct {
-      float o[kG][S::kRows][RowStride<D>::value], m[kG][S::kRows], l[kG][S::kRows];
+      float o[S::kParts][S::kRows][RowStride<D>::value], m[S::kParts][S::kRows], l[S::kParts][S::kRows];
     } out;
   };
   unsigned long long k_full[kG][NK], k_empty[kG][NK], v_full[kG][NV], v_empty[kG][NV];
@@ -145,7 +149,7 @@ struct Place {
 };
 
 template <typename T, int D, int NT, int WR>
-__global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<NT, WR>;
   using Mem = RowsSmem<D, NT, WR>;
   constexpr bool kSplit = sizeof(T) == 4;
@@ -156,10 +160,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
   const KvArgs& c = a.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t4 = lane & 3;
-  const int wr = warp % WR, wt = warp / WR;
+  constexpr int kH = S::kH, kT = 4 / kH;  // 16-token groups of a block per warp
+  const int half = warp % kH, wr = warp / kH % WR, wt = warp / kH / WR;
+  const bool feeds = wr == 0 && half == 0;  // the warp that copies for its token group
   const int log_pe = min(c.log_page, 6);  // tokens of a page within a block
 
-  UnitWalk<S::kRows, kUnit, kWarps, 0> w;
+  UnitWalk<S::kRows, kUnit, S::kWarps, 0> w;
   SharedTile mine{};
   if (!w.start(a)) {
     if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = mine;
@@ -167,8 +173,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < Mem::kG; ++i) {
-      for (int j = 0; j < Mem::NK; ++j) mbar_init(&sm.k_full[i][j], 1), mbar_init(&sm.k_empty[i][j], WR);
-      for (int j = 0; j < Mem::NV; ++j) mbar_init(&sm.v_full[i][j], 1), mbar_init(&sm.v_empty[i][j], WR);
+      for (int j = 0; j < Mem::NK; ++j) mbar_init(&sm.k_full[i][j], 1), mbar_init(&sm.k_empty[i][j], WR * kH);
+      for (int j = 0; j < Mem::NV; ++j) mbar_init(&sm.v_full[i][j], 1), mbar_init(&sm.v_empty[i][j], WR * kH);
     }
     sm.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -246,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
     Place nx[Mem::NK - 1];  // blocks whose keys are on their way behind it
 #pragma unroll
     for (int i = 0; i < Mem::NK - 1; ++i) nx[i] = find(b0 + (i + 1) * S::kTokWarps);
-    if (wr == 0) {
+    if (feeds) {
       if (b0 < sg.blk1) copy(cur, b0, true), copy(cur, b0, false);
 #pragma unroll
       for (int i = 0; i < Mem::NK - 1; ++i) {
@@ -325,21 +331,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
       const int ks = nk % Mem::NK;
       wait(&sm.k_full[wt][ks], (nk / Mem::NK) & 1);
       ++nk;
-      float x[NT][4][4];
+      float x[NT][kT][4];
       const uint8_t* kb = sm.ring.k[wt][ks] + (4 * (g >> 1) + (g & 1)) * 16 + 4 * t4;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kT; ++i) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[nt][i][j] = 0.0f;
-        const uint8_t* kp = kb + ((16 * i) >> log_pe) * (D << log_pe) + ((16 * i) & ((1 << log_pe) - 1)) * 16;
+        const int r16 = 16 * (kT * half + i);
+        const uint8_t* kp = kb + (r16 >> log_pe) * (D << log_pe) + (r16 & ((1 << log_pe) - 1)) * 16;
 #pragma unroll
         for (int j = 0; j < kI; ++j) {
-          const uint32_t w0 = *reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4)));
-          const uint32_t w1 = *reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4)) + 32);
-          const uint32_t fr[4] = {e4m3x2_half2(w0 & 0xFFFFu), e4m3x2_half2(w1 & 0xFFFFu), e4m3x2_half2(w0 >> 16),
-                                  e4m3x2_half2(w1 >> 16)};
+          uint32_t fr[4];
+          widen4(*reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4))), fr[0], fr[2]);
+          widen4(*reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4)) + 32), fr[1], fr[3]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -348,20 +354,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.k_empty[wt][ks]);
-      if (wr == 0 && blk + Mem::NK * S::kTokWarps < sg.blk1) copy(far, blk + Mem::NK * S::kTokWarps, true);
+      if (feeds && blk + Mem::NK * S::kTokWarps < sg.blk1) copy(far, blk + Mem::NK * S::kTokWarps, true);
 
       // ---- softmax weights
-      uint32_t pf[NT][kTerms][8];
+      uint32_t pf[NT][kTerms][2 * kT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ek = __shfl_sync(0xffffffffu, cur.ek, i), ev = __shfl_sync(0xffffffffu, cur.ev, i);
-          const int have = __shfl_sync(0xffffffffu, cur.have, i);
+        for (int i = 0; i < kT; ++i) {
+          const int gi = kT * half + i;
+          const int ek = __shfl_sync(0xffffffffu, cur.ek, gi), ev = __shfl_sync(0xffffffffu, cur.ev, gi);
+          const int have = __shfl_sync(0xffffffffu, cur.have, gi);
           const float sk = pow2f(ek), ef = ek == kExpNan || ev == kExpNan ? nan : (float)ev;
-          const int j0 = blk * kUnit + 16 * i + 4 * (g >> 1) + (g & 1);
-          const int end = blk * kUnit + 16 * i + have;
+          const int j0 = blk * kUnit + 16 * gi + 4 * (g >> 1) + (g & 1);
+          const int end = blk * kUnit + 16 * gi + have;
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
             const float k = __fmul_rn(rm[nt][q], sk);
@@ -392,8 +399,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
           }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ev = __shfl_sync(0xffffffffu, cur.ev, i);
+        for (int i = 0; i < kT; ++i) {
+          const int ev = __shfl_sync(0xffffffffu, cur.ev, kT * half + i);
           const float un = pow2f(ev == kExpNan ? 0 : -ev);
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
@@ -415,20 +422,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
       const int vs = nv % Mem::NV;
       wait(&sm.v_full[wt][vs], (nv / Mem::NV) & 1);
       ++nv;
-      uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
-      if (masked) {
+      uint32_t keep[kT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) keep[i] = first_bytes(__shfl_sync(0xffffffffu, cur.have, i) - 4 * t4);
-      }
+      for (int i = 0; i < kT; ++i) keep[i] = first_bytes(__shfl_sync(0xffffffffu, cur.have, kT * half + i) - 4 * t4);
       const uint8_t* vb = sm.ring.v[wt][vs] + g * 16 + 4 * t4;
 #pragma unroll
       for (int dt = 0; dt < kI; ++dt) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vb + (i * D + 16 * dt) * 16) & keep[i];
-          const uint32_t w1 = *reinterpret_cast<const uint32_t*>(vb + (i * D + 16 * dt + 8) * 16) & keep[i];
-          const uint32_t fr[4] = {e4m3x2_half2(w0 & 0xFFFFu), e4m3x2_half2(w1 & 0xFFFFu), e4m3x2_half2(w0 >> 16),
-                                  e4m3x2_half2(w1 >> 16)};
+        for (int i = 0; i < kT; ++i) {
+          const uint8_t* vp = vb + ((kT * half + i) * D + 16 * dt) * 16;
+          uint32_t fr[4];
+          widen4(*reinterpret_cast<const uint32_t*>(vp) & keep[i], fr[0], fr[2]);
+          widen4(*reinterpret_cast<const uint32_t*>(vp + 128) & keep[i], fr[1], fr[3]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -437,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.v_empty[wt][vs]);
-      if (wr == 0 && blk + Mem::NV * S::kTokWarps < sg.blk1)
+      if (feeds && blk + Mem::NV * S::kTokWarps < sg.blk1)
         copy(Mem::NV == Mem::NK ? far : nx[Mem::NV - 1], blk + Mem::NV * S::kTokWarps, false);
       cur = nx[0];
 #pragma unroll
@@ -456,26 +461,26 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
         for (int of = 4; of < 32; of <<= 1) t = __fadd_rn(t, __shfl_xor_sync(0xffffffffu, t, of));
         const int r = wr * S::kRowsPerWarp + 8 * nt + 2 * t4 + i;
         if (g == 0) {
-          sm.out.m[wt][r] = m[nt][i];
-          sm.out.l[wt][r] = t;
+          sm.out.m[wt * kH + half][r] = m[nt][i];
+          sm.out.l[wt * kH + half][r] = t;
         }
 #pragma unroll
         for (int dt = 0; dt < kI; ++dt) {
-          sm.out.o[wt][r][16 * dt + g] = o[nt][dt][i];
-          sm.out.o[wt][r][16 * dt + 8 + g] = o[nt][dt][2 + i];
+          sm.out.o[wt * kH + half][r][16 * dt + g] = o[nt][dt][i];
+          sm.out.o[wt * kH + half][r][16 * dt + 8 + g] = o[nt][dt][2 + i];
         }
       }
     __syncthreads();
     float* slot = partial_slot(a, blockIdx.x, sg.c0);
-    for (int i = threadIdx.x; i < rows * D; i += kThreads) {
+    for (int i = threadIdx.x; i < rows * D; i += S::kThreads) {
       const int r = i / D, d = i % D;
       float mx = sm.out.m[0][r];
 #pragma unroll
-      for (int k = 1; k < S::kTokWarps; ++k) mx = fmaxf(mx, sm.out.m[k][r]);
+      for (int k = 1; k < S::kParts; ++k) mx = fmaxf(mx, sm.out.m[k][r]);
       const float base = mx == -INFINITY ? 0.0f : mx;
       float os = 0.0f, ls = 0.0f;
 #pragma unroll
-      for (int k = 0; k < S::kTokWarps; ++k) {
+      for (int k = 0; k < S::kParts; ++k) {
         const float f = ex2(__fsub_rn(sm.out.m[k][r], base));
         os = __fmaf_rn(sm.out.o[k][r][d], f, os);
         ls = __fmaf_rn(sm.out.l[k][r], f, ls);
@@ -502,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
       __syncthreads();
       if (sm.last) {
         __threadfence();
-        for (int i = threadIdx.x; i < rows * D; i += kThreads) {
+        for (int i = threadIdx.x; i < rows * D; i += S::kThreads) {
           const int r = i / D, d = i % D;
           float mx = -INFINITY;
 #pragma unroll 4
@@ -525,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_rows_kernel(const __grid_co
     __syncthreads();
     w.advance(a, sg);
   }
-  if (sm.dead && wr == 0 && lane == 0) {  // copies in flight land before the block ends
+  if (sm.dead && feeds && lane == 0) {  // copies in flight land before the block ends
     for (uint32_t i = ik > Mem::NK ? ik - Mem::NK : 0; i < ik; ++i)
       (void)mbar_wait(&sm.k_full[wt][i % Mem::NK], (i / Mem::NK) & 1, a.wait_ns);
     for (uint32_t i = iv > Mem::NV ? iv - Mem::NV : 0; i < iv; ++i)
@@ -598,7 +603,7 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   // launch joins all tiles on the whole GPU.
   const bool join = max_blocks / b.min_units > kMaxParts;
   if (!join) b.shared = nullptr;
-  paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, kThreads, sizeof(Mem), st>>>(b);
+  paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, Shape<NT, WR>::kThreads, sizeof(Mem), st>>>(b);
   note_launches(1);
   if (join) {
     constexpr int kRows = Shape<NT, WR>::kRows, kRB = kRows <= 16 ? 1 : 8;
