@@ -13,7 +13,9 @@
 // run transposed, tokens (or dims) as the 16 MMA rows and 8 query rows as the
 // columns, so that a decode step of up to 8 heads per kv head wastes nothing.
 // F32 splits q (scaled by a power of two per row) and p into two binary16 terms;
-// the second term costs one more MMA on the same codes.
+// the second term costs one more MMA on the same widened codes. (8-bit warp-level
+// MMAs, which would take the codes as they are, run as conversions and 16-bit
+// products here: 44 instead of 26 million instructions for the same batch.)
 //
 // Bound by the cache's bytes when rows are few. A block is 64 tokens; its keys
 // and values come to shared memory by bulk copies (8 to 16 KB pieces, the cache's
@@ -152,9 +154,9 @@ template <typename T, int D, int NT, int WR>
 __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<NT, WR>;
   using Mem = RowsSmem<D, NT, WR>;
+  constexpr int kI = D / 16;           // runs of 16 dims, and row tiles of p . V
   constexpr bool kSplit = sizeof(T) == 4;
   constexpr int kTerms = kSplit ? 2 : 1;
-  constexpr int kI = D / 16;           // steps of q . k, and row tiles of p . V
   extern __shared__ __align__(128) unsigned char smem_raw[];
   Mem& sm = *reinterpret_cast<Mem*>(smem_raw);
   const KvArgs& c = a.c;
@@ -218,31 +220,33 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       }
       return p;
     };
-    // The copies of a block's keys or values by the group's first warp: whole
-    // pages, or half a page of 128 tokens (keys then in one piece per 16 dims).
+    // The copies of a block's keys or values by the group's feeding warp, to
+    // [D / 16][64][16] and [4][D][16] whatever the page: values are in one piece
+    // per page (half a page of 128), keys in one per page and 16 dims, or in one
+    // where a page is a block.
     auto copy = [&](const Place& p, int blk, bool keys) {
       const uint32_t n = keys ? ik++ : iv++;
       const int st = keys ? n % Mem::NK : n % Mem::NV;
       unsigned long long* full = keys ? &sm.k_full[wt][st] : &sm.v_full[wt][st];
       wait(keys ? &sm.k_empty[wt][st] : &sm.v_empty[wt][st], ((n / (keys ? Mem::NK : Mem::NV)) & 1) ^ 1);
+      if (a.stall >= 0 && (int)n >= a.stall) return;
       uint8_t* dst = keys ? sm.ring.k[wt][st] : sm.ring.v[wt][st];
-      const uint8_t* src = keys ? c.k : c.v;
-      // lane i < 4: group i; the first group of a page copies it
-      const bool first = lane < 4 && ((16 * lane) & ((1 << log_pe) - 1)) == 0 && p.have > 0;
-      const uint32_t bytes = (uint32_t)D << log_pe;
-      const uint32_t all = __popc(__ballot_sync(0xffffffffu, first)) * bytes;
-      const bool go = a.stall < 0 || (int)n < a.stall;
-      if (lane == 0 && go) mbar_expect_tx(full, all);
+      const uint8_t* src = (keys ? c.k : c.v) + (int64_t)h * (D << c.log_page);
+      const int64_t page_bytes = (int64_t)c.kv_heads * (D << c.log_page);
+      const int pe = 1 << log_pe, off = c.log_page > 6 ? (blk & 1) * kUnit : 0;  // tokens of a page in the block, first one
+      const int pages = kUnit >> log_pe;
+      // lane i < 4 holds group i; the first group of a page stands for it
+      const bool first = lane < 4 && ((16 * lane) & (pe - 1)) == 0 && p.have > 0;
+      const uint32_t got = __ballot_sync(0xffffffffu, first);
+      if (lane == 0) mbar_expect_tx(full, __popc(got) * D * pe);
       __syncwarp();
-      if (!go) return;
-      if (c.log_page <= 6) {
-        if (first) bulk_g2s(dst + lane * 16 * D, src + block_off<D>(c, p.pg, h), bytes, full);
-      } else {
-        const int pg = __shfl_sync(0xffffffffu, p.pg, 0), half = blk & 1;
-        const bool have = __shfl_sync(0xffffffffu, p.have, 0) > 0;
-        if (have && keys && lane < kI)
-          bulk_g2s(dst + lane * kUnit * 16, src + block_off<D>(c, pg, h) + ((lane * 128 + half * kUnit) << 4), kUnit * 16, full);
-        if (have && !keys && lane == 0) bulk_g2s(dst, src + block_off<D>(c, pg, h) + half * kUnit * D, kUnit * D, full);
+      const bool runs = keys && c.log_page != 6;
+      const int pieces = runs ? pages * kI : pages;  // at most 32
+      const int pgi = runs ? lane % pages : lane, run = runs ? lane / pages : 0, gi = (pgi << log_pe) >> 4;
+      const int pg = __shfl_sync(0xffffffffu, p.pg, gi & 3);
+      if (lane < pieces && ((got >> gi) & 1)) {
+        const uint8_t* from = src + pg * page_bytes + (runs ? ((run << c.log_page) + off) * 16 : off * D);
+        bulk_g2s(dst + (runs ? (run * kUnit + pgi * pe) * 16 : pgi * pe * D), from, runs ? pe * 16 : pe * D, full);
       }
     };
 
@@ -281,13 +285,14 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       for (int i = 0; i < kI; ++i) load4(p + 16 * i, a.vec, x + 4 * i);
       float amax = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4 * kI; ++i) amax = fmaxf(amax, fabsf(x[i]));
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      for (int i = 0; i < 4 * kI; ++i) amax = fmax_nan(amax, fabsf(x[i]));
+      amax = fmax_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmax_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
       // the row times 2^up has its largest element in [2^14, 2^15)
       const int ex = (int)(__float_as_uint(amax) >> 23) - 127;
       const int up = min(max(14 - ex, -120), 100);
-      const float f = pow2f(up), mul = a.score_mul * pow2f(-up);
+      const float f = pow2f(up);
+      const float mul = amax < INFINITY ? a.score_mul * pow2f(-up) : __int_as_float(0x7FC00000);
 #pragma unroll
       for (int i = 0; i < 2 * kI; ++i) {
         const float y0 = __fmul_rn(x[2 * i], f), y1 = __fmul_rn(x[2 * i + 1], f);
@@ -334,23 +339,30 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       float x[NT][kT][4];
       const uint8_t* kb = sm.ring.k[wt][ks] + (4 * (g >> 1) + (g & 1)) * 16 + 4 * t4;
 #pragma unroll
-      for (int i = 0; i < kT; ++i) {
+      for (int i = 0; i < kT; ++i)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[nt][i][j] = 0.0f;
-        const int r16 = 16 * (kT * half + i);
-        const uint8_t* kp = kb + (r16 >> log_pe) * (D << log_pe) + (r16 & ((1 << log_pe) - 1)) * 16;
+      const uint8_t* kp = kb + kT * half * 256;  // row tile i: 16 rows of 16 bytes further
+      auto key = [&](int i, int run, int row) {
+        return *reinterpret_cast<const uint32_t*>(kp + i * 256 + run * (kUnit * 16) + row * 16);
+      };
+      // products that follow one another go to different accumulators
 #pragma unroll
-        for (int j = 0; j < kI; ++j) {
-          uint32_t fr[4];
-          widen4(*reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4))), fr[0], fr[2]);
-          widen4(*reinterpret_cast<const uint32_t*>(kp + (j << (log_pe + 4)) + 32), fr[1], fr[3]);
+      for (int j = 0; j < kI; ++j) {
+        uint32_t fr[kT][4];
+#pragma unroll
+        for (int i = 0; i < kT; ++i) {
+          widen4(key(i, j, 0), fr[i][0], fr[i][2]);
+          widen4(key(i, j, 2), fr[i][1], fr[i][3]);
+        }
+#pragma unroll
+        for (int q = kTerms - 1; q >= 0; --q)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int q = kTerms - 1; q >= 0; --q) mma(x[nt][i], fr, qf[nt][q][2 * j], qf[nt][q][2 * j + 1]);
-        }
+            for (int i = 0; i < kT; ++i) mma(x[nt][i], fr[i], qf[nt][q][2 * j], qf[nt][q][2 * j + 1]);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.k_empty[wt][ks]);
@@ -374,29 +386,36 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
             const float k = __fmul_rn(rm[nt][q], sk);
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              float y = __fmaf_rn(x[nt][i][2 * hf + q], k, ef);
-              if (masked && (j0 + 2 * hf >= end || j0 + 2 * hf > lim[nt][q])) y = -INFINITY;
-              x[nt][i][2 * hf + q] = y;
-              mx[q] = fmaxf(mx[q], y);
+              x[nt][i][2 * hf + q] = __fmaf_rn(x[nt][i][2 * hf + q], k, ef);
             }
           }
+          if (masked) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf)
+                if (j0 + 2 * hf >= end || j0 + 2 * hf > lim[nt][q]) x[nt][i][2 * hf + q] = -INFINITY;
+          }
+#pragma unroll
+          for (int q = 0; q < 2; ++q) mx[q] = fmaxf(mx[q], fmaxf(x[nt][i][q], x[nt][i][2 + q]));
         }
-        float base[2];
+        float base[2], al[2];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
 #pragma unroll
           for (int of = 4; of < 32; of <<= 1) mx[q] = fmaxf(mx[q], __shfl_xor_sync(0xffffffffu, mx[q], of));
           const float mn = fmaxf(m[nt][q], mx[q]);
           const float bs = mn == -INFINITY ? 0.0f : mn;
-          const float al = ex2(__fsub_rn(m[nt][q], bs));
+          al[q] = ex2(__fsub_rn(m[nt][q], bs));
           m[nt][q] = mn;
           base[q] = __fsub_rn(bs, kPBits);
-          l[nt][q] = __fmul_rn(l[nt][q], al);
+          l[nt][q] = __fmul_rn(l[nt][q], al[q]);
+        }
+        if (__any_sync(0xffffffffu, al[0] != 1.0f || al[1] != 1.0f)) {  // a maximum moved
 #pragma unroll
-          for (int dt = 0; dt < kI; ++dt) {
-            o[nt][dt][q] = __fmul_rn(o[nt][dt][q], al);
-            o[nt][dt][2 + q] = __fmul_rn(o[nt][dt][2 + q], al);
-          }
+          for (int dt = 0; dt < kI; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[nt][dt][q] = __fmul_rn(o[nt][dt][q], al[q & 1]);
         }
 #pragma unroll
         for (int i = 0; i < kT; ++i) {
@@ -422,24 +441,36 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       const int vs = nv % Mem::NV;
       wait(&sm.v_full[wt][vs], (nv / Mem::NV) & 1);
       ++nv;
-      uint32_t keep[kT];
-#pragma unroll
-      for (int i = 0; i < kT; ++i) keep[i] = first_bytes(__shfl_sync(0xffffffffu, cur.have, kT * half + i) - 4 * t4);
-      const uint8_t* vb = sm.ring.v[wt][vs] + g * 16 + 4 * t4;
-#pragma unroll
-      for (int dt = 0; dt < kI; ++dt) {
-#pragma unroll
+      if (masked && __any_sync(0xffffffffu, lane < 4 && cur.have < 16)) {
+#pragma unroll 1
         for (int i = 0; i < kT; ++i) {
-          const uint8_t* vp = vb + ((kT * half + i) * D + 16 * dt) * 16;
-          uint32_t fr[4];
-          widen4(*reinterpret_cast<const uint32_t*>(vp) & keep[i], fr[0], fr[2]);
-          widen4(*reinterpret_cast<const uint32_t*>(vp + 128) & keep[i], fr[1], fr[3]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int q = kTerms - 1; q >= 0; --q) mma(o[nt][dt], fr, pf[nt][q][2 * i], pf[nt][q][2 * i + 1]);
+          const uint32_t keep = first_bytes(__shfl_sync(0xffffffffu, cur.have, kT * half + i) - 4 * t4);
+#pragma unroll 1
+          for (int d = g; d < D; d += 8)  // warps that share the ring all do it, to the same effect
+            *reinterpret_cast<uint32_t*>(sm.ring.v[wt][vs] + ((kT * half + i) * D + d) * 16 + 4 * t4) &= keep;
         }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // a copy overwrites it later
+        __syncwarp();
       }
+      const uint8_t* vb = sm.ring.v[wt][vs] + g * 16 + 4 * t4;
+      auto value = [&](int i, int dim) { return *reinterpret_cast<const uint32_t*>(vb + ((kT * half + i) * D + dim) * 16); };
+#pragma unroll
+      for (int i = 0; i < kT; ++i)
+#pragma unroll
+        for (int dt = 0; dt < kI; dt += 4) {
+          uint32_t fr[4][4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            widen4(value(i, 16 * (dt + e)), fr[e][0], fr[e][2]);
+            widen4(value(i, 16 * (dt + e) + 8), fr[e][1], fr[e][3]);
+          }
+#pragma unroll
+          for (int q = kTerms - 1; q >= 0; --q)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) mma(o[nt][dt + e], fr[e], pf[nt][q][2 * i], pf[nt][q][2 * i + 1]);
+        }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.v_empty[wt][vs]);
       if (feeds && blk + Mem::NV * S::kTokWarps < sg.blk1)
