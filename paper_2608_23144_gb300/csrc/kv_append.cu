@@ -5,12 +5,14 @@
 // exponent, e4m3 rounding. Per token it has to read (n_heads + 2 kv_heads) D
 // elements and 2 (rotary_dim / 2) floats of the tables, and to write n_heads D
 // elements and 2 kv_heads D codes: bytes bound, most of them q's. One launch
-// does both parts: the first blocks take one (page that gets tokens, kv head,
-// keys or values) each, the others rotate q, a few warps per token. A block's
-// codes depend on its amax, so the key/value blocks read their tokens twice
-// when they do not fit one item per thread (the second read hits L1/L2).
-// Every page is found by a block-wide scan over the sequences, so the launch
-// follows device-side lengths.
+// does both parts, thread blocks of either kind alternating so that the waits of
+// one pass under the other's bytes: a job is the keys or the values of one kv head
+// and one page that gets tokens, by a warp where those are few or small pages,
+// else by four; q is rotated by a few warps per token. A block's codes depend on
+// its amax, so a job reads its tokens twice when they do not fit one item per
+// thread (the second read hits L1/L2). Loads stand outside branches: behind one,
+// each waited for the one before. Pages are found by a block-wide scan over the
+// sequences, so the launch follows device-side lengths.
 #include "internal.h"
 #include "kv_paged.cuh"
 
@@ -26,7 +28,8 @@ struct AppendArgs {
   KvRows q, k, v, qo;
   const float *cos, *sin;
   int rope_rows, half, interleaved;  // half = rotary_dim / 2
-  int kv_blocks, warps_per_tok;
+  int kv_blocks, q_blocks, every;    // one block in `every` is of the kind with fewer
+  int warps_per_tok;
 };
 
 // W consecutive elements.
@@ -108,35 +111,36 @@ template <int W, typename T>
 __device__ __forceinline__ void load_item(const AppendArgs& a, const T* p, int it, const float* cr, const float* sr,
                                           Item<W>& o) {
   const int h = a.half;
-  if (W == 8 && a.interleaved) {
-    o.d1 = 8 * it;
-    o.two = false;
-    load_row<W>(p + o.d1, o.y);
-    if (o.d1 < 2 * h) {
-      float c[8], s[8];
-      const float4 cv = __ldg(reinterpret_cast<const float4*>(cr + 4 * it));
-      const float4 sv = __ldg(reinterpret_cast<const float4*>(sr + 4 * it));
-      c[0] = cv.x, c[1] = cv.y, c[2] = cv.z, c[3] = cv.w;
-      s[0] = sv.x, s[1] = sv.y, s[2] = sv.z, s[3] = sv.w;
+  const bool runs = W == 8 && a.interleaved;  // 4 pairs in 8 dims
+  const bool turned = runs ? 8 * it < 2 * h : it * W < h;
+  o.two = turned && !runs;
+  o.d1 = runs ? 8 * it : (turned ? (a.interleaved ? 2 * it : it * W) : h + it * W);  // plain items: dims 2h on
+  o.d2 = o.two ? (a.interleaved ? 2 * it + 1 : h + it * W) : o.d1;
+  load_row<W>(p + o.d1, o.y);
+  if (h == 0) return;
+  float c[W], s[W];
+  load_row<W>(p + o.d2, o.y + W);
+  if (runs) {
+    const int at = turned ? 4 * it : 0;
+    load_row<4>(cr + at, c);
+    load_row<4>(sr + at, s);
 #pragma unroll
-      for (int i = 0; i < W / 2; ++i) turn(o.y[2 * i], o.y[2 * i + 1], c[i], s[i]);
+    for (int i = 0; i < W / 2; ++i) {
+      float x1 = o.y[2 * i], x2 = o.y[2 * i + 1];
+      turn(x1, x2, c[i], s[i]);
+      o.y[2 * i] = turned ? x1 : o.y[2 * i];
+      o.y[2 * i + 1] = turned ? x2 : o.y[2 * i + 1];
     }
-    return;
-  }
-  o.two = it * W < h;
-  if (o.two) {
-    o.d1 = a.interleaved ? 2 * it : it * W;
-    o.d2 = a.interleaved ? 2 * it + 1 : h + it * W;
-    float c[W], s[W];
-    load_row<W>(p + o.d1, o.y);
-    load_row<W>(p + o.d2, o.y + W);
-    load_row<W>(cr + it * W, c);
-    load_row<W>(sr + it * W, s);
-#pragma unroll
-    for (int i = 0; i < W; ++i) turn(o.y[i], o.y[W + i], c[i], s[i]);
   } else {
-    o.d1 = h + it * W;  // items h / W on: dims 2h on
-    load_row<W>(p + o.d1, o.y);
+    const int at = turned ? it * W : 0;
+    load_row<W>(cr + at, c);
+    load_row<W>(sr + at, s);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      float x1 = o.y[i];
+      turn(x1, o.y[W + i], c[i], s[i]);
+      o.y[i] = turned ? x1 : o.y[i];
+    }
   }
 }
 
@@ -207,15 +211,20 @@ __device__ __forceinline__ bool find_visit(const KvArgs& a, int visit, int* seq,
   return found[0] >= 0;
 }
 
-__device__ __forceinline__ float block_amax(float m) {
-  __shared__ float wmax[kWarps];
+// Over the JW warps of a job.
+template <int JW>
+__device__ __forceinline__ float job_amax(float m) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmax_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if ((threadIdx.x & 31) == 0) wmax[threadIdx.x >> 5] = m;
-  __syncthreads();
-  m = wmax[0];
+  if constexpr (JW > 1) {
+    static_assert(JW == kWarps, "one job per thread block");
+    __shared__ float wmax[kWarps];
+    if ((threadIdx.x & 31) == 0) wmax[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = wmax[0];
 #pragma unroll
-  for (int w = 1; w < kWarps; ++w) m = fmax_nan(m, wmax[w]);
+    for (int w = 1; w < kWarps; ++w) m = fmax_nan(m, wmax[w]);
+  }
   return m;
 }
 
@@ -237,12 +246,12 @@ __device__ __forceinline__ void rescale16(uint4* p, int n, float f) {
   *p = v;
 }
 
-// The keys or values of one page visit and kv head.
-template <typename T, int D, int W>
-__device__ void append_block(const AppendArgs& a, int visit, int head, bool keys) {
+// The keys or values of one page visit (sequence b's nth) and kv head.
+template <typename T, int D, int W, int JW>
+__device__ void append_job(const AppendArgs& a, int b, int nth, int head, bool keys) {
+  constexpr int kThreads = 32 * JW;  // of the job
   const KvArgs& c = a.c;
-  int b, nth;
-  if (!find_visit(c, visit, &b, &nth)) return;
+  const int tid = JW == 1 ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
   const KvSeq s = kv_seq(c, b);
   const int P = 1 << c.log_page;
   const int first = s.kv - s.n;  // position of the first new token
@@ -252,7 +261,7 @@ __device__ void append_block(const AppendArgs& a, int visit, int head, bool keys
   const int p0 = (slot << c.log_page) + row0;
   const int row1 = min(P, row0 + s.kv - p0);
   if (pg < 0 || pg >= c.n_pages || s.kv > a.rope_rows) {
-    if (threadIdx.x == 0) atomicOr(c.status, kFaultBatch);
+    if (tid == 0) atomicOr(c.status, kFaultBatch);
     if (pg < 0 || pg >= c.n_pages) return;
   }
   // rows past the rotation tables are left out of keys and values alike
@@ -282,19 +291,14 @@ __device__ void append_block(const AppendArgs& a, int visit, int head, bool keys
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int r = r4 + j - row0;
-        if (r >= 0 && r < n) {
-          load_row<W>(sp + (int64_t)(tok0 + r) * src.ts + d, vy[j]);
-        } else {
-#pragma unroll
-          for (int x = 0; x < W; ++x) vy[j][x] = 0.0f;
-        }
+        load_row<W>(sp + (int64_t)(tok0 + min(max(r, 0), n - 1)) * src.ts + d, vy[j]);  // a row of the job if not r
       }
     } else {
       load_row<W>(sp + (int64_t)(tok0 + i / D) * src.ts + i % D, vy[0]);
     }
   };
   float m = 0.0f;
-  for (int i = threadIdx.x; i < items; i += kThreads) {
+  for (int i = tid; i < items; i += kThreads) {
     load(i);
     if (keys) {
       m = item_amax<W>(it, m);
@@ -305,25 +309,28 @@ __device__ void append_block(const AppendArgs& a, int visit, int head, bool keys
         for (int x = 0; x < W; ++x) m = fmax_nan(m, fabsf(vy[j][x]));
     }
   }
-  m = block_amax(m);
+  m = job_amax<JW>(m);
   const int need = block_exponent(m);
   const bool bad = need == kExpNan || e_old == kExpNan;
   const int e = bad ? kExpNan : max(need, e_old);
-  if (threadIdx.x == 0) *ep = (int8_t)e;
+  if (tid == 0) *ep = (int8_t)e;
   if (!bad && row0 > 0 && e > e_old) {  // older codes in the new scale
     const float f = pow2f(e_old - e);
     uint4* q = reinterpret_cast<uint4*>(blk);
     if (keys) {
-      for (int i = threadIdx.x; i < (D / 16) * row0; i += kThreads)
+      for (int i = tid; i < (D / 16) * row0; i += kThreads)
         rescale16(q + ((i / row0) << c.log_page) + i % row0, 16, f);
     } else {
-      for (int i = threadIdx.x; i < ((row0 + 15) >> 4) * D; i += kThreads)
+      for (int i = tid; i < ((row0 + 15) >> 4) * D; i += kThreads)
         rescale16(q + i, row0 - 16 * (i / D), f);
     }
-    __syncthreads();  // a 16-byte unit may get new codes too
+    if constexpr (JW > 1)  // a 16-byte unit may get new codes too
+      __syncthreads();
+    else
+      __syncwarp();
   }
   const float inv = bad ? 0.0f : pow2f(-e);
-  for (int i = threadIdx.x; i < items; i += kThreads) {
+  for (int i = tid; i < items; i += kThreads) {
     if (items > kThreads) load(i);
     if (keys) {
       const int row = row0 + i / per;
@@ -383,6 +390,35 @@ __device__ void rotate_q(const AppendArgs& a, int t, int part, int parts) {
   const float* sr = a.sin + (int64_t)pos * a.half;
   const T* qp = static_cast<const T*>(a.q.p) + (int64_t)t * a.q.ts;
   T* op = static_cast<T*>(a.qo.p) + (int64_t)t * a.qo.ts;
+  if (W == 8 && !a.interleaved && a.half == D / 2) {
+    // whole heads: a lane keeps its 8 pairs of the tables; four heads in flight
+    constexpr int kPer = D / 16, kHeads = 32 / kPer;  // lanes of a head, heads at a time
+    const int it = lane % kPer;
+    float cs[W], sn[W];
+    load_row<W>(cr + W * it, cs);
+    load_row<W>(sr + W * it, sn);
+    const int step = parts * kHeads;
+    for (int h0 = part * kHeads + lane / kPer; h0 < c.n_heads; h0 += 4 * step) {
+      float x[4][2 * W];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const T* p = qp + (int64_t)min(h0 + u * step, c.n_heads - 1) * a.q.hs + W * it;
+        load_row<W>(p, x[u]);
+        load_row<W>(p + D / 2, x[u] + W);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) turn(x[u][i], x[u][W + i], cs[i], sn[i]);
+        if (h0 + u * step < c.n_heads) {
+          T* o = op + (int64_t)(h0 + u * step) * a.qo.hs + W * it;
+          store_row<W>(o, x[u]);
+          store_row<W>(o + D / 2, x[u] + W);
+        }
+      }
+    }
+    return;
+  }
   const int items = c.n_heads * per;
 #pragma unroll 2
   for (int i = part * 32 + lane; i < items; i += parts * 32) {
@@ -395,24 +431,44 @@ __device__ void rotate_q(const AppendArgs& a, int t, int part, int parts) {
   }
 }
 
-template <typename T, int D, int W>
+template <typename T, int D, int W, int JW>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_constant__ AppendArgs a) {
-  if ((int)blockIdx.x < a.kv_blocks) {
-    const int i = blockIdx.x;
-    append_block<T, D, W>(a, i / (2 * a.c.kv_heads), (i >> 1) % a.c.kv_heads, (i & 1) == 0);
+  // which kind, and the how many-th of it
+  const int i = blockIdx.x, few = min(a.kv_blocks, a.q_blocks);
+  const int nth = i / a.every, before = min(few, nth + (i % a.every != 0));  // blocks of the rarer kind up to i
+  const bool rare = i % a.every == 0 && nth < few;
+  const bool kv = rare == (a.kv_blocks <= a.q_blocks);
+  const int k = rare ? nth : i - before;
+  if (kv) {
+    constexpr int kJobs = kWarps / JW;  // jobs of a thread block: of one visit
+    const int jobs = 2 * a.c.kv_heads, per = (jobs + kJobs - 1) / kJobs;
+    int b, visit;
+    if (!find_visit(a.c, k / per, &b, &visit)) return;
+    const int job = k % per * kJobs + (JW == 1 ? (int)(threadIdx.x >> 5) : 0);
+    if (job < jobs) append_job<T, D, W, JW>(a, b, visit, job >> 1, (job & 1) == 0);
     return;
   }
-  const int w = ((int)blockIdx.x - a.kv_blocks) * kWarps + (threadIdx.x >> 5);
+  const int w = k * kWarps + (threadIdx.x >> 5);
   const int t = w / a.warps_per_tok;
   if (t < a.c.n_tok) rotate_q<T, D, W>(a, t, w % a.warps_per_tok, a.warps_per_tok);
 }
 
 template <typename T, int D>
-cudaError_t launch(const AppendArgs& a, bool vec, int64_t blocks, cudaStream_t st) {
+cudaError_t launch(AppendArgs a, bool vec, int64_t visits, cudaStream_t st) {
+  // A warp per job where a visit has few tokens (mean of the batch) or a small
+  // page: 20 us less than four warps per job for 16k tokens in pages of 16.
+  const bool warp = a.c.page <= 32 || (int64_t)a.c.n_tok <= 8 * visits;
+  const int64_t jobs = 2ll * a.c.kv_heads, kv = visits * (warp ? (jobs + kWarps - 1) / kWarps : jobs);
+  const int64_t q = ((int64_t)a.c.n_tok * a.warps_per_tok + kWarps - 1) / kWarps;
+  if (kv + q > INT32_MAX) return cudaErrorInvalidValue;
+  a.kv_blocks = (int)kv;
+  a.q_blocks = (int)q;
+  a.every = (int)((kv + q) / (kv < q ? kv : q));
+  const unsigned grid = (unsigned)(kv + q);
   if (vec)
-    kv_append_kernel<T, D, 8><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    (warp ? kv_append_kernel<T, D, 8, 1> : kv_append_kernel<T, D, 8, 4>)<<<grid, kThreads, 0, st>>>(a);
   else
-    kv_append_kernel<T, D, 1><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    (warp ? kv_append_kernel<T, D, 1, 1> : kv_append_kernel<T, D, 1, 4>)<<<grid, kThreads, 0, st>>>(a);
   note_launches(1);
   return cudaGetLastError();
 }
@@ -437,21 +493,17 @@ cudaError_t launch_kv_append(const KvArgs& c, int head_dim, int dtype, const KvR
   // and at most n of them
   int64_t visits = (int64_t)c.n_tok / c.page + 2ll * c.n_seq;
   if (visits > c.n_tok) visits = c.n_tok;
-  const int64_t kvb = visits * c.kv_heads * 2;
   // a token's heads are shared by 4 warps while there are too few tokens for
   // one warp each to fill the GPU (152 SMs x 16 warps)
   a.warps_per_tok = c.n_tok >= 2432 ? 1 : kWarps;
-  const int64_t blocks = kvb + ((int64_t)c.n_tok * a.warps_per_tok + kWarps - 1) / kWarps;
-  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-  a.kv_blocks = (int)kvb;
   // vectors of 8 elements: every row, the tables and the rotated part in whole units
   const size_t elt = dtype == AWSRC_DTYPE_BF16 ? 2 : 4;
   const bool vec = rows_aligned(q, elt) && rows_aligned(k, elt) && rows_aligned(v, elt) && rows_aligned(qo, elt) &&
                    (reinterpret_cast<uintptr_t>(cos) | reinterpret_cast<uintptr_t>(sin)) % 16 == 0 &&
                    a.half % (interleaved ? 4 : 8) == 0;
   if (dtype == AWSRC_DTYPE_BF16)
-    return head_dim == 128 ? launch<__nv_bfloat16, 128>(a, vec, blocks, st) : launch<__nv_bfloat16, 64>(a, vec, blocks, st);
-  return head_dim == 128 ? launch<float, 128>(a, vec, blocks, st) : launch<float, 64>(a, vec, blocks, st);
+    return head_dim == 128 ? launch<__nv_bfloat16, 128>(a, vec, visits, st) : launch<__nv_bfloat16, 64>(a, vec, visits, st);
+  return head_dim == 128 ? launch<float, 128>(a, vec, visits, st) : launch<float, 64>(a, vec, visits, st);
 }
 
 }  // namespace awsrc
