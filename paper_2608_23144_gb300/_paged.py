@@ -8,7 +8,17 @@ from typing import Optional
 
 import torch
 
-from ._binding import AwsrcError, _check, _require, _stream, lib
+from ._binding import AwsrcError, _check, _require, lib
+from ._binding import _stream as _stream_of
+
+# The current stream's handle without a torch.cuda.Stream object: the object
+# alone costs 3 of a short call's 15 us.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _stream(stream, device: torch.device) -> int:
+    return _raw_stream(device.index) if stream is None else _stream_of(stream)
+
 
 PAGE_SIZES = (16, 32, 64, 128)
 HEAD_DIMS = (64, 128)
@@ -133,18 +143,21 @@ def awsrc_attention_workspace(cache: KvCache, n_heads: int, stream=None) -> torc
     n = ct.c_size_t()
     _check(lib.awsrc_attention_workspace_bytes(cache._ref, n_heads, ct.byref(n)), "attention_workspace_bytes")
     ws = torch.empty(n.value, dtype=torch.uint8, device=cache.device)
-    _check(lib.awsrc_attention_workspace_init(cache._ref, n_heads, ws.data_ptr(), n.value, _stream(stream)),
+    _check(lib.awsrc_attention_workspace_init(cache._ref, n_heads, ws.data_ptr(), n.value,
+                                              _stream(stream, ws.device)),
            "attention_workspace_init")
     return ws
 
 
-def _rows(t: torch.Tensor, name: str, n_tok: int, heads: Optional[int], dim: int, dtype, device) -> _Rows:
+_EMPTY = 16  # stands for the address of an empty tensor, which no kernel reads
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> _Rows:
     """Checks a [n_tok, heads, dim] tensor of any strides but dims in a row."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, not {type(t).__name__}")
-    shape = t.shape
-    if len(shape) != 3 or shape[0] != n_tok or shape[2] != dim or (heads is not None and shape[1] != heads):
-        raise ValueError(f"{name} has shape {tuple(shape)}, expected ({n_tok}, {'heads' if heads is None else heads}, {dim})")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if t.device != device:
@@ -152,25 +165,25 @@ def _rows(t: torch.Tensor, name: str, n_tok: int, heads: Optional[int], dim: int
     ts, hs, ds = t.stride()
     if ds != 1:
         raise ValueError(f"{name} must have its dims in a row (last stride 1, not {ds})")
-    return _Rows(t.data_ptr() or device_dummy, ts, hs, _DTYPES[dtype], 0)
-
-
-device_dummy = 16  # stands for the address of an empty tensor, which no kernel reads
+    return _Rows(t.data_ptr() or _EMPTY, ts, hs, _DTYPES[dtype], 0)
 
 
 def _common(cache: KvCache, batch: KvBatch, q: torch.Tensor, workspace: torch.Tensor):
+    """Checks what both calls take; returns (device, q's shape)."""
     if not isinstance(cache, KvCache) or not isinstance(batch, KvBatch):
         raise TypeError("cache and batch must come from awsrc_kv_cache and awsrc_kv_batch")
     if not isinstance(q, torch.Tensor) or q.dtype not in _DTYPES:
         raise TypeError("q must be a float32 or bfloat16 tensor")
-    if q.dim() != 3 or q.shape[1] < 1 or q.shape[1] % cache.kv_heads != 0:
-        raise ValueError(f"q has shape {tuple(q.shape)}: heads must be a multiple of the cache's {cache.kv_heads}")
+    shape = q.shape
+    if len(shape) != 3 or shape[0] != batch.n_tok or shape[1] < 1 or shape[1] % cache.kv_heads != 0 or shape[2] != cache.head_dim:
+        raise ValueError(f"q has shape {tuple(shape)}, expected ({batch.n_tok}, a multiple of {cache.kv_heads}, "
+                         f"{cache.head_dim})")
     dev = cache.device
     if dev.type != "cuda" or batch.device != dev:
         raise ValueError(f"the cache is on {dev}, the batch on {batch.device}: one CUDA device is needed")
     if workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
         raise ValueError("workspace must come from awsrc_attention_workspace")
-    return dev
+    return dev, shape
 
 
 def awsrc_kv_append(cache: KvCache, batch: KvBatch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -181,14 +194,15 @@ def awsrc_kv_append(cache: KvCache, batch: KvBatch, q: torch.Tensor, k: torch.Te
     rotated q (in `q_out`, which may be q). cos and sin are float32 [positions,
     rotary_dim / 2] tables (None: no rotation). Batch entries that cannot be
     right are skipped and reported by awsrc_workspace_status(workspace)."""
-    dev = _common(cache, batch, q, workspace)
-    n, dt, dim, heads = batch.n_tok, q.dtype, cache.head_dim, q.shape[1]
+    dev, shape = _common(cache, batch, q, workspace)
+    dt = q.dtype
     if q_out is None:
-        q_out = torch.empty(n, heads, dim, dtype=dt, device=dev)
-    rq = _rows(q, "q", n, None, dim, dt, dev)
-    rk = _rows(k, "k", n, cache.kv_heads, dim, dt, dev)
-    rv = _rows(v, "v", n, cache.kv_heads, dim, dt, dev)
-    ro = _rows(q_out, "q_out", n, heads, dim, dt, dev)
+        q_out = torch.empty(shape, dtype=dt, device=dev)
+    kv_shape = (shape[0], cache.kv_heads, shape[2])
+    rq = _rows(q, "q", shape, dt, dev)
+    rk = _rows(k, "k", kv_shape, dt, dev)
+    rv = _rows(v, "v", kv_shape, dt, dev)
+    ro = _rows(q_out, "q_out", shape, dt, dev)
     if cos is None and sin is None:
         cp = sp = None
         rows = half = 0
@@ -200,8 +214,10 @@ def awsrc_kv_append(cache: KvCache, batch: KvBatch, q: torch.Tensor, k: torch.Te
         if not (cos.is_contiguous() and sin.is_contiguous()):
             raise ValueError("cos and sin must be contiguous")
         cp, sp, (rows, half) = cos.data_ptr(), sin.data_ptr(), cos.shape
-    _check(lib.awsrc_kv_append(cache._ref, batch._ref, heads, rq, rk, rv, ro, cp, sp, rows, 2 * half, int(interleaved),
-                               workspace.data_ptr(), workspace.numel(), _stream(stream)), "kv_append")
+    st = lib.awsrc_kv_append(cache._ref, batch._ref, shape[1], rq, rk, rv, ro, cp, sp, rows, 2 * half, bool(interleaved),
+                             workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
+    if st:
+        _check(st, "kv_append")
     return q_out
 
 
@@ -213,21 +229,23 @@ def awsrc_paged_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, works
     given, the float32 [n_tok, heads] `lse` (natural log of the softmax sum).
     sm_scale defaults to dim ** -0.5. causal: query i of a sequence sees the
     tokens up to its own; else all. A query that sees none gets 0 and -inf."""
-    dev = _common(cache, batch, q, workspace)
-    n, dt, dim, heads = batch.n_tok, q.dtype, cache.head_dim, q.shape[1]
+    dev, shape = _common(cache, batch, q, workspace)
+    dt = q.dtype
     if out is None:
-        out = torch.empty(n, heads, dim, dtype=dt, device=dev)
-    rq = _rows(q, "q", n, None, dim, dt, dev)
-    ro = _rows(out, "out", n, heads, dim, dt, dev)
+        out = torch.empty(shape, dtype=dt, device=dev)
+    rq = _rows(q, "q", shape, dt, dev)
+    ro = _rows(out, "out", shape, dt, dev)
     lp = None
     if lse is not None:
-        _require(lse, "lse", dtype=torch.float32, shape=(n, heads), device=dev)
+        _require(lse, "lse", dtype=torch.float32, shape=shape[:2], device=dev)
         if not lse.is_contiguous():
             raise ValueError("lse must be contiguous")
         lp = lse.data_ptr()
-    _check(lib.awsrc_paged_attention(cache._ref, batch._ref, heads, rq, ro, lp,
-                                     dim ** -0.5 if sm_scale is None else sm_scale, int(causal), workspace.data_ptr(),
-                                     workspace.numel(), _stream(stream)), "paged_attention")
+    st = lib.awsrc_paged_attention(cache._ref, batch._ref, shape[1], rq, ro, lp,
+                                   shape[2] ** -0.5 if sm_scale is None else sm_scale, bool(causal),
+                                   workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
+    if st:
+        _check(st, "paged_attention")
     return out
 
 

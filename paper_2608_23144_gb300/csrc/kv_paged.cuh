@@ -117,6 +117,7 @@ template <int ROWS, int UNIT, int WARPS, int OVER>
 struct UnitWalk {
   int64_t chunk, u, u_end, tile_first;
   int b, t, blocks;  // sequence, tile and the tile's blocks
+  int pad;           // a (tile, head) takes a multiple of this many units
   KvSeq s;
 
   __device__ __forceinline__ static int blocks_of(const AttnArgs& a, const KvSeq& s, int t) {
@@ -130,17 +131,25 @@ struct UnitWalk {
   __device__ __forceinline__ static int tiles_of(const AttnArgs& a, const KvSeq& s) {
     return s.n > 0 ? (s.n * a.c.group + ROWS - 1) / ROWS : 0;
   }
+  __device__ __forceinline__ static int span_of(int blocks, int pad) {
+    const int n = blocks + OVER;
+    return pad == 1 ? n : (n + pad - 1) / pad * pad;
+  }
   // Units of the tiles of s, or with `want` >= 0 the tile that holds unit `want`
   // of them (*tile, and the units before it as the result). No division per tile:
   // the token of a tile's last row advances by ROWS / group.
-  __device__ static int64_t units_of(const AttnArgs& a, const KvSeq& s, int64_t want = -1, int* tile = nullptr) {
-    const int nt = tiles_of(a, s), g = a.c.group, heads = a.c.kv_heads;
-    const int dq = ROWS / g, dr = ROWS - dq * g;
+  __device__ static int64_t units_of(const AttnArgs& a, const KvSeq& s, int pad, int64_t want = -1, int* tile = nullptr) {
+    const int nt = tiles_of(a, s), heads = a.c.kv_heads;
+    if (nt == 1) {
+      if (tile) *tile = 0;
+      return want >= 0 ? 0 : (int64_t)span_of(max(1, (s.kv + UNIT - 1) / UNIT), pad) * heads;
+    }
+    const int g = a.c.group, dq = ROWS / g, dr = ROWS - dq * g;
     int q = (ROWS - 1) / g, r = ROWS - 1 - q * g;
     int64_t n = 0;
     for (int i = 0; i < nt; ++i) {
       const int see = a.causal && i + 1 < nt ? s.kv - s.n + q + 1 : s.kv;
-      const int64_t u = (int64_t)(max(1, (see + UNIT - 1) / UNIT) + OVER) * heads;
+      const int64_t u = (int64_t)span_of(max(1, (see + UNIT - 1) / UNIT), pad) * heads;
       if (want >= 0 && want < n + u) {
         *tile = i;
         return n;
@@ -152,14 +161,19 @@ struct UnitWalk {
     }
     return n;
   }
-  // Inclusive sum over the first WARPS warps of one value per thread; *all its total.
-  __device__ __forceinline__ static int64_t scan(int64_t x, int64_t* all) {
+  // Inclusive sum over the thread block (or, alone, the warp) of one value per
+  // thread; *all its total.
+  __device__ __forceinline__ static int64_t scan(int64_t x, int64_t* all, bool alone) {
     __shared__ int64_t wsum[WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
+    }
+    if (alone) {
+      *all = __shfl_sync(0xffffffffu, x, 31);
+      return x;
     }
     __syncthreads();  // an earlier call's readers are done
     if (lane == 31 && warp < WARPS) wsum[warp] = x;
@@ -173,60 +187,81 @@ struct UnitWalk {
     *all = t;
     return x;
   }
-  // Finds the share of this thread block (every thread calls it); false when it is empty.
+  // Finds the share of this thread block (every thread calls it); false when it
+  // is empty. Where all (tile, head) pairs fit the launch in shares of min_units,
+  // no share holds parts of two: short sequences are latency bound, and a share
+  // across a boundary does two pairs' chains of loads one after the other. Up to
+  // 32 sequences are one warp's work.
   __device__ bool start(const AttnArgs& a) {
-    __shared__ int64_t found[2];
+    struct Found {
+      KvSeq s;
+      int b, pad;
+      int64_t first, total;
+    };
+    __shared__ Found found;
     const KvArgs& c = a.c;
     constexpr int kN = 32 * WARPS;
-    int64_t total = 0, all, mine = 0, upto = 0;  // of this thread's sequence in the last chunk
-    for (int base = 0; base < c.n_seq; base += kN) {
-      const int i = base + (int)threadIdx.x;
-      mine = 0;
-      if (threadIdx.x < kN && i < c.n_seq) {
-        const KvSeq q = kv_seq(c, i);
+    const bool alone = c.n_seq <= 32;
+    if (!alone || threadIdx.x < 32) {
+      KvSeq q{0, 0, 0};
+      int64_t sum[2] = {0, 0}, all;  // units as they are, and padded
+      for (int base = 0; base < c.n_seq; base += kN) {
+        const int i = base + (int)threadIdx.x;
+        q = KvSeq{0, 0, 0};
+        if (threadIdx.x < kN && i < c.n_seq) q = kv_seq(c, i);
         if (q.n < 0 && blockIdx.x == 0) atomicOr(c.status, kFaultBatch);
-        mine = units_of(a, q);
+        int64_t n = units_of(a, q, 1);
+        scan(n, &all, alone);
+        sum[0] += all;
+        if (a.min_units > 1) {
+          scan(units_of(a, q, a.min_units), &all, alone);
+          sum[1] += all;
+        }
       }
-      upto = total + scan(mine, &all);
-      total += all;
-    }
-    chunk = max((int64_t)a.min_units, (total + gridDim.x - 1) / gridDim.x);
-    u = chunk * blockIdx.x;
-    u_end = min(total, u + chunk);
-    if (u >= u_end) return false;
-    int64_t before = 0;
-    for (int base = 0; base < c.n_seq; base += kN) {
-      const int i = base + (int)threadIdx.x;
-      if (c.n_seq > kN) {
-        mine = threadIdx.x < kN && i < c.n_seq ? units_of(a, kv_seq(c, i)) : 0;
-        upto = before + scan(mine, &all);
+      pad = a.min_units > 1 && sum[1] <= (int64_t)a.min_units * gridDim.x ? a.min_units : 1;
+      const int64_t total = sum[pad > 1];
+      set_chunk(a, total);
+      int64_t before = 0;
+      for (int base = 0; base < c.n_seq; base += kN) {
+        const int i = base + (int)threadIdx.x;
+        if (c.n_seq > kN) q = threadIdx.x < kN && i < c.n_seq ? kv_seq(c, i) : KvSeq{0, 0, 0};
+        const int64_t mine = units_of(a, q, pad), upto = before + scan(mine, &all, alone);
         before += all;
+        if (u < upto && u >= upto - mine) found = Found{q, i, pad, upto - mine, total};
+        if (u < before) break;
       }
-      if (u < upto && u >= upto - mine) {
-        found[0] = i;
-        found[1] = upto - mine;
-      }
-      if (c.n_seq > kN && u < before) break;
+      if (threadIdx.x == 0 && u >= total) found.total = total, found.pad = pad;
     }
     __syncthreads();
-    b = (int)found[0];
-    s = kv_seq(c, b);
-    tile_first = found[1] + units_of(a, s, u - found[1], &t);
+    pad = found.pad;
+    set_chunk(a, found.total);
+    if (u >= u_end) return false;
+    b = found.b;
+    s = found.s;
+    tile_first = found.first + units_of(a, s, pad, u - found.first, &t);
     blocks = blocks_of(a, s, t);
     return true;
+  }
+  __device__ __forceinline__ void set_chunk(const AttnArgs& a, int64_t total) {
+    const int64_t n = total + gridDim.x - 1;
+    const int64_t even = n <= INT32_MAX ? (int)n / (int)gridDim.x : n / gridDim.x;
+    chunk = pad > 1 ? pad : max((int64_t)a.min_units, even);
+    u = chunk * blockIdx.x;
+    u_end = min(total, u + chunk);
   }
   __device__ __forceinline__ bool more() const { return u < u_end; }
   __device__ __forceinline__ Segment segment(const AttnArgs& a) const {
     Segment g;
-    g.h = (int)(u - tile_first) / (blocks + OVER);
-    g.first = tile_first + (int64_t)g.h * (blocks + OVER) + OVER;
+    const int span = span_of(blocks, pad);
+    g.h = (int)(u - tile_first) / span;
+    g.first = tile_first + (int64_t)g.h * span + OVER;
     g.blk0 = max(0, (int)(u - g.first));
     g.blk1 = (int)min((int64_t)blocks, u_end - g.first);
     g.rows = min(ROWS, s.n * a.c.group - t * ROWS);
     g.empty = g.blk1 <= g.blk0;
     g.whole = g.blk0 == 0 && g.blk1 == blocks;
     // blocks before this share and from its end on, in shares (32-bit divisions)
-    if (g.empty) {
+    if (g.empty || g.whole) {
       g.c0 = g.c1 = blockIdx.x;
       return g;
     }
@@ -238,9 +273,10 @@ struct UnitWalk {
     return g;
   }
   __device__ __forceinline__ void advance(const AttnArgs& a, const Segment& g) {
-    u = g.first + g.blk1;
+    const int span = span_of(blocks, pad);
+    u = g.blk1 >= blocks ? g.first - OVER + span : max(u + 1, g.first + g.blk1);
     if (u >= u_end || g.h + 1 < a.c.kv_heads) return;
-    tile_first += (int64_t)(blocks + OVER) * a.c.kv_heads;
+    tile_first += (int64_t)span * a.c.kv_heads;
     if (++t >= tiles_of(a, s)) {
       t = 0;
       do {

@@ -112,9 +112,12 @@ struct RowStride { static constexpr int value = D + 4; };  // floats of a row in
 
 // Element d of row r of a finished tile, and its lse.
 template <typename T, int D>
-__device__ __forceinline__ void write_final(const AttnArgs& a, const KvSeq& s, int row, int h, int d, float o, float m,
-                                            float l) {
-  const int tok = s.first + row / a.c.group, head = h * a.c.group + row % a.c.group;
+__device__ __forceinline__ void write_final(const AttnArgs& a, const RowMap& map, int first, int r, int h, int d, float o,
+                                            float m, float l) {
+  int tok, head;
+  map.at(r, &tok, &head);
+  tok += first;
+  head += h * a.c.group;
   const float v = l == 0.0f ? 0.0f : __fdiv_rn(o, l);
   T* p = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.ts + (int64_t)head * a.out.hs + d;
   if constexpr (sizeof(T) == 2)
@@ -138,6 +141,7 @@ struct RowsSmem {
     } ring;
     struct {
       float o[S::kParts][S::kRows][RowStride<D>::value], m[S::kParts][S::kRows], l[S::kParts][S::kRows];
+      float f[S::kParts][S::kRows], mx[S::kRows], ls[S::kRows];  // a part's weight; the row's m and l
     } out;
   };
   unsigned long long k_full[kG][NK], k_empty[kG][NK], v_full[kG][NV], v_empty[kG][NV];
@@ -502,27 +506,36 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
         }
       }
     __syncthreads();
-    float* slot = partial_slot(a, blockIdx.x, sg.c0);
-    for (int i = threadIdx.x; i < rows * D; i += S::kThreads) {
-      const int r = i / D, d = i % D;
-      float mx = sm.out.m[0][r];
+    if ((int)threadIdx.x < rows) {
+      const int r = threadIdx.x;
+      float mx = sm.out.m[0][r], ls = 0.0f;
 #pragma unroll
       for (int k = 1; k < S::kParts; ++k) mx = fmaxf(mx, sm.out.m[k][r]);
       const float base = mx == -INFINITY ? 0.0f : mx;
-      float os = 0.0f, ls = 0.0f;
 #pragma unroll
       for (int k = 0; k < S::kParts; ++k) {
         const float f = ex2(__fsub_rn(sm.out.m[k][r], base));
-        os = __fmaf_rn(sm.out.o[k][r][d], f, os);
+        sm.out.f[k][r] = f;
         ls = __fmaf_rn(sm.out.l[k][r], f, ls);
       }
+      sm.out.mx[r] = mx;
+      sm.out.ls[r] = ls;
+    }
+    __syncthreads();
+    float* slot = partial_slot(a, blockIdx.x, sg.c0);
+    const RowMap map(c, row0);
+    for (int i = threadIdx.x; i < rows * D; i += S::kThreads) {
+      const int r = i / D, d = i % D;
+      float os = 0.0f;
+#pragma unroll
+      for (int k = 0; k < S::kParts; ++k) os = __fmaf_rn(sm.out.o[k][r][d], sm.out.f[k][r], os);
       if (sg.whole) {
-        write_final<T, D>(a, s, row0 + r, h, d, os, mx, ls);
+        write_final<T, D>(a, map, s.first, r, h, d, os, sm.out.mx[r], sm.out.ls[r]);
       } else {
         slot[r * D + d] = os;
         if (d == 0) {
-          slot[S::kRows * D + r] = mx;
-          slot[S::kRows * D + S::kRows + r] = ls;
+          slot[S::kRows * D + r] = sm.out.mx[r];
+          slot[S::kRows * D + S::kRows + r] = sm.out.ls[r];
         }
       }
     }
@@ -552,7 +565,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
             os = __fmaf_rn(__ldcg(sp + r * D + d), f, os);
             ls = __fmaf_rn(__ldcg(sp + S::kRows * D + S::kRows + r), f, ls);
           }
-          write_final<T, D>(a, s, row0 + r, h, d, os, mx, ls);
+          write_final<T, D>(a, map, s.first, r, h, d, os, mx, ls);
         }
       }
     }
@@ -605,13 +618,13 @@ __global__ void __launch_bounds__(256) paged_join_rows_kernel(const __grid_const
   l = 0.0f;
 #pragma unroll
   for (int k = 0; k < kG; ++k) l = __fadd_rn(l, sml[warp + k][0]);
-  KvSeq s{tile.first, 0, 0};
+  const RowMap map(a.c, tile.row0);
 #pragma unroll
   for (int j = 0; j < kV; ++j) {
     float v = 0.0f;
 #pragma unroll
     for (int k = 0; k < kG; ++k) v = __fadd_rn(v, so[warp + k][32 * j + lane]);
-    write_final<T, D>(a, s, tile.row0 + r, tile.h, 32 * j + lane, v, m, l);
+    write_final<T, D>(a, map, tile.first, r, tile.h, 32 * j + lane, v, m, l);
   }
 }
 
