@@ -113,6 +113,13 @@ struct Segment {
   bool whole;         // this one has it alone
 };
 
+// A segment as the kernels pass it through shared memory: blocks [blk0, blk1) of
+// kv head h for the query rows [row0, row0 + rows) of sequence b, whose new tokens
+// are rows first .. first + n of q; b < 0 ends the walk.
+struct SegRec {
+  int b, h, blk0, blk1, row0, rows, first, n, kv, c0, c1, whole;
+};
+
 template <int ROWS, int UNIT, int WARPS, int OVER>
 struct UnitWalk {
   int64_t chunk, u, u_end, tile_first;
@@ -250,6 +257,20 @@ struct UnitWalk {
     u_end = min(total, u + chunk);
   }
   __device__ __forceinline__ bool more() const { return u < u_end; }
+  __device__ __forceinline__ SegRec record(const Segment& g) const {
+    return SegRec{b, g.h, g.blk0, g.blk1, t * ROWS, g.rows, s.first, s.n, s.kv, g.c0, g.c1, g.whole};
+  }
+  // The record of this segment, the walk moved past it. In a function of its own:
+  // in line its registers cost the kernels theirs.
+  __device__ __noinline__ static void next(UnitWalk* w, const AttnArgs& a, SegRec* rec) {
+    if (!w->more()) {
+      rec->b = -1;
+      return;
+    }
+    const Segment g = w->segment(a);
+    *rec = w->record(g);
+    w->advance(a, g);
+  }
   __device__ __forceinline__ Segment segment(const AttnArgs& a) const {
     Segment g;
     const int span = span_of(blocks, pad);

@@ -128,23 +128,26 @@ __device__ __forceinline__ void write_final(const AttnArgs& a, const RowMap& map
     a.lse[(int64_t)tok * a.c.n_heads + head] = l == 0.0f ? -INFINITY : (m - kPBits + log2f(l)) * kLn2;
 }
 
-// Shared memory: a ring of key and value blocks per token group; the warps'
-// results lie over it at a segment's end.
+// Shared memory: a ring of key and value blocks per token group. At a segment's
+// end the warps' results lie over the values, while the next segment's first keys
+// are on their way.
 template <int D, int NT, int WR>
 struct RowsSmem {
   using S = Shape<NT, WR>;
   static constexpr int kG = S::kTokWarps;                            // token groups
   static constexpr int NK = WR == 1 ? 2 : 3, NV = WR == 1 ? (D == 64 ? 2 : 1) : 3;
+  using Walk = UnitWalk<S::kRows, kUnit, S::kWarps, 0>;
+  uint8_t k[kG][NK][kUnit * D];
   union {
-    struct {
-      uint8_t k[kG][NK][kUnit * D], v[kG][NV][kUnit * D];
-    } ring;
+    uint8_t v[kG][NV][kUnit * D];
     struct {
       float o[S::kParts][S::kRows][RowStride<D>::value], m[S::kParts][S::kRows], l[S::kParts][S::kRows];
       float f[S::kParts][S::kRows], mx[S::kRows], ls[S::kRows];  // a part's weight; the row's m and l
     } out;
   };
   unsigned long long k_full[kG][NK], k_empty[kG][NK], v_full[kG][NV], v_empty[kG][NV];
+  Walk walk;
+  SegRec rec[2];
   int dead, last;
 };
 
@@ -171,11 +174,15 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
   const bool feeds = wr == 0 && half == 0;  // the warp that copies for its token group
   const int log_pe = min(c.log_page, 6);  // tokens of a page within a block
 
-  UnitWalk<S::kRows, kUnit, S::kWarps, 0> w;
-  SharedTile mine{};
-  if (!w.start(a)) {
-    if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = mine;
-    return;
+  {
+    typename Mem::Walk w;
+    const bool any = w.start(a);
+    if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = SharedTile{};
+    if (!any) return;
+    if (threadIdx.x == 0) {
+      sm.walk = w;
+      Mem::Walk::next(&sm.walk, a, &sm.rec[0]);
+    }
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < Mem::kG; ++i) {
@@ -202,74 +209,76 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
 
   uint32_t nk = 0, nv = 0;  // blocks of this group so far: issued by its first warp, waited for by all
   uint32_t ik = 0, iv = 0;
-  while (w.more()) {
-    const Segment sg = w.segment(a);
-    const KvSeq s = w.s;
-    const int h = sg.h, rows = sg.rows, row0 = w.t * S::kRows;
-    const int32_t* table = c.table + (int64_t)w.b * c.table_stride;
-
-    auto find = [&](int blk) {  // lanes 0 .. 3
-      Place p{0, 0, 0, 0};
-      const int j = blk * kUnit + 16 * (lane & 3);
-      if (lane < 4 && blk < sg.blk1 && j < s.kv) {
-        const int pg = __ldg(table + (j >> c.log_page));
-        if (pg >= 0 && pg < c.n_pages) {
-          p.pg = pg;
-          p.have = min(16, s.kv - j);
-          p.ek = __ldg(c.k_exp + (int64_t)pg * c.kv_heads + h);
-          p.ev = __ldg(c.v_exp + (int64_t)pg * c.kv_heads + h);
-        } else {
-          atomicOr(c.status, kFaultBatch);
-        }
+  auto find = [&](const SegRec& sg, int blk) {  // lanes 0 .. 3
+    Place p{0, 0, 0, 0};
+    const int j = blk * kUnit + 16 * (lane & 3);
+    if (lane < 4 && blk < sg.blk1 && j < sg.kv) {
+      const int pg = __ldg(c.table + (int64_t)sg.b * c.table_stride + (j >> c.log_page));
+      if (pg >= 0 && pg < c.n_pages) {
+        p.pg = pg;
+        p.have = min(16, sg.kv - j);
+        p.ek = __ldg(c.k_exp + (int64_t)pg * c.kv_heads + sg.h);
+        p.ev = __ldg(c.v_exp + (int64_t)pg * c.kv_heads + sg.h);
+      } else {
+        atomicOr(c.status, kFaultBatch);
       }
-      return p;
-    };
-    // The copies of a block's keys or values by the group's feeding warp, to
-    // [D / 16][64][16] and [4][D][16] whatever the page: values are in one piece
-    // per page (half a page of 128), keys in one per page and 16 dims, or in one
-    // where a page is a block.
-    auto copy = [&](const Place& p, int blk, bool keys) {
-      const uint32_t n = keys ? ik++ : iv++;
-      const int st = keys ? n % Mem::NK : n % Mem::NV;
-      unsigned long long* full = keys ? &sm.k_full[wt][st] : &sm.v_full[wt][st];
-      wait(keys ? &sm.k_empty[wt][st] : &sm.v_empty[wt][st], ((n / (keys ? Mem::NK : Mem::NV)) & 1) ^ 1);
-      if (a.stall >= 0 && (int)n >= a.stall) return;
-      uint8_t* dst = keys ? sm.ring.k[wt][st] : sm.ring.v[wt][st];
-      const uint8_t* src = (keys ? c.k : c.v) + (int64_t)h * (D << c.log_page);
-      const int64_t page_bytes = (int64_t)c.kv_heads * (D << c.log_page);
-      const int pe = 1 << log_pe, off = c.log_page > 6 ? (blk & 1) * kUnit : 0;  // tokens of a page in the block, first one
-      const int pages = kUnit >> log_pe;
-      // lane i < 4 holds group i; the first group of a page stands for it
-      const bool first = lane < 4 && ((16 * lane) & (pe - 1)) == 0 && p.have > 0;
-      const uint32_t got = __ballot_sync(0xffffffffu, first);
-      if (lane == 0) mbar_expect_tx(full, __popc(got) * D * pe);
-      __syncwarp();
-      const bool runs = keys && c.log_page != 6;
-      const int pieces = runs ? pages * kI : pages;  // at most 32
-      const int pgi = runs ? lane % pages : lane, run = runs ? lane / pages : 0, gi = (pgi << log_pe) >> 4;
-      const int pg = __shfl_sync(0xffffffffu, p.pg, gi & 3);
-      if (lane < pieces && ((got >> gi) & 1)) {
-        const uint8_t* from = src + pg * page_bytes + (runs ? ((run << c.log_page) + off) * 16 : off * D);
-        bulk_g2s(dst + (runs ? (run * kUnit + pgi * pe) * 16 : pgi * pe * D), from, runs ? pe * 16 : pe * D, full);
-      }
-    };
+    }
+    return p;
+  };
+  // The copies of a block's keys or values by the group's feeding warp, to
+  // [D / 16][64][16] and [4][D][16] whatever the page: values are in one piece
+  // per page (half a page of 128), keys in one per page and 16 dims, or in one
+  // where a page is a block.
+  auto copy = [&](const Place& p, int h, int blk, bool keys) {
+    const uint32_t n = keys ? ik++ : iv++;
+    const int st = keys ? n % Mem::NK : n % Mem::NV;
+    unsigned long long* full = keys ? &sm.k_full[wt][st] : &sm.v_full[wt][st];
+    wait(keys ? &sm.k_empty[wt][st] : &sm.v_empty[wt][st], ((n / (keys ? Mem::NK : Mem::NV)) & 1) ^ 1);
+    if (a.stall >= 0 && (int)n >= a.stall) return;
+    uint8_t* dst = keys ? sm.k[wt][st] : sm.v[wt][st];
+    const uint8_t* src = (keys ? c.k : c.v) + (int64_t)h * (D << c.log_page);
+    const int64_t page_bytes = (int64_t)c.kv_heads * (D << c.log_page);
+    const int pe = 1 << log_pe, off = c.log_page > 6 ? (blk & 1) * kUnit : 0;  // tokens of a page in the block, first one
+    const int pages = kUnit >> log_pe;
+    // lane i < 4 holds group i; the first group of a page stands for it
+    const bool first = lane < 4 && ((16 * lane) & (pe - 1)) == 0 && p.have > 0;
+    const uint32_t got = __ballot_sync(0xffffffffu, first);
+    if (lane == 0) mbar_expect_tx(full, __popc(got) * D * pe);
+    __syncwarp();
+    const bool runs = keys && c.log_page != 6;
+    const int pieces = runs ? pages * kI : pages;  // at most 32
+    const int pgi = runs ? lane % pages : lane, run = runs ? lane / pages : 0, gi = (pgi << log_pe) >> 4;
+    const int pg = __shfl_sync(0xffffffffu, p.pg, gi & 3);
+    if (lane < pieces && ((got >> gi) & 1)) {
+      const uint8_t* from = src + pg * page_bytes + (runs ? ((run << c.log_page) + off) * 16 : off * D);
+      bulk_g2s(dst + (runs ? (run * kUnit + pgi * pe) * 16 : pgi * pe * D), from, runs ? pe * 16 : pe * D, full);
+    }
+  };
 
-    // ---- the first blocks on their way
+  // A segment's first blocks: their places, and their keys on their way.
+  Place cur, nx[Mem::NK - 1];
+  auto begin = [&](const SegRec& sg) {
     const int b0 = sg.blk0 + wt;
-    Place cur = find(b0);
-    Place nx[Mem::NK - 1];  // blocks whose keys are on their way behind it
+    cur = find(sg, b0);
 #pragma unroll
-    for (int i = 0; i < Mem::NK - 1; ++i) nx[i] = find(b0 + (i + 1) * S::kTokWarps);
+    for (int i = 0; i < Mem::NK - 1; ++i) nx[i] = find(sg, b0 + (i + 1) * S::kTokWarps);
     if (feeds) {
-      if (b0 < sg.blk1) copy(cur, b0, true), copy(cur, b0, false);
+      if (b0 < sg.blk1) copy(cur, sg.h, b0, true);
 #pragma unroll
-      for (int i = 0; i < Mem::NK - 1; ++i) {
-        const int b = b0 + (i + 1) * S::kTokWarps;
-        if (b < sg.blk1) {
-          copy(nx[i], b, true);
-          if (i + 1 < Mem::NV) copy(nx[i], b, false);
-        }
-      }
+      for (int i = 0; i < Mem::NK - 1; ++i)
+        if (b0 + (i + 1) * S::kTokWarps < sg.blk1) copy(nx[i], sg.h, b0 + (i + 1) * S::kTokWarps, true);
+    }
+  };
+  begin(sm.rec[0]);
+  for (int turn = 0; sm.rec[turn].b >= 0; turn ^= 1) {
+    const SegRec& sg = sm.rec[turn];
+    const int h = sg.h, rows = sg.rows, row0 = sg.row0, blk1 = sg.blk1, b0 = sg.blk0 + wt;
+    if (threadIdx.x == 0) Mem::Walk::next(&sm.walk, a, &sm.rec[turn ^ 1]);
+    if (feeds) {
+      if (b0 < blk1) copy(cur, h, b0, false);
+#pragma unroll
+      for (int i = 0; i + 1 < Mem::NV; ++i)
+        if (b0 + (i + 1) * S::kTokWarps < blk1) copy(nx[i], h, b0 + (i + 1) * S::kTokWarps, false);
     }
 
     // ---- query fragments: row wr kRowsPerWarp + 8 nt + g; a row past the last repeats it
@@ -283,7 +292,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       const bool have = r < rows;
       const int row = row0 + min(r, rows - 1), tok = row / c.group;
       float x[4 * kI];
-      const T* p = static_cast<const T*>(a.q.p) + (int64_t)(s.first + tok) * a.q.ts +
+      const T* p = static_cast<const T*>(a.q.p) + (int64_t)(sg.first + tok) * a.q.ts +
                    (int64_t)(h * c.group + row - tok * c.group) * a.q.hs + 4 * t4;
 #pragma unroll
       for (int i = 0; i < kI; ++i) load4(p + 16 * i, a.vec, x + 4 * i);
@@ -306,7 +315,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
           qf[nt][1][i] = half2_bits(__fsub_rn(y0, hi.x), __fsub_rn(y1, hi.y));
         }
       }
-      const int see = a.causal ? s.kv - s.n + tok : s.kv - 1;
+      const int see = a.causal ? sg.kv - sg.n + tok : sg.kv - 1;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         rm[nt][i] = __shfl_sync(0xffffffffu, mul, 4 * (2 * t4 + i));
@@ -329,9 +338,9 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
         for (int i = 0; i < 4; ++i) o[nt][dt][i] = 0.0f;
     }
 
-    for (int blk = b0; blk < sg.blk1; blk += S::kTokWarps) {
+    for (int blk = b0; blk < blk1; blk += S::kTokWarps) {
       const float nan = __int_as_float(0x7FC00000);
-      const Place far = find(blk + Mem::NK * S::kTokWarps);
+      const Place far = find(sg, blk + Mem::NK * S::kTokWarps);
       // some row is hidden from some token, or a group is short or marked
       const bool odd = cur.have < 16 || cur.ek == kExpNan || cur.ev == kExpNan;
       const bool masked = blk * kUnit + kUnit - 1 > lim_min || __any_sync(0xffffffffu, lane < 4 && odd);
@@ -341,7 +350,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       wait(&sm.k_full[wt][ks], (nk / Mem::NK) & 1);
       ++nk;
       float x[NT][kT][4];
-      const uint8_t* kb = sm.ring.k[wt][ks] + (4 * (g >> 1) + (g & 1)) * 16 + 4 * t4;
+      const uint8_t* kb = sm.k[wt][ks] + (4 * (g >> 1) + (g & 1)) * 16 + 4 * t4;
 #pragma unroll
       for (int i = 0; i < kT; ++i)
 #pragma unroll
@@ -370,7 +379,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.k_empty[wt][ks]);
-      if (feeds && blk + Mem::NK * S::kTokWarps < sg.blk1) copy(far, blk + Mem::NK * S::kTokWarps, true);
+      if (feeds && blk + Mem::NK * S::kTokWarps < blk1) copy(far, h, blk + Mem::NK * S::kTokWarps, true);
 
       // ---- softmax weights
       uint32_t pf[NT][kTerms][2 * kT];
@@ -451,12 +460,12 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
           const uint32_t keep = first_bytes(__shfl_sync(0xffffffffu, cur.have, kT * half + i) - 4 * t4);
 #pragma unroll 1
           for (int d = g; d < D; d += 8)  // warps that share the ring all do it, to the same effect
-            *reinterpret_cast<uint32_t*>(sm.ring.v[wt][vs] + ((kT * half + i) * D + d) * 16 + 4 * t4) &= keep;
+            *reinterpret_cast<uint32_t*>(sm.v[wt][vs] + ((kT * half + i) * D + d) * 16 + 4 * t4) &= keep;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // a copy overwrites it later
         __syncwarp();
       }
-      const uint8_t* vb = sm.ring.v[wt][vs] + g * 16 + 4 * t4;
+      const uint8_t* vb = sm.v[wt][vs] + g * 16 + 4 * t4;
       auto value = [&](int i, int dim) { return *reinterpret_cast<const uint32_t*>(vb + ((kT * half + i) * D + dim) * 16); };
 #pragma unroll
       for (int i = 0; i < kT; ++i)
@@ -477,16 +486,18 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
         }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.v_empty[wt][vs]);
-      if (feeds && blk + Mem::NV * S::kTokWarps < sg.blk1)
-        copy(Mem::NV == Mem::NK ? far : nx[Mem::NV - 1], blk + Mem::NV * S::kTokWarps, false);
+      if (feeds && blk + Mem::NV * S::kTokWarps < blk1)
+        copy(Mem::NV == Mem::NK ? far : nx[Mem::NV - 1], h, blk + Mem::NV * S::kTokWarps, false);
       cur = nx[0];
 #pragma unroll
       for (int i = 0; i + 1 < Mem::NK - 1; ++i) nx[i] = nx[i + 1];
       nx[Mem::NK - 2] = far;
     }
 
-    // ---- the warps' results to shared memory, over the ring
+    // ---- the warps' results to shared memory, over the values; the next
+    // segment's first keys meanwhile
     __syncthreads();
+    if (sm.rec[turn ^ 1].b >= 0) begin(sm.rec[turn ^ 1]);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -530,7 +541,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
 #pragma unroll
       for (int k = 0; k < S::kParts; ++k) os = __fmaf_rn(sm.out.o[k][r][d], sm.out.f[k][r], os);
       if (sg.whole) {
-        write_final<T, D>(a, map, s.first, r, h, d, os, sm.out.mx[r], sm.out.ls[r]);
+        write_final<T, D>(a, map, sg.first, r, h, d, os, sm.out.mx[r], sm.out.ls[r]);
       } else {
         slot[r * D + d] = os;
         if (d == 0) {
@@ -540,7 +551,8 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
       }
     }
     if (a.shared) {
-      if (!sg.whole && sg.c0 == (int)blockIdx.x) mine = SharedTile{row0, rows, s.first, h, sg.c1, {0, 0, 0}};
+      if (!sg.whole && sg.c0 == (int)blockIdx.x && threadIdx.x == 0)
+        a.shared[blockIdx.x] = SharedTile{row0, rows, sg.first, h, sg.c1, {0, 0, 0}};
     } else if (!sg.whole) {
       __threadfence();
       __syncthreads();
@@ -565,14 +577,13 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
             os = __fmaf_rn(__ldcg(sp + r * D + d), f, os);
             ls = __fmaf_rn(__ldcg(sp + S::kRows * D + S::kRows + r), f, ls);
           }
-          write_final<T, D>(a, map, s.first, r, h, d, os, mx, ls);
+          write_final<T, D>(a, map, sg.first, r, h, d, os, mx, ls);
         }
       }
     }
-    // the next segment's copies land where this one's results were
+    // the next segment's values land where this one's results were
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
-    w.advance(a, sg);
   }
   if (sm.dead && feeds && lane == 0) {  // copies in flight land before the block ends
     for (uint32_t i = ik > Mem::NK ? ik - Mem::NK : 0; i < ik; ++i)
@@ -580,7 +591,6 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(
     for (uint32_t i = iv > Mem::NV ? iv - Mem::NV : 0; i < iv; ++i)
       (void)mbar_wait(&sm.v_full[wt][i % Mem::NV], (i / Mem::NV) & 1, a.wait_ns);
   }
-  if (a.shared && threadIdx.x == 0) a.shared[blockIdx.x] = mine;
 }
 
 // Joins the parts of the shared tile that begins in block blockIdx.x's share. A

@@ -63,12 +63,6 @@ using Walk = UnitWalk<kRows, BN, 4, kOver>;
 template <int N>
 struct Idesc { static constexpr uint32_t value = idesc_f16(BM, N); };  // formats 0: e4m3, binary16
 
-// A segment as the roles read it: blocks [blk0, blk1) of kv head h for the query
-// rows [row0, row0 + rows) of sequence b; b < 0 ends the walk.
-struct SegRec {
-  int b, h, blk0, blk1, row0, rows, first, n, kv, c0, c1, whole;
-};
-
 template <int D>
 struct Smem {
   uint8_t q[2][2][D / 16][BM + 1][16];  // tile, term, 16 dims; runs one row apart in the banks
@@ -214,7 +208,7 @@ __device__ __noinline__ void walk_role(const AttnArgs& a, Walk w, Smem<D>& sm, c
       mine = SharedTile{w.t * kRows, g.rows, w.s.first, g.h, g.c1, {0, 0, 0}};
     if (!g.empty) {
       if (!wait_lane(x, &sm.seg_empty[i % kRing], ((i / kRing) & 1) ^ 1)) return;
-      sm.seg[i % kRing] = SegRec{w.b, g.h, g.blk0, g.blk1, w.t * kRows, g.rows, w.s.first, w.s.n, w.s.kv, g.c0, g.c1, g.whole};
+      sm.seg[i % kRing] = w.record(g);
       mbar_arrive(&sm.seg_full[i % kRing]);
       ++i;
     }
