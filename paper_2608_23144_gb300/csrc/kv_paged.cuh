@@ -74,11 +74,11 @@ __device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t codes) {
   return r;
 }
 
-// Attention: thread blocks a launch may have (one per SM), each with two slots
+// Attention: thread blocks a launch may have (two per SM), each with two slots
 // for partial results of the first and last tile it shares with others.
-constexpr int kMaxAttnBlocks = 152;
-constexpr int kSlotRows = 128;
-// The tensor-memory kernel: 256 rows.
+constexpr int kMaxAttnBlocks = 304;
+constexpr int kSlotRows = 64;
+// The tensor-memory kernel: one per SM, 256 rows.
 constexpr int kMaxTileBlocks = 152;
 constexpr int kTileSlotRows = 256;
 

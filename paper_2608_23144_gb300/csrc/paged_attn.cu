@@ -27,9 +27,10 @@
 // q . k, tokens 16 s + 4 t + {0..3} in step s of p . V; score row tile s has token
 // 16 s + 4 (g / 2) + g % 2 in row g and two further in row 8 + g.
 //
-// Decode (one row tile): eight rings, each with every eighth block of a segment
-// and two warps to halve it. Many rows: the warps hold 16 rows each and share one
-// ring.
+// Decode (one row tile): four rings, each with every fourth block of a segment and
+// two warps to halve it. Many rows: four warps hold 16 rows each and share one
+// ring. Two thread blocks per SM, so that one's starts and ends of segments (a
+// third of the time of 64 ragged sequences) pass under the other's products.
 //
 // Work: the (sequence, row tile, kv head, 64-token block) units of the batch in
 // this order are dealt out in equal contiguous shares to the thread blocks,
@@ -99,11 +100,11 @@ template <int NT, int WR>
 struct Shape {
   static constexpr int kRowsPerWarp = 8 * NT;
   static constexpr int kRows = kRowsPerWarp * WR;  // query rows of a tile
-  static constexpr int kTokWarps = 8 / WR;         // token groups: rings of blocks
+  static constexpr int kTokWarps = 4 / WR;         // token groups: rings of blocks
   // warps that share a group's blocks, 64 / kH tokens each: two for decode steps,
-  // whose few registers leave room for 16 warps
+  // whose few registers leave room for 16 warps on an SM
   static constexpr int kH = NT == 1 && WR == 1 ? 2 : 1;
-  static constexpr int kWarps = 8 * kH, kThreads = 32 * kWarps;
+  static constexpr int kWarps = 4 * kH, kThreads = 32 * kWarps;
   static constexpr int kParts = kTokWarps * kH;    // partial results of a row in the block
 };
 
@@ -158,7 +159,7 @@ struct Place {
 };
 
 template <typename T, int D, int NT, int WR>
-__global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 1) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 2) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<NT, WR>;
   using Mem = RowsSmem<D, NT, WR>;
   constexpr int kI = D / 16;           // runs of 16 dims, and row tiles of p . V
@@ -642,7 +643,7 @@ template <typename T, int D, int NT, int WR>
 cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   const int64_t tiles = tiles_upper(a.c, Shape<NT, WR>::kRows);
   using Mem = RowsSmem<D, NT, WR>;
-  static_assert(sizeof(Mem) <= 227 * 1024, "shared memory of a block");
+  static_assert(sizeof(Mem) <= 113 * 1024, "shared memory of two blocks");
   const cudaError_t e =
       cudaFuncSetAttribute(paged_rows_kernel<T, D, NT, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Mem));
   if (e != cudaSuccess) return e;
@@ -672,7 +673,7 @@ cudaError_t pick(const AttnArgs& a, int max_new, int64_t max_blocks, cudaStream_
   const int64_t rows = (int64_t)max_new * a.c.group;
   if (rows <= 8) return launch<T, D, 1, 1>(a, max_blocks, st);
   if (rows <= 16) return launch<T, D, 2, 1>(a, max_blocks, st);
-  return launch<T, D, 2, 8>(a, max_blocks, st);
+  return launch<T, D, 2, 4>(a, max_blocks, st);
 }
 
 }  // namespace
