@@ -87,7 +87,7 @@ struct AttnArgs {
   KvRows q, out;
   float* lse;
   float score_mul;  // sm_scale log2(e)
-  int causal, vec;  // vec: rows of q are 16-byte aligned
+  int causal, vec, vec_out;  // rows of q, of out are 16-byte aligned
   int min_units;    // least share of a block
   int* arrived;     // per block: arrivals at the shared tile that begins in its share (row kernel)
   struct SharedTile* shared;  // per block: the shared tile that begins in its share (tensor-memory kernel)

@@ -111,22 +111,36 @@ struct Shape {
 template <int D>
 struct RowStride { static constexpr int value = D + 4; };  // floats of a row in shared memory
 
-// Element d of row r of a finished tile, and its lse.
-template <typename T, int D>
-__device__ __forceinline__ void write_final(const AttnArgs& a, const RowMap& map, int first, int r, int h, int d, float o,
-                                            float m, float l) {
+__device__ __forceinline__ float inv_of(float l) { return l == 0.0f ? 0.0f : __frcp_rn(l); }
+
+// Dims d .. d + 3 of row r of a finished tile: o / l by `inv`, and its lse.
+template <typename T>
+__device__ __forceinline__ void write4(const AttnArgs& a, const RowMap& map, int first, int r, int h, int d, const float4& o,
+                                       float m, float l, float inv) {
   int tok, head;
   map.at(r, &tok, &head);
   tok += first;
   head += h * a.c.group;
-  const float v = l == 0.0f ? 0.0f : __fdiv_rn(o, l);
   T* p = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.ts + (int64_t)head * a.out.hs + d;
-  if constexpr (sizeof(T) == 2)
-    *p = __float2bfloat16_rn(v);
-  else
-    *p = v;
-  if (d == 0 && a.lse)
-    a.lse[(int64_t)tok * a.c.n_heads + head] = l == 0.0f ? -INFINITY : (m - kPBits + log2f(l)) * kLn2;
+  const float v[4] = {__fmul_rn(o.x, inv), __fmul_rn(o.y, inv), __fmul_rn(o.z, inv), __fmul_rn(o.w, inv)};
+  if constexpr (sizeof(T) == 2) {
+    const __nv_bfloat162 b0 = __floats2bfloat162_rn(v[0], v[1]), b1 = __floats2bfloat162_rn(v[2], v[3]);
+    if (a.vec_out) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
+    } else {
+      p[0] = b0.x, p[1] = b0.y, p[2] = b1.x, p[3] = b1.y;
+    }
+  } else if (a.vec_out) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = v[i];
+  }
+  if (d == 0 && a.lse) a.lse[(int64_t)tok * a.c.n_heads + head] = l == 0.0f ? -INFINITY : (m - kPBits + log2f(l)) * kLn2;
+}
+
+__device__ __forceinline__ float4 fma4(const float4& a, float f, const float4& c) {
+  return make_float4(__fmaf_rn(a.x, f, c.x), __fmaf_rn(a.y, f, c.y), __fmaf_rn(a.z, f, c.z), __fmaf_rn(a.w, f, c.w));
 }
 
 // Shared memory: a ring of key and value blocks per token group. At a segment's
@@ -143,7 +157,8 @@ struct RowsSmem {
     uint8_t v[kG][NV][kUnit * D];
     struct {
       float o[S::kParts][S::kRows][RowStride<D>::value], m[S::kParts][S::kRows], l[S::kParts][S::kRows];
-      float f[S::kParts][S::kRows], mx[S::kRows], ls[S::kRows];  // a part's weight; the row's m and l
+      float f[S::kParts][S::kRows];                             // a part's weight
+      float mx[S::kRows], ls[S::kRows], inv[S::kRows];          // the row's m, l and 1 / l
     } out;
   };
   unsigned long long k_full[kG][NK], k_empty[kG][NK], v_full[kG][NV], v_empty[kG][NV];
@@ -532,19 +547,22 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 2) paged_rows_kernel(
       }
       sm.out.mx[r] = mx;
       sm.out.ls[r] = ls;
+      sm.out.inv[r] = inv_of(ls);
     }
     __syncthreads();
     float* slot = partial_slot(a, blockIdx.x, sg.c0);
     const RowMap map(c, row0);
-    for (int i = threadIdx.x; i < rows * D; i += S::kThreads) {
-      const int r = i / D, d = i % D;
-      float os = 0.0f;
+    const bool whole = sg.whole;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < rows * (D / 4); i += S::kThreads) {
+      const int r = i / (D / 4), d = i % (D / 4) * 4;
+      float4 os = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-      for (int k = 0; k < S::kParts; ++k) os = __fmaf_rn(sm.out.o[k][r][d], sm.out.f[k][r], os);
-      if (sg.whole) {
-        write_final<T, D>(a, map, sg.first, r, h, d, os, sm.out.mx[r], sm.out.ls[r]);
+      for (int k = 0; k < S::kParts; ++k) os = fma4(*reinterpret_cast<const float4*>(&sm.out.o[k][r][d]), sm.out.f[k][r], os);
+      if (whole) {
+        write4<T>(a, map, sg.first, r, h, d, os, sm.out.mx[r], sm.out.ls[r], sm.out.inv[r]);
       } else {
-        slot[r * D + d] = os;
+        *reinterpret_cast<float4*>(slot + r * D + d) = os;
         if (d == 0) {
           slot[S::kRows * D + r] = sm.out.mx[r];
           slot[S::kRows * D + S::kRows + r] = sm.out.ls[r];
@@ -564,21 +582,39 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 2) paged_rows_kernel(
       __syncthreads();
       if (sm.last) {
         __threadfence();
-        for (int i = threadIdx.x; i < rows * D; i += S::kThreads) {
-          const int r = i / D, d = i % D;
-          float mx = -INFINITY;
-#pragma unroll 4
-          for (int k = sg.c0; k <= sg.c1; ++k) mx = fmaxf(mx, __ldcg(partial_slot(a, k, sg.c0) + S::kRows * D + r));
-          const float base = mx == -INFINITY ? 0.0f : mx;
-          float os = 0.0f, ls = 0.0f;
-#pragma unroll 4
-          for (int k = sg.c0; k <= sg.c1; ++k) {
-            const float* sp = partial_slot(a, k, sg.c0);
-            const float f = ex2(__fsub_rn(__ldcg(sp + S::kRows * D + r), base));
-            os = __fmaf_rn(__ldcg(sp + r * D + d), f, os);
-            ls = __fmaf_rn(__ldcg(sp + S::kRows * D + S::kRows + r), f, ls);
+        for (int i = threadIdx.x; i < rows * (D / 4); i += S::kThreads) {
+          const int r = i / (D / 4), d = i % (D / 4) * 4;
+          // four parts at a time, their loads in flight together, each batch's
+          // maximum before its sums
+          float mx = -INFINITY, ls = 0.0f;
+          float4 os = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int k0 = sg.c0; k0 <= sg.c1; k0 += 4) {
+            float pm[4], pl[4];
+            float4 po[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float* sp = partial_slot(a, min(k0 + k, sg.c1), sg.c0);
+              pm[k] = __ldcg(sp + S::kRows * D + r);
+              pl[k] = __ldcg(sp + S::kRows * D + S::kRows + r);
+              po[k] = __ldcg(reinterpret_cast<const float4*>(sp + r * D + d));
+            }
+            float mn = mx;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mn = fmaxf(mn, pm[k]);
+            const float base = mn == -INFINITY ? 0.0f : mn, al = ex2(__fsub_rn(mx, base));
+            mx = mn;
+            ls = __fmul_rn(ls, al);
+            os = make_float4(__fmul_rn(os.x, al), __fmul_rn(os.y, al), __fmul_rn(os.z, al), __fmul_rn(os.w, al));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (k0 + k <= sg.c1) {
+                const float f = ex2(__fsub_rn(pm[k], base));
+                ls = __fmaf_rn(pl[k], f, ls);
+                os = fma4(po[k], f, os);
+              }
+            }
           }
-          write_final<T, D>(a, map, sg.first, r, h, d, os, mx, ls);
+          write4<T>(a, map, sg.first, r, h, d, os, mx, ls, inv_of(ls));
         }
       }
     }
@@ -599,44 +635,40 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 2) paged_rows_kernel(
 // and are added in order.
 template <typename T, int D, int ROWS, int RB>
 __global__ void __launch_bounds__(256) paged_join_rows_kernel(const __grid_constant__ AttnArgs a) {
-  constexpr int kG = 8 / RB, kV = D / 32;  // warps of a row, dims of a lane
-  __shared__ float so[8][D], sml[8][2];
+  constexpr int kG = 8 / RB, kV = D / 4;  // warps of a row, lanes of a part of it
+  constexpr int kP = 32 / kV;             // parts a warp takes at a time
+  __shared__ float4 so[8][32];
+  __shared__ float sl[8][32];
   const SharedTile tile = a.shared[blockIdx.x];
   if ((int)blockIdx.y * RB >= tile.rows) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
   const int r = min((int)blockIdx.y * RB + warp / kG, tile.rows - 1), part = warp % kG;
-  float m = -INFINITY, l = 0.0f, o[kV];
+  const int d = lane % kV * 4, sub = lane / kV;
+  float m = -INFINITY, l = 0.0f;
   for (int k = c0 + lane; k <= tile.c1; k += 32) m = fmaxf(m, partial_slot(a, k, c0)[ROWS * D + r]);
 #pragma unroll
   for (int i = 16; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
   const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-  for (int j = 0; j < kV; ++j) o[j] = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-  for (int k = c0 + part; k <= tile.c1; k += kG) {
+  for (int k = c0 + part * kP + sub; k <= tile.c1; k += kG * kP) {
     const float* sp = partial_slot(a, k, c0);
     const float f = ex2(__fsub_rn(sp[ROWS * D + r], base));
     l = __fmaf_rn(sp[ROWS * D + ROWS + r], f, l);
-#pragma unroll
-    for (int j = 0; j < kV; ++j) o[j] = __fmaf_rn(sp[r * D + 32 * j + lane], f, o[j]);
+    o = fma4(*reinterpret_cast<const float4*>(sp + r * D + d), f, o);
   }
-#pragma unroll
-  for (int j = 0; j < kV; ++j) so[warp][32 * j + lane] = o[j];
-  if (lane == 0) sml[warp][0] = l;
+  so[warp][lane] = o;
+  sl[warp][lane] = l;
   __syncthreads();
-  if (part != 0 || (int)blockIdx.y * RB + warp / kG >= tile.rows) return;
-  // l of the row first, then its dims
+  if (part != 0 || sub != 0 || (int)blockIdx.y * RB + warp / kG >= tile.rows) return;
   l = 0.0f;
+  o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-  for (int k = 0; k < kG; ++k) l = __fadd_rn(l, sml[warp + k][0]);
-  const RowMap map(a.c, tile.row0);
-#pragma unroll
-  for (int j = 0; j < kV; ++j) {
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kG; ++k) v = __fadd_rn(v, so[warp + k][32 * j + lane]);
-    write_final<T, D>(a, map, tile.first, r, tile.h, 32 * j + lane, v, m, l);
+  for (int k = 0; k < kG * kP; ++k) {
+    l = __fadd_rn(l, sl[warp + k / kP][lane + k % kP * kV]);
+    o = fma4(so[warp + k / kP][lane + k % kP * kV], 1.0f, o);
   }
+  write4<T>(a, RowMap(a.c, tile.row0), tile.first, r, tile.h, d, o, m, l, inv_of(l));
 }
 
 template <typename T, int D, int NT, int WR>
@@ -648,15 +680,16 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
       cudaFuncSetAttribute(paged_rows_kernel<T, D, NT, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Mem));
   if (e != cudaSuccess) return e;
   AttnArgs b = a;
-  b.min_units = 2 * Shape<NT, WR>::kTokWarps;
+  b.min_units = 4 * Shape<NT, WR>::kTokWarps;
   b.vec = rows_aligned(a.q, sizeof(T));
+  b.vec_out = rows_aligned(a.out, sizeof(T));
   int64_t grid = kMaxAttnBlocks;
   const int64_t most = tiles * a.c.kv_heads * max_blocks;
   if (grid > most) grid = most;
   // A tile of few parts is joined by its last block to arrive; where there can be
   // more, its serial reading took 40 us of a 131k-token decode step, and a second
   // launch joins all tiles on the whole GPU.
-  const bool join = max_blocks / b.min_units > kMaxParts;
+  const bool join = max_blocks / b.min_units > (Shape<NT, WR>::kRows > 16 ? 1 : kMaxParts);
   if (!join) b.shared = nullptr;
   paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, Shape<NT, WR>::kThreads, sizeof(Mem), st>>>(b);
   note_launches(1);
