@@ -86,6 +86,21 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float* x) {
   }
 }
 
+// Element i of 8 in 16-byte vectors.
+template <typename T>
+__device__ __forceinline__ float element(const uint4* v, int i) {
+  const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[sizeof(T) / 4].x, v[sizeof(T) / 4].y, v[sizeof(T) / 4].z, v[sizeof(T) / 4].w};
+  if constexpr (sizeof(T) == 2)
+    return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+  else
+    return __uint_as_float(w[i]);
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4* v, float* x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = element<T>(v, i);
+}
+
 // One item of a rotated head: W dims at d1 and, when `two`, their partners at d2.
 template <int W>
 struct Item {
@@ -279,7 +294,9 @@ __device__ void append_job(const AppendArgs& a, int b, int nth, int head, bool k
   const T* sp = static_cast<const T*>(src.p) + (int64_t)head * src.hs;
 
   Item<W> it;
-  float vy[4][W];  // values: 4 rows
+  constexpr int kV = sizeof(T) == 2 ? 1 : 2;  // 16-byte vectors of 8 elements
+  uint4 vr[4][kV];                            // values: 4 rows as they came (in half the registers if bf16)
+  float v1 = 0.0f;                            // or one element
   auto load = [&](int i) {
     if (keys) {
       const int t = i / per;
@@ -291,10 +308,13 @@ __device__ void append_job(const AppendArgs& a, int b, int nth, int head, bool k
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int r = r4 + j - row0;
-        load_row<W>(sp + (int64_t)(tok0 + min(max(r, 0), n - 1)) * src.ts + d, vy[j]);  // a row of the job if not r
+        const uint4* p = reinterpret_cast<const uint4*>(  // a row of the job if not r
+            sp + (int64_t)(tok0 + min(max(r, 0), n - 1)) * src.ts + d);
+#pragma unroll
+        for (int x = 0; x < kV; ++x) vr[j][x] = p[x];
       }
     } else {
-      load_row<W>(sp + (int64_t)(tok0 + i / D) * src.ts + i % D, vy[0]);
+      load_row<1>(sp + (int64_t)(tok0 + i / D) * src.ts + i % D, &v1);
     }
   };
   float m = 0.0f;
@@ -302,11 +322,16 @@ __device__ void append_job(const AppendArgs& a, int b, int nth, int head, bool k
     load(i);
     if (keys) {
       m = item_amax<W>(it, m);
+    } else if (W == 8) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float y[8];
+        unpack<T>(vr[j], y);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) m = fmax_nan(m, fabsf(y[x]));
+      }
     } else {
-#pragma unroll
-      for (int j = 0; j < (W == 8 ? 4 : 1); ++j)
-#pragma unroll
-        for (int x = 0; x < W; ++x) m = fmax_nan(m, fabsf(vy[j][x]));
+      m = fmax_nan(m, fabsf(v1));
     }
   }
   m = job_amax<JW>(m);
@@ -344,10 +369,16 @@ __device__ void append_job(const AppendArgs& a, int b, int nth, int head, bool k
       const int r4 = (g0 + i / (D / 8)) * 4, d = i % (D / 8) * 8;
       uint8_t* p = blk + ((int64_t)((r4 >> 4) * D + d) << 4) + (r4 & 15);
       const bool whole = r4 >= row0 && r4 + 4 <= row0 + n;
+      if (bad) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int x = 0; x < kV; ++x) vr[j][x] = make_uint4(0, 0, 0, 0);
+      }
 #pragma unroll
       for (int x = 0; x < W; ++x) {
-        const float y0 = bad ? 0.0f : vy[0][x], y1 = bad ? 0.0f : vy[1][x];
-        const float y2 = bad ? 0.0f : vy[2][x], y3 = bad ? 0.0f : vy[3][x];
+        const float y0 = element<T>(vr[0], x), y1 = element<T>(vr[1], x);
+        const float y2 = element<T>(vr[2], x), y3 = element<T>(vr[3], x);
         const uint32_t w = e4m3x2(__fmul_rn(y0, inv), __fmul_rn(y1, inv)) |
                            (e4m3x2(__fmul_rn(y2, inv), __fmul_rn(y3, inv)) << 16);
         if (whole) {
@@ -360,7 +391,7 @@ __device__ void append_job(const AppendArgs& a, int b, int nth, int head, bool k
       }
     } else {
       const int row = row0 + i / D, d = i % D;
-      blk[(((row >> 4) * D + d) << 4) + (row & 15)] = (uint8_t)e4m3x2(__fmul_rn(bad ? 0.0f : vy[0][0], inv), 0.0f);
+      blk[(((row >> 4) * D + d) << 4) + (row & 15)] = (uint8_t)e4m3x2(__fmul_rn(bad ? 0.0f : v1, inv), 0.0f);
     }
   }
 }
@@ -391,29 +422,34 @@ __device__ void rotate_q(const AppendArgs& a, int t, int part, int parts) {
   const T* qp = static_cast<const T*>(a.q.p) + (int64_t)t * a.q.ts;
   T* op = static_cast<T*>(a.qo.p) + (int64_t)t * a.qo.ts;
   if (W == 8 && !a.interleaved && a.half == D / 2) {
-    // whole heads: a lane keeps its 8 pairs of the tables; four heads in flight
-    constexpr int kPer = D / 16, kHeads = 32 / kPer;  // lanes of a head, heads at a time
+    // whole heads: a lane keeps its 8 pairs of the tables; kU heads in flight,
+    // unpacked only when they are turned
+    constexpr int kPer = D / 16, kHeads = 32 / kPer, kU = 2;  // lanes of a head, heads at a time
+    constexpr int kV = sizeof(T) == 2 ? 1 : 2;                // 16-byte vectors of 8 elements
     const int it = lane % kPer;
     float cs[W], sn[W];
     load_row<W>(cr + W * it, cs);
     load_row<W>(sr + W * it, sn);
     const int step = parts * kHeads;
-    for (int h0 = part * kHeads + lane / kPer; h0 < c.n_heads; h0 += 4 * step) {
-      float x[4][2 * W];
+    for (int h0 = part * kHeads + lane / kPer; h0 < c.n_heads; h0 += kU * step) {
+      uint4 raw[kU][2][kV];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const T* p = qp + (int64_t)min(h0 + u * step, c.n_heads - 1) * a.q.hs + W * it;
-        load_row<W>(p, x[u]);
-        load_row<W>(p + D / 2, x[u] + W);
+      for (int u = 0; u < kU; ++u) {
+        const uint4* p = reinterpret_cast<const uint4*>(qp + (int64_t)min(h0 + u * step, c.n_heads - 1) * a.q.hs + W * it);
+#pragma unroll
+        for (int j = 0; j < kV; ++j) raw[u][0][j] = p[j], raw[u][1][j] = p[D / 16 * kV + j];
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kU; ++u) {
+        float x[2 * W];
+        unpack<T>(raw[u][0], x);
+        unpack<T>(raw[u][1], x + W);
 #pragma unroll
-        for (int i = 0; i < W; ++i) turn(x[u][i], x[u][W + i], cs[i], sn[i]);
+        for (int i = 0; i < W; ++i) turn(x[i], x[W + i], cs[i], sn[i]);
         if (h0 + u * step < c.n_heads) {
           T* o = op + (int64_t)(h0 + u * step) * a.qo.hs + W * it;
-          store_row<W>(o, x[u]);
-          store_row<W>(o + D / 2, x[u] + W);
+          store_row<W>(o, x);
+          store_row<W>(o + D / 2, x + W);
         }
       }
     }
@@ -431,8 +467,11 @@ __device__ void rotate_q(const AppendArgs& a, int t, int part, int parts) {
   }
 }
 
+// Bytes in flight come from warps, not from deeper loops: at 13k tokens of 40
+// heads (bf16) 3 thread blocks per SM with four heads in flight took 81 us, 6
+// with two 76, 8 (64 registers) 72; unrolling the jobs' loops cost 10 us.
 template <typename T, int D, int W, int JW>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 5) kv_append_kernel(const __grid_constant__ AppendArgs a) {
   // which kind, and the how many-th of it
   const int i = blockIdx.x, few = min(a.kv_blocks, a.q_blocks);
   const int nth = i / a.every, before = min(few, nth + (i % a.every != 0));  // blocks of the rarer kind up to i
