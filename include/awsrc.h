@@ -547,8 +547,8 @@ typedef struct awsrc_rows {
  * of sequences shared among blocks) use; one workspace serves any batch of this
  * cache on one stream. Host-only.
  * awsrc_attention_workspace_init — makes a new workspace usable (clears the
- * fault word and the arrival counters, which every call leaves cleared). Once
- * per workspace. The fault word of these calls accumulates until
+ * fault word and the arrival counters, which every call leaves cleared unless a
+ * wait of it gave up). Once per workspace. The fault word of these calls accumulates until
  * awsrc_workspace_status reads and clears it.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA.
  */
@@ -570,8 +570,7 @@ awsrc_status awsrc_attention_workspace_init(const awsrc_kv_cache* cache, int32_t
  * but for codes that leave e4m3's normal range). A block whose exponent is -128
  * stays so until its page is written from row 0 again; its new codes are 0.
  *   n_heads    query heads, a multiple of n_kv_heads (at most 1024 times as
- *              many, else UNSUPPORTED); q, q_out
- *              [n_tok][n_heads].
+ *              many, else UNSUPPORTED); q, q_out [n_tok][n_heads].
  *   k, v       [n_tok][n_kv_heads]; q, k, v and q_out share a dtype.
  *   cos, sin   device, rope_rows x rotary_dim / 2 floats (NULL when rotary_dim
  *              is 0); a token at p >= rope_rows is skipped and reported.
@@ -595,6 +594,8 @@ awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const awsrc_kv_batch* 
  * F32 keeps q and the softmax weights in two binary16 terms (22 bits) each and
  * sums in binary32. BF16 keeps q exact and the weights in 8 bits or more; out is
  * rounded once. Sums run in a fixed order: results repeat bit for bit.
+ * Visible tokens' codes must be finite (awsrc_kv_append writes no e4m3 NaN);
+ * the bytes of rows past kv_len may be anything. Two launches at most.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA.
  */
 awsrc_status awsrc_paged_attention(const awsrc_kv_cache* cache, const awsrc_kv_batch* batch, int32_t n_heads,
@@ -650,8 +651,8 @@ void awsrc_set_search_pruning(int32_t enabled);
 /*
  * awsrc_set_wait_test — a test of the kernels' failure handling, for the
  * calling host thread (no counterpart in the paper). Every wait inside the
- * tcgen05 search kernels (for bulk copies, tensor-core results and the release
- * of shared buffers) gives up after a time limit, 2 s by default; the block
+ * tcgen05 search and the attention kernels (for bulk copies, tensor-core results
+ * and the release of shared buffers) gives up after a time limit, 2 s by default; the block
  * then records bit 2 of the workspace's fault word, waits (with the same
  * limit) for its own copies and tensor-core work still in flight, frees its
  * tensor memory and exits, so the GPU context stays usable.
@@ -660,8 +661,9 @@ void awsrc_set_search_pruning(int32_t enabled);
  *   stall_chunk  >= 0: the C = 64, P = 4, AWSRC-U search issues no copies of
  *                its seed chunks from this one (counted within each block's
  *                range of 32-seed chunks) on, so its waits for that chunk run
- *                out; the tensor-memory kernel of awsrc_paged_attention stops
- *                its copies the same way, counted in blocks of 128 tokens; -1:
+ *                out; awsrc_paged_attention stops its copies the same way,
+ *                counted per ring of blocks of 128 tokens (the tensor-memory
+ *                kernel: one ring) or of 64 (the other: one or four); -1:
  *                normal operation.
  * The call's results are then undefined and awsrc_workspace_status reports
  * bit 2. awsrc_set_wait_test(0, -1) restores normal operation; an attention

@@ -211,16 +211,17 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 2) paged_rows_kernel(
   __syncthreads();
   // Bounded; once one has given up, all return at once and the results are void.
   auto wait = [&](unsigned long long* mb, uint32_t parity) {
-    if (mbar_try_wait(mb, parity)) return;
+    if (mbar_try_wait(mb, parity)) return true;
     const uint64_t t0 = globaltimer();
     while (!mbar_try_wait(mb, parity)) {
-      if (*(volatile int*)&sm.dead) return;
+      if (*(volatile int*)&sm.dead) return false;
       if (globaltimer() - t0 > a.wait_ns) {
         *(volatile int*)&sm.dead = 1;
         atomicOr(c.status, kFaultTimeout);
-        return;
+        return false;
       }
     }
+    return true;
   };
 
   uint32_t nk = 0, nv = 0;  // blocks of this group so far: issued by its first warp, waited for by all
@@ -249,8 +250,9 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 2) paged_rows_kernel(
     const uint32_t n = keys ? ik++ : iv++;
     const int st = keys ? n % Mem::NK : n % Mem::NV;
     unsigned long long* full = keys ? &sm.k_full[wt][st] : &sm.v_full[wt][st];
-    wait(keys ? &sm.k_empty[wt][st] : &sm.v_empty[wt][st], ((n / (keys ? Mem::NK : Mem::NV)) & 1) ^ 1);
-    if (a.stall >= 0 && (int)n >= a.stall) return;
+    const bool ok = wait(keys ? &sm.k_empty[wt][st] : &sm.v_empty[wt][st], ((n / (keys ? Mem::NK : Mem::NV)) & 1) ^ 1);
+    // nothing is copied into a stage that was not given back, or by the limit's test
+    if (!__all_sync(0xffffffffu, ok) || (a.stall >= 0 && (int)n >= a.stall)) return;
     uint8_t* dst = keys ? sm.k[wt][st] : sm.v[wt][st];
     const uint8_t* src = (keys ? c.k : c.v) + (int64_t)h * (D << c.log_page);
     const int64_t page_bytes = (int64_t)c.kv_heads * (D << c.log_page);

@@ -20,8 +20,9 @@
 // One thread block per SM and 256 rows (query tokens x the heads of a kv head)
 // in two tiles of 128, so that one tile's softmax runs under the other's
 // products. Warps 0-3 and 4-7: softmax, one row per thread; 8-11: widening; 12
-// and 13: MMA issue; 14: bulk copies (15 idle). Tensor memory: S 2 x 128 columns, over whose
-// first 64 P is written; O 2 x D columns. Per tile and block of 128 tokens:
+// and 13: MMA issue; 14: bulk copies; 15: the walk over the share. Tensor memory:
+// S 2 x 128 columns, over whose first 64 P is written; O 2 x D columns. Per tile
+// and block of 128 tokens:
 //   MMA:     P ready -> O += P V; S = Q K of the next block -> commit
 //   softmax: S ready -> m, P, l; O rescaled by its own threads, only when a row
 //            grew by more than 2^8 (the commit that made S ready also covers
@@ -49,7 +50,7 @@ using namespace tc05;
 constexpr int BM = 128, BN = 128;
 constexpr int kRows = 2 * BM;
 constexpr int kThreads = 512;
-constexpr int kMmaWarp = 12, kLoadWarp = 14, kWalkWarp = 15;
+constexpr int kMmaWarp = 12, kLoadWarp = 14;  // 15 walks the share
 constexpr int kRing = 4, kReaders = 15;  // segments handed out ahead; warps that read them
 constexpr int NK = 3, NV = 2, NW = 2;  // stages: keys, value codes, widened values
 constexpr uint32_t kTmemCols = 512;
@@ -73,7 +74,7 @@ struct Smem {
   unsigned long long q_full[2], s_full[2], p_full[2], o_full[2], turn[2], drain[2];
   unsigned long long seg_full[kRing], seg_empty[kRing];
   SegRec seg[kRing];
-  float4 group_of[8][2][8];  // softmax warp, block parity: scale of the keys, exponent and unscaling of the values, tokens
+  float4 group_of[8][2][8];  // softmax warp, block parity: scale of the keys, exponent and unscaling of the values, -
   uint32_t tmem;
   int dead;
 };
@@ -147,11 +148,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
-               : "memory");
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {  // one instruction of the half-rate pipe for two
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -168,16 +164,15 @@ __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.
 // lane i < 8 about group i: tokens in it (0 for a page that cannot be right)
 // and the exponents of its page.
 struct Groups {
-  int page, have, ek, ev;
+  int have, ek, ev;
 };
 __device__ __forceinline__ Groups load_groups(const KvArgs& c, const int32_t* table, int kv, int h, int blk) {
   const int lane = threadIdx.x & 31;
   const int j = blk * BN + 16 * (lane & 7);
-  Groups g{0, 0, 0, 0};
+  Groups g{0, 0, 0};
   if (lane < 8 && j < kv) {
     const int pg = __ldg(table + (j >> c.log_page));
     if (pg >= 0 && pg < c.n_pages) {
-      g.page = pg;
       g.have = min(16, kv - j);
       g.ek = __ldg(c.k_exp + (int64_t)pg * c.kv_heads + h);
       g.ev = __ldg(c.v_exp + (int64_t)pg * c.kv_heads + h);
@@ -721,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
         mbar_init(&sm.p_full[i], 128);
         mbar_init(&sm.o_full[i], 1);
         mbar_init(&sm.turn[i], 1);
-          mbar_init(&sm.drain[i], 1);
+        mbar_init(&sm.drain[i], 1);
       }
       for (int i = 0; i < kRing; ++i) mbar_init(&sm.seg_full[i], 1), mbar_init(&sm.seg_empty[i], kReaders);
       sm.dead = 0;

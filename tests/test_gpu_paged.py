@@ -425,3 +425,22 @@ def test_waits_that_run_out_are_reported(aw):
         finally:
             aw.awsrc_set_wait_test()
     check_attention(aw, cache, q, new, kv, table, True)
+
+
+@pytest.mark.parametrize("dtype,new", [(F32, 1), (F32, 40), (BF16, 2)])
+def test_waits_of_the_row_kernel_that_run_out_are_reported(aw, dtype, new):
+    """The same for the kernel of few rows, whose rings take blocks of 64 tokens: one ring of a thread block's share, or
+    four. 70000 tokens of two heads over at most 304 blocks give each ring two blocks and more."""
+    gen = torch.Generator().manual_seed(13)
+    _, table, pages = make_batch(aw, gen, [new], [70000], 64)
+    cache = random_cache(aw, gen, pages, 2, 128, 64)
+    q = torch.randn(new, 6, 128, generator=gen).to(dtype)
+    for stall in (0, 1):
+        ws = aw.awsrc_attention_workspace(cache, 6)
+        aw.awsrc_set_wait_test(100_000_000, stall)
+        try:
+            aw.awsrc_paged_attention(cache, step_batch(aw, [new], [70000], table), q.cuda(), ws)
+            assert aw.awsrc_workspace_status(ws) == 4
+        finally:
+            aw.awsrc_set_wait_test()
+    check_attention(aw, cache, q, [new], [70000], table, True)
