@@ -228,6 +228,16 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
     const SegRec& sg = sm.seg[is % kRing];
     if (sg.b < 0) break;
     const int32_t* table = c.table + (int64_t)sg.b * c.table_stride;
+    // the softmax warps stage the segment's query rows some blocks from now
+    const RowMap map(c, sg.row0);
+    for (int r = lane; r < sg.rows; r += 32) {
+      int tok, head;
+      map.at(r, &tok, &head);
+      const char* p = reinterpret_cast<const char*>(static_cast<const __nv_bfloat16*>(a.q.p) + (int64_t)(sg.first + tok) * a.q.ts +
+                                                    (int64_t)(sg.h * c.group + head) * a.q.hs);
+#pragma unroll
+      for (int i = 0; i < 2 * D; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
+    }
     for (int blk = sg.blk0; ok && blk < sg.blk1; ++blk, ++n) {
       if ((int)n == a.stall) {  // the limit's test
         ok = false;
@@ -279,6 +289,9 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
 // One warp issues the products of tile t, so that its waits pass under the other
 // tile's products. The two take turns, a block's products at a time: left to
 // interleave, both tiles' products ended together and so did their softmax.
+// A commit costs the tensor cores 74 cycles (measured; the 16 products of a block
+// take 1028), so there is one per block: weights handed over (p_full) say that the
+// scores they came from, and all products issued before those, are done.
 template <int D>
 __device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
   constexpr uint32_t kIdescS = Idesc<BN>::value, kIdescO = Idesc<D>::value;
@@ -298,9 +311,8 @@ __device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
     for (int s = 0; s < D / 16; ++s)  // both terms: 32 dims a step, 2 runs of 16 further each
       umma_f8(ts, q0 + s * (2 * (BM + 1) * 16 >> 4), kd + (s & (D / 32 - 1)) * (2 * BN * 16 >> 4), kIdescS, s > 0);
     umma_commit(&sm.s_full[t]);
-    umma_commit(&sm.k_empty[blk % NK]);
   };
-  bool ok = true;
+  bool ok = true, held = false;  // held: the widened values of block n - 1 are not given back yet
   for (; ok; ++is) {
     if (!(ok = wait_lane(x, &sm.seg_full[is % kRing], (is / kRing) & 1))) break;
     const SegRec& sg = sm.seg[is % kRing];
@@ -308,6 +320,8 @@ __device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
     const int nb = sg.blk1 - sg.blk0;
     if (sg.rows <= t * BM) {  // no row in this tile: its blocks pass
       if (!(ok = my_turn())) break;
+      if (held) umma_commit(&sm.w_empty[(n - 1) % NW]);
+      held = false;
       mbar_arrive(&sm.turn[t ^ 1]);
       for (int i = 0; ok && i < nb; ++i, ++n) {
         if (!(ok = wait_lane(x, &sm.k_full[n % NK], (n / NK) & 1))) break;
@@ -328,12 +342,15 @@ __device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
         if (i + 1 < nb && !(ok = wait_lane(x, &sm.k_full[n1 % NK], (n1 / NK) & 1))) break;
         if (!(ok = wait_lane(x, &sm.w_full[n % NW], (n / NW) & 1))) break;
         const uint64_t vd = v0 + (uint64_t)(n % NW) * (sizeof(sm.w[0]) >> 4);
-        if (!(ok = wait_lane(x, &sm.p_full[t], np++ & 1)) || !(ok = my_turn())) break;
+        if (!(ok = wait_lane(x, &sm.p_full[t], np++ & 1))) break;
+        mbar_arrive(&sm.k_empty[n % NK]);
+        if (held) mbar_arrive(&sm.w_empty[(n - 1) % NW]);
+        held = true;
+        if (!(ok = my_turn())) break;
         tc_fence_after();
 #pragma unroll
         for (int s = 0; s < BN / 16; ++s)
           umma_f16_ts(to, ts + s * 8, vd + s * (2 * D * 16 >> 4), kIdescO, i + s > 0);
-        umma_commit(&sm.w_empty[n % NW]);
         if (i + 1 < nb)
           qk(n1);
         else
