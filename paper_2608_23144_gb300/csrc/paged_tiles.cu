@@ -216,11 +216,20 @@ __device__ __noinline__ void walk_role(const AttnArgs& a, Walk w, Smem<D>& sm, c
 }
 
 // ------------------------------------------------------------------- copies --
+// Bulk copies, but for the keys of 16-token pages: 64 pieces of 256 bytes a block
+// took longer than its products (714 us for chunks that take 465 us from pages of
+// 64), so these go 16 bytes per lane.
+__device__ __forceinline__ bool small_pages(const KvArgs& c) { return c.log_page == 4; }
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
+
 template <int D>
 __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
   const KvArgs& c = a.c;
   const int lane = threadIdx.x & 31;
   const int per = BN >> c.log_page;  // pages of a block
+  const bool small = small_pages(c);
   uint32_t n = 0, is = 0;
   bool ok = true;
   for (; ok; ++is) {
@@ -256,14 +265,26 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
       const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, pg >= 0)) * D) << c.log_page;
       const int ks = n % NK, vs = n % NV;
       if (!(ok = wait_warp(x, &sm.k_empty[ks], ((n / NK) & 1) ^ 1))) break;
-      if (lane == 0) mbar_expect_tx(&sm.k_full[ks], bytes);
-      __syncwarp();
-      for (int i0 = 0; i0 < (D / 16) * per; i0 += 32) {
-        const int i = i0 + lane, p = i & (per - 1), run = i / per;
-        const int pp = __shfl_sync(0xffffffffu, pg, p);
-        if (pp >= 0 && run < D / 16)
-          bulk_g2s(&sm.k[ks][run][p << c.log_page][0], c.k + block_off<D>(c, pp, sg.h) + ((run << c.log_page) << 4),
-                   16u << c.log_page, &sm.k_full[ks]);
+      if (small) {
+#pragma unroll
+        for (int j = 0; j < BN / 32; ++j) {  // a page's run per half warp
+          const int pp = __shfl_sync(0xffffffffu, pg, 2 * j + (lane >> 4));
+          if (pp < 0) continue;
+          const uint8_t* src = c.k + block_off<D>(c, pp, sg.h) + 16 * (lane & 15);
+#pragma unroll
+          for (int run = 0; run < D / 16; ++run) copy16(&sm.k[ks][run][32 * j + lane][0], src + 256 * run);
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&sm.k_full[ks])) : "memory");
+      } else {
+        if (lane == 0) mbar_expect_tx(&sm.k_full[ks], bytes);
+        __syncwarp();
+        for (int i0 = 0; i0 < (D / 16) * per; i0 += 32) {
+          const int i = i0 + lane, p = i & (per - 1), run = i / per;
+          const int pp = __shfl_sync(0xffffffffu, pg, p);
+          if (pp >= 0 && run < D / 16)
+            bulk_g2s(&sm.k[ks][run][p << c.log_page][0], c.k + block_off<D>(c, pp, sg.h) + ((run << c.log_page) << 4),
+                     16u << c.log_page, &sm.k_full[ks]);
+        }
       }
       if (!(ok = wait_warp(x, &sm.v_empty[vs], ((n / NV) & 1) ^ 1))) {
         ++n;
@@ -279,6 +300,7 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
     __syncwarp();
     if (lane == 0) mbar_arrive(&sm.seg_empty[is % kRing]);
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   if (!ok && lane == 0) {  // copies in flight land before the block ends
     for (uint32_t j = n > NK ? n - NK : 0; j < n; ++j) (void)mbar_wait(&sm.k_full[j % NK], (j / NK) & 1, x.wait_ns);
     for (uint32_t j = n > NV ? n - NV : 0; j < n; ++j) (void)mbar_wait(&sm.v_full[j % NV], (j / NV) & 1, x.wait_ns);
@@ -293,13 +315,15 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
 // take 1028), so there is one per block: weights handed over (p_full) say that the
 // scores they came from, and all products issued before those, are done.
 template <int D>
-__device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
+__device__ void mma_role(Smem<D>& sm, const Ctx& x, int t, bool small) {
   constexpr uint32_t kIdescS = Idesc<BN>::value, kIdescO = Idesc<D>::value;
   const uint32_t ts = sm.tmem + t * BN, to = sm.tmem + 2 * BN + t * D;
   const uint64_t q0 = desc(smem_addr(&sm.q[t][0][0][0][0]), (BM + 1) * 16);
   const uint64_t k0 = desc(smem_addr(&sm.k[0][0][0][0]), BN * 16);
   const uint64_t v0 = desc(smem_addr(&sm.w[0][0][0][0]), D * 16);
   uint32_t n = 0, nq = 0, np = 0, turns = 0, is = 0;
+  // copies 16 bytes at a time are ordinary writes to shared memory
+  auto async_fence = [] { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); };
   // tile 0 has the first turn
   auto my_turn = [&]() {
     const uint32_t k = turns++;
@@ -335,6 +359,7 @@ __device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
       if (!(ok = wait_lane(x, &sm.q_full[t], nq++ & 1)) || !(ok = wait_lane(x, &sm.k_full[n % NK], (n / NK) & 1)) || !(ok = my_turn()))
         break;
       tc_fence_after();
+      if (small) async_fence();
       qk(n);
       mbar_arrive(&sm.turn[t ^ 1]);
       for (int i = 0; i < nb; ++i, ++n) {
@@ -348,6 +373,7 @@ __device__ void mma_role(Smem<D>& sm, const Ctx& x, int t) {
         held = true;
         if (!(ok = my_turn())) break;
         tc_fence_after();
+        if (small) async_fence();
 #pragma unroll
         for (int s = 0; s < BN / 16; ++s)
           umma_f16_ts(to, ts + s * 8, vd + s * (2 * D * 16 >> 4), kIdescO, i + s > 0);
@@ -724,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
   const int warp = threadIdx.x >> 5;
   if (warp == kLoadWarp) {
     if ((threadIdx.x & 31) == 0) {
-      for (int i = 0; i < NK; ++i) mbar_init(&sm.k_full[i], 1), mbar_init(&sm.k_empty[i], 2);
+      for (int i = 0; i < NK; ++i) mbar_init(&sm.k_full[i], small_pages(a.c) ? 32 : 1), mbar_init(&sm.k_empty[i], 2);
       for (int i = 0; i < NV; ++i) mbar_init(&sm.v_full[i], 1), mbar_init(&sm.v_empty[i], 128);
       for (int i = 0; i < NW; ++i) mbar_init(&sm.w_full[i], 128), mbar_init(&sm.w_empty[i], 2);
       for (int i = 0; i < 2; ++i) {
@@ -755,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_c
     if (warp < kMmaWarp) {
       widen_role<D>(a, sm, x);
     } else if (warp < kLoadWarp) {
-      if ((threadIdx.x & 31) == 0) mma_role<D>(sm, x, warp - kMmaWarp);
+      if ((threadIdx.x & 31) == 0) mma_role<D>(sm, x, warp - kMmaWarp, small_pages(a.c));
     } else if (warp == kLoadWarp) {
       load_role<D>(a, sm, x);
     } else if ((threadIdx.x & 31) == 0) {
