@@ -31,11 +31,12 @@ struct AttnLayout {
 AttnLayout attn_layout(const awsrc_kv_cache& c) {
   AttnLayout L{};
   L.arrived = kStatusBytes;
-  L.shared = L.arrived + align_up((size_t)kMaxAttnBlocks * sizeof(int), 256);
-  L.partial = L.shared + align_up((size_t)kMaxAttnBlocks * sizeof(SharedTile), 256);
+  const size_t blocks = max_attn_blocks(c.head_dim);
+  L.shared = L.arrived + align_up(blocks * sizeof(int), 256);
+  L.partial = L.shared + align_up(blocks * sizeof(SharedTile), 256);
   L.row_slot = (int64_t)kSlotRows * (c.head_dim + 2);
   L.tile_slot = (int64_t)kTileSlotRows * (c.head_dim + 2);
-  const size_t rows = (size_t)2 * kMaxAttnBlocks * L.row_slot, tiles = (size_t)2 * kMaxTileBlocks * L.tile_slot;
+  const size_t rows = 2 * blocks * L.row_slot, tiles = (size_t)2 * kMaxTileBlocks * L.tile_slot;
   L.total = L.partial + align_up((rows > tiles ? rows : tiles) * sizeof(float), 256);
   return L;
 }

@@ -74,9 +74,10 @@ __device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t codes) {
   return r;
 }
 
-// Attention: thread blocks a launch may have (two per SM), each with two slots
-// for partial results of the first and last tile it shares with others.
-constexpr int kMaxAttnBlocks = 304;
+// Attention: thread blocks a launch may have (two per SM, four with 64-dim
+// heads), each with two slots for partial results of the first and last tile it
+// shares with others.
+constexpr int max_attn_blocks(int dim) { return dim == 64 ? 608 : 304; }
 constexpr int kSlotRows = 64;
 // The tensor-memory kernel: one per SM, 256 rows.
 constexpr int kMaxTileBlocks = 152;
@@ -90,7 +91,7 @@ struct AttnArgs {
   int causal, vec, vec_out;  // rows of q, of out are 16-byte aligned
   int min_units;    // least share of a block
   int* arrived;     // per block: arrivals at the shared tile that begins in its share (row kernel)
-  struct SharedTile* shared;  // per block: the shared tile that begins in its share (tensor-memory kernel)
+  struct SharedTile* shared;  // per block: the shared tile that begins in its share, when a second launch joins
   float* partial;
   int64_t slot_floats;
   uint64_t wait_ns;  // limit of the kernels' waits

@@ -106,6 +106,8 @@ struct Shape {
   static constexpr int kH = NT == 1 && WR == 1 ? 2 : 1;
   static constexpr int kWarps = 4 * kH, kThreads = 32 * kWarps;
   static constexpr int kParts = kTokWarps * kH;    // partial results of a row in the block
+  // thread blocks per SM: more where 64-dim heads leave registers for them
+  static constexpr int blocks(int dim) { return dim == 64 && WR == 4 ? 4 : 2; }
 };
 
 template <int D>
@@ -174,7 +176,7 @@ struct Place {
 };
 
 template <typename T, int D, int NT, int WR>
-__global__ void __launch_bounds__(Shape<NT, WR>::kThreads, 2) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks(D)) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<NT, WR>;
   using Mem = RowsSmem<D, NT, WR>;
   constexpr int kI = D / 16;           // runs of 16 dims, and row tiles of p . V
@@ -677,7 +679,7 @@ template <typename T, int D, int NT, int WR>
 cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   const int64_t tiles = tiles_upper(a.c, Shape<NT, WR>::kRows);
   using Mem = RowsSmem<D, NT, WR>;
-  static_assert(sizeof(Mem) <= 113 * 1024, "shared memory of two blocks");
+  static_assert((sizeof(Mem) + 1024) * Shape<NT, WR>::blocks(D) <= 228 * 1024, "shared memory of an SM");
   const cudaError_t e =
       cudaFuncSetAttribute(paged_rows_kernel<T, D, NT, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Mem));
   if (e != cudaSuccess) return e;
@@ -685,7 +687,8 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   b.min_units = 4 * Shape<NT, WR>::kTokWarps;
   b.vec = rows_aligned(a.q, sizeof(T));
   b.vec_out = rows_aligned(a.out, sizeof(T));
-  int64_t grid = kMaxAttnBlocks;
+  int64_t grid = 152 * Shape<NT, WR>::blocks(D);
+  static_assert(152 * Shape<NT, WR>::blocks(D) <= max_attn_blocks(D), "partial results in the workspace");
   const int64_t most = tiles * a.c.kv_heads * max_blocks;
   if (grid > most) grid = most;
   // A tile of few parts is joined by its last block to arrive; where there can be
