@@ -103,7 +103,7 @@ struct AttnArgs {
 // of UNIT tokens), in this order; rows are query tokens x the heads of a kv
 // head. A tile has as many blocks as its last row sees tokens, at least one;
 // OVER further units in front of them stand for what starting and finishing a
-// tile costs. The thread blocks of a launch take equal contiguous shares, a
+// tile costs (but not where shares are padded, below). The thread blocks of a launch take equal contiguous shares, a
 // segment being the part of one (tile, head) in a share.
 struct Segment {
   int h, blk0, blk1;  // kv head, blocks [blk0, blk1)
@@ -140,9 +140,9 @@ struct UnitWalk {
     return s.n > 0 ? (s.n * a.c.group + ROWS - 1) / ROWS : 0;
   }
   __device__ __forceinline__ static int span_of(int blocks, int pad) {
-    const int n = blocks + OVER;
-    return pad == 1 ? n : (n + pad - 1) / pad * pad;
+    return pad == 1 ? blocks + OVER : (blocks + pad - 1) / pad * pad;
   }
+  __device__ __forceinline__ int lead() const { return pad == 1 ? OVER : 0; }  // units in front of block 0
   // Units of the tiles of s, or with `want` >= 0 the tile that holds unit `want`
   // of them (*tile, and the units before it as the result). No division per tile:
   // the token of a tile's last row advances by ROWS / group.
@@ -264,19 +264,19 @@ struct UnitWalk {
   // The record of this segment, the walk moved past it. In a function of its own:
   // in line its registers cost the kernels theirs.
   __device__ __noinline__ static void next(UnitWalk* w, const AttnArgs& a, SegRec* rec) {
-    if (!w->more()) {
-      rec->b = -1;
-      return;
+    rec->b = -1;
+    while (w->more()) {
+      const Segment g = w->segment(a);
+      if (!g.empty) *rec = w->record(g);
+      w->advance(a, g);
+      if (!g.empty) return;
     }
-    const Segment g = w->segment(a);
-    *rec = w->record(g);
-    w->advance(a, g);
   }
   __device__ __forceinline__ Segment segment(const AttnArgs& a) const {
     Segment g;
     const int span = span_of(blocks, pad);
     g.h = (int)(u - tile_first) / span;
-    g.first = tile_first + (int64_t)g.h * span + OVER;
+    g.first = tile_first + (int64_t)g.h * span + lead();
     g.blk0 = max(0, (int)(u - g.first));
     g.blk1 = (int)min((int64_t)blocks, u_end - g.first);
     g.rows = min(ROWS, s.n * a.c.group - t * ROWS);
@@ -296,7 +296,7 @@ struct UnitWalk {
   }
   __device__ __forceinline__ void advance(const AttnArgs& a, const Segment& g) {
     const int span = span_of(blocks, pad);
-    u = g.blk1 >= blocks ? g.first - OVER + span : max(u + 1, g.first + g.blk1);
+    u = g.blk1 >= blocks ? g.first - lead() + span : max(u + 1, g.first + g.blk1);
     if (u >= u_end || g.h + 1 < a.c.kv_heads) return;
     tile_first += (int64_t)span * a.c.kv_heads;
     if (++t >= tiles_of(a, s)) {

@@ -58,7 +58,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPBits = 6.0f;         // p is at most 2^6 when m is the maximum,
 constexpr float kTiny = 0x1p-80f;      // least score multiplier: times a block's scale, hidden scores of -inf stay -inf
 constexpr float kGrow = 8.0f;          // and at most 2^(6 + 8) < 65504 when m lags
-constexpr int kOver = 4;               // a tile's start and end, in blocks
+constexpr int kOver = 6;               // a tile's start and end and its masked blocks, in blocks (four prompts: 2: 423 us, 4: 330, 6: 321, 8: 337)
 using Walk = UnitWalk<kRows, BN, 4, kOver>;
 
 template <int N>
