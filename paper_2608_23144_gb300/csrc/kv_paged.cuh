@@ -342,6 +342,20 @@ __device__ __forceinline__ float ex2(float x) {
 // A word whose first n bytes are ones.
 __device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (n <= 0 ? 0u : (1u << (8 * n)) - 1u); }
 
+// Bulk copies bring blocks of tokens to shared memory, but for the keys of
+// 16-token pages: pieces of 256 bytes took longer than the block's products (chunks
+// that take 465 us from pages of 64 took 714 us, decode steps that take 66 us 77),
+// so these go 16 bytes per lane.
+__host__ __device__ __forceinline__ bool small_pages(const KvArgs& c) { return c.log_page == 4; }
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+// Arrives at mb once this lane's copies so far are there.
+__device__ __forceinline__ void copies_arrive(unsigned long long* mb) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"((uint32_t)__cvta_generic_to_shared(mb)) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // 4 codes -> binary16 pairs.
 __device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"

@@ -179,7 +179,9 @@ struct Place {
   int pg, have, ek, ev;
 };
 
-template <typename T, int D, int NT, int WR>
+// SMALL: pages of 16 tokens. A case of its own, since its copies cost the others
+// 1 to 3 us of a decode step in registers.
+template <typename T, int D, int NT, int WR, bool SMALL>
 __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks(D)) paged_rows_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<NT, WR>;
   using Mem = RowsSmem<D, NT, WR>;
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < Mem::kG; ++i) {
-      for (int j = 0; j < Mem::NK; ++j) mbar_init(&sm.k_full[i][j], 1), mbar_init(&sm.k_empty[i][j], WR * kH);
+      for (int j = 0; j < Mem::NK; ++j) mbar_init(&sm.k_full[i][j], SMALL ? 32 : 1), mbar_init(&sm.k_empty[i][j], WR * kH);
       for (int j = 0; j < Mem::NV; ++j) mbar_init(&sm.v_full[i][j], 1), mbar_init(&sm.v_empty[i][j], WR * kH);
     }
     sm.dead = 0;
@@ -267,6 +269,19 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
     // lane i < 4 holds group i; the first group of a page stands for it
     const bool first = lane < 4 && ((16 * lane) & (pe - 1)) == 0 && p.have > 0;
     const uint32_t got = __ballot_sync(0xffffffffu, first);
+    if (SMALL && keys) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {  // a page's run per half warp
+        const int gi = 2 * j + (lane >> 4), pg = __shfl_sync(0xffffffffu, p.pg, gi);
+        const uint8_t* from = src + pg * page_bytes + 16 * (lane & 15);
+        if ((got >> gi) & 1) {
+#pragma unroll
+          for (int run = 0; run < kI; ++run) copy16(dst + (run * kUnit + 32 * j + lane) * 16, from + 256 * run);
+        }
+      }
+      copies_arrive(full);
+      return;
+    }
     if (lane == 0) mbar_expect_tx(full, __popc(got) * D * pe);
     __syncwarp();
     const bool runs = keys && c.log_page != 6;
@@ -630,6 +645,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
   }
+  if (SMALL) copies_wait();
   if (sm.dead && feeds && lane == 0) {  // copies in flight land before the block ends
     for (uint32_t i = ik > Mem::NK ? ik - Mem::NK : 0; i < ik; ++i)
       (void)mbar_wait(&sm.k_full[wt][i % Mem::NK], (i / Mem::NK) & 1, a.wait_ns);
@@ -684,8 +700,8 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   const int64_t tiles = tiles_upper(a.c, Shape<NT, WR>::kRows);
   using Mem = RowsSmem<D, NT, WR>;
   static_assert((sizeof(Mem) + 1024) * Shape<NT, WR>::blocks(D) <= 228 * 1024, "shared memory of an SM");
-  const cudaError_t e =
-      cudaFuncSetAttribute(paged_rows_kernel<T, D, NT, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Mem));
+  const auto kernel = small_pages(a.c) ? paged_rows_kernel<T, D, NT, WR, true> : paged_rows_kernel<T, D, NT, WR, false>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Mem));
   if (e != cudaSuccess) return e;
   AttnArgs b = a;
   b.min_units = 4 * Shape<NT, WR>::kTokWarps;
@@ -700,7 +716,7 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   // launch joins all tiles on the whole GPU.
   const bool join = max_blocks / b.min_units > (Shape<NT, WR>::kRows > 16 ? 1 : kMaxParts);
   if (!join) b.shared = nullptr;
-  paged_rows_kernel<T, D, NT, WR><<<(unsigned)grid, Shape<NT, WR>::kThreads, sizeof(Mem), st>>>(b);
+  kernel<<<(unsigned)grid, Shape<NT, WR>::kThreads, sizeof(Mem), st>>>(b);
   note_launches(1);
   if (join) {
     constexpr int kRows = Shape<NT, WR>::kRows, kRB = kRows <= 16 ? 1 : 8;

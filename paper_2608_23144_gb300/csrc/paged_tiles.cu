@@ -216,14 +216,6 @@ __device__ __noinline__ void walk_role(const AttnArgs& a, Walk w, Smem<D>& sm, c
 }
 
 // ------------------------------------------------------------------- copies --
-// Bulk copies, but for the keys of 16-token pages: 64 pieces of 256 bytes a block
-// took longer than its products (714 us for chunks that take 465 us from pages of
-// 64), so these go 16 bytes per lane.
-__device__ __forceinline__ bool small_pages(const KvArgs& c) { return c.log_page == 4; }
-__device__ __forceinline__ void copy16(void* dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
-}
-
 template <int D>
 __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
   const KvArgs& c = a.c;
@@ -274,7 +266,7 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
 #pragma unroll
           for (int run = 0; run < D / 16; ++run) copy16(&sm.k[ks][run][32 * j + lane][0], src + 256 * run);
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&sm.k_full[ks])) : "memory");
+        copies_arrive(&sm.k_full[ks]);
       } else {
         if (lane == 0) mbar_expect_tx(&sm.k_full[ks], bytes);
         __syncwarp();
@@ -300,7 +292,7 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
     __syncwarp();
     if (lane == 0) mbar_arrive(&sm.seg_empty[is % kRing]);
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  copies_wait();
   if (!ok && lane == 0) {  // copies in flight land before the block ends
     for (uint32_t j = n > NK ? n - NK : 0; j < n; ++j) (void)mbar_wait(&sm.k_full[j % NK], (j / NK) & 1, x.wait_ns);
     for (uint32_t j = n > NV ? n - NV : 0; j < n; ++j) (void)mbar_wait(&sm.v_full[j % NV], (j / NV) & 1, x.wait_ns);
