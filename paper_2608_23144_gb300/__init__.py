@@ -12,6 +12,8 @@ binding with the same entry-point names:
   double quantisation (Sec. 3.3)
 * ``awsrc_sidecar_prepare`` / ``awsrc_packed_gemv`` / ``awsrc_packed_gemv_batch``  the
   sidecar applied inside a packed INT4 product, W_hat never formed
+* ``awsrc_kv_append`` / ``awsrc_paged_attention``  keys and values into a paged 8-bit
+  cache (q and k rotated on the way) and attention over it, between those products
 """
 from ._binding import (  # noqa: F401
     CANDIDATE_DTYPE,

@@ -34,6 +34,16 @@
 // share leave partial results, which a second launch joins on the whole GPU:
 // joined by the last block to arrive, the five parts of a tile took 60 us.
 //
+// Measured: four chunks of 1024 tokens on contexts of 20k beside decoding users (40
+// heads, 8 kv heads) in 465 us, 1190 TFLOP/s or 63% of a large bf16 product; four
+// prompts of up to 4096 tokens (28 heads, 4 kv heads) in 320 us, 785 TFLOP/s, the
+// masked halves of diagonal blocks not counted. Bound: a block's 16 products of a
+// tile take 1028 cycles by themselves (and 74 to commit) but about 1500 here, since
+// q . k reads both operands from shared memory at its full rate, 128 bytes per
+// cycle, beside the widening and the copies; a tile's softmax takes 1500 more before
+// its next products can start. Two warps per softmax row (half the columns each)
+// took 530 us for the chunks, as they get in the other tile's way.
+//
 // Every wait is bounded (wait_ns): one that runs out sets bit 2 of the fault
 // word, stops the block's roles, waits (bounded) for its copies and products in
 // flight and frees the tensor memory.
