@@ -370,6 +370,25 @@ __device__ __forceinline__ void widen(const uint4& v, uint32_t* f) {
   for (int i = 0; i < 4; ++i) widen4(w[i], f[2 * i], f[2 * i + 1]);
 }
 
+// A joining launch may be set up while the attention kernel before it ends: that
+// one's blocks all run at once and say so when they start, and the joining blocks
+// wait for its end and its writes before they read any.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename K>
+cudaError_t launch_join(K kernel, dim3 grid, int threads, const AttnArgs& a, cudaStream_t st) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 // Row tiles a batch can have at most.
 inline int64_t tiles_upper(const KvArgs& c, int tile_rows) {
   return (int64_t)c.n_tok * c.group / tile_rows + (c.n_seq < c.n_tok ? c.n_seq : c.n_tok);

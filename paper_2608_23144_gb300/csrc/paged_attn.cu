@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
   const bool feeds = wr == 0 && half == 0;  // the warp that copies for its token group
   const int log_pe = min(c.log_page, 6);  // tokens of a page within a block
 
+  let_next_start();
   {
     typename Mem::Walk w;
     const bool any = w.start(a);
@@ -675,6 +676,7 @@ __global__ void __launch_bounds__(256) paged_join_rows_kernel(const __grid_const
   constexpr int kP = 32 / kV;             // parts a warp takes at a time
   __shared__ float4 so[8][32];
   __shared__ float sl[8][32];
+  wait_for_previous();
   const SharedTile tile = a.shared[blockIdx.x];
   if ((int)blockIdx.y * RB >= tile.rows) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
@@ -732,7 +734,8 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   note_launches(1);
   if (join) {
     constexpr int kRows = Shape<NT, WR>::kRows, kRB = kRows <= 16 ? 1 : 8;
-    paged_join_rows_kernel<T, D, kRows, kRB><<<dim3((unsigned)grid, kRows / kRB), 256, 0, st>>>(b);
+    const cudaError_t j = launch_join(paged_join_rows_kernel<T, D, kRows, kRB>, dim3((unsigned)grid, kRows / kRB), 256, b, st);
+    if (j != cudaSuccess) return j;
     note_launches(1);
   }
   return cudaGetLastError();

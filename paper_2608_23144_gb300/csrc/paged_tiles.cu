@@ -744,6 +744,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_constant__ AttnArgs a) {
   extern __shared__ unsigned char smem_raw[];
   Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
+  let_next_start();
   Walk w;
   if (!w.start(a)) {
     if (threadIdx.x == 0) a.shared[blockIdx.x] = SharedTile{};
@@ -806,6 +807,7 @@ template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int kD = D / 8;
   __shared__ float rows[32][D + 1];
+  wait_for_previous();
   const SharedTile tile = a.shared[blockIdx.x];
   const int r0 = 32 * blockIdx.y;
   if (r0 >= tile.rows) return;
@@ -868,7 +870,8 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   paged_tiles_kernel<D><<<(unsigned)grid, kThreads, kSmem, st>>>(b);
   note_launches(1);
   if (grid > 1) {  // one block shares no tile
-    paged_join_kernel<D><<<dim3((unsigned)grid, kRows / 32), 256, 0, st>>>(b);
+    const cudaError_t j = launch_join(paged_join_kernel<D>, dim3((unsigned)grid, kRows / 32), 256, b, st);
+    if (j != cudaSuccess) return j;
     note_launches(1);
   }
   return cudaGetLastError();
