@@ -481,6 +481,8 @@ __device__ void rotate_q(const AppendArgs& a, int t, int part, int parts) {
 // with two 76, 8 (64 registers) 72; unrolling the jobs' loops cost 10 us.
 template <typename T, int D, int W, int JW>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 5) kv_append_kernel(const __grid_constant__ AppendArgs a) {
+  wait_for_previous();
+  let_next_start();
   // which kind, and the how many-th of it
   const int i = blockIdx.x, few = min(a.kv_blocks, a.q_blocks);
   const int nth = i / a.every, before = min(few, nth + (i % a.every != 0));  // blocks of the rarer kind up to i
@@ -513,12 +515,10 @@ cudaError_t launch(AppendArgs a, bool vec, int64_t visits, cudaStream_t st) {
   a.q_blocks = (int)q;
   a.every = (int)((kv + q) / (kv < q ? kv : q));
   const unsigned grid = (unsigned)(kv + q);
-  if (vec)
-    (warp ? kv_append_kernel<T, D, 8, 1> : kv_append_kernel<T, D, 8, 4>)<<<grid, kThreads, 0, st>>>(a);
-  else
-    (warp ? kv_append_kernel<T, D, 1, 1> : kv_append_kernel<T, D, 1, 4>)<<<grid, kThreads, 0, st>>>(a);
+  const auto kernel = vec ? (warp ? kv_append_kernel<T, D, 8, 1> : kv_append_kernel<T, D, 8, 4>)
+                          : (warp ? kv_append_kernel<T, D, 1, 1> : kv_append_kernel<T, D, 1, 4>);
   note_launches(1);
-  return cudaGetLastError();
+  return launch_next(kernel, dim3(grid), kThreads, 0, a, st);
 }
 
 }  // namespace

@@ -370,19 +370,21 @@ __device__ __forceinline__ void widen(const uint4& v, uint32_t* f) {
   for (int i = 0; i < 4; ++i) widen4(w[i], f[2 * i], f[2 * i + 1]);
 }
 
-// A joining launch may be set up while the attention kernel before it ends: that
-// one's blocks all run at once and say so when they start, and the joining blocks
-// wait for its end and its writes before they read any.
+// These kernels' launches are set up while the kernel before them in the stream
+// ends (append, attention and joining launch follow one another): every thread
+// first waits for that kernel's end and its writes, so nothing is read early. 1 to 3
+// us a call.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-template <typename K>
-cudaError_t launch_join(K kernel, dim3 grid, int threads, const AttnArgs& a, cudaStream_t st) {
+template <typename K, typename A>
+cudaError_t launch_next(K kernel, dim3 grid, int threads, size_t smem, const A& a, cudaStream_t st) {
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;

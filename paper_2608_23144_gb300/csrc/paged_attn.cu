@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
   const bool feeds = wr == 0 && half == 0;  // the warp that copies for its token group
   const int log_pe = min(c.log_page, 6);  // tokens of a page within a block
 
+  wait_for_previous();
   let_next_start();
   {
     typename Mem::Walk w;
@@ -730,11 +731,12 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   // launch joins all tiles on the whole GPU.
   const bool join = max_blocks / b.min_units > (Shape<NT, WR>::kRows > 16 ? 1 : kMaxParts);
   if (!join) b.shared = nullptr;
-  kernel<<<(unsigned)grid, Shape<NT, WR>::kThreads, sizeof(Mem), st>>>(b);
+  const cudaError_t k = launch_next(kernel, dim3((unsigned)grid), Shape<NT, WR>::kThreads, sizeof(Mem), b, st);
+  if (k != cudaSuccess) return k;
   note_launches(1);
   if (join) {
     constexpr int kRows = Shape<NT, WR>::kRows, kRB = kRows <= 16 ? 1 : 8;
-    const cudaError_t j = launch_join(paged_join_rows_kernel<T, D, kRows, kRB>, dim3((unsigned)grid, kRows / kRB), 256, b, st);
+    const cudaError_t j = launch_next(paged_join_rows_kernel<T, D, kRows, kRB>, dim3((unsigned)grid, kRows / kRB), 256, 0, b, st);
     if (j != cudaSuccess) return j;
     note_launches(1);
   }

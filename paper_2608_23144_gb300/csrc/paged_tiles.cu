@@ -744,6 +744,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1) paged_tiles_kernel(const __grid_constant__ AttnArgs a) {
   extern __shared__ unsigned char smem_raw[];
   Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
+  wait_for_previous();
   let_next_start();
   Walk w;
   if (!w.start(a)) {
@@ -867,10 +868,11 @@ cudaError_t launch(const AttnArgs& a, int64_t max_blocks, cudaStream_t st) {
   int64_t grid = kMaxTileBlocks;
   const int64_t most = tiles_upper(a.c, kRows) * a.c.kv_heads * max_blocks;
   if (grid > most) grid = most;
-  paged_tiles_kernel<D><<<(unsigned)grid, kThreads, kSmem, st>>>(b);
+  const cudaError_t k = launch_next(paged_tiles_kernel<D>, dim3((unsigned)grid), kThreads, kSmem, b, st);
+  if (k != cudaSuccess) return k;
   note_launches(1);
   if (grid > 1) {  // one block shares no tile
-    const cudaError_t j = launch_join(paged_join_kernel<D>, dim3((unsigned)grid, kRows / 32), 256, b, st);
+    const cudaError_t j = launch_next(paged_join_kernel<D>, dim3((unsigned)grid, kRows / 32), 256, 0, b, st);
     if (j != cudaSuccess) return j;
     note_launches(1);
   }
