@@ -40,7 +40,7 @@
 //
 // Measured: 64 ragged decode steps on contexts up to 8192 (28 heads, 4 kv heads,
 // bf16) in 66 us, 5.2 TB/s of the cache; one on 131k tokens (40 heads, 8 kv heads,
-// float32) in 58 us, 4.6 TB/s. In the loop the copies keep up with the memory;
+// float32) in 56 us, 4.8 TB/s. In the loop the copies keep up with the memory;
 // what is lost are the starts of blocks and the ends of segments (a tenth each) and,
 // in float32, the second terms' products. Many float32 rows are bound by the
 // warp-level MMAs, whose rate is a third of the fifth-generation cores': four
@@ -48,7 +48,10 @@
 //
 // Rounding: q (bf16: exact; float32: 22 bits), p (11 bits, float32: 22) and the
 // widened codes (exact) to binary16; scores, m, l, O and the joins in binary32; out
-// once.
+// once. An MMA cuts its binary32 sums off instead of rounding them, so q's second
+// terms have sums of their own, and a float32 weight gets its 2^15 after the power,
+// whose argument near zero keeps its last bits: together 8.5e-7 -> 4e-7 of the
+// result for a token on 516.
 #include "internal.h"
 #include "kv_paged.cuh"
 #include "tc05.cuh"
@@ -61,7 +64,7 @@ using namespace tc05;
 
 constexpr int kUnit = 64;         // tokens per unit
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kPBits = 15.0f;   // p is at most 2^15
+constexpr float kPBits = 15.0f, kPMax = 32768.0f;  // p is at most 2^15
 constexpr int kMaxParts = 8;      // parts of a tile that its last block joins
 
 __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -402,14 +405,14 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
       const int ks = nk % Mem::NK;
       wait(&sm.k_full[wt][ks], (nk / Mem::NK) & 1);
       ++nk;
-      float x[NT][kT][4];
+      float x[NT][kT][4], xl[NT][kT][4];  // of q's first and second terms
       const uint8_t* kb = sm.k[wt][ks] + (4 * (g >> 1) + (g & 1)) * 16 + 4 * t4;
 #pragma unroll
       for (int i = 0; i < kT; ++i)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[nt][i][j] = 0.0f;
+          for (int j = 0; j < 4; ++j) x[nt][i][j] = 0.0f, xl[nt][i][j] = 0.0f;
       const uint8_t* kp = kb + kT * half * 256;  // row tile i: 16 rows of 16 bytes further
       auto key = [&](int i, int run, int row) {
         return *reinterpret_cast<const uint32_t*>(kp + i * 256 + run * (kUnit * 16) + row * 16);
@@ -428,7 +431,15 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < kT; ++i) mma(x[nt][i], fr[i], qf[nt][q][2 * j], qf[nt][q][2 * j + 1]);
+            for (int i = 0; i < kT; ++i) mma(q == 0 ? x[nt][i] : xl[nt][i], fr[i], qf[nt][q][2 * j], qf[nt][q][2 * j + 1]);
+      }
+      if constexpr (kSplit) {
+#pragma unroll
+        for (int i = 0; i < kT; ++i)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[nt][i][j] = __fadd_rn(x[nt][i][j], xl[nt][i][j]);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.k_empty[wt][ks]);
@@ -474,7 +485,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
           const float bs = mn == -INFINITY ? 0.0f : mn;
           al[q] = ex2(__fsub_rn(m[nt][q], bs));
           m[nt][q] = mn;
-          base[q] = __fsub_rn(bs, kPBits);
+          base[q] = kSplit ? bs : __fsub_rn(bs, kPBits);
           l[nt][q] = __fmul_rn(l[nt][q], al[q]);
         }
         if (__any_sync(0xffffffffu, al[0] != 1.0f || al[1] != 1.0f)) {  // a maximum moved
@@ -489,7 +500,8 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
           const float un = pow2f(ev == kExpNan ? 0 : -ev);
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
-            const float p0 = ex2(__fsub_rn(x[nt][i][2 * hf], base[0])), p1 = ex2(__fsub_rn(x[nt][i][2 * hf + 1], base[1]));
+            float p0 = ex2(__fsub_rn(x[nt][i][2 * hf], base[0])), p1 = ex2(__fsub_rn(x[nt][i][2 * hf + 1], base[1]));
+            if constexpr (kSplit) p0 = __fmul_rn(p0, kPMax), p1 = __fmul_rn(p1, kPMax);
             l[nt][0] = __fmaf_rn(p0, un, l[nt][0]);
             l[nt][1] = __fmaf_rn(p1, un, l[nt][1]);
             const uint32_t hi = half2_bits(p0, p1);

@@ -36,7 +36,7 @@
 //
 // Measured: four chunks of 1024 tokens on contexts of 20k beside decoding users (40
 // heads, 8 kv heads) in 465 us, 1190 TFLOP/s or 63% of a large bf16 product; four
-// prompts of up to 4096 tokens (28 heads, 4 kv heads) in 320 us, 785 TFLOP/s, the
+// prompts of up to 4096 tokens (28 heads, 4 kv heads) in 315 us, 800 TFLOP/s, the
 // masked halves of diagonal blocks not counted. Bound: a block's 16 products of a
 // tile take 1028 cycles by themselves (and 74 to commit) but about 1500 here, since
 // q . k reads both operands from shared memory at its full rate, 128 bytes per
