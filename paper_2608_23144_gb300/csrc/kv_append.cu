@@ -14,9 +14,9 @@
 // each waited for the one before. Pages are found by a block-wide scan over the
 // sequences, so the launch follows device-side lengths.
 //
-// Measured: 13k new tokens of 40 query and 8 kv heads (bf16, pages of 16) in 70 us,
-// 4.9 TB/s of what it has to move; 8k tokens of 28 and 4 heads (pages of 64) in 34
-// us, 4.5 TB/s. What is left is latency: a warp's loads (lengths, page, tables,
+// Measured: 13k new tokens of 40 query and 8 kv heads (bf16, pages of 16) in 69 us,
+// 4.9 TB/s of what it has to move; 8k tokens of 28 and 4 heads (pages of 64) in 33
+// us, 4.7 TB/s. What is left is latency: a warp's loads (lengths, page, tables,
 // rows) follow from one another, and 64 registers leave 32 warps an SM. One token:
 // 3 us.
 //

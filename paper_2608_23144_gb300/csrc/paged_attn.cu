@@ -39,8 +39,8 @@
 // second launch; nothing waits.
 //
 // Measured: 64 ragged decode steps on contexts up to 8192 (28 heads, 4 kv heads,
-// bf16) in 66 us, 5.2 TB/s of the cache; one on 131k tokens (40 heads, 8 kv heads,
-// float32) in 56 us, 4.8 TB/s. In the loop the copies keep up with the memory;
+// bf16) in 64 us, 5.4 TB/s of the cache; one on 131k tokens (40 heads, 8 kv heads,
+// float32) in 55 us, 4.9 TB/s. In the loop the copies keep up with the memory;
 // what is lost are the starts of blocks and the ends of segments (a tenth each) and,
 // in float32, the second terms' products. Many float32 rows are bound by the
 // warp-level MMAs, whose rate is a third of the fifth-generation cores': four
