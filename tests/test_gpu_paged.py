@@ -444,3 +444,43 @@ def test_waits_of_the_row_kernel_that_run_out_are_reported(aw, dtype, new):
         finally:
             aw.awsrc_set_wait_test()
     check_attention(aw, cache, q, [new], [70000], table, True)
+
+
+def test_graphs_with_copies_and_fills_between_the_calls(aw):
+    """A captured step whose inputs are copied and outputs cleared right before each call: the calls' launches, which are
+    set up early behind another kernel, wait for such nodes too. The replays give what the calls gave one by one."""
+    gen = torch.Generator().manual_seed(14)
+    new, kv = [1, 3, 0, 1], [700, 90, 5, 64]
+    _, table, pages = make_batch(aw, gen, new, kv, 16)
+    batch = step_batch(aw, new, kv, table)
+    caches = [random_cache(aw, torch.Generator().manual_seed(15), pages, 2, 128, 16) for _ in range(2)]
+    ws = [aw.awsrc_attention_workspace(c, 4) for c in caches]
+    n = sum(new)
+    src = [torch.randn(n, h, 128, generator=gen).to(BF16).cuda() for h in (4, 2, 2)]
+    cos, sin = (t.cuda() for t in tables(800, 64, gen))
+    q, k, v = (torch.empty_like(t) for t in src)
+    out, lse = torch.empty_like(q), torch.empty(n, 4, device="cuda")
+
+    def step(i):
+        for a, b in zip((q, k, v), src):
+            a.copy_(b)
+        aw.awsrc_kv_append(caches[i], batch, q, k, v, cos, sin, ws[i], q_out=q)
+        out.zero_()
+        lse.zero_()
+        aw.awsrc_paged_attention(caches[i], batch, q, ws[i], out=out, lse=lse)
+
+    step(0)
+    want = [t.clone() for t in (q, out, lse)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step(1)
+    for _ in range(3):
+        for t in (q, k, v, out, lse):
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((q, out, lse), want))
+    assert aw.awsrc_workspace_status(ws[1]) == 0
