@@ -592,8 +592,10 @@ awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const awsrc_kv_batch* 
  *   q, out   [n_tok][n_heads], the same dtype (out must not overlap q).
  *   lse      device, n_tok x n_heads floats, or NULL.
  * F32 keeps q and the softmax weights in two binary16 terms (22 bits) each and
- * sums in binary32. BF16 keeps q exact and the weights in 8 bits or more; out is
- * rounded once. Sums run in a fixed order: results repeat bit for bit.
+ * sums in binary32. BF16 keeps q exact (calls of max_new * n_heads / n_kv_heads
+ * > 16 rows and 16-byte aligned q and out: but for elements below 2^-13 of their
+ * row's largest, which they keep to 2^-21 of that) and the weights in 8 bits or
+ * more; out is rounded once. Sums run in a fixed order: results repeat bit for bit.
  * Visible tokens' codes must be finite (awsrc_kv_append writes no e4m3 NaN);
  * the bytes of rows past kv_len may be anything. Two launches at most.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA.

@@ -8,9 +8,17 @@
 //
 // Precision at the cost of one 16-bit product each:
 //   q . k   kind::f8f6f4 on the key codes as they lie in the cache; q, scaled by
-//           a power of two per row, is split into two e4m3 terms, which hold the
-//           8 significant bits of a bf16 (two 8-bit products cost what one
-//           16-bit product costs; no key is ever converted);
+//           a power of two per row to a largest element in [2^7, 2^8), is split into
+//           an e4m3 term and an e5m2 one (two 8-bit products cost what one 16-bit
+//           product costs; no key is ever converted). Beside the 4 bits of the first
+//           a bf16 leaves at most 8 signed units, which e5m2 holds: elements from 2^-6
+//           on are exact, smaller ones, whose first term is subnormal, within 2^-14
+//           (all bf16 values tried). Of a row's largest element that is 2^-13 and
+//           2^-21. An e4m3 second term ended at 2^-9: it lost bits from 2^-9 of the
+//           largest element down and kept 2^-17. q in binary16 beside keys widened
+//           like the values would be exact to 2^-39, and took 7% (four prompts) to
+//           16% (chunks) longer: the widened keys' stores compete with the products
+//           for shared memory;
 //   p . V   kind::f16 with p in binary16 (from tensor memory) and the value
 //           codes widened to binary16, exactly, by four warps. Splitting p into
 //           8-bit terms instead would cost the softmax warps two more
@@ -73,10 +81,11 @@ using Walk = UnitWalk<kRows, BN, 4, kOver>;
 
 template <int N>
 struct Idesc { static constexpr uint32_t value = idesc_f16(BM, N); };  // formats 0: e4m3, binary16
+constexpr uint32_t kIdescAE5M2 = 1u << 7;  // format 1 of A in kind::f8f6f4
 
 template <int D>
 struct Smem {
-  uint8_t q[2][2][D / 16][BM + 1][16];  // tile, term, 16 dims; runs one row apart in the banks
+  uint8_t q[2][2][D / 16][BM + 1][16];  // tile, term (e4m3, e5m2), 16 dims; runs one row apart in the banks
   uint8_t k[NK][D / 16][BN][16];
   uint8_t v[NV][BN / 16][D][16];
   uint8_t w[NW][BN / 8][D][16];     // binary16, 8 tokens
@@ -130,7 +139,7 @@ __device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t kbytes) {
          (1ull << 46);
 }
 
-// D(tmem) (+)= A(smem, e4m3) B(smem, e4m3), 32 deep.
+// D(tmem) (+)= A(smem, e4m3 or e5m2) B(smem, e4m3), 32 deep.
 __device__ __forceinline__ void umma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -335,7 +344,8 @@ __device__ void mma_role(Smem<D>& sm, const Ctx& x, int t, bool small) {
     const uint64_t kd = k0 + (uint64_t)(blk % NK) * (sizeof(sm.k[0]) >> 4);
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)  // both terms: 32 dims a step, 2 runs of 16 further each
-      umma_f8(ts, q0 + s * (2 * (BM + 1) * 16 >> 4), kd + (s & (D / 32 - 1)) * (2 * BN * 16 >> 4), kIdescS, s > 0);
+      umma_f8(ts, q0 + s * (2 * (BM + 1) * 16 >> 4), kd + (s & (D / 32 - 1)) * (2 * BN * 16 >> 4),
+              s < D / 32 ? kIdescS : kIdescS | kIdescAE5M2, s > 0);
     umma_commit(&sm.s_full[t]);
   };
   bool ok = true, held = false;  // held: the widened values of block n - 1 are not given back yet
@@ -449,7 +459,13 @@ __device__ __forceinline__ uint32_t e4m3x2_h(__half2 v) {
   return r;
 }
 
-// The warp's 32 query rows of tile t -> two e4m3 terms in shared memory; returns
+__device__ __forceinline__ uint32_t e5m2x2_h(__half2 v) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t*>(&v)));
+  return r;
+}
+
+// The warp's 32 query rows of tile t -> two 8-bit terms in shared memory; returns
 // the multiplier of the scores of row 32 (warp % 4) + lane. Consecutive lanes
 // read consecutive dims of a row (8 each), loads of the next
 // rows in flight.
@@ -501,7 +517,7 @@ __device__ __noinline__ float stage_q(const AttnArgs& a, Smem<D>& sm, int t, con
                                             __fmul_rn(__uint_as_float(w[j] & 0xFFFF0000u), f));
         hi[j] = e4m3x2_h(y);
         const uint32_t back = e4m3x2_half2(hi[j]);
-        lo[j] = e4m3x2_h(__hsub2(y, *reinterpret_cast<const __half2*>(&back)));
+        lo[j] = e5m2x2_h(__hsub2(y, *reinterpret_cast<const __half2*>(&back)));
       }
       const int r = r0 + kPer * (i0 + b) + lane / kLanes;
       *reinterpret_cast<uint2*>(&sm.q[t][0][sub >> 1][r][8 * (sub & 1)]) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);

@@ -1,0 +1,52 @@
+"""The paged cache over the ranges of its inputs: what queries, marks, scales and
+batches may hold, beside the sizes of test_gpu_paged.py. The references and the
+derived bounds are those of paged_ref.py."""
+import pytest
+import torch
+
+import paged_ref as ref
+from test_gpu_paged import BF16, F32, aw, check_attention, make_batch, random_cache, step_batch, tables  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ queries
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(6, 2, 128), (3, 3, 64)])
+@pytest.mark.parametrize("new", [1, 40, 300])
+@pytest.mark.parametrize("ratio", [2.0 ** 8, 2.0 ** 11, 2.0 ** 14])
+def test_a_query_channel_far_above_the_others(aw, dtype, heads, kv_heads, dim, new, ratio):  # noqa: F811
+    """One dim of every query is `ratio` times the others and meets keys of zero there, so that the scores come from the
+    small dims alone. The bounds of paged_ref.py take q as exact (BF16) or to 2^-22 of each element (float32). BF16 with
+    more than 16 rows per kv head adds an error of 2^-21 of a row's largest element for elements below 2^-13 of it: dx
+    in a score, so dx (relative) in the softmax sum and 2 dx sum_j p_j |v_j| in out."""
+    gen = torch.Generator().manual_seed(20)
+    kv = [max(new, 333)]
+    _, table, pages = make_batch(aw, gen, [new], kv, 32)
+    cache = random_cache(aw, gen, pages, kv_heads, dim, 32)
+    cache.k.view(torch.uint8)[:, :, 2, :, 5] = 0  # dim 37
+    q = torch.randn(new, heads, dim, generator=gen)
+    q[..., 37] = torch.where(q[..., 37] < 0, -ratio, ratio)
+    q = q.to(dtype)
+    if dtype == F32 or new * heads // kv_heads <= 16:
+        check_attention(aw, cache, q, [new], kv, table, True)
+        return
+    c = ref.Cache.of(cache)
+    want, wl, ob, lb = ref.attention(c, q, [new], kv, table, dim ** -0.5, True, 0.0, 2.0 ** -9)
+    x = q.double().abs()
+    top = x.amax(-1, keepdim=True)
+    small = torch.where(x < top * 2.0 ** -13, top * 2.0 ** -21, 0.0)
+    used = [int(p) for p in table[0][:-(-kv[0] // 32)]]
+    for h in range(heads):
+        k, v = (c.values(w, used, h // (heads // kv_heads), kv[0]) for w in "kv")
+        hide = torch.arange(kv[0])[None] > (kv[0] - new + torch.arange(new))[:, None]
+        dx = (small[:, h] @ k.abs().T * dim ** -0.5).masked_fill(hide, 0.0).amax(1)
+        p = torch.softmax((q[:, h].double() @ k.T * dim ** -0.5).masked_fill(hide, -torch.inf), 1)
+        ob[:, h] += 2 * dx[:, None] * (p @ v.abs())
+        lb[:, h] += dx
+    lse = torch.empty(new, heads, device="cuda")
+    out = aw.awsrc_paged_attention(cache, step_batch(aw, [new], kv, table), q.cuda(),
+                                   aw.awsrc_attention_workspace(cache, heads), lse=lse).cpu().double()
+    assert ((out - want).abs() <= ob + (want.abs() + ob) * 2.0 ** -9).all()  # out is rounded once
+    assert ((lse.cpu().double() - wl).abs() <= lb).all()
