@@ -588,7 +588,9 @@ awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const awsrc_kv_batch* 
  * + i) and query head h, over the cached tokens j of kv head
  * h / (n_heads / n_kv_heads): s_j = sm_scale * q . k_j for j < kv_len and, when
  * causal, j <= p; out = sum_j softmax(s)_j v_j, lse = log sum_j exp(s_j). A query
- * that sees no token gets out = 0, lse = -inf.
+ * that sees no token gets out = 0, lse = -inf. Keys of a block whose exponent is
+ * -128 make the scores of its tokens NaN, so out and lse of the queries that see
+ * one; values of such a block make out NaN, lse stays that of the scores.
  *   q, out   [n_tok][n_heads], the same dtype (out must not overlap q).
  *   lse      device, n_tok x n_heads floats, or NULL.
  * F32 keeps q and the softmax weights in two binary16 terms (22 bits) each and

@@ -449,13 +449,13 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
       uint32_t pf[NT][kTerms][2 * kT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float mx[2] = {-INFINITY, -INFINITY};
+        float mx[2] = {-INFINITY, -INFINITY}, out[2] = {1.0f, 1.0f};
 #pragma unroll
         for (int i = 0; i < kT; ++i) {
           const int gi = kT * half + i;
           const int ek = __shfl_sync(0xffffffffu, cur.ek, gi), ev = __shfl_sync(0xffffffffu, cur.ev, gi);
           const int have = __shfl_sync(0xffffffffu, cur.have, gi);
-          const float sk = pow2f(ek), ef = ek == kExpNan || ev == kExpNan ? nan : (float)ev;
+          const float sk = pow2f(ek), ef = ek == kExpNan ? nan : (ev == kExpNan ? 0.0f : (float)ev);
           const int j0 = blk * kUnit + 16 * gi + 4 * (g >> 1) + (g & 1);
           const int end = blk * kUnit + 16 * gi + have;
 #pragma unroll
@@ -472,6 +472,12 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
 #pragma unroll
               for (int hf = 0; hf < 2; ++hf)
                 if (j0 + 2 * hf >= end || j0 + 2 * hf > lim[nt][q]) x[nt][i][2 * hf + q] = -INFINITY;
+            // a row that sees marked values: O is NaN, the scores and l are what they are
+            if (ev == kExpNan) {
+#pragma unroll
+              for (int q = 0; q < 2; ++q)
+                if (blk * kUnit + 16 * gi <= lim[nt][q]) out[q] = nan;
+            }
           }
 #pragma unroll
           for (int q = 0; q < 2; ++q) mx[q] = fmaxf(mx[q], fmaxf(x[nt][i][q], x[nt][i][2 + q]));
@@ -487,6 +493,7 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
           m[nt][q] = mn;
           base[q] = kSplit ? bs : __fsub_rn(bs, kPBits);
           l[nt][q] = __fmul_rn(l[nt][q], al[q]);
+          al[q] = __fmul_rn(al[q], out[q]);
         }
         if (__any_sync(0xffffffffu, al[0] != 1.0f || al[1] != 1.0f)) {  // a maximum moved
 #pragma unroll

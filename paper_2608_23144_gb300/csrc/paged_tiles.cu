@@ -94,6 +94,7 @@ struct Smem {
   unsigned long long seg_full[kRing], seg_empty[kRing];
   SegRec seg[kRing];
   float4 group_of[8][2][8];  // softmax warp, block parity: scale of the keys, exponent and unscaling of the values, -
+  uint8_t bad[kRows];        // the row sees marked values
   uint32_t tmem;
   int dead;
 };
@@ -567,11 +568,16 @@ __device__ __noinline__ bool finish_tile(const AttnArgs& a, Smem<D>& sm, const C
   float* slot = partial_slot(a, blockIdx.x, cs.c0) + (int64_t)t * BM * (D + 2) + r;
   __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(cs.first + tok) * a.out.ts + (int64_t)head * a.out.hs;
   const float inv = l == 0.0f ? 0.0f : __frcp_rn(l);
+  const bool bad = sm.bad[t * BM + r];
 #pragma unroll 1
   for (int q = 0; q < D / 16; ++q) {
     float v[16];
     tmem_ld16(to + 16 * q, v);
     tmem_wait_ld(v);
+    if (bad) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = __int_as_float(0x7FC00000);
+    }
     if (have && cs.whole) {
       put16(op + 16 * q, v, inv);
     } else if (have) {
@@ -637,20 +643,24 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) lim_min = min(lim_min, __shfl_xor_sync(0xffffffffu, lim_min, o));
     float m = -INFINITY, l = 0.0f;
+    sm.bad[threadIdx.x] = 0;
     Groups g = load_groups(c, table, kv, h, cs.blk0);
     for (int blk = cs.blk0; blk < blk1; ++blk) {
       const Groups cur = g;
       if (blk + 1 < blk1) g = load_groups(c, table, kv, h, blk + 1);
       // lane i < 8: the scale of group i's keys, the exponent and unscaling of its values, its tokens
-      const bool mark = cur.ek == kExpNan || cur.ev == kExpNan;
+      const bool mark = cur.ek == kExpNan, mark_v = cur.ev == kExpNan;
       const bool masked = blk * BN + BN - 1 > lim_min || __any_sync(0xffffffffu, lane < 8 && (cur.have < 16 || mark));
+      // marked values: O will be NaN for the rows that see one, the scores and l are what they are
+      const uint32_t bad_groups = __ballot_sync(0xffffffffu, mark_v);
+      if (bad_groups && lim >= blk * BN + 16 * (__ffs(bad_groups) - 1)) sm.bad[threadIdx.x] = 1;
       float4* gc = sm.group_of[warp][blk & 1];
       if (lane < 8)
-        gc[lane] = make_float4(mark ? 1.0f : pow2f(cur.ek), mark ? 0.0f : (float)cur.ev, mark ? 1.0f : pow2f(-cur.ev), 0.0f);
+        gc[lane] = make_float4(mark ? 1.0f : pow2f(cur.ek), mark_v ? 0.0f : (float)cur.ev, mark_v ? 1.0f : pow2f(-cur.ev), 0.0f);
       __syncwarp();
       if (!wait_warp(x, &sm.s_full[t], ns++ & 1)) return;
       tc_fence_after();
-      if (masked) {  // hidden tokens to -inf, visible ones of a marked block to NaN, in place
+      if (masked) {  // hidden tokens to -inf, visible ones of marked keys to NaN, in place
         const int col = lim == INT32_MAX ? BN : lim - blk * BN;  // last column this row sees
 #pragma unroll 1
         for (int i = 0; i < 8; ++i) {

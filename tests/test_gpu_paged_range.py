@@ -50,3 +50,38 @@ def test_a_query_channel_far_above_the_others(aw, dtype, heads, kv_heads, dim, n
                                    aw.awsrc_attention_workspace(cache, heads), lse=lse).cpu().double()
     assert ((out - want).abs() <= ob + (want.abs() + ob) * 2.0 ** -9).all()  # out is rounded once
     assert ((lse.cpu().double() - wl).abs() <= lb).all()
+
+
+# -------------------------------------------------------------------- marks
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new,kv,page", [(1, 300, 16), (40, 300, 16), (40, 300, 64), (1, 9000, 32), (40, 9000, 128)])
+def test_marked_blocks(aw, dtype, which, dim, new, kv, page):  # noqa: F811
+    """A block marked as not finite reaches the queries and heads that see it, and no others. Marked keys: scores, so out
+    and lse, are NaN. Marked values: out is NaN, but the scores and lse are what they were."""
+    gen = torch.Generator().manual_seed(21)
+    _, table, pages = make_batch(aw, gen, [new], [kv], page)
+    cache = random_cache(aw, gen, pages, 2, dim, page)
+    slot = (kv - 20) // page  # some of 40 queries end before it (pages of 16), some do not
+    pg = int(table[0, slot])
+    q = torch.randn(new, 6, dim, generator=gen).to(dtype)
+    ws = aw.awsrc_attention_workspace(cache, 6)
+    batch = step_batch(aw, [new], [kv], table)
+    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else (0.0, 2.0 ** -9)
+    want, wl, ob, lb = ref.attention(ref.Cache.of(cache), q, [new], [kv], table, dim ** -0.5, True, *eps)
+    if dtype == BF16:
+        ob = ob + (want.abs() + ob) * 2.0 ** -9
+    (cache.k_exp if which == "k" else cache.v_exp)[pg, 1] = -128
+    lse = torch.empty(new, 6, device="cuda")
+    out = aw.awsrc_paged_attention(cache, batch, q.cuda(), ws, lse=lse).cpu().double()
+    lse = lse.cpu().double()
+    assert aw.awsrc_workspace_status(ws) == 0
+    hit = (torch.arange(kv - new, kv) >= slot * page)[:, None] & (torch.arange(6) >= 3)[None]
+    assert torch.equal(torch.isnan(out).all(-1), hit) and torch.equal(torch.isnan(out).any(-1), hit)
+    assert ((out - want).abs() <= ob + 1e-30)[~hit].all()
+    if which == "k":
+        assert torch.equal(torch.isnan(lse), hit)
+    ok = ~hit if which == "k" else torch.ones_like(hit)
+    assert ((lse - wl).abs() <= lb)[ok].all()
