@@ -194,7 +194,8 @@ __device__ __forceinline__ void put_key(uint8_t* blk, int log_page, int row, int
 }
 
 // The sequence and page of visit number `visit` (pages that get new tokens,
-// counted over the sequences in order). False past the last one.
+// counted over the sequences in order). False past the last one. Visit 0 looks at
+// all sequences and reports the entries that cannot be right.
 __device__ __forceinline__ bool find_visit(const KvArgs& a, int visit, int* seq, int* nth) {
   __shared__ int wsum[kWarps], found[2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -228,7 +229,7 @@ __device__ __forceinline__ bool find_visit(const KvArgs& a, int visit, int* seq,
     }
     __syncthreads();
     before += all;
-    if (visit < before) break;
+    if (visit > 0 && visit < before) break;
   }
   *seq = found[0];
   *nth = found[1];

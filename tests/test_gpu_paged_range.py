@@ -85,3 +85,46 @@ def test_marked_blocks(aw, dtype, which, dim, new, kv, page):  # noqa: F811
         assert torch.equal(torch.isnan(lse), hit)
     ok = ~hit if which == "k" else torch.ones_like(hit)
     assert ((lse - wl).abs() <= lb)[ok].all()
+
+
+# ------------------------------------------------------------------ batches
+
+@pytest.mark.parametrize("n_seq,at", [(20, 17), (130, 128), (300, 290)])
+@pytest.mark.parametrize("kind", ["negative length", "length beyond the table", "falling start"])
+def test_append_reports_every_entry_that_cannot_be_right(aw, n_seq, at, kind):  # noqa: F811
+    """Bad entries without rows of their own, in any place of the batch; the sequences that overlap no bad entry's rows
+    get what they get without it."""
+    gen = torch.Generator().manual_seed(22)
+    page, heads, dim = 16, 2, 64
+    new, kv = [2] * n_seq, [37] * n_seq
+    new[at] = 0
+    _, table, pages = make_batch(aw, gen, new, kv, page)
+    base = random_cache(aw, gen, pages, heads, dim, page)
+    n = sum(new)
+    x = torch.randn(3, n, heads, dim, generator=gen).cuda()
+    start = [sum(new[:b]) for b in range(n_seq + 1)]
+
+    def run(start, kv):
+        c = aw.awsrc_kv_cache(*(b.clone() for b in (base.k, base.v, base.k_exp, base.v_exp)))
+        ws = aw.awsrc_attention_workspace(c, heads)
+        batch = aw.awsrc_kv_batch(torch.tensor(start, dtype=torch.int32).cuda(), torch.tensor(kv, dtype=torch.int32).cuda(),
+                                  table.cuda(), n, 4, 48)
+        aw.awsrc_kv_append(c, batch, *x, None, None, ws)
+        return c, aw.awsrc_workspace_status(ws)
+
+    good, flags = run(start, kv)
+    assert flags == 0
+    start, kv = list(start), list(kv)
+    if kind == "negative length":
+        kv[at] = -1
+    elif kind == "length beyond the table":
+        kv[at] = page * table.shape[1] + 1
+    else:  # entry `at` ends before it starts, so that the one behind it takes two rows of the one before it
+        start[at + 1] -= 2
+    got, flags = run(start, kv)
+    assert flags == 8
+    same = [b for b in range(n_seq) if b not in (at, at + 1)]
+    pg = table[same].long().cuda().flatten()
+    for a, b in ((got.k, good.k), (got.v, good.v)):
+        assert torch.equal(a.view(torch.uint8)[pg], b.view(torch.uint8)[pg])
+    assert torch.equal(got.k_exp[pg], good.k_exp[pg]) and torch.equal(got.v_exp[pg], good.v_exp[pg])
