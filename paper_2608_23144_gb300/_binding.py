@@ -554,7 +554,9 @@ def awsrc_decode_apply_inplace_noalloc(prm: Params, modules, stream_bytes: torch
 
 def awsrc_workspace_status(workspace: torch.Tensor, stream=None) -> int:
     flags = ct.c_uint32()
-    _check(lib.awsrc_workspace_status(_dev_ptr(workspace), _stream(stream), ct.byref(flags)), "workspace_status")
+    ptr = _dev_ptr(workspace)
+    with torch.cuda.device(workspace.device):
+        _check(lib.awsrc_workspace_status(ptr, _stream(stream), ct.byref(flags)), "workspace_status")
     return flags.value
 
 

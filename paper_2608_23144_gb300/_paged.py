@@ -16,8 +16,20 @@ from ._binding import _stream as _stream_of
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
+_current_device = torch._C._cuda_getDevice
+
+
 def _stream(stream, device: torch.device) -> int:
     return _raw_stream(device.index) if stream is None else _stream_of(stream)
+
+
+def _on(device: torch.device, call, *args) -> int:
+    """call(*args) with `device` current: the library launches on the current
+    device, and the default stream's handle does not name one."""
+    if _current_device() == device.index:
+        return call(*args)
+    with torch.cuda.device(device):
+        return call(*args)
 
 
 PAGE_SIZES = (16, 32, 64, 128)
@@ -143,8 +155,8 @@ def awsrc_attention_workspace(cache: KvCache, n_heads: int, stream=None) -> torc
     n = ct.c_size_t()
     _check(lib.awsrc_attention_workspace_bytes(cache._ref, n_heads, ct.byref(n)), "attention_workspace_bytes")
     ws = torch.empty(n.value, dtype=torch.uint8, device=cache.device)
-    _check(lib.awsrc_attention_workspace_init(cache._ref, n_heads, ws.data_ptr(), n.value,
-                                              _stream(stream, ws.device)),
+    _check(_on(ws.device, lib.awsrc_attention_workspace_init, cache._ref, n_heads, ws.data_ptr(), n.value,
+               _stream(stream, ws.device)),
            "attention_workspace_init")
     return ws
 
@@ -214,8 +226,8 @@ def awsrc_kv_append(cache: KvCache, batch: KvBatch, q: torch.Tensor, k: torch.Te
         if not (cos.is_contiguous() and sin.is_contiguous()):
             raise ValueError("cos and sin must be contiguous")
         cp, sp, (rows, half) = cos.data_ptr(), sin.data_ptr(), cos.shape
-    st = lib.awsrc_kv_append(cache._ref, batch._ref, shape[1], rq, rk, rv, ro, cp, sp, rows, 2 * half, bool(interleaved),
-                             workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
+    st = _on(dev, lib.awsrc_kv_append, cache._ref, batch._ref, shape[1], rq, rk, rv, ro, cp, sp, rows, 2 * half,
+             bool(interleaved), workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
     if st:
         _check(st, "kv_append")
     return q_out
@@ -241,9 +253,9 @@ def awsrc_paged_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, works
         if not lse.is_contiguous():
             raise ValueError("lse must be contiguous")
         lp = lse.data_ptr()
-    st = lib.awsrc_paged_attention(cache._ref, batch._ref, shape[1], rq, ro, lp,
-                                   shape[2] ** -0.5 if sm_scale is None else sm_scale, bool(causal),
-                                   workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
+    st = _on(dev, lib.awsrc_paged_attention, cache._ref, batch._ref, shape[1], rq, ro, lp,
+             shape[2] ** -0.5 if sm_scale is None else sm_scale, bool(causal), workspace.data_ptr(), workspace.numel(),
+             _stream(stream, dev))
     if st:
         _check(st, "paged_attention")
     return out
