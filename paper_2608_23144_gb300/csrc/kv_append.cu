@@ -281,7 +281,7 @@ __device__ void append_job(const AppendArgs& a, int b, int nth, int head, bool k
   const int P = 1 << c.log_page;
   const int first = s.kv - s.n;  // position of the first new token
   const int slot = (first >> c.log_page) + nth;
-  const int pg = __ldg(c.table + (int64_t)b * c.table_stride + slot);
+  const int pg = c.table[(int64_t)b * c.table_stride + slot];
   const int row0 = nth == 0 ? first & (P - 1) : 0;
   const int p0 = (slot << c.log_page) + row0;
   const int row1 = min(P, row0 + s.kv - p0);
@@ -414,7 +414,7 @@ __device__ void rotate_q(const AppendArgs& a, int t, int part, int parts) {
   // its sequence: the last one that starts at or before t
   int b = -1;
   for (int base = 0; base < c.n_seq; base += 32) {
-    const bool le = base + lane < c.n_seq && __ldg(c.q_start + base + lane) <= t;
+    const bool le = base + lane < c.n_seq && c.q_start[base + lane] <= t;
     const unsigned m = __ballot_sync(0xffffffffu, le);
     if (m) b = base + 31 - __clz(m);
     if (m != 0xffffffffu) break;  // starts do not fall in a batch that can be right

@@ -39,7 +39,7 @@ struct KvSeq {
 };
 
 __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int b) {
-  const int q0 = __ldg(a.q_start + b), q1 = __ldg(a.q_start + b + 1), kv = __ldg(a.kv_len + b);
+  const int q0 = a.q_start[b], q1 = a.q_start[b + 1], kv = a.kv_len[b];
   const bool ok = q0 >= 0 && q0 <= q1 && q1 <= a.n_tok && kv >= q1 - q0 &&
                   (int64_t)kv <= ((int64_t)a.table_stride << a.log_page);
   return KvSeq{q0, ok ? q1 - q0 : -1, ok ? kv : 0};
@@ -373,7 +373,8 @@ __device__ __forceinline__ void widen(const uint4& v, uint32_t* f) {
 // These kernels' launches are set up while the kernel before them in the stream
 // ends (append, attention and joining launch follow one another): every thread
 // first waits for that kernel's end and its writes, so nothing is read early. 1 to 3
-// us a call.
+// us a call. What that kernel may write was not read-only for the whole life of this
+// one, so it is read by ordinary loads, exponents past L1, never by non-coherent ones.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename K, typename A>

@@ -255,12 +255,12 @@ __global__ void __launch_bounds__(Shape<NT, WR>::kThreads, Shape<NT, WR>::blocks
     Place p{0, 0, 0, 0};
     const int j = blk * kUnit + 16 * (lane & 3);
     if (lane < 4 && blk < sg.blk1 && j < sg.kv) {
-      const int pg = __ldg(c.table + (int64_t)sg.b * c.table_stride + (j >> c.log_page));
+      const int pg = c.table[(int64_t)sg.b * c.table_stride + (j >> c.log_page)];
       if (pg >= 0 && pg < c.n_pages) {
         p.pg = pg;
         p.have = min(16, sg.kv - j);
-        p.ek = __ldg(c.k_exp + (int64_t)pg * c.kv_heads + sg.h);
-        p.ev = __ldg(c.v_exp + (int64_t)pg * c.kv_heads + sg.h);
+        p.ek = __ldcg(c.k_exp + (int64_t)pg * c.kv_heads + sg.h);
+        p.ev = __ldcg(c.v_exp + (int64_t)pg * c.kv_heads + sg.h);
       } else {
         atomicOr(c.status, kFaultBatch);
       }

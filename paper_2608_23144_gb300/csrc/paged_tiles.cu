@@ -191,11 +191,11 @@ __device__ __forceinline__ Groups load_groups(const KvArgs& c, const int32_t* ta
   const int j = blk * BN + 16 * (lane & 7);
   Groups g{0, 0, 0};
   if (lane < 8 && j < kv) {
-    const int pg = __ldg(table + (j >> c.log_page));
+    const int pg = table[j >> c.log_page];
     if (pg >= 0 && pg < c.n_pages) {
       g.have = min(16, kv - j);
-      g.ek = __ldg(c.k_exp + (int64_t)pg * c.kv_heads + h);
-      g.ev = __ldg(c.v_exp + (int64_t)pg * c.kv_heads + h);
+      g.ek = __ldcg(c.k_exp + (int64_t)pg * c.kv_heads + h);
+      g.ev = __ldcg(c.v_exp + (int64_t)pg * c.kv_heads + h);
     }
   }
   return g;
@@ -205,7 +205,7 @@ __device__ __forceinline__ Groups load_groups(const KvArgs& c, const int32_t* ta
 __device__ __forceinline__ int group_tokens(const KvArgs& c, const int32_t* table, int kv, int blk) {
   const int j = blk * BN + 16 * (threadIdx.x & 7);
   if (j >= kv) return 0;
-  const int pg = __ldg(table + (j >> c.log_page));
+  const int pg = table[j >> c.log_page];
   return pg >= 0 && pg < c.n_pages ? min(16, kv - j) : 0;
 }
 
@@ -268,7 +268,7 @@ __device__ void load_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
       int pg = -1;
       const int j = blk * BN + (lane << c.log_page);
       if (lane < per && j < sg.kv) {
-        pg = __ldg(table + (j >> c.log_page));
+        pg = table[j >> c.log_page];
         if (pg < 0 || pg >= c.n_pages) {
           atomicOr(c.status, kFaultBatch);
           pg = -1;
@@ -488,7 +488,7 @@ __device__ __noinline__ float stage_q(const AttnArgs& a, Smem<D>& sm, int t, con
     for (int b = 0; b < kB; ++b) {
       int tok, head;  // rows past the last repeat it: no branch holds a load back
       map.at(min(first + kPer * (i0 + b), rows - 1), &tok, &head);
-      v[b] = __ldg(reinterpret_cast<const uint4*>(qp + tok * ts + head * hs));
+      v[b] = __ldcg(reinterpret_cast<const uint4*>(qp + tok * ts + head * hs));
     }
     uint32_t am[kB];  // largest magnitude, as bits: bf16 patterns order like their values, NaN above infinity
 #pragma unroll
