@@ -567,17 +567,14 @@ __device__ __noinline__ bool finish_tile(const AttnArgs& a, Smem<D>& sm, const C
   tc_fence_after();
   float* slot = partial_slot(a, blockIdx.x, cs.c0) + (int64_t)t * BM * (D + 2) + r;
   __nv_bfloat16* op = static_cast<__nv_bfloat16*>(a.out.p) + (int64_t)(cs.first + tok) * a.out.ts + (int64_t)head * a.out.hs;
-  const float inv = l == 0.0f ? 0.0f : __frcp_rn(l);
+  const float nan = __int_as_float(0x7FC00000);
   const bool bad = sm.bad[t * BM + r];
+  const float inv = bad ? nan : (l == 0.0f ? 0.0f : __frcp_rn(l));
 #pragma unroll 1
   for (int q = 0; q < D / 16; ++q) {
     float v[16];
     tmem_ld16(to + 16 * q, v);
     tmem_wait_ld(v);
-    if (bad) {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = __int_as_float(0x7FC00000);
-    }
     if (have && cs.whole) {
       put16(op + 16 * q, v, inv);
     } else if (have) {
@@ -592,6 +589,10 @@ __device__ __noinline__ bool finish_tile(const AttnArgs& a, Smem<D>& sm, const C
   } else {
     slot[D * BM] = m;
     slot[(D + 1) * BM] = l;
+    if (bad) {
+#pragma unroll 1
+      for (int d = 0; d < D; ++d) slot[d * BM] = nan;
+    }
   }
   return true;
 }
@@ -650,10 +651,12 @@ __device__ void softmax_role(const AttnArgs& a, Smem<D>& sm, const Ctx& x) {
       if (blk + 1 < blk1) g = load_groups(c, table, kv, h, blk + 1);
       // lane i < 8: the scale of group i's keys, the exponent and unscaling of its values, its tokens
       const bool mark = cur.ek == kExpNan, mark_v = cur.ev == kExpNan;
-      const bool masked = blk * BN + BN - 1 > lim_min || __any_sync(0xffffffffu, lane < 8 && (cur.have < 16 || mark));
-      // marked values: O will be NaN for the rows that see one, the scores and l are what they are
-      const uint32_t bad_groups = __ballot_sync(0xffffffffu, mark_v);
-      if (bad_groups && lim >= blk * BN + 16 * (__ffs(bad_groups) - 1)) sm.bad[threadIdx.x] = 1;
+      const bool odd = __any_sync(0xffffffffu, lane < 8 && (cur.have < 16 || mark || mark_v));
+      const bool masked = blk * BN + BN - 1 > lim_min || odd;
+      if (odd) {  // marked values: O will be NaN for the rows that see one, the scores and l are what they are
+        const uint32_t groups = __ballot_sync(0xffffffffu, mark_v);
+        if (groups && lim >= blk * BN + 16 * (__ffs(groups) - 1)) sm.bad[threadIdx.x] = 1;
+      }
       float4* gc = sm.group_of[warp][blk & 1];
       if (lane < 8)
         gc[lane] = make_float4(mark ? 1.0f : pow2f(cur.ek), mark_v ? 0.0f : (float)cur.ev, mark_v ? 1.0f : pow2f(-cur.ev), 0.0f);
