@@ -128,3 +128,55 @@ def test_append_reports_every_entry_that_cannot_be_right(aw, n_seq, at, kind):  
     for a, b in ((got.k, good.k), (got.v, good.v)):
         assert torch.equal(a.view(torch.uint8)[pg], b.view(torch.uint8)[pg])
     assert torch.equal(got.k_exp[pg], good.k_exp[pg]) and torch.equal(got.v_exp[pg], good.v_exp[pg])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n_seq", [33, 129, 300])
+@pytest.mark.parametrize("most", [1, 9])
+def test_batches_of_many_sequences(aw, dtype, n_seq, most):  # noqa: F811
+    """More sequences than a warp, a thread block and two of them look at together, some without new tokens and some
+    empty: appended bit for bit, then read by the kernel of few rows (one token each) and by that of many."""
+    gen = torch.Generator().manual_seed(n_seq)
+    heads, kv_heads, dim, page = 6, 2, 64, 16
+    new = torch.randint(0, most + 1, (n_seq,), generator=gen)
+    ctx = torch.randint(0, 60, (n_seq,), generator=gen) * (torch.rand(n_seq, generator=gen) < 0.8)
+    kv = (new + ctx).tolist()
+    new = new.tolist()
+    batch, table, pages = make_batch(aw, gen, new, kv, page)
+    cache = random_cache(aw, gen, pages, kv_heads, dim, page)
+    want = ref.Cache.of(cache)
+    ws = aw.awsrc_attention_workspace(cache, heads)
+    x = torch.randn(sum(new), heads + 2 * kv_heads, dim, generator=gen).to(dtype)
+    cos, sin = tables(max(kv), dim // 2, gen)
+    cut = (slice(0, heads), slice(heads, heads + kv_heads), slice(heads + kv_heads, None))
+    q = aw.awsrc_kv_append(cache, batch, *(x.cuda()[:, c] for c in cut), cos.cuda(), sin.cuda(), ws)
+    assert aw.awsrc_workspace_status(ws) == 0
+    want_q = ref.append(want, *(x[:, c] for c in cut), new, kv, table, cos, sin, False)
+    assert torch.equal(q.cpu(), want_q.to(dtype))
+    got = ref.Cache.of(cache)
+    for w in "kv":
+        assert torch.equal(got.exp[w], want.exp[w]) and torch.equal(got.code[w], want.code[w])
+    check_attention(aw, cache, q.cpu(), new, kv, table, True, batch=batch, ws=ws)
+
+
+# ------------------------------------------------------------------- scales
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("scale", [0.0, -0.11, 1e-30])
+def test_score_scales_of_either_sign_and_zero(aw, dtype, new, scale):  # noqa: F811
+    """sm_scale q and |sm_scale| (-q) are the same scores, and the bounds are those of the second."""
+    gen = torch.Generator().manual_seed(23)
+    kv = [new + 211]
+    _, table, pages = make_batch(aw, gen, [new], kv, 16)
+    cache = random_cache(aw, gen, pages, 2, 128, 16)
+    q = torch.randn(new, 6, 128, generator=gen).to(dtype)
+    out, lse = torch.empty_like(q, device="cuda"), torch.empty(new, 6, device="cuda")
+    ws = aw.awsrc_attention_workspace(cache, 6)
+    aw.awsrc_paged_attention(cache, step_batch(aw, [new], kv, table), q.cuda(), ws, sm_scale=scale, out=out, lse=lse)
+    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else (0.0, 2.0 ** -9)
+    want, wl, ob, lb = ref.attention(ref.Cache.of(cache), -q if scale < 0 else q, [new], kv, table, abs(scale), True, *eps)
+    if dtype == BF16:
+        ob = ob + (want.abs() + ob) * 2.0 ** -9
+    assert ((out.cpu().double() - want).abs() <= ob + 1e-30).all()
+    assert ((lse.cpu().double() - wl).abs() <= lb).all()
