@@ -593,11 +593,15 @@ awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const awsrc_kv_batch* 
  * one; values of such a block make out NaN, lse stays that of the scores.
  *   q, out   [n_tok][n_heads], the same dtype (out must not overlap q).
  *   lse      device, n_tok x n_heads floats, or NULL.
- * F32 keeps q and the softmax weights in two binary16 terms (22 bits) each and
- * sums in binary32. BF16 keeps q exact (calls of max_new * n_heads / n_kv_heads
- * > 16 rows and 16-byte aligned q and out: but for elements below 2^-13 of their
- * row's largest, which they keep to 2^-21 of that) and the weights in 8 bits or
- * more; out is rounded once. Sums run in a fixed order: results repeat bit for bit.
+ * Precision: sums in binary32, out rounded once. Of a row, let M be the largest
+ * |q| and W the largest softmax weight times the scale of its values' block.
+ *   F32      q and the weights in two binary16 terms each: q to 2^-22 of an element
+ *            or 2^-39 M, a weight times its scale to 2^-22 of it or 2^-40 W;
+ *   BF16     q exact or to 2^-39 M, weights in one binary16: to 2^-11 or 2^-40 W;
+ *   BF16, max_new * n_heads / n_kv_heads > 16, 16-byte aligned rows of q and out:
+ *            q exact but for elements below 2^-13 M, which are kept to 2^-21 M;
+ *            weights to 2^-11 or 2^-31 W.
+ * Sums run in a fixed order: results repeat bit for bit.
  * Visible tokens' codes must be finite (awsrc_kv_append writes no e4m3 NaN);
  * the bytes of rows past kv_len may be anything. Two launches at most.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA.

@@ -46,8 +46,9 @@
 // warp-level MMAs, whose rate is a third of the fifth-generation cores': four
 // prompts of up to 4096 tokens (28 heads) in 1.7 ms, 150 TFLOP/s.
 //
-// Rounding: q (bf16: exact; float32: 22 bits), p (11 bits, float32: 22) and the
-// widened codes (exact) to binary16; scores, m, l, O and the joins in binary32; out
+// Rounding: q (bf16: exact; float32: 22 bits; either to 2^-25 under a largest element
+// of 2^14), p (11 bits, float32: 22; either to 2^-25 under a largest p of 2^15; l takes
+// it unrounded) and the widened codes (exact) to binary16; scores, m, l, O and the joins in binary32; out
 // once. An MMA cuts its binary32 sums off instead of rounding them, so q's second
 // terms have sums of their own, and a float32 weight gets its 2^15 after the power,
 // whose argument near zero keeps its last bits: together 8.5e-7 -> 4e-7 of the

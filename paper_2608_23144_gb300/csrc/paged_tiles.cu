@@ -19,7 +19,8 @@
 //           like the values would be exact to 2^-39, and took 7% (four prompts) to
 //           16% (chunks) longer: the widened keys' stores compete with the products
 //           for shared memory;
-//   p . V   kind::f16 with p in binary16 (from tensor memory) and the value
+//   p . V   kind::f16 with p in binary16 (from tensor memory: 11 bits, or 2^-25 under
+//           a largest p of 2^6 or more; l takes it unrounded) and the value
 //           codes widened to binary16, exactly, by four warps. Splitting p into
 //           8-bit terms instead would cost the softmax warps two more
 //           conversions per weight, five times the widening's instructions.

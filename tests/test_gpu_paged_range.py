@@ -180,3 +180,45 @@ def test_score_scales_of_either_sign_and_zero(aw, dtype, new, scale):  # noqa: F
         ob = ob + (want.abs() + ob) * 2.0 ** -9
     assert ((out.cpu().double() - want).abs() <= ob + 1e-30).all()
     assert ((lse.cpu().double() - wl).abs() <= lb).all()
+
+
+# ------------------------------------------------------------------ weights
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new,kv", [(1, 200), (40, 200), (40, 5000)])
+@pytest.mark.parametrize("spread", [8, 16, 24])
+def test_values_of_one_block_far_above_the_others(aw, dtype, new, kv, spread):  # noqa: F811
+    """One block's value scale is 2^spread times the others', for the sake of one dim; its other dims are zero, so that the
+    rest of the output comes from weights that count 2^-spread as much. A weight times its scale is held to 2^-22
+    (float32) or 2^-11 of itself, or to W 2^-40 (tiles kernel: 2^-31), W the row's largest: sum_j |c_j| W 2^-40 more in out."""
+    gen = torch.Generator().manual_seed(24)
+    page, dim, heads = 16, 64, 6
+    _, table, pages = make_batch(aw, gen, [new], [kv], page)
+    cache = random_cache(aw, gen, pages, 1, dim, page)
+    cache.k_exp.fill_(-9)
+    cache.v_exp.fill_(-12)
+    big = int(table[0, 5])
+    cache.v_exp[big] = spread - 12
+    raw = cache.v.view(torch.uint8)
+    raw[big, :, :, :7] = 0
+    raw[big, :, :, 8:] = 0  # dim 7 alone
+    q = torch.randn(new, heads, dim, generator=gen).to(dtype)
+    c = ref.Cache.of(cache)
+    tiles = dtype == BF16 and new * heads > 16
+    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else (0.0, 2.0 ** -11)
+    want, wl, ob, lb = ref.attention(c, q, [new], [kv], table, dim ** -0.5, True, *eps)
+    used = [int(p) for p in table[0][:-(-kv // page)]]
+    k, v = (c.values(w, used, 0, kv) for w in "kv")
+    scale = torch.exp2(c.exp["v"][used, 0].double()).repeat_interleave(page)[:kv]
+    hide = torch.arange(kv)[None] > (kv - new + torch.arange(new))[:, None]
+    for h in range(heads):
+        p = torch.softmax((q[:, h].double() @ k.T * dim ** -0.5).masked_fill(hide, -torch.inf), 1)
+        codes = (v / scale[:, None]).abs()
+        ob[:, h] += 2.0 ** (-31 if tiles else -40) * (p * scale).amax(1, keepdim=True) * ((~hide).double() @ codes)
+    if dtype == BF16:
+        ob = ob + (want.abs() + ob) * 2.0 ** -9
+    lse = torch.empty(new, heads, device="cuda")
+    out = aw.awsrc_paged_attention(cache, step_batch(aw, [new], [kv], table), q.cuda(),
+                                   aw.awsrc_attention_workspace(cache, heads), lse=lse).cpu().double()
+    assert ((out - want).abs() <= ob).all()
+    assert ((lse.cpu().double() - wl).abs() <= lb).all()
