@@ -39,20 +39,20 @@
 // second launch; nothing waits.
 //
 // Measured: 64 ragged decode steps on contexts up to 8192 (28 heads, 4 kv heads,
-// bf16) in 64 us, 5.4 TB/s of the cache; one on 131k tokens (40 heads, 8 kv heads,
-// float32) in 55 us, 4.9 TB/s. In the loop the copies keep up with the memory;
+// bf16) in 64 us, 5.3 TB/s of the cache; one on 131k tokens (40 heads, 8 kv heads,
+// float32) in 54 us, 5.0 TB/s. In the loop the copies keep up with the memory;
 // what is lost are the starts of blocks and the ends of segments (a tenth each) and,
 // in float32, the second terms' products. Many float32 rows are bound by the
 // warp-level MMAs, whose rate is a third of the fifth-generation cores': four
-// prompts of up to 4096 tokens (28 heads) in 1.7 ms, 150 TFLOP/s.
+// prompts of up to 4096 tokens (28 heads, 4 kv heads) in 1.77 ms, 142 TFLOP/s.
 //
 // Rounding: q (bf16: exact; float32: 22 bits; either to 2^-25 under a largest element
 // of 2^14), p (11 bits, float32: 22; either to 2^-25 under a largest p of 2^15; l takes
-// it unrounded) and the widened codes (exact) to binary16; scores, m, l, O and the joins in binary32; out
-// once. An MMA cuts its binary32 sums off instead of rounding them, so q's second
-// terms have sums of their own, and a float32 weight gets its 2^15 after the power,
-// whose argument near zero keeps its last bits: together 8.5e-7 -> 4e-7 of the
-// result for a token on 516.
+// it unrounded) and the widened codes (exact) to binary16; scores, m, l, O and the
+// joins in binary32; out once. An MMA cuts its binary32 sums off instead of rounding
+// them, so q's second terms have sums of their own, and a float32 weight gets its 2^15
+// after the power, whose argument near zero keeps its last bits: together 8.5e-7 ->
+// 4e-7 of the result for a token on 516 (4e-7 to 6e-7 over inputs).
 #include "internal.h"
 #include "kv_paged.cuh"
 #include "tc05.cuh"

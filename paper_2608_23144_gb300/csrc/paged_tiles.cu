@@ -44,8 +44,8 @@
 // joined by the last block to arrive, the five parts of a tile took 60 us.
 //
 // Measured: four chunks of 1024 tokens on contexts of 20k beside decoding users (40
-// heads, 8 kv heads) in 465 us, 1190 TFLOP/s or 63% of a large bf16 product; four
-// prompts of up to 4096 tokens (28 heads, 4 kv heads) in 315 us, 800 TFLOP/s, the
+// heads, 8 kv heads) in 463 us, 1195 TFLOP/s or 63% of a large bf16 product; four
+// prompts of up to 4096 tokens (28 heads, 4 kv heads) in 316 us, 796 TFLOP/s, the
 // masked halves of diagonal blocks not counted. Bound: a block's 16 products of a
 // tile take 1028 cycles by themselves (and 74 to commit) but about 1500 here, since
 // q . k reads both operands from shared memory at its full rate, 128 bytes per
