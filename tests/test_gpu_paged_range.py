@@ -9,6 +9,9 @@ from test_gpu_paged import BF16, F32, aw, check_attention, make_batch, random_ca
 
 pytestmark = pytest.mark.gpu
 
+BF16_EPS = (0.0, 2.0 ** -11)  # q exact, weights in one binary16
+BF16_ROUND = 2.0 ** -8  # out, once, to 8 significant bits: half a unit of the last, 2^-8 of a power of two
+
 
 # ------------------------------------------------------------------ queries
 
@@ -33,7 +36,7 @@ def test_a_query_channel_far_above_the_others(aw, dtype, heads, kv_heads, dim, n
         check_attention(aw, cache, q, [new], kv, table, True)
         return
     c = ref.Cache.of(cache)
-    want, wl, ob, lb = ref.attention(c, q, [new], kv, table, dim ** -0.5, True, 0.0, 2.0 ** -9)
+    want, wl, ob, lb = ref.attention(c, q, [new], kv, table, dim ** -0.5, True, *BF16_EPS)
     x = q.double().abs()
     top = x.amax(-1, keepdim=True)
     small = torch.where(x < top * 2.0 ** -13, top * 2.0 ** -21, 0.0)
@@ -48,7 +51,7 @@ def test_a_query_channel_far_above_the_others(aw, dtype, heads, kv_heads, dim, n
     lse = torch.empty(new, heads, device="cuda")
     out = aw.awsrc_paged_attention(cache, step_batch(aw, [new], kv, table), q.cuda(),
                                    aw.awsrc_attention_workspace(cache, heads), lse=lse).cpu().double()
-    assert ((out - want).abs() <= ob + (want.abs() + ob) * 2.0 ** -9).all()  # out is rounded once
+    assert ((out - want).abs() <= ob + (want.abs() + ob) * BF16_ROUND).all()  # out is rounded once
     assert ((lse.cpu().double() - wl).abs() <= lb).all()
 
 
@@ -69,10 +72,10 @@ def test_marked_blocks(aw, dtype, which, dim, new, kv, page):  # noqa: F811
     q = torch.randn(new, 6, dim, generator=gen).to(dtype)
     ws = aw.awsrc_attention_workspace(cache, 6)
     batch = step_batch(aw, [new], [kv], table)
-    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else (0.0, 2.0 ** -9)
+    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else BF16_EPS
     want, wl, ob, lb = ref.attention(ref.Cache.of(cache), q, [new], [kv], table, dim ** -0.5, True, *eps)
     if dtype == BF16:
-        ob = ob + (want.abs() + ob) * 2.0 ** -9
+        ob = ob + (want.abs() + ob) * BF16_ROUND
     (cache.k_exp if which == "k" else cache.v_exp)[pg, 1] = -128
     lse = torch.empty(new, 6, device="cuda")
     out = aw.awsrc_paged_attention(cache, batch, q.cuda(), ws, lse=lse).cpu().double()
@@ -174,10 +177,10 @@ def test_score_scales_of_either_sign_and_zero(aw, dtype, new, scale):  # noqa: F
     out, lse = torch.empty_like(q, device="cuda"), torch.empty(new, 6, device="cuda")
     ws = aw.awsrc_attention_workspace(cache, 6)
     aw.awsrc_paged_attention(cache, step_batch(aw, [new], kv, table), q.cuda(), ws, sm_scale=scale, out=out, lse=lse)
-    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else (0.0, 2.0 ** -9)
+    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else BF16_EPS
     want, wl, ob, lb = ref.attention(ref.Cache.of(cache), -q if scale < 0 else q, [new], kv, table, abs(scale), True, *eps)
     if dtype == BF16:
-        ob = ob + (want.abs() + ob) * 2.0 ** -9
+        ob = ob + (want.abs() + ob) * BF16_ROUND
     assert ((out.cpu().double() - want).abs() <= ob + 1e-30).all()
     assert ((lse.cpu().double() - wl).abs() <= lb).all()
 
@@ -205,7 +208,7 @@ def test_values_of_one_block_far_above_the_others(aw, dtype, new, kv, spread):  
     q = torch.randn(new, heads, dim, generator=gen).to(dtype)
     c = ref.Cache.of(cache)
     tiles = dtype == BF16 and new * heads > 16
-    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else (0.0, 2.0 ** -11)
+    eps = (2.0 ** -22, 2.0 ** -22) if dtype == F32 else BF16_EPS
     want, wl, ob, lb = ref.attention(c, q, [new], [kv], table, dim ** -0.5, True, *eps)
     used = [int(p) for p in table[0][:-(-kv // page)]]
     k, v = (c.values(w, used, 0, kv) for w in "kv")
@@ -216,7 +219,7 @@ def test_values_of_one_block_far_above_the_others(aw, dtype, new, kv, spread):  
         codes = (v / scale[:, None]).abs()
         ob[:, h] += 2.0 ** (-31 if tiles else -40) * (p * scale).amax(1, keepdim=True) * ((~hide).double() @ codes)
     if dtype == BF16:
-        ob = ob + (want.abs() + ob) * 2.0 ** -9
+        ob = ob + (want.abs() + ob) * BF16_ROUND
     lse = torch.empty(new, heads, device="cuda")
     out = aw.awsrc_paged_attention(cache, step_batch(aw, [new], [kv], table), q.cuda(),
                                    aw.awsrc_attention_workspace(cache, heads), lse=lse).cpu().double()
