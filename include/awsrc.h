@@ -562,7 +562,8 @@ awsrc_status awsrc_attention_workspace_init(const awsrc_kv_cache* cache, int32_t
  * i < rotary_dim / 2: (x1, x2) = dims (i, i + rotary_dim / 2), or (2i, 2i + 1)
  * when interleaved; x1' = x1 cos[p][i] - x2 sin[p][i], x2' = x2 cos[p][i] +
  * x1 sin[p][i] in binary32, every operation rounded; the other dims pass
- * unchanged. q_out = the rotated q rounded to its dtype (q_out may be q).
+ * unchanged. q_out = the rotated q rounded to its dtype (q_out may be q, and has no
+ * element in common with k or v).
  * A block's exponent becomes e = max(e_old, e(amax of its new tokens)); e_old
  * counts only when the page already held tokens of the sequence (its first new
  * row is not 0). Codes are x * 2^-e rounded to nearest even; when e grows, the
