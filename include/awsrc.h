@@ -611,6 +611,157 @@ awsrc_status awsrc_paged_attention(const awsrc_kv_cache* cache, const awsrc_kv_b
                                    const awsrc_rows* q, const awsrc_rows* out, float* lse, float sm_scale,
                                    int32_t causal, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------- serving steps -- */
+
+/*
+ * What a serving loop needs around the paged cache and the packed products: the
+ * step's tables made on the device from the requests' lengths (awsrc_kv_plan),
+ * products for more rows than awsrc_packed_gemv takes (awsrc_fp8_*), and the
+ * verification of drafted tokens (awsrc_verify_drafts), whose `keep` is the next
+ * step's. The paper has none of them; they are this library's serving extension.
+ *
+ * awsrc_step_workspace_bytes — device bytes of the workspace these calls share:
+ *   its fault word (awsrc_workspace_status) and scratch. Host-only.
+ * awsrc_step_workspace_init — makes a new workspace usable. Once per workspace;
+ *   one stream at a time. The fault word accumulates until it is read.
+ */
+awsrc_status awsrc_step_workspace_bytes(size_t* bytes);
+awsrc_status awsrc_step_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The pages of a cache and who holds them, all on the device. Sequence b holds
+ * the first ceil(kv_len[b] / page) entries of its row of page_table; free_pages
+ * is a stack of *free_count pages that nobody holds (n_pages entries of room).
+ *   page       16, 32, 64 or 128;  n_seq  0 to 8192 (slots; an idle one has
+ *              kv_len 0).
+ */
+typedef struct awsrc_kv_pool {
+  int32_t n_pages, page, n_seq, table_stride;
+  int32_t* page_table;  /* n_seq x table_stride */
+  int32_t* kv_len;      /* n_seq */
+  int32_t* free_pages;  /* n_pages */
+  int32_t* free_count;  /* 1 */
+} awsrc_kv_pool;
+
+/*
+ * awsrc_kv_plan — the tables of the next step. Sequence b keeps its first
+ * keep[b] tokens (all when `keep` is NULL; fewer after rejected drafts, 0 when it
+ * has ended) and is to get add[b] new ones. With held = ceil(kv_len / page) and
+ * want = ceil((keep + add) / page) it needs max(0, want - held) pages and gives
+ * back max(0, held - want).
+ *   Room. A sequence gets its new tokens when the needs of all sequences up to
+ *     it do not exceed free_count + all pages given back (or it needs none), and
+ *     the new tokens of all sequences up to it do not exceed n_tok; else it gets
+ *     none in this step, keeps its keep[b] tokens and gives back what those do
+ *     not use. awsrc_workspace_status then has bit 4 (16).
+ *   Stack. Pages given back go on top in the order of (sequence, table entry);
+ *     then pages are taken from the top in the same order.
+ *   On return, kv_len[b] = keep[b] + the tokens it got, page_table and the stack
+ *   are up to date, and
+ *   q_start    n_seq + 1: exclusive sums of the tokens got (awsrc_kv_batch).
+ *   tok_seq, tok_pos, tok_slot  n_tok each, or NULL: sequence, position and
+ *              page * page size + row of token t < q_start[n_seq]; -1 behind.
+ * Table entries past a sequence's pages keep what they held. Entries that
+ * cannot be right (kv_len < 0 or beyond the table's row, keep outside [0,
+ * kv_len], add < 0, keep + add beyond the row) leave their sequence as it is,
+ * without new tokens, and are reported (bit 3); so is a stack that cannot be
+ * right (free_count outside [0, n_pages], or more pages given back than it has
+ * room for): nothing changes then, q_start is 0 and the maps are -1.
+ * The arrays must not overlap. Errors: INVALID_ARG, SHAPE, UNSUPPORTED (n_seq >
+ * 8192, table_stride * page > 2^30), WORKSPACE, CUDA.
+ */
+awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const int32_t* add, int32_t n_tok,
+                           int32_t* q_start, int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows [n][vocab] of probabilities, F32 or BF16: element (t, j) at t * stride + j. */
+typedef struct awsrc_probs {
+  const void* p;
+  int64_t stride;
+  int32_t dtype, pad_;
+} awsrc_probs;
+
+/*
+ * awsrc_verify_drafts — which drafted tokens the target model accepts, and the
+ * token that follows them. Sequence b has the rows [row_start[b], row_start[b +
+ * 1]) (none is allowed: nothing is done for it): ids of its last token and its
+ * drafts in order; row t of `target` holds the probabilities of the token after
+ * ids[t], row t of `draft` those that the draft ids[t + 1] was drawn from. NULL
+ * for `draft`: drafts of certainty (looked up, or greedy), 1 at ids[t + 1].
+ *   Draft ids[t + 1] is accepted when u[t] * draft[t][id] < target[t][id]
+ *   (exactly), up to the first that is not, in row s. The token then comes from
+ *   the weights w_j = max(0, target[s][j] - draft[s][j]); when all drafts are
+ *   accepted, from w_j = target[s][j] of the last row s. It is the smallest j
+ *   with w_0 + .. + w_j > r[b] * (w_0 + .. + w_V-1), the sums exact over
+ *   probabilities rounded down to multiples of 2^-62. Where all w_j are 0 the row
+ *   of `target` takes their place; where that is 0 too the token is -1.
+ *   Probabilities count as 0 when NaN or negative and as 1 above 1; u and r as
+ *   0 when NaN or negative; r as the largest value below 1 from 1 on.
+ *   accepted   n_seq: accepted drafts;  tokens  n_seq x (max_draft + 1): those,
+ *              the token, -1 behind.
+ *   kv_len, keep  n_seq each, or both NULL: keep = kv_len less the drafts not
+ *              accepted (what awsrc_kv_plan takes; keep may be kv_len).
+ * A draft outside the vocabulary is not accepted and is reported (bit 3), as are
+ * rows that cannot be right (row_start outside [0, n_rows] or falling, more than
+ * max_draft drafts): their sequence, like one without rows, gets accepted 0,
+ * tokens -1 and keep = kv_len.
+ * Bit-reproducible. Errors: INVALID_ARG, SHAPE (vocab < 1), UNSUPPORTED (n_seq >
+ * 65535, vocab > 2^24), WORKSPACE, CUDA.
+ */
+awsrc_status awsrc_verify_drafts(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t max_draft,
+                                 const int32_t* row_start, const int32_t* ids, const awsrc_probs* target,
+                                 const awsrc_probs* draft, const float* u, const float* r, const int32_t* kv_len,
+                                 int32_t* accepted, int32_t* tokens, int32_t* keep, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * A rows x cols matrix held in 8 bits: e4m3 codes with one power-of-two scale 2^e
+ * per row and 128 columns (a block; the last one of a row may be shorter), e =
+ * smallest integer with amax <= 448 * 2^e, at least -64 (the convention of the
+ * records' POW2 scales and of the paged cache); code = x * 2^-e rounded to
+ * nearest even. All codes of a block that has a non-finite element are NaN
+ * (0x7F), its e is 0. Byte layout, the operand order of the tensor cores; B =
+ * ceil(cols / 128), R = rows rounded up to a multiple of 8:
+ *   codes  [B][R][128]: of row r, the 16 columns 16 c .. of a block lie at byte
+ *          16 (c ^ (r % 8)); columns past cols are 0, rows past rows anything.
+ *   exps   [ceil(B / 4)][ceil(rows / 128)][32][4][4]: e + 127 of (row, block) at
+ *          [block / 4][row / 128][row % 32][row % 128 / 32][block % 4].
+ *   codes  device, 128-byte aligned;  exps  device, 16-byte aligned.
+ *   rows   0 to 2^30;  cols  1 to 2^24.
+ *
+ * awsrc_fp8_matrix_bytes — bytes of the two arrays. Host-only.
+ * awsrc_fp8_quantize — x (rows of `dtype`, element (i, j) at i * stride + j) to
+ *   an awsrc_fp8_matrix of its shape. Padding past rows is not written.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, CUDA.
+ */
+typedef struct awsrc_fp8_matrix {
+  int32_t rows, cols;
+  uint8_t* codes;
+  uint8_t* exps;
+} awsrc_fp8_matrix;
+
+awsrc_status awsrc_fp8_matrix_bytes(int32_t rows, int32_t cols, size_t* codes_bytes, size_t* exps_bytes);
+awsrc_status awsrc_fp8_quantize(const void* x, int32_t dtype, int64_t stride, const awsrc_fp8_matrix* out,
+                                void* stream);
+
+/*
+ * awsrc_fp8_gemm — y[t][i] = sum_k x[t][k] w[i][k] for two matrices held in 8
+ * bits (activations x, weights w laid out once), y of dtype F32 or BF16 with
+ * element (t, i) at t * y_stride + i. Products and scales are exact, sums are in
+ * binary32 in a fixed order (results repeat bit for bit); the tensor cores cut
+ * their running sums off instead of rounding them, so F32 sums are taken over at
+ * most 2048 columns there and joined by rounded additions. A block that holds
+ * NaN makes the sums it takes part in NaN.
+ * awsrc_fp8_linear — awsrc_fp8_quantize of x to x8 and awsrc_fp8_gemm with it in
+ * one call, the same results bit for bit: y = x w^T.
+ * Errors: INVALID_ARG, SHAPE (x.cols != w.cols), UNSUPPORTED, WORKSPACE, CUDA.
+ */
+awsrc_status awsrc_fp8_gemm(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, void* y, int32_t y_dtype,
+                            int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
+awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, const awsrc_fp8_matrix* x8,
+                              const awsrc_fp8_matrix* w, void* y, int32_t y_dtype, int64_t y_stride,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 /*
  * awsrc_workspace_status — synchronises `stream`, then reads and clears the
  * device fault word kept in the first bytes of an encode/select/decode
@@ -622,8 +773,11 @@ awsrc_status awsrc_paged_attention(const awsrc_kv_cache* cache, const awsrc_kv_b
  *            (for its codes) gave a different gain than the search found
  *            (never expected).
  * Bit 2 (4): a bounded wait inside a kernel gave up (never expected).
- * Bit 3 (8): a paged-cache batch held an entry that cannot be right (skipped).
- *            The paged-cache calls do not clear the word when they start.
+ * Bit 3 (8): a paged-cache batch, plan or verification held an entry that cannot
+ *            be right (skipped).
+ * Bit 4 (16): awsrc_kv_plan found no room for some sequence's new tokens.
+ *            The calls of the paged cache and of serving steps do not clear the
+ *            word when they start.
  */
 awsrc_status awsrc_workspace_status(void* workspace, void* stream, uint32_t* flags);
 

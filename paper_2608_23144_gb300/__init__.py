@@ -67,3 +67,16 @@ from ._paged import (  # noqa: F401
     awsrc_kv_cache_alloc,
     awsrc_paged_attention,
 )
+from ._step import (  # noqa: F401
+    Fp8Matrix,
+    KvPool,
+    awsrc_fp8_gemm,
+    awsrc_fp8_linear,
+    awsrc_fp8_matrix,
+    awsrc_fp8_quantize,
+    awsrc_kv_plan,
+    awsrc_kv_pool,
+    awsrc_kv_pool_alloc,
+    awsrc_step_workspace,
+    awsrc_verify_drafts,
+)

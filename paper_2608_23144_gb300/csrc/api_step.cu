@@ -1,0 +1,163 @@
+// api_step.cu — the extern "C" entry points of serving steps declared in
+// include/awsrc.h: argument validation and launches.
+#include <climits>
+
+#include "internal.h"
+#include "step.cuh"
+
+namespace awsrc {
+
+namespace {
+
+constexpr size_t kStepWorkspace = kStatusBytes;
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool is_dtype(int32_t d) { return d == AWSRC_DTYPE_F32 || d == AWSRC_DTYPE_BF16; }
+uintptr_t size_of(int32_t dtype) { return dtype == AWSRC_DTYPE_BF16 ? 2 : 4; }
+
+awsrc_status check_workspace(const void* ws, size_t bytes) {
+  if (!ws || bytes < kStepWorkspace) return AWSRC_ERR_WORKSPACE;
+  return aligned(ws, 256) ? AWSRC_OK : AWSRC_ERR_INVALID_ARG;
+}
+
+awsrc_status check_matrix(const awsrc_fp8_matrix* m, bool pointers, Fp8Mat* out) {
+  if (!m || m->rows < 0) return AWSRC_ERR_INVALID_ARG;
+  if (m->cols < 1) return AWSRC_ERR_SHAPE;
+  if (m->rows > (1 << 30) || m->cols > (1 << 24)) return AWSRC_ERR_UNSUPPORTED;
+  if (pointers && (!m->codes || !m->exps || !aligned(m->codes, 128) || !aligned(m->exps, 16))) return AWSRC_ERR_INVALID_ARG;
+  *out = Fp8Mat{m->rows, m->cols, m->codes, m->exps};
+  return AWSRC_OK;
+}
+
+awsrc_status check_rows(const void* x, int32_t dtype) {
+  return is_dtype(dtype) && x && aligned(x, size_of(dtype)) ? AWSRC_OK : AWSRC_ERR_INVALID_ARG;
+}
+
+awsrc_status gemm_args(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, void* y, int32_t y_dtype, int64_t y_stride,
+                       void* workspace, size_t workspace_bytes, GemmArgs* out) {
+  GemmArgs a{};
+  awsrc_status s;
+  if ((s = check_matrix(x, true, &a.x)) != AWSRC_OK || (s = check_matrix(w, true, &a.w)) != AWSRC_OK ||
+      (s = check_rows(y, y_dtype)) != AWSRC_OK)
+    return s;
+  if (x->cols != w->cols) return AWSRC_ERR_SHAPE;
+  if ((s = check_workspace(workspace, workspace_bytes)) != AWSRC_OK) return s;
+  // tiles are numbered in 32 bits
+  if ((int64_t)a.w.tiles() * ((a.x.rows + 15) / 16) > INT_MAX / 2) return AWSRC_ERR_UNSUPPORTED;
+  a.y = y;
+  a.ys = y_stride;
+  a.status = static_cast<uint32_t*>(workspace);
+  a.wait_ns = wait_limit_ns();
+  a.stall = wait_test_stall();
+  *out = a;
+  return AWSRC_OK;
+}
+
+}  // namespace
+
+}  // namespace awsrc
+
+using namespace awsrc;
+
+extern "C" {
+
+awsrc_status awsrc_step_workspace_bytes(size_t* bytes) {
+  if (!bytes) return AWSRC_ERR_INVALID_ARG;
+  *bytes = kStepWorkspace;
+  return AWSRC_OK;
+}
+
+awsrc_status awsrc_step_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
+  const awsrc_status s = check_workspace(workspace, workspace_bytes);
+  if (s != AWSRC_OK) return s;
+  const cudaError_t e = cudaMemsetAsync(workspace, 0, kStepWorkspace, (cudaStream_t)stream);
+  return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "step_workspace_init");
+}
+
+awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const int32_t* add, int32_t n_tok,
+                           int32_t* q_start, int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  if (!pool || pool->n_pages < 1 || pool->n_seq < 0 || pool->table_stride < 1 || n_tok < 0) return AWSRC_ERR_INVALID_ARG;
+  if (pool->page != 16 && pool->page != 32 && pool->page != 64 && pool->page != 128) return AWSRC_ERR_SHAPE;
+  if (pool->n_seq > kPlanMaxSeq || (int64_t)pool->table_stride * pool->page > (1 << 30)) return AWSRC_ERR_UNSUPPORTED;
+  if (!pool->page_table || !pool->kv_len || !pool->free_pages || !pool->free_count || !add || !q_start)
+    return AWSRC_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)pool->page_table, (const void*)pool->kv_len, (const void*)pool->free_pages,
+                        (const void*)pool->free_count, (const void*)keep, (const void*)add, (const void*)q_start,
+                        (const void*)tok_seq, (const void*)tok_pos})
+    if (!aligned(p, 4)) return AWSRC_ERR_INVALID_ARG;
+  if (!aligned(tok_slot, 8)) return AWSRC_ERR_INVALID_ARG;
+  const awsrc_status s = check_workspace(workspace, workspace_bytes);
+  if (s != AWSRC_OK) return s;
+  PlanArgs a{pool->n_pages, pool->page, 4, pool->n_seq, pool->table_stride, n_tok, pool->page_table, pool->kv_len,
+             pool->free_pages, pool->free_count, keep, add, q_start, tok_seq, tok_pos, tok_slot,
+             static_cast<uint32_t*>(workspace)};
+  while ((1 << a.log_page) < a.page) ++a.log_page;
+  const cudaError_t e = launch_plan(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "kv_plan");
+}
+
+awsrc_status awsrc_verify_drafts(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t max_draft, const int32_t* row_start,
+                                 const int32_t* ids, const awsrc_probs* target, const awsrc_probs* draft, const float* u,
+                                 const float* r, const int32_t* kv_len, int32_t* accepted, int32_t* tokens, int32_t* keep,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  if (n_seq < 0 || n_rows < 0 || max_draft < 0) return AWSRC_ERR_INVALID_ARG;
+  if (vocab < 1) return AWSRC_ERR_SHAPE;
+  if (n_seq > 65535 || vocab > (1 << 24) || max_draft > (1 << 20)) return AWSRC_ERR_UNSUPPORTED;
+  if (!row_start || !ids || !target || !u || !r || !accepted || !tokens || !kv_len != !keep) return AWSRC_ERR_INVALID_ARG;
+  awsrc_status s = check_rows(target->p, target->dtype);
+  if (s != AWSRC_OK || (draft && (s = check_rows(draft->p, draft->dtype)) != AWSRC_OK)) return s;
+  for (const void* p : {(const void*)row_start, (const void*)ids, (const void*)u, (const void*)r, (const void*)kv_len,
+                        (const void*)accepted, (const void*)tokens, (const void*)keep})
+    if (!aligned(p, 4)) return AWSRC_ERR_INVALID_ARG;
+  if ((s = check_workspace(workspace, workspace_bytes)) != AWSRC_OK) return s;
+  if (n_seq == 0) return AWSRC_OK;
+  const VerifyArgs a{n_seq, n_rows, vocab, max_draft, row_start, ids, target->p, draft ? draft->p : nullptr, target->stride,
+                     draft ? draft->stride : 0, u, r, kv_len, accepted, tokens, keep, static_cast<uint32_t*>(workspace)};
+  const cudaError_t e = launch_verify(a, target->dtype, draft ? draft->dtype : AWSRC_DTYPE_F32, (cudaStream_t)stream);
+  return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "verify_drafts");
+}
+
+awsrc_status awsrc_fp8_matrix_bytes(int32_t rows, int32_t cols, size_t* codes_bytes, size_t* exps_bytes) {
+  if (!codes_bytes || !exps_bytes) return AWSRC_ERR_INVALID_ARG;
+  const awsrc_fp8_matrix m{rows, cols, nullptr, nullptr};
+  Fp8Mat f;
+  const awsrc_status s = check_matrix(&m, false, &f);
+  if (s != AWSRC_OK) return s;
+  *codes_bytes = (size_t)f.blocks() * f.rows8() * 128;
+  *exps_bytes = (size_t)((f.blocks() + 3) / 4) * f.tiles() * 512;
+  return AWSRC_OK;
+}
+
+awsrc_status awsrc_fp8_quantize(const void* x, int32_t dtype, int64_t stride, const awsrc_fp8_matrix* out, void* stream) {
+  Fp8Mat m;
+  awsrc_status s = check_matrix(out, true, &m);
+  if (s != AWSRC_OK || (s = check_rows(x, dtype)) != AWSRC_OK) return s;
+  if (m.rows == 0) return AWSRC_OK;
+  const cudaError_t e = launch_fp8_quantize(x, dtype, stride, m, (cudaStream_t)stream);
+  return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "fp8_quantize");
+}
+
+awsrc_status awsrc_fp8_gemm(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, void* y, int32_t y_dtype, int64_t y_stride,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  GemmArgs a;
+  const awsrc_status s = gemm_args(x, w, y, y_dtype, y_stride, workspace, workspace_bytes, &a);
+  if (s != AWSRC_OK) return s;
+  if (a.x.rows == 0 || a.w.rows == 0) return AWSRC_OK;
+  const cudaError_t e = launch_fp8_gemm(a, y_dtype, (cudaStream_t)stream);
+  return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "fp8_gemm");
+}
+
+awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, const awsrc_fp8_matrix* x8,
+                              const awsrc_fp8_matrix* w, void* y, int32_t y_dtype, int64_t y_stride, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  GemmArgs a;
+  awsrc_status s = gemm_args(x8, w, y, y_dtype, y_stride, workspace, workspace_bytes, &a);
+  if (s != AWSRC_OK || (s = check_rows(x, x_dtype)) != AWSRC_OK) return s;
+  if (a.x.rows == 0 || a.w.rows == 0) return AWSRC_OK;
+  cudaError_t e = launch_fp8_quantize(x, x_dtype, x_stride, a.x, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = launch_fp8_gemm(a, y_dtype, (cudaStream_t)stream);
+  return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "fp8_linear");
+}
+
+}  // extern "C"

@@ -1,0 +1,207 @@
+// step_plan.cu — the tables of a serving step from the requests' lengths: which
+// pages come back and which are handed out, q_start, and each new token's
+// sequence, position and slot.
+//
+// All sums are prefix sums over the sequences: needs and new tokens decide who
+// finds room; pages given back, pages handed out and tokens got (of those who
+// did) say where each page and token goes. One cluster does the call: every
+// thread block sums over all sequences (at most 8192) for itself, then pages and
+// tokens, numbered through, are dealt out over the cluster's threads, each
+// finding its sequence by bisection of the sums in shared memory. Two cluster
+// barriers: all inputs are read before any is overwritten, and pages given back
+// lie on the stack before they are handed out again.
+#include "internal.h"
+#include "step.cuh"
+
+namespace awsrc {
+
+namespace {
+
+constexpr int kThreads = 1024;
+
+// Sums of a block's threads before this one, and of all; three sums at a time.
+struct Sum3 {
+  int64_t a, b, c;
+};
+__device__ __forceinline__ int64_t warp_incl(int64_t v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t o = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+__device__ Sum3 block_excl(Sum3 v, Sum3* total, Sum3* warps) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Sum3 i{warp_incl(v.a), warp_incl(v.b), warp_incl(v.c)};
+  __syncthreads();  // warps[] of the sum before is read
+  if (lane == 31) warps[warp] = i;
+  __syncthreads();
+  const Sum3 w = warps[lane];
+  const Sum3 wi{warp_incl(w.a), warp_incl(w.b), warp_incl(w.c)};
+  *total = Sum3{__shfl_sync(0xffffffffu, wi.a, 31), __shfl_sync(0xffffffffu, wi.b, 31), __shfl_sync(0xffffffffu, wi.c, 31)};
+  const Sum3 before{__shfl_sync(0xffffffffu, wi.a - w.a, warp), __shfl_sync(0xffffffffu, wi.b - w.b, warp),
+                    __shfl_sync(0xffffffffu, wi.c - w.c, warp)};
+  return Sum3{before.a + i.a - v.a, before.b + i.b - v.b, before.c + i.c - v.c};
+}
+
+struct Entry {
+  int len, keep, add;  // add 0 and keep = len for an entry that cannot be right
+  bool ok;
+};
+
+__device__ __forceinline__ int pages_of(int64_t tokens, int log_page) {
+  return (int)((tokens + (1 << log_page) - 1) >> log_page);
+}
+
+__device__ __forceinline__ Entry load_entry(const PlanArgs& a, int b) {
+  Entry e;
+  e.len = a.len[b];
+  e.keep = a.keep ? a.keep[b] : e.len;
+  e.add = a.add[b];
+  const int64_t most = (int64_t)a.stride << a.log_page;
+  e.ok = e.len >= 0 && e.len <= most && e.keep >= 0 && e.keep <= e.len && e.add >= 0 && (int64_t)e.keep + e.add <= most;
+  if (!e.ok) e.keep = e.len, e.add = 0;
+  return e;
+}
+
+// Largest b with start[b] <= i, start[0] = 0: the sequence that item i belongs to
+// (sequences without items are passed over).
+__device__ __forceinline__ int find(const int* start, int n, int i) {
+  int lo = 0, hi = n;  // start[lo] <= i < start[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= i) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ PlanArgs a) {
+  extern __shared__ int sm[];
+  __shared__ Sum3 warps[32];
+  const int n = a.n_seq;
+  int* s_tok = sm;               // n + 1: first token of a sequence
+  int* s_pop = sm + (n + 1);     // first page handed out
+  int* s_back = sm + 2 * (n + 1);  // first page given back
+  int* s_held = sm + 3 * (n + 1);  // pages held, -1 for an entry that cannot be right
+  int* s_keep = sm + 4 * (n + 1);
+  step_wait();
+  step_trigger();
+  const int tid = threadIdx.x, rank = cluster_rank();
+  const int per = (n + kThreads - 1) / kThreads;
+  const int b0 = min(n, tid * per), b1 = min(n, b0 + per);
+  const int count = *a.count;
+
+  // who finds room
+  Sum3 v{0, 0, 0}, total;
+  bool bad = false;
+  for (int b = b0; b < b1; ++b) {
+    const Entry e = load_entry(a, b);
+    bad |= !e.ok;
+    const int held = e.ok ? pages_of(e.len, a.log_page) : 0, want = e.ok ? pages_of((int64_t)e.keep + e.add, a.log_page) : 0;
+    v.a += max(0, want - held);
+    v.b += e.add;
+    v.c += max(0, held - want);
+  }
+  Sum3 before = block_excl(v, &total, warps);
+  const int64_t room = count + total.c;
+  Sum3 got{0, 0, 0};
+  bool short_ = false;
+  for (int b = b0; b < b1; ++b) {
+    const Entry e = load_entry(a, b);
+    const int held = e.ok ? pages_of(e.len, a.log_page) : 0;
+    int want = e.ok ? pages_of((int64_t)e.keep + e.add, a.log_page) : 0, add = e.add;
+    before.a += max(0, want - held);
+    before.b += add;
+    if ((want > held && before.a > room) || before.b > a.n_tok) {
+      short_ |= add > 0;
+      add = 0;
+      want = e.ok ? pages_of(e.keep, a.log_page) : 0;
+    }
+    s_held[b] = e.ok ? held : -1;
+    s_keep[b] = e.keep;
+    s_tok[b] = add;
+    got.a += max(0, want - held);
+    got.b += add;
+    got.c += max(0, held - want);
+  }
+  before = block_excl(got, &total, warps);
+  const bool wrong = count < 0 || count > a.n_pages || count + total.c > a.n_pages;
+  for (int b = b0; b < b1; ++b) {
+    const int add = s_tok[b], held = max(0, s_held[b]);
+    const int want = s_held[b] < 0 ? 0 : pages_of((int64_t)s_keep[b] + add, a.log_page);
+    s_pop[b] = (int)before.a;
+    s_tok[b] = (int)before.b;
+    s_back[b] = (int)before.c;
+    before.a += max(0, want - held);
+    before.b += add;
+    before.c += max(0, held - want);
+  }
+  if (tid == 0) {
+    s_pop[n] = (int)total.a;
+    s_tok[n] = (int)total.b;
+    s_back[n] = (int)total.c;
+  }
+  cluster_sync();  // sums are in shared memory, and every block has read the inputs
+  const int step = gridDim.x * kThreads, at = rank * kThreads + tid;
+  const uint32_t fault = (bad || wrong ? kFaultBatch : 0u) | (short_ ? kFaultRoom : 0u);
+  if (rank == 0 && fault) atomicOr(a.status, fault);
+  if (wrong) {
+    for (int b = at; b <= n; b += step) a.q_start[b] = 0;
+    for (int t = at; t < a.n_tok; t += step) {
+      if (a.tok_seq) a.tok_seq[t] = -1;
+      if (a.tok_pos) a.tok_pos[t] = -1;
+      if (a.tok_slot) a.tok_slot[t] = -1;
+    }
+    return;
+  }
+  const int top = count + s_back[n];
+  for (int b = at; b <= n; b += step) {
+    a.q_start[b] = s_tok[b];
+    if (b < n) a.len[b] = s_keep[b] + s_tok[b + 1] - s_tok[b];
+  }
+  if (at == 0) *a.count = top - s_pop[n];
+  for (int i = at; i < s_back[n]; i += step) {
+    const int b = find(s_back, n, i);
+    const int want = pages_of((int64_t)s_keep[b] + s_tok[b + 1] - s_tok[b], a.log_page);
+    a.free[count + i] = a.table[(int64_t)b * a.stride + want + i - s_back[b]];
+  }
+  cluster_sync();
+  for (int i = at; i < s_pop[n]; i += step) {
+    const int b = find(s_pop, n, i);
+    a.table[(int64_t)b * a.stride + s_held[b] + i - s_pop[b]] = __ldcg(a.free + top - 1 - i);
+  }
+  if (!a.tok_seq && !a.tok_pos && !a.tok_slot) return;
+  for (int t = at; t < a.n_tok; t += step) {
+    int b = -1, pos = -1;
+    int64_t slot = -1;
+    if (t < s_tok[n]) {
+      b = find(s_tok, n, t);
+      pos = s_keep[b] + t - s_tok[b];
+      const int j = pos >> a.log_page;
+      const int page = j < s_held[b] ? a.table[(int64_t)b * a.stride + j] : __ldcg(a.free + top - 1 - (s_pop[b] + j - s_held[b]));
+      slot = ((int64_t)page << a.log_page) + (pos & (a.page - 1));
+    }
+    if (a.tok_seq) a.tok_seq[t] = b;
+    if (a.tok_pos) a.tok_pos[t] = pos;
+    if (a.tok_slot) a.tok_slot[t] = slot;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_plan(const PlanArgs& a, cudaStream_t st) {
+  const size_t smem = (size_t)5 * (a.n_seq + 1) * sizeof(int);
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  const cudaError_t e = launch_step(plan_kernel, dim3(1), kThreads, smem, 1, st, a);
+  if (e != cudaSuccess) return e;
+  note_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace awsrc
