@@ -668,7 +668,7 @@ typedef struct awsrc_kv_pool {
  * right (free_count outside [0, n_pages], or more pages given back than it has
  * room for): nothing changes then, q_start is 0 and the maps are -1.
  * The arrays must not overlap. Errors: INVALID_ARG, SHAPE, UNSUPPORTED (n_seq >
- * 8192, table_stride * page > 2^30), WORKSPACE, CUDA.
+ * 8192, table_stride * page, n_pages or n_tok > 2^30), WORKSPACE, CUDA.
  */
 awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const int32_t* add, int32_t n_tok,
                            int32_t* q_start, int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot,

@@ -79,7 +79,8 @@ awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const
                            size_t workspace_bytes, void* stream) {
   if (!pool || pool->n_pages < 1 || pool->n_seq < 0 || pool->table_stride < 1 || n_tok < 0) return AWSRC_ERR_INVALID_ARG;
   if (pool->page != 16 && pool->page != 32 && pool->page != 64 && pool->page != 128) return AWSRC_ERR_SHAPE;
-  if (pool->n_seq > kPlanMaxSeq || (int64_t)pool->table_stride * pool->page > (1 << 30)) return AWSRC_ERR_UNSUPPORTED;
+  if (pool->n_seq > kPlanMaxSeq || pool->n_pages > (1 << 30) || n_tok > (1 << 30) ||
+      (int64_t)pool->table_stride * pool->page > (1 << 30)) return AWSRC_ERR_UNSUPPORTED;
   if (!pool->page_table || !pool->kv_len || !pool->free_pages || !pool->free_count || !add || !q_start)
     return AWSRC_ERR_INVALID_ARG;
   for (const void* p : {(const void*)pool->page_table, (const void*)pool->kv_len, (const void*)pool->free_pages,
@@ -91,7 +92,7 @@ awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const
   if (s != AWSRC_OK) return s;
   PlanArgs a{pool->n_pages, pool->page, 4, pool->n_seq, pool->table_stride, n_tok, pool->page_table, pool->kv_len,
              pool->free_pages, pool->free_count, keep, add, q_start, tok_seq, tok_pos, tok_slot,
-             static_cast<uint32_t*>(workspace)};
+             static_cast<uint32_t*>(workspace), 0};
   while ((1 << a.log_page) < a.page) ++a.log_page;
   const cudaError_t e = launch_plan(a, (cudaStream_t)stream);
   return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "kv_plan");
@@ -154,7 +155,10 @@ awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, 
   GemmArgs a;
   awsrc_status s = gemm_args(x8, w, y, y_dtype, y_stride, workspace, workspace_bytes, &a);
   if (s != AWSRC_OK || (s = check_rows(x, x_dtype)) != AWSRC_OK) return s;
+  if (x8->codes == w->codes || x8->exps == w->exps) return AWSRC_ERR_INVALID_ARG;
   if (a.x.rows == 0 || a.w.rows == 0) return AWSRC_OK;
+  // the quantising kernel lets the product start only after it has waited for all kernels before it
+  a.early = 1;
   cudaError_t e = launch_fp8_quantize(x, x_dtype, x_stride, a.x, (cudaStream_t)stream);
   if (e == cudaSuccess) e = launch_fp8_gemm(a, y_dtype, (cudaStream_t)stream);
   return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "fp8_linear");

@@ -28,6 +28,8 @@ constexpr int BM = 128;
 constexpr int kThreads = 320, kCopyWarp = 8, kMmaWarp = 9;
 constexpr int kSfSets = 4;    // scales of 4 blocks each in tensor memory; more ahead than stages
 constexpr int kChunk = 16;    // blocks summed in tensor memory for F32 results
+constexpr int kMaxSplit = 8;  // thread blocks that share a tile's columns
+constexpr int kLeast = 4;     // blocks that one of them has at least
 
 template <int N, bool kF32>
 struct Cfg {
@@ -36,7 +38,8 @@ struct Cfg {
   static constexpr int kXSf = N > 128 ? 2 : 1;  // 512-byte scale tiles of x
   static constexpr int kSfBytes = 512 * (1 + kXSf);
   static constexpr int kBufs = N > 128 ? 1 : 2;  // accumulators
-  static constexpr int kStages = N > 128 ? 4 : N > 64 ? 6 : 8;
+  static constexpr int kPerSm = N > 64 ? 1 : 2;  // thread blocks
+  static constexpr int kStages = N > 128 ? 4 : N > 64 ? 6 : N > 32 ? 4 : 5;
   static constexpr int kAccCols = kBufs * N;
   static constexpr int kSfCols = 4 * (1 + kXSf);
   static constexpr int kCols = kAccCols + kSfSets * kSfCols;
@@ -114,26 +117,29 @@ __device__ __forceinline__ void umma_mx(uint32_t d, uint64_t a, uint64_t b, uint
 
 // The walk that all roles take: tiles of this block, in chunks of blocks.
 struct Walk {
-  int tiles_w, tiles, blocks, chunk;
-  int tile, k0, k1;
+  int tiles_w, tiles, chunk, step;
+  int tile, lo, hi, k0, k1;
   __device__ Walk(const GemmArgs& a, int n, bool f32) {
     tiles_w = a.w.tiles();
     tiles = tiles_w * ((a.x.rows + n - 1) / n);
-    blocks = a.x.blocks();
+    const int blocks = a.x.blocks(), rank = blockIdx.x % a.split;
+    step = gridDim.x / a.split;
+    tile = blockIdx.x / a.split;
+    lo = (int)((int64_t)blocks * rank / a.split);
+    hi = (int)((int64_t)blocks * (rank + 1) / a.split);
     chunk = f32 ? kChunk : blocks;
-    tile = blockIdx.x;
-    k0 = 0;
-    k1 = min(chunk, blocks);
+    k0 = lo;
+    k1 = min(k0 + chunk, hi);
   }
   __device__ bool more() const { return tile < tiles; }
-  __device__ bool first() const { return k0 == 0; }
-  __device__ bool last() const { return k1 == blocks; }
+  __device__ bool first() const { return k0 == lo; }
+  __device__ bool last() const { return k1 == hi; }
   __device__ int row() const { return tile % tiles_w * BM; }
   __device__ int tok(int n) const { return tile / tiles_w * n; }
   __device__ void next() {
-    if (last()) tile += gridDim.x, k0 = 0;
+    if (last()) tile += step, k0 = lo;
     else k0 = k1;
-    k1 = min(k0 + chunk, blocks);
+    k1 = min(k0 + chunk, hi);
   }
 };
 
@@ -142,25 +148,41 @@ __device__ void copy_role(const GemmArgs& a, Smem<N, kF32>& sm, const Ctx& x) {
   using C = Cfg<N, kF32>;
   const int64_t w8 = a.w.rows8(), x8 = a.x.rows8();
   uint32_t n = 0;
+  int ahead = 0;  // blocks whose rows of w are on their way before x is ready
   bool ok = true;
-  for (Walk w(a, N, kF32); ok && w.more(); w.next()) {
+  Walk w(a, N, kF32);
+  // block kb of the tile to stage s: what comes of w, then what comes of x
+  const auto begin = [&](int kb, uint32_t s) {
     const int row = w.row(), tok = w.tok(N);
+    const bool sf = (kb & 3) == 0 || kb == w.lo;
     const uint32_t wb = 128u * (uint32_t)min((int64_t)BM, w8 - row), xb = 128u * (uint32_t)min((int64_t)N, x8 - tok);
     const uint32_t xs = 512u * (uint32_t)min(C::kXSf, a.x.tiles() - (tok >> 7));
+    mbar_expect_tx(&sm.full[s], wb + xb + (sf ? 512u + xs : 0u));
+    bulk_g2s(sm.tile[s], a.w.codes + (kb * w8 + row) * 128, wb, &sm.full[s]);
+    if (sf) bulk_g2s(sm.sf[s], a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + (row >> 7)) * 512, 512, &sm.full[s]);
+  };
+  const auto finish = [&](int kb, uint32_t s) {
+    const int tok = w.tok(N);
+    const uint32_t xb = 128u * (uint32_t)min((int64_t)N, x8 - tok);
+    bulk_g2s(sm.tile[s] + BM * 128, a.x.codes + (kb * x8 + tok) * 128, xb, &sm.full[s]);
+    if ((kb & 3) == 0 || kb == w.lo)
+      bulk_g2s(sm.sf[s] + 512, a.x.exps + ((int64_t)(kb >> 2) * a.x.tiles() + (tok >> 7)) * 512,
+               512u * (uint32_t)min(C::kXSf, a.x.tiles() - (tok >> 7)), &sm.full[s]);
+  };
+  if (a.early && a.stall < 0 && w.more())
+    for (; ahead < min(C::kStages, w.hi - w.lo); ++ahead) begin(w.lo + ahead, ahead);
+  step_wait();
+  for (; ok && w.more(); w.next()) {
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
       const uint32_t s = n % C::kStages;
-      if (kb == a.stall || !wait_lane(x, &sm.empty[s], ((n / C::kStages) & 1) ^ 1)) {
-        ok = false;
-        break;
+      if ((int)n >= ahead) {
+        if (kb == a.stall || !wait_lane(x, &sm.empty[s], ((n / C::kStages) & 1) ^ 1)) {
+          ok = false;
+          break;
+        }
+        begin(kb, s);
       }
-      const bool sf = (kb & 3) == 0;
-      mbar_expect_tx(&sm.full[s], wb + xb + (sf ? 512u + xs : 0u));
-      bulk_g2s(sm.tile[s], a.w.codes + (kb * w8 + row) * 128, wb, &sm.full[s]);
-      bulk_g2s(sm.tile[s] + BM * 128, a.x.codes + (kb * x8 + tok) * 128, xb, &sm.full[s]);
-      if (sf) {
-        bulk_g2s(sm.sf[s], a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + (row >> 7)) * 512, 512, &sm.full[s]);
-        bulk_g2s(sm.sf[s] + 512, a.x.exps + ((int64_t)(kb >> 2) * a.x.tiles() + (tok >> 7)) * 512, xs, &sm.full[s]);
-      }
+      finish(kb, s);
     }
   }
   if (!ok)  // copies in flight land before the block ends
@@ -181,7 +203,7 @@ __device__ void mma_role(const GemmArgs& a, Smem<N, kF32>& sm, const Ctx& x, uin
       const uint32_t s = n % C::kStages;
       if (!(ok = wait_lane(x, &sm.full[s], (n / C::kStages) & 1))) break;
       tc_fence_after();
-      if ((kb & 3) == 0) {
+      if ((kb & 3) == 0 || kb == w.lo) {
         ++g;
         const uint32_t at = tmem + C::kAccCols + (g % kSfSets) * C::kSfCols;
 #pragma unroll
@@ -203,8 +225,16 @@ __device__ void mma_role(const GemmArgs& a, Smem<N, kF32>& sm, const Ctx& x, uin
   }
 }
 
+template <bool kF32>
+__device__ __forceinline__ void put(const GemmArgs& a, int tok, int row, float v) {
+  const int64_t at = (int64_t)tok * a.ys + row;
+  if (kF32) static_cast<float*>(a.y)[at] = v;
+  else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+}
+
+// Sums of this thread's row and columns; false once a wait has given up.
 template <int N, bool kF32>
-__device__ void write_role(const GemmArgs& a, Smem<N, kF32>& sm, const Ctx& x, uint32_t tmem) {
+__device__ bool write_role(const GemmArgs& a, Smem<N, kF32>& sm, const Ctx& x, uint32_t tmem) {
   using C = Cfg<N, kF32>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t quarter = warp & 3, c0 = (warp >> 2) * C::kPer;
@@ -212,7 +242,7 @@ __device__ void write_role(const GemmArgs& a, Smem<N, kF32>& sm, const Ctx& x, u
   uint32_t c = 0;
   for (Walk w(a, N, kF32); w.more(); w.next(), ++c) {
     const uint32_t buf = c % C::kBufs;
-    if (!wait_warp(x, &sm.acc_full[buf], (c / C::kBufs) & 1)) return;
+    if (!wait_warp(x, &sm.acc_full[buf], (c / C::kBufs) & 1)) return false;
     tc_fence_after();
     const uint32_t t = tmem + ((quarter * 32) << 16) + buf * N + c0;
 #pragma unroll
@@ -225,23 +255,45 @@ __device__ void write_role(const GemmArgs& a, Smem<N, kF32>& sm, const Ctx& x, u
     }
     tc_fence_before();
     mbar_arrive(&sm.acc_empty[buf]);
-    if (w.last()) {
-      const int row = w.row() + quarter * 32 + lane, tok = w.tok(N) + c0;
-      if (row < a.w.rows) {
+    if (!w.last()) continue;
+    const int row = w.row() + quarter * 32 + lane, tok = w.tok(N) + c0;
+    if (a.split > 1) {  // the part stays here until the cluster joins it; all copies and products of the block are done
+      float* part = reinterpret_cast<float*>(sm.tile[0]);
 #pragma unroll
-        for (int i = 0; i < C::kPer; ++i)
-          if (tok + i < a.x.rows) {
-            const int64_t at = (int64_t)(tok + i) * a.ys + row;
-            if (kF32) static_cast<float*>(a.y)[at] = acc[i];
-            else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(acc[i]);
-          }
-      }
+      for (int i = 0; i < C::kPer; ++i) part[(c0 + i) * BM + quarter * 32 + lane] = acc[i];
+    } else if (row < a.w.rows) {
+#pragma unroll
+      for (int i = 0; i < C::kPer; ++i)
+        if (tok + i < a.x.rows) put<kF32>(a, tok + i, row, acc[i]);
     }
+  }
+  return true;
+}
+
+// The cluster's parts of a tile, in shared memory, joined in the order of their
+// columns of w; each thread block joins its share of the tile's elements.
+template <int N, bool kF32>
+__device__ void join(const GemmArgs& a, Smem<N, kF32>& sm) {
+  const Walk w(a, N, kF32);
+  const int rank = blockIdx.x % a.split, row0 = w.row(), tok0 = w.tok(N);
+  const int cols = min(N, a.x.rows - tok0);
+  for (int e = rank * kThreads + threadIdx.x; e < cols * BM; e += a.split * kThreads) {
+    const int row = row0 + e % BM;
+    const uint32_t at = smem_addr(sm.tile[0]) + 4 * e;
+    float sum = 0.0f;
+    for (int z = 0; z < a.split; ++z) {
+      uint32_t peer;
+      float v;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(at), "r"(z));
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer) : "memory");
+      sum = z ? __fadd_rn(sum, v) : v;
+    }
+    if (row < a.w.rows) put<kF32>(a, tok0 + e / BM, row, sum);
   }
 }
 
 template <int N, bool kF32>
-__global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
+__global__ void __launch_bounds__(kThreads, Cfg<N, kF32>::kPerSm) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
   using C = Cfg<N, kF32>;
   extern __shared__ unsigned char smem_raw[];
   Smem<N, kF32>& sm = *reinterpret_cast<Smem<N, kF32>*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
@@ -263,11 +315,12 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
   }
   __syncthreads();
   tc_fence_after();
-  step_wait();
+  if (!a.early) step_wait();
   step_trigger();
   const Ctx x{a.wait_ns, a.status, &sm.dead};
   const uint32_t tmem = sm.tmem;
   if (warp < 8) {
+    step_wait();
     write_role<N, kF32>(a, sm, x, tmem);
   } else if ((threadIdx.x & 31) == 0) {
     if (warp == kCopyWarp) copy_role<N, kF32>(a, sm, x);
@@ -280,16 +333,33 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmem) : "memory");
   }
+  if (a.split > 1) {  // every block gets here: all its waits are bounded
+    __syncwarp();
+    cluster_sync();
+    join<N, kF32>(a, sm);
+    __syncwarp();
+    cluster_sync();  // no block leaves while others read its part
+  }
 }
 
 template <int N, bool kF32>
-cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
+cudaError_t launch(const GemmArgs& in, cudaStream_t st) {
+  using C = Cfg<N, kF32>;
   constexpr int kSmem = (int)sizeof(Smem<N, kF32>) + 1024;
-  static_assert(kSmem <= 227 * 1024, "shared memory of a block");
+  static_assert(C::kPerSm * (kSmem + 1024) <= 228 * 1024, "shared memory of an SM");
+  static_assert(N * BM * 4 <= C::kStages * C::kStageBytes, "a part of a tile fits into the stages");
   const cudaError_t e = cudaFuncSetAttribute(fp8_gemm_kernel<N, kF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
+  GemmArgs a = in;
   const int64_t tiles = (int64_t)a.w.tiles() * ((a.x.rows + N - 1) / N);
-  return launch_step(fp8_gemm_kernel<N, kF32>, dim3((unsigned)(tiles < 152 ? tiles : 152)), kThreads, kSmem, 1, st, a);
+  const int slots = 152 * C::kPerSm, blocks = a.x.blocks();
+  // few tiles: the columns of each are split over a cluster, at least kLeast blocks each
+  a.split = (int)(slots / tiles);
+  if (a.split > kMaxSplit) a.split = kMaxSplit;
+  if (a.split > blocks / kLeast) a.split = blocks / kLeast;
+  if (a.split < 1) a.split = 1;
+  const int64_t grid = a.split > 1 ? tiles * a.split : tiles < slots ? tiles : slots;
+  return launch_step(fp8_gemm_kernel<N, kF32>, dim3((unsigned)grid), kThreads, kSmem, a.split, st, a);
 }
 
 }  // namespace
@@ -298,9 +368,11 @@ cudaError_t launch_fp8_gemm(const GemmArgs& a, int y_dtype, cudaStream_t st) {
   const bool f32 = y_dtype == AWSRC_DTYPE_F32;
   cudaError_t e;
   if (a.x.rows <= 16) e = f32 ? launch<16, true>(a, st) : launch<16, false>(a, st);
+  else if (a.x.rows <= 32) e = f32 ? launch<32, true>(a, st) : launch<32, false>(a, st);
   else if (a.x.rows <= 64) e = f32 ? launch<64, true>(a, st) : launch<64, false>(a, st);
-  else if (f32) e = launch<128, true>(a, st);
-  else e = a.x.rows <= 128 ? launch<128, false>(a, st) : launch<256, false>(a, st);
+  else if (f32 || a.x.rows <= 128 || (int64_t)a.w.tiles() * ((a.x.rows + 255) / 256) < 152)
+    e = f32 ? launch<128, true>(a, st) : launch<128, false>(a, st);
+  else e = launch<256, false>(a, st);
   if (e != cudaSuccess) return e;
   note_launches(1);
   return cudaGetLastError();

@@ -51,6 +51,7 @@ struct PlanArgs {
   int32_t *q_start, *tok_seq, *tok_pos;
   int64_t* tok_slot;
   uint32_t* status;
+  int vec;  // the maps start on 16-byte boundaries
 };
 cudaError_t launch_plan(const PlanArgs& a, cudaStream_t st);
 
@@ -83,6 +84,8 @@ struct GemmArgs {
   uint32_t* status;
   uint64_t wait_ns;  // limit of the kernel's waits
   int stall;         // test of that limit: no copies from this block of 128 columns on (-1: never)
+  int early;         // w was written before the kernel before this one began: its rows need no wait
+  int split;         // thread blocks that share a tile's columns (set by the launch)
 };
 cudaError_t launch_fp8_gemm(const GemmArgs& a, int y_dtype, cudaStream_t st);
 

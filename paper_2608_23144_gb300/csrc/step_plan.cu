@@ -17,8 +17,6 @@ namespace awsrc {
 
 namespace {
 
-constexpr int kThreads = 1024;
-
 // Sums of a block's threads before this one, and of all; three sums at a time.
 struct Sum3 {
   int64_t a, b, c;
@@ -32,13 +30,14 @@ __device__ __forceinline__ int64_t warp_incl(int64_t v) {
   }
   return v;
 }
+template <int kThreads>
 __device__ Sum3 block_excl(Sum3 v, Sum3* total, Sum3* warps) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Sum3 i{warp_incl(v.a), warp_incl(v.b), warp_incl(v.c)};
   __syncthreads();  // warps[] of the sum before is read
   if (lane == 31) warps[warp] = i;
   __syncthreads();
-  const Sum3 w = warps[lane];
+  const Sum3 w = lane < kThreads / 32 ? warps[lane] : Sum3{0, 0, 0};
   const Sum3 wi{warp_incl(w.a), warp_incl(w.b), warp_incl(w.c)};
   *total = Sum3{__shfl_sync(0xffffffffu, wi.a, 31), __shfl_sync(0xffffffffu, wi.b, 31), __shfl_sync(0xffffffffu, wi.c, 31)};
   const Sum3 before{__shfl_sync(0xffffffffu, wi.a - w.a, warp), __shfl_sync(0xffffffffu, wi.b - w.b, warp),
@@ -78,6 +77,25 @@ __device__ __forceinline__ int find(const int* start, int n, int i) {
   return lo;
 }
 
+// Four maps' values from index t on.
+template <typename T>
+__device__ __forceinline__ void put4(T* p, int t, int n, bool vec, const T* v) {
+  if (!p) return;
+  if (vec && t + 4 <= n) {
+    if (sizeof(T) == 4) {
+      *reinterpret_cast<int4*>(p + t) = make_int4((int)v[0], (int)v[1], (int)v[2], (int)v[3]);
+    } else {
+      reinterpret_cast<longlong2*>(p + t)[0] = make_longlong2(v[0], v[1]);
+      reinterpret_cast<longlong2*>(p + t)[1] = make_longlong2(v[2], v[3]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (t + i < n) p[t + i] = v[i];
+}
+
+template <int kThreads>
 __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ PlanArgs a) {
   extern __shared__ int sm[];
   __shared__ Sum3 warps[32];
@@ -105,7 +123,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
     v.b += e.add;
     v.c += max(0, held - want);
   }
-  Sum3 before = block_excl(v, &total, warps);
+  Sum3 before = block_excl<kThreads>(v, &total, warps);
   const int64_t room = count + total.c;
   Sum3 got{0, 0, 0};
   bool short_ = false;
@@ -127,7 +145,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
     got.b += add;
     got.c += max(0, held - want);
   }
-  before = block_excl(got, &total, warps);
+  before = block_excl<kThreads>(got, &total, warps);
   const bool wrong = count < 0 || count > a.n_pages || count + total.c > a.n_pages;
   for (int b = b0; b < b1; ++b) {
     const int add = s_tok[b], held = max(0, s_held[b]);
@@ -174,31 +192,54 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
     a.table[(int64_t)b * a.stride + s_held[b] + i - s_pop[b]] = __ldcg(a.free + top - 1 - i);
   }
   if (!a.tok_seq && !a.tok_pos && !a.tok_slot) return;
-  for (int t = at; t < a.n_tok; t += step) {
-    int b = -1, pos = -1;
-    int64_t slot = -1;
-    if (t < s_tok[n]) {
-      b = find(s_tok, n, t);
-      pos = s_keep[b] + t - s_tok[b];
-      const int j = pos >> a.log_page;
-      const int page = j < s_held[b] ? a.table[(int64_t)b * a.stride + j] : __ldcg(a.free + top - 1 - (s_pop[b] + j - s_held[b]));
-      slot = ((int64_t)page << a.log_page) + (pos & (a.page - 1));
+  // four tokens at a time: one bisection, mostly one page, and vector stores
+  const int live = s_tok[n];
+  for (int t0 = 4 * at; t0 < a.n_tok; t0 += 4 * step) {
+    int seq[4], pos[4];
+    int64_t slot[4];
+    int b = t0 < live ? find(s_tok, n, t0) : n, page = 0, held_j = -1, held_b = -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + i;
+      seq[i] = pos[i] = -1;
+      slot[i] = -1;
+      if (t >= live) continue;
+      while (t >= s_tok[b + 1]) ++b;
+      const int p = s_keep[b] + t - s_tok[b], j = p >> a.log_page;
+      if (b != held_b || j != held_j) {
+        held_b = b;
+        held_j = j;
+        page = j < s_held[b] ? a.table[(int64_t)b * a.stride + j] : __ldcg(a.free + top - 1 - (s_pop[b] + j - s_held[b]));
+      }
+      seq[i] = b;
+      pos[i] = p;
+      slot[i] = ((int64_t)page << a.log_page) + (p & (a.page - 1));
     }
-    if (a.tok_seq) a.tok_seq[t] = b;
-    if (a.tok_pos) a.tok_pos[t] = pos;
-    if (a.tok_slot) a.tok_slot[t] = slot;
+    put4(a.tok_seq, t0, a.n_tok, a.vec, seq);
+    put4(a.tok_pos, t0, a.n_tok, a.vec, pos);
+    put4(a.tok_slot, t0, a.n_tok, a.vec, slot);
   }
+}
+
+template <int kThreads>
+cudaError_t launch(const PlanArgs& a, int cluster, cudaStream_t st) {
+  const size_t smem = (size_t)5 * (a.n_seq + 1) * sizeof(int);
+  if (smem > 47 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(plan_kernel<kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               5 * (kPlanMaxSeq + 1) * (int)sizeof(int));
+    if (e != cudaSuccess) return e;
+  }
+  return launch_step(plan_kernel<kThreads>, dim3(cluster), kThreads, smem, cluster, st, a);
 }
 
 }  // namespace
 
-cudaError_t launch_plan(const PlanArgs& a, cudaStream_t st) {
-  const size_t smem = (size_t)5 * (a.n_seq + 1) * sizeof(int);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
-  const cudaError_t e = launch_step(plan_kernel, dim3(1), kThreads, smem, 1, st, a);
+cudaError_t launch_plan(const PlanArgs& in, cudaStream_t st) {
+  PlanArgs a = in;
+  a.vec = ((reinterpret_cast<uintptr_t>(a.tok_seq) | reinterpret_cast<uintptr_t>(a.tok_pos) |
+            reinterpret_cast<uintptr_t>(a.tok_slot)) & 15) == 0;
+  const bool small = a.n_seq <= 512 && a.n_tok <= 2048;
+  const cudaError_t e = small ? launch<256>(a, 1, st) : launch<1024>(a, 8, st);
   if (e != cudaSuccess) return e;
   note_launches(1);
   return cudaGetLastError();

@@ -31,7 +31,8 @@ def plan(p=None, keep=P, add=P, n_tok=0, q_start=P, seq=None, pos=None, slot=Non
     (dict(p=pool(kv_len=None)), INVALID), (dict(p=pool(free_pages=P + 2)), INVALID), (dict(p=pool(free_count=None)), INVALID),
     (dict(add=None), INVALID), (dict(keep=P + 1), INVALID), (dict(n_tok=-1), INVALID), (dict(q_start=None), INVALID),
     (dict(seq=P + 2), INVALID), (dict(pos=P + 1), INVALID), (dict(slot=P + 4), INVALID), (dict(ws=None), WORKSPACE),
-    (dict(ws_bytes=255), WORKSPACE), (dict(ws=P + 16), INVALID),
+    (dict(ws_bytes=255), WORKSPACE), (dict(ws=P + 16), INVALID), (dict(p=pool(n_pages=(1 << 30) + 1)), UNSUPPORTED),
+    (dict(n_tok=(1 << 30) + 1), UNSUPPORTED),
 ])
 def test_plan_refuses(kw, status):
     assert plan(**kw) == status
@@ -73,12 +74,12 @@ def mat(**over):
 
 
 def gemm(x=None, w=None, y=P, dtype=0, stride=10, ws=P, ws_bytes=1 << 30):
-    return aw.lib.awsrc_fp8_gemm(ct.byref(x or mat()), ct.byref(w or mat(rows=10)), y, dtype, stride, ws, ws_bytes, None)
+    return aw.lib.awsrc_fp8_gemm(ct.byref(x or mat()), ct.byref(w or mat(rows=10, codes=2 * P, exps=2 * P)), y, dtype, stride, ws, ws_bytes, None)
 
 
 def linear(x=None, w=None, y=P, dtype=0, stride=10, ws=P, ws_bytes=1 << 30, src=P, src_dtype=0):
-    return aw.lib.awsrc_fp8_linear(src, src_dtype, 256, ct.byref(x or mat()), ct.byref(w or mat(rows=10)), y, dtype, stride, ws,
-                                   ws_bytes, None)
+    return aw.lib.awsrc_fp8_linear(src, src_dtype, 256, ct.byref(x or mat()),
+                                   ct.byref(w or mat(rows=10, codes=2 * P, exps=2 * P)), y, dtype, stride, ws, ws_bytes, None)
 
 
 def quantize(src=P, dtype=0, stride=256, out=None):
@@ -112,6 +113,10 @@ def test_quantize_refuses(kw, status):
     if "out" not in kw:
         k = {"src": P, "dtype": 0, **kw}
         assert linear(src=k["src"], src_dtype=k["dtype"]) == status
+
+
+def test_linear_refuses_to_write_over_the_weights():
+    assert linear(w=mat(rows=10)) == INVALID and linear(w=mat(rows=10, codes=2 * P)) == INVALID
 
 
 def test_matrix_bytes_are_host_only():
