@@ -1,0 +1,141 @@
+// fp8_mma.cuh — what the kernels of 8-bit products share: bounded waits,
+// descriptors of operands and scales, results.
+#pragma once
+
+#include "step.cuh"
+#include "tc05.cuh"
+
+namespace awsrc {
+namespace fp8 {
+
+using namespace tc05;
+
+constexpr int BM = 128;
+constexpr int kThreads = 320, kCopyWarp = 8, kMmaWarp = 9;  // of a thread block; warps 0-7 write results
+constexpr int kChunk = 16;  // blocks summed in tensor memory for F32 results
+
+struct Ctx {
+  uint64_t wait_ns;
+  uint32_t* status;
+  volatile int* dead;
+};
+
+// Bounded wait; false once any wait of the block has given up.
+static __device__ __noinline__ bool wait_slow(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+  const uint64_t t0 = globaltimer();
+  for (;;) {
+    if (mbar_try_wait(mb, parity)) return true;
+    if (*x.dead) return false;
+    if (globaltimer() - t0 > x.wait_ns) {
+      *x.dead = 1;
+      atomicOr(x.status, kFaultTimeout);
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ bool wait_lane(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+  return mbar_try_wait(mb, parity) || wait_slow(x, mb, parity);
+}
+__device__ __forceinline__ bool wait_warp(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+  return __all_sync(0xffffffffu, wait_lane(x, mb, parity));
+}
+
+// Scales of 4 blocks lie in tensor memory in one of 4 sets, used in turn. Set k + 4
+// overwrites set k, whose products must be done: with 4 blocks a set they are, as the
+// ring of stages has been around since (13 blocks lie between, kMaxStages is no more);
+// where tiles or shares end early, the products of set k's last block are waited for.
+constexpr int kSfSets = 4, kMaxStages = 13;
+struct SfSets {
+  uint32_t count = 0, o1 = 0, o2 = 0, o3 = 0;  // sets so far; first blocks of the last three
+  // Opens the set of block n; false once a wait has given up.
+  template <int kStages>
+  __device__ __forceinline__ bool open(const Ctx& x, unsigned long long* empty, uint32_t n) {
+    static_assert(kStages <= kMaxStages, "a set's products are done when it is used again");
+    bool ok = true;
+    if (count >= kSfSets && n - (o3 - 1) < kStages) {
+      const uint32_t last = o3 - 1;
+      ok = wait_lane(x, &empty[last % kStages], (last / kStages) & 1);
+    }
+    o3 = o2;
+    o2 = o1;
+    o1 = n;
+    ++count;
+    return ok;
+  }
+  __device__ __forceinline__ uint32_t at() const { return (count - 1) % kSfSets; }
+};
+
+// Rows of 128 bytes, 16-byte pieces exchanged by row (128-byte swizzle), groups of
+// 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_rows(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// 32 rows of 16 bytes: what a copy of scales to tensor memory reads.
+__device__ __forceinline__ uint64_t desc_sf(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(128u >> 4) << 32) | (1ull << 46);
+}
+// Byte `id` of the scale words is the one to use.
+__device__ __forceinline__ uint32_t with_sf_id(uint32_t idesc, uint32_t id) { return idesc | (id << 4) | (id << 29); }
+
+// e4m3 x e4m3, scales of 8 exponent bits, one per 32 columns; M rows of w, n of x.
+__device__ __forceinline__ uint32_t idesc_mx(int m, int n) {
+  return (1u << 23) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// 16 sums of a row from tensor memory on: kept, or added to those of the chunks before.
+template <bool kAdd>
+__device__ __forceinline__ void take16(float* acc, const float* v) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) acc[j] = kAdd ? __fadd_rn(acc[j], v[j]) : v[j];
+}
+
+template <bool kF32>
+__device__ __forceinline__ void put(const GemmArgs& a, int tok, int row, float v) {
+  const int64_t at = (int64_t)tok * a.ys + row;
+  if (kF32) static_cast<float*>(a.y)[at] = v;
+  else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+}
+
+// Element e of a tile's parts in the shared memory of `split` thread blocks, rank0
+// being the first and `every` the step between them: summed in their order.
+__device__ __forceinline__ float4 join4(uint32_t addr, int rank0, int every, int split) {
+  float4 v[8], sum;
+#pragma unroll
+  for (int z = 0; z < 8; ++z)
+    if (z < split) {
+      uint32_t peer;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(addr), "r"(rank0 + z * every));
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                   : "=f"(v[z].x), "=f"(v[z].y), "=f"(v[z].z), "=f"(v[z].w) : "r"(peer) : "memory");
+    }
+  sum = v[0];
+#pragma unroll
+  for (int z = 1; z < 8; ++z)
+    if (z < split)
+      sum = make_float4(__fadd_rn(sum.x, v[z].x), __fadd_rn(sum.y, v[z].y), __fadd_rn(sum.z, v[z].z), __fadd_rn(sum.w, v[z].w));
+  return sum;
+}
+
+// Four rows of w of one row of y.
+template <bool kF32>
+__device__ __forceinline__ void put4(const GemmArgs& a, int tok, int row, float4 v) {
+  const int have = a.w.rows - row;
+  if (have >= 4 && a.vec_y) {
+    const int64_t at = (int64_t)tok * a.ys + row;
+    if (kF32) {
+      *reinterpret_cast<float4*>(static_cast<float*>(a.y) + at) = v;
+    } else {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + at) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    }
+    return;
+  }
+  if (have > 0) put<kF32>(a, tok, row, v.x);
+  if (have > 1) put<kF32>(a, tok, row + 1, v.y);
+  if (have > 2) put<kF32>(a, tok, row + 2, v.z);
+  if (have > 3) put<kF32>(a, tok, row + 3, v.w);
+}
+
+}  // namespace fp8
+}  // namespace awsrc

@@ -1,0 +1,421 @@
+// fp8_pairs.cu — y = x w^T for matrices held in 8 bits and more than 64 rows of x
+// (chunks, prompts): mathematics and layouts as in fp8_gemm.cu, products by pairs of
+// SMs (cta_group::2).
+//
+// Bound: a tile of 128 x 256 by one SM takes 48 KB per block of 128 columns, at the
+// tensor cores' rate 96 bytes per cycle; the L2 gave 52, so such tiles ran at 55% of
+// that rate. A pair's tile is 256 rows of w x n rows of x (64, 128, 192 or 256): each thread block brings 128 rows of w and half of the n rows of x, 32 KB per
+// block, and its tensor core reads the other half from its partner.
+//
+// Roles in each thread block as in fp8_gemm.cu; the pair's even rank issues all
+// products. Copies are of tensors, as only those can report to a partner's barrier:
+// each thread block's count at the even rank's (a thread of the partner that waited
+// for its own copies and passed it on took 950 cycles a block). One commit tells both
+// that a stage is free, or the sums are ready; both tell the even rank when they have
+// read them. Two accumulators where they fit beside the scales (n <= 192),
+// so that one tile's results are read under the next one's products.
+// Few tiles: a cluster of pairs shares a tile's columns and joins its parts.
+//
+// Every wait is bounded as in fp8_gemm.cu; no thread block of a cluster leaves before
+// all have stopped, as products and arrivals reach into a partner's memory.
+#include <cuda.h>
+
+#include "fp8_mma.cuh"
+#include "internal.h"
+
+namespace awsrc {
+
+namespace {
+
+using namespace fp8;
+
+constexpr int kMaxN = 256;
+constexpr int kStages = 6;
+constexpr int kStageBytes = (BM + kMaxN / 2) * 128;
+constexpr int kSfBytes = 512 * 3;  // scales of 128 rows of w, of up to 256 of x
+constexpr int kSfCols = 12, kSfAt = 512 - kSfSets * kSfCols;
+constexpr int kTwoBufs = 192;      // two accumulators of so many columns end before the scales
+constexpr int kMaxSplit = 4;       // pairs that share a tile's columns
+constexpr int kLeast = 4;          // blocks that one of them has at least
+constexpr int kPairs = 76;
+constexpr int kGroup = 8;          // tiles of rows of x that are walked together
+
+struct Smem {
+  uint8_t tile[kStages][kStageBytes];
+  uint8_t sf[kStages][kSfBytes];
+  unsigned long long empty[kStages], acc_full[2];
+  unsigned long long full[kStages], acc_empty[2], drain;  // of the even rank
+  uint32_t tmem;
+  int dead;
+};
+
+// What the kernel takes: the codes as [block][row][128], the scales as [4 blocks][128
+// rows][512 bytes]; rows past the last are read as 0.
+struct PairArgs {
+  CUtensorMap w_codes, x_codes, w_exps, x_exps;
+  GemmArgs g;
+};
+
+// A box of a tensor to this thread block's shared memory; its bytes count at `mbar`, of either thread block of the pair.
+__device__ __forceinline__ void copy_box(void* dst, const CUtensorMap* map, int row, int block, uint32_t mbar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_addr(dst)),
+      "l"(map), "r"(0), "r"(row), "r"(block), "r"(mbar)
+      : "memory");
+}
+
+__device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t mbar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
+}
+// As mbar_try_wait, for arrivals from the partner.
+__device__ __forceinline__ bool try_wait_cluster(unsigned long long* mb, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 20000;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_addr(mb)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __noinline__ bool wait_cluster_slow(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+  const uint64_t t0 = globaltimer();
+  for (;;) {
+    if (try_wait_cluster(mb, parity)) return true;
+    if (*x.dead) return false;
+    if (globaltimer() - t0 > x.wait_ns) {
+      *x.dead = 1;
+      atomicOr(x.status, kFaultTimeout);
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ bool wait_cluster(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+  return try_wait_cluster(mb, parity) || wait_cluster_slow(x, mb, parity);
+}
+
+__device__ __forceinline__ void copy_sf(uint32_t taddr, uint64_t desc) {  // in both thread blocks, each from its own
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void umma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+      : "memory");
+}
+// Arrives at both thread blocks' barriers when the products so far are done.
+__device__ __forceinline__ void commit_both(unsigned long long* mb, uint16_t mask) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          smem_addr(mb)),
+      "h"(mask)
+      : "memory");
+}
+
+// The walk that all roles take: tiles of this pair, its share of their columns in
+// chunks of blocks. Tiles go by groups of kGroup tiles of rows of x, in a group by
+// rows of w, so that what the pairs read together stays in the L2.
+struct Walk {
+  int tiles_w, tiles_x, tiles, chunk, step;
+  int tile, lo, hi, k0, k1, row, tok;
+  __device__ Walk(const GemmArgs& a, bool f32) {
+    tiles_w = (a.w.tiles() + 1) >> 1;
+    tiles_x = (a.x.rows + a.n - 1) / a.n;
+    tiles = tiles_w * tiles_x;
+    const int pair = blockIdx.x >> 1, rank = pair % a.split, blocks = a.x.blocks();
+    step = (gridDim.x >> 1) / a.split;
+    tile = pair / a.split;
+    lo = (int)((int64_t)blocks * rank / a.split);
+    hi = (int)((int64_t)blocks * (rank + 1) / a.split);
+    chunk = f32 ? kChunk : blocks;
+    k0 = lo;
+    k1 = min(k0 + chunk, hi);
+    place(a.n);
+  }
+  __device__ void place(int n) {
+    const int g = tile / (kGroup * tiles_w) * kGroup, in = tile % (kGroup * tiles_w), many = min(kGroup, tiles_x - g);
+    if (many < 1) return;  // past the last tile
+    row = in / many * 2 * BM;
+    tok = (g + in % many) * n;
+  }
+  __device__ bool more() const { return tile < tiles; }
+  __device__ bool first() const { return k0 == lo; }
+  __device__ bool last() const { return k1 == hi; }
+  __device__ void next(int n) {
+    if (last()) {
+      tile += step;
+      k0 = lo;
+      place(n);
+    } else {
+      k0 = k1;
+    }
+    k1 = min(k0 + chunk, hi);
+  }
+};
+
+// Scale tiles of 128 rows that the rows of x of a tile lie in.
+__host__ __device__ constexpr int sf_tiles(int n) { return n > 128 ? 2 : 1; }
+
+template <bool kF32>
+__device__ void copy_role(const PairArgs& p, Smem& sm, const Ctx& x, uint32_t half, uint32_t even) {
+  const GemmArgs& a = p.g;
+  uint32_t n = 0;
+  int ahead = 0;  // blocks whose rows of w are on their way before x is ready
+  bool ok = true;
+  Walk w(a, kF32);
+  const int half_n = a.n >> 1;
+  const uint32_t bytes = 2u * (BM * 128u + half_n * 128u), sf_bytes = 2u * 512u * (1 + sf_tiles(a.n));
+  const auto has_sf = [&](int kb) { return (kb & 3) == 0 || kb == w.lo; };
+  const auto begin = [&](int kb, uint32_t s) {  // what comes of w; the even rank's barrier counts both thread blocks' bytes
+    const uint32_t mbar = peer_addr(&sm.full[s], even);
+    if (!half) mbar_expect_tx(&sm.full[s], bytes + (has_sf(kb) ? sf_bytes : 0u));
+    copy_box(sm.tile[s], &p.w_codes, w.row + BM * half, kb, mbar);
+    if (has_sf(kb)) copy_box(sm.sf[s], &p.w_exps, (w.row >> 7) + half, kb >> 2, mbar);
+  };
+  if (a.early && a.stall < 0 && w.more())
+    for (; ahead < min(kStages, w.hi - w.lo); ++ahead) begin(w.lo + ahead, ahead);
+  step_wait();
+  for (; ok && w.more(); w.next(a.n)) {
+    for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
+      const uint32_t s = n % kStages;
+      if ((int)n >= ahead) {
+        if (kb == a.stall || !wait_cluster(x, &sm.empty[s], ((n / kStages) & 1) ^ 1)) {
+          ok = false;
+          break;
+        }
+        begin(kb, s);
+      }
+      const uint32_t mbar = peer_addr(&sm.full[s], even);
+      copy_box(sm.tile[s] + BM * 128, &p.x_codes, w.tok + half_n * half, kb, mbar);
+      if (has_sf(kb)) copy_box(sm.sf[s] + 512, &p.x_exps, w.tok >> 7, kb >> 2, mbar);
+    }
+  }
+  if (!ok && !half)  // copies in flight, the partner's too, land before either block ends
+    for (uint32_t j = n > kStages ? n - kStages : 0; j < n; ++j)
+      (void)mbar_wait(&sm.full[j % kStages], (j / kStages) & 1, x.wait_ns);
+}
+
+template <bool kF32>
+__device__ void mma_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tmem, uint16_t both) {
+  uint32_t n = 0, c = 0;  // blocks, chunks so far
+  SfSets sets;
+  bool ok = true;
+  const uint32_t bufs = a.n <= kTwoBufs ? 2 : 1, idesc0 = idesc_mx(2 * BM, a.n);
+  for (Walk w(a, kF32); ok && w.more(); w.next(a.n), ++c) {
+    const uint32_t buf = c % bufs, d = tmem + buf * a.n;
+    if (!(ok = wait_cluster(x, &sm.acc_empty[buf], ((c / bufs) & 1) ^ 1))) break;
+    tc_fence_after();
+    for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
+      const uint32_t s = n % kStages;
+      if (!(ok = wait_cluster(x, &sm.full[s], (n / kStages) & 1))) break;
+      tc_fence_after();
+      if ((kb & 3) == 0 || kb == w.lo) {
+        if (!(ok = sets.open<kStages>(x, sm.empty, n))) break;
+        const uint32_t at = tmem + kSfAt + sets.at() * kSfCols;
+        for (int i = 0; i < 1 + sf_tiles(a.n); ++i) copy_sf(at + 4 * i, desc_sf(smem_addr(sm.sf[s] + 512 * i)));
+      }
+      const uint32_t sfa = tmem + kSfAt + sets.at() * kSfCols, sfb = sfa + 4 + ((uint32_t)(w.tok & 127) >> 5);
+      const uint32_t idesc = with_sf_id(idesc0, kb & 3);
+      const uint64_t da = desc_rows(smem_addr(sm.tile[s])), db = desc_rows(smem_addr(sm.tile[s] + BM * 128));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfb, kb != w.k0 || j != 0);
+      commit_both(&sm.empty[s], both);
+    }
+    if (ok) commit_both(&sm.acc_full[buf], both);
+  }
+  if (!ok) {  // products in flight end before the block does
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(&sm.drain)) : "memory");
+    (void)mbar_wait(&sm.drain, 0, x.wait_ns);
+  }
+}
+
+template <bool kF32>
+__device__ void write_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tmem, uint32_t half, uint32_t even) {
+  constexpr int kPer = kMaxN / 2;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = a.n >> 1;
+  const uint32_t quarter = warp & 3, c0 = (warp >> 2) * per, bufs = a.n <= kTwoBufs ? 2 : 1;
+  float acc[kPer];
+  uint32_t c = 0;
+  for (Walk w(a, kF32); w.more(); w.next(a.n), ++c) {
+    const uint32_t buf = c % bufs;
+    if (!wait_warp(x, &sm.acc_full[buf], (c / bufs) & 1)) return;
+    tc_fence_after();
+    const uint32_t t = tmem + ((quarter * 32) << 16) + buf * a.n + c0;
+    if (!kF32 || w.first()) {
+#pragma unroll
+      for (int i = 0; i < kPer; i += 16)
+        if (i < per) tmem_ld16(t + i, acc + i);
+      tmem_wait_ld(acc);
+#pragma unroll
+      for (int i = 16; i < kPer; i += 16) tmem_tie(acc + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; i += 16)
+        if (i < per) {
+          float v[16];
+          tmem_ld16(t + i, v);
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[i + j] = __fadd_rn(acc[i + j], v[j]);
+        }
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) arrive_at(peer_addr(&sm.acc_empty[buf], even));
+    if (!w.last()) continue;
+    const int r = quarter * 32 + lane, row = w.row + BM * half + r;
+    if (a.split > 1) {  // the part stays here until the cluster joins it; all copies and products of the pair are done
+      float* part = reinterpret_cast<float*>(sm.tile[0]);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (i < per) part[(c0 + i) * BM + r] = acc[i];
+    } else if (row < a.w.rows) {
+      const int have = min(per, a.x.rows - w.tok - (int)c0);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (i < have) put<kF32>(a, w.tok + c0 + i, row, acc[i]);
+    }
+  }
+}
+
+template <bool kF32>
+__device__ void join(const GemmArgs& a, Smem& sm, uint32_t half) {
+  const Walk w(a, kF32);
+  const int share = (blockIdx.x >> 1) % a.split, row0 = w.row + BM * half;
+  const int cols = min(a.n, a.x.rows - w.tok);
+  for (int e = share * kThreads + threadIdx.x; e < cols * (BM / 4); e += a.split * kThreads)
+    put4<kF32>(a, w.tok + e / (BM / 4), row0 + e % (BM / 4) * 4, join4(smem_addr(sm.tile[0]) + 16 * e, half, 2, a.split));
+}
+
+template <bool kF32>
+__global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_constant__ PairArgs p) {
+  const GemmArgs& a = p.g;
+  extern __shared__ unsigned char smem_raw[];
+  Smem& sm = *reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
+  const int warp = threadIdx.x >> 5;
+  const uint32_t rank = cluster_rank(), half = rank & 1, even = rank & ~1u;
+  if (warp == kMmaWarp) {
+    if ((threadIdx.x & 31) == 0) {
+      for (int i = 0; i < kStages; ++i) mbar_init(&sm.full[i], 1), mbar_init(&sm.empty[i], 1);
+      for (int i = 0; i < 2; ++i) mbar_init(&sm.acc_full[i], 1), mbar_init(&sm.acc_empty[i], 16);
+      mbar_init(&sm.drain, 1);
+      sm.dead = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sm.tmem)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    tc_fence_before();
+  }
+  __syncwarp();
+  cluster_sync();  // both thread blocks' barriers and tensor memory are there
+  tc_fence_after();
+  if (!a.early) step_wait();
+  step_trigger();
+  const Ctx x{a.wait_ns, a.status, &sm.dead};
+  const uint32_t tmem = sm.tmem;
+  if (warp < 8) {
+    step_wait();
+    write_role<kF32>(a, sm, x, tmem, half, even);
+  } else if ((threadIdx.x & 31) == 0) {
+    if (warp == kCopyWarp) copy_role<kF32>(p, sm, x, half, even);
+    else if (!half) mma_role<kF32>(a, sm, x, tmem, (uint16_t)(3u << even));
+  }
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync();  // every block gets here: all its waits are bounded
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+  if (a.split > 1) {
+    __syncwarp();
+    join<kF32>(a, sm, half);
+    __syncwarp();
+    cluster_sync();  // no block leaves while others read its part
+  }
+}
+
+// Rows of x in a tile and pairs per tile: the fewest cycles by a model of both. A
+// block costs a pair what its bytes take at 52 bytes per cycle and SM, or its
+// products at 2 cycles per row of x, the larger; a tile 2500 more, and 8 per row of
+// x and further pair where pairs join their parts.
+void choose(GemmArgs* a) {
+  const int blocks = a->x.blocks();
+  const int64_t tiles_w = (a->w.tiles() + 1) / 2;
+  double best = 0;
+  for (int n = 64; n <= kMaxN; n += 64)
+    for (int split = 1; split <= kMaxSplit && (split == 1 || split * kLeast <= blocks); ++split) {
+      const int64_t tiles = tiles_w * ((a->x.rows + n - 1) / n);
+      if (split > 1 && tiles * split > kPairs) break;
+      const double load = (16384.0 + 64.0 * n) / 52.0, mma = 2.0 * n;
+      const double tile = (double)((blocks + split - 1) / split) * (load > mma ? load : mma) + 2500.0 + 8.0 * n * (split - 1);
+      const double all = (double)((tiles * split + kPairs - 1) / kPairs) * tile;
+      if (best == 0 || all < best) best = all, a->n = n, a->split = split;
+    }
+}
+
+// A tensor [blocks][rows][`row` bytes], read in boxes of `box` rows.
+cudaError_t tensor(CUtensorMap* map, CUtensorMapDataType type, int size, const void* p, int row, int64_t rows, int64_t blocks,
+                   int box) {
+  typedef decltype(&cuTensorMapEncodeTiled) Encode;
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(f) : nullptr;
+  }();
+  if (!encode) return cudaErrorNotSupported;
+  const cuuint64_t dims[3] = {(cuuint64_t)(row / size), (cuuint64_t)rows, (cuuint64_t)blocks};
+  const cuuint64_t strides[2] = {(cuuint64_t)row, (cuuint64_t)(row * rows)};
+  const cuuint32_t boxes[3] = {(cuuint32_t)(row / size), (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+  const CUresult r = encode(map, type, 3, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <bool kF32>
+cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
+  constexpr int kSmem = (int)sizeof(Smem) + 1024;
+  static_assert(kSmem <= 227 * 1024, "shared memory of a block");
+  static_assert(kMaxN * BM * 4 <= kStages * kStageBytes, "a part of a tile fits into the stages");
+  static_assert(2 * kTwoBufs <= kSfAt && kMaxN <= kSfAt, "accumulators end before the scales");
+  cudaError_t e = cudaFuncSetAttribute(fp8_pairs_kernel<kF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  PairArgs p;
+  p.g = a;
+  const int blocks = a.x.blocks(), fours = (blocks + 3) / 4;
+  for (const bool is_x : {false, true}) {
+    const Fp8Mat& m = is_x ? a.x : a.w;
+    if (e == cudaSuccess)
+      e = tensor(is_x ? &p.x_codes : &p.w_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, m.codes, 128, m.rows8(), blocks,
+                 is_x ? a.n / 2 : BM);
+    if (e == cudaSuccess)
+      e = tensor(is_x ? &p.x_exps : &p.w_exps, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, m.exps, 512, m.tiles(), fours,
+                 is_x ? sf_tiles(a.n) : 1);
+  }
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = (int64_t)((a.w.tiles() + 1) / 2) * ((a.x.rows + a.n - 1) / a.n);
+  const int64_t pairs = a.split > 1 ? tiles * a.split : tiles < kPairs ? tiles : kPairs;
+  return launch_step(fp8_pairs_kernel<kF32>, dim3((unsigned)(2 * pairs)), kThreads, kSmem, 2 * a.split, st, p);
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_pairs(const GemmArgs& in, bool f32, cudaStream_t st) {
+  GemmArgs a = in;
+  choose(&a);
+  return f32 ? launch<true>(a, st) : launch<false>(a, st);
+}
+
+}  // namespace awsrc

@@ -85,8 +85,12 @@ struct GemmArgs {
   uint64_t wait_ns;  // limit of the kernel's waits
   int stall;         // test of that limit: no copies from this block of 128 columns on (-1: never)
   int early;         // w was written before the kernel before this one began: its rows need no wait
-  int split;         // thread blocks that share a tile's columns (set by the launch)
+  // set by the launch
+  int split;         // thread blocks (pairs of them) that share a tile's columns
+  int n;             // rows of x in a tile
+  int vec_y;         // four elements of y lie on a boundary of their size
 };
+cudaError_t launch_fp8_pairs(const GemmArgs& a, bool f32, cudaStream_t st);
 cudaError_t launch_fp8_gemm(const GemmArgs& a, int y_dtype, cudaStream_t st);
 
 }  // namespace awsrc
