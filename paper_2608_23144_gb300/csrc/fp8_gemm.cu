@@ -146,7 +146,7 @@ __device__ void mma_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x, uint32_t 
       if (!(ok = wait_lane(x, &sm.full[s], (n / C::kStages) & 1))) break;
       tc_fence_after();
       if ((kb & 3) == 0 || kb == w.lo) {
-        if (!(ok = sets.open<C::kStages>(x, sm.empty, n))) break;
+        if (!(ok = sets.open<C::kStages, 1>(x, sm.empty, n))) break;
         const uint32_t at = tmem + C::kAccCols + sets.at() * C::kSfCols;
         copy_sf(at, desc_sf(smem_addr(sm.sf[s])));
         copy_sf(at + 4, desc_sf(smem_addr(sm.sf[s] + 512)));

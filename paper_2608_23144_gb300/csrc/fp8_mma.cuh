@@ -47,14 +47,16 @@ __device__ __forceinline__ bool wait_warp(const Ctx& x, unsigned long long* mb, 
 constexpr int kSfSets = 4, kMaxStages = 13;
 struct SfSets {
   uint32_t count = 0, o1 = 0, o2 = 0, o3 = 0;  // sets so far; first blocks of the last three
-  // Opens the set of block n; false once a wait has given up.
-  template <int kStages>
+  // Opens the set of block n; false once a wait has given up. empty[] has a barrier for
+  // each kPer stages, told after the last of their blocks (at least 4 lie between).
+  template <int kStages, int kPer>
   __device__ __forceinline__ bool open(const Ctx& x, unsigned long long* empty, uint32_t n) {
-    static_assert(kStages <= kMaxStages, "a set's products are done when it is used again");
+    static_assert(kStages <= kMaxStages - (kPer - 1), "a set's products are done when it is used again");
+    static_assert(kPer <= 4, "a set's last products have been told of");
     bool ok = true;
     if (count >= kSfSets && n - (o3 - 1) < kStages) {
       const uint32_t last = o3 - 1;
-      ok = wait_lane(x, &empty[last % kStages], (last / kStages) & 1);
+      ok = wait_lane(x, &empty[last % kStages / kPer], (last / kStages) & 1);
     }
     o3 = o2;
     o2 = o1;

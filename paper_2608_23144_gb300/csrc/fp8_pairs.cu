@@ -43,7 +43,7 @@ constexpr int kGroup = 8;          // tiles of rows of x that are walked togethe
 struct Smem {
   uint8_t tile[kStages][kStageBytes];
   uint8_t sf[kStages][kSfBytes];
-  unsigned long long empty[kStages], acc_full[2];
+  unsigned long long empty[kStages / 2], acc_full[2];
   unsigned long long full[kStages], acc_empty[2], drain;  // of the even rank
   uint32_t tmem;
   int dead;
@@ -70,8 +70,10 @@ __device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(rank));
   return r;
 }
+// The default form: what has to be in order are reads of tensor memory, which tcgen05
+// fences order. A release of the cluster's scope waits for the results stored before.
 __device__ __forceinline__ void arrive_at(uint32_t mbar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
 }
 // As mbar_try_wait, for arrivals from the partner.
 __device__ __forceinline__ bool try_wait_cluster(unsigned long long* mb, uint32_t parity) {
@@ -189,7 +191,7 @@ __device__ void copy_role(const PairArgs& p, Smem& sm, const Ctx& x, uint32_t ha
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
       const uint32_t s = n % kStages;
       if ((int)n >= ahead) {
-        if (kb == a.stall || !wait_cluster(x, &sm.empty[s], ((n / kStages) & 1) ^ 1)) {
+        if (kb == a.stall || ((n & 1) == 0 && !wait_cluster(x, &sm.empty[s >> 1], ((n / kStages) & 1) ^ 1))) {
           ok = false;
           break;
         }
@@ -207,29 +209,37 @@ __device__ void copy_role(const PairArgs& p, Smem& sm, const Ctx& x, uint32_t ha
 
 template <bool kF32>
 __device__ void mma_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tmem, uint16_t both) {
-  uint32_t n = 0, c = 0;  // blocks, chunks so far
+  uint32_t n = 0, c = 0;           // blocks, chunks so far
+  uint32_t s = 0, phase = 0;       // stage of block n
   SfSets sets;
   bool ok = true;
-  const uint32_t bufs = a.n <= kTwoBufs ? 2 : 1, idesc0 = idesc_mx(2 * BM, a.n);
+  const uint32_t bufs = a.n <= kTwoBufs ? 2 : 1, idesc0 = idesc_mx(2 * BM, a.n), sfs = sf_tiles(a.n);
+  const uint64_t tile0 = desc_rows(smem_addr(sm.tile[0])), sf0 = desc_sf(smem_addr(sm.sf[0]));
   for (Walk w(a, kF32); ok && w.more(); w.next(a.n), ++c) {
     const uint32_t buf = c % bufs, d = tmem + buf * a.n;
+    const uint32_t shift = 4 + ((uint32_t)(w.tok & 127) >> 5);
+    uint32_t sfa = tmem + kSfAt + sets.at() * kSfCols;
     if (!(ok = wait_cluster(x, &sm.acc_empty[buf], ((c / bufs) & 1) ^ 1))) break;
     tc_fence_after();
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-      const uint32_t s = n % kStages;
-      if (!(ok = wait_cluster(x, &sm.full[s], (n / kStages) & 1))) break;
+      if (!(ok = wait_cluster(x, &sm.full[s], phase))) break;
       tc_fence_after();
       if ((kb & 3) == 0 || kb == w.lo) {
-        if (!(ok = sets.open<kStages>(x, sm.empty, n))) break;
-        const uint32_t at = tmem + kSfAt + sets.at() * kSfCols;
-        for (int i = 0; i < 1 + sf_tiles(a.n); ++i) copy_sf(at + 4 * i, desc_sf(smem_addr(sm.sf[s] + 512 * i)));
+        if (!(ok = sets.open<kStages, 2>(x, sm.empty, n))) break;
+        sfa = tmem + kSfAt + sets.at() * kSfCols;
+        const uint64_t ds = sf0 + s * (kSfBytes / 16);
+        copy_sf(sfa, ds);
+        copy_sf(sfa + 4, ds + 32);
+        if (sfs > 1) copy_sf(sfa + 8, ds + 64);
       }
-      const uint32_t sfa = tmem + kSfAt + sets.at() * kSfCols, sfb = sfa + 4 + ((uint32_t)(w.tok & 127) >> 5);
       const uint32_t idesc = with_sf_id(idesc0, kb & 3);
-      const uint64_t da = desc_rows(smem_addr(sm.tile[s])), db = desc_rows(smem_addr(sm.tile[s] + BM * 128));
+      const uint64_t da = tile0 + s * (kStageBytes / 16), db = da + BM * 128 / 16;
+      umma_mx(d, da, db, idesc, sfa, sfa + shift, kb != w.k0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfb, kb != w.k0 || j != 0);
-      commit_both(&sm.empty[s], both);
+      for (int j = 1; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfa + shift, 1);
+      // a commit holds the tensor cores up for 74 cycles (a block's products take 512): one for two stages
+      if (n & 1) commit_both(&sm.empty[s >> 1], both);
+      if (++s == kStages) s = 0, phase ^= 1;
     }
     if (ok) commit_both(&sm.acc_full[buf], both);
   }
@@ -306,7 +316,8 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_con
   const uint32_t rank = cluster_rank(), half = rank & 1, even = rank & ~1u;
   if (warp == kMmaWarp) {
     if ((threadIdx.x & 31) == 0) {
-      for (int i = 0; i < kStages; ++i) mbar_init(&sm.full[i], 1), mbar_init(&sm.empty[i], 1);
+      for (int i = 0; i < kStages; ++i) mbar_init(&sm.full[i], 1);
+      for (int i = 0; i < kStages / 2; ++i) mbar_init(&sm.empty[i], 1);
       for (int i = 0; i < 2; ++i) mbar_init(&sm.acc_full[i], 1), mbar_init(&sm.acc_empty[i], 16);
       mbar_init(&sm.drain, 1);
       sm.dead = 0;
