@@ -94,35 +94,45 @@ struct Walk {
 template <int N, bool kF32>
 __device__ void copy_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x) {
   using C = Cfg<N>;
+  const int lane = threadIdx.x & 31;
   const int64_t w8 = a.w.rows8(), x8 = a.x.rows8();
   const uint32_t xb = 128u * (uint32_t)x8;
-  uint32_t n = 0;
-  int ahead = 0;  // blocks whose rows of w are on their way before x is ready
   bool ok = true;
   Walk w(a, kF32);
   const auto has_sf = [&](int kb) { return (kb & 3) == 0 || kb == w.lo; };
-  const auto begin = [&](int kb, uint32_t s) {  // block kb of the tile to stage s: what comes of w
+  const auto copy_w = [&](int kb, uint32_t s) {  // block kb of the tile to stage s: what comes of w
     const int row = w.tile * BM;
     const uint32_t wb = 128u * (uint32_t)min((int64_t)BM, w8 - row);
     mbar_expect_tx(&sm.full[s], wb + xb + (has_sf(kb) ? 1024u : 0u));
     bulk_g2s(sm.tile[s], a.w.codes + (kb * w8 + row) * 128, wb, &sm.full[s]);
     if (has_sf(kb)) bulk_g2s(sm.sf[s], a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + w.tile) * 512, 512, &sm.full[s]);
   };
-  if (a.early && a.stall < 0 && w.more())
-    for (; ahead < min(C::kStages, w.hi - w.lo); ++ahead) begin(w.lo + ahead, ahead);
+  const auto copy_x = [&](int kb, uint32_t s) {
+    bulk_g2s(sm.tile[s] + BM * 128, a.x.codes + kb * x8 * 128, xb, &sm.full[s]);
+    if (has_sf(kb)) bulk_g2s(sm.sf[s] + 512, a.x.exps + (int64_t)(kb >> 2) * 512, 512, &sm.full[s]);
+  };
+  // the first blocks fill the stages, a lane each; rows of w are on their way before x is ready
+  int ahead = w.more() ? min(C::kStages, w.hi - w.lo) : 0;
+  if (a.stall >= 0) ahead = 0;
+  if (a.early && lane < ahead) copy_w(w.lo + lane, lane);
   step_wait();
+  if (lane < ahead) {
+    if (!a.early) copy_w(w.lo + lane, lane);
+    copy_x(w.lo + lane, lane);
+  }
+  __syncwarp();
+  if (lane != 0) return;
+  uint32_t n = 0;
   for (; ok && w.more(); w.next()) {
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
+      if ((int)n < ahead) continue;
       const uint32_t s = n % C::kStages;
-      if ((int)n >= ahead) {
-        if (kb == a.stall || !wait_lane(x, &sm.empty[s], ((n / C::kStages) & 1) ^ 1)) {
-          ok = false;
-          break;
-        }
-        begin(kb, s);
+      if (kb == a.stall || !wait_lane(x, &sm.empty[s], ((n / C::kStages) & 1) ^ 1)) {
+        ok = false;
+        break;
       }
-      bulk_g2s(sm.tile[s] + BM * 128, a.x.codes + kb * x8 * 128, xb, &sm.full[s]);
-      if (has_sf(kb)) bulk_g2s(sm.sf[s] + 512, a.x.exps + (int64_t)(kb >> 2) * 512, 512, &sm.full[s]);
+      copy_w(kb, s);
+      copy_x(kb, s);
     }
   }
   if (!ok)  // copies in flight land before the block ends
@@ -133,35 +143,44 @@ __device__ void copy_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x) {
 template <int N, bool kF32>
 __device__ void mma_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x, uint32_t tmem) {
   using C = Cfg<N>;
-  uint32_t n = 0, c = 0;  // blocks, chunks so far
+  uint32_t n = 0, c = 0;      // blocks, chunks so far
+  uint32_t s = 0, phase = 0;  // stage of block n
   SfSets sets;
   bool ok = true;
   const uint32_t idesc0 = idesc_mx(BM, N);
+  const uint64_t tile0 = desc_rows(smem_addr(sm.tile[0])), sf0 = desc_sf(smem_addr(sm.sf[0]));
   for (Walk w(a, kF32); ok && w.more(); w.next(), ++c) {
-    const uint32_t buf = c & 1;
-    if (!(ok = wait_lane(x, &sm.acc_empty[buf], ((c >> 1) & 1) ^ 1))) break;
+    const uint32_t buf = c & 1, d = tmem + buf * N;
+    uint32_t sfa = tmem + C::kAccCols + sets.at() * C::kSfCols;
+    if (!(ok = wait_warp(x, &sm.acc_empty[buf], ((c >> 1) & 1) ^ 1))) break;
     tc_fence_after();
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-      const uint32_t s = n % C::kStages;
-      if (!(ok = wait_lane(x, &sm.full[s], (n / C::kStages) & 1))) break;
+      if (!(ok = wait_warp(x, &sm.full[s], phase))) break;
       tc_fence_after();
-      if ((kb & 3) == 0 || kb == w.lo) {
+      const bool sf = (kb & 3) == 0 || kb == w.lo;
+      if (sf) {
         if (!(ok = sets.open<C::kStages, 1>(x, sm.empty, n))) break;
-        const uint32_t at = tmem + C::kAccCols + sets.at() * C::kSfCols;
-        copy_sf(at, desc_sf(smem_addr(sm.sf[s])));
-        copy_sf(at + 4, desc_sf(smem_addr(sm.sf[s] + 512)));
+        sfa = tmem + C::kAccCols + sets.at() * C::kSfCols;
       }
-      const uint32_t sfa = tmem + C::kAccCols + sets.at() * C::kSfCols;
+      const uint64_t ds = sf0 + s * (1024 / 16);
       const uint32_t idesc = with_sf_id(idesc0, kb & 3);
-      const uint64_t da = desc_rows(smem_addr(sm.tile[s])), db = desc_rows(smem_addr(sm.tile[s] + BM * 128));
+      const uint64_t da = tile0 + s * (C::kStageBytes / 16), db = da + BM * 128 / 16;
+      if (one_lane()) {
+        if (sf) {
+          copy_sf(sfa, ds);
+          copy_sf(sfa + 4, ds + 32);
+        }
+        umma_mx(d, da, db, idesc, sfa, sfa + 4, kb != w.k0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        umma_mx(tmem + buf * N, da + 2 * j, db + 2 * j, idesc, sfa, sfa + 4, kb != w.k0 || j != 0);
-      umma_commit(&sm.empty[s]);
+        for (int j = 1; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfa + 4, 1);
+        umma_commit(&sm.empty[s]);
+        if (kb + 1 == w.k1) umma_commit(&sm.acc_full[buf]);
+      }
+      __syncwarp();
+      if (++s == C::kStages) s = 0, phase ^= 1;
     }
-    if (ok) umma_commit(&sm.acc_full[buf]);
   }
-  if (!ok) {  // products in flight end before the block does
+  if (!ok && one_lane()) {  // products in flight end before the block does
     umma_commit(&sm.drain);
     (void)mbar_wait(&sm.drain, 0, x.wait_ns);
   }
@@ -241,9 +260,10 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_few_kernel(const __grid_const
   if (warp < 8) {
     step_wait();
     write_role<N, kF32>(a, sm, x, tmem);
-  } else if ((threadIdx.x & 31) == 0) {
-    if (warp == kCopyWarp) copy_role<N, kF32>(a, sm, x);
-    else mma_role<N, kF32>(a, sm, x, tmem);
+  } else if (warp == kCopyWarp) {
+    copy_role<N, kF32>(a, sm, x);
+  } else {
+    mma_role<N, kF32>(a, sm, x, tmem);
   }
   __syncwarp();
   tc_fence_before();

@@ -40,6 +40,15 @@ __device__ __forceinline__ bool wait_warp(const Ctx& x, unsigned long long* mb, 
   return __all_sync(0xffffffffu, wait_lane(x, mb, parity));
 }
 
+// One lane of a converged warp. The products' warp runs as a whole, so that what its
+// instructions take is computed once per warp, and one lane issues them: a lane that
+// ran alone took 340 ns a block, whatever the products.
+__device__ __forceinline__ bool one_lane() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+
 // Scales of 4 blocks lie in tensor memory in one of 4 sets, used in turn. Set k + 4
 // overwrites set k, whose products must be done: with 4 blocks a set they are, as the
 // ring of stages has been around since (13 blocks lie between, kMaxStages is no more);
@@ -56,7 +65,7 @@ struct SfSets {
     bool ok = true;
     if (count >= kSfSets && n - (o3 - 1) < kStages) {
       const uint32_t last = o3 - 1;
-      ok = wait_lane(x, &empty[last % kStages / kPer], (last / kStages) & 1);
+      ok = wait_warp(x, &empty[last % kStages / kPer], (last / kStages) & 1);
     }
     o3 = o2;
     o2 = o1;

@@ -102,6 +102,9 @@ __device__ __noinline__ bool wait_cluster_slow(const Ctx& x, unsigned long long*
 __device__ __forceinline__ bool wait_cluster(const Ctx& x, unsigned long long* mb, uint32_t parity) {
   return try_wait_cluster(mb, parity) || wait_cluster_slow(x, mb, parity);
 }
+__device__ __forceinline__ bool wait_cluster_warp(const Ctx& x, unsigned long long* mb, uint32_t parity) {
+  return __all_sync(0xffffffffu, wait_cluster(x, mb, parity));
+}
 
 __device__ __forceinline__ void copy_sf(uint32_t taddr, uint64_t desc) {  // in both thread blocks, each from its own
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
@@ -172,34 +175,44 @@ template <bool kF32>
 __device__ void copy_role(const PairArgs& p, Smem& sm, const Ctx& x, uint32_t half, uint32_t even) {
   const GemmArgs& a = p.g;
   uint32_t n = 0;
-  int ahead = 0;  // blocks whose rows of w are on their way before x is ready
+  int ahead;  // blocks whose copies begin together
   bool ok = true;
   Walk w(a, kF32);
   const int half_n = a.n >> 1;
   const uint32_t bytes = 2u * (BM * 128u + half_n * 128u), sf_bytes = 2u * 512u * (1 + sf_tiles(a.n));
   const auto has_sf = [&](int kb) { return (kb & 3) == 0 || kb == w.lo; };
-  const auto begin = [&](int kb, uint32_t s) {  // what comes of w; the even rank's barrier counts both thread blocks' bytes
+  const auto copy_x = [&](int kb, uint32_t s) {
+    const uint32_t mbar = peer_addr(&sm.full[s], even);
+    copy_box(sm.tile[s] + BM * 128, &p.x_codes, w.tok + half_n * half, kb, mbar);
+    if (has_sf(kb)) copy_box(sm.sf[s] + 512, &p.x_exps, w.tok >> 7, kb >> 2, mbar);
+  };
+  const auto copy_w = [&](int kb, uint32_t s) {  // what comes of w; the even rank's barrier counts both thread blocks' bytes
     const uint32_t mbar = peer_addr(&sm.full[s], even);
     if (!half) mbar_expect_tx(&sm.full[s], bytes + (has_sf(kb) ? sf_bytes : 0u));
     copy_box(sm.tile[s], &p.w_codes, w.row + BM * half, kb, mbar);
     if (has_sf(kb)) copy_box(sm.sf[s], &p.w_exps, (w.row >> 7) + half, kb >> 2, mbar);
   };
-  if (a.early && a.stall < 0 && w.more())
-    for (; ahead < min(kStages, w.hi - w.lo); ++ahead) begin(w.lo + ahead, ahead);
+  // the first blocks fill the stages, a lane each; rows of w are on their way before x is ready
+  const int lane = threadIdx.x & 31;
+  ahead = w.more() && a.stall < 0 ? min(kStages, w.hi - w.lo) : 0;
+  if (a.early && lane < ahead) copy_w(w.lo + lane, lane);
   step_wait();
+  if (lane < ahead) {
+    if (!a.early) copy_w(w.lo + lane, lane);
+    copy_x(w.lo + lane, lane);
+  }
+  __syncwarp();
+  if (lane != 0) return;
   for (; ok && w.more(); w.next(a.n)) {
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
+      if ((int)n < ahead) continue;
       const uint32_t s = n % kStages;
-      if ((int)n >= ahead) {
-        if (kb == a.stall || ((n & 1) == 0 && !wait_cluster(x, &sm.empty[s >> 1], ((n / kStages) & 1) ^ 1))) {
-          ok = false;
-          break;
-        }
-        begin(kb, s);
+      if (kb == a.stall || ((n & 1) == 0 && !wait_cluster(x, &sm.empty[s >> 1], ((n / kStages) & 1) ^ 1))) {
+        ok = false;
+        break;
       }
-      const uint32_t mbar = peer_addr(&sm.full[s], even);
-      copy_box(sm.tile[s] + BM * 128, &p.x_codes, w.tok + half_n * half, kb, mbar);
-      if (has_sf(kb)) copy_box(sm.sf[s] + 512, &p.x_exps, w.tok >> 7, kb >> 2, mbar);
+      copy_w(kb, s);
+      copy_x(kb, s);
     }
   }
   if (!ok && !half)  // copies in flight, the partner's too, land before either block ends
@@ -219,31 +232,37 @@ __device__ void mma_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tme
     const uint32_t buf = c % bufs, d = tmem + buf * a.n;
     const uint32_t shift = 4 + ((uint32_t)(w.tok & 127) >> 5);
     uint32_t sfa = tmem + kSfAt + sets.at() * kSfCols;
-    if (!(ok = wait_cluster(x, &sm.acc_empty[buf], ((c / bufs) & 1) ^ 1))) break;
+    if (!(ok = wait_cluster_warp(x, &sm.acc_empty[buf], ((c / bufs) & 1) ^ 1))) break;
     tc_fence_after();
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-      if (!(ok = wait_cluster(x, &sm.full[s], phase))) break;
+      if (!(ok = wait_cluster_warp(x, &sm.full[s], phase))) break;
       tc_fence_after();
-      if ((kb & 3) == 0 || kb == w.lo) {
+      const bool sf = (kb & 3) == 0 || kb == w.lo;
+      if (sf) {
         if (!(ok = sets.open<kStages, 2>(x, sm.empty, n))) break;
         sfa = tmem + kSfAt + sets.at() * kSfCols;
-        const uint64_t ds = sf0 + s * (kSfBytes / 16);
-        copy_sf(sfa, ds);
-        copy_sf(sfa + 4, ds + 32);
-        if (sfs > 1) copy_sf(sfa + 8, ds + 64);
       }
-      const uint32_t idesc = with_sf_id(idesc0, kb & 3);
+      const uint64_t ds = sf0 + s * (kSfBytes / 16);
+      const uint32_t idesc = with_sf_id(idesc0, kb & 3), sfb = sfa + shift;
       const uint64_t da = tile0 + s * (kStageBytes / 16), db = da + BM * 128 / 16;
-      umma_mx(d, da, db, idesc, sfa, sfa + shift, kb != w.k0);
+      if (one_lane()) {
+        if (sf) {
+          copy_sf(sfa, ds);
+          copy_sf(sfa + 4, ds + 32);
+          if (sfs > 1) copy_sf(sfa + 8, ds + 64);
+        }
+        umma_mx(d, da, db, idesc, sfa, sfb, kb != w.k0);
 #pragma unroll
-      for (int j = 1; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfa + shift, 1);
-      // a commit holds the tensor cores up for 74 cycles (a block's products take 512): one for two stages
-      if (n & 1) commit_both(&sm.empty[s >> 1], both);
+        for (int j = 1; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfb, 1);
+        // a commit holds the tensor cores up for 74 cycles (a block's products take 512): one for two stages
+        if (n & 1) commit_both(&sm.empty[s >> 1], both);
+        if (kb + 1 == w.k1) commit_both(&sm.acc_full[buf], both);
+      }
+      __syncwarp();
       if (++s == kStages) s = 0, phase ^= 1;
     }
-    if (ok) commit_both(&sm.acc_full[buf], both);
   }
-  if (!ok) {  // products in flight end before the block does
+  if (!ok && one_lane()) {  // products in flight end before the block does
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(&sm.drain)) : "memory");
     (void)mbar_wait(&sm.drain, 0, x.wait_ns);
   }
@@ -339,9 +358,10 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_con
   if (warp < 8) {
     step_wait();
     write_role<kF32>(a, sm, x, tmem, half, even);
-  } else if ((threadIdx.x & 31) == 0) {
-    if (warp == kCopyWarp) copy_role<kF32>(p, sm, x, half, even);
-    else if (!half) mma_role<kF32>(a, sm, x, tmem, (uint16_t)(3u << even));
+  } else if (warp == kCopyWarp) {
+    copy_role<kF32>(p, sm, x, half, even);
+  } else if (!half) {
+    mma_role<kF32>(a, sm, x, tmem, (uint16_t)(3u << even));
   }
   __syncwarp();
   tc_fence_before();
