@@ -121,18 +121,33 @@ __device__ void copy_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x) {
     copy_x(w.lo + lane, lane);
   }
   __syncwarp();
-  if (lane != 0) return;
-  uint32_t n = 0;
+  uint32_t n = 0;             // blocks so far
+  uint32_t s = 0, phase = 1;  // stage of block n
+  const int64_t w_step = w8 * 128, x_step = x8 * 128;
   for (; ok && w.more(); w.next()) {
-    for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-      if ((int)n < ahead) continue;
-      const uint32_t s = n % C::kStages;
-      if (kb == a.stall || !wait_lane(x, &sm.empty[s], ((n / C::kStages) & 1) ^ 1)) {
-        ok = false;
-        break;
+    const int row = w.tile * BM;
+    const uint32_t wb = 128u * (uint32_t)min((int64_t)BM, w8 - row);
+    const uint8_t *wp = a.w.codes + w.k0 * w_step + row * 128ll, *xp = a.x.codes + w.k0 * x_step;
+    for (int kb = w.k0; kb < w.k1; ++kb, ++n, wp += w_step, xp += x_step) {
+      if ((int)n >= ahead) {
+        if (kb == a.stall || !wait_warp(x, &sm.empty[s], phase)) {
+          ok = false;
+          break;
+        }
+        const bool sf = has_sf(kb);
+        const uint8_t *ws = a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + w.tile) * 512, *xs = a.x.exps + (int64_t)(kb >> 2) * 512;
+        if (one_lane()) {
+          mbar_expect_tx(&sm.full[s], wb + xb + (sf ? 1024u : 0u));
+          bulk_g2s(sm.tile[s], wp, wb, &sm.full[s]);
+          bulk_g2s(sm.tile[s] + BM * 128, xp, xb, &sm.full[s]);
+          if (sf) {
+            bulk_g2s(sm.sf[s], ws, 512, &sm.full[s]);
+            bulk_g2s(sm.sf[s] + 512, xs, 512, &sm.full[s]);
+          }
+        }
+        __syncwarp();
       }
-      copy_w(kb, s);
-      copy_x(kb, s);
+      if (++s == C::kStages) s = 0, phase ^= 1;
     }
   }
   if (!ok)  // copies in flight land before the block ends

@@ -202,17 +202,30 @@ __device__ void copy_role(const PairArgs& p, Smem& sm, const Ctx& x, uint32_t ha
     copy_x(w.lo + lane, lane);
   }
   __syncwarp();
-  if (lane != 0) return;
+  uint32_t s = 0, phase = 1;  // stage of block n
+  const uint32_t full0 = peer_addr(&sm.full[0], even);
   for (; ok && w.more(); w.next(a.n)) {
+    const int row = w.row + BM * half, tok = w.tok + half_n * half;
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-      if ((int)n < ahead) continue;
-      const uint32_t s = n % kStages;
-      if (kb == a.stall || ((n & 1) == 0 && !wait_cluster(x, &sm.empty[s >> 1], ((n / kStages) & 1) ^ 1))) {
-        ok = false;
-        break;
+      if ((int)n >= ahead) {
+        if (kb == a.stall || ((n & 1) == 0 && !wait_cluster_warp(x, &sm.empty[s >> 1], phase))) {
+          ok = false;
+          break;
+        }
+        const bool sf = has_sf(kb);
+        const uint32_t mbar = full0 + 8 * s;
+        if (one_lane()) {
+          if (!half) mbar_expect_tx(&sm.full[s], bytes + (sf ? sf_bytes : 0u));
+          copy_box(sm.tile[s], &p.w_codes, row, kb, mbar);
+          copy_box(sm.tile[s] + BM * 128, &p.x_codes, tok, kb, mbar);
+          if (sf) {
+            copy_box(sm.sf[s], &p.w_exps, (w.row >> 7) + half, kb >> 2, mbar);
+            copy_box(sm.sf[s] + 512, &p.x_exps, w.tok >> 7, kb >> 2, mbar);
+          }
+        }
+        __syncwarp();
       }
-      copy_w(kb, s);
-      copy_x(kb, s);
+      if (++s == kStages) s = 0, phase ^= 1;
     }
   }
   if (!ok && !half)  // copies in flight, the partner's too, land before either block ends
