@@ -46,6 +46,7 @@ awsrc_status gemm_args(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, voi
   if ((int64_t)a.w.tiles() * ((a.x.rows + 15) / 16) > INT_MAX / 2) return AWSRC_ERR_UNSUPPORTED;
   a.y = y;
   a.ys = y_stride;
+  a.y_f32 = y_dtype == AWSRC_DTYPE_F32;
   a.status = static_cast<uint32_t*>(workspace);
   a.wait_ns = wait_limit_ns();
   a.stall = wait_test_stall();
@@ -145,7 +146,7 @@ awsrc_status awsrc_fp8_gemm(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w
   const awsrc_status s = gemm_args(x, w, y, y_dtype, y_stride, workspace, workspace_bytes, &a);
   if (s != AWSRC_OK) return s;
   if (a.x.rows == 0 || a.w.rows == 0) return AWSRC_OK;
-  const cudaError_t e = launch_fp8_gemm(a, y_dtype, (cudaStream_t)stream);
+  const cudaError_t e = launch_fp8_gemm(a, (cudaStream_t)stream);
   return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "fp8_gemm");
 }
 
@@ -157,10 +158,17 @@ awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, 
   if (s != AWSRC_OK || (s = check_rows(x, x_dtype)) != AWSRC_OK) return s;
   if (x8->codes == w->codes || x8->exps == w->exps) return AWSRC_ERR_INVALID_ARG;
   if (a.x.rows == 0 || a.w.rows == 0) return AWSRC_OK;
-  // the quantising kernel lets the product start only after it has waited for all kernels before it
-  a.early = 1;
-  cudaError_t e = launch_fp8_quantize(x, x_dtype, x_stride, a.x, (cudaStream_t)stream);
-  if (e == cudaSuccess) e = launch_fp8_gemm(a, y_dtype, (cudaStream_t)stream);
+  cudaError_t e = cudaSuccess;
+  if (fp8_gemm_quantizes(a)) {
+    a.raw = x;
+    a.raw_stride = x_stride;
+    a.raw_bf16 = x_dtype == AWSRC_DTYPE_BF16;
+  } else {
+    // the quantising kernel lets the product start only after it has waited for all kernels before it
+    a.early = 1;
+    e = launch_fp8_quantize(x, x_dtype, x_stride, a.x, (cudaStream_t)stream);
+  }
+  if (e == cudaSuccess) e = launch_fp8_gemm(a, (cudaStream_t)stream);
   return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "fp8_linear");
 }
 

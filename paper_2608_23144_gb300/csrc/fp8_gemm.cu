@@ -7,18 +7,27 @@
 // (kind::mxf8f6f4, scales of 8 exponent bits): one scale stands for four groups of
 // 32 columns, the same byte for each of a block's four products.
 //
-// Few rows of x (up to 64: single tokens, drafts): the bytes of w bound it. A tile is
-// 128 rows of w (tensor memory's lanes) x N rows of x (columns). Warp 8 copies: both
-// matrices lie in memory as the tensor cores read them (rows of 128 bytes, their
-// 16-byte pieces exchanged by row), so a block's rows are one bulk copy each, and a
-// ring of stages as deep as shared memory keeps 200 KB per SM in flight. Rows of w
-// start on their way while x is still being quantised. Warp 9 issues the products,
-// warps 0-7 read the sums and write y. Few tiles: a cluster shares a tile's columns
-// and joins its parts, in their order, through shared memory.
+// Few rows of x (up to 64: single tokens, drafts): the bytes of w bound it. A tile is R
+// rows of w (tensor memory's lanes, up to 128 used) x N rows of x (columns), R such that
+// every SM has the same share: one SM draws 50 GB/s, so the copy rate needs all of them.
+//   Warp 8 copies: codes lie in memory as the tensor cores read them (rows of 128 bytes,
+//     their 16-byte pieces exchanged by row), so a block's rows are one bulk copy, and a
+//     ring of stages keeps the memory busy.
+//   Up to 16 rows of x lie in shared memory before the products start, their codes copied
+//     or, by warps 0-7, made here: a kernel for that in front took 2.5 to 4 us until the
+//     products could start. Longer x, and 17 to 64 rows, come with w, block by block (made
+//     here block by block, 40 rows took 29 us where both kernels took 17: each stage waited
+//     for a copy, the codes and a fence).
+//   Warp 10 puts the scales of the tile's rows of w in the order of its lanes. Warp 9
+//     issues the products (270 ns a block whatever N: the cores read w's 128 rows at 64
+//     bytes per cycle); warps 0-7 read the sums and write y.
+// Few rows of w: a cluster shares a tile's columns and joins its parts, in their order,
+// through shared memory.
 //
 // Every wait is bounded (wait_ns): one that runs out sets bit 2 of the fault word,
 // stops the block's roles, waits (bounded) for its copies and products in flight
 // and frees the tensor memory.
+#include "fp8_codes.cuh"
 #include "fp8_mma.cuh"
 #include "internal.h"
 
@@ -28,29 +37,40 @@ namespace {
 
 using namespace fp8;
 
+constexpr int kThreads = 352, kXWarps = 8, kCopyWarp = 8, kMmaWarp = 9, kScaleWarp = 10;
 constexpr int kMaxSplit = 8;  // thread blocks that share a tile's columns
-constexpr int kLeast = 4;     // blocks that one of them has at least
+constexpr int kSms = 152;
 
-template <int N>
+// Where x comes from: its codes with the blocks of w; all codes first; all rows first, quantised here.
+enum Source { kCodes, kCodesFirst, kF32First, kBf16First };
+
+template <int N, Source X>
 struct Cfg {
-  static constexpr int kStageBytes = (BM + N) * 128;
-  static constexpr int kStages = N > 32 ? 8 : N > 16 ? 10 : 11;
-  static constexpr int kAccCols = 2 * N;  // two accumulators
-  static constexpr int kSfCols = 8;       // a set of scales: 4 columns for w, 4 for x
+  static constexpr bool kFirst = X != kCodes, kRaw = X == kF32First || X == kBf16First;
+  static constexpr int kXAt = BM * 128;  // in a stage: rows of w, then of x
+  static constexpr int kStageBytes = kXAt + (kFirst ? 0 : N * 128);
+  static constexpr int kStages = kFirst ? 8 : N > 32 ? 8 : 10;
+  static constexpr int kXBytes = kFirst ? 64 * 1024 : 0;  // codes of x that come first
+  static constexpr int kXGroups = kFirst ? 18 : kStages;  // their scales, 512 bytes for 4 blocks; else of a stage
+  static constexpr int kAccCols = 2 * N;                  // two accumulators
+  static constexpr int kSfCols = 8;                       // a set of scales: 4 columns for w, 4 for x
   static constexpr int kCols = kAccCols + kSfSets * kSfCols;
   static constexpr int kTmem = kCols > 128 ? 256 : 128;
-  static constexpr int kPer = N / 2;  // columns of an epilogue thread
 };
 
-template <int N>
+template <int N, Source X>
 struct Smem {
-  using C = Cfg<N>;
+  using C = Cfg<N, X>;
   uint8_t tile[C::kStages][C::kStageBytes];
-  uint8_t sf[C::kStages][1024];  // scales of w, of x
-  unsigned long long full[C::kStages], empty[C::kStages], acc_full[2], acc_empty[2], drain;
+  uint8_t x[C::kXBytes + 1024];  // a block's last rows of 16 may lie in the next one's place
+  uint8_t sf_w[C::kStages][512], sf_raw[C::kStages][1024], sf_x[C::kXGroups][512];
+  unsigned long long full[C::kStages], empty[C::kStages / 2], raw_full[C::kStages], acc_full[2], acc_empty[2], x_full, drain;
   uint32_t tmem;
   int dead;
 };
+
+// Bytes of a block of x's codes: 8 or 16 rows.
+__device__ __forceinline__ uint32_t x_block(const GemmArgs& a) { return a.x.rows8() * 128; }
 
 __device__ __forceinline__ void copy_sf(uint32_t taddr, uint64_t desc) {  // 512 bytes to 4 columns, in all lanes' quarters
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
@@ -70,14 +90,14 @@ __device__ __forceinline__ void umma_mx(uint32_t d, uint64_t a, uint64_t b, uint
 struct Walk {
   int tiles, chunk, step;
   int tile, lo, hi, k0, k1;
-  __device__ Walk(const GemmArgs& a, bool f32) {
-    tiles = a.w.tiles();  // one tile of rows of x
-    const int blocks = a.x.blocks(), rank = blockIdx.x % a.split;
-    step = gridDim.x / a.split;
-    tile = blockIdx.x / a.split;
-    lo = (int)((int64_t)blocks * rank / a.split);
-    hi = (int)((int64_t)blocks * (rank + 1) / a.split);
-    chunk = f32 ? kChunk : blocks;
+  __device__ explicit Walk(const GemmArgs& a) {
+    tiles = (a.w.rows + a.n - 1) / a.n;
+    const unsigned blocks = a.w.blocks(), split = a.split, rank = blockIdx.x % split;  // at most 2^17 blocks, 8 shares
+    step = gridDim.x / split;
+    tile = blockIdx.x / split;
+    lo = blocks * rank / split;
+    hi = blocks * (rank + 1) / split;
+    chunk = a.y_f32 ? kChunk : (int)blocks;
     k0 = lo;
     k1 = min(k0 + chunk, hi);
   }
@@ -91,108 +111,186 @@ struct Walk {
   }
 };
 
-template <int N, bool kF32>
-__device__ void copy_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x) {
-  using C = Cfg<N>;
+// ------------------------------------------------------------------- copies
+template <int N, Source X>
+__device__ void copy_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x) {
+  using C = Cfg<N, X>;
   const int lane = threadIdx.x & 31;
-  const int64_t w8 = a.w.rows8(), x8 = a.x.rows8();
-  const uint32_t xb = 128u * (uint32_t)x8;
-  bool ok = true;
-  Walk w(a, kF32);
+  const int64_t w8 = a.w.rows8(), w_step = w8 * 128;
+  const uint32_t xb = x_block(a);
+  Walk w(a);
   const auto has_sf = [&](int kb) { return (kb & 3) == 0 || kb == w.lo; };
-  const auto copy_w = [&](int kb, uint32_t s) {  // block kb of the tile to stage s: what comes of w
-    const int row = w.tile * BM;
-    const uint32_t wb = 128u * (uint32_t)min((int64_t)BM, w8 - row);
-    mbar_expect_tx(&sm.full[s], wb + xb + (has_sf(kb) ? 1024u : 0u));
-    bulk_g2s(sm.tile[s], a.w.codes + (kb * w8 + row) * 128, wb, &sm.full[s]);
-    if (has_sf(kb)) bulk_g2s(sm.sf[s], a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + w.tile) * 512, 512, &sm.full[s]);
+  const auto copy_w = [&](int kb, uint32_t s, const uint8_t* rows) {
+    const int row = w.tile * a.n;
+    const uint32_t bytes = 128u * (uint32_t)min((int64_t)a.n, w8 - row);
+    mbar_expect_tx(&sm.full[s], bytes + (C::kFirst ? 0u : xb + (has_sf(kb) ? 512u : 0u)));
+    bulk_g2s(sm.tile[s], rows, bytes, &sm.full[s]);
+    // scales of the one or two tiles of 128 rows that this tile's rows lie in
+    const uint32_t sf = has_sf(kb) ? 512u * (uint32_t)min(2, a.w.tiles() - (row >> 7)) : 0u;
+    mbar_expect_tx(&sm.raw_full[s], sf);
+    if (sf) bulk_g2s(sm.sf_raw[s], a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + (row >> 7)) * 512, sf, &sm.raw_full[s]);
   };
   const auto copy_x = [&](int kb, uint32_t s) {
-    bulk_g2s(sm.tile[s] + BM * 128, a.x.codes + kb * x8 * 128, xb, &sm.full[s]);
-    if (has_sf(kb)) bulk_g2s(sm.sf[s] + 512, a.x.exps + (int64_t)(kb >> 2) * 512, 512, &sm.full[s]);
+    bulk_g2s(sm.tile[s] + C::kXAt, a.x.codes + (int64_t)kb * xb, xb, &sm.full[s]);
+    if (has_sf(kb)) bulk_g2s(sm.sf_x[s], a.x.exps + (int64_t)(kb >> 2) * 512, 512, &sm.full[s]);
   };
-  // the first blocks fill the stages, a lane each; rows of w are on their way before x is ready
-  int ahead = w.more() ? min(C::kStages, w.hi - w.lo) : 0;
-  if (a.stall >= 0) ahead = 0;
-  if (a.early && lane < ahead) copy_w(w.lo + lane, lane);
-  step_wait();
-  if (lane < ahead) {
-    if (!a.early) copy_w(w.lo + lane, lane);
-    copy_x(w.lo + lane, lane);
+  int ahead = 0;
+  if (a.early && a.stall < 0 && w.more()) {
+    ahead = min(C::kStages, w.hi - w.lo);
+    if (lane < ahead) copy_w(w.lo + lane, lane, a.w.codes + (w.lo + lane) * w_step + w.tile * a.n * 128ll);
+    __syncwarp();
   }
-  __syncwarp();
-  uint32_t n = 0;             // blocks so far
-  uint32_t s = 0, phase = 1;  // stage of block n
-  const int64_t w_step = w8 * 128, x_step = x8 * 128;
+  step_wait();
+  if (X == kCodesFirst && w.more()) {
+    if (lane == 0) {
+      const int g0 = w.lo >> 2, groups = ((w.hi - 1) >> 2) - g0 + 1;
+      mbar_expect_tx(&sm.x_full, (w.hi - w.lo) * xb + groups * 512u);
+    }
+    __syncwarp();
+    for (int kb = w.lo + lane; kb < w.hi; kb += 32) {
+      bulk_g2s(sm.x + (kb - w.lo) * xb, a.x.codes + (int64_t)kb * xb, xb, &sm.x_full);
+      if (has_sf(kb)) bulk_g2s(sm.sf_x[(kb >> 2) - (w.lo >> 2)], a.x.exps + (int64_t)(kb >> 2) * 512, 512, &sm.x_full);
+    }
+    __syncwarp();
+  }
+  uint32_t n = 0, s = 0, phase = 1;  // blocks so far; stage of block n
+  bool ok = true;
   for (; ok && w.more(); w.next()) {
-    const int row = w.tile * BM;
-    const uint32_t wb = 128u * (uint32_t)min((int64_t)BM, w8 - row);
-    const uint8_t *wp = a.w.codes + w.k0 * w_step + row * 128ll, *xp = a.x.codes + w.k0 * x_step;
-    for (int kb = w.k0; kb < w.k1; ++kb, ++n, wp += w_step, xp += x_step) {
-      if ((int)n >= ahead) {
-        if (kb == a.stall || !wait_warp(x, &sm.empty[s], phase)) {
-          ok = false;
-          break;
-        }
-        const bool sf = has_sf(kb);
-        const uint8_t *ws = a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + w.tile) * 512, *xs = a.x.exps + (int64_t)(kb >> 2) * 512;
-        if (one_lane()) {
-          mbar_expect_tx(&sm.full[s], wb + xb + (sf ? 1024u : 0u));
-          bulk_g2s(sm.tile[s], wp, wb, &sm.full[s]);
-          bulk_g2s(sm.tile[s] + BM * 128, xp, xb, &sm.full[s]);
-          if (sf) {
-            bulk_g2s(sm.sf[s], ws, 512, &sm.full[s]);
-            bulk_g2s(sm.sf[s] + 512, xs, 512, &sm.full[s]);
-          }
-        }
-        __syncwarp();
+    const uint8_t* rows = a.w.codes + w.k0 * w_step + w.tile * a.n * 128ll;
+    for (int kb = w.k0; kb < w.k1; ++kb, ++n, rows += w_step) {
+      if (kb == a.stall || ((s & 1) == 0 && !wait_warp(x, &sm.empty[s >> 1], phase))) {
+        ok = false;
+        break;
       }
+      if (one_lane()) {
+        if (!C::kFirst) copy_x(kb, s);
+        if ((int)n >= ahead) copy_w(kb, s, rows);
+      }
+      __syncwarp();
       if (++s == C::kStages) s = 0, phase ^= 1;
     }
   }
-  if (!ok)  // copies in flight land before the block ends
+  if (!ok)  // copies in flight land before the block ends; where others did not come, the limit is time enough for all
     for (uint32_t j = n > C::kStages ? n - C::kStages : 0; j < n; ++j)
-      (void)mbar_wait(&sm.full[j % C::kStages], (j / C::kStages) & 1, x.wait_ns);
+      if (!mbar_wait(&sm.full[j % C::kStages], (j / C::kStages) & 1, x.wait_ns)) break;
 }
 
-template <int N, bool kF32>
-__device__ void mma_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x, uint32_t tmem) {
-  using C = Cfg<N>;
+// --------------------------------------------------- scales of the rows of w
+// The scale word of row r of the tile goes to lane r % 32, word r / 32.
+template <int N, Source X>
+__device__ void scale_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x) {
+  using C = Cfg<N, X>;
+  const int lane = threadIdx.x & 31;
+  uint32_t s = 0, phase = 0;
+  for (Walk w(a); w.more(); w.next())
+    for (int kb = w.k0; kb < w.k1; ++kb) {
+      if (!wait_warp(x, &sm.raw_full[s], phase)) return;
+      if ((kb & 3) == 0 || kb == w.lo) {
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = (w.tile * a.n & 127) + lane + 32 * i;
+          v[i] = r < 256 ? *reinterpret_cast<const uint32_t*>(&sm.sf_raw[s][(r >> 7) * 512 + (r & 31) * 16 + ((r & 127) >> 5) * 4]) : 0u;
+        }
+        *reinterpret_cast<uint4*>(&sm.sf_w[s][lane * 16]) = make_uint4(v[0], v[1], v[2], v[3]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
+      if (lane == 0) mbar_arrive(&sm.full[s]);
+      if (++s == C::kStages) s = 0, phase ^= 1;
+    }
+}
+
+// --------------------------------------------------------------- codes of x
+__device__ __forceinline__ void get4(const float* p, int have, bool vec, float* v) { vec ? load4<true>(p, have, v) : load4<false>(p, have, v); }
+__device__ __forceinline__ void get4(const __nv_bfloat16* p, int have, bool vec, float* v) { vec ? load4<true>(p, have, v) : load4<false>(p, have, v); }
+
+// All of this block's columns of all rows of x: (row, block) pairs over the warps, four in flight.
+template <int N, Source X, typename T>
+__device__ void quantize_role(const GemmArgs& a, Smem<N, X>& sm) {
+  constexpr int kAhead = 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, M = a.x.rows, blocks = a.w.blocks();
+  const uint32_t xb = x_block(a);
+  const Walk w(a);
+  const int pairs = w.more() ? (w.hi - w.lo) * M : 0;
+  step_wait();
+  for (int p0 = warp; p0 < pairs; p0 += kAhead * kXWarps) {
+    float v[kAhead][4];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int p = p0 + i * kXWarps, kb = w.lo + p / M, r = p % M;
+      if (p < pairs)
+        get4(static_cast<const T*>(a.raw) + r * a.raw_stride + 128ll * kb + 4 * lane, a.x.cols - (128 * kb + 4 * lane), a.vec_raw, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int p = p0 + i * kXWarps, kb = w.lo + p / M, r = p % M;
+      if (p >= pairs) break;
+      const Codes4 c = codes_of(v[i], a.x.cols - (128 * kb + 4 * lane));
+      const int at = r * 128 + 16 * ((lane >> 2) ^ (r & 7)) + 4 * (lane & 3);
+      const bool keep = kb % w.tiles == w.tile;  // each block's codes are left in x8 by one tile's thread block
+      *reinterpret_cast<uint32_t*>(sm.x + (kb - w.lo) * xb + at) = c.codes;
+      if (keep) *reinterpret_cast<uint32_t*>(a.x.codes + (int64_t)kb * xb + at) = c.codes;
+      if (lane == 0) {
+        sm.sf_x[(kb >> 2) - (w.lo >> 2)][r * 16 + (kb & 3)] = (uint8_t)c.biased;
+        if (keep) {
+          uint8_t* e = a.x.exps + (int64_t)(kb >> 2) * 512 + r * 16;
+          e[kb & 3] = (uint8_t)c.biased;
+          if (kb + 1 == blocks)
+            for (int b = (kb & 3) + 1; b < 4; ++b) e[b] = 0;
+        }
+      }
+    }
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) mbar_arrive(&sm.x_full);
+}
+
+// ----------------------------------------------------------------- products
+template <int N, Source X>
+__device__ void mma_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x, uint32_t tmem) {
+  using C = Cfg<N, X>;
   uint32_t n = 0, c = 0;      // blocks, chunks so far
   uint32_t s = 0, phase = 0;  // stage of block n
   SfSets sets;
-  bool ok = true;
-  const uint32_t idesc0 = idesc_mx(BM, N);
-  const uint64_t tile0 = desc_rows(smem_addr(sm.tile[0])), sf0 = desc_sf(smem_addr(sm.sf[0]));
-  for (Walk w(a, kF32); ok && w.more(); w.next(), ++c) {
+  const uint32_t idesc0 = idesc_mx(BM, N), xb = x_block(a) / 16;
+  const uint64_t tile0 = desc_rows(smem_addr(sm.tile[0])), x0 = desc_rows(smem_addr(sm.x));
+  const uint64_t w_sf = desc_sf(smem_addr(sm.sf_w[0])), x_sf = desc_sf(smem_addr(sm.sf_x[0]));
+  bool ok = true, ready = false;  // the stage of the next block was seen full
+  Walk w(a);
+  if (C::kFirst && w.more()) ok = wait_warp(x, &sm.x_full, 0);
+  for (; ok && w.more(); w.next(), ++c) {
     const uint32_t buf = c & 1, d = tmem + buf * N;
-    uint32_t sfa = tmem + C::kAccCols + sets.at() * C::kSfCols;
+    uint32_t sfa = tmem + C::kAccCols + C::kSfCols * sets.at();
     if (!(ok = wait_warp(x, &sm.acc_empty[buf], ((c >> 1) & 1) ^ 1))) break;
     tc_fence_after();
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-      if (!(ok = wait_warp(x, &sm.full[s], phase))) break;
+      if (!__all_sync(0xffffffffu, ready) && !(ok = wait_warp(x, &sm.full[s], phase))) break;
       tc_fence_after();
       const bool sf = (kb & 3) == 0 || kb == w.lo;
       if (sf) {
-        if (!(ok = sets.open<C::kStages, 1>(x, sm.empty, n))) break;
-        sfa = tmem + C::kAccCols + sets.at() * C::kSfCols;
+        if (!(ok = sets.open<C::kStages, 2>(x, sm.empty, n))) break;
+        sfa = tmem + C::kAccCols + C::kSfCols * sets.at();
       }
-      const uint64_t ds = sf0 + s * (1024 / 16);
       const uint32_t idesc = with_sf_id(idesc0, kb & 3);
-      const uint64_t da = tile0 + s * (C::kStageBytes / 16), db = da + BM * 128 / 16;
+      const uint64_t da = tile0 + s * (C::kStageBytes / 16), db = C::kFirst ? x0 + (kb - w.lo) * xb : da + C::kXAt / 16;
+      const bool end = s + 1 == C::kStages;
+      ready = mbar_test(&sm.full[end ? 0 : s + 1], end ? phase ^ 1 : phase);
       if (one_lane()) {
         if (sf) {
-          copy_sf(sfa, ds);
-          copy_sf(sfa + 4, ds + 32);
+          copy_sf(sfa, w_sf + s * 32);
+          copy_sf(sfa + 4, x_sf + (C::kFirst ? (kb >> 2) - (w.lo >> 2) : (int)s) * 32);
         }
         umma_mx(d, da, db, idesc, sfa, sfa + 4, kb != w.k0);
 #pragma unroll
         for (int j = 1; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfa + 4, 1);
-        umma_commit(&sm.empty[s]);
+        if (s & 1) umma_commit(&sm.empty[s >> 1]);  // a commit holds the cores up for 74 cycles: one for two stages
         if (kb + 1 == w.k1) umma_commit(&sm.acc_full[buf]);
       }
       __syncwarp();
-      if (++s == C::kStages) s = 0, phase ^= 1;
+      s = end ? 0 : s + 1;
+      phase ^= end;
     }
   }
   if (!ok && one_lane()) {  // products in flight end before the block does
@@ -201,60 +299,66 @@ __device__ void mma_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x, uint32_t 
   }
 }
 
-template <int N, bool kF32>
-__device__ void write_role(const GemmArgs& a, Smem<N>& sm, const Ctx& x, uint32_t tmem) {
-  using C = Cfg<N>;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t quarter = warp & 3, c0 = (warp >> 2) * C::kPer;
-  float acc[C::kPer];
+// ------------------------------------------------------------------ results
+template <int N, Source X>
+__device__ void write_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x, uint32_t tmem) {
+  constexpr int kPer = N / 2;  // columns of a warp
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = 32 * (warp & 3) + lane, c0 = (warp >> 2) * kPer;
+  float acc[kPer];
   uint32_t c = 0;
-  for (Walk w(a, kF32); w.more(); w.next(), ++c) {
+  for (Walk w(a); w.more(); w.next(), ++c) {
     const uint32_t buf = c & 1;
     if (!wait_warp(x, &sm.acc_full[buf], (c >> 1) & 1)) return;
     tc_fence_after();
-    const uint32_t t = tmem + ((quarter * 32) << 16) + buf * N + c0;
-    float v[C::kPer];
+    const uint32_t t = tmem + ((uint32_t)(r & ~31) << 16) + buf * N + c0;
+    float v[kPer];
 #pragma unroll
-    for (int i = 0; i < C::kPer; i += 8) tmem_ld8(t + i, v + i);
+    for (int i = 0; i < kPer; i += 8) tmem_ld8(t + i, v + i);
     tmem_wait_ld8(v);
 #pragma unroll
-    for (int i = 8; i < C::kPer; i += 8) tmem_tie8(v + i);
-#pragma unroll
-    for (int i = 0; i < C::kPer; ++i) acc[i] = kF32 && !w.first() ? __fadd_rn(acc[i], v[i]) : v[i];
+    for (int i = 8; i < kPer; i += 8) tmem_tie8(v + i);
     tc_fence_before();
     mbar_arrive(&sm.acc_empty[buf]);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) acc[i] = w.first() ? v[i] : __fadd_rn(acc[i], v[i]);
     if (!w.last()) continue;
-    const int r = quarter * 32 + lane, row = w.tile * BM + r;
     if (a.split > 1) {  // the part stays here until the cluster joins it; all copies and products of the block are done
       float* part = reinterpret_cast<float*>(sm.tile[0]);
 #pragma unroll
-      for (int i = 0; i < C::kPer; ++i) part[(c0 + i) * BM + r] = acc[i];
-    } else if (row < a.w.rows) {
+      for (int i = 0; i < kPer; ++i) part[(c0 + i) * BM + r] = acc[i];
+    } else if (const int row = w.tile * a.n + r; r < a.n && row < a.w.rows) {
 #pragma unroll
-      for (int i = 0; i < C::kPer; ++i)
-        if ((int)c0 + i < a.x.rows) put<kF32>(a, c0 + i, row, acc[i]);
+      for (int i = 0; i < kPer; ++i)
+        if (c0 + i < a.x.rows) put(a, c0 + i, row, acc[i]);
     }
   }
 }
 
 // The cluster's parts of a tile joined; each thread block joins its share of the elements.
-template <int N, bool kF32>
-__device__ void join(const GemmArgs& a, Smem<N>& sm) {
-  const int rank = blockIdx.x % a.split, row0 = blockIdx.x / a.split * BM;
-  for (int e = rank * kThreads + threadIdx.x; e < a.x.rows * (BM / 4); e += a.split * kThreads)
-    put4<kF32>(a, e / (BM / 4), row0 + e % (BM / 4) * 4, join4(smem_addr(sm.tile[0]) + 16 * e, 0, 1, a.split));
+template <int N, Source X>
+__device__ void join(const GemmArgs& a, Smem<N, X>& sm) {
+  const int rank = blockIdx.x % a.split, row0 = blockIdx.x / a.split * a.n, per = a.n / 4;
+  for (int e = rank * kThreads + threadIdx.x; e < a.x.rows * per; e += a.split * kThreads) {
+    const int tok = e / per, r = e % per * 4;
+    put4(a, tok, row0 + r, join4(smem_addr(sm.tile[0]) + 4 * (tok * BM + r), 0, 1, a.split));
+  }
 }
 
-template <int N, bool kF32>
+template <int N, Source X>
 __global__ void __launch_bounds__(kThreads, 1) fp8_few_kernel(const __grid_constant__ GemmArgs a) {
-  using C = Cfg<N>;
+  using C = Cfg<N, X>;
   extern __shared__ unsigned char smem_raw[];
-  Smem<N>& sm = *reinterpret_cast<Smem<N>*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
+  Smem<N, X>& sm = *reinterpret_cast<Smem<N, X>*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
   const int warp = threadIdx.x >> 5;
   if (warp == kMmaWarp) {
     if ((threadIdx.x & 31) == 0) {
-      for (int i = 0; i < C::kStages; ++i) mbar_init(&sm.full[i], 1), mbar_init(&sm.empty[i], 1);
+      for (int i = 0; i < C::kStages; ++i) {
+        mbar_init(&sm.full[i], 2);
+        if (i & 1) mbar_init(&sm.empty[i >> 1], 1);
+        mbar_init(&sm.raw_full[i], 1);
+      }
       for (int i = 0; i < 2; ++i) mbar_init(&sm.acc_full[i], 1), mbar_init(&sm.acc_empty[i], 256);
+      mbar_init(&sm.x_full, C::kRaw ? kXWarps : 1);
       mbar_init(&sm.drain, 1);
       sm.dead = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -268,17 +372,20 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_few_kernel(const __grid_const
   }
   __syncthreads();
   tc_fence_after();
-  if (!a.early) step_wait();
   step_trigger();
   const Ctx x{a.wait_ns, a.status, &sm.dead};
   const uint32_t tmem = sm.tmem;
-  if (warp < 8) {
+  if (warp < kXWarps) {
+    if constexpr (X == kF32First) quantize_role<N, X, float>(a, sm);
+    if constexpr (X == kBf16First) quantize_role<N, X, __nv_bfloat16>(a, sm);
     step_wait();
-    write_role<N, kF32>(a, sm, x, tmem);
+    write_role(a, sm, x, tmem);
   } else if (warp == kCopyWarp) {
-    copy_role<N, kF32>(a, sm, x);
+    copy_role(a, sm, x);
+  } else if (warp == kMmaWarp) {
+    mma_role(a, sm, x, tmem);
   } else {
-    mma_role<N, kF32>(a, sm, x, tmem);
+    scale_role(a, sm, x);
   }
   __syncwarp();
   tc_fence_before();
@@ -290,43 +397,79 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_few_kernel(const __grid_const
   if (a.split > 1) {  // every block gets here: all its waits are bounded
     __syncwarp();
     cluster_sync();
-    join<N, kF32>(a, sm);
+    join(a, sm);
     __syncwarp();
     cluster_sync();  // no block leaves while others read its part
   }
 }
 
-template <int N, bool kF32>
-cudaError_t launch(const GemmArgs& in, cudaStream_t st) {
-  using C = Cfg<N>;
-  constexpr int kSmem = (int)sizeof(Smem<N>) + 1024;
+// Rows of w in a tile and thread blocks per tile: the least time by a model of a thread
+// block's blocks of 128 columns, each 270 ns (its products) or its bytes at 50 GB/s,
+// and 1.2 us where parts are joined.
+void choose(GemmArgs* a) {
+  const int rows = a->w.rows, blocks = a->w.blocks();
+  const double x_bytes = 256.0 * a->x.rows;  // as if bf16: the choice, and so the sums, are the same for x and for its codes
+  double best = 0;
+  for (int split = 1; split <= kMaxSplit && split <= blocks; ++split) {
+    const int64_t most = split > 1 ? max_clusters(split) : kSms;  // tiles at a time
+    int64_t waves = 1, r;
+    for (;; ++waves) {
+      r = (rows + most * waves - 1) / (most * waves);
+      r = (r + 7) / 8 * 8;
+      if (r <= BM || split > 1) break;
+    }
+    if (r > BM || most < 1) continue;  // parts are joined in one wave
+    const double bytes = (128.0 * r + x_bytes) / 50.0, block = bytes > 270.0 ? bytes : 270.0;
+    const double all = (double)waves * ((blocks + split - 1) / split) * block + (split > 1 ? 1200.0 : 0.0);
+    if (best == 0 || all < best) best = all, a->n = (int)r, a->split = split;
+  }
+}
+
+template <int N, Source X>
+cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
+  using C = Cfg<N, X>;
+  constexpr int kSmem = (int)sizeof(Smem<N, X>) + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
   static_assert(N * BM * 4 <= C::kStages * C::kStageBytes, "a part of a tile fits into the stages");
-  const cudaError_t e = cudaFuncSetAttribute(fp8_few_kernel<N, kF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  const cudaError_t e = cudaFuncSetAttribute(fp8_few_kernel<N, X>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
-  GemmArgs a = in;
-  const int tiles = a.w.tiles(), slots = 152, blocks = a.x.blocks();
-  // few tiles: the columns of each are split over a cluster, at least kLeast blocks each
-  a.split = slots / tiles;
-  if (a.split > kMaxSplit) a.split = kMaxSplit;
-  if (a.split > blocks / kLeast) a.split = blocks / kLeast;
-  if (a.split < 1) a.split = 1;
-  const int grid = a.split > 1 ? tiles * a.split : tiles < slots ? tiles : slots;
-  return launch_step(fp8_few_kernel<N, kF32>, dim3((unsigned)grid), kThreads, kSmem, a.split, st, a);
+  const int tiles = (a.w.rows + a.n - 1) / a.n;
+  const int grid = a.split > 1 ? tiles * a.split : tiles < kSms ? tiles : kSms;
+  static_assert(C::kStages % 2 == 0, "stages are told of in twos");
+  return launch_step(fp8_few_kernel<N, X>, dim3((unsigned)grid), kThreads, kSmem, a.split, st, a);
+}
+
+constexpr int kFewRows = 64, kFirstRows = 16;  // of x
+
+// Whether all codes of x of a thread block's columns fit beside the stages.
+bool x_first(const GemmArgs& a) {
+  const int blocks = (a.w.blocks() + a.split - 1) / a.split;
+  return a.x.rows <= kFirstRows && blocks * a.x.rows8() * 128 <= Cfg<16, kCodesFirst>::kXBytes;
 }
 
 }  // namespace
 
-cudaError_t launch_fp8_gemm(const GemmArgs& in, int y_dtype, cudaStream_t st) {
-  const bool f32 = y_dtype == AWSRC_DTYPE_F32;
+bool fp8_gemm_quantizes(const GemmArgs& in) {
   GemmArgs a = in;
-  const uintptr_t size = f32 ? 4 : 2;
+  choose(&a);
+  return x_first(a);
+}
+
+cudaError_t launch_fp8_gemm(const GemmArgs& in, cudaStream_t st) {
+  GemmArgs a = in;
+  const uintptr_t size = a.y_f32 ? 4 : 2, raw_size = a.raw_bf16 ? 2 : 4;
   a.vec_y = (reinterpret_cast<uintptr_t>(a.y) | (uintptr_t)a.ys * size) % (4 * size) == 0;
+  a.vec_raw = (reinterpret_cast<uintptr_t>(a.raw) | (uintptr_t)a.raw_stride * raw_size) % (4 * raw_size) == 0;
   cudaError_t e;
-  if (a.x.rows <= 16) e = f32 ? launch<16, true>(a, st) : launch<16, false>(a, st);
-  else if (a.x.rows <= 32) e = f32 ? launch<32, true>(a, st) : launch<32, false>(a, st);
-  else if (a.x.rows <= 64) e = f32 ? launch<64, true>(a, st) : launch<64, false>(a, st);
-  else e = launch_fp8_pairs(a, f32, st);
+  if (a.x.rows > kFewRows) {
+    e = launch_fp8_pairs(a, st);
+  } else {
+    choose(&a);
+    if (x_first(a))
+      e = !a.raw ? launch<16, kCodesFirst>(a, st) : a.raw_bf16 ? launch<16, kBf16First>(a, st) : launch<16, kF32First>(a, st);
+    else
+      e = a.x.rows <= 16 ? launch<16, kCodes>(a, st) : a.x.rows <= 32 ? launch<32, kCodes>(a, st) : launch<64, kCodes>(a, st);
+  }
   if (e != cudaSuccess) return e;
   note_launches(1);
   return cudaGetLastError();

@@ -2,16 +2,26 @@
 // descriptors of operands and scales, results.
 #pragma once
 
+#include <cuda.h>
+
 #include "step.cuh"
 #include "tc05.cuh"
 
 namespace awsrc {
+
+// Clusters of `size` thread blocks, one per SM, that the current device runs at a time
+// (fewer than its SMs allow: a cluster lies in one group of them).
+int max_clusters(int size);
+
+// A tiled tensor of up to 3 dimensions (innermost first), rows past the last read as 0.
+cudaError_t make_tensor_map(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* p, const cuuint64_t* dims,
+                            const cuuint64_t* strides, const cuuint32_t* box);
+
 namespace fp8 {
 
 using namespace tc05;
 
 constexpr int BM = 128;
-constexpr int kThreads = 320, kCopyWarp = 8, kMmaWarp = 9;  // of a thread block; warps 0-7 write results
 constexpr int kChunk = 16;  // blocks summed in tensor memory for F32 results
 
 struct Ctx {
@@ -76,6 +86,19 @@ struct SfSets {
   __device__ __forceinline__ uint32_t at() const { return (count - 1) % kSfSets; }
 };
 
+// Whether the phase is over, without waiting: asked ahead, its answer comes while products are issued.
+__device__ __forceinline__ bool mbar_test(unsigned long long* mb, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_addr(mb)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Rows of 128 bytes, 16-byte pieces exchanged by row (128-byte swizzle), groups of
 // 8 rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t desc_rows(uint32_t addr) {
@@ -93,17 +116,9 @@ __device__ __forceinline__ uint32_t idesc_mx(int m, int n) {
   return (1u << 23) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-// 16 sums of a row from tensor memory on: kept, or added to those of the chunks before.
-template <bool kAdd>
-__device__ __forceinline__ void take16(float* acc, const float* v) {
-#pragma unroll
-  for (int j = 0; j < 16; ++j) acc[j] = kAdd ? __fadd_rn(acc[j], v[j]) : v[j];
-}
-
-template <bool kF32>
 __device__ __forceinline__ void put(const GemmArgs& a, int tok, int row, float v) {
   const int64_t at = (int64_t)tok * a.ys + row;
-  if (kF32) static_cast<float*>(a.y)[at] = v;
+  if (a.y_f32) static_cast<float*>(a.y)[at] = v;
   else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
 }
 
@@ -128,12 +143,11 @@ __device__ __forceinline__ float4 join4(uint32_t addr, int rank0, int every, int
 }
 
 // Four rows of w of one row of y.
-template <bool kF32>
 __device__ __forceinline__ void put4(const GemmArgs& a, int tok, int row, float4 v) {
   const int have = a.w.rows - row;
   if (have >= 4 && a.vec_y) {
     const int64_t at = (int64_t)tok * a.ys + row;
-    if (kF32) {
+    if (a.y_f32) {
       *reinterpret_cast<float4*>(static_cast<float*>(a.y) + at) = v;
     } else {
       const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
@@ -142,10 +156,10 @@ __device__ __forceinline__ void put4(const GemmArgs& a, int tok, int row, float4
     }
     return;
   }
-  if (have > 0) put<kF32>(a, tok, row, v.x);
-  if (have > 1) put<kF32>(a, tok, row + 1, v.y);
-  if (have > 2) put<kF32>(a, tok, row + 2, v.z);
-  if (have > 3) put<kF32>(a, tok, row + 3, v.w);
+  if (have > 0) put(a, tok, row, v.x);
+  if (have > 1) put(a, tok, row + 1, v.y);
+  if (have > 2) put(a, tok, row + 2, v.z);
+  if (have > 3) put(a, tok, row + 3, v.w);
 }
 
 }  // namespace fp8

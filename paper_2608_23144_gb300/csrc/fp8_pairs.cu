@@ -18,7 +18,7 @@
 //
 // Every wait is bounded as in fp8_gemm.cu; no thread block of a cluster leaves before
 // all have stopped, as products and arrivals reach into a partner's memory.
-#include <cuda.h>
+#include <atomic>
 
 #include "fp8_mma.cuh"
 #include "internal.h"
@@ -29,6 +29,7 @@ namespace {
 
 using namespace fp8;
 
+constexpr int kThreads = 320, kCopyWarp = 8, kMmaWarp = 9;
 constexpr int kMaxN = 256;
 constexpr int kStages = 6;
 constexpr int kStageBytes = (BM + kMaxN / 2) * 128;
@@ -87,6 +88,17 @@ __device__ __forceinline__ bool try_wait_cluster(unsigned long long* mb, uint32_
       : "memory");
   return ok != 0;
 }
+__device__ __forceinline__ bool mbar_test_cluster(unsigned long long* mb, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_addr(mb)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __noinline__ bool wait_cluster_slow(const Ctx& x, unsigned long long* mb, uint32_t parity) {
   const uint64_t t0 = globaltimer();
   for (;;) {
@@ -133,16 +145,16 @@ __device__ __forceinline__ void commit_both(unsigned long long* mb, uint16_t mas
 struct Walk {
   int tiles_w, tiles_x, tiles, chunk, step;
   int tile, lo, hi, k0, k1, row, tok;
-  __device__ Walk(const GemmArgs& a, bool f32) {
+  __device__ explicit Walk(const GemmArgs& a) {
     tiles_w = (a.w.tiles() + 1) >> 1;
     tiles_x = (a.x.rows + a.n - 1) / a.n;
     tiles = tiles_w * tiles_x;
-    const int pair = blockIdx.x >> 1, rank = pair % a.split, blocks = a.x.blocks();
-    step = (gridDim.x >> 1) / a.split;
-    tile = pair / a.split;
-    lo = (int)((int64_t)blocks * rank / a.split);
-    hi = (int)((int64_t)blocks * (rank + 1) / a.split);
-    chunk = f32 ? kChunk : blocks;
+    const unsigned pair = blockIdx.x >> 1, split = a.split, rank = pair % split, blocks = a.x.blocks();  // at most 2^17 blocks
+    step = (gridDim.x >> 1) / split;
+    tile = pair / split;
+    lo = blocks * rank / split;
+    hi = blocks * (rank + 1) / split;
+    chunk = a.y_f32 ? kChunk : (int)blocks;
     k0 = lo;
     k1 = min(k0 + chunk, hi);
     place(a.n);
@@ -171,13 +183,12 @@ struct Walk {
 // Scale tiles of 128 rows that the rows of x of a tile lie in.
 __host__ __device__ constexpr int sf_tiles(int n) { return n > 128 ? 2 : 1; }
 
-template <bool kF32>
 __device__ void copy_role(const PairArgs& p, Smem& sm, const Ctx& x, uint32_t half, uint32_t even) {
   const GemmArgs& a = p.g;
   uint32_t n = 0;
   int ahead;  // blocks whose copies begin together
   bool ok = true;
-  Walk w(a, kF32);
+  Walk w(a);
   const int half_n = a.n >> 1;
   const uint32_t bytes = 2u * (BM * 128u + half_n * 128u), sf_bytes = 2u * 512u * (1 + sf_tiles(a.n));
   const auto has_sf = [&](int kb) { return (kb & 3) == 0 || kb == w.lo; };
@@ -233,22 +244,21 @@ __device__ void copy_role(const PairArgs& p, Smem& sm, const Ctx& x, uint32_t ha
       (void)mbar_wait(&sm.full[j % kStages], (j / kStages) & 1, x.wait_ns);
 }
 
-template <bool kF32>
 __device__ void mma_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tmem, uint16_t both) {
   uint32_t n = 0, c = 0;           // blocks, chunks so far
   uint32_t s = 0, phase = 0;       // stage of block n
   SfSets sets;
-  bool ok = true;
+  bool ok = true, ready = false;  // the stage of the next block was seen full
   const uint32_t bufs = a.n <= kTwoBufs ? 2 : 1, idesc0 = idesc_mx(2 * BM, a.n), sfs = sf_tiles(a.n);
   const uint64_t tile0 = desc_rows(smem_addr(sm.tile[0])), sf0 = desc_sf(smem_addr(sm.sf[0]));
-  for (Walk w(a, kF32); ok && w.more(); w.next(a.n), ++c) {
+  for (Walk w(a); ok && w.more(); w.next(a.n), ++c) {
     const uint32_t buf = c % bufs, d = tmem + buf * a.n;
     const uint32_t shift = 4 + ((uint32_t)(w.tok & 127) >> 5);
     uint32_t sfa = tmem + kSfAt + sets.at() * kSfCols;
     if (!(ok = wait_cluster_warp(x, &sm.acc_empty[buf], ((c / bufs) & 1) ^ 1))) break;
     tc_fence_after();
     for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-      if (!(ok = wait_cluster_warp(x, &sm.full[s], phase))) break;
+      if (!__all_sync(0xffffffffu, ready) && !(ok = wait_cluster_warp(x, &sm.full[s], phase))) break;
       tc_fence_after();
       const bool sf = (kb & 3) == 0 || kb == w.lo;
       if (sf) {
@@ -258,6 +268,8 @@ __device__ void mma_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tme
       const uint64_t ds = sf0 + s * (kSfBytes / 16);
       const uint32_t idesc = with_sf_id(idesc0, kb & 3), sfb = sfa + shift;
       const uint64_t da = tile0 + s * (kStageBytes / 16), db = da + BM * 128 / 16;
+      const bool end = s + 1 == kStages;
+      ready = mbar_test_cluster(&sm.full[end ? 0 : s + 1], end ? phase ^ 1 : phase);
       if (one_lane()) {
         if (sf) {
           copy_sf(sfa, ds);
@@ -272,7 +284,8 @@ __device__ void mma_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tme
         if (kb + 1 == w.k1) commit_both(&sm.acc_full[buf], both);
       }
       __syncwarp();
-      if (++s == kStages) s = 0, phase ^= 1;
+      s = end ? 0 : s + 1;
+      phase ^= end;
     }
   }
   if (!ok && one_lane()) {  // products in flight end before the block does
@@ -281,19 +294,18 @@ __device__ void mma_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tme
   }
 }
 
-template <bool kF32>
 __device__ void write_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t tmem, uint32_t half, uint32_t even) {
   constexpr int kPer = kMaxN / 2;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = a.n >> 1;
   const uint32_t quarter = warp & 3, c0 = (warp >> 2) * per, bufs = a.n <= kTwoBufs ? 2 : 1;
   float acc[kPer];
   uint32_t c = 0;
-  for (Walk w(a, kF32); w.more(); w.next(a.n), ++c) {
+  for (Walk w(a); w.more(); w.next(a.n), ++c) {
     const uint32_t buf = c % bufs;
     if (!wait_warp(x, &sm.acc_full[buf], (c / bufs) & 1)) return;
     tc_fence_after();
     const uint32_t t = tmem + ((quarter * 32) << 16) + buf * a.n + c0;
-    if (!kF32 || w.first()) {
+    if (w.first()) {
 #pragma unroll
       for (int i = 0; i < kPer; i += 16)
         if (i < per) tmem_ld16(t + i, acc + i);
@@ -325,21 +337,19 @@ __device__ void write_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t t
       const int have = min(per, a.x.rows - w.tok - (int)c0);
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
-        if (i < have) put<kF32>(a, w.tok + c0 + i, row, acc[i]);
+        if (i < have) put(a, w.tok + c0 + i, row, acc[i]);
     }
   }
 }
 
-template <bool kF32>
 __device__ void join(const GemmArgs& a, Smem& sm, uint32_t half) {
-  const Walk w(a, kF32);
+  const Walk w(a);
   const int share = (blockIdx.x >> 1) % a.split, row0 = w.row + BM * half;
   const int cols = min(a.n, a.x.rows - w.tok);
   for (int e = share * kThreads + threadIdx.x; e < cols * (BM / 4); e += a.split * kThreads)
-    put4<kF32>(a, w.tok + e / (BM / 4), row0 + e % (BM / 4) * 4, join4(smem_addr(sm.tile[0]) + 16 * e, half, 2, a.split));
+    put4(a, w.tok + e / (BM / 4), row0 + e % (BM / 4) * 4, join4(smem_addr(sm.tile[0]) + 16 * e, half, 2, a.split));
 }
 
-template <bool kF32>
 __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_constant__ PairArgs p) {
   const GemmArgs& a = p.g;
   extern __shared__ unsigned char smem_raw[];
@@ -364,17 +374,16 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_con
   __syncwarp();
   cluster_sync();  // both thread blocks' barriers and tensor memory are there
   tc_fence_after();
-  if (!a.early) step_wait();
   step_trigger();
   const Ctx x{a.wait_ns, a.status, &sm.dead};
   const uint32_t tmem = sm.tmem;
   if (warp < 8) {
     step_wait();
-    write_role<kF32>(a, sm, x, tmem, half, even);
+    write_role(a, sm, x, tmem, half, even);
   } else if (warp == kCopyWarp) {
-    copy_role<kF32>(p, sm, x, half, even);
+    copy_role(p, sm, x, half, even);
   } else if (!half) {
-    mma_role<kF32>(a, sm, x, tmem, (uint16_t)(3u << even));
+    mma_role(a, sm, x, tmem, (uint16_t)(3u << even));
   }
   __syncwarp();
   tc_fence_before();
@@ -385,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_con
   }
   if (a.split > 1) {
     __syncwarp();
-    join<kF32>(a, sm, half);
+    join(a, sm, half);
     __syncwarp();
     cluster_sync();  // no block leaves while others read its part
   }
@@ -402,10 +411,10 @@ void choose(GemmArgs* a) {
   for (int n = 64; n <= kMaxN; n += 64)
     for (int split = 1; split <= kMaxSplit && (split == 1 || split * kLeast <= blocks); ++split) {
       const int64_t tiles = tiles_w * ((a->x.rows + n - 1) / n);
-      if (split > 1 && tiles * split > kPairs) break;
+      if (split > 1 && tiles > max_clusters(2 * split)) continue;
       const double load = (16384.0 + 64.0 * n) / 52.0, mma = 2.0 * n;
       const double tile = (double)((blocks + split - 1) / split) * (load > mma ? load : mma) + 2500.0 + 8.0 * n * (split - 1);
-      const double all = (double)((tiles * split + kPairs - 1) / kPairs) * tile;
+      const double all = (split > 1 ? 1.0 : (double)((tiles + kPairs - 1) / kPairs)) * tile;
       if (best == 0 || all < best) best = all, a->n = n, a->split = split;
     }
 }
@@ -413,29 +422,18 @@ void choose(GemmArgs* a) {
 // A tensor [blocks][rows][`row` bytes], read in boxes of `box` rows.
 cudaError_t tensor(CUtensorMap* map, CUtensorMapDataType type, int size, const void* p, int row, int64_t rows, int64_t blocks,
                    int box) {
-  typedef decltype(&cuTensorMapEncodeTiled) Encode;
-  static const Encode encode = [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
-    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(f) : nullptr;
-  }();
-  if (!encode) return cudaErrorNotSupported;
   const cuuint64_t dims[3] = {(cuuint64_t)(row / size), (cuuint64_t)rows, (cuuint64_t)blocks};
   const cuuint64_t strides[2] = {(cuuint64_t)row, (cuuint64_t)(row * rows)};
-  const cuuint32_t boxes[3] = {(cuuint32_t)(row / size), (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
-  const CUresult r = encode(map, type, 3, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+  const cuuint32_t boxes[3] = {(cuuint32_t)(row / size), (cuuint32_t)box, 1};
+  return make_tensor_map(map, type, 3, p, dims, strides, boxes);
 }
 
-template <bool kF32>
 cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
   constexpr int kSmem = (int)sizeof(Smem) + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
   static_assert(kMaxN * BM * 4 <= kStages * kStageBytes, "a part of a tile fits into the stages");
   static_assert(2 * kTwoBufs <= kSfAt && kMaxN <= kSfAt, "accumulators end before the scales");
-  cudaError_t e = cudaFuncSetAttribute(fp8_pairs_kernel<kF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  cudaError_t e = cudaFuncSetAttribute(fp8_pairs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   PairArgs p;
   p.g = a;
   const int blocks = a.x.blocks(), fours = (blocks + 3) / 4;
@@ -451,15 +449,57 @@ cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)((a.w.tiles() + 1) / 2) * ((a.x.rows + a.n - 1) / a.n);
   const int64_t pairs = a.split > 1 ? tiles * a.split : tiles < kPairs ? tiles : kPairs;
-  return launch_step(fp8_pairs_kernel<kF32>, dim3((unsigned)(2 * pairs)), kThreads, kSmem, 2 * a.split, st, p);
+  return launch_step(fp8_pairs_kernel, dim3((unsigned)(2 * pairs)), kThreads, kSmem, 2 * a.split, st, p);
 }
 
 }  // namespace
 
-cudaError_t launch_fp8_pairs(const GemmArgs& in, bool f32, cudaStream_t st) {
+cudaError_t make_tensor_map(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* p, const cuuint64_t* dims,
+                            const cuuint64_t* strides, const cuuint32_t* box) {
+  typedef decltype(&cuTensorMapEncodeTiled) Encode;
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(f) : nullptr;
+  }();
+  if (!encode) return cudaErrorNotSupported;
+  const cuuint32_t ones[3] = {1, 1, 1};
+  const CUresult r = encode(map, type, rank, const_cast<void*>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+int max_clusters(int size) {
+  constexpr int kDevices = 64, kMost = 8;
+  static std::atomic<int> known[kDevices][kMost + 1];  // 1 + the answer
+  int dev = 0;
+  if (size < 1 || size > kMost || cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return 0;
+  if (const int k = known[dev][size].load(std::memory_order_relaxed)) return k - 1;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = size;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(size);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Smem) + 1024;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaFuncSetAttribute(fp8_pairs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, fp8_pairs_kernel, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();  // no split, then
+    n = 0;
+  }
+  known[dev][size].store(n + 1, std::memory_order_relaxed);
+  return n;
+}
+
+cudaError_t launch_fp8_pairs(const GemmArgs& in, cudaStream_t st) {
   GemmArgs a = in;
   choose(&a);
-  return f32 ? launch<true>(a, st) : launch<false>(a, st);
+  return launch(a, st);
 }
 
 }  // namespace awsrc

@@ -81,16 +81,23 @@ struct GemmArgs {
   Fp8Mat x, w;
   void* y;
   int64_t ys;
+  int y_f32;         // y is binary32, else bf16
+  const void* raw;   // x before quantising, when the product does that itself (few rows); else null
+  int64_t raw_stride;
+  int raw_bf16;
   uint32_t* status;
   uint64_t wait_ns;  // limit of the kernel's waits
   int stall;         // test of that limit: no copies from this block of 128 columns on (-1: never)
   int early;         // w was written before the kernel before this one began: its rows need no wait
   // set by the launch
   int split;         // thread blocks (pairs of them) that share a tile's columns
-  int n;             // rows of x in a tile
+  int n;             // rows of x in a tile; of w in the kernel for few rows of x
   int vec_y;         // four elements of y lie on a boundary of their size
+  int vec_raw;       // so do four of every row of x
 };
-cudaError_t launch_fp8_pairs(const GemmArgs& a, bool f32, cudaStream_t st);
-cudaError_t launch_fp8_gemm(const GemmArgs& a, int y_dtype, cudaStream_t st);
+// Whether the product can quantise these rows of x itself (fp8_gemm.cu).
+bool fp8_gemm_quantizes(const GemmArgs& a);
+cudaError_t launch_fp8_pairs(const GemmArgs& a, cudaStream_t st);
+cudaError_t launch_fp8_gemm(const GemmArgs& a, cudaStream_t st);
 
 }  // namespace awsrc
