@@ -19,8 +19,8 @@
 //     here block by block, 40 rows took 29 us where both kernels took 17: each stage waited
 //     for a copy, the codes and a fence).
 //   Warp 10 puts the scales of the tile's rows of w in the order of its lanes. Warp 9
-//     issues the products (270 ns a block whatever N: the cores read w's 128 rows at 64
-//     bytes per cycle); warps 0-7 read the sums and write y.
+//     issues the products: 22 ns for each of a block's four and 167 ns for what a stage
+//     costs all roles, so a stage holds two blocks. Warps 0-7 read the sums and write y.
 // Few rows of w: a cluster shares a tile's columns and joins its parts, in their order,
 // through shared memory.
 //
@@ -47,9 +47,9 @@ enum Source { kCodes, kCodesFirst, kF32First, kBf16First };
 template <int N, Source X>
 struct Cfg {
   static constexpr bool kFirst = X != kCodes, kRaw = X == kF32First || X == kBf16First;
-  static constexpr int kXAt = BM * 128;  // in a stage: rows of w, then of x
-  static constexpr int kStageBytes = kXAt + (kFirst ? 0 : N * 128);
-  static constexpr int kStages = kFirst ? 8 : N > 32 ? 8 : 10;
+  static constexpr int kWBytes = BM * 128, kXAt = 2 * kWBytes;  // a stage holds two blocks: rows of w, then of x
+  static constexpr int kStageBytes = kXAt + (kFirst ? 0 : 2 * N * 128);
+  static constexpr int kStages = kFirst || N > 32 ? 4 : 5;
   static constexpr int kXBytes = kFirst ? 64 * 1024 : 0;  // codes of x that come first
   static constexpr int kXGroups = kFirst ? 18 : kStages;  // their scales, 512 bytes for 4 blocks; else of a stage
   static constexpr int kAccCols = 2 * N;                  // two accumulators
@@ -64,7 +64,7 @@ struct Smem {
   uint8_t tile[C::kStages][C::kStageBytes];
   uint8_t x[C::kXBytes + 1024];  // a block's last rows of 16 may lie in the next one's place
   uint8_t sf_w[C::kStages][512], sf_raw[C::kStages][1024], sf_x[C::kXGroups][512];
-  unsigned long long full[C::kStages], empty[C::kStages / 2], raw_full[C::kStages], acc_full[2], acc_empty[2], x_full, drain;
+  unsigned long long full[C::kStages], empty[C::kStages], raw_full[C::kStages], acc_full[2], acc_empty[2], x_full, drain;
   uint32_t tmem;
   int dead;
 };
@@ -85,18 +85,19 @@ __device__ __forceinline__ void umma_mx(uint32_t d, uint64_t a, uint64_t b, uint
       : "memory");
 }
 
-// The walk that all roles take: tiles of this block, its share of their columns in
-// chunks of blocks.
+// The walk that all roles take: tiles of this block, its share of their columns (whole
+// stages but for the last) in chunks of blocks.
 struct Walk {
   int tiles, chunk, step;
   int tile, lo, hi, k0, k1;
   __device__ explicit Walk(const GemmArgs& a) {
     tiles = (a.w.rows + a.n - 1) / a.n;
     const unsigned blocks = a.w.blocks(), split = a.split, rank = blockIdx.x % split;  // at most 2^17 blocks, 8 shares
+    const unsigned twos = (blocks + 1) / 2;
     step = gridDim.x / split;
     tile = blockIdx.x / split;
-    lo = blocks * rank / split;
-    hi = blocks * (rank + 1) / split;
+    lo = 2 * (twos * rank / split);
+    hi = min(blocks, 2 * (twos * (rank + 1) / split));
     chunk = a.y_f32 ? kChunk : (int)blocks;
     k0 = lo;
     k1 = min(k0 + chunk, hi);
@@ -120,24 +121,29 @@ __device__ void copy_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x) {
   const uint32_t xb = x_block(a);
   Walk w(a);
   const auto has_sf = [&](int kb) { return (kb & 3) == 0 || kb == w.lo; };
-  const auto copy_w = [&](int kb, uint32_t s, const uint8_t* rows) {
-    const int row = w.tile * a.n;
-    const uint32_t bytes = 128u * (uint32_t)min((int64_t)a.n, w8 - row);
-    mbar_expect_tx(&sm.full[s], bytes + (C::kFirst ? 0u : xb + (has_sf(kb) ? 512u : 0u)));
-    bulk_g2s(sm.tile[s], rows, bytes, &sm.full[s]);
+  // a stage begins: what its barriers count
+  const auto expect = [&](int kb, uint32_t s) {
+    const int row = w.tile * a.n, m = min(2, w.hi - kb);
+    mbar_expect_tx(&sm.full[s], m * 128u * (uint32_t)min((int64_t)a.n, w8 - row) + (C::kFirst ? 0u : m * xb + (has_sf(kb) ? 512u : 0u)));
     // scales of the one or two tiles of 128 rows that this tile's rows lie in
     const uint32_t sf = has_sf(kb) ? 512u * (uint32_t)min(2, a.w.tiles() - (row >> 7)) : 0u;
     mbar_expect_tx(&sm.raw_full[s], sf);
     if (sf) bulk_g2s(sm.sf_raw[s], a.w.exps + ((int64_t)(kb >> 2) * a.w.tiles() + (row >> 7)) * 512, sf, &sm.raw_full[s]);
   };
+  const auto copy_w = [&](int kb, uint32_t s, const uint8_t* rows) {
+    bulk_g2s(sm.tile[s] + (kb & 1) * C::kWBytes, rows, 128u * (uint32_t)min((int64_t)a.n, w8 - w.tile * a.n), &sm.full[s]);
+  };
   const auto copy_x = [&](int kb, uint32_t s) {
-    bulk_g2s(sm.tile[s] + C::kXAt, a.x.codes + (int64_t)kb * xb, xb, &sm.full[s]);
+    bulk_g2s(sm.tile[s] + C::kXAt, a.x.codes + (int64_t)kb * xb, min(2, w.hi - kb) * xb, &sm.full[s]);
     if (has_sf(kb)) bulk_g2s(sm.sf_x[s], a.x.exps + (int64_t)(kb >> 2) * 512, 512, &sm.full[s]);
   };
-  int ahead = 0;
+  int ahead = 0;  // blocks of w on their way before x is ready
   if (a.early && a.stall < 0 && w.more()) {
-    ahead = min(C::kStages, w.hi - w.lo);
-    if (lane < ahead) copy_w(w.lo + lane, lane, a.w.codes + (w.lo + lane) * w_step + w.tile * a.n * 128ll);
+    ahead = min(2 * C::kStages, w.hi - w.lo);
+    if (lane < ahead) {
+      if ((lane & 1) == 0) expect(w.lo + lane, lane >> 1);
+      copy_w(w.lo + lane, lane >> 1, a.w.codes + (w.lo + lane) * w_step + w.tile * a.n * 128ll);
+    }
     __syncwarp();
   }
   step_wait();
@@ -153,18 +159,23 @@ __device__ void copy_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x) {
     }
     __syncwarp();
   }
-  uint32_t n = 0, s = 0, phase = 1;  // blocks so far; stage of block n
+  uint32_t n = 0, s = 0, phase = 1;  // stages so far; stage of block kb
   bool ok = true;
   for (; ok && w.more(); w.next()) {
     const uint8_t* rows = a.w.codes + w.k0 * w_step + w.tile * a.n * 128ll;
-    for (int kb = w.k0; kb < w.k1; ++kb, ++n, rows += w_step) {
-      if (kb == a.stall || ((s & 1) == 0 && !wait_warp(x, &sm.empty[s >> 1], phase))) {
+    for (int kb = w.k0; kb < w.k1; kb += 2, ++n, rows += 2 * w_step) {
+      if (kb == (a.stall & ~1) || !wait_warp(x, &sm.empty[s], phase)) {
         ok = false;
         break;
       }
       if (one_lane()) {
+        const bool begun = (int)(2 * n) < ahead;
+        if (!begun) expect(kb, s);
         if (!C::kFirst) copy_x(kb, s);
-        if ((int)n >= ahead) copy_w(kb, s, rows);
+        if (!begun) {
+          copy_w(kb, s, rows);
+          if (kb + 1 < w.k1) copy_w(kb + 1, s, rows + w_step);
+        }
       }
       __syncwarp();
       if (++s == C::kStages) s = 0, phase ^= 1;
@@ -183,7 +194,7 @@ __device__ void scale_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x) {
   const int lane = threadIdx.x & 31;
   uint32_t s = 0, phase = 0;
   for (Walk w(a); w.more(); w.next())
-    for (int kb = w.k0; kb < w.k1; ++kb) {
+    for (int kb = w.k0; kb < w.k1; kb += 2) {
       if (!wait_warp(x, &sm.raw_full[s], phase)) return;
       if ((kb & 3) == 0 || kb == w.lo) {
         uint32_t v[4];
@@ -251,13 +262,13 @@ __device__ void quantize_role(const GemmArgs& a, Smem<N, X>& sm) {
 template <int N, Source X>
 __device__ void mma_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x, uint32_t tmem) {
   using C = Cfg<N, X>;
-  uint32_t n = 0, c = 0;      // blocks, chunks so far
-  uint32_t s = 0, phase = 0;  // stage of block n
+  uint32_t n = 0, c = 0;      // stages, chunks so far
+  uint32_t s = 0, phase = 0;  // stage of block kb
   SfSets sets;
   const uint32_t idesc0 = idesc_mx(BM, N), xb = x_block(a) / 16;
   const uint64_t tile0 = desc_rows(smem_addr(sm.tile[0])), x0 = desc_rows(smem_addr(sm.x));
   const uint64_t w_sf = desc_sf(smem_addr(sm.sf_w[0])), x_sf = desc_sf(smem_addr(sm.sf_x[0]));
-  bool ok = true, ready = false;  // the stage of the next block was seen full
+  bool ok = true, ready = false;  // the next stage was seen full
   Walk w(a);
   if (C::kFirst && w.more()) ok = wait_warp(x, &sm.x_full, 0);
   for (; ok && w.more(); w.next(), ++c) {
@@ -265,28 +276,32 @@ __device__ void mma_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x, uint32
     uint32_t sfa = tmem + C::kAccCols + C::kSfCols * sets.at();
     if (!(ok = wait_warp(x, &sm.acc_empty[buf], ((c >> 1) & 1) ^ 1))) break;
     tc_fence_after();
-    for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
+    for (int kb = w.k0; kb < w.k1; kb += 2, ++n) {
       if (!__all_sync(0xffffffffu, ready) && !(ok = wait_warp(x, &sm.full[s], phase))) break;
       tc_fence_after();
       const bool sf = (kb & 3) == 0 || kb == w.lo;
       if (sf) {
-        if (!(ok = sets.open<C::kStages, 2>(x, sm.empty, n))) break;
+        if (!(ok = sets.open<C::kStages, 1>(x, sm.empty, n))) break;
         sfa = tmem + C::kAccCols + C::kSfCols * sets.at();
       }
-      const uint32_t idesc = with_sf_id(idesc0, kb & 3);
+      const uint32_t id0 = with_sf_id(idesc0, kb & 3), id1 = with_sf_id(idesc0, (kb & 3) + 1);
       const uint64_t da = tile0 + s * (C::kStageBytes / 16), db = C::kFirst ? x0 + (kb - w.lo) * xb : da + C::kXAt / 16;
-      const bool end = s + 1 == C::kStages;
+      const bool end = s + 1 == C::kStages, two = kb + 1 < w.k1;
       ready = mbar_test(&sm.full[end ? 0 : s + 1], end ? phase ^ 1 : phase);
       if (one_lane()) {
         if (sf) {
           copy_sf(sfa, w_sf + s * 32);
           copy_sf(sfa + 4, x_sf + (C::kFirst ? (kb >> 2) - (w.lo >> 2) : (int)s) * 32);
         }
-        umma_mx(d, da, db, idesc, sfa, sfa + 4, kb != w.k0);
+        umma_mx(d, da, db, id0, sfa, sfa + 4, kb != w.k0);
 #pragma unroll
-        for (int j = 1; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, idesc, sfa, sfa + 4, 1);
-        if (s & 1) umma_commit(&sm.empty[s >> 1]);  // a commit holds the cores up for 74 cycles: one for two stages
-        if (kb + 1 == w.k1) umma_commit(&sm.acc_full[buf]);
+        for (int j = 1; j < 4; ++j) umma_mx(d, da + 2 * j, db + 2 * j, id0, sfa, sfa + 4, 1);
+        if (two) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) umma_mx(d, da + C::kWBytes / 16 + 2 * j, db + xb + 2 * j, id1, sfa, sfa + 4, 1);
+        }
+        umma_commit(&sm.empty[s]);
+        if (kb + 2 >= w.k1) umma_commit(&sm.acc_full[buf]);
       }
       __syncwarp();
       s = end ? 0 : s + 1;
@@ -354,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_few_kernel(const __grid_const
     if ((threadIdx.x & 31) == 0) {
       for (int i = 0; i < C::kStages; ++i) {
         mbar_init(&sm.full[i], 2);
-        if (i & 1) mbar_init(&sm.empty[i >> 1], 1);
+        mbar_init(&sm.empty[i], 1);
         mbar_init(&sm.raw_full[i], 1);
       }
       for (int i = 0; i < 2; ++i) mbar_init(&sm.acc_full[i], 1), mbar_init(&sm.acc_empty[i], 256);
@@ -404,13 +419,14 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_few_kernel(const __grid_const
 }
 
 // Rows of w in a tile and thread blocks per tile: the least time by a model of a thread
-// block's blocks of 128 columns, each 270 ns (its products) or its bytes at 50 GB/s,
-// and 1.2 us where parts are joined.
+// block's stages, each 350 ns (its products) or its bytes at 50 GB/s, and 1.8 us where
+// parts are joined.
 void choose(GemmArgs* a) {
   const int rows = a->w.rows, blocks = a->w.blocks();
-  const double x_bytes = 256.0 * a->x.rows;  // as if bf16: the choice, and so the sums, are the same for x and for its codes
+  const double x_bytes = 512.0 * a->x.rows;  // as if bf16: the choice, and so the sums, are the same for x and for its codes
   double best = 0;
-  for (int split = 1; split <= kMaxSplit && split <= blocks; ++split) {
+  const int twos = (blocks + 1) / 2;
+  for (int split = 1; split <= kMaxSplit && split <= twos; ++split) {
     const int64_t most = split > 1 ? max_clusters(split) : kSms;  // tiles at a time
     int64_t waves = 1, r;
     for (;; ++waves) {
@@ -419,8 +435,8 @@ void choose(GemmArgs* a) {
       if (r <= BM || split > 1) break;
     }
     if (r > BM || most < 1) continue;  // parts are joined in one wave
-    const double bytes = (128.0 * r + x_bytes) / 50.0, block = bytes > 270.0 ? bytes : 270.0;
-    const double all = (double)waves * ((blocks + split - 1) / split) * block + (split > 1 ? 1200.0 : 0.0);
+    const double bytes = (256.0 * r + x_bytes) / 50.0, stage = bytes > 350.0 ? bytes : 350.0;
+    const double all = (double)waves * ((twos + split - 1) / split) * stage + (split > 1 ? 1800.0 : 0.0);
     if (best == 0 || all < best) best = all, a->n = (int)r, a->split = split;
   }
 }
@@ -435,7 +451,7 @@ cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int tiles = (a.w.rows + a.n - 1) / a.n;
   const int grid = a.split > 1 ? tiles * a.split : tiles < kSms ? tiles : kSms;
-  static_assert(C::kStages % 2 == 0, "stages are told of in twos");
+  static_assert(kChunk % 2 == 0, "chunks are whole stages");
   return launch_step(fp8_few_kernel<N, X>, dim3((unsigned)grid), kThreads, kSmem, a.split, st, a);
 }
 
@@ -443,7 +459,7 @@ constexpr int kFewRows = 64, kFirstRows = 16;  // of x
 
 // Whether all codes of x of a thread block's columns fit beside the stages.
 bool x_first(const GemmArgs& a) {
-  const int blocks = (a.w.blocks() + a.split - 1) / a.split;
+  const int blocks = ((a.w.blocks() + 1) / 2 + a.split - 1) / a.split * 2;
   return a.x.rows <= kFirstRows && blocks * a.x.rows8() * 128 <= Cfg<16, kCodesFirst>::kXBytes;
 }
 
