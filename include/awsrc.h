@@ -693,7 +693,7 @@ typedef struct awsrc_probs {
  *   the weights w_j = max(0, target[s][j] - draft[s][j]); when all drafts are
  *   accepted, from w_j = target[s][j] of the last row s. It is the smallest j
  *   with w_0 + .. + w_j > r[b] * (w_0 + .. + w_V-1), the sums exact over
- *   probabilities rounded down to multiples of 2^-62. Where all w_j are 0 the row
+ *   probabilities rounded to the nearest multiple of 2^-45 (ties to even). Where all w_j are 0 the row
  *   of `target` takes their place; where that is 0 too the token is -1.
  *   Probabilities count as 0 when NaN or negative and as 1 above 1; u and r as
  *   0 when NaN or negative; r as the largest value below 1 from 1 on.
@@ -706,7 +706,7 @@ typedef struct awsrc_probs {
  * max_draft drafts): their sequence, like one without rows, gets accepted 0,
  * tokens -1 and keep = kv_len.
  * Bit-reproducible. Errors: INVALID_ARG, SHAPE (vocab < 1), UNSUPPORTED (n_seq >
- * 65535, vocab > 2^24), WORKSPACE, CUDA.
+ * 65535, vocab > 2^18, max_draft > 2^20), WORKSPACE, CUDA.
  */
 awsrc_status awsrc_verify_drafts(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t max_draft,
                                  const int32_t* row_start, const int32_t* ids, const awsrc_probs* target,

@@ -105,7 +105,7 @@ awsrc_status awsrc_verify_drafts(int32_t n_seq, int32_t n_rows, int32_t vocab, i
                                  void* workspace, size_t workspace_bytes, void* stream) {
   if (n_seq < 0 || n_rows < 0 || max_draft < 0) return AWSRC_ERR_INVALID_ARG;
   if (vocab < 1) return AWSRC_ERR_SHAPE;
-  if (n_seq > 65535 || vocab > (1 << 24) || max_draft > (1 << 20)) return AWSRC_ERR_UNSUPPORTED;
+  if (n_seq > 65535 || vocab > (1 << 18) || max_draft > (1 << 20)) return AWSRC_ERR_UNSUPPORTED;
   if (!row_start || !ids || !target || !u || !r || !accepted || !tokens || !kv_len != !keep) return AWSRC_ERR_INVALID_ARG;
   awsrc_status s = check_rows(target->p, target->dtype);
   if (s != AWSRC_OK || (draft && (s = check_rows(draft->p, draft->dtype)) != AWSRC_OK)) return s;

@@ -55,10 +55,10 @@ def plan(page, table, length, free, count, keep, add, n_tok):
 
 
 def units(p):
-    """A probability in units of 2^-62, rounded down."""
+    """A probability in units of 2^-45, rounded to nearest even."""
     if math.isnan(p) or p <= 0:
         return 0
-    return int(Fraction(min(p, 1.0)) * 2 ** 62)
+    return round(Fraction(min(p, 1.0)) * 2 ** 45)
 
 
 def clean(p):

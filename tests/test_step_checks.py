@@ -56,7 +56,7 @@ def test_verification_of_no_sequences_passes():
 
 @pytest.mark.parametrize("kw,status", [
     (dict(n_seq=-1), INVALID), (dict(n_rows=-1), INVALID), (dict(max_draft=-1), INVALID), (dict(vocab=0), SHAPE),
-    (dict(n_seq=65536), UNSUPPORTED), (dict(vocab=(1 << 24) + 1), UNSUPPORTED), (dict(max_draft=(1 << 20) + 1), UNSUPPORTED),
+    (dict(n_seq=65536), UNSUPPORTED), (dict(vocab=(1 << 18) + 1), UNSUPPORTED), (dict(max_draft=(1 << 20) + 1), UNSUPPORTED),
     (dict(start=None), INVALID), (dict(ids=P + 2), INVALID), (dict(p=probs(p=None)), INVALID), (dict(p=probs(dtype=2)), INVALID),
     (dict(p=probs(p=P + 2)), INVALID), (dict(q=probs(dtype=3)), INVALID), (dict(q=probs(dtype=1, p=P + 1)), INVALID),
     (dict(u=None), INVALID), (dict(r=P + 1), INVALID), (dict(kv=None), INVALID), (dict(keep=None), INVALID),
