@@ -44,10 +44,16 @@ def _declare():
 _declare()
 
 
-def _ints(t, name: str, shape, device, dtype=torch.int32) -> int:
-    """Checks a contiguous tensor of whole numbers and returns its address."""
-    _require(t, name, dtype=dtype, shape=shape, device=device)
-    if not t.is_contiguous():
+_Tensor = torch.Tensor
+_I32, _I64, _F32, _U8 = torch.int32, torch.int64, torch.float32, torch.uint8
+
+
+# The checks are a small call's largest part: each looks at a tensor once and only
+# then finds out what is wrong with it.
+def _ints(t, name: str, shape, device, dtype=_I32) -> int:
+    """Checks a contiguous tensor of one dtype and returns its address."""
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous()):
+        _require(t, name, dtype=dtype, shape=shape, device=device)
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr() or _EMPTY
 
@@ -58,8 +64,8 @@ def _cuda(device: torch.device, what: str):
 
 
 def _workspace(t, device) -> torch.Tensor:
-    _require(t, "workspace", dtype=torch.uint8, device=device)
-    if not t.is_contiguous():
+    if not (isinstance(t, _Tensor) and t.dtype is _U8 and t.device == device and t.is_contiguous()):
+        _require(t, "workspace", dtype=_U8, device=device)
         raise ValueError("workspace must come from awsrc_step_workspace")
     return t
 
@@ -138,23 +144,27 @@ def awsrc_kv_plan(pool: KvPool, keep: Optional[torch.Tensor], add: torch.Tensor,
         raise TypeError("pool must come from awsrc_kv_pool")
     dev, n = pool.device, pool.n_seq
     if n_tok is None:
-        some = next((t for t in (tok_seq, tok_pos, tok_slot) if isinstance(t, torch.Tensor)), None)
-        if some is None:
+        for some in (tok_slot, tok_pos, tok_seq):
+            if isinstance(some, _Tensor):
+                n_tok = some.numel()
+                break
+        else:
             raise ValueError("n_tok is needed without tok_seq, tok_pos and tok_slot")
-        n_tok = some.numel()
     if n_tok < 0:
         raise ValueError("n_tok must not be negative")
-    kp = None if keep is None else _ints(keep, "keep", (n,), dev)
-    ap = _ints(add, "add", (n,), dev)
-    maps = [None if t is None else _ints(t, name, (n_tok,), dev, dt)
-            for name, t, dt in (("tok_seq", tok_seq, torch.int32), ("tok_pos", tok_pos, torch.int32),
-                                ("tok_slot", tok_slot, torch.int64))]
+    seqs, toks = (n,), (n_tok,)
+    kp = None if keep is None else _ints(keep, "keep", seqs, dev)
+    ap = _ints(add, "add", seqs, dev)
+    tp = None if tok_seq is None else _ints(tok_seq, "tok_seq", toks, dev)
+    pp = None if tok_pos is None else _ints(tok_pos, "tok_pos", toks, dev)
+    sp = None if tok_slot is None else _ints(tok_slot, "tok_slot", toks, dev, _I64)
     _workspace(workspace, dev)
-    _cuda(dev, "the pool")
+    if dev.type != "cuda":
+        _cuda(dev, "the pool")
     if q_start is None:
-        q_start = torch.empty(n + 1, dtype=torch.int32, device=dev)
+        q_start = torch.empty(n + 1, dtype=_I32, device=dev)
     qp = _ints(q_start, "q_start", (n + 1,), dev)
-    st = _on(dev, lib.awsrc_kv_plan, pool._ref, kp, ap, n_tok, qp, *maps, workspace.data_ptr(), workspace.numel(),
+    st = _on(dev, lib.awsrc_kv_plan, pool._ref, kp, ap, n_tok, qp, tp, pp, sp, workspace.data_ptr(), workspace.numel(),
              _stream(stream, dev))
     if st:
         _check(st, "kv_plan")
@@ -165,6 +175,10 @@ def awsrc_kv_plan(pool: KvPool, keep: Optional[torch.Tensor], add: torch.Tensor,
 
 
 def _probs(t, name: str, shape, device) -> _Probs:
+    if isinstance(t, _Tensor) and t.shape == shape and t.device == device:
+        dtype, (stride, one) = _DTYPES.get(t.dtype), t.stride()
+        if dtype is not None and (one == 1 or shape[1] == 1):
+            return _Probs(t.data_ptr() or _EMPTY, stride, dtype, 0)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, not {type(t).__name__}")
     if t.dtype not in _DTYPES:
@@ -173,9 +187,7 @@ def _probs(t, name: str, shape, device) -> _Probs:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have its rows' elements in a row (last stride 1, not {t.stride(1)})")
-    return _Probs(t.data_ptr() or _EMPTY, t.stride(0), _DTYPES[t.dtype], 0)
+    raise ValueError(f"{name} must have its rows' elements in a row (last stride 1, not {t.stride(1)})")
 
 
 def awsrc_verify_drafts(row_start: torch.Tensor, ids: torch.Tensor, target: torch.Tensor, draft: Optional[torch.Tensor],
@@ -191,38 +203,42 @@ def awsrc_verify_drafts(row_start: torch.Tensor, ids: torch.Tensor, target: torc
     accepted drafts, the token, -1 behind), int32. With kv_len (int32 [n_seq]),
     `keep` receives it less the drafts not accepted, as awsrc_kv_plan takes it;
     keep may be kv_len. max_draft defaults to that of `tokens`."""
-    _require(row_start, "row_start", dtype=torch.int32)
-    if row_start.dim() != 1 or row_start.shape[0] < 1:
+    if not isinstance(row_start, _Tensor) or row_start.dim() != 1 or row_start.shape[0] < 1:
+        _require(row_start, "row_start", dtype=_I32)
         raise ValueError(f"row_start has shape {tuple(row_start.shape)}, expected (n_seq + 1,)")
     n, dev = row_start.shape[0] - 1, row_start.device
     sp = _ints(row_start, "row_start", (n + 1,), dev)
-    if not isinstance(target, torch.Tensor) or target.dim() != 2 or target.shape[1] < 1:
+    if not isinstance(target, _Tensor) or target.dim() != 2 or target.shape[1] < 1:
         raise ValueError("target must be a 2-D tensor (rows x vocab)")
-    rows, vocab = target.shape
-    tp = _probs(target, "target", (rows, vocab), dev)
-    dp = None if draft is None else _probs(draft, "draft", (rows, vocab), dev)
-    ip = _ints(ids, "ids", (rows,), dev)
-    up = _ints(u, "u", (rows,), dev, torch.float32)
-    rp = _ints(r, "r", (n,), dev, torch.float32)
+    shape = target.shape
+    rows, vocab = shape
+    tp = _probs(target, "target", shape, dev)
+    dp = None if draft is None else _probs(draft, "draft", shape, dev)
+    seqs, all_rows = (n,), (rows,)
+    ip = _ints(ids, "ids", all_rows, dev)
+    up = _ints(u, "u", all_rows, dev, _F32)
+    rp = _ints(r, "r", seqs, dev, _F32)
     if tokens is not None:
-        _require(tokens, "tokens")
-        if tokens.dim() != 2 or tokens.shape[1] < 1:
+        if not isinstance(tokens, _Tensor) or tokens.dim() != 2 or tokens.shape[1] < 1:
+            _require(tokens, "tokens")
             raise ValueError(f"tokens has shape {tuple(tokens.shape)}, expected ({n}, max_draft + 1)")
         max_draft = tokens.shape[1] - 1 if max_draft is None else max_draft
     if max_draft is None or max_draft < 0:
         raise ValueError("max_draft (the most drafts of a sequence, not negative) is needed without tokens")
-    if (kv_len is None) and keep is not None:
+    if keep is not None and kv_len is None:
         raise ValueError("keep needs kv_len")
     _workspace(workspace, dev)
-    _cuda(dev, "row_start")
+    if dev.type != "cuda":
+        _cuda(dev, "row_start")
     if accepted is None:
-        accepted = torch.empty(n, dtype=torch.int32, device=dev)
+        accepted = torch.empty(n, dtype=_I32, device=dev)
     if tokens is None:
-        tokens = torch.empty(n, max_draft + 1, dtype=torch.int32, device=dev)
-    cp, op = _ints(accepted, "accepted", (n,), dev), _ints(tokens, "tokens", (n, max_draft + 1), dev)
+        tokens = torch.empty(n, max_draft + 1, dtype=_I32, device=dev)
+    cp, op = _ints(accepted, "accepted", seqs, dev), _ints(tokens, "tokens", (n, max_draft + 1), dev)
     lp = kp = None
-    if kv_len is not None and keep is not None:
-        lp, kp = _ints(kv_len, "kv_len", (n,), dev), _ints(keep, "keep", (n,), dev)
+    if keep is not None:
+        kp = _ints(keep, "keep", seqs, dev)
+        lp = kp if kv_len is keep else _ints(kv_len, "kv_len", seqs, dev)
     st = _on(dev, lib.awsrc_verify_drafts, n, rows, vocab, max_draft, sp, ip, tp, dp, up, rp, lp, cp, op, kp,
              workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
     if st:
@@ -274,6 +290,10 @@ def awsrc_fp8_matrix(rows: int, cols: int, device="cuda") -> Fp8Matrix:
 
 def _matrix(x, name: str, device=None):
     """Checks a 2-D float32 or bfloat16 tensor of any row stride: (address, dtype, stride)."""
+    if isinstance(x, _Tensor) and x.dim() == 2 and (device is None or x.device == device):
+        dtype, (stride, one) = _DTYPES.get(x.dtype), x.stride()
+        if dtype is not None and (one == 1 or x.shape[1] <= 1):
+            return x.data_ptr() or _EMPTY, dtype, stride
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, not {type(x).__name__}")
     if x.dtype not in _DTYPES:
@@ -282,9 +302,7 @@ def _matrix(x, name: str, device=None):
         raise ValueError(f"{name} must be 2-D, not {x.dim()}-D")
     if device is not None and x.device != device:
         raise ValueError(f"{name} is on {x.device}, expected {device}")
-    if x.shape[1] > 1 and x.stride(1) != 1:
-        raise ValueError(f"{name} must have its rows' elements in a row (last stride 1, not {x.stride(1)})")
-    return x.data_ptr() or _EMPTY, _DTYPES[x.dtype], x.stride(0)
+    raise ValueError(f"{name} must have its rows' elements in a row (last stride 1, not {x.stride(1)})")
 
 
 def _fp8(m, name: str, device=None) -> Fp8Matrix:
@@ -299,7 +317,8 @@ def awsrc_fp8_quantize(x: torch.Tensor, out: Optional[Fp8Matrix] = None, stream=
     """x (2-D, float32 or bfloat16, any row stride) in 8 bits; `out` reuses a matrix of its shape."""
     p, dt, stride = _matrix(x, "x")
     dev = x.device
-    _cuda(dev, "x")
+    if dev.type != "cuda":
+        _cuda(dev, "x")
     if out is None:
         out = awsrc_fp8_matrix(x.shape[0], x.shape[1], dev)
     _fp8(out, "out", dev)
@@ -329,7 +348,8 @@ def awsrc_fp8_gemm(x: Fp8Matrix, w: Fp8Matrix, workspace: torch.Tensor, out: Opt
     dev = _fp8(w, "w").device
     _fp8(x, "x", dev)
     _workspace(workspace, dev)
-    _cuda(dev, "w")
+    if dev.type != "cuda":
+        _cuda(dev, "w")
     out, yp, dt, ys = _product(x.rows, x.cols, w, out, out_dtype, dev)
     st = _on(dev, lib.awsrc_fp8_gemm, x._ref, w._ref, yp, dt, ys, workspace.data_ptr(), workspace.numel(),
              _stream(stream, dev))
@@ -350,7 +370,8 @@ def awsrc_fp8_linear(x: torch.Tensor, w: Fp8Matrix, x8: Fp8Matrix, workspace: to
     if (x8.rows, x8.cols) != tuple(x.shape):
         raise ValueError(f"x8 is {x8.rows} x {x8.cols}, x {x.shape[0]} x {x.shape[1]}")
     _workspace(workspace, dev)
-    _cuda(dev, "x")
+    if dev.type != "cuda":
+        _cuda(dev, "x")
     out, yp, yt, ys = _product(x.shape[0], x.shape[1], w, out, x.dtype, dev)
     st = _on(dev, lib.awsrc_fp8_linear, xp, xt, xs, x8._ref, w._ref, yp, yt, ys, workspace.data_ptr(), workspace.numel(),
              _stream(stream, dev))

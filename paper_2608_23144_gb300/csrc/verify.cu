@@ -24,11 +24,12 @@ namespace awsrc {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxThreads = 1024, kMaxWarps = kMaxThreads / 32;
+constexpr int kMaxCluster = 8, kMaxVocab = 1 << 18;
 constexpr int kGroup = 4;              // elements of a lane at a time, one vector load where rows allow it
 constexpr int kPiece = 32 * kGroup;    // of a warp
 constexpr int kAhead = 4;              // pieces whose loads are in flight together
+constexpr int kStep = kAhead * kPiece;
 
 // A probability p in [0, 1] in units of 2^-45, rounded to nearest even, as hi 2^23 + lo
 // and a constant. p + 2 rounds p to units of 2^-22, which the sum's bits count; what is
@@ -64,21 +65,39 @@ __device__ __forceinline__ uint64_t peer_sum(uint64_t* own, uint32_t rank) {
   return v;
 }
 
-// 4 elements from j on; 0 past `have`.
+// 4 elements from j on, as they lie in memory; 0 past `have`.
+template <typename T>
+struct Raw {
+  uint32_t w[sizeof(T)];
+};
 template <bool kVec>
-__device__ __forceinline__ float4 group(const float* p, int j, int have) {
-  if (kVec && have >= kGroup) return __ldcg(reinterpret_cast<const float4*>(p + j));
-  return make_float4(have > 0 ? p[j] : 0.0f, have > 1 ? p[j + 1] : 0.0f, have > 2 ? p[j + 2] : 0.0f, have > 3 ? p[j + 3] : 0.0f);
+__device__ __forceinline__ Raw<float> group(const float* p, int j, int have) {
+  Raw<float> r;
+  if (kVec && have >= kGroup) {
+    const uint4 v = __ldcg(reinterpret_cast<const uint4*>(p + j));
+    r.w[0] = v.x, r.w[1] = v.y, r.w[2] = v.z, r.w[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) r.w[i] = i < have ? __float_as_uint(p[j + i]) : 0u;
+  }
+  return r;
 }
 template <bool kVec>
-__device__ __forceinline__ float4 group(const __nv_bfloat16* p, int j, int have) {
+__device__ __forceinline__ Raw<__nv_bfloat16> group(const __nv_bfloat16* p, int j, int have) {
+  Raw<__nv_bfloat16> r;
   if (kVec && have >= kGroup) {
-    const uint2 x = __ldcg(reinterpret_cast<const uint2*>(p + j));
-    return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16),
-                       __uint_as_float(x.y & 0xFFFF0000u));
+    const uint2 v = __ldcg(reinterpret_cast<const uint2*>(p + j));
+    r.w[0] = v.x, r.w[1] = v.y;
+  } else {
+    const unsigned short* h = reinterpret_cast<const unsigned short*>(p + j);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r.w[i] = (2 * i < have ? h[2 * i] : 0u) | (2 * i + 1 < have ? (uint32_t)h[2 * i + 1] << 16 : 0u);
   }
-  return make_float4(have > 0 ? __bfloat162float(p[j]) : 0.0f, have > 1 ? __bfloat162float(p[j + 1]) : 0.0f,
-                     have > 2 ? __bfloat162float(p[j + 2]) : 0.0f, have > 3 ? __bfloat162float(p[j + 3]) : 0.0f);
+  return r;
+}
+__device__ __forceinline__ float at(const Raw<float>& r, int i) { return clean(__uint_as_float(r.w[i])); }
+__device__ __forceinline__ float at(const Raw<__nv_bfloat16>& r, int i) {
+  return clean(__uint_as_float(i & 1 ? r.w[i >> 1] & 0xFFFF0000u : r.w[i >> 1] << 16));
 }
 
 // The row that decides: weights p, p less q, or p but for one column.
@@ -94,44 +113,45 @@ struct Row {
 template <bool kVec, typename P, typename Q, typename F>
 __device__ __forceinline__ void pieces(const Row<P, Q>& r, int j0, int j1, F&& f) {
   const int lane = threadIdx.x & 31;
-  float4 p[kAhead], q[kAhead];
+  Raw<P> p[kAhead];
+  Raw<Q> q[kAhead];
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
     const int j = j0 + i * kPiece + lane * kGroup;
     p[i] = group<kVec>(r.p, j, j1 - j);
-    q[i] = r.q ? group<kVec>(r.q, j, j1 - j) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (r.q) q[i] = group<kVec>(r.q, j, j1 - j);
   }
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
-    const int at = r.drop - (j0 + i * kPiece + lane * kGroup);
-    float a[kGroup] = {clean(p[i].x), clean(p[i].y), clean(p[i].z), clean(p[i].w)};
-    const float b[kGroup] = {clean(q[i].x), clean(q[i].y), clean(q[i].z), clean(q[i].w)};
-    if (at >= 0 && at < kGroup) {
+    const int drop = r.drop - (j0 + i * kPiece + lane * kGroup);
+    float a[kGroup], b[kGroup];
 #pragma unroll
-      for (int k = 0; k < kGroup; ++k)
-        if (k == at) a[k] = 0.0f;
+    for (int k = 0; k < kGroup; ++k) {
+      a[k] = k == drop ? 0.0f : at(p[i], k);
+      b[k] = r.q ? at(q[i], k) : 0.0f;
     }
     if (f(i, a, b)) return;
   }
 }
 
 template <typename P, typename Q, bool kVec>
-__global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_constant__ VerifyArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const __grid_constant__ VerifyArgs a) {
   const P* probs_p = static_cast<const P*>(a.p);
   const Q* probs_q = static_cast<const Q*>(a.q);
-  __shared__ uint64_t s_warp[kWarps];
+  __shared__ uint64_t s_warp[kMaxWarps];
+  __shared__ uint64_t s_step[kMaxVocab / kStep];  // sums of the warps' steps
   __shared__ uint64_t s_all[2];  // this block's sum, of the first and of the second choice of weights
   __shared__ int s_stop;
   step_wait();
   step_trigger();
   const int size = (int)(gridDim.x / a.n_seq), b = blockIdx.x / size, rank = blockIdx.x % size;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int first = a.row_start[b], end = a.row_start[b + 1];
   const int drafts = end - first - 1;
   int32_t* tokens = a.tokens + (int64_t)b * (a.max_draft + 1);
   if (first < 0 || end < first || end > a.n_rows || drafts > a.max_draft || drafts < 0) {  // the same for the whole cluster
     if (rank == 0) {
-      for (int i = threadIdx.x; i <= a.max_draft; i += kThreads) tokens[i] = -1;
+      for (int i = threadIdx.x; i <= a.max_draft; i += blockDim.x) tokens[i] = -1;
       if (threadIdx.x == 0) {
         a.accepted[b] = 0;
         if (a.keep) a.keep[b] = a.kv_len[b];
@@ -171,13 +191,14 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     else row.drop = a.ids[t + 1];
   }
   // the run of a warp: whole pieces
-  const int runs = size * kWarps;
+  const int runs = size * warps;
   const int run = (a.vocab + kPiece * runs - 1) / (kPiece * runs) * kPiece;
-  const int j0 = min(a.vocab, (rank * kWarps + warp) * run), j1 = min(a.vocab, j0 + run);
+  const int j0 = min(a.vocab, (rank * warps + warp) * run), j1 = min(a.vocab, j0 + run);
   uint64_t total = 0, below = 0, mine = 0;
   for (int choice = 0; choice < 2; ++choice) {
     uint64_t sum = 0;
-    for (int j = j0; j < j1; j += kAhead * kPiece) {
+    uint64_t* step = s_step + warp * ((run + kStep - 1) / kStep);
+    for (int j = j0; j < j1; j += kStep, ++step) {
       int hi = 0, lo = 0;  // of 16 elements: far from 2^31
       pieces<kVec>(row, j, j1, [&](int, const float* p, const float* q) {
 #pragma unroll
@@ -187,14 +208,19 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         }
         return false;
       });
-      sum += (uint64_t)(((int64_t)hi << 23) + lo);
+      // units of a step, at most 2^45 for each of 16 elements a lane
+      uint64_t all = (uint64_t)(((int64_t)hi << 23) + lo);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+      if (lane == 0) *step = all;
+      sum += all;
     }
-    mine = __shfl_sync(0xffffffffu, warp_incl(sum), 31);
+    mine = sum;
     if (lane == 0) s_warp[warp] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
       uint64_t all = 0;
-      for (int w = 0; w < kWarps; ++w) all += s_warp[w];
+      for (int w = 0; w < warps; ++w) all += s_warp[w];
       s_all[choice] = all;
     }
     cluster_sync();
@@ -212,37 +238,39 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
   // floor(r total), r in units of 2^-64
   const float r = a.r[b];
   const uint64_t ru = r >= 1.0f ? ~0ull : r > 0.0f ? __float2ull_rz(__fmul_rn(r, 0x1p64f)) : 0;
-  const uint64_t at = __umul64hi(total, ru);
-  if (total != 0 && below <= at && at < below + mine) {
+  const uint64_t bar = __umul64hi(total, ru);
+  if (total != 0 && below <= bar && bar < below + mine) {
+    // the step that it falls in, and its elements again
     uint64_t sum = below;
-    bool found = false;
-    for (int j = j0; j < j1 && !found; j += kAhead * kPiece)
-      pieces<kVec>(row, j, j1, [&](int i, const float* p, const float* q) {
-        uint64_t w[kGroup], own = 0;
+    const uint64_t* step = s_step + warp * ((run + kStep - 1) / kStep);
+    int j = j0;
+    for (; sum + *step <= bar; j += kStep) sum += *step++;
+    pieces<kVec>(row, j, j1, [&](int i, const float* p, const float* q) {
+      uint64_t w[kGroup], own = 0;
 #pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-          const Units up = units(p[k]), uq = units(q[k]);
-          w[k] = p[k] > q[k] ? (uint64_t)(((int64_t)(up.hi - uq.hi) << 23) + (up.lo - uq.lo)) : 0;
-          own += w[k];
+      for (int k = 0; k < kGroup; ++k) {
+        const Units up = units(p[k]), uq = units(q[k]);
+        w[k] = p[k] > q[k] ? (uint64_t)(((int64_t)(up.hi - uq.hi) << 23) + (up.lo - uq.lo)) : 0;
+        own += w[k];
+      }
+      const uint64_t upto = sum + warp_incl(own);
+      const uint32_t hit = __ballot_sync(0xffffffffu, upto > bar);
+      sum = __shfl_sync(0xffffffffu, upto, 31);
+      if (!hit) return false;
+      if (lane == __ffs(hit) - 1) {
+        uint64_t c = upto - own;
+        int k = 0;
+        for (; k < kGroup - 1; ++k) {
+          c += w[k];
+          if (c > bar) break;
         }
-        const uint64_t upto = sum + warp_incl(own);
-        const uint32_t hit = __ballot_sync(0xffffffffu, upto > at);
-        sum = __shfl_sync(0xffffffffu, upto, 31);
-        if (!hit) return false;
-        if (lane == __ffs(hit) - 1) {
-          uint64_t c = upto - own;
-          int k = 0;
-          for (; k < kGroup - 1; ++k) {
-            c += w[k];
-            if (c > at) break;
-          }
-          tokens[stop] = j + i * kPiece + lane * kGroup + k;
-        }
-        return found = true;
-      });
+        tokens[stop] = j + i * kPiece + lane * kGroup + k;
+      }
+      return true;
+    });
   }
   if (rank == 0) {
-    for (int i = threadIdx.x; i <= a.max_draft; i += kThreads)
+    for (int i = threadIdx.x; i <= a.max_draft; i += blockDim.x)
       if (i != stop) tokens[i] = i < stop ? a.ids[first + 1 + i] : -1;
       else if (total == 0) tokens[i] = -1;
     if (threadIdx.x == 0) {
@@ -255,10 +283,12 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
 
 template <typename P, typename Q, bool kVec>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
-  // as many thread blocks as run at a time, twice: no more are of use to a sequence
-  int size = kMaxCluster;
-  while (size > 1 && (int64_t)a.n_seq * size > 2 * 608) size /= 2;
-  return launch_step(verify_kernel<P, Q, kVec>, dim3((unsigned)(a.n_seq * size)), kThreads, 0, size, st, a);
+  // all SMs for few sequences, up to 1024 threads each while a warp has a whole step;
+  // 8 blocks a sequence until there are twice as many as run at a time
+  int size = kMaxCluster, threads = kMaxThreads;
+  while (threads > 256 && ((int64_t)a.n_seq * size * threads > 152 * 1024 || a.vocab < size * threads / 32 * kStep)) threads /= 2;
+  while (size > 1 && (int64_t)a.n_seq * size > 2 * 152 * 4) size /= 2;
+  return launch_step(verify_kernel<P, Q, kVec>, dim3((unsigned)(a.n_seq * size)), threads, 0, size, st, a);
 }
 template <typename P, typename Q>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
