@@ -352,10 +352,20 @@ __device__ void write_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x, uint
 // The cluster's parts of a tile joined; each thread block joins its share of the elements.
 template <int N, Source X>
 __device__ void join(const GemmArgs& a, Smem<N, X>& sm) {
-  const int rank = blockIdx.x % a.split, row0 = blockIdx.x / a.split * a.n, per = a.n / 4;
-  for (int e = rank * kThreads + threadIdx.x; e < a.x.rows * per; e += a.split * kThreads) {
-    const int tok = e / per, r = e % per * 4;
-    put4(a, tok, row0 + r, join4(smem_addr(sm.tile[0]) + 4 * (tok * BM + r), 0, 1, a.split));
+  constexpr int kAhead = 2;  // parts of so many elements under way together
+  const int rank = blockIdx.x % a.split, row0 = blockIdx.x / a.split * a.n, per = a.n / 4, step = a.split * kThreads;
+  for (int e0 = rank * kThreads + threadIdx.x; e0 < a.x.rows * per; e0 += kAhead * step) {
+    float4 v[kAhead][kMaxSplit];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int e = e0 + i * step;
+      if (e < a.x.rows * per) get_parts<kMaxSplit>(v[i], smem_addr(sm.tile[0]) + 4 * (e / per * BM + e % per * 4), 0, 1, a.split);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int e = e0 + i * step;
+      if (e < a.x.rows * per) put4(a, e / per, row0 + e % per * 4, sum_parts<kMaxSplit>(v[i], a.split));
+    }
   }
 }
 
@@ -447,7 +457,7 @@ cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
   constexpr int kSmem = (int)sizeof(Smem<N, X>) + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
   static_assert(N * BM * 4 <= C::kStages * C::kStageBytes, "a part of a tile fits into the stages");
-  const cudaError_t e = cudaFuncSetAttribute(fp8_few_kernel<N, X>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  const cudaError_t e = allow_smem<C>(fp8_few_kernel<N, X>, kSmem);
   if (e != cudaSuccess) return e;
   const int tiles = (a.w.rows + a.n - 1) / a.n;
   const int grid = a.split > 1 ? tiles * a.split : tiles < kSms ? tiles : kSms;

@@ -122,21 +122,24 @@ __device__ __forceinline__ void put(const GemmArgs& a, int tok, int row, float v
   else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
 }
 
-// Element e of a tile's parts in the shared memory of `split` thread blocks, rank0
-// being the first and `every` the step between them: summed in their order.
-__device__ __forceinline__ float4 join4(uint32_t addr, int rank0, int every, int split) {
-  float4 v[8], sum;
+// Four floats at `addr` in the shared memory of each of `split` thread blocks, rank0
+// being the first and `every` the step between them.
+template <int kSplit>
+__device__ __forceinline__ void get_parts(float4* v, uint32_t addr, int rank0, int every, int split) {
 #pragma unroll
-  for (int z = 0; z < 8; ++z)
+  for (int z = 0; z < kSplit; ++z)
     if (z < split) {
       uint32_t peer;
       asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(addr), "r"(rank0 + z * every));
       asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
                    : "=f"(v[z].x), "=f"(v[z].y), "=f"(v[z].z), "=f"(v[z].w) : "r"(peer) : "memory");
     }
-  sum = v[0];
+}
+template <int kSplit>
+__device__ __forceinline__ float4 sum_parts(const float4* v, int split) {
+  float4 sum = v[0];
 #pragma unroll
-  for (int z = 1; z < 8; ++z)
+  for (int z = 1; z < kSplit; ++z)
     if (z < split)
       sum = make_float4(__fadd_rn(sum.x, v[z].x), __fadd_rn(sum.y, v[z].y), __fadd_rn(sum.z, v[z].z), __fadd_rn(sum.w, v[z].w));
   return sum;

@@ -346,8 +346,19 @@ __device__ void join(const GemmArgs& a, Smem& sm, uint32_t half) {
   const Walk w(a);
   const int share = (blockIdx.x >> 1) % a.split, row0 = w.row + BM * half;
   const int cols = min(a.n, a.x.rows - w.tok);
-  for (int e = share * kThreads + threadIdx.x; e < cols * (BM / 4); e += a.split * kThreads)
-    put4(a, w.tok + e / (BM / 4), row0 + e % (BM / 4) * 4, join4(smem_addr(sm.tile[0]) + 16 * e, half, 2, a.split));
+  constexpr int kAhead = 4;  // parts of so many elements under way together
+  const int step = a.split * kThreads;
+  for (int e0 = share * kThreads + threadIdx.x; e0 < cols * (BM / 4); e0 += kAhead * step) {
+    float4 v[kAhead][kMaxSplit];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (e0 + i * step < cols * (BM / 4)) get_parts<kMaxSplit>(v[i], smem_addr(sm.tile[0]) + 16 * (e0 + i * step), half, 2, a.split);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int e = e0 + i * step;
+      if (e < cols * (BM / 4)) put4(a, w.tok + e / (BM / 4), row0 + e % (BM / 4) * 4, sum_parts<kMaxSplit>(v[i], a.split));
+    }
+  }
 }
 
 __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_constant__ PairArgs p) {
@@ -433,7 +444,7 @@ cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
   static_assert(kMaxN * BM * 4 <= kStages * kStageBytes, "a part of a tile fits into the stages");
   static_assert(2 * kTwoBufs <= kSfAt && kMaxN <= kSfAt, "accumulators end before the scales");
-  cudaError_t e = cudaFuncSetAttribute(fp8_pairs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  cudaError_t e = allow_smem<Smem>(fp8_pairs_kernel, kSmem);
   PairArgs p;
   p.g = a;
   const int blocks = a.x.blocks(), fours = (blocks + 3) / 4;
@@ -487,7 +498,7 @@ int max_clusters(int size) {
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   int n = 0;
-  if (cudaFuncSetAttribute(fp8_pairs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
+  if (allow_smem<Smem>(fp8_pairs_kernel, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
       cudaOccupancyMaxActiveClusters(&n, fp8_pairs_kernel, &cfg) != cudaSuccess) {
     (void)cudaGetLastError();  // no split, then
     n = 0;

@@ -2,6 +2,8 @@
 // share: their arguments and the launch that overlaps the kernel before.
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace awsrc {
@@ -30,6 +32,20 @@ cudaError_t launch_step(K kernel, dim3 grid, int threads, size_t smem, int clust
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, a...);
+}
+
+// Lets a kernel use `bytes` of shared memory: once per device and kernel (K: a type of
+// its own for each, such as its configuration).
+template <typename K, typename F>
+cudaError_t allow_smem(F kernel, int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return cudaSuccess;
+  const cudaError_t s = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (s == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return s;
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {

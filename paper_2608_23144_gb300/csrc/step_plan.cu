@@ -30,18 +30,28 @@ __device__ __forceinline__ int64_t warp_incl(int64_t v) {
   }
   return v;
 }
-template <int kThreads>
+// Of the first kGroup threads' sums; every thread of the block calls it.
+template <int kGroup>
 __device__ Sum3 block_excl(Sum3 v, Sum3* total, Sum3* warps) {
+  constexpr int kWarps = kGroup / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Sum3 i{warp_incl(v.a), warp_incl(v.b), warp_incl(v.c)};
+  Sum3 i{0, 0, 0};
   __syncthreads();  // warps[] of the sum before is read
-  if (lane == 31) warps[warp] = i;
+  if (warp < kWarps) {
+    i = Sum3{warp_incl(v.a), warp_incl(v.b), warp_incl(v.c)};
+    if (lane == 31) warps[warp] = i;
+  }
   __syncthreads();
-  const Sum3 w = lane < kThreads / 32 ? warps[lane] : Sum3{0, 0, 0};
-  const Sum3 wi{warp_incl(w.a), warp_incl(w.b), warp_incl(w.c)};
-  *total = Sum3{__shfl_sync(0xffffffffu, wi.a, 31), __shfl_sync(0xffffffffu, wi.b, 31), __shfl_sync(0xffffffffu, wi.c, 31)};
-  const Sum3 before{__shfl_sync(0xffffffffu, wi.a - w.a, warp), __shfl_sync(0xffffffffu, wi.b - w.b, warp),
-                    __shfl_sync(0xffffffffu, wi.c - w.c, warp)};
+  if (warp == 0) {
+    const Sum3 w = lane < kWarps ? warps[lane] : Sum3{0, 0, 0};
+    const Sum3 wi{warp_incl(w.a), warp_incl(w.b), warp_incl(w.c)};
+    __syncwarp();
+    if (lane < kWarps) warps[lane] = Sum3{wi.a - w.a, wi.b - w.b, wi.c - w.c};
+    if (lane == 31) warps[32] = wi;
+  }
+  __syncthreads();
+  *total = warps[32];
+  const Sum3 before = warps[warp < kWarps ? warp : 0];
   return Sum3{before.a + i.a - v.a, before.b + i.b - v.b, before.c + i.c - v.c};
 }
 
@@ -95,12 +105,18 @@ __device__ __forceinline__ void put4(T* p, int t, int n, bool vec, const T* v) {
     if (t + i < n) p[t + i] = v[i];
 }
 
-template <int kThreads>
+// Needs and pages given back of a sequence, from shared memory.
+__device__ __forceinline__ int want_of(int held, int keep, int add, int log_page) {
+  return held < 0 ? 0 : pages_of((int64_t)keep + add, log_page);  // -1: an entry that cannot be right
+}
+
+// kGroup threads make the sums (a shuffle passes one warp per cycle, so 32 warps' took 4 us).
+template <int kThreads, int kGroup>
 __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ PlanArgs a) {
   extern __shared__ int sm[];
-  __shared__ Sum3 warps[32];
+  __shared__ Sum3 warps[33];
   const int n = a.n_seq;
-  int* s_tok = sm;               // n + 1: first token of a sequence
+  int* s_tok = sm;               // n + 1: first token of a sequence (first: its new tokens)
   int* s_pop = sm + (n + 1);     // first page handed out
   int* s_back = sm + 2 * (n + 1);  // first page given back
   int* s_held = sm + 3 * (n + 1);  // pages held, -1 for an entry that cannot be right
@@ -108,48 +124,49 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
   step_wait();
   step_trigger();
   const int tid = threadIdx.x, rank = cluster_rank();
-  const int per = (n + kThreads - 1) / kThreads;
-  const int b0 = min(n, tid * per), b1 = min(n, b0 + per);
   const int count = *a.count;
-
-  // who finds room
-  Sum3 v{0, 0, 0}, total;
   bool bad = false;
-  for (int b = b0; b < b1; ++b) {
+  for (int b = tid; b < n; b += kThreads) {
     const Entry e = load_entry(a, b);
     bad |= !e.ok;
-    const int held = e.ok ? pages_of(e.len, a.log_page) : 0, want = e.ok ? pages_of((int64_t)e.keep + e.add, a.log_page) : 0;
+    s_held[b] = e.ok ? pages_of(e.len, a.log_page) : -1;
+    s_keep[b] = e.keep;
+    s_tok[b] = e.add;
+  }
+  __syncthreads();
+  const int per = (n + kGroup - 1) / kGroup;
+  const int b0 = tid < kGroup ? min(n, tid * per) : n, b1 = min(n, b0 + per);
+  Sum3 v{0, 0, 0}, total;
+  for (int b = b0; b < b1; ++b) {
+    const int held = max(0, s_held[b]), want = want_of(s_held[b], s_keep[b], s_tok[b], a.log_page);
     v.a += max(0, want - held);
-    v.b += e.add;
+    v.b += s_tok[b];
     v.c += max(0, held - want);
   }
-  Sum3 before = block_excl<kThreads>(v, &total, warps);
+  Sum3 before = block_excl<kGroup>(v, &total, warps);
   const int64_t room = count + total.c;
-  Sum3 got{0, 0, 0};
   bool short_ = false;
-  for (int b = b0; b < b1; ++b) {
-    const Entry e = load_entry(a, b);
-    const int held = e.ok ? pages_of(e.len, a.log_page) : 0;
-    int want = e.ok ? pages_of((int64_t)e.keep + e.add, a.log_page) : 0, add = e.add;
-    before.a += max(0, want - held);
-    before.b += add;
-    if ((want > held && before.a > room) || before.b > a.n_tok) {
-      short_ |= add > 0;
-      add = 0;
-      want = e.ok ? pages_of(e.keep, a.log_page) : 0;
+  if (total.a > room || total.b > a.n_tok) {  // not all find room: who does
+    Sum3 got{0, 0, 0};
+    for (int b = b0; b < b1; ++b) {
+      const int held = max(0, s_held[b]), add = s_tok[b];
+      int want = want_of(s_held[b], s_keep[b], add, a.log_page);
+      before.a += max(0, want - held);
+      before.b += add;
+      if ((want > held && before.a > room) || before.b > a.n_tok) {
+        short_ |= add > 0;
+        s_tok[b] = 0;
+        want = want_of(s_held[b], s_keep[b], 0, a.log_page);
+      }
+      got.a += max(0, want - held);
+      got.b += s_tok[b];
+      got.c += max(0, held - want);
     }
-    s_held[b] = e.ok ? held : -1;
-    s_keep[b] = e.keep;
-    s_tok[b] = add;
-    got.a += max(0, want - held);
-    got.b += add;
-    got.c += max(0, held - want);
+    before = block_excl<kGroup>(got, &total, warps);
   }
-  before = block_excl<kThreads>(got, &total, warps);
   const bool wrong = count < 0 || count > a.n_pages || count + total.c > a.n_pages;
   for (int b = b0; b < b1; ++b) {
-    const int add = s_tok[b], held = max(0, s_held[b]);
-    const int want = s_held[b] < 0 ? 0 : pages_of((int64_t)s_keep[b] + add, a.log_page);
+    const int add = s_tok[b], held = max(0, s_held[b]), want = want_of(s_held[b], s_keep[b], add, a.log_page);
     s_pop[b] = (int)before.a;
     s_tok[b] = (int)before.b;
     s_back[b] = (int)before.c;
@@ -221,15 +238,15 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
   }
 }
 
-template <int kThreads>
+template <int kThreads, int kGroup>
 cudaError_t launch(const PlanArgs& a, int cluster, cudaStream_t st) {
   const size_t smem = (size_t)5 * (a.n_seq + 1) * sizeof(int);
   if (smem > 47 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(plan_kernel<kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    const cudaError_t e = cudaFuncSetAttribute(plan_kernel<kThreads, kGroup>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                5 * (kPlanMaxSeq + 1) * (int)sizeof(int));
     if (e != cudaSuccess) return e;
   }
-  return launch_step(plan_kernel<kThreads>, dim3(cluster), kThreads, smem, cluster, st, a);
+  return launch_step(plan_kernel<kThreads, kGroup>, dim3(cluster), kThreads, smem, cluster, st, a);
 }
 
 }  // namespace
@@ -239,7 +256,7 @@ cudaError_t launch_plan(const PlanArgs& in, cudaStream_t st) {
   a.vec = ((reinterpret_cast<uintptr_t>(a.tok_seq) | reinterpret_cast<uintptr_t>(a.tok_pos) |
             reinterpret_cast<uintptr_t>(a.tok_slot)) & 15) == 0;
   const bool small = a.n_seq <= 512 && a.n_tok <= 2048;
-  const cudaError_t e = small ? launch<256>(a, 1, st) : launch<1024>(a, 8, st);
+  const cudaError_t e = small ? launch<256, 256>(a, 1, st) : a.n_seq <= 2048 ? launch<1024, 256>(a, 8, st) : launch<1024, 1024>(a, 8, st);
   if (e != cudaSuccess) return e;
   note_launches(1);
   return cudaGetLastError();

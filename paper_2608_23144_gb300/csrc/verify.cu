@@ -41,7 +41,7 @@ __device__ __forceinline__ Units units(float p) {
   const float t = __fadd_rn(p, 2.0f), rest = __fsub_rn(p, __fsub_rn(t, 2.0f));
   return Units{__float_as_int(t), __float_as_int(__fadd_rn(rest, 0x3p-23f))};
 }
-__device__ __forceinline__ float clean(float p) { return fminf(fmaxf(p, 0.0f), 1.0f); }  // NaN: 0
+__device__ __forceinline__ float clean(float p) { return __saturatef(p); }  // to [0, 1], NaN: 0
 
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -100,17 +100,17 @@ __device__ __forceinline__ float at(const Raw<__nv_bfloat16>& r, int i) {
   return clean(__uint_as_float(i & 1 ? r.w[i >> 1] & 0xFFFF0000u : r.w[i >> 1] << 16));
 }
 
-// The row that decides: weights p, p less q, or p but for one column.
+// The row that decides: weights p less q (kDiff), or p but for at most one column.
 template <typename P, typename Q>
 struct Row {
   const P* p;
-  const Q* q;     // row of the draft model, or null
+  const Q* q;     // row of the draft model
   int drop;       // column whose weight is 0 (a draft of certainty that was not accepted), or -1
 };
 
-// kAhead pieces of the row from j0 on, up to j1: f(piece, the lane's probabilities, made
-// clean; q below p everywhere where there is none); true ends the walk.
-template <bool kVec, typename P, typename Q, typename F>
+// kAhead pieces of the row from j0 on, up to j1: f(piece, hi, lo) with the units of the
+// lane's 4 weights; true ends the walk.
+template <bool kVec, bool kDiff, typename P, typename Q, typename F>
 __device__ __forceinline__ void pieces(const Row<P, Q>& r, int j0, int j1, F&& f) {
   const int lane = threadIdx.x & 31;
   Raw<P> p[kAhead];
@@ -119,19 +119,68 @@ __device__ __forceinline__ void pieces(const Row<P, Q>& r, int j0, int j1, F&& f
   for (int i = 0; i < kAhead; ++i) {
     const int j = j0 + i * kPiece + lane * kGroup;
     p[i] = group<kVec>(r.p, j, j1 - j);
-    if (r.q) q[i] = group<kVec>(r.q, j, j1 - j);
+    if (kDiff) q[i] = group<kVec>(r.q, j, j1 - j);
   }
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
-    const int drop = r.drop - (j0 + i * kPiece + lane * kGroup);
-    float a[kGroup], b[kGroup];
+    int hi[kGroup], lo[kGroup];
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) {
-      a[k] = k == drop ? 0.0f : at(p[i], k);
-      b[k] = r.q ? at(q[i], k) : 0.0f;
+      const float a = at(p[i], k), b = kDiff ? at(q[i], k) : 0.0f;
+      const Units ua = units(a), ub = units(b);
+      const bool more = kDiff ? a > b : j0 + i * kPiece + lane * kGroup + k != r.drop;
+      hi[k] = more ? ua.hi - ub.hi : 0;
+      lo[k] = more ? ua.lo - ub.lo : 0;
     }
-    if (f(i, a, b)) return;
+    if (f(i, hi, lo)) return;
   }
+}
+
+// Sum of a warp's run [j0, j1); the sums of its steps in step[].
+template <bool kVec, bool kDiff, typename P, typename Q>
+__device__ __forceinline__ uint64_t run_sum(const Row<P, Q>& row, int j0, int j1, uint64_t* step) {
+  uint64_t sum = 0;
+  for (int j = j0; j < j1; j += kStep, ++step) {
+    int hi = 0, lo = 0;  // of 16 elements: far from 2^31
+    pieces<kVec, kDiff>(row, j, j1, [&](int, const int* h, const int* l) {
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) hi += h[k], lo += l[k];
+      return false;
+    });
+    uint64_t all = (uint64_t)(((int64_t)hi << 23) + lo);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+    if ((threadIdx.x & 31) == 0) *step = all;
+    sum += all;
+  }
+  return sum;
+}
+
+// The first element of the step from j on whose running sum, `sum` before the step, is above bar; -1 on lanes that do not hold it.
+template <bool kVec, bool kDiff, typename P, typename Q>
+__device__ __forceinline__ int find_in(const Row<P, Q>& row, int j, int j1, uint64_t sum, uint64_t bar) {
+  const int lane = threadIdx.x & 31;
+  int found = -1;
+  pieces<kVec, kDiff>(row, j, j1, [&](int i, const int* h, const int* l) {
+    uint64_t w[kGroup], own = 0;
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) own += w[k] = (uint64_t)(((int64_t)h[k] << 23) + l[k]);
+    const uint64_t upto = sum + warp_incl(own);
+    const uint32_t hit = __ballot_sync(0xffffffffu, upto > bar);
+    sum = __shfl_sync(0xffffffffu, upto, 31);
+    if (!hit) return false;
+    if (lane == __ffs(hit) - 1) {
+      uint64_t c = upto - own;
+      int k = 0;
+      for (; k < kGroup - 1; ++k) {
+        c += w[k];
+        if (c > bar) break;
+      }
+      found = j + i * kPiece + lane * kGroup + k;
+    }
+    return true;
+  });
+  return found;
 }
 
 template <typename P, typename Q, bool kVec>
@@ -171,8 +220,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const __grid_con
         refuse = true;
         if (x >= 0 && x < a.vocab) {
           const float p = value(probs_p[t * a.ps + x]), q = a.q ? value(probs_q[t * a.qs + x]) : 1.0f, u = a.u[t];
-          const float pc = fminf(fmaxf(p, 0.0f), 1.0f), qc = fminf(fmaxf(q, 0.0f), 1.0f), uc = fmaxf(u, 0.0f);
-          refuse = !((double)uc * (double)qc < (double)pc);
+          refuse = !((double)fmaxf(u, 0.0f) * (double)clean(q) < (double)clean(p));
         } else if (rank == 0) {
           atomicOr(a.status, kFaultBatch);
         }
@@ -195,27 +243,9 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const __grid_con
   const int run = (a.vocab + kPiece * runs - 1) / (kPiece * runs) * kPiece;
   const int j0 = min(a.vocab, (rank * warps + warp) * run), j1 = min(a.vocab, j0 + run);
   uint64_t total = 0, below = 0, mine = 0;
+  uint64_t* step = s_step + warp * ((run + kStep - 1) / kStep);
   for (int choice = 0; choice < 2; ++choice) {
-    uint64_t sum = 0;
-    uint64_t* step = s_step + warp * ((run + kStep - 1) / kStep);
-    for (int j = j0; j < j1; j += kStep, ++step) {
-      int hi = 0, lo = 0;  // of 16 elements: far from 2^31
-      pieces<kVec>(row, j, j1, [&](int, const float* p, const float* q) {
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-          const Units up = units(p[k]), uq = units(q[k]);
-          if (p[k] > q[k]) hi += up.hi - uq.hi, lo += up.lo - uq.lo;
-        }
-        return false;
-      });
-      // units of a step, at most 2^45 for each of 16 elements a lane
-      uint64_t all = (uint64_t)(((int64_t)hi << 23) + lo);
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
-      if (lane == 0) *step = all;
-      sum += all;
-    }
-    mine = sum;
+    mine = row.q ? run_sum<kVec, true>(row, j0, j1, step) : run_sum<kVec, false>(row, j0, j1, step);
     if (lane == 0) s_warp[warp] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -242,32 +272,10 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const __grid_con
   if (total != 0 && below <= bar && bar < below + mine) {
     // the step that it falls in, and its elements again
     uint64_t sum = below;
-    const uint64_t* step = s_step + warp * ((run + kStep - 1) / kStep);
     int j = j0;
     for (; sum + *step <= bar; j += kStep) sum += *step++;
-    pieces<kVec>(row, j, j1, [&](int i, const float* p, const float* q) {
-      uint64_t w[kGroup], own = 0;
-#pragma unroll
-      for (int k = 0; k < kGroup; ++k) {
-        const Units up = units(p[k]), uq = units(q[k]);
-        w[k] = p[k] > q[k] ? (uint64_t)(((int64_t)(up.hi - uq.hi) << 23) + (up.lo - uq.lo)) : 0;
-        own += w[k];
-      }
-      const uint64_t upto = sum + warp_incl(own);
-      const uint32_t hit = __ballot_sync(0xffffffffu, upto > bar);
-      sum = __shfl_sync(0xffffffffu, upto, 31);
-      if (!hit) return false;
-      if (lane == __ffs(hit) - 1) {
-        uint64_t c = upto - own;
-        int k = 0;
-        for (; k < kGroup - 1; ++k) {
-          c += w[k];
-          if (c > bar) break;
-        }
-        tokens[stop] = j + i * kPiece + lane * kGroup + k;
-      }
-      return true;
-    });
+    const int token = row.q ? find_in<kVec, true>(row, j, j1, sum, bar) : find_in<kVec, false>(row, j, j1, sum, bar);
+    if (token >= 0) tokens[stop] = token;
   }
   if (rank == 0) {
     for (int i = threadIdx.x; i <= a.max_draft; i += blockDim.x)
