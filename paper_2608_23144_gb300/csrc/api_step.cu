@@ -9,7 +9,8 @@ namespace awsrc {
 
 namespace {
 
-constexpr size_t kStepWorkspace = kStatusBytes;
+constexpr size_t kStepWorkspace = kStatusBytes;  // the fault word, and the plan's counter
+constexpr int kArrivedAt = 32;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool is_dtype(int32_t d) { return d == AWSRC_DTYPE_F32 || d == AWSRC_DTYPE_BF16; }
@@ -93,7 +94,7 @@ awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const
   if (s != AWSRC_OK) return s;
   PlanArgs a{pool->n_pages, pool->page, 4, pool->n_seq, pool->table_stride, n_tok, pool->page_table, pool->kv_len,
              pool->free_pages, pool->free_count, keep, add, q_start, tok_seq, tok_pos, tok_slot,
-             static_cast<uint32_t*>(workspace), 0};
+             static_cast<uint32_t*>(workspace), static_cast<uint32_t*>(workspace) + kArrivedAt, 0};
   while ((1 << a.log_page) < a.page) ++a.log_page;
   const cudaError_t e = launch_plan(a, (cudaStream_t)stream);
   return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "kv_plan");

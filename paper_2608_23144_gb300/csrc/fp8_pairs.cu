@@ -367,6 +367,8 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_con
   Smem& sm = *reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u));
   const int warp = threadIdx.x >> 5;
   const uint32_t rank = cluster_rank(), half = rank & 1, even = rank & ~1u;
+  if (warp == kCopyWarp && (threadIdx.x & 31) < 4)  // the four tensors' descriptors
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.w_codes + (threadIdx.x & 31)) : "memory");
   if (warp == kMmaWarp) {
     if ((threadIdx.x & 31) == 0) {
       for (int i = 0; i < kStages; ++i) mbar_init(&sm.full[i], 1);

@@ -67,7 +67,8 @@ struct PlanArgs {
   int32_t *q_start, *tok_seq, *tok_pos;
   int64_t* tok_slot;
   uint32_t* status;
-  int vec;  // the maps start on 16-byte boundaries
+  uint32_t* arrived;  // thread blocks that have read the lengths: 0 between calls
+  int vec;            // the maps start on 16-byte boundaries
 };
 cudaError_t launch_plan(const PlanArgs& a, cudaStream_t st);
 
