@@ -747,14 +747,16 @@ awsrc_status awsrc_fp8_quantize(const void* x, int32_t dtype, int64_t stride, co
 /*
  * awsrc_fp8_gemm — y[t][i] = sum_k x[t][k] w[i][k] for two matrices held in 8
  * bits (activations x, weights w laid out once), y of dtype F32 or BF16 with
- * element (t, i) at t * y_stride + i. Products and scales are exact, sums are in
- * binary32 in a fixed order (results repeat bit for bit); the tensor cores cut
- * their running sums off instead of rounding them, so F32 sums are taken over at
- * most 2048 columns there and joined by rounded additions. A block that holds
+ * element (t, i) at t * y_stride + i; its rows must not share elements, nor y any
+ * with the inputs. Products and scales are exact, sums are in binary32 in a fixed
+ * order (results repeat bit for bit on a device); the tensor cores cut their
+ * running sums off instead of rounding them, so sums are taken over at most 2048
+ * columns there (BF16: 32768) and joined by rounded additions. A block that holds
  * NaN makes the sums it takes part in NaN.
  * awsrc_fp8_linear — awsrc_fp8_quantize of x to x8 and awsrc_fp8_gemm with it in
- * one call, the same results bit for bit: y = x w^T.
- * Errors: INVALID_ARG, SHAPE (x.cols != w.cols), UNSUPPORTED, WORKSPACE, CUDA.
+ * one call, the same results bit for bit: y = x w^T. x8 is not w.
+ * Errors: INVALID_ARG, SHAPE (x.cols != w.cols), UNSUPPORTED (more tiles than 32
+ * bits number), WORKSPACE, CUDA.
  */
 awsrc_status awsrc_fp8_gemm(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, void* y, int32_t y_dtype,
                             int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
@@ -819,15 +821,17 @@ void awsrc_set_search_pruning(int32_t enabled);
  * then records bit 2 of the workspace's fault word, waits (with the same
  * limit) for its own copies and tensor-core work still in flight, frees its
  * tensor memory and exits, so the GPU context stays usable.
- *   wait_ns      the limit of every such wait in later awsrc_encode_tiles and
- *                awsrc_paged_attention calls (0: the default 2 s).
+ *   wait_ns      the limit of every such wait in later awsrc_encode_tiles,
+ *                awsrc_paged_attention and awsrc_fp8_gemm / _linear calls (0: the
+ *                default 2 s).
  *   stall_chunk  >= 0: the C = 64, P = 4, AWSRC-U search issues no copies of
  *                its seed chunks from this one (counted within each block's
  *                range of 32-seed chunks) on, so its waits for that chunk run
  *                out; awsrc_paged_attention stops its copies the same way,
  *                counted per ring of blocks of 128 tokens (the tensor-memory
- *                kernel: one ring) or of 64 (the other: one or four); -1:
- *                normal operation.
+ *                kernel: one ring) or of 64 (the other: one or four); the 8-bit
+ *                products from this block of 128 columns on (for few rows of x
+ *                from the pair of blocks it lies in); -1: normal operation.
  * The call's results are then undefined and awsrc_workspace_status reports
  * bit 2. awsrc_set_wait_test(0, -1) restores normal operation; an attention
  * workspace has to go through awsrc_attention_workspace_init again.

@@ -271,6 +271,8 @@ class Fp8Matrix:
     def values(self) -> torch.Tensor:
         """The matrix that the codes and scales stand for, float32 [rows, cols]."""
         blocks, rows8, _ = self.codes.shape
+        if self.rows == 0:
+            return torch.empty(0, self.cols, device=self.device)
         r = torch.arange(8, device=self.device)
         c = self.codes.view(torch.uint8).view(blocks, rows8 // 8, 8, 8, 16)
         c = c[:, :, r[:, None], r[:, None] ^ r].view(blocks, rows8, 128)  # a row's pieces back in their order

@@ -42,6 +42,8 @@ awsrc_status gemm_args(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, voi
       (s = check_rows(y, y_dtype)) != AWSRC_OK)
     return s;
   if (x->cols != w->cols) return AWSRC_ERR_SHAPE;
+  // rows of y that share elements would be written by several thread blocks
+  if (x->rows > 1 && y_stride < w->rows && y_stride > -(int64_t)w->rows) return AWSRC_ERR_INVALID_ARG;
   if ((s = check_workspace(workspace, workspace_bytes)) != AWSRC_OK) return s;
   // tiles are numbered in 32 bits
   if ((int64_t)a.w.tiles() * ((a.x.rows + 15) / 16) > INT_MAX / 2) return AWSRC_ERR_UNSUPPORTED;

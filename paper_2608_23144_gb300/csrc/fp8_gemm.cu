@@ -98,7 +98,7 @@ struct Walk {
     tile = blockIdx.x / split;
     lo = 2 * (twos * rank / split);
     hi = min(blocks, 2 * (twos * (rank + 1) / split));
-    chunk = a.y_f32 ? kChunk : (int)blocks;
+    chunk = a.y_f32 ? kChunkF32 : kChunkBf16;
     k0 = lo;
     k1 = min(k0 + chunk, hi);
   }
@@ -461,7 +461,7 @@ cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int tiles = (a.w.rows + a.n - 1) / a.n;
   const int grid = a.split > 1 ? tiles * a.split : tiles < kSms ? tiles : kSms;
-  static_assert(kChunk % 2 == 0, "chunks are whole stages");
+  static_assert(kChunkF32 % 2 == 0 && kChunkBf16 % 2 == 0, "chunks are whole stages");
   return launch_step(fp8_few_kernel<N, X>, dim3((unsigned)grid), kThreads, kSmem, a.split, st, a);
 }
 

@@ -89,6 +89,12 @@ SIZES = [(1, 1, 1), (1, 128, 128), (1, 2048, 300), (2, 130, 129), (7, 77, 5), (1
          (256, 512, 384), (257, 129, 1000), (333, 5000, 177), (513, 900, 2100), (1024, 640, 1024), (2500, 520, 600)]
 
 
+# many tiles for each thread block, one block of columns in a tile, long sums, shares of columns in every number, 16 rows whose
+# codes do not fit beside the stages
+SIZES += [(3, 256, 40000), (33, 384, 25000), (5, 100, 40000), (300, 100, 40000), (130, 4224, 12000), (16, 30000, 300), (9, 70000, 64),
+          (16, 8320, 2000), (1, 640, 5000), (64, 11008, 2048), (48, 6400, 700), (100, 1280, 9000), (1, 40000, 8)]
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("m,k,n", SIZES)
 def test_products_of_whole_numbers_are_exact(aw, dtype, m, k, n):
@@ -97,8 +103,8 @@ def test_products_of_whole_numbers_are_exact(aw, dtype, m, k, n):
     gen = torch.Generator().manual_seed(m * 31 + k + n)
     x, xs = int_matrix(m, k, gen)
     w, wss = int_matrix(n, k, gen)
-    want = (x.double() @ w.double().T) * xs.double() * wss.double().T
-    assert float((x.double().abs() @ w.double().abs().T).max()) < 2 ** 24
+    want = ((x.double().cuda() @ w.double().cuda().T) * xs.double().cuda() * wss.double().cuda().T).cpu()
+    assert k * 9 < 2 ** 24
     ws = aw.awsrc_step_workspace()
     xq, wq = aw.awsrc_fp8_quantize((x * xs).cuda()), aw.awsrc_fp8_quantize((w * wss).cuda())
     out = torch.full((m, n + 5), -7.0, dtype=dtype, device="cuda")
@@ -175,6 +181,68 @@ def test_rows_behind_the_last_may_hold_anything(aw):
     assert torch.equal(aw.awsrc_fp8_gemm(ms[0], ms[1], ws), want)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m,k,n,pad", [(1, 2048, 300, 0), (7, 1000, 5000, 3), (16, 515, 129, 1), (13, 3000, 700, 8), (31, 700, 300, 2),
+                                       (64, 2048, 512, 5), (90, 640, 300, 4), (16, 30000, 200, 0)])
+def test_linear_is_quantize_and_gemm(aw, dtype, m, k, n, pad):
+    """Bit for bit, and x8 holds what awsrc_fp8_quantize gives, whether or not the product quantises the rows itself; a block that
+    is not finite among them."""
+    gen = torch.Generator().manual_seed(m * k)
+    x = spread(m, k + pad, gen).to(dtype)
+    x[m // 2, k // 2] = math.nan
+    x = x.cuda()[:, :k]
+    w = aw.awsrc_fp8_quantize(torch.randn(n, k, generator=gen).cuda())
+    ws, x8, want8 = aw.awsrc_step_workspace(), aw.awsrc_fp8_matrix(m, k), aw.awsrc_fp8_quantize(x)
+    y = aw.awsrc_fp8_linear(x, w, x8, ws)
+    want = aw.awsrc_fp8_gemm(want8, w, ws, out_dtype=dtype)
+    assert torch.equal(x8.codes.view(torch.uint8), want8.codes.view(torch.uint8)) and torch.equal(x8.exps, want8.exps)
+    assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
+    assert y[m // 2].isnan().all() and (m == 1 or y[(m // 2 + 1) % m].isfinite().all())
+    again = aw.awsrc_fp8_linear(x, w, x8, ws)
+    assert torch.equal(again.nan_to_num(), y.nan_to_num())
+    stale = torch.full_like(y, 3.0).t().contiguous().t() if m > 1 and n > 1 else None
+    if stale is not None:  # columns apart: refused
+        with pytest.raises(ValueError):
+            aw.awsrc_fp8_linear(x, w, x8, ws, out=stale)
+
+
+def test_products_on_two_streams_at_once(aw):
+    """Each with its own workspace and codes; both kernels need tensor memory."""
+    gen = torch.Generator().manual_seed(2)
+    w = aw.awsrc_fp8_quantize(torch.randn(3000, 2000, generator=gen).cuda())
+    xs = [torch.randn(m, 2000, generator=gen).cuda() for m in (5, 300)]
+    want = [aw.awsrc_fp8_gemm(aw.awsrc_fp8_quantize(x), w, aw.awsrc_step_workspace()) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    sets = [(aw.awsrc_fp8_matrix(x.shape[0], 2000), aw.awsrc_step_workspace(), torch.empty_like(y)) for x, y in zip(xs, want)]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for x, (x8, ws, y), s in zip(xs, sets, streams):
+            aw.awsrc_fp8_linear(x, w, x8, ws, out=y, stream=s)
+    torch.cuda.synchronize()
+    for (x8, ws, y), v in zip(sets, want):
+        assert torch.equal(y, v) and aw.awsrc_workspace_status(ws) == 0
+
+
+def test_weights_made_just_before_the_product(aw):
+    """The product's early copies of w come after the kernel that wrote it: new weights before every call, no waiting between."""
+    gen = torch.Generator().manual_seed(6)
+    ws = aw.awsrc_step_workspace()
+    for m in (3, 40, 200):
+        x = torch.randn(m, 1500, generator=gen).cuda()
+        raw = [torch.randn(2500, 1500, generator=gen).cuda() for _ in range(4)]
+        want = [aw.awsrc_fp8_gemm(aw.awsrc_fp8_quantize(x), aw.awsrc_fp8_quantize(r), ws) for r in raw]
+        torch.cuda.synchronize()
+        w, x8 = aw.awsrc_fp8_matrix(2500, 1500), aw.awsrc_fp8_matrix(m, 1500)
+        ys = []
+        for r in raw * 5:
+            aw.awsrc_fp8_quantize(r, out=w)
+            ys.append(aw.awsrc_fp8_linear(x, w, x8, ws))
+        torch.cuda.synchronize()
+        for i, y in enumerate(ys):
+            assert torch.equal(y, want[i % 4]), (m, i)
+
+
 def test_empty_products(aw):
     ws = aw.awsrc_step_workspace()
     w = aw.awsrc_fp8_quantize(torch.randn(10, 64).cuda())
@@ -182,6 +250,7 @@ def test_empty_products(aw):
     assert aw.awsrc_fp8_gemm(none, w, ws).shape == (0, 10)
     assert aw.awsrc_fp8_gemm(w, none, ws).shape == (10, 0)
     assert aw.awsrc_fp8_linear(torch.empty(0, 64, device="cuda"), w, none, ws).shape == (0, 10)
+    assert none.values().shape == (0, 64)
 
 
 def test_waits_that_run_out_are_reported(aw):

@@ -98,7 +98,8 @@ def test_products_without_rows_pass():
     (dict(x=mat(codes=P + 64)), INVALID), (dict(w=mat(exps=P + 8)), INVALID), (dict(w=mat(cols=128)), SHAPE),
     (dict(y=None), INVALID), (dict(y=P + 2), INVALID), (dict(dtype=2), INVALID), (dict(ws=None), WORKSPACE),
     (dict(ws_bytes=255), WORKSPACE), (dict(ws=P + 128), INVALID),
-    (dict(x=mat(rows=1 << 30), w=mat(rows=1 << 30)), UNSUPPORTED),
+    (dict(x=mat(rows=1 << 30), w=mat(rows=1 << 30), stride=1 << 30), UNSUPPORTED),
+    (dict(x=mat(rows=2), stride=9), INVALID), (dict(x=mat(rows=2), stride=0), INVALID), (dict(x=mat(rows=2), stride=-9), INVALID),
 ])
 def test_products_refuse(call, kw, status):
     assert call(**kw) == status
