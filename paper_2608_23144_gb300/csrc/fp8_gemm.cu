@@ -341,6 +341,14 @@ __device__ void write_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x, uint
       float* part = reinterpret_cast<float*>(sm.tile[0]);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) part[(c0 + i) * BM + r] = acc[i];
+    } else if (a.vec_y) {
+      const int row = w.tile * a.n + (r & ~3);  // a.n is a multiple of 8
+#pragma unroll
+      for (int i = 0; i < kPer; i += 4) {
+        if (c0 + i >= a.x.rows) break;
+        const float4 v = quad(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+        if (c0 + i + (lane & 3) < a.x.rows && r < a.n) put4(a, c0 + i + (lane & 3), row, v);
+      }
     } else if (const int row = w.tile * a.n + r; r < a.n && row < a.w.rows) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i)

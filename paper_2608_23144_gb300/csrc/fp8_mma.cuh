@@ -125,8 +125,22 @@ __device__ __forceinline__ void put(const GemmArgs& a, int tok, int row, float v
   else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
 }
 
+// Four columns of a lane's row become four rows of a column: of lanes 4 a .. 4 a + 3, lane
+// 4 a + b gets column b. A store instruction takes 9 cycles however little of it there is
+// (results of one column a warp, 64 or 128 bytes, took 150 us where 50 or 96 write as much).
+__device__ __forceinline__ float4 quad(float r0, float r1, float r2, float r3) {
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+  const float s = __shfl_xor_sync(0xffffffffu, odd ? r0 : r1, 1), t = __shfl_xor_sync(0xffffffffu, odd ? r2 : r3, 1);
+  r0 = odd ? s : r0;
+  r1 = odd ? r1 : s;
+  r2 = odd ? t : r2;
+  r3 = odd ? r3 : t;
+  const float u = __shfl_xor_sync(0xffffffffu, high ? r0 : r2, 2), v = __shfl_xor_sync(0xffffffffu, high ? r1 : r3, 2);
+  return high ? make_float4(u, v, r2, r3) : make_float4(r0, r1, u, v);
+}
+
 // Four floats at `addr` in the shared memory of each of `split` thread blocks, rank0
-// being the first and `every` the step between them.
+// being the first and `every` the step between them. (25 GB/s from a partner.)
 template <int kSplit>
 __device__ __forceinline__ void get_parts(float4* v, uint32_t addr, int rank0, int every, int split) {
 #pragma unroll

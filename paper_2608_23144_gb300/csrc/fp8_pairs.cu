@@ -333,6 +333,14 @@ __device__ void write_role(const GemmArgs& a, Smem& sm, const Ctx& x, uint32_t t
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
         if (i < per) part[(c0 + i) * BM + r] = acc[i];
+    } else if (a.vec_y) {
+      const int have = min(per, a.x.rows - w.tok - (int)c0) - (lane & 3), tok = w.tok + c0 + (lane & 3);
+#pragma unroll
+      for (int i = 0; i < kPer; i += 4)
+        if (i < per) {
+          const float4 v = quad(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+          if (i < have) put4(a, tok + i, row & ~3, v);
+        }
     } else if (row < a.w.rows) {
       const int have = min(per, a.x.rows - w.tok - (int)c0);
 #pragma unroll
