@@ -14,6 +14,11 @@ binding with the same entry-point names:
   sidecar applied inside a packed INT4 product, W_hat never formed
 * ``awsrc_kv_append`` / ``awsrc_paged_attention``  keys and values into a paged 8-bit
   cache (q and k rotated on the way) and attention over it, between those products
+* ``awsrc_kv_plan`` / ``awsrc_verify_drafts``  a step's tables from the requests'
+  lengths, and drafted tokens against the target's probabilities, on the device
+* ``awsrc_fp8_quantize`` / ``awsrc_fp8_gemm`` / ``awsrc_fp8_linear``  products of
+  matrices held in e4m3 with a power-of-two scale per 128 columns, for more rows than
+  the packed products take
 """
 from ._binding import (  # noqa: F401
     CANDIDATE_DTYPE,
