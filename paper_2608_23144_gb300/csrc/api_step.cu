@@ -34,6 +34,23 @@ awsrc_status check_rows(const void* x, int32_t dtype) {
   return is_dtype(dtype) && x && aligned(x, size_of(dtype)) ? AWSRC_OK : AWSRC_ERR_INVALID_ARG;
 }
 
+// Whether `rows` rows here and there share any byte. Rows at the same step may lie
+// between each other's (columns of one wider matrix); at different steps their extents must not meet.
+struct Rows {
+  const void* p;
+  int64_t step, row;  // bytes
+};
+bool share(const Rows& x, const Rows& y, int64_t rows) {
+  const auto lo = [&](const Rows& m) { return (__int128)reinterpret_cast<uintptr_t>(m.p) + (m.step < 0 ? (rows - 1) * (__int128)m.step : 0); };
+  const auto hi = [&](const Rows& m) { return (__int128)reinterpret_cast<uintptr_t>(m.p) + (m.step > 0 ? (rows - 1) * (__int128)m.step : 0) + m.row; };
+  if (hi(x) <= lo(y) || hi(y) <= lo(x)) return false;
+  if (rows == 1 || x.step != y.step || x.step == 0) return true;
+  const __int128 step = x.step < 0 ? -(__int128)x.step : (__int128)x.step;
+  __int128 d = ((__int128)reinterpret_cast<uintptr_t>(y.p) - (__int128)reinterpret_cast<uintptr_t>(x.p)) % step;
+  if (d < 0) d += step;
+  return d < x.row || step - d < y.row;
+}
+
 awsrc_status gemm_args(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, void* y, int32_t y_dtype, int64_t y_stride,
                        void* workspace, size_t workspace_bytes, GemmArgs* out) {
   GemmArgs a{};
@@ -161,6 +178,9 @@ awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, 
   if (s != AWSRC_OK || (s = check_rows(x, x_dtype)) != AWSRC_OK) return s;
   if (x8->codes == w->codes || x8->exps == w->exps) return AWSRC_ERR_INVALID_ARG;
   if (a.x.rows == 0 || a.w.rows == 0) return AWSRC_OK;
+  // few rows of x are read while others' results are written
+  const int64_t xs = size_of(x_dtype), ys = size_of(y_dtype);
+  if (share(Rows{x, x_stride * xs, a.x.cols * xs}, Rows{y, y_stride * ys, a.w.rows * ys}, a.x.rows)) return AWSRC_ERR_INVALID_ARG;
   cudaError_t e = cudaSuccess;
   if (fp8_gemm_quantizes(a)) {
     a.raw = x;

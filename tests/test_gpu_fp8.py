@@ -294,3 +294,21 @@ def test_linear_in_a_graph_on_another_stream(aw):
         torch.cuda.synchronize()
         want = aw.awsrc_fp8_gemm(aw.awsrc_fp8_quantize(new.cuda()), w, ws)
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("m", [1, 7, 40, 100])
+def test_linear_between_columns_of_one_matrix(aw, m):
+    """x and y as columns of one buffer are a right call; y over x is none, whatever the rows."""
+    gen = torch.Generator().manual_seed(m)
+    k, n = 512, 256
+    buf = torch.randn(m, k + n, generator=gen).cuda()
+    w = aw.awsrc_fp8_quantize(torch.randn(n, k, generator=gen).cuda())
+    x8, ws = aw.awsrc_fp8_matrix(m, k), aw.awsrc_step_workspace()
+    x = buf[:, :k].clone()
+    want = aw.awsrc_fp8_linear(x, w, x8, ws)
+    aw.awsrc_fp8_linear(buf[:, :k], w, x8, ws, out=buf[:, k:])
+    assert torch.equal(buf[:, k:], want) and torch.equal(buf[:, :k], x)
+    for out in (buf[:, :n], buf[:, k - 1:k - 1 + n]):
+        with pytest.raises(aw.AwsrcError):
+            aw.awsrc_fp8_linear(buf[:, :k], w, x8, ws, out=out)
+    assert torch.equal(buf[:, k:], want) and torch.equal(buf[:, :k], x)

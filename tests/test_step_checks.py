@@ -120,6 +120,25 @@ def test_linear_refuses_to_write_over_the_weights():
     assert linear(w=mat(rows=10)) == INVALID and linear(w=mat(rows=10, codes=2 * P)) == INVALID
 
 
+def linear_over(src, y, stride_x, stride_y, rows=4, src_dtype=0, dtype=0):
+    """x of 256 columns at src, y of 10 at y; strides in elements. The weights are far away."""
+    return aw.lib.awsrc_fp8_linear(src, src_dtype, stride_x, ct.byref(mat(rows=rows, codes=P << 4, exps=P << 5)),
+                                   ct.byref(mat(rows=10, codes=P << 6, exps=P << 7)), y, dtype, stride_y, P << 8, 1 << 30, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(src=P, y=P, stride_x=256, stride_y=256), dict(src=P, y=P, stride_x=256, stride_y=10, rows=1),
+    dict(src=P, y=P + 4 * 255, stride_x=300, stride_y=300), dict(src=P + 36, y=P, stride_x=300, stride_y=300),
+    dict(src=P, y=P + 4 * (300 * 2 + 255), stride_x=300, stride_y=300),   # two rows further down
+    dict(src=P + 4 * 295, y=P, stride_x=300, stride_y=300),               # y's rows against the ends of x's
+    dict(src=P, y=P + 2 * 200, stride_x=300, stride_y=150, src_dtype=1),  # bf16 and float32, the same bytes a row
+    dict(src=P, y=P + 4 * 300, stride_x=300, stride_y=12),                # steps that differ
+    dict(src=P, y=P + 4 * 100, stride_x=0, stride_y=300),                 # one row for all of x
+])
+def test_linear_refuses_to_write_over_x(kw):
+    assert linear_over(**kw) == INVALID
+
+
 def test_matrix_bytes_are_host_only():
     def need(rows, cols):
         c, e = ct.c_size_t(), ct.c_size_t()
