@@ -177,7 +177,8 @@ awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, 
   awsrc_status s = gemm_args(x8, w, y, y_dtype, y_stride, workspace, workspace_bytes, &a);
   if (s != AWSRC_OK || (s = check_rows(x, x_dtype)) != AWSRC_OK) return s;
   if (x8->codes == w->codes || x8->exps == w->exps) return AWSRC_ERR_INVALID_ARG;
-  if (a.x.rows == 0 || a.w.rows == 0) return AWSRC_OK;
+  if (a.x.rows == 0) return AWSRC_OK;
+  if (a.w.rows == 0) return awsrc_fp8_quantize(x, x_dtype, x_stride, x8, stream);  // x8 is written all the same
   // few rows of x are read while others' results are written
   const int64_t xs = size_of(x_dtype), ys = size_of(y_dtype);
   if (share(Rows{x, x_stride * xs, a.x.cols * xs}, Rows{y, y_stride * ys, a.w.rows * ys}, a.x.rows)) return AWSRC_ERR_INVALID_ARG;

@@ -312,3 +312,11 @@ def test_linear_between_columns_of_one_matrix(aw, m):
         with pytest.raises(aw.AwsrcError):
             aw.awsrc_fp8_linear(buf[:, :k], w, x8, ws, out=out)
     assert torch.equal(buf[:, k:], want) and torch.equal(buf[:, :k], x)
+
+
+@pytest.mark.parametrize("m", [1, 40, 100])
+def test_linear_leaves_codes_where_w_has_no_rows(aw, m):
+    x = torch.randn(m, 300, generator=torch.Generator().manual_seed(m)).cuda()
+    x8, want = aw.awsrc_fp8_matrix(m, 300), aw.awsrc_fp8_quantize(x)
+    y = aw.awsrc_fp8_linear(x, aw.awsrc_fp8_matrix(0, 300), x8, aw.awsrc_step_workspace())
+    assert y.shape == (m, 0) and torch.equal(x8.values(), want.values()) and bool(x8.values().any())
