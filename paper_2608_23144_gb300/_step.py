@@ -46,6 +46,7 @@ _declare()
 
 _Tensor = torch.Tensor
 _I32, _I64, _F32, _U8 = torch.int32, torch.int64, torch.float32, torch.uint8
+_INT = (1 << 31) - 1  # what the library's lengths hold: ctypes would cut them off
 
 
 # The checks are a small call's largest part: each looks at a tensor once and only
@@ -103,6 +104,8 @@ class KvPool:
             raise ValueError(f"free_pages has shape {tuple(free_pages.shape)}, expected (pages of the cache,)")
         if page not in PAGE_SIZES:
             raise ValueError(f"page {page} must be one of {PAGE_SIZES}")
+        if max(n, page_table.shape[1], free_pages.shape[0]) > _INT:
+            raise ValueError("a pool has 2^31 - 1 entries of a kind at most")
         ptr = [_ints(page_table, "page_table", page_table.shape, self.device), _ints(kv_len, "kv_len", (n,), self.device),
                _ints(free_pages, "free_pages", free_pages.shape, self.device),
                _ints(free_count, "free_count", (1,), self.device)]
@@ -150,8 +153,8 @@ def awsrc_kv_plan(pool: KvPool, keep: Optional[torch.Tensor], add: torch.Tensor,
                 break
         else:
             raise ValueError("n_tok is needed without tok_seq, tok_pos and tok_slot")
-    if n_tok < 0:
-        raise ValueError("n_tok must not be negative")
+    if not 0 <= n_tok <= _INT:
+        raise ValueError(f"n_tok must not be {'negative' if n_tok < 0 else 'above 2^31 - 1'}")
     seqs, toks = (n,), (n_tok,)
     kp = None if keep is None else _ints(keep, "keep", seqs, dev)
     ap = _ints(add, "add", seqs, dev)
@@ -212,6 +215,8 @@ def awsrc_verify_drafts(row_start: torch.Tensor, ids: torch.Tensor, target: torc
         raise ValueError("target must be a 2-D tensor (rows x vocab)")
     shape = target.shape
     rows, vocab = shape
+    if rows > _INT or vocab > _INT:
+        raise ValueError(f"target of {rows} rows and a vocab of {vocab}: 2^31 - 1 at most")
     tp = _probs(target, "target", shape, dev)
     dp = None if draft is None else _probs(draft, "draft", shape, dev)
     seqs, all_rows = (n,), (rows,)
@@ -223,8 +228,8 @@ def awsrc_verify_drafts(row_start: torch.Tensor, ids: torch.Tensor, target: torc
             _require(tokens, "tokens")
             raise ValueError(f"tokens has shape {tuple(tokens.shape)}, expected ({n}, max_draft + 1)")
         max_draft = tokens.shape[1] - 1 if max_draft is None else max_draft
-    if max_draft is None or max_draft < 0:
-        raise ValueError("max_draft (the most drafts of a sequence, not negative) is needed without tokens")
+    if max_draft is None or not 0 <= max_draft <= _INT:
+        raise ValueError("max_draft (the most drafts of a sequence, from 0 to 2^31 - 1) is needed without tokens")
     if keep is not None and kv_len is None:
         raise ValueError("keep needs kv_len")
     _workspace(workspace, dev)

@@ -216,6 +216,24 @@ def test_verification_arguments_are_checked(kw, exc, msg):
         aw.awsrc_verify_drafts(**a)
 
 
+def test_lengths_past_31_bits_are_refused():
+    """The library takes 32-bit lengths: none may arrive there cut off."""
+    big = 1 << 32
+    with pytest.raises(ValueError, match="n_tok"):
+        aw.awsrc_kv_plan(cpu_pool(), None, ints(2), WS, n_tok=big + 5)
+    a = dict(row_start=ints(3), draft=None, u=torch.zeros(5), r=torch.zeros(2), workspace=WS)
+    with pytest.raises(ValueError, match="rows"):
+        aw.awsrc_verify_drafts(ids=ints(5), target=torch.zeros(1, 9).expand(big + 5, 9), max_draft=2, **a)
+    with pytest.raises(ValueError, match="max_draft"):
+        aw.awsrc_verify_drafts(ids=ints(5), target=torch.zeros(5, 9), max_draft=big + 2, **a)
+    meta = dict(dtype=torch.int32, device="meta")
+    with pytest.raises(ValueError, match="vocab"):
+        aw.awsrc_verify_drafts(torch.empty(3, **meta), torch.empty(5, **meta), torch.empty(5, big + 9, device="meta"), None,
+                               a["u"], a["r"], WS, max_draft=2)
+    with pytest.raises(ValueError, match="entries"):
+        aw.awsrc_kv_pool(torch.empty(2, 4, **meta), torch.empty(2, **meta), torch.empty(big + 8, **meta), torch.empty(1, **meta), 64)
+
+
 @pytest.mark.parametrize("make,exc,msg", [
     (lambda: aw.awsrc_fp8_matrix(3, 0, "cpu"), ValueError, "cannot be held"),
     (lambda: aw.awsrc_fp8_matrix(-1, 5, "cpu"), ValueError, "cannot be held"),
