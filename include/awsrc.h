@@ -667,7 +667,8 @@ typedef struct awsrc_kv_pool {
  * without new tokens, and are reported (bit 3); so is a stack that cannot be
  * right (free_count outside [0, n_pages], or more pages given back than it has
  * room for): nothing changes then, q_start is 0 and the maps are -1.
- * The arrays must not overlap. Errors: INVALID_ARG, SHAPE, UNSUPPORTED (n_seq >
+ * The arrays must not overlap (keep that is kv_len is refused: kv_len says which
+ * pages a sequence holds). Errors: INVALID_ARG, SHAPE, UNSUPPORTED (n_seq >
  * 8192, table_stride * page, n_pages or n_tok > 2^30), WORKSPACE, CUDA.
  */
 awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const int32_t* add, int32_t n_tok,
@@ -700,7 +701,8 @@ typedef struct awsrc_probs {
  *   accepted   n_seq: accepted drafts;  tokens  n_seq x (max_draft + 1): those,
  *              the token, -1 behind.
  *   kv_len, keep  n_seq each, or both NULL: keep = kv_len less the drafts not
- *              accepted (what awsrc_kv_plan takes; keep may be kv_len).
+ *              accepted (what awsrc_kv_plan takes; keep may be kv_len, but not a
+ *              pool's, where awsrc_kv_plan has to find what the sequences hold).
  * A draft outside the vocabulary is not accepted and is reported (bit 3), as are
  * rows that cannot be right (row_start outside [0, n_rows] or falling, more than
  * max_draft drafts): their sequence, like one without rows, gets accepted 0,

@@ -135,7 +135,7 @@ def awsrc_kv_plan(pool: KvPool, keep: Optional[torch.Tensor], add: torch.Tensor,
                   tok_seq: Optional[torch.Tensor] = None, tok_pos: Optional[torch.Tensor] = None,
                   tok_slot: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The next step's tables, on the device: every sequence keeps its first
-    keep[b] tokens (None: all) and gets add[b] new ones if pages and the n_tok
+    keep[b] tokens (None: all; not pool.kv_len itself) and gets add[b] new ones if pages and the n_tok
     rows of the step have room for them; the pool's kv_len, page_table and stack
     are brought up to date. Returns q_start (int32 [n_seq + 1]); with it, kv_len
     and page_table are awsrc_kv_batch's arguments. tok_seq, tok_pos (int32) and
@@ -205,7 +205,8 @@ def awsrc_verify_drafts(row_start: torch.Tensor, ids: torch.Tensor, target: torc
     in [0, 1). Returns (accepted [n_seq], tokens [n_seq, max_draft + 1]: the
     accepted drafts, the token, -1 behind), int32. With kv_len (int32 [n_seq]),
     `keep` receives it less the drafts not accepted, as awsrc_kv_plan takes it;
-    keep may be kv_len. max_draft defaults to that of `tokens`."""
+    keep may be kv_len, but not a pool's: awsrc_kv_plan has to find there what the
+    sequences hold. max_draft defaults to that of `tokens`."""
     if not isinstance(row_start, _Tensor) or row_start.dim() != 1 or row_start.shape[0] < 1:
         _require(row_start, "row_start", dtype=_I32)
         raise ValueError(f"row_start has shape {tuple(row_start.shape)}, expected (n_seq + 1,)")

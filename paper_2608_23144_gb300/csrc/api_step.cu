@@ -111,6 +111,7 @@ awsrc_status awsrc_kv_plan(const awsrc_kv_pool* pool, const int32_t* keep, const
   if (!aligned(tok_slot, 8)) return AWSRC_ERR_INVALID_ARG;
   const awsrc_status s = check_workspace(workspace, workspace_bytes);
   if (s != AWSRC_OK) return s;
+  if (keep == pool->kv_len) return AWSRC_ERR_INVALID_ARG;  // what was held would be lost: its pages never came back
   PlanArgs a{pool->n_pages, pool->page, 4, pool->n_seq, pool->table_stride, n_tok, pool->page_table, pool->kv_len,
              pool->free_pages, pool->free_count, keep, add, q_start, tok_seq, tok_pos, tok_slot,
              static_cast<uint32_t*>(workspace), static_cast<uint32_t*>(workspace) + kArrivedAt, 0};

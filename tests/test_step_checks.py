@@ -38,6 +38,11 @@ def test_plan_refuses(kw, status):
     assert plan(**kw) == status
 
 
+def test_plan_refuses_the_lengths_themselves_as_keep():
+    """With keep in kv_len's place nothing says what a sequence held before."""
+    assert plan(p=pool(kv_len=2 * P), keep=2 * P) == INVALID
+
+
 def probs(**over):
     c = dict(p=P, stride=100, dtype=0, pad_=0)
     c.update(over)
