@@ -194,6 +194,20 @@ def test_verify_follows_the_definition(aw, dtype, vocab, kind):
         assert any(a < d for a, d in zip(want[0], drafts))  # some were not accepted
 
 
+@pytest.mark.parametrize("n_seq", [76, 77, 152, 153, 304, 305, 700])
+def test_verify_many_sequences(aw, n_seq):
+    """Eight thread blocks a sequence down to one, as the number of sequences grows."""
+    rng, gen = random.Random(n_seq), torch.Generator().manual_seed(n_seq)
+    vocab = 700
+    lens = [rng.randrange(0, 3) for _ in range(n_seq)]  # no rows, none drafted, one drafted
+    starts = [sum(lens[:b]) for b in range(n_seq + 1)]
+    n = starts[-1]
+    p, q = rows_of(rng, gen, n, vocab, "wide", torch.float32)
+    ids = [rng.randrange(vocab) for _ in range(n)]
+    check(aw, starts, ids, p, q, torch.rand(n, generator=gen), torch.rand(n_seq, generator=gen), 1,
+          [rng.randrange(20, 900) for _ in lens])
+
+
 def test_verify_many_drafts_and_a_large_vocabulary(aw):
     gen = torch.Generator().manual_seed(8)
     vocab, drafts = 60001, 70
