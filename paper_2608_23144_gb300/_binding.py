@@ -164,6 +164,23 @@ def _stream(stream=None) -> int:
     return s.cuda_stream
 
 
+def _made_for(stream, make, *shape, **kw) -> torch.Tensor:
+    """make(*shape, **kw) for a call on `stream` (None: the current one). Nothing orders another
+    stream's kernels with a fill queued on the current one, or with the work that last
+    used the memory there: the tensor is made on `stream`, and its memory is not handed
+    out again before the current stream, where the caller goes on, is done with it too."""
+    if stream is None:
+        return make(*shape, **kw)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=kw["device"])
+    with torch.cuda.stream(stream):
+        t = make(*shape, **kw)
+    now = torch.cuda.current_stream(t.device)
+    if t.is_cuda and now != stream:
+        t.record_stream(now)
+    return t
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return DTYPE_F32

@@ -8,7 +8,7 @@ from typing import Optional
 
 import torch
 
-from ._binding import _check, _require, lib
+from ._binding import _check, _made_for, _require, lib
 from ._paged import _DTYPES, _EMPTY, PAGE_SIZES, KvCache, _on, _stream
 
 
@@ -76,7 +76,7 @@ def awsrc_step_workspace(device="cuda", stream=None) -> torch.Tensor:
     awsrc_fp8_linear, ready for use; one stream at a time."""
     n = ct.c_size_t()
     _check(lib.awsrc_step_workspace_bytes(ct.byref(n)), "step_workspace_bytes")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    ws = _made_for(stream, torch.empty, n.value, dtype=torch.uint8, device=device)
     _check(_on(ws.device, lib.awsrc_step_workspace_init, ws.data_ptr(), n.value, _stream(stream, ws.device)),
            "step_workspace_init")
     return ws
@@ -165,7 +165,7 @@ def awsrc_kv_plan(pool: KvPool, keep: Optional[torch.Tensor], add: torch.Tensor,
     if dev.type != "cuda":
         _cuda(dev, "the pool")
     if q_start is None:
-        q_start = torch.empty(n + 1, dtype=_I32, device=dev)
+        q_start = _made_for(stream, torch.empty, n + 1, dtype=_I32, device=dev)
     qp = _ints(q_start, "q_start", (n + 1,), dev)
     st = _on(dev, lib.awsrc_kv_plan, pool._ref, kp, ap, n_tok, qp, tp, pp, sp, workspace.data_ptr(), workspace.numel(),
              _stream(stream, dev))
@@ -237,9 +237,9 @@ def awsrc_verify_drafts(row_start: torch.Tensor, ids: torch.Tensor, target: torc
     if dev.type != "cuda":
         _cuda(dev, "row_start")
     if accepted is None:
-        accepted = torch.empty(n, dtype=_I32, device=dev)
+        accepted = _made_for(stream, torch.empty, n, dtype=_I32, device=dev)
     if tokens is None:
-        tokens = torch.empty(n, max_draft + 1, dtype=_I32, device=dev)
+        tokens = _made_for(stream, torch.empty, n, max_draft + 1, dtype=_I32, device=dev)
     cp, op = _ints(accepted, "accepted", seqs, dev), _ints(tokens, "tokens", (n, max_draft + 1), dev)
     lp = kp = None
     if keep is not None:
@@ -288,11 +288,12 @@ class Fp8Matrix:
         return (c * scale[..., None]).flatten(1)[:, :self.cols]
 
 
-def awsrc_fp8_matrix(rows: int, cols: int, device="cuda") -> Fp8Matrix:
-    """A new matrix of zeros held in 8 bits."""
+def awsrc_fp8_matrix(rows: int, cols: int, device="cuda", stream=None) -> Fp8Matrix:
+    """A new matrix of zeros held in 8 bits, filled on `stream` (None: the current one)."""
     blocks = -(-cols // 128)
-    codes = torch.zeros(max(0, blocks), max(0, -(-rows // 8) * 8), 128, dtype=torch.uint8, device=device)
-    exps = torch.zeros(max(0, -(-blocks // 4)), max(0, -(-rows // 128)), 32, 4, 4, dtype=torch.uint8, device=device)
+    codes = _made_for(stream, torch.zeros, max(0, blocks), max(0, -(-rows // 8) * 8), 128, dtype=torch.uint8, device=device)
+    exps = _made_for(stream, torch.zeros, max(0, -(-blocks // 4)), max(0, -(-rows // 128)), 32, 4, 4, dtype=torch.uint8,
+                     device=device)
     return Fp8Matrix(rows, cols, codes.view(torch.float8_e4m3fn), exps)
 
 
@@ -328,7 +329,7 @@ def awsrc_fp8_quantize(x: torch.Tensor, out: Optional[Fp8Matrix] = None, stream=
     if dev.type != "cuda":
         _cuda(dev, "x")
     if out is None:
-        out = awsrc_fp8_matrix(x.shape[0], x.shape[1], dev)
+        out = awsrc_fp8_matrix(x.shape[0], x.shape[1], dev, stream)
     _fp8(out, "out", dev)
     if (out.rows, out.cols) != tuple(x.shape):
         raise ValueError(f"out is {out.rows} x {out.cols}, x {x.shape[0]} x {x.shape[1]}")
@@ -338,11 +339,11 @@ def awsrc_fp8_quantize(x: torch.Tensor, out: Optional[Fp8Matrix] = None, stream=
     return out
 
 
-def _product(x_rows: int, x_cols: int, w: Fp8Matrix, out, out_dtype, dev):
+def _product(x_rows: int, x_cols: int, w: Fp8Matrix, out, out_dtype, dev, stream=None):
     if x_cols != w.cols:
         raise ValueError(f"x has {x_cols} columns, w {w.cols}")
     if out is None:
-        out = torch.empty(x_rows, w.rows, dtype=out_dtype, device=dev)
+        out = _made_for(stream, torch.empty, x_rows, w.rows, dtype=out_dtype, device=dev)
     res = _matrix(out, "out", dev)
     if tuple(out.shape) != (x_rows, w.rows):
         raise ValueError(f"out has shape {tuple(out.shape)}, expected ({x_rows}, {w.rows})")
@@ -358,7 +359,7 @@ def awsrc_fp8_gemm(x: Fp8Matrix, w: Fp8Matrix, workspace: torch.Tensor, out: Opt
     _workspace(workspace, dev)
     if dev.type != "cuda":
         _cuda(dev, "w")
-    out, yp, dt, ys = _product(x.rows, x.cols, w, out, out_dtype, dev)
+    out, yp, dt, ys = _product(x.rows, x.cols, w, out, out_dtype, dev, stream)
     st = _on(dev, lib.awsrc_fp8_gemm, x._ref, w._ref, yp, dt, ys, workspace.data_ptr(), workspace.numel(),
              _stream(stream, dev))
     if st:
@@ -380,7 +381,7 @@ def awsrc_fp8_linear(x: torch.Tensor, w: Fp8Matrix, x8: Fp8Matrix, workspace: to
     _workspace(workspace, dev)
     if dev.type != "cuda":
         _cuda(dev, "x")
-    out, yp, yt, ys = _product(x.shape[0], x.shape[1], w, out, x.dtype, dev)
+    out, yp, yt, ys = _product(x.shape[0], x.shape[1], w, out, x.dtype, dev, stream)
     st = _on(dev, lib.awsrc_fp8_linear, xp, xt, xs, x8._ref, w._ref, yp, yt, ys, workspace.data_ptr(), workspace.numel(),
              _stream(stream, dev))
     if st:

@@ -1,0 +1,40 @@
+"""GPU parity of the serving-step calls in forms beside the usual ones: other streams,
+launch forms of large vocabularies, thresholds of tiny random numbers, long sums."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+@pytest.fixture(scope="module")
+def aw():
+    import paper_2608_23144_gb300 as aw
+    assert torch.cuda.is_available()
+    return aw
+
+
+def cuda_ints(v, dtype=I32):
+    return torch.tensor(v, dtype=dtype).cuda()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_quantize_on_another_stream_than_the_busy_current_one(aw, dtype):
+    """A matrix made by the call itself while the current stream has work queued: what the fill would
+    overwrite if it came behind that work. The product on the same stream reads the codes."""
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(300, 1000, generator=gen).to(dtype).cuda()
+    want = aw.awsrc_fp8_quantize(x)
+    ws = aw.awsrc_step_workspace()
+    product = aw.awsrc_fp8_gemm(want, want, ws)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda._sleep(20_000_000)  # some 10 ms of the current stream
+        m = aw.awsrc_fp8_quantize(x, stream=side)
+        y = aw.awsrc_fp8_gemm(m, m, ws, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(m.codes.view(torch.uint8), want.codes.view(torch.uint8)) and torch.equal(m.exps, want.exps)
+        assert torch.equal(y, product)
+    assert aw.awsrc_workspace_status(ws) == 0
