@@ -164,6 +164,11 @@ def _stream(stream=None) -> int:
     return s.cuda_stream
 
 
+def _as_stream(stream, device):
+    """A stream that torch makes current, from anything with a handle."""
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
+
 def _made_for(stream, make, *shape, **kw) -> torch.Tensor:
     """make(*shape, **kw) for a call on `stream` (None: the current one). Nothing orders another
     stream's kernels with a fill queued on the current one, or with the work that last
@@ -171,8 +176,7 @@ def _made_for(stream, make, *shape, **kw) -> torch.Tensor:
     out again before the current stream, where the caller goes on, is done with it too."""
     if stream is None:
         return make(*shape, **kw)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=kw["device"])
+    stream = _as_stream(stream, kw["device"])
     with torch.cuda.stream(stream):
         t = make(*shape, **kw)
     now = torch.cuda.current_stream(t.device)
@@ -281,19 +285,19 @@ def awsrc_encode_tiles(prm: Params, modules, out: Optional[torch.Tensor] = None,
     T = _tiles(prm, modules)
     dev = modules[0]["W0"].device
     if out is None:
-        out = torch.empty((T, 16), dtype=torch.uint8, device=dev)
+        out = _made_for(stream, torch.empty, T, 16, dtype=torch.uint8, device=dev)
     _require(out, "out", dtype=torch.uint8, numel=16 * T, device=dev)
     mods = module_array(modules)
     need = awsrc_encode_workspace_bytes(prm, modules)
     if workspace is None or workspace.numel() < need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _made_for(stream, torch.empty, need, dtype=torch.uint8, device=dev)
     _check(lib.awsrc_encode_tiles(ct.byref(prm), len(modules), mods, _dev_ptr(out), _dev_ptr(workspace),
                                   workspace.numel(), _stream(stream)), "encode_tiles")
     out._awsrc_workspace = workspace  # keep alive for awsrc_workspace_status
     return out
 
 
-def _rtn_buffers(W: torch.Tensor, sdq: bool, w0_dtype, out: Optional[Dict[str, torch.Tensor]]):
+def _rtn_buffers(W: torch.Tensor, sdq: bool, w0_dtype, out: Optional[Dict[str, torch.Tensor]], stream=None):
     """Checks W (and `out`, when given) or allocates the outputs of one module."""
     _require(W, "W")
     if W.dim() != 2:
@@ -310,13 +314,13 @@ def _rtn_buffers(W: torch.Tensor, sdq: bool, w0_dtype, out: Optional[Dict[str, t
             _require(out["sdq_consts"], "out['sdq_consts']", dtype=torch.float32, numel=2 * ((G + 255) // 256),
                      device=dev)
         return out
-    out = {"codes": torch.empty(rows * cols // 2, dtype=torch.uint8, device=dev),
-           "scales": torch.empty(G, dtype=torch.int16, device=dev)}
+    out = {"codes": _made_for(stream, torch.empty, rows * cols // 2, dtype=torch.uint8, device=dev),
+           "scales": _made_for(stream, torch.empty, G, dtype=torch.int16, device=dev)}
     if sdq:
-        out["sdq_codes"] = torch.empty(G, dtype=torch.int8, device=dev)
-        out["sdq_consts"] = torch.empty(2 * ((G + 255) // 256), dtype=torch.float32, device=dev)
+        out["sdq_codes"] = _made_for(stream, torch.empty, G, dtype=torch.int8, device=dev)
+        out["sdq_consts"] = _made_for(stream, torch.empty, 2 * ((G + 255) // 256), dtype=torch.float32, device=dev)
     w0t = W.dtype if w0_dtype is None else w0_dtype
-    out["W0"] = torch.empty(rows, cols, dtype=w0t, device=dev)
+    out["W0"] = _made_for(stream, torch.empty, rows, cols, dtype=w0t, device=dev)
     return out
 
 
@@ -327,7 +331,7 @@ def awsrc_rtn_quantize(W: torch.Tensor, sdq: bool = False, w0_dtype=None, stream
     sdq_codes (int8) and sdq_consts (float32 mean, step per 256 groups) when
     sdq, and W0 (in w0_dtype, default W's dtype). `out` reuses the buffers of
     an earlier call on the same shape."""
-    out = _rtn_buffers(W, sdq, w0_dtype, out)
+    out = _rtn_buffers(W, sdq, w0_dtype, out, stream)
     rows, cols = W.shape
     _check(lib.awsrc_rtn_quantize(rows, cols, _dev_ptr(W), _dtype_code(W), int(sdq), _dev_ptr(out["codes"]),
                                   _dev_ptr(out["scales"]), _dev_ptr(out.get("sdq_codes")),
@@ -342,7 +346,7 @@ def awsrc_rtn_quantize_batch(Ws: Sequence[torch.Tensor], sdq: bool = False, w0_d
     dtypes); returns one output dict per module, as the single call does."""
     if outs is not None and len(outs) != len(Ws):
         raise ValueError(f"{len(outs)} output sets for {len(Ws)} modules")
-    res = [_rtn_buffers(W, sdq, w0_dtype, None if outs is None else outs[i]) for i, W in enumerate(Ws)]
+    res = [_rtn_buffers(W, sdq, w0_dtype, None if outs is None else outs[i], stream) for i, W in enumerate(Ws)]
     arr = (RtnTask * len(Ws))()
     for i, (W, o) in enumerate(zip(Ws, res)):
         arr[i] = RtnTask(W.shape[0], W.shape[1], _dev_ptr(W), _dtype_code(W), int(sdq), _dev_ptr(o["codes"]),
@@ -383,23 +387,26 @@ def awsrc_sidecar_prepare(prm: Params, shapes, stream_bytes: torch.Tensor, K: in
     n = ct.c_size_t()
     _check(lib.awsrc_sidecar_workspace_bytes(ct.byref(prm), len(shapes), mods, ct.byref(n)), "sidecar_workspace_bytes")
     if workspace is None or workspace.numel() < n.value:
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=stream_bytes.device)
+        workspace = _made_for(stream, torch.empty, n.value, dtype=torch.uint8, device=stream_bytes.device)
     _check(lib.awsrc_sidecar_prepare(ct.byref(prm), len(shapes), mods, _dev_ptr(stream_bytes), stream_bytes.numel(),
                                      K, _dev_ptr(workspace), workspace.numel(), _stream(stream)), "sidecar_prepare")
     return workspace
 
 
 def _gemv_operands(shapes, m: int, backbone: Dict[str, torch.Tensor], x: torch.Tensor,
-                   y: Optional[torch.Tensor]):
+                   y: Optional[torch.Tensor], stream=None):
     """Checks one product's operands; returns (x as M x cols, y, PackedWeights)."""
     rows, cols = shapes[m]
     _require(x, "x", dtype=torch.float32)
     if x.numel() % cols != 0:
         raise ValueError(f"x holds {x.numel()} elements, not a whole number of rows of {cols}")
-    x = x.reshape(-1, cols)
     dev = x.device
+    if x.is_contiguous():
+        x = x.reshape(-1, cols)
+    else:  # a copy
+        x = _made_for(stream, lambda device: x.reshape(-1, cols), device=dev)
     if y is None:
-        y = torch.empty(x.shape[0], rows, dtype=torch.float32, device=dev)
+        y = _made_for(stream, torch.empty, x.shape[0], rows, dtype=torch.float32, device=dev)
     _require(y, "y", dtype=torch.float32, shape=(x.shape[0], rows), device=dev)
     sdq = "sdq_codes" in backbone
     G = rows * cols // 128
@@ -424,7 +431,7 @@ def awsrc_packed_gemv(prm: Params, shapes, m: int, backbone: Dict[str, torch.Ten
     _require(x, "x", dtype=torch.float32)
     if sidecar is not None:
         _require(sidecar, "sidecar", dtype=torch.uint8, device=x.device)
-    x, y, pw = _gemv_operands(shapes, m, backbone, x, y)
+    x, y, pw = _gemv_operands(shapes, m, backbone, x, y, stream)
     _check(lib.awsrc_packed_gemv(ct.byref(prm), len(shapes), mods, m, ct.byref(pw), _dev_ptr(sidecar),
                                  0 if sidecar is None else sidecar.numel(), x.shape[0], _dev_ptr(x), _dev_ptr(y),
                                  _stream(stream)), "packed_gemv")
@@ -443,7 +450,7 @@ def awsrc_packed_gemv_batch(prm: Params, shapes, tasks, sidecar: Optional[torch.
     ys, Ms, dev = [], set(), None
     for i, t in enumerate(tasks):
         m, backbone, x = t[0], t[1], t[2]
-        x, y, pw = _gemv_operands(shapes, m, backbone, x, t[3] if len(t) > 3 else None)
+        x, y, pw = _gemv_operands(shapes, m, backbone, x, t[3] if len(t) > 3 else None, stream)
         if dev is not None and x.device != dev:
             raise ValueError("every task's tensors must be on one device")
         dev = x.device
@@ -460,7 +467,7 @@ def awsrc_packed_gemv_batch(prm: Params, shapes, tasks, sidecar: Optional[torch.
 
 def awsrc_gen_basis(prm: Params, stream=None, device="cuda") -> torch.Tensor:
     W = (prm.C + 63) // 64
-    masks = torch.empty(prm.S * prm.P * W, dtype=torch.int64, device=device)
+    masks = _made_for(stream, torch.empty, prm.S * prm.P * W, dtype=torch.int64, device=device)
     _check(lib.awsrc_gen_basis(ct.byref(prm), _dev_ptr(masks), _stream(stream)), "gen_basis")
     return masks
 
@@ -492,14 +499,14 @@ def awsrc_select_records(prm: Params, modules, cands: torch.Tensor, rates: Seque
     n = ct.c_size_t()
     _check(lib.awsrc_select_workspace_bytes(ct.byref(prm), len(modules), mods, ct.byref(n)), "select_workspace_bytes")
     if workspace is None or workspace.numel() < n.value:
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        workspace = _made_for(stream, torch.empty, n.value, dtype=torch.uint8, device=dev)
     if out is None or out.numel() < cap:
-        out = torch.zeros(cap, dtype=torch.uint8, device=dev)
+        out = _made_for(stream, torch.zeros, cap, dtype=torch.uint8, device=dev)
     ncount = len(modules) if prm.variant == VARIANT_U else len(rates)
     if counts is None or counts.numel() < ncount:
-        counts = torch.empty(ncount, dtype=torch.int64, device=dev)
+        counts = _made_for(stream, torch.empty, ncount, dtype=torch.int64, device=dev)
     if nbytes is None or nbytes.numel() < len(rates):
-        nbytes = torch.empty(len(rates), dtype=torch.int64, device=dev)
+        nbytes = _made_for(stream, torch.empty, len(rates), dtype=torch.int64, device=dev)
     _check(lib.awsrc_select_records(ct.byref(prm), len(modules), mods, _dev_ptr(cands), r, len(rates),
                                     _dev_ptr(out), out.numel(), _dev_ptr(counts), _dev_ptr(nbytes),
                                     _dev_ptr(workspace), workspace.numel(), _stream(stream)), "select_records")
@@ -528,14 +535,14 @@ def awsrc_decode_apply(prm: Params, modules, stream_bytes: torch.Tensor, K: int,
         raise TypeError(f"out_dtype must be torch.float32 or torch.bfloat16, not {out_dtype}")
     code = DTYPE_F32 if out_dtype == torch.float32 else DTYPE_BF16
     if outs is None:
-        outs = [torch.empty_like(m["W0"], dtype=out_dtype) for m in modules]
+        outs = [_made_for(stream, torch.empty_like, m["W0"], dtype=out_dtype, device=m["W0"].device) for m in modules]
     _check_outs(modules, outs, out_dtype)
     mods = module_array(modules, decoder=True)
     ptrs = (ct.c_void_p * len(outs))(*[_dev_ptr(o) for o in outs])
     n = ct.c_size_t()
     _check(lib.awsrc_decode_workspace_bytes(ct.byref(prm), len(modules), mods, mode, ct.byref(n)), "decode_workspace_bytes")
     if workspace is None or workspace.numel() < n.value:
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        workspace = _made_for(stream, torch.empty, n.value, dtype=torch.uint8, device=dev)
     _check(lib.awsrc_decode_apply(ct.byref(prm), len(modules), mods, _dev_ptr(stream_bytes),
                                   stream_bytes.numel(), int(K), ptrs,
                                   code, mode, _dev_ptr(workspace), workspace.numel(), _stream(stream)),
@@ -608,9 +615,10 @@ def awsrc_set_wait_test(wait_ns: int = 0, stall_chunk: int = -1):
 def awsrc_verify_reciprocal(first: int, last: int, stream=None, device="cuda") -> int:
     """Bit patterns in [first, last) where the library's reciprocal differs from
     CUDA's correctly rounded one (synchronises)."""
-    bad = torch.zeros(1, dtype=torch.int64, device=device)
+    bad = _made_for(stream, torch.zeros, 1, dtype=torch.int64, device=device)
     _check(lib.awsrc_verify_reciprocal(first, last, _dev_ptr(bad), _stream(stream)), "verify_reciprocal")
-    return int(bad.item())
+    with torch.cuda.stream(None if stream is None else _as_stream(stream, device)):  # the count is read behind the kernel
+        return int(bad.item())
 
 
 def candidates_to_numpy(cands: torch.Tensor) -> np.ndarray:

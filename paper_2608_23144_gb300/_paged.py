@@ -8,7 +8,7 @@ from typing import Optional
 
 import torch
 
-from ._binding import AwsrcError, _check, _require, lib
+from ._binding import AwsrcError, _check, _made_for, _require, lib
 from ._binding import _stream as _stream_of
 
 # The current stream's handle without a torch.cuda.Stream object: the object
@@ -154,7 +154,7 @@ def awsrc_attention_workspace(cache: KvCache, n_heads: int, stream=None) -> torc
     cache, ready for use: any batch, one stream at a time."""
     n = ct.c_size_t()
     _check(lib.awsrc_attention_workspace_bytes(cache._ref, n_heads, ct.byref(n)), "attention_workspace_bytes")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=cache.device)
+    ws = _made_for(stream, torch.empty, n.value, dtype=torch.uint8, device=cache.device)
     _check(_on(ws.device, lib.awsrc_attention_workspace_init, cache._ref, n_heads, ws.data_ptr(), n.value,
                _stream(stream, ws.device)),
            "attention_workspace_init")
@@ -209,7 +209,7 @@ def awsrc_kv_append(cache: KvCache, batch: KvBatch, q: torch.Tensor, k: torch.Te
     dev, shape = _common(cache, batch, q, workspace)
     dt = q.dtype
     if q_out is None:
-        q_out = torch.empty(shape, dtype=dt, device=dev)
+        q_out = _made_for(stream, torch.empty, *shape, dtype=dt, device=dev)
     kv_shape = (shape[0], cache.kv_heads, shape[2])
     rq = _rows(q, "q", shape, dt, dev)
     rk = _rows(k, "k", kv_shape, dt, dev)
@@ -244,7 +244,7 @@ def awsrc_paged_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, works
     dev, shape = _common(cache, batch, q, workspace)
     dt = q.dtype
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=dev)
+        out = _made_for(stream, torch.empty, *shape, dtype=dt, device=dev)
     rq = _rows(q, "q", shape, dt, dev)
     ro = _rows(out, "out", shape, dt, dev)
     lp = None

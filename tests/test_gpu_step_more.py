@@ -38,3 +38,30 @@ def test_quantize_on_another_stream_than_the_busy_current_one(aw, dtype):
         assert torch.equal(m.codes.view(torch.uint8), want.codes.view(torch.uint8)) and torch.equal(m.exps, want.exps)
         assert torch.equal(y, product)
     assert aw.awsrc_workspace_status(ws) == 0
+
+
+def test_older_calls_on_another_stream_than_the_busy_current_one(aw):
+    """Backbone, seed search, selection (whose stream starts as zeros) and decoding on a side stream, every
+    buffer made by the calls, while the current stream has work queued."""
+    from synth import make_module
+    m = make_module(256, 512, seed=5, device="cuda")
+    prm = aw.params(C=64, P=4, b=4, S=128)
+
+    def run(s=None):
+        back = aw.awsrc_rtn_quantize(m["W"], stream=s)
+        cands = aw.awsrc_encode_tiles(prm, [m], stream=s)
+        out, counts, nbytes = aw.awsrc_select_records(prm, [m], cands, [0.3], stream=s)
+        return [back["codes"], back["scales"].view(torch.uint8), cands, counts, nbytes, out, *aw.awsrc_decode_apply(prm, [m], out, -1, stream=s)]
+
+    want = run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(2):
+        torch.cuda._sleep(20_000_000)
+        got = run(side)
+        torch.cuda.synchronize()
+        used = int(want[4][0])
+        for a, b in zip(got, want):
+            assert torch.equal(a[:used] if b is want[5] else a, b[:used] if b is want[5] else b)
+    torch.cuda._sleep(20_000_000)
+    assert aw.awsrc_verify_reciprocal(0x3F800000, 0x3F900000, stream=side) == 0
