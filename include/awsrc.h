@@ -697,7 +697,7 @@ typedef struct awsrc_probs {
  *   probabilities rounded to the nearest multiple of 2^-45 (ties to even). Where all w_j are 0 the row
  *   of `target` takes their place; where that is 0 too the token is -1.
  *   Probabilities count as 0 when NaN or negative and as 1 above 1; u and r as
- *   0 when NaN or negative; r as the largest value below 1 from 1 on.
+ *   0 when NaN or negative; r from 1 on draws the last j with a weight.
  *   accepted   n_seq: accepted drafts;  tokens  n_seq x (max_draft + 1): those,
  *              the token, -1 behind.
  *   kv_len, keep  n_seq each, or both NULL: keep = kv_len less the drafts not

@@ -187,6 +187,18 @@ __device__ __forceinline__ int find_in(const Row<P, Q>& row, int j, int j1, uint
   return found;
 }
 
+// floor(r total), exactly: r is a whole number of 24 bits by 2^-s, and their product has 88
+// bits. (r cut off to units of 2^-64 missed whole numbers by less than 2^-18 below 2^-40.)
+// From 1 on the last weight is drawn.
+__device__ __forceinline__ uint64_t threshold(float r, uint64_t total) {
+  if (r >= 1.0f) return total - 1;
+  if (!(r > 0.0f)) return 0;
+  const uint32_t u = __float_as_uint(r), e = u >> 23;
+  const uint64_t m = (u & 0x7FFFFFu) | (e ? 1u << 23 : 0u), lo = m * total, hi = __umul64hi(m, total);
+  const int s = 150 - (int)max(e, 1u);  // 24 to 149
+  return s < 64 ? hi << (64 - s) | lo >> s : s < 128 ? hi >> (s - 64) : 0;
+}
+
 template <typename P, typename Q, bool kVec>
 __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const __grid_constant__ VerifyArgs a) {
   const P* probs_p = static_cast<const P*>(a.p);
@@ -269,10 +281,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const __grid_con
     row.drop = -1;
   }
   for (int w = 0; w < warp; ++w) below += s_warp[w];
-  // floor(r total), r in units of 2^-64
-  const float r = a.r[b];
-  const uint64_t ru = r >= 1.0f ? ~0ull : r > 0.0f ? __float2ull_rz(__fmul_rn(r, 0x1p64f)) : 0;
-  const uint64_t bar = __umul64hi(total, ru);
+  const uint64_t bar = threshold(a.r[b], total);
   if (total != 0 && below <= bar && bar < below + mine) {
     // the step that it falls in, and its elements again
     uint64_t sum = below;

@@ -65,3 +65,27 @@ def test_older_calls_on_another_stream_than_the_busy_current_one(aw):
             assert torch.equal(a[:used] if b is want[5] else a, b[:used] if b is want[5] else b)
     torch.cuda._sleep(20_000_000)
     assert aw.awsrc_verify_reciprocal(0x3F800000, 0x3F900000, stream=side) == 0
+
+
+def test_verify_thresholds_of_tiny_random_numbers(aw):
+    """r C_V just above a whole number of units with r below 2^-40: weights k, rest, of T = ceil(k 2^65 / m) units in all, and
+    r = m 2^-65, so k <= r T < k + 2^-18: the first weight does not reach above it, the second does. m is odd, so r has bits
+    below 2^-64. Random numbers down to the smallest of binary32 beside them."""
+    from test_gpu_step import check
+    rows, r = [], []
+    for m in (2 ** 23 + 1, 2 ** 23 + 4097, 2 ** 24 - 1, 12345679):
+        for k in (1, 3, 7):
+            total = -(-k * 2 ** 65 // m)
+            assert total < 2 ** 45 and k * 2 ** 65 <= m * total < k * 2 ** 65 + m
+            rest = total - k
+            rows.append([k, rest >> 23 << 23, rest & (2 ** 23 - 1), 0, 0])
+            r.append(m * 2.0 ** -65)
+    for tiny in (2.0 ** -149, 2.0 ** -127, 2.0 ** -64, 2.0 ** -46, 3 * 2.0 ** -47, 2.0 ** -45, 1 - 2.0 ** -24):
+        rows.append([1, 2, 2 ** 44, 0, 1])
+        r.append(tiny)
+    p = (torch.tensor(rows, dtype=torch.float64) * 2.0 ** -45).float()
+    assert torch.equal(p.double() * 2.0 ** 45, torch.tensor(rows, dtype=torch.float64))
+    n = len(rows)
+    for q in (None, torch.zeros_like(p)):
+        want = check(aw, list(range(n + 1)), [0] * n, p, q, torch.rand(n), torch.tensor(r, dtype=F32), 0, [5] * n)
+        assert [t[0] for t in want[1][:12]] == [1] * 12
