@@ -703,7 +703,7 @@ typedef struct awsrc_probs {
  *   kv_len, keep  n_seq each, or both NULL: keep = kv_len less the drafts not
  *              accepted (what awsrc_kv_plan takes; keep may be kv_len, but not a
  *              pool's, where awsrc_kv_plan has to find what the sequences hold).
- * A draft outside the vocabulary is not accepted and is reported (bit 3), as are
+ * A draft outside the vocabulary is not accepted and is reported (bit 3) wherever it stands, as are
  * rows that cannot be right (row_start outside [0, n_rows] or falling, more than
  * max_draft drafts): their sequence, like one without rows, gets accepted 0,
  * tokens -1 and keep = kv_len.

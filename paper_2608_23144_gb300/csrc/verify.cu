@@ -227,19 +227,18 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const __grid_con
   }
   if (warp == 0) {
     int stop = drafts;
-    for (int i0 = 0; i0 < drafts && stop == drafts; i0 += 32) {
+    // up to the first refused; the ids behind it are looked at all the same
+    for (int i0 = 0; i0 < drafts && (stop == drafts || rank == 0); i0 += 32) {
       const int i = i0 + lane;
-      bool refuse = false;
-      if (i < drafts) {
-        const int64_t t = first + i;
-        const int x = a.ids[t + 1];
-        refuse = true;
-        if (x >= 0 && x < a.vocab) {
-          const float p = value(probs_p[t * a.ps + x]), q = a.q ? value(probs_q[t * a.qs + x]) : 1.0f, u = a.u[t];
-          refuse = !((double)fmaxf(u, 0.0f) * (double)clean(q) < (double)clean(p));
-        } else if (rank == 0) {
-          atomicOr(a.status, kFaultBatch);
-        }
+      const int64_t t = first + i;
+      const int x = i < drafts ? a.ids[t + 1] : 0;
+      const bool outside = x < 0 || x >= a.vocab;
+      if (outside && rank == 0) atomicOr(a.status, kFaultBatch);
+      if (stop < drafts) continue;
+      bool refuse = outside;
+      if (i < drafts && !outside) {
+        const float p = value(probs_p[t * a.ps + x]), q = a.q ? value(probs_q[t * a.qs + x]) : 1.0f, u = a.u[t];
+        refuse = !((double)fmaxf(u, 0.0f) * (double)clean(q) < (double)clean(p));
       }
       const uint32_t no = __ballot_sync(0xffffffffu, refuse);
       if (no) stop = i0 + __ffs(no) - 1;

@@ -89,3 +89,19 @@ def test_verify_thresholds_of_tiny_random_numbers(aw):
     for q in (None, torch.zeros_like(p)):
         want = check(aw, list(range(n + 1)), [0] * n, p, q, torch.rand(n), torch.tensor(r, dtype=F32), 0, [5] * n)
         assert [t[0] for t in want[1][:12]] == [1] * 12
+
+
+@pytest.mark.parametrize("bad,value", [(1, -1), (20, 50), (33, 2 ** 31 - 1), (36, -5), (65, 50), (70, 99)])
+@pytest.mark.parametrize("stop", [0, 31, 32, 40, 70])
+def test_verify_reports_drafts_outside_wherever_they_are(aw, bad, value, stop):
+    """70 drafts, the one at `stop` refused, the one at `bad` (counted from 1) outside the vocabulary: reported, whether it is
+    looked at for acceptance or not, and never accepted."""
+    from test_gpu_step import check
+    gen = torch.Generator().manual_seed(bad)
+    p = torch.softmax(torch.randn(71, 50, generator=gen) * 3, -1)
+    ids = [0] + p[:-1].argmax(-1).tolist()
+    ids[bad] = value
+    u = torch.zeros(71)
+    u[stop:] = 1.0
+    want = check(aw, [0, 71], ids, p, None, u, torch.rand(1, generator=gen), 70, [500], flags=8)
+    assert want[0] == [min(stop, bad - 1)]
