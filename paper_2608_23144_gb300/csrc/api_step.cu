@@ -183,12 +183,13 @@ awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, 
   // few rows of x are read while others' results are written
   const int64_t xs = size_of(x_dtype), ys = size_of(y_dtype);
   if (share(Rows{x, x_stride * xs, a.x.cols * xs}, Rows{y, y_stride * ys, a.w.rows * ys}, a.x.rows)) return AWSRC_ERR_INVALID_ARG;
-  cudaError_t e = cudaSuccess;
-  if (fp8_gemm_quantizes(a)) {
+  bool itself;
+  cudaError_t e = fp8_gemm_quantizes(a, &itself);
+  if (e == cudaSuccess && itself) {
     a.raw = x;
     a.raw_stride = x_stride;
     a.raw_bf16 = x_dtype == AWSRC_DTYPE_BF16;
-  } else {
+  } else if (e == cudaSuccess) {
     // the quantising kernel lets the product start only after it has waited for all kernels before it
     a.early = 1;
     e = launch_fp8_quantize(x, x_dtype, x_stride, a.x, (cudaStream_t)stream);

@@ -43,8 +43,7 @@ namespace {
 using namespace fp8;
 
 constexpr int kThreads = 352, kXWarps = 8, kCopyWarp = 8, kMmaWarp = 9, kScaleWarp = 10;
-constexpr int kMaxSplit = 8;  // thread blocks that share a tile's columns
-constexpr int kSms = 152;
+constexpr int kMaxSplit = kFewSplit;
 
 // Where x comes from: its codes with the blocks of w; all codes first; all rows first, quantised here.
 enum Source { kCodes, kCodesFirst, kF32First, kBf16First };
@@ -441,27 +440,14 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_few_kernel(const __grid_const
   }
 }
 
-// Rows of w in a tile and thread blocks per tile: the least time by a model of a thread
-// block's stages, each 350 ns (its products) or its bytes at 50 GB/s, and 1.8 us where
-// parts are joined.
-void choose(GemmArgs* a) {
-  const int rows = a->w.rows, blocks = a->w.blocks();
-  const double x_bytes = 512.0 * a->x.rows;  // as if bf16: the choice, and so the sums, are the same for x and for its codes
-  double best = 0;
-  const int twos = (blocks + 1) / 2;
-  for (int split = 1; split <= kMaxSplit && split <= twos; ++split) {
-    const int64_t most = split > 1 ? max_clusters(split) : kSms;  // tiles at a time
-    int64_t waves = 1, r;
-    for (;; ++waves) {
-      r = (rows + most * waves - 1) / (most * waves);
-      r = (r + 7) / 8 * 8;
-      if (r <= BM || split > 1) break;
-    }
-    if (r > BM || most < 1) continue;  // parts are joined in one wave
-    const double bytes = (256.0 * r + x_bytes) / 50.0, stage = bytes > 350.0 ? bytes : 350.0;
-    const double all = (double)waves * ((twos + split - 1) / split) * stage + (split > 1 ? 1800.0 : 0.0);
-    if (best == 0 || all < best) best = all, a->n = (int)r, a->split = split;
-  }
+cudaError_t choose(GemmArgs* a) {
+  Clusters most;
+  const cudaError_t e = max_clusters(&most);
+  if (e != cudaSuccess) return e;
+  const Choice c = choose_few(a->w.rows, a->w.blocks(), a->x.rows, most);
+  a->n = c.n;
+  a->split = c.split;
+  return cudaSuccess;
 }
 
 template <int N, Source X>
@@ -488,10 +474,13 @@ bool x_first(const GemmArgs& a) {
 
 }  // namespace
 
-bool fp8_gemm_quantizes(const GemmArgs& in) {
+cudaError_t fp8_gemm_quantizes(const GemmArgs& in, bool* itself) {
   GemmArgs a = in;
-  choose(&a);
-  return x_first(a);
+  *itself = false;
+  if (a.x.rows > kFirstRows) return cudaSuccess;
+  const cudaError_t e = choose(&a);
+  if (e == cudaSuccess) *itself = x_first(a);
+  return e;
 }
 
 cudaError_t launch_fp8_gemm(const GemmArgs& in, cudaStream_t st) {
@@ -502,8 +491,7 @@ cudaError_t launch_fp8_gemm(const GemmArgs& in, cudaStream_t st) {
   cudaError_t e;
   if (a.x.rows > kFewRows) {
     e = launch_fp8_pairs(a, st);
-  } else {
-    choose(&a);
+  } else if ((e = choose(&a)) == cudaSuccess) {
     if (x_first(a))
       e = !a.raw ? launch<16, kCodesFirst>(a, st) : a.raw_bf16 ? launch<16, kBf16First>(a, st) : launch<16, kF32First>(a, st);
     else

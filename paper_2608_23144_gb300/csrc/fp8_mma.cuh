@@ -4,14 +4,16 @@
 
 #include <cuda.h>
 
+#include "fp8_choice.h"
 #include "step.cuh"
 #include "tc05.cuh"
 
 namespace awsrc {
 
-// Clusters of `size` thread blocks, one per SM, that the current device runs at a time
-// (fewer than its SMs allow: a cluster lies in one group of them).
-int max_clusters(int size);
+// Clusters of thread blocks, one per SM, that the current device runs at a time (fewer than
+// its SMs allow: a cluster lies in one group of them). An answer is kept, a failure is the
+// call's: with other shares the sums would have another order.
+cudaError_t max_clusters(fp8::Clusters* most);
 
 // A tiled tensor of up to 3 dimensions (innermost first), rows past the last read as 0.
 cudaError_t make_tensor_map(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* p, const cuuint64_t* dims,
@@ -21,7 +23,7 @@ namespace fp8 {
 
 using namespace tc05;
 
-constexpr int BM = 128;
+constexpr int BM = kTileRows;
 // Blocks summed in tensor memory before the sums leave it: the cores cut a running sum off
 // (below 2^-24 of it, measured) at each of a block's four products. Positive terms are off by
 // 3e-7 after 2048 columns and 1.2e-5 after 27648; bf16 results take 2^-9 of their own.

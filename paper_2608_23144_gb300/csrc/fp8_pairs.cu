@@ -37,15 +37,13 @@ namespace {
 using namespace fp8;
 
 constexpr int kThreads = 320, kCopyWarp = 8, kMmaWarp = 9;
-constexpr int kMaxN = 256;
+constexpr int kMaxN = kPairMaxN;
 constexpr int kStages = 6;
 constexpr int kStageBytes = (BM + kMaxN / 2) * 128;
 constexpr int kSfBytes = 512 * 3;  // scales of 128 rows of w, of up to 256 of x
 constexpr int kSfCols = 12, kSfAt = 512 - kSfSets * kSfCols;
 constexpr int kTwoBufs = 192;      // two accumulators of so many columns end before the scales
-constexpr int kMaxSplit = 4;       // pairs that share a tile's columns
-constexpr int kLeast = 4;          // blocks that one of them has at least
-constexpr int kPairs = 76;
+constexpr int kMaxSplit = kPairSplit;
 constexpr int kGroup = 16;         // tiles of rows of x that are walked together (2: 354 us, 8: 332, 16: 325, 32: 333)
 
 struct Smem {
@@ -428,25 +426,6 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_pairs_kernel(const __grid_con
   }
 }
 
-// Rows of x in a tile and pairs per tile: the fewest cycles by a model of both. A
-// block costs a pair what its bytes take at 52 bytes per cycle and SM, or its
-// products at 2 cycles per row of x, the larger; a tile 2500 more, and 8 per row of
-// x and further pair where pairs join their parts.
-void choose(GemmArgs* a) {
-  const int blocks = a->x.blocks();
-  const int64_t tiles_w = (a->w.tiles() + 1) / 2;
-  double best = 0;
-  for (int n = 64; n <= kMaxN; n += 64)
-    for (int split = 1; split <= kMaxSplit && (split == 1 || split * kLeast <= blocks); ++split) {
-      const int64_t tiles = tiles_w * ((a->x.rows + n - 1) / n);
-      if (split > 1 && tiles > max_clusters(2 * split)) continue;
-      const double load = (16384.0 + 64.0 * n) / 52.0, mma = 2.0 * n;
-      const double tile = (double)((blocks + split - 1) / split) * (load > mma ? load : mma) + 2500.0 + 8.0 * n * (split - 1);
-      const double all = (split > 1 ? 1.0 : (double)((tiles + kPairs - 1) / kPairs)) * tile;
-      if (best == 0 || all < best) best = all, a->n = n, a->split = split;
-    }
-}
-
 // A tensor [blocks][rows][`row` bytes], read in boxes of `box` rows.
 cudaError_t tensor(CUtensorMap* map, CUtensorMapDataType type, int size, const void* p, int row, int64_t rows, int64_t blocks,
                    int box) {
@@ -498,35 +477,44 @@ cudaError_t make_tensor_map(CUtensorMap* map, CUtensorMapDataType type, int rank
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-int max_clusters(int size) {
+cudaError_t max_clusters(fp8::Clusters* most) {
   constexpr int kDevices = 64, kMost = 8;
-  static std::atomic<int> known[kDevices][kMost + 1];  // 1 + the answer
+  static std::atomic<int> known[kDevices][kMost + 1];  // 1 + the answer; 0: not asked yet, or the question failed
   int dev = 0;
-  if (size < 1 || size > kMost || cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return 0;
-  if (const int k = known[dev][size].load(std::memory_order_relaxed)) return k - 1;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = size;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(size);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(Smem) + 1024;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  int n = 0;
-  if (allow_smem<Smem>(fp8_pairs_kernel, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&n, fp8_pairs_kernel, &cfg) != cudaSuccess) {
-    (void)cudaGetLastError();  // no split, then
-    n = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  most->of[0] = 0;
+  most->of[1] = kSms;
+  for (int size = 2; size <= kMost && e == cudaSuccess; ++size) {
+    const int k = dev < kDevices ? known[dev][size].load(std::memory_order_relaxed) : 0;
+    if (k) {
+      most->of[size] = k - 1;
+      continue;
+    }
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = size;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(size);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(Smem) + 1024;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = allow_smem<Smem>(fp8_pairs_kernel, (int)cfg.dynamicSmemBytes);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&most->of[size], fp8_pairs_kernel, &cfg);
+    if (e == cudaSuccess && dev < kDevices) known[dev][size].store(most->of[size] + 1, std::memory_order_relaxed);
   }
-  known[dev][size].store(n + 1, std::memory_order_relaxed);
-  return n;
+  return e;
 }
 
 cudaError_t launch_fp8_pairs(const GemmArgs& in, cudaStream_t st) {
   GemmArgs a = in;
-  choose(&a);
+  Clusters most;
+  const cudaError_t e = max_clusters(&most);
+  if (e != cudaSuccess) return e;
+  const Choice c = choose_pairs(a.w.rows, a.x.blocks(), a.x.rows, most);
+  a.n = c.n;
+  a.split = c.split;
   return launch(a, st);
 }
 
