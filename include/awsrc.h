@@ -517,7 +517,9 @@ typedef struct awsrc_kv_cache {
  * none is allowed); token p of it lies in page page_table[b * table_stride +
  * p / page], row p % page. The arrays are read on the device, so that a
  * captured graph follows their contents.
- *   n_tok    rows of q, k and v (q_start[n_seq]); 0 makes every call a no-op.
+ *   n_tok    rows of q, k and v, q_start[n_seq] or more: rows behind the last
+ *            sequence are left as they are (a step of fixed size that not all
+ *            sequences got into); 0 makes every call a no-op.
  *   max_new, max_kv  the largest number of new tokens and kv_len the arrays may
  *            hold: they choose launch shapes. Results stay right for larger
  *            contents, only slower.

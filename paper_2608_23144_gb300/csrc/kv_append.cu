@@ -422,8 +422,10 @@ __device__ void rotate_q(const AppendArgs& a, int t, int part, int parts) {
   }
   KvSeq s{0, -1, 0};
   if (b >= 0) s = kv_seq(c, b);
+  // a row behind the last sequence: left as it is (with a start that falls, visit 0 has reported it)
+  if (s.n >= 0 && t >= s.first + s.n) return;
   const int pos = s.kv - s.n + t - s.first;
-  if (s.n < 0 || t >= s.first + s.n || pos >= a.rope_rows) {
+  if (s.n < 0 || pos >= a.rope_rows) {
     if (lane == 0) atomicOr(c.status, kFaultBatch);
     return;
   }
