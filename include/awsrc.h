@@ -655,7 +655,11 @@ typedef struct awsrc_kv_pool {
  *     it do not exceed free_count + all pages given back (or it needs none), and
  *     the new tokens of all sequences up to it do not exceed n_tok; else it gets
  *     none in this step, keeps its keep[b] tokens and gives back what those do
- *     not use. awsrc_workspace_status then has bit 4 (16).
+ *     not use. awsrc_workspace_status then has bit 4 (16), and on the device
+ *     q_start[b + 1] == q_start[b] with add[b] > 0 says who. Its needs count
+ *     against all behind it all the same, in every step until pages come back or
+ *     its add is 0: a prompt that does not fit stops those behind it at their
+ *     next page. Sequences under way belong in front of those that wait.
  *   Stack. Pages given back go on top in the order of (sequence, table entry);
  *     then pages are taken from the top in the same order.
  *   On return, kv_len[b] = keep[b] + the tokens it got, page_table and the stack
@@ -696,8 +700,10 @@ typedef struct awsrc_probs {
  *   the weights w_j = max(0, target[s][j] - draft[s][j]); when all drafts are
  *   accepted, from w_j = target[s][j] of the last row s. It is the smallest j
  *   with w_0 + .. + w_j > r[b] * (w_0 + .. + w_V-1), the sums exact over
- *   probabilities rounded to the nearest multiple of 2^-45 (ties to even). Where all w_j are 0 the row
- *   of `target` takes their place; where that is 0 too the token is -1.
+ *   probabilities rounded to the nearest multiple of 2^-45 (ties to even; the
+ *   rounding moves at most 2^-46 of probability an entry, and one below that is
+ *   never drawn). Where all w_j are 0 the row of `target` takes their place;
+ *   where that is 0 too the token is -1.
  *   Probabilities count as 0 when NaN or negative and as 1 above 1; u and r as
  *   0 when NaN or negative; r from 1 on draws the last j with a weight.
  *   accepted   n_seq: accepted drafts;  tokens  n_seq x (max_draft + 1): those,
@@ -705,10 +711,12 @@ typedef struct awsrc_probs {
  *   kv_len, keep  n_seq each, or both NULL: keep = kv_len less the drafts not
  *              accepted (what awsrc_kv_plan takes; keep may be kv_len, but not a
  *              pool's, where awsrc_kv_plan has to find what the sequences hold).
- * A draft outside the vocabulary is not accepted and is reported (bit 3) wherever it stands, as are
- * rows that cannot be right (row_start outside [0, n_rows] or falling, more than
- * max_draft drafts): their sequence, like one without rows, gets accepted 0,
- * tokens -1 and keep = kv_len.
+ * A draft outside the vocabulary is not accepted and is reported (bit 3) wherever
+ * it stands, as are rows that cannot be right (row_start outside [0, n_rows] or
+ * falling, more than max_draft drafts): their sequence, like one without rows,
+ * gets accepted 0, tokens -1 and keep = kv_len. A sequence that awsrc_kv_plan left
+ * out of the step is one without rows: the token that it had is still its next,
+ * and the caller keeps it (row_start[b + 1] == row_start[b] says so).
  * Bit-reproducible. Errors: INVALID_ARG, SHAPE (vocab < 1), UNSUPPORTED (n_seq >
  * 65535, vocab > 2^18, max_draft > 2^20), WORKSPACE, CUDA.
  */

@@ -142,7 +142,8 @@ def awsrc_kv_plan(pool: KvPool, keep: Optional[torch.Tensor], add: torch.Tensor,
     tok_slot (int64), [n_tok] each, receive every new token's sequence, position
     and page * page size + row, -1 behind the last. n_tok defaults to their
     length. awsrc_workspace_status(workspace): 8 an entry that cannot be right
-    (its sequence was left as it is), 16 a sequence that found no room."""
+    (its sequence was left as it is), 16 a sequence that found no room: it has no
+    rows in q_start and holds up those behind it that need pages."""
     if not isinstance(pool, KvPool):
         raise TypeError("pool must come from awsrc_kv_pool")
     dev, n = pool.device, pool.n_seq
@@ -206,7 +207,9 @@ def awsrc_verify_drafts(row_start: torch.Tensor, ids: torch.Tensor, target: torc
     accepted drafts, the token, -1 behind), int32. With kv_len (int32 [n_seq]),
     `keep` receives it less the drafts not accepted, as awsrc_kv_plan takes it;
     keep may be kv_len, but not a pool's: awsrc_kv_plan has to find there what the
-    sequences hold. max_draft defaults to that of `tokens`."""
+    sequences hold. A sequence without rows gets tokens of -1: one that the plan
+    left out goes on with the token it had, torch.where(row_start[1:] >
+    row_start[:-1], next, had). max_draft defaults to that of `tokens`."""
     if not isinstance(row_start, _Tensor) or row_start.dim() != 1 or row_start.shape[0] < 1:
         _require(row_start, "row_start", dtype=_I32)
         raise ValueError(f"row_start has shape {tuple(row_start.shape)}, expected (n_seq + 1,)")

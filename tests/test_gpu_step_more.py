@@ -105,3 +105,93 @@ def test_verify_reports_drafts_outside_wherever_they_are(aw, bad, value, stop):
     u[stop:] = 1.0
     want = check(aw, [0, 71], ids, p, None, u, torch.rand(1, generator=gen), 70, [500], flags=8)
     assert want[0] == [min(stop, bad - 1)]
+
+
+def test_a_captured_round_with_a_pool_that_runs_out(aw):
+    """Five users, rounds of drafts as one captured graph, pages for about half of what they want. A user that finds no room has no
+    rows in the round; it goes on with the token it had (verification gives -1 for it) once others' pages come back. Rows of
+    the round are found through the maps, so that they are right whoever was admitted. Every round against the definitions."""
+    import step_ref as ref
+    gen = torch.Generator().manual_seed(21)
+    users, heads, kv_heads, dim, page, vocab, drafts, pages = 5, 4, 2, 64, 16, 300, 3, 7
+    hidden, per, most = heads * dim, drafts + 1, 128
+    cache = aw.awsrc_kv_cache_alloc(pages, kv_heads, dim, page)
+    pool = aw.awsrc_kv_pool_alloc(cache, users, most)
+    attn_ws, ws, n_tok = aw.awsrc_attention_workspace(cache, heads), aw.awsrc_step_workspace(), users * per
+
+    def weights(n, k):
+        return aw.awsrc_fp8_quantize((torch.randn(n, k, generator=gen) * k ** -0.5).cuda())
+
+    wqkv, wo, head = weights(hidden + 2 * kv_heads * dim, hidden), weights(hidden, hidden), weights(vocab, hidden)
+    embed = torch.randn(vocab, hidden, generator=gen).cuda()
+    x8 = aw.awsrc_fp8_matrix(n_tok, hidden)
+    q_start, keep = torch.empty(users + 1, dtype=I32, device="cuda"), torch.zeros(users, dtype=I32, device="cuda")
+    seq, pos = (torch.empty(n_tok, dtype=I32, device="cuda") for _ in range(2))
+    add, last = torch.full((users,), per, dtype=I32, device="cuda"), cuda_ints([3, 1, 4, 1, 5])
+    guess = torch.zeros(users, drafts, dtype=I32, device="cuda")
+    u, r = torch.zeros(n_tok, device="cuda"), torch.zeros(users, device="cuda")
+    ids, probs = torch.zeros(n_tok, dtype=I32, device="cuda"), torch.zeros(n_tok, vocab, device="cuda")
+    accepted, tokens = torch.empty(users, dtype=I32, device="cuda"), torch.empty(users, per, dtype=I32, device="cuda")
+    step = aw.awsrc_kv_batch(q_start, pool.kv_len, pool.page_table, n_tok, per, most)
+
+    def one_round():
+        aw.awsrc_kv_plan(pool, keep, add, ws, q_start=q_start, tok_seq=seq, tok_pos=pos)
+        who = seq.long().clamp(min=0)
+        window = torch.cat([last[:, None], guess], 1)
+        ids.copy_(window[who, (pos - keep[who]).long().clamp(0, drafts)])
+        x = embed[ids.long()]
+        qkv = aw.awsrc_fp8_linear(x, wqkv, x8, ws).view(n_tok, -1, dim)
+        q = aw.awsrc_kv_append(cache, step, qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:], None, None,
+                               attn_ws, q_out=torch.zeros(n_tok, heads, dim, device="cuda"))
+        o = aw.awsrc_paged_attention(cache, step, q, attn_ws, out=torch.zeros(n_tok, heads, dim, device="cuda")).view(n_tok, hidden)
+        x = x + aw.awsrc_fp8_linear(o, wo, x8, ws)
+        probs.copy_(torch.softmax(4 * aw.awsrc_fp8_linear(x, head, x8, ws), -1))
+        aw.awsrc_verify_drafts(q_start, ids, probs, None, u, r, ws, kv_len=pool.kv_len, keep=keep, accepted=accepted, tokens=tokens)
+        token = tokens.gather(1, accepted.long()[:, None])[:, 0]
+        last.copy_(torch.where(q_start[1:] > q_start[:-1], token, last))  # who had no rows keeps its token
+
+    state = (pool.page_table, pool.kv_len, pool.free_pages, pool.free_count, keep, last)
+    before = [s.clone() for s in state]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        one_round()
+        for s, b in zip(state, before):
+            s.copy_(b)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            one_round()
+    torch.cuda.synchronize()
+
+    table, length, free, count = [pool.page_table.tolist(), [0] * users, pool.free_pages.tolist(), pages]
+    kept, mine, waited, resumed = [0] * users, last.tolist(), set(), set()
+    for i in range(30):
+        adds = [per if k + per <= most else 0 for k in kept]
+        if i % 6 == 5:  # the longest ends: its pages come back, a new text of its begins
+            b = max(range(users), key=lambda b: kept[b])
+            kept[b], mine[b] = 0, 7
+            keep[b], last[b] = 0, 7
+        add.copy_(torch.tensor(adds, dtype=I32))
+        guess.copy_(torch.randint(vocab, (users, drafts), generator=gen))
+        u.uniform_(0, 0.02)
+        r.copy_(torch.rand(users, generator=gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        table, length, free, count, starts, seqs, poss, _, flags = ref.plan(page, table, length, free, count, kept, adds, n_tok)
+        assert aw.awsrc_workspace_status(ws) == flags and aw.awsrc_workspace_status(attn_ws) == 0
+        assert q_start.tolist() == starts and seq.tolist() == seqs and pos.tolist() == poss
+        assert pool.kv_len.tolist() == length and pool.page_table.tolist() == table and pool.free_count.item() == count
+        fed, g = ids.tolist(), guess.tolist()
+        for b in range(users):
+            rows = fed[starts[b]:starts[b + 1]]
+            assert rows == ([mine[b]] + g[b])[:len(rows)]
+            if rows and b in waited:
+                resumed.add(b)
+            if adds[b] and not rows:
+                waited.add(b)
+        want = ref.verify(starts, fed, probs.double().tolist(), None, u.tolist(), r.tolist(), drafts, length)
+        assert accepted.tolist() == want[0] and tokens.tolist() == want[1] and keep.tolist() == want[2]
+        kept = want[2]
+        mine = [want[1][b][want[0][b]] if starts[b + 1] > starts[b] else mine[b] for b in range(users)]
+        assert last.tolist() == mine and min(mine) >= 0
+    assert waited and resumed  # some had to wait, and went on
