@@ -1,0 +1,102 @@
+"""GPU parity of the 8-bit products where sums are long, waits run out in every kernel,
+rows are written beside others that stay, and weights come out of the records' decoder."""
+import pytest
+import torch
+
+import step_ref as ref
+from test_gpu_fp8 import aw, int_matrix, spread  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def test_quantize_writes_its_rows_and_no_others(aw):  # noqa: F811
+    """13 of 16 rows of codes and of 128 of scales: the first as the recipe has them, the others as they were."""
+    x = spread(13, 200, torch.Generator().manual_seed(4))
+    m = aw.awsrc_fp8_matrix(13, 200)
+    m.codes.view(torch.uint8).fill_(0x55)
+    m.exps.fill_(0x77)
+    aw.awsrc_fp8_quantize(x.cuda(), out=m)
+    codes, exps = ref.place(*ref.quantize(x.double()))
+    assert torch.equal(m.codes.cpu()[:, :13].double(), codes[:, :13])
+    assert (m.codes.view(torch.uint8)[:, 13:] == 0x55).all()
+    rows = m.exps.cpu().permute(1, 3, 2, 0, 4).reshape(128, -1)
+    assert torch.equal(rows[:13], exps.permute(1, 3, 2, 0, 4).reshape(128, -1)[:13]) and (rows[13:] == 0x77).all()
+
+
+@pytest.mark.parametrize("m", [1, 5, 40, 70, 300])
+@pytest.mark.parametrize("dtype,blocks", [(F32, 16), (BF16, 256)])
+def test_sums_leave_the_tensor_cores_as_often_as_stated(aw, m, dtype, blocks):  # noqa: F811
+    """A one in the first 2048 columns (bf16: 32768), small products in the second, a one taken off in the third. The
+    stretches' sums are 1, 2^-23 and -1, exact, and so are their additions in binary32: the result is 2^-23 to the bit. In one
+    sum without a stop the small products, 2^-29 of the one (2^-33) per 32 columns, would be cut off beside it. Rows enough
+    that columns are not shared; another power of two for each row."""
+    n, k = 9800, 3 * blocks * 128
+    x, w = (torch.zeros(r, k, dtype=BF16, device="cuda") for r in (m, n))
+    low = slice(blocks * 128, 2 * blocks * 128)
+    x[:, 0], w[:, 0] = 1.0, 1.0
+    x[:, low] = 2.0 ** -17
+    w[:, low] = 2.0 ** -23 / (blocks * 128) * 2.0 ** 17
+    x[:, 2 * blocks * 128], w[:, 2 * blocks * 128] = 1.0, -1.0
+    xs, wsc = (torch.exp2((torch.arange(r, device="cuda") * 7 % 9 - 4).float()) for r in (m, n))
+    x8, w8 = aw.awsrc_fp8_quantize(x * xs[:, None].to(BF16)), aw.awsrc_fp8_quantize(w * wsc[:, None].to(BF16))
+    ws = aw.awsrc_step_workspace()
+    y = aw.awsrc_fp8_gemm(x8, w8, ws, out_dtype=dtype)
+    assert torch.equal(y.float(), 2.0 ** -23 * xs[:, None] * wsc)
+    assert aw.awsrc_workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("m,n", [(1, 300), (5, 1000), (16, 10000), (40, 700), (64, 10000), (100, 300), (300, 1111)])
+def test_long_sums_of_positive_terms(aw, m, n):  # noqa: F811
+    """Where cutting off adds up. A stretch of 2048 columns is 64 steps of 32 columns, each cut off by less than a unit of
+    binary32, 2^-23 of the running sum S_i at most; factors between 1/2 and 1 keep S_i within 3% of i / 64 of the whole, so
+    sum_i 2^-23 S_i <= 33.5 2^-23 of it. The 14 stretches of 27648 columns (at most 8 shares of columns begin one more each) join with
+    22 roundings of 2^-24 at most: 4.0e-6 + 1.4e-6, every element. Without stops 864 steps are off by 1.2e-5 (measured)."""
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    x, w = (0.5 + 0.5 * torch.rand(r, 27648, generator=gen, device="cuda") for r in (m, n))
+    x8, w8, ws = aw.awsrc_fp8_matrix(m, 27648), aw.awsrc_fp8_quantize(w), aw.awsrc_step_workspace()
+    y = aw.awsrc_fp8_linear(x, w8, x8, ws)
+    want = x8.values().double() @ w8.values().double().T
+    off = ((y.double() - want) / want).abs().max()
+    assert off <= 33.5 * 2.0 ** -23 + 22 * 2.0 ** -24, float(off)
+    # bf16: one sum of 864 steps, 432.5 2^-23 at most, and a rounding of half a step
+    y = aw.awsrc_fp8_gemm(x8, w8, ws, out_dtype=BF16)
+    off = ((y.double() - want) / want).abs().max()
+    assert off <= 2.0 ** -8 + 445 * 2.0 ** -23, float(off)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m,k,n", [(100, 70000, 300), (300, 40000, 600), (65, 98400, 129)])
+def test_whole_numbers_over_many_columns_by_pairs(aw, dtype, m, k, n):  # noqa: F811
+    """Several stretches of 32768 columns in the pairs' kernel: sums of whole numbers below 2^24, exact."""
+    gen = torch.Generator().manual_seed(k)
+    (x, xs), (w, wss) = int_matrix(m, k, gen), int_matrix(n, k, gen)
+    want = (x.double().cuda() @ w.double().cuda().T) * xs.double().cuda() * wss.double().cuda().T
+    assert k * 9 < 2 ** 24
+    ws = aw.awsrc_step_workspace()
+    y = aw.awsrc_fp8_gemm(aw.awsrc_fp8_quantize((x * xs).cuda()), aw.awsrc_fp8_quantize((w * wss).cuda()), ws, out_dtype=dtype)
+    assert torch.equal(y, want.to(dtype)) and aw.awsrc_workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 1024), (7, 10000, 1024), (16, 300, 2048), (40, 300, 1024), (64, 10000, 640), (16, 200, 30000),
+                                   (100, 300, 1024)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("stall", [0, 3])
+def test_waits_that_run_out_in_every_kernel(aw, m, n, k, dtype, stall):  # noqa: F811
+    """Copies stop after `stall` blocks, in awsrc_fp8_linear (rows quantised in the kernel, or in one before it) and
+    awsrc_fp8_gemm: the waits of 2 ms run out, the call ends and reports it, the next one is right."""
+    gen = torch.Generator().manual_seed(m + k)
+    x = torch.randn(m, k, generator=gen).to(dtype).cuda()
+    w8, ws, x8 = aw.awsrc_fp8_quantize(torch.randn(n, k, generator=gen).cuda()), aw.awsrc_step_workspace(), aw.awsrc_fp8_matrix(m, k)
+    want = aw.awsrc_fp8_linear(x, w8, x8, ws)
+    calls = (lambda: aw.awsrc_fp8_linear(x, w8, x8, ws), lambda: aw.awsrc_fp8_gemm(x8, w8, ws, out_dtype=dtype))
+    for call in calls:
+        aw.awsrc_set_wait_test(2_000_000, stall)
+        try:
+            call()
+            torch.cuda.synchronize()
+        finally:
+            aw.awsrc_set_wait_test()
+        assert aw.awsrc_workspace_status(ws) == 4
+        assert torch.equal(call(), want) and aw.awsrc_workspace_status(ws) == 0
