@@ -1,5 +1,7 @@
 """GPU parity of the serving-step calls in forms beside the usual ones: other streams,
 launch forms of large vocabularies, thresholds of tiny random numbers, long sums."""
+import random
+
 import pytest
 import torch
 
@@ -195,3 +197,57 @@ def test_a_captured_round_with_a_pool_that_runs_out(aw):
         mine = [want[1][b][want[0][b]] if starts[b + 1] > starts[b] else mine[b] for b in range(users)]
         assert last.tolist() == mine and min(mine) >= 0
     assert waited and resumed  # some had to wait, and went on
+
+
+@pytest.mark.parametrize("p_dtype,q_dtype", [(F32, BF16), (BF16, F32), (F32, F32), (BF16, BF16), (F32, None)])
+@pytest.mark.parametrize("vocab,n_seq", [(131071, 2), (131072, 1), (151936, 1), (151937, 19), (2 ** 18 - 1, 3), (2 ** 18, 1)])
+def test_verify_large_vocabularies(aw, p_dtype, q_dtype, vocab, n_seq):
+    """1024 threads (131072 columns and up to 19 sequences) and what is beside them, up to the largest vocabulary; a model's and a
+    draft model's probabilities of the same type and of two; thresholds in every part of a row."""
+    from test_gpu_step import check
+    gen = torch.Generator().manual_seed(vocab + n_seq)
+    n = 2 * n_seq if n_seq < 4 else n_seq + 1  # one draft each, or one for the last sequence alone
+    starts = list(range(0, n + 1, 2)) if n_seq < 4 else list(range(n_seq)) + [n]
+    x = torch.randn(n, vocab, generator=gen)
+    p = torch.softmax(x, -1).to(p_dtype)
+    q = None if q_dtype is None else torch.softmax(x + torch.randn(n, vocab, generator=gen), -1).to(q_dtype)
+    ids = torch.randint(vocab, (n,), generator=gen).tolist()
+    ids[-1] = vocab - 1
+    r = (torch.arange(n_seq) + torch.rand(n_seq, generator=gen)) / n_seq
+    want = check(aw, starts, ids, p, q, torch.rand(n, generator=gen), r, 1, [100] * n_seq, pad=vocab % 4)
+    assert all(-1 not in t[:a + 1] for a, t in zip(*want[:2]))
+
+
+@pytest.mark.parametrize("p_dtype,q_dtype", [(F32, BF16), (BF16, F32)])
+@pytest.mark.parametrize("vocab,pad", [(1, 0), (31, 1), (1000, 0), (1000, 4), (1001, 3), (4099, 0)])
+def test_verify_probabilities_of_two_types(aw, p_dtype, q_dtype, vocab, pad):
+    """Rows that start on each type's vector boundary, on one of them, and on neither."""
+    from test_gpu_step import check, rows_of
+    rng, gen = random.Random(vocab + pad), torch.Generator().manual_seed(vocab + pad)
+    lens = [1, 4, 0, 7, 2, 3]
+    starts = [sum(lens[:b]) for b in range(len(lens) + 1)]
+    n = starts[-1]
+    p, q = rows_of(rng, gen, n, vocab, "wide", torch.float64)
+    p, q = p.to(p_dtype), q.to(q_dtype)
+    ids = [rng.randrange(vocab) for _ in range(n)]
+    for t in range(n - 1):
+        if rng.random() < 0.6:
+            ids[t + 1] = int(p[t].argmax())
+    check(aw, starts, ids, p, q, torch.rand(n, generator=gen), torch.rand(len(lens), generator=gen), 6,
+          [rng.randrange(20, 900) for _ in lens], pad=pad)
+
+
+@pytest.mark.parametrize("n_seq", [1, 20, 700])
+def test_verify_the_largest_sums(aw, n_seq):
+    """Every entry of the largest vocabulary 1 (or above): running sums up to 2^63 units. The token is floor(r 2^18)."""
+    vocab = 2 ** 18
+    p = torch.ones(n_seq, vocab, device="cuda", dtype=BF16)
+    p[:, ::3] = 7.0
+    r = torch.rand(n_seq, generator=torch.Generator().manual_seed(n_seq))
+    r[0] = 1 - 2.0 ** -24
+    ws = aw.awsrc_step_workspace()
+    starts = torch.arange(n_seq + 1, dtype=I32).cuda()
+    ids = torch.zeros(n_seq, dtype=I32, device="cuda")
+    acc, tok = aw.awsrc_verify_drafts(starts, ids, p, None, torch.zeros(n_seq, device="cuda"), r.cuda(), ws, max_draft=0)
+    assert tok[:, 0].tolist() == (r.double() * vocab).floor().int().tolist() and not acc.any()
+    assert aw.awsrc_workspace_status(ws) == 0
