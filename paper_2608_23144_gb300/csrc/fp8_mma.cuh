@@ -26,7 +26,7 @@ using namespace tc05;
 constexpr int BM = kTileRows;
 // Blocks summed in tensor memory before the sums leave it: the cores cut a running sum off
 // (below 2^-24 of it, measured) at each of a block's four products. Positive terms are off by
-// 3e-7 after 2048 columns and 1.2e-5 after 27648; bf16 results take 2^-9 of their own.
+// 3e-7 after 2048 columns and 1.2e-5 after 27648; bf16 results are rounded by up to 2^-8 of their own.
 constexpr int kChunkF32 = 16, kChunkBf16 = 256;
 
 struct Ctx {

@@ -35,17 +35,13 @@ __device__ __forceinline__ int64_t warp_incl(int64_t v) {
   }
   return v;
 }
-// Of the first kGroup threads' sums; every thread of the block calls it.
-template <int kGroup>
+template <int kThreads>
 __device__ Sum3 block_excl(Sum3 v, Sum3* total, Sum3* warps) {
-  constexpr int kWarps = kGroup / 32;
+  constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  Sum3 i{0, 0, 0};
   __syncthreads();  // warps[] of the sum before is read
-  if (warp < kWarps) {
-    i = Sum3{warp_incl(v.a), warp_incl(v.b), warp_incl(v.c)};
-    if (lane == 31) warps[warp] = i;
-  }
+  const Sum3 i{warp_incl(v.a), warp_incl(v.b), warp_incl(v.c)};
+  if (lane == 31) warps[warp] = i;
   __syncthreads();
   if (warp == 0) {
     const Sum3 w = lane < kWarps ? warps[lane] : Sum3{0, 0, 0};
@@ -56,7 +52,7 @@ __device__ Sum3 block_excl(Sum3 v, Sum3* total, Sum3* warps) {
   }
   __syncthreads();
   *total = warps[32];
-  const Sum3 before = warps[warp < kWarps ? warp : 0];
+  const Sum3 before = warps[warp];
   return Sum3{before.a + i.a - v.a, before.b + i.b - v.b, before.c + i.c - v.c};
 }
 
@@ -118,7 +114,6 @@ __device__ __forceinline__ int want_of(int held, int keep, int add, int log_page
   return held < 0 ? 0 : pages_of((int64_t)keep + add, log_page);  // -1: an entry that cannot be right
 }
 
-// kGroup threads make the sums (a shuffle passes one warp per cycle, so 32 warps' took 4 us).
 // Page of the table's places [held, ..) that is handed out p-th.
 struct Handed {
   const PlanArgs& a;
@@ -132,7 +127,7 @@ struct Handed {
   }
 };
 
-template <int kThreads, int kGroup>
+template <int kThreads>
 __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ PlanArgs a) {
   extern __shared__ int sm[];
   __shared__ Sum3 warps[33];
@@ -162,8 +157,8 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
     last = said == gridDim.x - 1;
     if (last) *a.arrived = 0;
   }
-  const int per = (n + kGroup - 1) / kGroup;
-  const int b0 = tid < kGroup ? min(n, tid * per) : n, b1 = min(n, b0 + per);
+  const int per = (n + kThreads - 1) / kThreads;
+  const int b0 = min(n, tid * per), b1 = min(n, b0 + per);
   Sum3 v{0, 0, 0}, total;
   for (int b = b0; b < b1; ++b) {
     const int held = max(0, s_held[b]), want = want_of(s_held[b], s_keep[b], s_tok[b], a.log_page);
@@ -171,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
     v.b += s_tok[b];
     v.c += max(0, held - want);
   }
-  Sum3 before = block_excl<kGroup>(v, &total, warps);
+  Sum3 before = block_excl<kThreads>(v, &total, warps);
   const int64_t room = count + total.c;
   bool short_ = false;
   if (total.a > room || total.b > a.n_tok) {  // not all find room: who does
@@ -190,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
       got.b += s_tok[b];
       got.c += max(0, held - want);
     }
-    before = block_excl<kGroup>(got, &total, warps);
+    before = block_excl<kThreads>(got, &total, warps);
   }
   const bool wrong = count < 0 || count > a.n_pages || count + total.c > a.n_pages;
   for (int b = b0; b < b1; ++b) {
@@ -266,17 +261,17 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(const __grid_constant__ 
   }
 }
 
-template <int kThreads, int kGroup>
+template <int kThreads>
 cudaError_t launch(const PlanArgs& a, cudaStream_t st) {
   const size_t smem = (size_t)5 * (a.n_seq + 1) * sizeof(int);
   if (smem > 46 * 1024) {
-    const cudaError_t e = allow_smem<Threads<kThreads>>(plan_kernel<kThreads, kGroup>, 5 * (kPlanMaxSeq + 1) * (int)sizeof(int));
+    const cudaError_t e = allow_smem<Threads<kThreads>>(plan_kernel<kThreads>, 5 * (kPlanMaxSeq + 1) * (int)sizeof(int));
     if (e != cudaSuccess) return e;
   }
   // a thread block for every four tokens of its threads, as many as SMs; each sums over all sequences
   const int64_t want = ((int64_t)a.n_tok + 4 * kThreads - 1) / (4 * kThreads);
   const int grid = (int)(want < 1 ? 1 : want > 152 ? 152 : want);
-  return launch_step(plan_kernel<kThreads, kGroup>, dim3(grid), kThreads, smem, 1, st, a);
+  return launch_step(plan_kernel<kThreads>, dim3(grid), kThreads, smem, 1, st, a);
 }
 
 }  // namespace
@@ -285,8 +280,9 @@ cudaError_t launch_plan(const PlanArgs& in, cudaStream_t st) {
   PlanArgs a = in;
   a.vec = ((reinterpret_cast<uintptr_t>(a.tok_seq) | reinterpret_cast<uintptr_t>(a.tok_pos) |
             reinterpret_cast<uintptr_t>(a.tok_slot)) & 15) == 0;
-  // 8 sequences or more a thread in the sums are what a larger block is for
-  const cudaError_t e = a.n_seq <= 2048 ? launch<256, 256>(a, st) : launch<1024, 1024>(a, st);
+  // 8 sequences or more a thread in the sums are what a larger block is for; below, 8 warps: a
+  // shuffle passes one warp per cycle, and 32 warps' sums took 4 us
+  const cudaError_t e = a.n_seq <= 2048 ? launch<256>(a, st) : launch<1024>(a, st);
   if (e != cudaSuccess) return e;
   note_launches(1);
   return cudaGetLastError();

@@ -251,3 +251,20 @@ def test_verify_the_largest_sums(aw, n_seq):
     acc, tok = aw.awsrc_verify_drafts(starts, ids, p, None, torch.zeros(n_seq, device="cuda"), r.cuda(), ws, max_draft=0)
     assert tok[:, 0].tolist() == (r.double() * vocab).floor().int().tolist() and not acc.any()
     assert aw.awsrc_workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("n_seq", [2048, 2049, 8192])
+def test_plan_of_the_most_sequences(aw, n_seq):
+    """Around the change to larger thread blocks, and as many sequences as there may be: decoding with pages for all, drafts
+    that go back, prompts that do not all fit."""
+    from test_gpu_step import Pool
+    rng = random.Random(n_seq)
+    lengths = [rng.choice([0, 1, 15, 16, 17, rng.randrange(90)]) for _ in range(n_seq)]
+    pool = Pool(aw, rng, n_seq, 16, 14, lengths, spare=n_seq // 2)
+    flags = [pool.step(None, [1] * n_seq, n_seq)]
+    keep = [max(0, k - rng.randrange(4)) for k in pool.length]
+    flags.append(pool.step(keep, [rng.randrange(5) for _ in keep], 5 * n_seq))
+    keep = [0 if rng.random() < 0.1 else k for k in pool.length]
+    flags.append(pool.step(keep, [rng.randrange(90) if k == 0 else 1 for k in keep], 3 * n_seq))
+    assert flags[0] in (0, 16) and 16 in flags
+    assert pool.step([0] * n_seq, [0] * n_seq, 3) == 0
