@@ -766,7 +766,10 @@ awsrc_status awsrc_fp8_quantize(const void* x, int32_t dtype, int64_t stride, co
  * columns there (BF16: 32768) and joined by rounded additions. A block that holds
  * NaN makes the sums it takes part in NaN.
  * awsrc_fp8_linear — awsrc_fp8_quantize of x to x8 and awsrc_fp8_gemm with it in
- * one call, the same results bit for bit: y = x w^T. x8 is not w.
+ * one call, the same results bit for bit: y = x w^T. x8 shares no bytes with w.
+ * Two launches but for few rows, of which the second reads w before the first
+ * has ended: work that writes w is queued on the stream before the call or after
+ * it, not by another host thread during it.
  * y that shares elements with x is refused, as is one whose rows are another step
  * apart and whose extent meets that of x.
  * Errors: INVALID_ARG, SHAPE (x.cols != w.cols), UNSUPPORTED (more tiles than 32

@@ -374,7 +374,8 @@ def awsrc_fp8_linear(x: torch.Tensor, w: Fp8Matrix, x8: Fp8Matrix, workspace: to
                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """x w^T for activations x (2-D, float32 or bfloat16, any row stride), which
     are held in 8 bits in x8 (a matrix of x's shape) on the way; the result has
-    x's dtype unless `out` says otherwise. `out` shares no elements with x."""
+    x's dtype unless `out` says otherwise. `out` shares no elements with x. While a
+    call is made, no other host thread queues work on its stream that writes w."""
     xp, xt, xs = _matrix(x, "x")
     dev = x.device
     _fp8(x8, "x8", dev)
