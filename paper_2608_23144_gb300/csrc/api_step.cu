@@ -51,6 +51,19 @@ bool share(const Rows& x, const Rows& y, int64_t rows) {
   return d < x.row || step - d < y.row;
 }
 
+size_t codes_bytes(const Fp8Mat& m) { return (size_t)m.blocks() * m.rows8() * 128; }
+size_t exps_bytes(const Fp8Mat& m) { return (size_t)((m.blocks() + 3) / 4) * m.tiles() * 512; }
+
+// Whether two matrices held in 8 bits share a byte, of codes or of exponents.
+bool share(const Fp8Mat& x, const Fp8Mat& w) {
+  const auto meet = [](const uint8_t* a, size_t n, const uint8_t* b, size_t m) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return n && m && (p <= q ? q - p < n : p - q < m);
+  };
+  return meet(x.codes, codes_bytes(x), w.codes, codes_bytes(w)) || meet(x.exps, exps_bytes(x), w.exps, exps_bytes(w)) ||
+         meet(x.codes, codes_bytes(x), w.exps, exps_bytes(w)) || meet(x.exps, exps_bytes(x), w.codes, codes_bytes(w));
+}
+
 awsrc_status gemm_args(const awsrc_fp8_matrix* x, const awsrc_fp8_matrix* w, void* y, int32_t y_dtype, int64_t y_stride,
                        void* workspace, size_t workspace_bytes, GemmArgs* out) {
   GemmArgs a{};
@@ -141,14 +154,14 @@ awsrc_status awsrc_verify_drafts(int32_t n_seq, int32_t n_rows, int32_t vocab, i
   return e == cudaSuccess ? AWSRC_OK : cuda_fail(e, "verify_drafts");
 }
 
-awsrc_status awsrc_fp8_matrix_bytes(int32_t rows, int32_t cols, size_t* codes_bytes, size_t* exps_bytes) {
-  if (!codes_bytes || !exps_bytes) return AWSRC_ERR_INVALID_ARG;
+awsrc_status awsrc_fp8_matrix_bytes(int32_t rows, int32_t cols, size_t* codes, size_t* exps) {
+  if (!codes || !exps) return AWSRC_ERR_INVALID_ARG;
   const awsrc_fp8_matrix m{rows, cols, nullptr, nullptr};
   Fp8Mat f;
   const awsrc_status s = check_matrix(&m, false, &f);
   if (s != AWSRC_OK) return s;
-  *codes_bytes = (size_t)f.blocks() * f.rows8() * 128;
-  *exps_bytes = (size_t)((f.blocks() + 3) / 4) * f.tiles() * 512;
+  *codes = codes_bytes(f);
+  *exps = exps_bytes(f);
   return AWSRC_OK;
 }
 
@@ -177,7 +190,7 @@ awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, 
   GemmArgs a;
   awsrc_status s = gemm_args(x8, w, y, y_dtype, y_stride, workspace, workspace_bytes, &a);
   if (s != AWSRC_OK || (s = check_rows(x, x_dtype)) != AWSRC_OK) return s;
-  if (x8->codes == w->codes || x8->exps == w->exps) return AWSRC_ERR_INVALID_ARG;
+  if (x8->codes == w->codes || x8->exps == w->exps || share(a.x, a.w)) return AWSRC_ERR_INVALID_ARG;
   if (a.x.rows == 0) return AWSRC_OK;
   if (a.w.rows == 0) return awsrc_fp8_quantize(x, x_dtype, x_stride, x8, stream);  // x8 is written all the same
   // few rows of x are read while others' results are written
