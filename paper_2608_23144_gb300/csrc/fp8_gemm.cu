@@ -14,8 +14,10 @@
 //     their 16-byte pieces exchanged by row), so a block's rows are one bulk copy, and a
 //     ring of stages keeps the memory busy.
 //   Up to 16 rows of x lie in shared memory before the products start, their codes copied
-//     or, by warps 0-7, made here: a kernel for that in front took 2.5 to 4 us until the
-//     products could start. Longer x, and 17 to 64 rows, come with w, block by block (made
+//     or, by warps 0-7, made here. Made here where one round of loads takes all of a thread
+//     block's (row, block) pairs, 32: one row x 2048 x 11008 took 6.1 us and with a kernel
+//     for that in front 7.4, but every thread block makes all rows' codes, and 16 rows took
+//     16.9 and 7.8. Longer x, and 17 to 64 rows, come with w, block by block (made
 //     here block by block, 40 rows took 29 us where both kernels took 17: each stage waited
 //     for a copy, the codes and a fence).
 //   Warp 10 puts the scales of the tile's rows of w in the order of its lanes. Warp 9
@@ -44,6 +46,7 @@ using namespace fp8;
 
 constexpr int kThreads = 352, kXWarps = 8, kCopyWarp = 8, kMmaWarp = 9, kScaleWarp = 10;
 constexpr int kMaxSplit = kFewSplit;
+constexpr int kPairsAhead = 32;  // (row, block) pairs of x whose loads are in flight when the kernel quantises x
 
 // Where x comes from: its codes with the blocks of w; all codes first; all rows first, quantised here.
 enum Source { kCodes, kCodesFirst, kF32First, kBf16First };
@@ -220,10 +223,11 @@ __device__ void scale_role(const GemmArgs& a, Smem<N, X>& sm, const Ctx& x) {
 __device__ __forceinline__ void get4(const float* p, int have, bool vec, float* v) { vec ? load4<true>(p, have, v) : load4<false>(p, have, v); }
 __device__ __forceinline__ void get4(const __nv_bfloat16* p, int have, bool vec, float* v) { vec ? load4<true>(p, have, v) : load4<false>(p, have, v); }
 
-// All of this block's columns of all rows of x: (row, block) pairs over the warps, four in flight.
+// All of this block's columns of all rows of x: (row, block) pairs over the warps, four in flight
+// in each.
 template <int N, Source X, typename T>
 __device__ void quantize_role(const GemmArgs& a, Smem<N, X>& sm) {
-  constexpr int kAhead = 4;
+  constexpr int kAhead = kPairsAhead / kXWarps;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, M = a.x.rows, blocks = a.w.blocks();
   const uint32_t xb = x_block(a);
   const Walk w(a);
@@ -466,10 +470,12 @@ cudaError_t launch(const GemmArgs& a, cudaStream_t st) {
 
 constexpr int kFewRows = 64, kFirstRows = 16;  // of x
 
+// Blocks of columns that a thread block has at most.
+int share_of(const GemmArgs& a) { return ((a.w.blocks() + 1) / 2 + a.split - 1) / a.split * 2; }
+
 // Whether all codes of x of a thread block's columns fit beside the stages.
 bool x_first(const GemmArgs& a) {
-  const int blocks = ((a.w.blocks() + 1) / 2 + a.split - 1) / a.split * 2;
-  return a.x.rows <= kFirstRows && blocks * a.x.rows8() * 128 <= Cfg<16, kCodesFirst>::kXBytes;
+  return a.x.rows <= kFirstRows && share_of(a) * a.x.rows8() * 128 <= Cfg<16, kCodesFirst>::kXBytes;
 }
 
 }  // namespace
@@ -479,7 +485,7 @@ cudaError_t fp8_gemm_quantizes(const GemmArgs& in, bool* itself) {
   *itself = false;
   if (a.x.rows > kFirstRows) return cudaSuccess;
   const cudaError_t e = choose(&a);
-  if (e == cudaSuccess) *itself = x_first(a);
+  if (e == cudaSuccess) *itself = x_first(a) && a.x.rows * share_of(a) <= kPairsAhead;
   return e;
 }
 
