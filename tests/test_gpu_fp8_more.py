@@ -126,3 +126,44 @@ def test_few_rows_are_quantised_where_one_round_of_loads_takes_them(aw, dtype): 
         torch.cuda.synchronize()
         assert all(torch.equal(y, want[i % 2]) for i, y in enumerate(ys))
         assert torch.equal(x8.codes.view(torch.uint8), want8.codes.view(torch.uint8)) and torch.equal(x8.exps, want8.exps)
+
+
+@pytest.mark.parametrize("m", [4, 100])
+def test_products_of_decoded_weights(aw, m):  # noqa: F811
+    """W_hat out of the records' decoder, held in 8 bits for the rows that the packed product does not take. A code is within half
+    a step, 2^-4 of a normal value or 2^-10 2^e of a subnormal one, of what it stands for, on both sides of the product:
+    dx = 2^-4 |x| + 2^(ex - 10), dw likewise, so |y - x W_hat^T| <= |x| dw + dx |w| + dx dw, and sums off by 4.0e-6 + 22 2^-24 of
+    |x| |w| at most (as for positive terms). The packed product of the same records is within its own stated bound."""
+    from synth import make_module
+    rows, cols, gen = 512, 2048, torch.Generator().manual_seed(m)
+    mod = make_module(rows, cols, seed=9, device="cuda")
+    prm = aw.params(C=64, P=4, b=4, S=256)
+    back = aw.awsrc_rtn_quantize(mod["W"], w0_dtype=F32)
+    mod = dict(mod, W=mod["W"].float(), W0=back["W0"])
+    cands = aw.awsrc_encode_tiles(prm, [mod])
+    stream, counts, _ = aw.awsrc_select_records(prm, [mod], cands, [0.162])
+    k = int(counts.sum())
+    assert k > 100
+    w = aw.awsrc_decode_apply(prm, [mod], stream, k, out_dtype=F32)[0]
+    x = torch.randn(m, cols, generator=gen).cuda()
+    w8, x8, ws = aw.awsrc_fp8_quantize(w), aw.awsrc_fp8_matrix(m, cols), aw.awsrc_step_workspace()
+    y = aw.awsrc_fp8_linear(x, w8, x8, ws).double()
+
+    def half(t):
+        amax = t.double().abs().view(t.shape[0], -1, 128).amax(2)
+        e = torch.ceil(torch.log2(amax / 448)).clamp(min=-64)
+        return 2.0 ** -4 * t.double().abs() + torch.exp2(e - 10).repeat_interleave(128, 1)
+
+    absx, absw, dx, dw = x.double().abs(), w.double().abs(), half(x), half(w)
+    want = x.double() @ w.double().T
+    bound = absx @ dw.T + dx @ absw.T + dx @ dw.T + (33.5 * 2.0 ** -23 + 22 * 2.0 ** -24) * ((absx + dx) @ (absw + dw).T)
+    assert ((y - want).abs() <= bound).all()
+    # in the mean square 2^-4 / sqrt(3) a side at most, 0.051 together; half as much again
+    assert (y - want).norm() <= 0.077 * want.norm()
+    if m <= 8:
+        side = aw.awsrc_sidecar_prepare(prm, [(rows, cols)], stream, k)
+        packed = aw.awsrc_packed_gemv(prm, [(rows, cols)], 0, back, x, sidecar=side).double()
+        w0 = back["W0"].double()
+        own = (cols / 32 + 32) * 2.0 ** -24 * (absx @ (w0.abs() + (w.double() - w0).abs()).T) + 2.0 ** -24 * (absx @ absw.T)
+        assert ((packed - want).abs() <= own).all()
+        assert ((y - packed).abs() <= bound + own).all()
