@@ -197,7 +197,7 @@ awsrc_status awsrc_fp8_linear(const void* x, int32_t x_dtype, int64_t x_stride, 
   const int64_t xs = size_of(x_dtype), ys = size_of(y_dtype);
   if (share(Rows{x, x_stride * xs, a.x.cols * xs}, Rows{y, y_stride * ys, a.w.rows * ys}, a.x.rows)) return AWSRC_ERR_INVALID_ARG;
   bool itself;
-  cudaError_t e = fp8_gemm_quantizes(a, &itself);
+  cudaError_t e = fp8_gemm_quantizes(a, x_dtype == AWSRC_DTYPE_BF16, &itself);
   if (e == cudaSuccess && itself) {
     a.raw = x;
     a.raw_stride = x_stride;

@@ -14,10 +14,10 @@
 //     their 16-byte pieces exchanged by row), so a block's rows are one bulk copy, and a
 //     ring of stages keeps the memory busy.
 //   Up to 16 rows of x lie in shared memory before the products start, their codes copied
-//     or, by warps 0-7, made here. Made here where one round of loads takes all of a thread
-//     block's (row, block) pairs, 32: one row x 2048 x 11008 took 6.1 us and with a kernel
-//     for that in front 7.4, but every thread block makes all rows' codes, and 16 rows took
-//     16.9 and 7.8. Longer x, and 17 to 64 rows, come with w, block by block (made
+//     or, by warps 0-7, made here. Every thread block makes all rows' codes of its columns:
+//     x 2048 x 11008 float32 took 6.9 us for one row, 8.4 for three, 17.6 for 16; with a
+//     kernel for that in front 9.1, 9.5 and 9.6 (bf16 7.3, 9.7, 21.6 and 9.6 each; weights
+//     from memory). Longer x, and 17 to 64 rows, come with w, block by block (made
 //     here block by block, 40 rows took 29 us where both kernels took 17: each stage waited
 //     for a copy, the codes and a fence).
 //   Warp 10 puts the scales of the tile's rows of w in the order of its lanes. Warp 9
@@ -46,7 +46,9 @@ using namespace fp8;
 
 constexpr int kThreads = 352, kXWarps = 8, kCopyWarp = 8, kMmaWarp = 9, kScaleWarp = 10;
 constexpr int kMaxSplit = kFewSplit;
-constexpr int kPairsAhead = 32;  // (row, block) pairs of x whose loads are in flight when the kernel quantises x
+// (row, block) pairs of x that a thread block quantises in the product's kernel at most; each takes
+// 45 ns (bf16 60), a kernel for that in front and its end 2 to 2.5 us
+constexpr int kOwnF32 = 56, kOwnBf16 = 32;
 
 // Where x comes from: its codes with the blocks of w; all codes first; all rows first, quantised here.
 enum Source { kCodes, kCodesFirst, kF32First, kBf16First };
@@ -224,10 +226,10 @@ __device__ __forceinline__ void get4(const float* p, int have, bool vec, float* 
 __device__ __forceinline__ void get4(const __nv_bfloat16* p, int have, bool vec, float* v) { vec ? load4<true>(p, have, v) : load4<false>(p, have, v); }
 
 // All of this block's columns of all rows of x: (row, block) pairs over the warps, four in flight
-// in each.
+// in each warp.
 template <int N, Source X, typename T>
 __device__ void quantize_role(const GemmArgs& a, Smem<N, X>& sm) {
-  constexpr int kAhead = kPairsAhead / kXWarps;
+  constexpr int kAhead = 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, M = a.x.rows, blocks = a.w.blocks();
   const uint32_t xb = x_block(a);
   const Walk w(a);
@@ -480,12 +482,12 @@ bool x_first(const GemmArgs& a) {
 
 }  // namespace
 
-cudaError_t fp8_gemm_quantizes(const GemmArgs& in, bool* itself) {
+cudaError_t fp8_gemm_quantizes(const GemmArgs& in, bool bf16, bool* itself) {
   GemmArgs a = in;
   *itself = false;
   if (a.x.rows > kFirstRows) return cudaSuccess;
   const cudaError_t e = choose(&a);
-  if (e == cudaSuccess) *itself = x_first(a) && a.x.rows * share_of(a) <= kPairsAhead;
+  if (e == cudaSuccess) *itself = x_first(a) && a.x.rows * share_of(a) <= (bf16 ? kOwnBf16 : kOwnF32);
   return e;
 }
 

@@ -112,8 +112,8 @@ struct GemmArgs {
   int vec_y;         // four elements of y lie on a boundary of their size
   int vec_raw;       // so do four of every row of x
 };
-// Whether the product quantises these rows of x itself (fp8_gemm.cu).
-cudaError_t fp8_gemm_quantizes(const GemmArgs& a, bool* itself);
+// Whether the product quantises these rows of x, float32 or bf16, itself (fp8_gemm.cu).
+cudaError_t fp8_gemm_quantizes(const GemmArgs& a, bool bf16, bool* itself);
 cudaError_t launch_fp8_pairs(const GemmArgs& a, cudaStream_t st);
 cudaError_t launch_fp8_gemm(const GemmArgs& a, cudaStream_t st);
 
