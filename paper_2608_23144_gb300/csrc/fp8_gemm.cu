@@ -26,10 +26,11 @@
 // Few rows of w: a cluster shares a tile's columns and joins its parts, in their order,
 // through shared memory.
 //
-// Measured with the quantising of x, among calls of their kind: one row x 2048 x 11008
-// float32 5.9 us (floor 3.4, w's bytes at the copy rate), 40 x 3584 x 18944 bf16 17.0 us
-// (floor 10.4). Left are what lies before the first product (2.3 us; with a kernel in
-// front 3.8, while the first stages of w arrive) and the results' way out (1 us).
+// Measured with the quantising of x, in a captured run with weights from memory: one row x
+// 2048 x 11008 float32 7.4 us (floor 3.4, w's bytes at the copy rate; out of the L2 5.9), 40
+// x 3584 x 18944 bf16 17.4 us (floor 10.4). Left are what lies before the first product (2.3
+// us; with a kernel in front 3.8, while the first stages of w arrive) and the results' way
+// out (1 us).
 //
 // Every wait is bounded (wait_ns): one that runs out sets bit 2 of the fault word,
 // stops the block's roles, waits (bounded) for its copies and products in flight

@@ -17,10 +17,11 @@
 // Few tiles: a cluster of pairs shares a tile's columns and joins its parts.
 //
 // Measured: 8192 x 3584 x 18944 to bf16 318 to 336 us from one machine to the next, 3.3
-// to 3.5 PFLOP/s or 85 to 90% of twice a large bf16 product's rate; the tensor pipe is
+// to 3.5 PFLOP/s or 85 to 90% of twice a large bf16 product's rate, to float32 375 (sums
+// leave tensor memory every 2048 columns, results are twice the bytes); the tensor pipe is
 // busy 71% of the cycles (2048 rows). Bound: the gap at a tile's end, where one
 // accumulator of 256 columns has to be read (5%), commits, and under sustained load the
-// power limit (2.8 PFLOP/s). 333 x 5000 x 1777 float32 11 us: 2.5 until the first
+// power limit (2.8 PFLOP/s). 333 x 5000 x 1777 float32 11.6 us: 2.5 until the first
 // product, 4 of products, 4 for parts that partners read at 25 GB/s.
 //
 // Every wait is bounded as in fp8_gemm.cu; no thread block of a cluster leaves before

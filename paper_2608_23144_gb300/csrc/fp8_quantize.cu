@@ -4,8 +4,10 @@
 // One pass: a warp holds 4 blocks of a row in registers, finds each block's
 // largest magnitude over the warp and writes the codes; its 4 exponents are one
 // word of the scale layout. Floor: the rows read, the codes written, once.
-// Measured: 11008 x 2048 float32 17.3 us, 6.5 TB/s or 97% of the measured copy; 1023 x
-// 3584 bf16 3.0 us (floor 1.6), the latency of one round of loads.
+// Measured, rows from memory: 11008 x 2048 float32 17.4 us, 6.5 TB/s or 96% of the measured
+// copy (an odd stride, loads of one element, 19.0); 1023 x 3584 bf16 4.6 us (floor 1.6; out
+// of the L2 3.0), the latency of one round of loads; 8192 x 3584 bf16 22 to 28 (floor 13):
+// a warp has half the bytes in flight there that it has in float32.
 #include "fp8_codes.cuh"
 #include "internal.h"
 #include "step.cuh"

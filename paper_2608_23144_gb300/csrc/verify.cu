@@ -6,11 +6,17 @@
 // not, the token has the weights max(0, p - q); after the last, p. It is the
 // smallest j with C_j > r C_V, C the running sum. Sums are of whole numbers
 // (probabilities in units of 2^-45, rounded to nearest), so that they are exact in
-// any order and the token does not depend on how the row is cut up.
+// any order and the token does not depend on how the row is cut up. Given up for that:
+// p and q are rounded before they are subtracted, by 2^-46 of probability an entry at
+// most (4e-9 over a row of 2^18), and entries below are never drawn. Units of 2^-62 cost
+// 64-bit shifts, 43 us where these take 17.
 //
 // Floor: one row of p and one of q per sequence (only the row that decides is
 // read) at the copy rate; a small call is a chain of four loads (rows, ids,
 // probabilities, the row) and the two passes below.
+//
+// At most 2^18 columns: the running sums have 63 bits, the table of the warps' steps
+// (s_step) one entry per 512 columns.
 //
 // A cluster per sequence: its thread blocks sum equal slices of the row, each
 // warp a run of it in steps of 512, exchange the slices' sums, and the warp in whose
@@ -18,9 +24,11 @@
 // two binary32 additions whose sums' bits count them (Units); 64-bit shifts of the
 // significands took four times the instructions (43 us in place of 24).
 //
-// Measured: 64 sequences of up to 5 drafts over 151936 float32 probabilities 16.8 us
+// Measured: 64 sequences of up to 5 drafts over 151936 float32 probabilities 17.0 us
 // (floor 8.6: 2 us of chain, 9 of rows on SMs with three or four blocks each, 5 of
-// exchange, search and end); one of 32000 4.8 us; 24 of 50257 in bf16 5.9 us.
+// exchange, search and end), 15.5 where a model's are bf16; one of 151936 8.7 us, of 32000
+// 4.8; 24 of 50257 in bf16 6.0 us. 64 of 50257 float32 9.8 us, and 11.5 where rows lie off
+// 16 bytes, so that all loads are of one element.
 #include "internal.h"
 #include "step.cuh"
 
