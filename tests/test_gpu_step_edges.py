@@ -179,3 +179,36 @@ def test_the_most_columns(aw, m):  # noqa: F811
     y = aw.awsrc_fp8_gemm(aw.awsrc_fp8_quantize(x), aw.awsrc_fp8_quantize(w), ws)
     assert torch.equal(y, want) and aw.awsrc_workspace_status(ws) == 0
     torch.cuda.empty_cache()
+
+
+def test_verify_the_most_sequences(aw):  # noqa: F811
+    """65535 sequences of one row each: the token is the first whose running sum of units is above r of them all."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    n, vocab = 65535, 37
+    p = torch.rand(n, vocab, generator=gen, device="cuda") / 64
+    k = torch.randint(256, (n,), generator=gen, device="cuda")  # r = k / 256
+    sums = torch.round(p.double() * 2.0 ** 45).long().cumsum(1)  # float32 below 2^-6 in units of 2^-45: exact but for their last bits
+    want = (sums * 256 <= k[:, None] * sums[:, -1:]).sum(1)
+    ws = aw.awsrc_step_workspace()
+    starts, ids = torch.arange(n + 1, dtype=I32, device="cuda"), torch.zeros(n, dtype=I32, device="cuda")
+    acc, tok = aw.awsrc_verify_drafts(starts, ids, p, None, torch.zeros(n, device="cuda"), k.float() / 256, ws, max_draft=0)
+    assert torch.equal(tok[:, 0].long(), want) and not acc.any() and aw.awsrc_workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("stop", [0, 1, 31, 1024, 2999, 3000])
+def test_verify_thousands_of_drafts(aw, stop):  # noqa: F811
+    """3000 drafts of one sequence beside one of none: accepted up to the first whose random number refuses it."""
+    gen = torch.Generator().manual_seed(stop)
+    drafts, vocab = 3000, 20
+    p = torch.softmax(torch.randn(drafts + 2, vocab, generator=gen) * 2, -1)
+    ids = torch.randint(vocab, (drafts + 2,), generator=gen)
+    u = torch.zeros(drafts + 2)
+    u[stop:] = 1.0
+    ws = aw.awsrc_step_workspace()
+    acc, tok = aw.awsrc_verify_drafts(cuda_ints([0, drafts + 1, drafts + 2]), ids.to(I32).cuda(), p.cuda(), None, u.cuda(),
+                                      torch.tensor([0.4, 0.6]).cuda(), ws, max_draft=drafts + 5)
+    assert acc.tolist() == [stop, 0] and tok.shape == (2, drafts + 6)
+    assert tok[0, :stop].tolist() == ids[1:stop + 1].tolist() and (tok[0, stop + 1:] == -1).all() and (tok[1, 1:] == -1).all()
+    rows = ref.verify([0, 1], [0], p[stop:stop + 1].double().tolist(), None, [0.0], [0.4], 0, [9])[1][0][0] if stop == drafts else None
+    assert 0 <= tok[0, stop] < vocab and (tok[0, stop] == rows if rows is not None else tok[0, stop] != ids[stop + 1])
+    assert aw.awsrc_workspace_status(ws) == 0
