@@ -104,7 +104,8 @@ class KvBatch:
     sequence b are the last of its kv_len[b] tokens, token p of it in page
     page_table[b, p // page]. int32 device tensors, read by the kernels when
     they run; max_new and max_kv (the most new tokens and kv_len they may hold)
-    choose launch shapes."""
+    choose launch shapes. n_tok rows may be more than the sequences have: those
+    behind the last are left as they are."""
 
     def __init__(self, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, n_tok: int, max_new: int,
                  max_kv: int):
